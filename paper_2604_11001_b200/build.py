@@ -13,8 +13,10 @@ LIB = os.path.join(HERE, "libfcsim.so")
 HOST_SOURCE = os.path.join(CSRC, "fcsim.cu")
 KERNEL_SOURCE = os.path.join(CSRC, "fcsim_step_kernels.cu")   # compiled once per policy
 N_KERNEL_POLICIES = 7
-SOURCES = [HOST_SOURCE, KERNEL_SOURCE]
-HEADERS = [os.path.join(CSRC, "fcsim_device.cuh"), os.path.join(ROOT, "include", "fcsim.h")]
+KV_SOURCES = [os.path.join(CSRC, "fcsim_kv.cu")]               # the paged key-value cache
+SOURCES = [HOST_SOURCE, KERNEL_SOURCE] + KV_SOURCES
+HEADERS = [os.path.join(CSRC, "fcsim_device.cuh"), os.path.join(ROOT, "include", "fcsim.h"),
+           os.path.join(CSRC, "fcsim_kv_device.cuh"), os.path.join(ROOT, "include", "fcsim_kv.h")]
 OBJ_DIR = os.path.join(HERE, "_build")
 
 
@@ -54,6 +56,8 @@ def _compile(lib: str, verbose: bool, extra) -> str:
     jobs = [(HOST_SOURCE, [], os.path.join(OBJ_DIR, f"{tag}_host.o"))]
     for pol in range(N_KERNEL_POLICIES):
         jobs.append((KERNEL_SOURCE, [f"-DFCSIM_KERNEL_POLICY={pol}"], os.path.join(OBJ_DIR, f"{tag}_policy{pol}.o")))
+    for src in KV_SOURCES:
+        jobs.append((src, [], os.path.join(OBJ_DIR, f"{tag}_{os.path.splitext(os.path.basename(src))[0]}.o")))
 
     def one(job):
         src, defs, obj = job

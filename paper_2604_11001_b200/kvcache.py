@@ -1,0 +1,296 @@
+"""ctypes binding of the paged key-value cache (include/fcsim_kv.h): append, attend, evict.
+
+Argument checks and marshalling only -- the work is done by the CUDA library, on the current stream of the cache's
+device.  PyTorch provides device memory and streams; there is no CPU fallback.
+
+    cache = PagedKV.allocate(n_pages=1024, page_size=16, n_kv_heads=8, head_dim=128, weight=True)
+    q = cache.append(q, k, v, positions, slots, rope=table, q_norm=w_q, k_norm=w_k)   # a slot's new tokens
+    out = cache.attend(q, table, lengths, add_weight=True)                            # one query per request
+    new_lengths, kept = cache.evict(table, lengths, budget, new_table, max_budget=512, recent=64, first=4)
+    cache.check()                                                                     # synchronises
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import torch
+
+from . import binding as _fb
+
+F16, BF16, E4M3 = 0, 1, 2
+BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET = 1, 2, 4, 8
+_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+
+
+class fcsim_kv_cache(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "weight", "k_scale", "v_scale")]
+                + [(n, C.c_int64) for n in ("stride_page", "stride_slot", "stride_head")]
+                + [(n, C.c_int32) for n in ("dtype", "n_pages", "page_size", "n_kv_heads", "head_dim", "reserved")])
+
+
+class fcsim_kv_append_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "q_norm", "k_norm", "rope", "positions", "slots",
+                                           "status")]
+                + [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")]
+                + [(n, C.c_int32) for n in ("n_tokens", "n_heads", "dtype", "rope_dim", "n_positions",
+                                            "interleaved")]
+                + [("eps", C.c_float), ("reserved", C.c_int32)])
+
+
+class fcsim_kv_attend_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "lse", "table", "lengths", "status")]
+                + [(n, C.c_int64) for n in ("q_row", "q_head", "table_row")]
+                + [(n, C.c_int32) for n in ("n_requests", "n_heads", "dtype", "table_cols", "max_length", "window",
+                                            "add_weight")]
+                + [("scale", C.c_float)])
+
+
+class fcsim_kv_evict_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("table", "lengths", "budget", "new_table", "new_lengths", "kept",
+                                           "status")]
+                + [(n, C.c_int64) for n in ("table_row", "new_row")]
+                + [(n, C.c_int32) for n in ("n_requests", "table_cols", "new_cols", "max_length", "max_budget",
+                                            "recent", "first", "reserved")])
+
+
+class fcsim_kv_workspace(C.Structure):
+    _fields_ = [("bytes", C.c_size_t), ("zeroed", C.c_size_t)]
+
+
+EXPORTS = ("fcsim_kv_append", "fcsim_kv_attend_workspace", "fcsim_kv_attend", "fcsim_kv_evict_workspace",
+           "fcsim_kv_evict", "fcsim_kv_last_cuda_error")
+
+_lib = None
+
+
+def load():
+    """The CUDA library with the signatures of this module's entry points."""
+    global _lib
+    if _lib is None:
+        lib = _fb.load()
+        vp, cache = C.c_void_p, C.POINTER(fcsim_kv_cache)
+        lib.fcsim_kv_append.argtypes = [cache, C.POINTER(fcsim_kv_append_args), vp]
+        for name, args in (("attend", fcsim_kv_attend_args), ("evict", fcsim_kv_evict_args)):
+            getattr(lib, f"fcsim_kv_{name}_workspace").argtypes = [cache, C.POINTER(args),
+                                                                   C.POINTER(fcsim_kv_workspace)]
+            getattr(lib, f"fcsim_kv_{name}").argtypes = [cache, C.POINTER(args), vp, C.c_size_t, vp]
+        lib.fcsim_kv_last_cuda_error.argtypes = []
+        for name in EXPORTS:
+            getattr(lib, name).restype = C.c_int
+        _lib = lib
+    return _lib
+
+
+def _raise(code, where):
+    e = _fb.FcsimError(code, where)
+    if code == -5:
+        e.args = (f"{e.args[0]} [cudaError {load().fcsim_kv_last_cuda_error()}]",)
+    raise e
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+class PagedKV:
+    """One layer's cache: ``k`` and ``v`` as [n_pages, page_size, n_kv_heads, head_dim] views of either memory order
+    (head_dim contiguous), and what belongs to them.
+
+    ``weight``: [n_pages, n_kv_heads, page_size] float32, the attention each cached token has received.
+    ``k_scale``, ``v_scale``: [n_kv_heads] float32 for 8-bit caches: a stored x stands for x * scale.
+
+    Calls run on the current stream; calls on different streams that touch the same pages are the caller's to order.
+    The object is not thread-safe."""
+
+    def __init__(self, k, v, weight=None, k_scale=None, v_scale=None):
+        _need(k.dim() == 4 and k.dtype in _TYPES and k.is_cuda, "k: a CUDA tensor [n_pages, page_size, n_kv_heads, "
+              "head_dim] of float16, bfloat16 or float8_e4m3fn")
+        _need(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device and v.stride() == k.stride(),
+              "v: shape, strides, type and device of k")
+        n_pages, page_size, n_kv, head_dim = k.shape
+        _need(k.stride(3) == 1 or head_dim == 1, "k, v: head_dim has to be contiguous")
+        if weight is not None:
+            _need(tuple(weight.shape) == (n_pages, n_kv, page_size) and weight.dtype == torch.float32
+                  and weight.is_contiguous() and weight.device == k.device,
+                  "weight: contiguous float32 [n_pages, n_kv_heads, page_size] on k's device")
+        wide = k.dtype != torch.float8_e4m3fn
+        for s in (k_scale, v_scale):
+            _need(s is None if wide else (s is not None and tuple(s.shape) == (n_kv,) and s.dtype == torch.float32
+                                          and s.is_contiguous() and s.device == k.device),
+                  "k_scale, v_scale: None for 16-bit caches, contiguous float32 [n_kv_heads] for 8-bit ones")
+        self.k, self.v, self.weight, self.k_scale, self.v_scale = k, v, weight, k_scale, v_scale
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_pages, page_size, n_kv, head_dim
+        self.device = k.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._workspaces = {}   # stream -> zero-initialised workspace, so that streams never share one
+        self._c = fcsim_kv_cache(k.data_ptr(), v.data_ptr(), _pointer(weight), _pointer(k_scale), _pointer(v_scale),
+                                 k.stride(0), k.stride(1), k.stride(2), _TYPES[k.dtype], n_pages, page_size, n_kv,
+                                 head_dim, 0)
+        self._c_ref = C.byref(self._c)
+        load()
+
+    @classmethod
+    def allocate(cls, n_pages, page_size, n_kv_heads, head_dim, dtype=torch.bfloat16, *, heads_first=False,
+                 weight=False, k_scale=None, v_scale=None, device="cuda:0"):
+        """A zeroed cache.  ``heads_first``: pages laid out [n_kv_heads, page_size, head_dim] in memory."""
+        def pool():
+            if heads_first:
+                return torch.zeros(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device).transpose(1, 2)
+            return torch.zeros(n_pages, page_size, n_kv_heads, head_dim, dtype=dtype, device=device)
+        w = torch.zeros(n_pages, n_kv_heads, page_size, device=device) if weight else None
+        if dtype == torch.float8_e4m3fn:
+            one = torch.ones(n_kv_heads, device=device)
+            k_scale = one if k_scale is None else k_scale
+            v_scale = one.clone() if v_scale is None else v_scale
+        return cls(pool(), pool(), w, k_scale, v_scale)
+
+    # ------------------------------------------------------------------------------------------ helpers
+    def _same_device(self, *tensors):
+        for t in tensors:
+            if t is not None and t.device != self.device:
+                raise ValueError(f"tensors have to be on the cache's device {self.device}, got {t.device}")
+
+    def _heads(self, x, name, n, heads, dtype):
+        _need(x.dim() == 3 and x.shape[0] == n and (heads is None or x.shape[1] == heads)
+              and x.shape[2] == self.head_dim and x.dtype == dtype and x.stride(2) == 1,
+              f"{name}: [tokens, heads, head_dim] of one 16-bit type, head_dim contiguous")
+
+    def _table(self, table, name, n):
+        _need(table.dim() == 2 and table.shape[0] == n and table.dtype == torch.int32
+              and (table.shape[1] <= 1 or table.stride(1) == 1), f"{name}: int32 [requests, pages], rows contiguous")
+
+    def _ints(self, x, name, n, dtype=torch.int32):
+        _need(x.dim() == 1 and x.shape[0] == n and x.dtype == dtype and (n <= 1 or x.stride(0) == 1),
+              f"{name}: contiguous {dtype} [{n}]")
+
+    def _call(self, name, args, workspace):
+        lib = _lib
+        if torch.cuda.current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self._call(name, args, workspace)
+        stream = torch.cuda.current_stream().cuda_stream
+        ref = C.byref(args)
+        if not workspace:
+            code = getattr(lib, name)(self._c_ref, ref, stream)
+        else:
+            need = fcsim_kv_workspace()
+            code = getattr(lib, name + "_workspace")(self._c_ref, ref, C.byref(need))
+            if code == 0:
+                buf = self._workspace(stream, need.bytes) if need.bytes else None
+                code = getattr(lib, name)(self._c_ref, ref, _pointer(buf), need.bytes, stream)
+        if code != 0:
+            _raise(code, name)
+
+    def _workspace(self, stream, size):
+        """Zeroed when new; every call leaves the part that has to be zero as it found it.  A graph under capture
+        gets its own, whose zeroing is part of the graph."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.zeros(size, dtype=torch.uint8, device=self.device)
+        buf = self._workspaces.get(stream)
+        if buf is None or buf.numel() < size:
+            buf = self._workspaces[stream] = torch.zeros(size, dtype=torch.uint8, device=self.device)
+        return buf
+
+    # ------------------------------------------------------------------------------------------ operators
+    def append(self, q, k, v, positions, slots, *, rope=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6):
+        """Normalise and rotate the heads of ``q`` [n, heads, head_dim] and ``k`` [n, n_kv_heads, head_dim], store k
+        and ``v`` at ``slots`` (int64 [n], page * page_size + place, negative = not stored) and return q.
+
+        ``rope``: float32 [positions, rope_dim], cosines then sines; ``positions``: int32 [n].  ``q_norm``,
+        ``k_norm``: [head_dim] weights of the norms over each head.  ``q`` may be None (nothing is returned)."""
+        n = k.shape[0]
+        dtype = k.dtype
+        self._heads(k, "k", n, self.n_kv_heads, dtype)
+        self._heads(v, "v", n, self.n_kv_heads, dtype)
+        self._ints(slots, "slots", n, torch.int64)
+        _need(dtype in _TYPES and dtype != torch.float8_e4m3fn, "k: float16 or bfloat16")
+        out, heads, q_row, q_head = None, 0, 0, 0
+        if q is not None:
+            self._heads(q, "q", n, None, dtype)
+            heads = q.shape[1]
+            q_row, q_head = q.stride(0), q.stride(1)
+            out = torch.empty((n, heads, self.head_dim), dtype=dtype, device=self.device)
+        rope_dim = n_positions = 0
+        if rope is not None:
+            _need(rope.dim() == 2 and rope.dtype == torch.float32 and rope.is_contiguous(),
+                  "rope: contiguous float32 [positions, rope_dim]")
+            self._ints(positions, "positions", n)
+            n_positions, rope_dim = rope.shape
+        for w in (q_norm, k_norm):
+            _need(w is None or (tuple(w.shape) == (self.head_dim,) and w.dtype == dtype and w.stride(0) == 1),
+                  "q_norm, k_norm: [head_dim] of q's type")
+        self._same_device(q, k, v, slots, rope, positions if rope is not None else None, q_norm, k_norm)
+        args = fcsim_kv_append_args(
+            _pointer(q), k.data_ptr(), v.data_ptr(), _pointer(out), _pointer(q_norm), _pointer(k_norm), _pointer(rope),
+            _pointer(positions) if rope is not None else None, slots.data_ptr(), self.status.data_ptr(),
+            q_row, q_head, k.stride(0), k.stride(1), v.stride(0), v.stride(1), n, heads, _TYPES[dtype], rope_dim,
+            n_positions, 1 if interleaved else 0, eps, 0)
+        self._call("fcsim_kv_append", args, False)
+        return out
+
+    def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, add_weight=False,
+               return_lse=False):
+        """Attention of one token per request: ``q`` [requests, heads, head_dim] over the ``lengths`` (int32) tokens
+        that the rows of ``table`` (int32 [requests, pages]) hold; returns [requests, heads, head_dim], with
+        ``return_lse`` also the float32 [requests, heads] log-sum-exp.
+
+        ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
+        only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
+        _need(q.dim() == 3, "q: [requests, heads, head_dim]")
+        n, heads = q.shape[0], q.shape[1]
+        self._heads(q, "q", n, None, q.dtype)
+        _need(q.dtype == torch.float16 or q.dtype == torch.bfloat16, "q: float16 or bfloat16")
+        self._table(table, "table", n)
+        self._ints(lengths, "lengths", n)
+        self._same_device(q, table, lengths)
+        if max_length is None:
+            max_length = table.shape[1] * self.page_size
+        out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device) if return_lse else None
+        args = fcsim_kv_attend_args(
+            q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self.status.data_ptr(),
+            q.stride(0), q.stride(1), table.stride(0), n, heads, _TYPES[q.dtype], table.shape[1], max_length, window,
+            1 if add_weight else 0, 1.0 / math.sqrt(self.head_dim) if scale is None else scale)
+        self._call("fcsim_kv_attend", args, True)
+        return (out, lse) if return_lse else out
+
+    def evict(self, table, lengths, budget, new_table, *, max_budget=None, recent=0, first=0, max_length=None):
+        """Cut every request to its ``budget`` (int32 [requests]) of tokens per kv head: the ``recent`` newest, the
+        ``first`` oldest and the largest weights, copied in order to the pages of ``new_table`` (none of which the
+        call may read).  Returns the new lengths (int32 [requests]) and the old index of every kept token (int32
+        [requests, n_kv_heads, max_budget], -1 beyond)."""
+        n = lengths.shape[0]
+        self._table(table, "table", n)
+        self._table(new_table, "new_table", n)
+        self._ints(lengths, "lengths", n)
+        self._ints(budget, "budget", n)
+        self._same_device(table, lengths, budget, new_table)
+        if max_length is None:
+            max_length = table.shape[1] * self.page_size
+        if max_budget is None:
+            max_budget = new_table.shape[1] * self.page_size
+        new_lengths = torch.empty(n, dtype=torch.int32, device=self.device)
+        kept = torch.empty((n, self.n_kv_heads, max_budget), dtype=torch.int32, device=self.device)
+        args = fcsim_kv_evict_args(
+            table.data_ptr(), lengths.data_ptr(), budget.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(),
+            kept.data_ptr(), self.status.data_ptr(), table.stride(0), new_table.stride(0), n, table.shape[1],
+            new_table.shape[1], max_length, max_budget, recent, first, 0)
+        self._call("fcsim_kv_evict", args, True)
+        return new_lengths, kept
+
+    def check(self):
+        """Read and clear the device status; raise when a call met a bad page, length, position or budget."""
+        bits = int(self.status.item())
+        if bits:
+            self.status.zero_()
+            names = [s for b, s in ((BAD_PAGE, "page or slot outside the pool"),
+                                    (BAD_LENGTH, "length outside 0 .. max_length"),
+                                    (BAD_POSITION, "position outside the rope table"),
+                                    (BAD_BUDGET, "budget outside 0 .. max_budget")) if bits & b]
+            raise ValueError("; ".join(names))
