@@ -13,10 +13,13 @@ LIB = os.path.join(HERE, "libfcsim.so")
 HOST_SOURCE = os.path.join(CSRC, "fcsim.cu")
 KERNEL_SOURCE = os.path.join(CSRC, "fcsim_step_kernels.cu")   # compiled once per policy
 N_KERNEL_POLICIES = 7
-KV_SOURCES = [os.path.join(CSRC, "fcsim_kv.cu")]               # the paged key-value cache
-SOURCES = [HOST_SOURCE, KERNEL_SOURCE] + KV_SOURCES
+KV_SOURCE = os.path.join(CSRC, "fcsim_kv.cu")                  # the paged key-value cache
+KV_ATTEND_SOURCE = os.path.join(CSRC, "fcsim_kv_attend.cu")    # its attention, compiled once per pair of types
+N_KV_TYPES = 4
+SOURCES = [HOST_SOURCE, KERNEL_SOURCE, KV_SOURCE, KV_ATTEND_SOURCE]
 HEADERS = [os.path.join(CSRC, "fcsim_device.cuh"), os.path.join(ROOT, "include", "fcsim.h"),
-           os.path.join(CSRC, "fcsim_kv_device.cuh"), os.path.join(ROOT, "include", "fcsim_kv.h")]
+           os.path.join(CSRC, "fcsim_kv_device.cuh"), os.path.join(CSRC, "fcsim_kv_attend.cuh"),
+           os.path.join(ROOT, "include", "fcsim_kv.h")]
 OBJ_DIR = os.path.join(HERE, "_build")
 
 
@@ -56,8 +59,9 @@ def _compile(lib: str, verbose: bool, extra) -> str:
     jobs = [(HOST_SOURCE, [], os.path.join(OBJ_DIR, f"{tag}_host.o"))]
     for pol in range(N_KERNEL_POLICIES):
         jobs.append((KERNEL_SOURCE, [f"-DFCSIM_KERNEL_POLICY={pol}"], os.path.join(OBJ_DIR, f"{tag}_policy{pol}.o")))
-    for src in KV_SOURCES:
-        jobs.append((src, [], os.path.join(OBJ_DIR, f"{tag}_{os.path.splitext(os.path.basename(src))[0]}.o")))
+    jobs.append((KV_SOURCE, [], os.path.join(OBJ_DIR, f"{tag}_kv.o")))
+    for types in range(N_KV_TYPES):
+        jobs.append((KV_ATTEND_SOURCE, [f"-DFCSIM_KV_TYPES={types}"], os.path.join(OBJ_DIR, f"{tag}_kv_attend{types}.o")))
 
     def one(job):
         src, defs, obj = job

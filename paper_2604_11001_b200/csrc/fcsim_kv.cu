@@ -4,7 +4,10 @@
 
 #include <math.h>
 
-#include "fcsim_kv_device.cuh"
+#include <algorithm>
+#include <atomic>
+
+#include "fcsim_kv_attend.cuh"
 
 using namespace fcsim_kv_dev;
 
@@ -146,17 +149,13 @@ int launch_append(const AppendParams& p, cudaStream_t stream) {
     return launched();
 }
 
-// ------------------------------------------------------------------------------------------------ attend
-struct AttendParams {
+// ------------------------------------------------------------------------------------------------ evict
+struct EvictParams {
     Pool pool;
-    const char* q;
-    char* out;
-    float *lse, *ws;
-    const int32_t *table, *lengths;
-    int32_t* status;
-    int64_t q_row, q_head, table_row;
-    int n_requests, n_heads, max_length, window, add_weight;
-    float scale;
+    const int32_t *table, *lengths, *budget, *new_table;
+    int32_t *new_lengths, *kept, *status;
+    int64_t table_row, new_row;
+    int max_length, max_budget, recent, first, bytes;
 };
 
 __device__ __forceinline__ int length_of(const int32_t* lengths, int r, int max_length, int32_t* status) {
@@ -167,93 +166,6 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int r, int max_
     }
     return n;
 }
-
-// One query head by one CTA of four warps; a warp takes every fourth token.
-template <class T, class C>
-__global__ void __launch_bounds__(128) fcsim_kv_attend_kernel(const AttendParams p) {
-    const int r = blockIdx.y, head = blockIdx.x, D = p.pool.head_dim;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int kv = head / (p.n_heads / p.pool.n_kv);
-    const bool mine = lane * 8 < D;
-    const int n = length_of(p.lengths, r, p.max_length, p.status);
-    const int start = p.window > 0 && n > p.window ? n - p.window : 0;
-    float q[8] = {0, 0, 0, 0, 0, 0, 0, 0}, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (mine) load8<T>(p.q + ((int64_t)r * p.q_row + (int64_t)head * p.q_head + lane * 8) * 2, q);
-    const float scale = p.scale * (C::bytes == 1 ? p.pool.k_scale[kv] : 1.0f);
-    float m = -INFINITY, l = 0;
-    for (int t = start + warp; t < n; t += 4) {
-        const int page = p.table[r * p.table_row + t / p.pool.page_size];
-        if (page < 0 || page >= p.pool.n_pages) {
-            flag(p.status, FCSIM_KV_BAD_PAGE);
-            continue;
-        }
-        const int64_t at = (page * p.pool.stride_page + (t % p.pool.page_size) * p.pool.stride_slot +
-                            kv * p.pool.stride_head + lane * 8) * C::bytes;
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, s = 0;
-        if (mine) load8<C>(p.pool.k + at, x);
-#pragma unroll
-        for (int i = 0; i < 8; i++) s += q[i] * x[i];
-#pragma unroll
-        for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(~0u, s, k);
-        s *= scale;
-        if (p.add_weight && lane == 0) p.ws[((int64_t)r * p.n_heads + head) * p.max_length + t] = s;
-        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.0f : top;
-        const float shrink = expf(m - base), e = expf(s - base);
-        if (mine) load8<C>(p.pool.v + at, x);
-#pragma unroll
-        for (int i = 0; i < 8; i++) o[i] = o[i] * shrink + e * x[i];
-        l = l * shrink + e;
-        m = top;
-    }
-    __shared__ float sm[4], sl[4], so[4][256];
-    if (lane == 0) sm[warp] = m, sl[warp] = l;
-    if (mine)
-        for (int i = 0; i < 8; i++) so[warp][lane * 8 + i] = o[i];
-    __syncthreads();
-    const float top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), base = top == -INFINITY ? 0.0f : top;
-    float f[4], total = 0;
-    for (int w = 0; w < 4; w++) f[w] = expf(sm[w] - base), total += f[w] * sl[w];
-    const float lse = total == 0.0f ? -INFINITY : base + logf(total);
-    if (threadIdx.x == 0) {
-        if (p.lse) p.lse[(int64_t)r * p.n_heads + head] = lse;
-        if (p.add_weight) p.ws[(int64_t)p.n_requests * p.n_heads * p.max_length + (int64_t)r * p.n_heads + head] = lse;
-    }
-    const float v = C::bytes == 1 ? p.pool.v_scale[kv] : 1.0f;
-    if (threadIdx.x * 2 < D) {
-        float y[2];
-        for (int i = 0; i < 2; i++) {
-            float s = 0;
-            for (int w = 0; w < 4; w++) s += f[w] * so[w][threadIdx.x * 2 + i];
-            y[i] = total == 0.0f ? 0.0f : s / total * v;
-        }
-        reinterpret_cast<uint32_t*>(p.out)[(((int64_t)r * p.n_heads + head) * D) / 2 + threadIdx.x] = T::pack(y[0], y[1]);
-    }
-}
-
-__global__ void __launch_bounds__(256) fcsim_kv_weight_kernel(const AttendParams p) {
-    const int r = blockIdx.z, kv = blockIdx.y, group = p.n_heads / p.pool.n_kv;
-    const int n = length_of(p.lengths, r, p.max_length, nullptr);
-    const int start = p.window > 0 && n > p.window ? n - p.window : 0;
-    const int t = start + blockIdx.x * 256 + threadIdx.x;
-    if (t >= n) return;
-    const int page = p.table[r * p.table_row + t / p.pool.page_size];
-    if (page < 0 || page >= p.pool.n_pages) return;
-    float sum = 0;
-    for (int g = 0; g < group; g++) {
-        const int64_t row = (int64_t)r * p.n_heads + kv * group + g;
-        sum += expf(p.ws[row * p.max_length + t] - p.ws[(int64_t)p.n_requests * p.n_heads * p.max_length + row]);
-    }
-    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t % p.pool.page_size] += sum;
-}
-
-// ------------------------------------------------------------------------------------------------ evict
-struct EvictParams {
-    Pool pool;
-    const int32_t *table, *lengths, *budget, *new_table;
-    int32_t *new_lengths, *kept, *status;
-    int64_t table_row, new_row;
-    int max_length, max_budget, recent, first, bytes;
-};
 
 // A weight as an unsigned key of the same order: NaN lowest, -0 as 0.
 __device__ __forceinline__ uint32_t order_key(float w) {
@@ -385,9 +297,62 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     return FCSIM_OK;
 }
 
-fcsim_kv_workspace attend_workspace(const AttendParams& p) {
-    const size_t floats = p.add_weight ? (size_t)p.n_requests * p.n_heads * ((size_t)p.max_length + 1) : 0;
-    return {floats * 4, 0};
+AttendVariant attend_variant(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a) {
+    const int group = a->n_heads / c->n_kv_heads;
+    if (c->dtype == FCSIM_KV_E4M3)
+        return a->dtype == FCSIM_KV_F16 ? attend_variant_f16_e4m3(c->head_dim, group) : attend_variant_bf16_e4m3(c->head_dim, group);
+    return a->dtype == FCSIM_KV_F16 ? attend_variant_f16(c->head_dim, group) : attend_variant_bf16(c->head_dim, group);
+}
+
+// SMs of the current device (asked once per device).
+int sm_count(int* out) {
+    static std::atomic<int> known[64];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return cuda_status(e);
+    int n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return cuda_status(e);
+        if (device < 64) known[device].store(n, std::memory_order_relaxed);
+    }
+    *out = n;
+    return FCSIM_OK;
+}
+
+// Where things lie in attend's workspace, and its grid.  The counters come first.
+struct AttendLayout {
+    size_t counters, parts, stats, logits, bytes;
+    int64_t logit_tiles;
+    int grid, weight_grid;
+};
+
+// requests that share no page hold at most the pool's tokens, and each at most one tile that is not full
+int64_t logit_tiles(const AttendParams& p) {
+    if (!p.add_weight) return 0;
+    const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
+    return std::min((seen + kTile - 1) / kTile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / kTile + p.n_requests);
+}
+// The part of the workspace that does not depend on the device.
+size_t attend_kept(const AttendParams& p) {
+    return (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0) + (size_t)logit_tiles(p) * kTile * p.n_heads * 4;
+}
+
+int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l) {
+    int sms = 0, per_sm = 0, rc = sm_count(&sms);
+    if (rc != FCSIM_OK) return rc;
+    if ((rc = v.ctas_per_sm(&per_sm)) != 0) return cuda_status((cudaError_t)rc);
+    const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
+    const int64_t tiles = (seen + kTile - 1) / kTile, group = p.n_heads / p.pool.n_kv;
+    const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
+    l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most, p.n_requests)}));
+    l->counters = (size_t)l->grid * 4;
+    l->parts = (l->counters + 15) / 16 * 16;
+    l->stats = l->parts + (size_t)2 * l->grid * v.head_cols * (v.width + 2) * 4;
+    l->logit_tiles = logit_tiles(p);
+    l->logits = l->stats + (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0);
+    l->bytes = l->stats + attend_kept(p);
+    l->weight_grid = (int)std::max<int64_t>(1, std::min<int64_t>(sms * 8, l->logit_tiles));
+    return FCSIM_OK;
 }
 
 int check_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args* a, EvictParams* p) {
@@ -448,7 +413,11 @@ extern "C" int fcsim_kv_attend_workspace(const fcsim_kv_cache* c, const fcsim_kv
     int rc = check_attend(c, a, &p);
     if (rc != FCSIM_OK) return rc;
     if (!out) return FCSIM_EINVAL;
-    *out = attend_workspace(p);
+    *out = {0, 0};
+    if (p.n_requests == 0) return FCSIM_OK;
+    AttendLayout l;
+    if ((rc = attend_layout(p, attend_variant(c, a), &l)) != FCSIM_OK) return rc;
+    *out = {l.bytes, l.counters};
     return FCSIM_OK;
 }
 
@@ -458,20 +427,18 @@ extern "C" int fcsim_kv_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_ar
     int rc = check_attend(c, a, &p);
     if (rc != FCSIM_OK) return rc;
     if (p.n_requests == 0) return FCSIM_OK;
-    const fcsim_kv_workspace need = attend_workspace(p);
-    if (need.bytes && (!workspace || workspace_bytes < need.bytes || !aligned16(workspace))) return FCSIM_ESIZE;
-    p.ws = (float*)workspace;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < attend_kept(p)) return FCSIM_ESIZE;
+    const AttendVariant v = attend_variant(c, a);
+    AttendLayout l;
+    if ((rc = attend_layout(p, v, &l)) != FCSIM_OK) return rc;
+    if (workspace_bytes < l.bytes) return FCSIM_ESIZE;
+    char* ws = (char*)workspace;
+    p.counters = (int*)ws, p.parts = (float*)(ws + l.parts), p.stats = (float*)(ws + l.stats), p.logits = (float*)(ws + l.logits);
+    p.logit_tiles = l.logit_tiles;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const dim3 grid(p.n_heads, p.n_requests);
-    if (c->dtype == FCSIM_KV_E4M3) {
-        if (a->dtype == FCSIM_KV_F16) fcsim_kv_attend_kernel<F16, E4M3><<<grid, 128, 0, stream>>>(p);
-        else fcsim_kv_attend_kernel<BF16, E4M3><<<grid, 128, 0, stream>>>(p);
-    } else if (a->dtype == FCSIM_KV_F16) fcsim_kv_attend_kernel<F16, F16><<<grid, 128, 0, stream>>>(p);
-    else fcsim_kv_attend_kernel<BF16, BF16><<<grid, 128, 0, stream>>>(p);
-    if ((rc = launched()) != FCSIM_OK || !p.add_weight || p.max_length == 0) return rc;
-    const int seen = p.window > 0 && p.window < p.max_length ? p.window : p.max_length;
-    fcsim_kv_weight_kernel<<<dim3((seen + 255) / 256, p.pool.n_kv, p.n_requests), 256, 0, stream>>>(p);
-    return launched();
+    if ((rc = v.launch(p, l.grid, stream)) != 0) return cuda_status((cudaError_t)rc);
+    if (p.add_weight && (rc = launch_weights(p, l.weight_grid, stream)) != 0) return cuda_status((cudaError_t)rc);
+    return FCSIM_OK;
 }
 
 extern "C" int fcsim_kv_evict_workspace(const fcsim_kv_cache* c, const fcsim_kv_evict_args* a, fcsim_kv_workspace* out) {

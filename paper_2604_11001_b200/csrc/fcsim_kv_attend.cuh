@@ -1,0 +1,43 @@
+// Attention of one query token per request over a paged cache: parameters, and what the host side needs to launch it.
+#pragma once
+#include "fcsim_kv_device.cuh"
+
+namespace fcsim_kv_dev {
+
+constexpr int kTile = 64;        // tokens a CTA takes at once: 16 by each of its four warps
+constexpr int kThreads = 128;
+constexpr int kMaxCtas = 4096;   // bound of the grid (the work is divided among the CTAs at run time)
+
+struct AttendParams {
+    Pool pool;
+    const char* q;
+    char* out;
+    float* lse;
+    const int32_t *table, *lengths;
+    int32_t* status;
+    int64_t q_row, q_head, table_row;
+    int n_requests, n_heads, max_length, window, add_weight;
+    float scale;
+    // workspace
+    int* counters;       // [grid], zero between calls
+    float* parts;        // [2 * grid][heads of a tile][head_dim + 2]
+    float* stats;        // add_weight: [n_requests][n_heads][4]: largest logit, its unit, 1 / sum, -
+    float* logits;       // add_weight: per request [n_heads][tiles * kTile]
+    int64_t logit_tiles; // what `logits` has room for, in tiles
+};
+
+// A variant of the kernel.  The functions return a cudaError_t.
+struct AttendVariant {
+    int (*launch)(const AttendParams&, int grid, cudaStream_t);
+    int (*ctas_per_sm)(int* out);  // also raises the kernel's limit of shared memory
+    int head_cols, width;          // query heads and elements of its tile
+};
+
+// The variant for a type of q, a type of cache, a head width and a group of query heads per kv head.
+AttendVariant attend_variant_f16(int head_dim, int group);
+AttendVariant attend_variant_bf16(int head_dim, int group);
+AttendVariant attend_variant_f16_e4m3(int head_dim, int group);
+AttendVariant attend_variant_bf16_e4m3(int head_dim, int group);
+int launch_weights(const AttendParams&, int grid, cudaStream_t);
+
+}  // namespace fcsim_kv_dev

@@ -18,12 +18,12 @@ struct Pool {
     int n_pages, page_size, n_kv, head_dim;
 };
 
+// Sets a bit of the caller's status word (if there is one).
 __device__ __forceinline__ void flag(int32_t* status, int bit) {
     if (status) atomicOr(status, bit);
 }
 
 struct F16 {
-    using pair = __half2;
     static constexpr int bytes = 2;
     static __device__ __forceinline__ float2 unpack(uint32_t w) {
         return __half22float2(*reinterpret_cast<const __half2*>(&w));
