@@ -2,6 +2,7 @@
 // include/fcsim_kv.h.
 #include "fcsim_kv.h"
 
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <algorithm>
@@ -174,20 +175,59 @@ __device__ __forceinline__ uint32_t order_key(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// One kv head of one request by one CTA: the threshold bit by bit, then places by a running sum, then the copies.
-__global__ void __launch_bounds__(256) fcsim_kv_evict_kernel(const EvictParams p) {
-    const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-    const int n = length_of(p.lengths, r, p.max_length, p.status);
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kMaxCluster = 8;            // CTAs that share a row: the portable size of a cluster
+constexpr int kMaxKeys = 48 * 1024;       // keys a CTA keeps in shared memory (192 KB)
+
+// What request r keeps: `keep` tokens, of which [0, lo) and [hi, n) are sure and `places` go to the largest of [lo, hi).
+struct Cut {
+    int n, keep, lo, hi, places;
+};
+__device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* status) {
+    Cut c;
+    c.n = length_of(p.lengths, r, p.max_length, status);
     int budget = p.budget[r];
     if (budget < 0 || budget > p.max_budget) {
-        flag(p.status, FCSIM_KV_BAD_BUDGET);
+        flag(status, FCSIM_KV_BAD_BUDGET);
         budget = budget < 0 ? 0 : p.max_budget;
     }
-    const int keep = min(n, budget), recent = min(p.recent, budget), first = min(p.first, budget - recent);
-    // tokens [lo, hi) compete for `places`
-    const int lo = keep == n ? n : first, hi = keep == n ? n : n - recent, places = keep - (n - hi) - lo;
-    __shared__ int count;
-    auto key = [&](int t) {
+    c.keep = min(c.n, budget);
+    const int recent = min(p.recent, budget), first = min(p.first, budget - recent);
+    const bool all = c.keep == c.n;
+    c.lo = all ? c.n : first;
+    c.hi = all ? c.n : c.n - recent;
+    c.places = c.keep - (c.n - c.hi) - c.lo;
+    return c;
+}
+
+// Which tokens one kv head of one request keeps, by one cluster.  Every CTA takes an equal slice of the candidates and
+// keeps their keys in shared memory, so that the weights are read once; four counts by 8 bits each, from the top, give
+// the smallest key that is kept and how many of its equals are.  The counts of the CTAs meet over distributed shared
+// memory, one cluster barrier for each (every count has a buffer of its own).  Places then follow from running sums in
+// the order of the tokens.  Bound by the latency of these few passes: a slice is 16 to 32 KB.
+__global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const EvictParams p, const int capacity) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    extern __shared__ uint32_t keys[];
+    __shared__ uint32_t counts[4][256], sums[256];
+    __shared__ int warp_above[kSelectWarps], warp_equal[kSelectWarps], mine[2], chosen[2];
+    const int r = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x, ctas = gridDim.x;
+    const Cut c = cut_of(p, r, h == 0 && rank == 0 && tid == 0 ? p.status : nullptr);
+    int32_t* const kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
+    for (int i = rank * kSelectThreads + tid; i < p.max_budget; i += ctas * kSelectThreads) {
+        if (i < c.lo && i < c.keep) kept[i] = i;
+        else if (i >= c.keep) kept[i] = -1;
+        else if (i >= c.lo + c.places) kept[i] = c.n - c.keep + i;
+    }
+    if (h == 0 && rank == 0 && tid == 0) p.new_lengths[r] = c.keep;
+    if (c.places == 0) return;  // the same for the whole cluster
+
+    const int all = c.hi - c.lo, each = (all + ctas - 1) / ctas;
+    const int begin = min(all, rank * each), count = min(all, begin + each) - begin;
+    const bool resident = each <= capacity;
+    auto weight_key = [&](int i) {
+        const int t = c.lo + begin + i;
         const int page = p.table[r * p.table_row + t / p.pool.page_size];
         if (page < 0 || page >= p.pool.n_pages) {
             flag(p.status, FCSIM_KV_BAD_PAGE);
@@ -195,60 +235,144 @@ __global__ void __launch_bounds__(256) fcsim_kv_evict_kernel(const EvictParams p
         }
         return order_key(p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + t % p.pool.page_size]);
     };
+    auto key = [&](int i) { return resident ? keys[i] : weight_key(i); };
+    for (int i = tid; i < 4 * 256; i += kSelectThreads) counts[0][i] = 0;
+    __syncthreads();
     uint32_t threshold = 0;
-    if (places > 0) {
-        for (int bit = 31; bit >= 0; bit--) {  // the largest threshold that at least `places` keys reach
-            const uint32_t attempt = threshold | (1u << bit);
-            int c = 0;
-            for (int t = lo + tid; t < hi; t += 256) c += key(t) >= attempt;
-            __syncthreads();
-            if (tid == 0) count = 0;
-            __syncthreads();
-            atomicAdd(&count, c);
-            __syncthreads();
-            if (count >= places) threshold = attempt;
-        }
-    }
-    int above = 0;
-    for (int t = lo + tid; t < hi; t += 256) above += key(t) > threshold;
-    __syncthreads();
-    if (tid == 0) count = 0;
-    __syncthreads();
-    atomicAdd(&count, above);
-    __syncthreads();
-    const int ties = places - count;  // the oldest of the keys equal to the threshold
-    int32_t* kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
-    if (tid == 0) {
-        int at = 0, equal = 0;
-        for (int t = 0; t < n; t++) {
-            bool take = t < lo || t >= hi;
-            if (!take && places > 0) {
-                const uint32_t k = key(t);
-                take = k > threshold || (k == threshold && equal++ < ties);
+    int need = c.places;  // how many of the keys with the digits found so far are kept
+#pragma unroll
+    for (int pass = 0; pass < 4; pass++) {
+        const int shift = 24 - 8 * pass;
+        if (pass == 0) {
+#pragma unroll 4
+            for (int i = tid; i < count; i += kSelectThreads) {
+                const uint32_t k = weight_key(i);
+                if (resident) keys[i] = k;
+                atomicAdd(&counts[0][k >> 24], 1u);
             }
-            if (take) kept[at++] = t;
+        } else {
+#pragma unroll 4
+            for (int i = tid; i < count; i += kSelectThreads) {
+                const uint32_t k = key(i);
+                if ((k ^ threshold) >> (shift + 8) == 0) atomicAdd(&counts[pass][(k >> shift) & 255], 1u);
+            }
         }
-        for (int i = keep; i < p.max_budget; i++) kept[i] = -1;
-        if (h == 0) p.new_lengths[r] = keep;
+        cluster.sync();
+        if (tid < 256) {
+            uint32_t sum = 0;
+            for (int i = 0; i < ctas; i++) sum += cluster.map_shared_rank(&counts[pass][0], i)[tid];
+            sums[tid] = sum;
+        }
+        __syncthreads();
+        if (warp == 0) {  // lane i has digits 255 - 8 i .. 248 - 8 i
+            int own[8], total = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) total += own[i] = (int)sums[255 - 8 * lane - i];
+            int upto = total;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int x = __shfl_up_sync(~0u, upto, d);
+                if (lane >= d) upto += x;
+            }
+            int before = upto - total;
+            if (before < need && upto >= need) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    if (before < need && before + own[i] >= need) chosen[0] = 255 - 8 * lane - i, chosen[1] = need - before;
+                    before += own[i];
+                }
+            }
+        }
+        __syncthreads();
+        threshold |= (uint32_t)chosen[0] << shift;
+        need = chosen[1];
     }
+    // places: keys above the threshold, and of its equals the first `need`, in order; a warp has a run of the slice
+    const int run = ((count + kSelectWarps - 1) / kSelectWarps + 31) / 32 * 32;
+    const int from = min(count, warp * run), to = min(count, from + run);
+    int above = 0, equal = 0;
+    for (int i = from + lane; i < to; i += 32) {
+        const uint32_t k = key(i);
+        above += k > threshold;
+        equal += k == threshold;
+    }
+    above = __reduce_add_sync(~0u, above);
+    equal = __reduce_add_sync(~0u, equal);
+    if (lane == 0) warp_above[warp] = above, warp_equal[warp] = equal;
     __syncthreads();
-    const int chunks = p.pool.head_dim * p.bytes / 16;
-    for (int i = tid; i < keep * chunks; i += 256) {
-        const int row = i / chunks, c = i % chunks, t = kept[row];
-        const int page = p.table[r * p.table_row + t / p.pool.page_size];
-        const int to = p.new_table[r * p.new_row + row / p.pool.page_size];
+    if (tid == 0) {
+        int a = 0, e = 0;
+        for (int w = 0; w < kSelectWarps; w++) {
+            const int x = warp_above[w], y = warp_equal[w];
+            warp_above[w] = a, warp_equal[w] = e;
+            a += x, e += y;
+        }
+        mine[0] = a, mine[1] = e;
+    }
+    cluster.sync();
+    above = warp_above[warp], equal = warp_equal[warp];
+    for (int i = 0; i < rank; i++) {
+        const int* other = cluster.map_shared_rank(mine, i);
+        above += other[0], equal += other[1];
+    }
+    const uint32_t earlier = (1u << lane) - 1;
+    for (int i0 = from; i0 < to; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t k = i < to ? key(i) : 0;
+        const bool a = i < to && k > threshold, e = i < to && k == threshold;
+        const uint32_t as = __ballot_sync(~0u, a), es = __ballot_sync(~0u, e);
+        const int equals = equal + __popc(es & earlier);
+        if (a || (e && equals < need)) kept[c.lo + above + __popc(as & earlier) + min(equals, need)] = c.lo + begin + i;
+        above += __popc(as), equal += __popc(es);
+    }
+    cluster.sync();  // the others may still read this CTA's counts
+}
+
+// Copies the kept rows: 16 bytes a lane, LPR lanes a row, four rows of K and V in flight per lane.  Bound by memory.
+template <int LPR>
+__global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p) {
+    constexpr int kAtOnce = 256 / LPR, kRows = 4;
+    const int r = blockIdx.z, h = blockIdx.y, lane = threadIdx.x % LPR;
+    const Cut c = cut_of(p, r, nullptr);
+    const int row0 = blockIdx.x * kAtOnce * kRows + threadIdx.x / LPR;
+    const int chunks = p.pool.head_dim * p.bytes / 16, size = p.pool.page_size;
+    const int32_t* kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
+    int64_t dst[kRows];
+    uint4 k[kRows], v[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; i++) {
+        const int row = row0 + i * kAtOnce;
+        dst[i] = -1;
+        if (row >= c.keep) continue;
+        const int t = kept[row];
+        const int page = p.table[r * p.table_row + t / size], to = p.new_table[r * p.new_row + row / size];
         if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
             flag(p.status, FCSIM_KV_BAD_PAGE);
             continue;
         }
-        const int64_t from = (page * p.pool.stride_page + (t % p.pool.page_size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + c * 16;
-        const int64_t dest = (to * p.pool.stride_page + (row % p.pool.page_size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + c * 16;
-        *reinterpret_cast<uint4*>(p.pool.k + dest) = *reinterpret_cast<const uint4*>(p.pool.k + from);
-        *reinterpret_cast<uint4*>(p.pool.v + dest) = *reinterpret_cast<const uint4*>(p.pool.v + from);
-        if (c == 0)
-            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * p.pool.page_size + row % p.pool.page_size] =
-                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + t % p.pool.page_size];
+        if (lane < chunks) {
+            const int64_t src = (page * p.pool.stride_page + (t % size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            dst[i] = (to * p.pool.stride_page + (row % size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            k[i] = *reinterpret_cast<const uint4*>(p.pool.k + src);
+            v[i] = *reinterpret_cast<const uint4*>(p.pool.v + src);
+        }
+        if (lane == 0)
+            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row % size] =
+                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t % size];
     }
+#pragma unroll
+    for (int i = 0; i < kRows; i++)
+        if (dst[i] >= 0) {
+            *reinterpret_cast<uint4*>(p.pool.k + dst[i]) = k[i];
+            *reinterpret_cast<uint4*>(p.pool.v + dst[i]) = v[i];
+        }
+}
+
+template <int LPR>
+int launch_move(const EvictParams& p, int n_requests, cudaStream_t stream) {
+    const int rows = 256 / LPR * 4;
+    fcsim_kv_move_kernel<LPR><<<dim3((p.max_budget + rows - 1) / rows, p.pool.n_kv, n_requests), 256, 0, stream>>>(p);
+    return launched();
 }
 
 // ------------------------------------------------------------------------------------------------ validation
@@ -304,16 +428,15 @@ AttendVariant attend_variant(const fcsim_kv_cache* c, const fcsim_kv_attend_args
     return a->dtype == FCSIM_KV_F16 ? attend_variant_f16(c->head_dim, group) : attend_variant_bf16(c->head_dim, group);
 }
 
-// SMs of the current device (asked once per device).
-int sm_count(int* out) {
-    static std::atomic<int> known[64];
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
+// The current device and its SMs (asked once per device).
+int device_and_sms(int* device, int* out) {
+    static std::atomic<int> known[kMaxDevices];
+    cudaError_t e = cudaGetDevice(device);
     if (e != cudaSuccess) return cuda_status(e);
-    int n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    int n = *device < kMaxDevices ? known[*device].load(std::memory_order_relaxed) : 0;
     if (n == 0) {
-        if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return cuda_status(e);
-        if (device < 64) known[device].store(n, std::memory_order_relaxed);
+        if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, *device)) != cudaSuccess) return cuda_status(e);
+        if (*device < kMaxDevices) known[*device].store(n, std::memory_order_relaxed);
     }
     *out = n;
     return FCSIM_OK;
@@ -338,9 +461,9 @@ size_t attend_kept(const AttendParams& p) {
 }
 
 int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l) {
-    int sms = 0, per_sm = 0, rc = sm_count(&sms);
+    int device = 0, sms = 0, per_sm = 0, rc = device_and_sms(&device, &sms);
     if (rc != FCSIM_OK) return rc;
-    if ((rc = v.ctas_per_sm(&per_sm)) != 0) return cuda_status((cudaError_t)rc);
+    if ((rc = v.ctas_per_sm(device, &per_sm)) != 0) return cuda_status((cudaError_t)rc);
     const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
     const int64_t tiles = (seen + kTile - 1) / kTile, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
@@ -456,8 +579,38 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     int rc = check_evict(c, a, &p);
     if (rc != FCSIM_OK) return rc;
     if (a->n_requests == 0) return FCSIM_OK;
-    fcsim_kv_evict_kernel<<<dim3(p.pool.n_kv, a->n_requests), 256, 0, (cudaStream_t)cuda_stream>>>(p);
-    return launched();
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    int device = 0, sms = 0;
+    if ((rc = device_and_sms(&device, &sms)) != FCSIM_OK) return rc;
+    // a cluster per (request, kv head), doubled while SMs are idle and a CTA still has two rounds of keys to read
+    int ctas = 1;
+    while (ctas < kMaxCluster && (int64_t)a->n_requests * p.pool.n_kv * ctas < sms && p.max_length / ctas > 2 * kSelectThreads) ctas *= 2;
+    // (and so that the keys fit, whatever the number of rows)
+    while (ctas < kMaxCluster && (p.max_length + ctas - 1) / ctas > kMaxKeys) ctas *= 2;
+    const int capacity = std::min((p.max_length + ctas - 1) / ctas, kMaxKeys);
+    static std::atomic<bool> raised[kMaxDevices];
+    if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxKeys * 4);
+        if (e != cudaSuccess) return cuda_status(e);
+        if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(ctas, p.pool.n_kv, a->n_requests);
+    config.blockDim = dim3(kSelectThreads);
+    config.dynamicSmemBytes = (size_t)capacity * 4;
+    config.stream = stream;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = ctas, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    if ((rc = cuda_status(cudaLaunchKernelEx(&config, fcsim_kv_select_kernel, (const EvictParams)p, capacity))) != FCSIM_OK) return rc;
+    if (p.max_budget == 0) return FCSIM_OK;
+    const int chunks = p.pool.head_dim * p.bytes / 16;
+    if (chunks <= 4) return launch_move<4>(p, a->n_requests, stream);
+    if (chunks <= 8) return launch_move<8>(p, a->n_requests, stream);
+    if (chunks <= 16) return launch_move<16>(p, a->n_requests, stream);
+    return launch_move<32>(p, a->n_requests, stream);
 }
 
 extern "C" int fcsim_kv_last_cuda_error(void) { return g_last_cuda_error; }

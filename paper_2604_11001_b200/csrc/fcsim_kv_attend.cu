@@ -21,6 +21,7 @@
 //   power of two per head to lie in f16's range, with at least 38 bits below its largest element.
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "fcsim_kv_attend.cuh"
@@ -622,11 +623,19 @@ int launch(const AttendParams& p, int grid, cudaStream_t stream) {
     return (int)cudaGetLastError();
 }
 template <class T, class C, int DP, int NT>
-int ctas_per_sm(int* out) {
+int ctas_per_sm(int device, int* out) {
     using S = Shape<T, C, DP, NT>;
-    auto* kernel = fcsim_kv_attend_kernel<T, C, DP, NT>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-    return (int)(e != cudaSuccess ? e : cudaOccupancyMaxActiveBlocksPerMultiprocessor(out, kernel, kThreads, S::kBytes));
+    static std::atomic<int> known[kMaxDevices];
+    int n = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        auto* kernel = fcsim_kv_attend_kernel<T, C, DP, NT>;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, S::kBytes);
+        if (e != cudaSuccess) return (int)e;
+        if (device < kMaxDevices) known[device].store(n, std::memory_order_relaxed);
+    }
+    *out = n;
+    return 0;
 }
 template <class T, class C, int DP>
 AttendVariant of_group(int group) {

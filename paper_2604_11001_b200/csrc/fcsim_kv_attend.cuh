@@ -6,6 +6,7 @@ namespace fcsim_kv_dev {
 
 constexpr int kTile = 64;        // tokens a CTA takes at once: 16 by each of its four warps
 constexpr int kThreads = 128;
+constexpr int kMaxDevices = 64;   // devices for which answers of the runtime are remembered
 constexpr int kMaxCtas = 4096;   // bound of the grid (the work is divided among the CTAs at run time)
 
 struct AttendParams {
@@ -29,7 +30,7 @@ struct AttendParams {
 // A variant of the kernel.  The functions return a cudaError_t.
 struct AttendVariant {
     int (*launch)(const AttendParams&, int grid, cudaStream_t);
-    int (*ctas_per_sm)(int* out);  // also raises the kernel's limit of shared memory
+    int (*ctas_per_sm)(int device, int* out);  // asked once per device; also raises the kernel's limit of shared memory
     int head_cols, width;          // query heads and elements of its tile
 };
 

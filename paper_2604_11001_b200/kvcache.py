@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 
 import torch
 
@@ -21,6 +22,10 @@ from . import binding as _fb
 F16, BF16, E4M3 = 0, 1, 2
 BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET = 1, 2, 4, 8
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+_WIDE = (torch.float16, torch.bfloat16)
+_ESIZE = -3
+# the current device's number and a device's current stream as plain integers, without the objects around them
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 class fcsim_kv_cache(C.Structure):
@@ -58,6 +63,11 @@ class fcsim_kv_workspace(C.Structure):
     _fields_ = [("bytes", C.c_size_t), ("zeroed", C.c_size_t)]
 
 
+# the argument structs as one packing each (native sizes and alignment, as the compiler's)
+_APPEND, _ATTEND, _EVICT = struct.Struct("10P6q6ifi"), struct.Struct("6P3q7if"), struct.Struct("7P2q8i")
+assert (_APPEND.size, _ATTEND.size, _EVICT.size) == (C.sizeof(fcsim_kv_append_args), C.sizeof(fcsim_kv_attend_args),
+                                                     C.sizeof(fcsim_kv_evict_args))
+
 EXPORTS = ("fcsim_kv_append", "fcsim_kv_attend_workspace", "fcsim_kv_attend", "fcsim_kv_evict_workspace",
            "fcsim_kv_evict", "fcsim_kv_last_cuda_error")
 
@@ -69,12 +79,11 @@ def load():
     global _lib
     if _lib is None:
         lib = _fb.load()
-        vp, cache = C.c_void_p, C.POINTER(fcsim_kv_cache)
-        lib.fcsim_kv_append.argtypes = [cache, C.POINTER(fcsim_kv_append_args), vp]
-        for name, args in (("attend", fcsim_kv_attend_args), ("evict", fcsim_kv_evict_args)):
-            getattr(lib, f"fcsim_kv_{name}_workspace").argtypes = [cache, C.POINTER(args),
-                                                                   C.POINTER(fcsim_kv_workspace)]
-            getattr(lib, f"fcsim_kv_{name}").argtypes = [cache, C.POINTER(args), vp, C.c_size_t, vp]
+        vp = C.c_void_p
+        lib.fcsim_kv_append.argtypes = [vp, vp, vp]
+        for name in ("attend", "evict"):
+            getattr(lib, f"fcsim_kv_{name}_workspace").argtypes = [vp, vp, C.POINTER(fcsim_kv_workspace)]
+            getattr(lib, f"fcsim_kv_{name}").argtypes = [vp, vp, vp, C.c_size_t, vp]
         lib.fcsim_kv_last_cuda_error.argtypes = []
         for name in EXPORTS:
             getattr(lib, name).restype = C.c_int
@@ -95,7 +104,7 @@ def _need(ok, what):
 
 
 def _pointer(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
 class PagedKV:
@@ -126,8 +135,9 @@ class PagedKV:
                   "k_scale, v_scale: None for 16-bit caches, contiguous float32 [n_kv_heads] for 8-bit ones")
         self.k, self.v, self.weight, self.k_scale, self.v_scale = k, v, weight, k_scale, v_scale
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = n_pages, page_size, n_kv, head_dim
-        self.device = k.device
+        self.device, self._index = k.device, k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self._status = self.status.data_ptr()
         self._workspaces = {}   # stream -> zero-initialised workspace, so that streams never share one
         self._c = fcsim_kv_cache(k.data_ptr(), v.data_ptr(), _pointer(weight), _pointer(k_scale), _pointer(v_scale),
                                  k.stride(0), k.stride(1), k.stride(2), _TYPES[k.dtype], n_pages, page_size, n_kv,
@@ -151,50 +161,63 @@ class PagedKV:
         return cls(pool(), pool(), w, k_scale, v_scale)
 
     # ------------------------------------------------------------------------------------------ helpers
-    def _same_device(self, *tensors):
+    # A slot's calls take a few microseconds on the device: checks are plain comparisons, the argument struct is packed
+    # in one go, and messages are only made when they are needed.
+    def _on_device(self, *tensors):
         for t in tensors:
-            if t is not None and t.device != self.device:
+            if t is not None and t.get_device() != self._index:
                 raise ValueError(f"tensors have to be on the cache's device {self.device}, got {t.device}")
 
-    def _heads(self, x, name, n, heads, dtype):
-        _need(x.dim() == 3 and x.shape[0] == n and (heads is None or x.shape[1] == heads)
-              and x.shape[2] == self.head_dim and x.dtype == dtype and x.stride(2) == 1,
-              f"{name}: [tokens, heads, head_dim] of one 16-bit type, head_dim contiguous")
+    def _rows(self, x, name, n, heads, dtype):
+        """Strides of [tokens, heads, head_dim]."""
+        if x.dim() != 3 or x.dtype != dtype or x.shape[0] != n or x.shape[1] != heads or x.shape[2] != self.head_dim:
+            raise ValueError(f"{name}: {dtype} [{n}, {heads}, {self.head_dim}], got {x.dtype} {list(x.shape)}")
+        row, head, one = x.stride()
+        if one != 1:
+            raise ValueError(f"{name}: head_dim has to be contiguous")
+        return row, head
 
-    def _table(self, table, name, n):
-        _need(table.dim() == 2 and table.shape[0] == n and table.dtype == torch.int32
-              and (table.shape[1] <= 1 or table.stride(1) == 1), f"{name}: int32 [requests, pages], rows contiguous")
+    @staticmethod
+    def _table(table, name, n):
+        if (table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != n
+                or (table.stride(1) != 1 and table.shape[1] > 1)):
+            raise ValueError(f"{name}: int32 [{n}, pages], rows contiguous")
+        return table.shape[1]
 
-    def _ints(self, x, name, n, dtype=torch.int32):
-        _need(x.dim() == 1 and x.shape[0] == n and x.dtype == dtype and (n <= 1 or x.stride(0) == 1),
-              f"{name}: contiguous {dtype} [{n}]")
+    @staticmethod
+    def _ints(x, name, n, dtype=torch.int32):
+        if x.dim() != 1 or x.dtype != dtype or x.shape[0] != n or (n > 1 and x.stride(0) != 1):
+            raise ValueError(f"{name}: contiguous {dtype} [{n}]")
 
-    def _call(self, name, args, workspace):
-        lib = _lib
-        if torch.cuda.current_device() != self.device.index:
+    def _call(self, entry, args, size=None):
+        """Run an entry point on the current stream of the cache's device.  ``size``: the entry point that tells the size
+        of its workspace, asked when the one at hand is too small."""
+        if _current_device() != self._index:
             with torch.cuda.device(self.device):
-                return self._call(name, args, workspace)
-        stream = torch.cuda.current_stream().cuda_stream
-        ref = C.byref(args)
-        if not workspace:
-            code = getattr(lib, name)(self._c_ref, ref, stream)
+                return self._call(entry, args, size)
+        stream = _current_stream(self._index)
+        if size is None:
+            code = entry(self._c_ref, args, stream)
         else:
-            need = fcsim_kv_workspace()
-            code = getattr(lib, name + "_workspace")(self._c_ref, ref, C.byref(need))
-            if code == 0:
-                buf = self._workspace(stream, need.bytes) if need.bytes else None
-                code = getattr(lib, name)(self._c_ref, ref, _pointer(buf), need.bytes, stream)
+            buf = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream)
+            code = _ESIZE
+            if buf is not None:
+                code = entry(self._c_ref, args, buf.data_ptr(), buf.numel(), stream)
+            if code == _ESIZE:
+                need = fcsim_kv_workspace()
+                code = size(self._c_ref, args, C.byref(need))
+                if code == 0:
+                    buf = self._workspace(stream, need.bytes)
+                    code = entry(self._c_ref, args, buf.data_ptr(), buf.numel(), stream)
         if code != 0:
-            _raise(code, name)
+            _raise(code, entry.__name__)
 
     def _workspace(self, stream, size):
         """Zeroed when new; every call leaves the part that has to be zero as it found it.  A graph under capture
         gets its own, whose zeroing is part of the graph."""
-        if torch.cuda.is_current_stream_capturing():
-            return torch.zeros(size, dtype=torch.uint8, device=self.device)
-        buf = self._workspaces.get(stream)
-        if buf is None or buf.numel() < size:
-            buf = self._workspaces[stream] = torch.zeros(size, dtype=torch.uint8, device=self.device)
+        buf = torch.zeros(max(size, 16), dtype=torch.uint8, device=self.device)
+        if not torch.cuda.is_current_stream_capturing():
+            self._workspaces[stream] = buf
         return buf
 
     # ------------------------------------------------------------------------------------------ operators
@@ -204,34 +227,36 @@ class PagedKV:
 
         ``rope``: float32 [positions, rope_dim], cosines then sines; ``positions``: int32 [n].  ``q_norm``,
         ``k_norm``: [head_dim] weights of the norms over each head.  ``q`` may be None (nothing is returned)."""
-        n = k.shape[0]
-        dtype = k.dtype
-        self._heads(k, "k", n, self.n_kv_heads, dtype)
-        self._heads(v, "v", n, self.n_kv_heads, dtype)
+        n, dtype = k.shape[0], k.dtype
+        if dtype not in _WIDE:
+            raise ValueError("k: float16 or bfloat16")
+        k_row, k_head = self._rows(k, "k", n, self.n_kv_heads, dtype)
+        v_row, v_head = self._rows(v, "v", n, self.n_kv_heads, dtype)
         self._ints(slots, "slots", n, torch.int64)
-        _need(dtype in _TYPES and dtype != torch.float8_e4m3fn, "k: float16 or bfloat16")
         out, heads, q_row, q_head = None, 0, 0, 0
         if q is not None:
-            self._heads(q, "q", n, None, dtype)
             heads = q.shape[1]
-            q_row, q_head = q.stride(0), q.stride(1)
-            out = torch.empty((n, heads, self.head_dim), dtype=dtype, device=self.device)
+            q_row, q_head = self._rows(q, "q", n, heads, dtype)
         rope_dim = n_positions = 0
         if rope is not None:
-            _need(rope.dim() == 2 and rope.dtype == torch.float32 and rope.is_contiguous(),
-                  "rope: contiguous float32 [positions, rope_dim]")
+            if rope.dim() != 2 or rope.dtype != torch.float32 or not rope.is_contiguous():
+                raise ValueError("rope: contiguous float32 [positions, rope_dim]")
+            if positions is None:
+                raise ValueError("positions: needed with rope")
             self._ints(positions, "positions", n)
             n_positions, rope_dim = rope.shape
+        else:
+            positions = None
         for w in (q_norm, k_norm):
-            _need(w is None or (tuple(w.shape) == (self.head_dim,) and w.dtype == dtype and w.stride(0) == 1),
-                  "q_norm, k_norm: [head_dim] of q's type")
-        self._same_device(q, k, v, slots, rope, positions if rope is not None else None, q_norm, k_norm)
-        args = fcsim_kv_append_args(
+            if w is not None and (w.dim() != 1 or w.shape[0] != self.head_dim or w.dtype != dtype or w.stride(0) != 1):
+                raise ValueError(f"q_norm, k_norm: contiguous {dtype} [{self.head_dim}]")
+        self._on_device(q, k, v, slots, rope, positions, q_norm, k_norm)
+        if q is not None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        self._call(_lib.fcsim_kv_append, _APPEND.pack(
             _pointer(q), k.data_ptr(), v.data_ptr(), _pointer(out), _pointer(q_norm), _pointer(k_norm), _pointer(rope),
-            _pointer(positions) if rope is not None else None, slots.data_ptr(), self.status.data_ptr(),
-            q_row, q_head, k.stride(0), k.stride(1), v.stride(0), v.stride(1), n, heads, _TYPES[dtype], rope_dim,
-            n_positions, 1 if interleaved else 0, eps, 0)
-        self._call("fcsim_kv_append", args, False)
+            _pointer(positions), slots.data_ptr(), self._status, q_row, q_head, k_row, k_head, v_row, v_head, n, heads,
+            _TYPES[dtype], rope_dim, n_positions, 1 if interleaved else 0, eps, 0))
         return out
 
     def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, add_weight=False,
@@ -242,22 +267,20 @@ class PagedKV:
 
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
         only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
-        _need(q.dim() == 3, "q: [requests, heads, head_dim]")
-        n, heads = q.shape[0], q.shape[1]
-        self._heads(q, "q", n, None, q.dtype)
-        _need(q.dtype == torch.float16 or q.dtype == torch.bfloat16, "q: float16 or bfloat16")
-        self._table(table, "table", n)
+        if q.dim() != 3 or q.dtype not in _WIDE:
+            raise ValueError("q: float16 or bfloat16 [requests, heads, head_dim]")
+        n, heads, dtype = q.shape[0], q.shape[1], q.dtype
+        q_row, q_head = self._rows(q, "q", n, heads, dtype)
+        cols = self._table(table, "table", n)
         self._ints(lengths, "lengths", n)
-        self._same_device(q, table, lengths)
-        if max_length is None:
-            max_length = table.shape[1] * self.page_size
-        out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
-        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device) if return_lse else None
-        args = fcsim_kv_attend_args(
-            q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self.status.data_ptr(),
-            q.stride(0), q.stride(1), table.stride(0), n, heads, _TYPES[q.dtype], table.shape[1], max_length, window,
-            1 if add_weight else 0, 1.0 / math.sqrt(self.head_dim) if scale is None else scale)
-        self._call("fcsim_kv_attend", args, True)
+        self._on_device(q, table, lengths)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = q.new_empty((n, heads), dtype=torch.float32) if return_lse else None
+        self._call(_lib.fcsim_kv_attend, _ATTEND.pack(
+            q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self._status, q_row,
+            q_head, table.stride(0), n, heads, _TYPES[dtype], cols,
+            cols * self.page_size if max_length is None else max_length, window, 1 if add_weight else 0,
+            1.0 / math.sqrt(self.head_dim) if scale is None else scale), _lib.fcsim_kv_attend_workspace)
         return (out, lse) if return_lse else out
 
     def evict(self, table, lengths, budget, new_table, *, max_budget=None, recent=0, first=0, max_length=None):
@@ -266,22 +289,21 @@ class PagedKV:
         call may read).  Returns the new lengths (int32 [requests]) and the old index of every kept token (int32
         [requests, n_kv_heads, max_budget], -1 beyond)."""
         n = lengths.shape[0]
-        self._table(table, "table", n)
-        self._table(new_table, "new_table", n)
+        cols, new_cols = self._table(table, "table", n), self._table(new_table, "new_table", n)
         self._ints(lengths, "lengths", n)
         self._ints(budget, "budget", n)
-        self._same_device(table, lengths, budget, new_table)
-        if max_length is None:
-            max_length = table.shape[1] * self.page_size
+        self._on_device(table, lengths, budget, new_table)
         if max_budget is None:
-            max_budget = new_table.shape[1] * self.page_size
-        new_lengths = torch.empty(n, dtype=torch.int32, device=self.device)
-        kept = torch.empty((n, self.n_kv_heads, max_budget), dtype=torch.int32, device=self.device)
-        args = fcsim_kv_evict_args(
+            max_budget = new_cols * self.page_size
+        if max_budget < 0:
+            raise ValueError("max_budget: 0 or more")
+        new_lengths = torch.empty_like(lengths)
+        kept = lengths.new_empty((n, self.n_kv_heads, max_budget))
+        self._call(_lib.fcsim_kv_evict, _EVICT.pack(
             table.data_ptr(), lengths.data_ptr(), budget.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(),
-            kept.data_ptr(), self.status.data_ptr(), table.stride(0), new_table.stride(0), n, table.shape[1],
-            new_table.shape[1], max_length, max_budget, recent, first, 0)
-        self._call("fcsim_kv_evict", args, True)
+            kept.data_ptr(), self._status, table.stride(0), new_table.stride(0), n, cols, new_cols,
+            cols * self.page_size if max_length is None else max_length, max_budget, recent, first, 0),
+            _lib.fcsim_kv_evict_workspace)
         return new_lengths, kept
 
     def check(self):
