@@ -61,7 +61,8 @@ typedef struct {
  * norm weights; a 16-bit cache must have the same.
  * q_norm, k_norm: [head_dim], or NULL = that norm is left out.  x <- x / sqrt(mean(x^2) + eps) * w over each head.
  * rope: fp32 [n_positions][rope_dim], the cosines of the rope_dim / 2 angles, then their sines; NULL = no rotation.
- *   The first rope_dim elements of a head turn in pairs: (i, i + rope_dim / 2) (rope_dim a multiple of 16), or with
+ *   The first rope_dim elements of a head turn in pairs: (i, i + rope_dim / 2) (rope_dim a multiple of 16, the table 16-byte
+ *   aligned), or with
  *   `interleaved` (2i, 2i + 1) (rope_dim even); the others pass.
  * positions: [n] int32 (unused without rope).  slots: [n] int64 = page * page_size + place, negative = not stored.  No two tokens
  *   of a call may have the same slot.

@@ -41,113 +41,169 @@ struct AppendParams {
     float eps;
 };
 
-// One row (a head of a token of q, k or v) by a group of LPR lanes, 8 elements a lane.
-template <class T, class C, int LPR>
+// Lanes with work from which a group takes four heads instead of one.
+constexpr int64_t kAppendMany = 1 << 20;
+
+// 16 bytes of a lane as 8 elements.
+template <class T>
+__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
+    const float2 a = T::unpack(w.x), b = T::unpack(w.y), c = T::unpack(w.z), d = T::unpack(w.w);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
+}
+
+// A group of LPR lanes takes HPG heads of one token, 8 elements a lane; a CTA takes the same heads of 256 / LPR tokens, so
+// that all its branches on the kind of head are uniform.  The heads' loads are issued together, and the token's
+// cosines and sines are read once for all of them (they are twice a row's bytes).  Bound by the bytes of q, k and v
+// when there are many tokens, by latency when there are few.
+template <class T, class C, int LPR, int HPG>
 __global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams p) {
-    const int heads = p.n_heads + 2 * p.pool.n_kv, D = p.pool.head_dim;
+    const int heads = p.n_heads + 2 * p.pool.n_kv, D = p.pool.head_dim, first = blockIdx.y * HPG;
     const int lane = threadIdx.x & (LPR - 1);
-    const int64_t item = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / LPR;
-    const bool there = item < (int64_t)p.n_tokens * heads;
-    const int token = there ? (int)(item / heads) : 0, j = there ? (int)(item - (int64_t)token * heads) : 0;
-    const bool is_q = j < p.n_heads, is_v = j >= p.n_heads + p.pool.n_kv;
-    const int h = is_q ? j : is_v ? j - p.n_heads - p.pool.n_kv : j - p.n_heads;
-    const bool mine = there && lane * 8 < D;
-    int position = 0;
-    bool turned = p.rope != nullptr, good = true;
-    if (turned) {
-        position = p.positions[token];
+    const int at = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const bool there = at < p.n_tokens, mine = there && lane * 8 < D;
+    const int64_t token = there ? at : 0;
+    uint4 raw[HPG];
+#pragma unroll
+    for (int i = 0; i < HPG; i++) {
+        const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
+        if (mine && j < heads) {
+            const char* src = k < 0 ? p.q + (token * p.q_row + j * p.q_head) * 2
+                            : v < 0 ? p.k + (token * p.k_row + k * p.k_head) * 2
+                                    : p.v + (token * p.v_row + v * p.v_head) * 2;
+            raw[i] = *reinterpret_cast<const uint4*>(src + lane * 16);
+        } else
+            raw[i] = make_uint4(0, 0, 0, 0);
+    }
+    // the token's rotation: 8 cosines and sines a lane, or 4 of pairs that are neighbours
+    bool good = true, turned = false;
+    float cosine[8], sine[8];
+    const bool any_turned = p.rope != nullptr && first < p.n_heads + p.pool.n_kv;
+    const bool lower = lane * 16 < p.rope_dim;  // this lane's half of the pairs
+    if (p.rope != nullptr) {
+        const int position = p.positions[token];
         good = position >= 0 && position < p.n_positions;
-        if (!good && there && lane == 0) flag(p.status, FCSIM_KV_BAD_POSITION);
-    }
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (mine) {
-        const char* src = is_q ? p.q + ((int64_t)token * p.q_row + (int64_t)h * p.q_head) * 2
-                        : is_v ? p.v + ((int64_t)token * p.v_row + (int64_t)h * p.v_head) * 2
-                               : p.k + ((int64_t)token * p.k_row + (int64_t)h * p.k_head) * 2;
-        load8<T>(src + lane * 16, x);
-    }
-    const char* w = is_q ? p.q_norm : is_v ? nullptr : p.k_norm;
-    float sum = 0;
+        if (!good && there && lane == 0 && first == 0) flag(p.status, FCSIM_KV_BAD_POSITION);
+        turned = lane * 8 < p.rope_dim;
+        if (any_turned && turned) {
+            const int half = p.rope_dim / 2;
+            const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim;
+            if (p.interleaved) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) sum += x[i] * x[i];
+                for (int i = 0; i < 4; i++) {
+                    const bool in = lane * 8 + 2 * i < p.rope_dim;
+                    cosine[i] = in ? row[lane * 4 + i] : 1.0f;
+                    sine[i] = in ? row[half + lane * 4 + i] : 0.0f;
+                }
+            } else {
+                row += lower ? lane * 8 : lane * 8 - half;
 #pragma unroll
-    for (int m = LPR / 2; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
-    if (w && mine) {
-        float y[8];
-        load8<T>(w + lane * 16, y);
-        const float r = 1.0f / sqrtf(sum / (float)D + p.eps);
+                for (int i = 0; i < 8; i += 4) {
+                    *reinterpret_cast<float4*>(cosine + i) = *reinterpret_cast<const float4*>(row + i);
+                    *reinterpret_cast<float4*>(sine + i) = *reinterpret_cast<const float4*>(row + half + i);
+                }
+                if (lower) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = x[i] * r * y[i];
-    }
-    if (turned) {
-        const int half = p.rope_dim / 2;
-        const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim;
-        float mate[8];
-        // pairs half a rotation apart: the other element sits rope_dim / 16 lanes away, at the same place
-        const int first = lane * 8 < half;
-        const int other = first ? lane + p.rope_dim / 16 : lane - p.rope_dim / 16;
-#pragma unroll
-        for (int i = 0; i < 8; i++) mate[i] = __shfl_sync(~0u, x[i], other & (LPR - 1), LPR);
-        if (mine && !is_v) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int e = lane * 8 + i;
-                if (e < p.rope_dim) {
-                    if (p.interleaved) {
-                        if (!(i & 1)) {
-                            const float c = row[e / 2], s = row[half + e / 2], a = x[i], b = x[i + 1];
-                            x[i] = a * c - b * s;
-                            x[i + 1] = b * c + a * s;
-                        }
-                    } else {
-                        const int a = first ? e : e - half;
-                        const float c = row[a], s = row[half + a];
-                        x[i] = first ? x[i] * c - mate[i] * s : x[i] * c + mate[i] * s;
-                    }
+                    for (int i = 0; i < 8; i++) sine[i] = -sine[i];
                 }
             }
         }
     }
-    if (!there) return;
-    if (is_q) {
-        if (!good) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = 0;
+    // the token's place in the cache
+    int64_t place = -1;
+    int page = 0, in_page = 0;
+    if (there && good && first + HPG > p.n_heads) {
+        const int64_t slot = p.slots[token];
+        if (slot >= (int64_t)p.pool.n_pages * p.pool.page_size) {
+            if (lane == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
+        } else if (slot >= 0) {
+            page = (int)((uint32_t)slot / (uint32_t)p.pool.page_size);
+            in_page = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)p.pool.page_size);
+            place = page * p.pool.stride_page + in_page * p.pool.stride_slot;
         }
-        if (mine) store8<T>(p.q_out + (((int64_t)token * p.n_heads + h) * D + lane * 8) * 2, x);
-        return;
     }
-    const int64_t slot = p.slots[token];
-    if (slot < 0 || !good) return;
-    if (slot >= (int64_t)p.pool.n_pages * p.pool.page_size) {
-        if (lane == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
-        return;
-    }
-    const int page = (int)((uint32_t)slot / (uint32_t)p.pool.page_size);
-    const int place = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)p.pool.page_size);
-    if (C::bytes == 1 && mine) {
-        const float s = is_v ? p.pool.v_scale[h] : p.pool.k_scale[h];
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = x[i] / s;
+    for (int i = 0; i < HPG; i++) {
+        const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
+        if (j >= heads) break;
+        float x[8];
+        unpack8<T>(raw[i], x);
+        if (v < 0) {
+            const char* w = k < 0 ? p.q_norm : p.k_norm;
+            if (w) {
+                float sum = 0, y[8];
+#pragma unroll
+                for (int e = 0; e < 8; e++) sum += x[e] * x[e];
+#pragma unroll
+                for (int m = LPR / 2; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
+                if (mine) {
+                    unpack8<T>(*reinterpret_cast<const uint4*>(w + lane * 16), y);
+                    const float r = 1.0f / sqrtf(sum / (float)D + p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = x[e] * r * y[e];
+                }
+            }
+            if (p.rope != nullptr) {
+                if (p.interleaved) {
+                    if (turned) {
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const float a = x[2 * e], b = x[2 * e + 1];
+                            if (lane * 8 + 2 * e < p.rope_dim) {
+                                x[2 * e] = a * cosine[e] - b * sine[e];
+                                x[2 * e + 1] = b * cosine[e] + a * sine[e];
+                            }
+                        }
+                    }
+                } else {
+                    // the other element of a pair sits rope_dim / 16 lanes away, at the same place
+                    const int other = (lower ? lane + p.rope_dim / 16 : lane - p.rope_dim / 16) & (LPR - 1);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const float mate = __shfl_sync(~0u, x[e], other, LPR);
+                        if (turned) x[e] = x[e] * cosine[e] + mate * sine[e];
+                    }
+                }
+            }
+        }
+        if (k < 0) {
+            if (!good) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = 0;
+            }
+            if (mine) store8<T>(p.q_out + ((token * p.n_heads + j) * D + lane * 8) * 2, x);
+            continue;
+        }
+        if (place < 0) continue;
+        const int h = v < 0 ? k : v;
+        if (C::bytes == 1) {
+            const float s = 1.0f / (v < 0 ? p.pool.k_scale[h] : p.pool.v_scale[h]);
+#pragma unroll
+            for (int e = 0; e < 8; e++) x[e] *= s;
+        }
+        if (mine) store8<C>((v < 0 ? p.pool.k : p.pool.v) + (place + h * p.pool.stride_head + lane * 8) * C::bytes, x);
+        if (v < 0 && lane == 0 && p.pool.weight)
+            p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + in_page] = 0.0f;
     }
-    char* dst = (is_v ? p.pool.v : p.pool.k) +
-                (page * p.pool.stride_page + place * p.pool.stride_slot + h * p.pool.stride_head + lane * 8) * C::bytes;
-    if (mine) store8<C>(dst, x);
-    if (!is_v && lane == 0 && p.pool.weight)
-        p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + place] = 0.0f;
 }
 
+template <class T, class C, int LPR, int HPG>
+int launch_append_as(const AppendParams& p, cudaStream_t stream) {
+    const int heads = p.n_heads + 2 * p.pool.n_kv, tokens = 256 / LPR;
+    const dim3 grid((p.n_tokens + tokens - 1) / tokens, (heads + HPG - 1) / HPG);
+    fcsim_kv_append_kernel<T, C, LPR, HPG><<<grid, 256, 0, stream>>>(p);
+    return launched();
+}
+template <class T, class C, int LPR>
+int launch_append_lanes(const AppendParams& p, cudaStream_t stream) {
+    const int64_t lanes = (int64_t)p.n_tokens * (p.n_heads + 2 * p.pool.n_kv) * LPR;
+    return lanes >= kAppendMany ? launch_append_as<T, C, LPR, 4>(p, stream) : launch_append_as<T, C, LPR, 1>(p, stream);
+}
 template <class T, class C>
 int launch_append(const AppendParams& p, cudaStream_t stream) {
     const int lanes = p.pool.head_dim / 8;
-    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads + 2 * p.pool.n_kv);
-    const int lpr = lanes <= 8 ? 8 : lanes <= 16 ? 16 : 32;
-    const int64_t blocks = (rows * lpr + 255) / 256;
-    if (blocks > 0x7fffffff) return FCSIM_EINVAL;
-    if (lpr == 8) fcsim_kv_append_kernel<T, C, 8><<<(unsigned)blocks, 256, 0, stream>>>(p);
-    else if (lpr == 16) fcsim_kv_append_kernel<T, C, 16><<<(unsigned)blocks, 256, 0, stream>>>(p);
-    else fcsim_kv_append_kernel<T, C, 32><<<(unsigned)blocks, 256, 0, stream>>>(p);
-    return launched();
+    if (lanes <= 8) return launch_append_lanes<T, C, 8>(p, stream);
+    if (lanes <= 16) return launch_append_lanes<T, C, 16>(p, stream);
+    return launch_append_lanes<T, C, 32>(p, stream);
 }
 
 // ------------------------------------------------------------------------------------------------ evict
@@ -506,14 +562,14 @@ extern "C" int fcsim_kv_append(const fcsim_kv_cache* c, const fcsim_kv_append_ar
     if (!a) return FCSIM_EINVAL;
     if ((rc = check_type(c, a->dtype)) != FCSIM_OK) return rc;
     if (a->n_tokens < 0 || a->n_heads < 0 || !(a->eps >= 0) || !isfinite(a->eps)) return FCSIM_EINVAL;
-    if ((int64_t)a->n_heads + 2 * c->n_kv_heads > 1 << 20) return FCSIM_EINVAL;
+    if ((int64_t)a->n_heads + 2 * c->n_kv_heads > 65535) return FCSIM_EINVAL;
     if (!good_stride(a->q_row, 2) || !good_stride(a->q_head, 2) || !good_stride(a->k_row, 2) ||
         !good_stride(a->k_head, 2) || !good_stride(a->v_row, 2) || !good_stride(a->v_head, 2))
         return FCSIM_EINVAL;
     if (a->rope) {
         if (a->rope_dim < 2 || a->rope_dim > c->head_dim || a->rope_dim % (a->interleaved ? 2 : 16) || a->n_positions < 1)
             return FCSIM_EINVAL;
-        if ((uintptr_t)a->rope & 3) return FCSIM_ESIZE;
+        if ((uintptr_t)a->rope & (a->interleaved ? 3 : 15)) return FCSIM_ESIZE;
     }
     if (a->n_tokens == 0) return FCSIM_OK;
     if (!a->k || !a->v || !a->slots || (a->rope && !a->positions) || (a->n_heads && (!a->q || !a->q_out))) return FCSIM_ESIZE;
