@@ -474,6 +474,7 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
     p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length, p->window = a->window;
     p->add_weight = a->add_weight != 0, p->scale = a->scale;
+    p->page_magic = ((1ull << 62) + c->page_size - 1) / c->page_size;
     return FCSIM_OK;
 }
 

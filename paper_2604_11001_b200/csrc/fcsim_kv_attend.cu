@@ -32,6 +32,9 @@ namespace {
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 // 16 bytes global -> shared; with `bytes` = 0 nothing is read and zeros are written
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -39,6 +42,12 @@ __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;"
 template <int N>
 __device__ __forceinline__ void wait_group() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// 2^x for x <= 0; results below 2^-126 are 0
+__device__ __forceinline__ float power2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ void load_matrices(uint32_t a, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -83,10 +92,17 @@ template <class T>
 struct OperandOf<T, E4M3> { using type = F16; };
 
 // ---------------------------------------------------------------------------------------------- the walk over the work
-// A place in the work: request b, head tile r of its `per` (kv head, head tile) pairs, tile j of `tiles`.
+// The work is counted in units: a tile is one, and every (request, kv head, head tile) group counts kOverhead more for its
+// start and its end (q, the warps' merge, the output), which is what they cost beside a tile.  The units before a
+// group's first tile stand for these.
+constexpr int kOverhead = 4;
+constexpr int kLeast = kOverhead + 4;  // units of a CTA at least: below that, joining costs more than it spreads
+
+// A place in the work: request b, group r of its `per`, tile j of `tiles`.
 struct Place {
     int b, r, j, tiles, start, len;
-    int64_t base;  // tiles of the requests before b
+    int64_t tiles_before;  // tiles of the requests before b
+    int64_t left;          // units from this tile to the end of the CTA's stretch; none: the place is beyond it
 };
 
 __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
@@ -105,104 +121,126 @@ __device__ __forceinline__ void enter(const AttendParams& p, Place& w, int b) {
     w.start = start_of(p, w.len);
     w.tiles = tiles_of(p, w.len);
 }
-// The next tile of the work; the caller knows that there is one.
+// The next tile, if the stretch has one more.
+template <int OVERHEAD>
 __device__ __forceinline__ void advance(const AttendParams& p, Place& w, int per) {
+    w.left--;
     if (++w.j < w.tiles) return;
+    w.left -= OVERHEAD;
+    if (w.left <= 0) return;
     w.j = 0;
     if (++w.r < per) return;
     w.r = 0;
-    w.base += w.tiles;
+    w.tiles_before += w.tiles;
     do enter(p, w, w.b + 1);
     while (w.tiles == 0);
 }
 
 struct Shares {
-    int64_t first, end, share;  // this CTA's tiles [first, end); a CTA's share
+    int64_t first, end, share;  // this CTA's units [first, end); a CTA's share
 };
 
-// Divides the tiles of all requests among the CTAs and finds where this CTA's stretch begins.  `per`: how often each
-// request's tiles count.  A share is at least `least` tiles, below which joining costs more than it spreads.
+// Divides the units of all requests among the CTAs and finds where this CTA's stretch begins.  `per`: groups of a request.
+template <int OVERHEAD>
 __device__ __forceinline__ Shares divide(const AttendParams& p, int per, int least, Place& w) {
-    __shared__ int64_t warp_sums[kThreads / 32];
-    __shared__ int64_t found_base;
+    __shared__ int64_t warp_tiles[kThreads / 32], warp_units[kThreads / 32];
+    __shared__ int64_t found_tiles, found_units;
     __shared__ int found_request;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int each = (p.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, p.n_requests), b1 = min(b0 + each, p.n_requests);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; b++) mine += tiles_of(p, length_of(p, b));
-    int64_t upto = mine;
+    int64_t tiles = 0, units = 0;
+    for (int b = b0; b < b1; b++) {
+        const int t = tiles_of(p, length_of(p, b));
+        tiles += t;
+        units += t ? t + OVERHEAD : 0;
+    }
+    int64_t tiles_upto = tiles, units_upto = units;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(~0u, upto, d);
-        if (lane >= d) upto += x;
+        const int64_t x = __shfl_up_sync(~0u, tiles_upto, d), y = __shfl_up_sync(~0u, units_upto, d);
+        if (lane >= d) tiles_upto += x, units_upto += y;
     }
-    if (lane == 31) warp_sums[warp] = upto;
+    if (lane == 31) warp_tiles[warp] = tiles_upto, warp_units[warp] = units_upto;
     __syncthreads();
-    int64_t before = 0, total = 0;
+    int64_t total = 0, tiles_at = tiles_upto - tiles, units_at = units_upto - units;
 #pragma unroll
     for (int i = 0; i < kThreads / 32; i++) {
-        if (i < warp) before += warp_sums[i];
-        total += warp_sums[i];
+        if (i < warp) tiles_at += warp_tiles[i], units_at += warp_units[i];
+        total += warp_units[i];
     }
-    int64_t at = before + upto - mine;  // tiles before this thread's requests
     total *= per;
     Shares s;
     s.share = (total + gridDim.x - 1) / gridDim.x;
     if (s.share < least) s.share = least;
     s.first = min(s.share * (int64_t)blockIdx.x, total);
     s.end = min(s.first + s.share, total);
-    if (s.first < s.end && mine > 0 && s.first >= at * per && s.first < (at + mine) * per) {
+    if (s.first < s.end && units > 0 && s.first >= units_at * per && s.first < (units_at + units) * per) {
         int b = b0;
-        for (int t; b < b1 && (at + (t = tiles_of(p, length_of(p, b)))) * per <= s.first; b++) at += t;
+        for (; b < b1; b++) {
+            const int t = tiles_of(p, length_of(p, b)), u = t ? t + OVERHEAD : 0;
+            if ((units_at + u) * per > s.first) break;
+            tiles_at += t, units_at += u;
+        }
         found_request = b;
-        found_base = at;
+        found_tiles = tiles_at;
+        found_units = units_at * per;
     }
     __syncthreads();
+    w.left = 0;
     if (s.first < s.end) {
         enter(p, w, found_request);
-        w.base = found_base;
-        const int64_t in = s.first - w.base * per;
-        w.r = (int)(in / w.tiles);
-        w.j = (int)(in - (int64_t)w.r * w.tiles);
+        w.tiles_before = found_tiles;
+        const int64_t in = s.first - found_units;
+        const int cost = w.tiles + OVERHEAD;
+        w.r = (int)(in / cost);
+        const int x = (int)(in - (int64_t)w.r * cost);
+        w.j = max(0, x - OVERHEAD);
+        w.left = s.end - s.first - max(0, OVERHEAD - x);
     }
     return s;
+}
+
+// t / page_size by a multiplication: page_magic = ceil(2^62 / page_size), exact for t < 2^31
+__device__ __forceinline__ int page_of(const AttendParams& p, int t) {
+    return (int)__umul64hi((uint64_t)(uint32_t)t << 2, p.page_magic);
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
 // DP: head_dim rounded up to 64, 128 or 256.  NT: column tiles of 8 query heads.
 template <class T, class C, int DP, int NT>
 struct Shape {
-    static constexpr int kRow = DP * C::bytes;                  // bytes of a token's row in shared memory
-    static constexpr int kStage = kTile * 2 * kRow;             // K and V of a tile
-    static constexpr int kPitch = DP + 4;                       // floats; 4 more: heads fall on different banks
-    static constexpr int kMerge = 2 * 8 * NT * kPitch * 4;      // two warps' outputs
-    static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 128;     // statistics of the columns, masks of the ring, a flag
-    static constexpr int kTwo = 113 * 1024, kOne = 227 * 1024;  // shared memory of a CTA when two, or one, fit an SM
-    static constexpr int kStagesTwo = (kTwo - kMerge - kSmall) / kStage;
-    static constexpr int kStagesOne = (kOne - kMerge - kSmall) / kStage;
-    // at least three: one in use, two under way
-    static constexpr int kStages = kStagesTwo >= 3 ? (kStagesTwo > 6 ? 6 : kStagesTwo) : (kStagesOne > 6 ? 6 : kStagesOne);
+    static constexpr int kRow = DP * C::bytes;
+    static constexpr int kPitch = kRow + 16;                    // bytes of a row in shared memory: 8 rows of a column cover all banks
+    static constexpr int kStage = kTile * 2 * kPitch;           // K and V of a tile
+    static constexpr int kOutPitch = DP + 4;                    // floats; 4 more: heads fall on different banks
+    static constexpr int kMerge = 2 * 8 * NT * kOutPitch * 4;   // two warps' outputs
+    static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 512;     // statistics of the columns; barriers and masks of the rings, a flag
+    static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall) / kStage; }
+    // As many CTAs on an SM (four at most, and as registers allow) as leave each three stages, one in use and two under way;
+    // the largest tiles, one CTA on an SM, make do with two.
+    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 ? 3 : 2;
+    static constexpr int kCtas = kRegisterCtas >= 4 && stages(4) >= 3 ? 4 : kRegisterCtas >= 3 && stages(3) >= 3 ? 3 : stages(2) >= 3 ? 2 : 1;
+    static constexpr int kStages = stages(kCtas) > 6 ? 6 : stages(kCtas);
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
-    static_assert(kStages >= 3 && kBytes <= kOne, "shared memory of a CTA");
-    // 16-byte chunk c of row t lies at chunk c ^ swizzle(t): eight rows of one column cover all banks
-    static __device__ __forceinline__ int swizzle(int t) { return kRow >= 128 ? t & 7 : (t >> 1) & 3; }
+    static_assert(kStages >= 2, "shared memory of a CTA");
 };
 
 template <class T, class C, int DP, int NT>
-__global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv_attend_kernel(const AttendParams p) {
     using S = Shape<T, C, DP, NT>;
     using M = typename OperandOf<T, C>::type;
     constexpr bool kNarrow = C::bytes == 1, kRescaled = kNarrow && std::is_same<T, BF16>::value;
     constexpr bool kSplit = !kRescaled;  // f16 weights are 8 times finer than a bf16 output as they are
-    constexpr int kCols = 8 * NT, kSteps = DP / 16, kChunks = S::kRow / 16;
+    constexpr int kCols = 8 * NT, kSteps = DP / 16;
+    constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
-    float* const warp_m = merge + 2 * kCols * S::kPitch;   // [4][kCols]
+    float* const warp_m = merge + 2 * kCols * S::kOutPitch;  // [4][kCols]
     float* const warp_l = warp_m + 4 * kCols;
-    float* const col_unit = warp_l + 4 * kCols;            // [kCols]
-    int* const last_flag = reinterpret_cast<int*>(col_unit + 4 * kCols);
-    uint32_t* const masks = reinterpret_cast<uint32_t*>(last_flag + 1) + (threadIdx.x >> 5) * S::kStages;
+    float* const col_unit = warp_l + 4 * kCols;              // [kCols]
+    uint32_t* const masks = reinterpret_cast<uint32_t*>(col_unit + 4 * kCols) + (threadIdx.x >> 5) * S::kStages;
+    int* const last_flag = reinterpret_cast<int*>(col_unit + 4 * kCols) + 4 * S::kStages;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int D = p.pool.head_dim, group = p.n_heads / p.pool.n_kv;
@@ -220,62 +258,65 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
     }
 
     Place in;  // the tile whose loads are issued next
-    const Shares sh = divide(p, per, 4, in);
-    int64_t to_load = sh.end - sh.first, to_do = to_load;
-    if (to_do == 0) return;
+    const Shares sh = divide<kOverhead>(p, per, kLeast, in);
+    if (in.left <= 0) return;
     Place at = in;  // the tile that is computed next
 
-    // columns of a row beyond head_dim are never loaded: zero them once
+    // stage s of this warp: + s * kStage; 16 rows of K, then 16 of V
+    const uint32_t ring = smem_address(smem + warp * 32 * S::kPitch);
     const int chunks = D * C::bytes / 16;
-    char* const ring = smem + warp * 16 * 2 * S::kRow;  // stage s of this warp: + s * kStage; 16 rows of K, 16 of V
-    if (chunks < kChunks) {
+    if (chunks * 16 < S::kRow)  // elements beyond head_dim are never copied to: zero them once
         for (int s = 0; s < S::kStages; s++)
-            for (int i = lane; i < 32 * kChunks; i += 32) {
-                const int t = i / kChunks, c = i % kChunks;
-                if (c >= chunks)
-                    *reinterpret_cast<uint4*>(ring + s * S::kStage + t * S::kRow + ((c ^ S::swizzle(t & 15)) * 16)) =
-                        make_uint4(0, 0, 0, 0);
-            }
-        __syncwarp();
-    }
+            for (int i = chunks * 16; i < S::kRow; i += 16)
+                *reinterpret_cast<uint4*>(smem + (warp * 32 + lane) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
 
-    // ---- loads: lane i < 16 knows where token i of the warp's 16 lies; the page number is fetched one tile ahead
+    // ---- loads: a row is kLanes lanes' 16 bytes, kRows rows at once; the page numbers (of token lane % 16) are fetched
+    // one tile ahead
+    constexpr int kLanes = S::kRow / 16, kRows = 32 / kLanes;
+    const int chunk = lane % kLanes, lane_row = lane / kLanes;
+    const bool copies = chunk < chunks;
+    const int64_t v_from_k = p.pool.v - p.pool.k, slot_bytes = p.pool.stride_slot * C::bytes;
+    const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1;
-    const int my_token = warp * 16 + (lane & 15);
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * kTile + my_token;
-        page = t < in.len ? p.table[in.b * p.table_row + t / p.pool.page_size] : -1;
-    };
-    auto issue = [&](int stage) {
-        const int t = in.start + in.j * kTile + my_token;
-        const bool live = t < in.len, good = live && page >= 0 && page < p.pool.n_pages;
-        if (live && !good) flag(p.status, FCSIM_KV_BAD_PAGE);
-        const uint32_t mask = __ballot_sync(~0u, good);
-        if (lane == 0) masks[stage] = mask;  // tokens that exist, for the computation of this tile
-        int64_t offset = -1;
-        if (good)
-            offset = (page * p.pool.stride_page + (t % p.pool.page_size) * p.pool.stride_slot +
-                      (in.r / head_tiles) * p.pool.stride_head) * C::bytes;
-        const uint32_t dst = smem_address(ring + stage * S::kStage);
-#pragma unroll
-        for (int i = 0; i < 16 * kChunks / 32; i++) {
-            const int row = (i * 32 + lane) / kChunks, c = lane % kChunks;
-            const int64_t o = __shfl_sync(~0u, offset, row);
-            if (c < chunks) {
-                const uint32_t d = dst + row * S::kRow + ((c ^ S::swizzle(row)) * 16);
-                const int64_t src = o < 0 ? 0 : o + c * 16;
-                copy16(d, p.pool.k + src, o < 0 ? 0 : 16);
-                copy16(d + 16 * S::kRow, p.pool.v + src, o < 0 ? 0 : 16);
-            }
-        }
+        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15);
+        page = t < in.len ? p.table[in.b * p.table_row + page_of(p, t)] : -1;
     };
     auto load_next = [&](int stage) {
-        if (to_load > 0) {
-            issue(stage);
-            if (--to_load > 0) {
-                advance(p, in, per);
-                fetch_page();
+        if (in.left > 0) {
+            const int t0 = in.start + in.j * kTile + warp * 16, t = t0 + (lane & 15);
+            const bool live = t < in.len, good = (unsigned)page < (unsigned)p.pool.n_pages;
+            if (live && !good) flag(p.status, FCSIM_KV_BAD_PAGE);
+            const uint32_t mask = __ballot_sync(~0u, good) & 0xffff;
+            if (lane == 0) masks[stage] = mask;  // for the computation of this tile
+            const uint32_t dst = lane_dst + stage * S::kStage;
+            const int place0 = t0 - page_of(p, t0) * p.pool.page_size;
+            const int64_t head = (in.r / head_tiles) * p.pool.stride_head;
+            if (mask == 0xffff && place0 + 16 <= p.pool.page_size) {  // 16 tokens of one page: rows at equal distances
+                const char* src = p.pool.k + (page * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
+                if (copies) {
+#pragma unroll
+                    for (int i = 0; i < 16 / kRows; i++) {
+                        copy16(dst + i * kRows * S::kPitch, src);
+                        copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k);
+                        src += kRows * slot_bytes;
+                    }
+                }
+            } else if (mask) {
+                const int64_t row = (page * p.pool.stride_page + (t - page_of(p, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes;
+                const int64_t mine = good ? row : -1;
+#pragma unroll
+                for (int i = 0; i < 16 / kRows; i++) {
+                    const int64_t x = __shfl_sync(~0u, mine, i * kRows + lane_row);
+                    const char* src = p.pool.k + (x < 0 ? 0 : x + chunk * 16);
+                    if (copies) {  // rows that do not exist: zeros, for weights of zero
+                        copy16(dst + i * kRows * S::kPitch, src, x < 0 ? 0 : 16);
+                        copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k, x < 0 ? 0 : 16);
+                    }
+                }
             }
+            advance<kOverhead>(p, in, per);
+            if (in.left > 0) fetch_page();
         }
         commit();
     };
@@ -289,7 +330,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
     int stage = 0;
     const float flip = p.scale < 0 ? -1.0f : 1.0f;  // a negative scale turns the order around: turn q instead
 
-    for (int64_t done = 0; done < to_do; done++) {
+    while (at.left > 0) {
         const int kv = at.r / head_tiles, col0 = (at.r % head_tiles) * kCols, cols = min(kCols, group - col0);
         if (fresh) {
             fresh = false;
@@ -344,18 +385,20 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
         wait_group<S::kStages - 2>();
         __syncwarp();
         load_next(stage == 0 ? S::kStages - 1 : stage - 1);  // into what the last step has read
+        const bool some = masks[stage] != 0;
 
-        const uint32_t krow = smem_address(ring + stage * S::kStage), vrow = krow + 16 * S::kRow;
+        if (some) {  // (a warp may have no token of a request's last tile)
+        const uint32_t krow = ring + stage * S::kStage, vrow = krow + 16 * S::kPitch;
         // ---- s^T = K q^T: 16 tokens by 8 heads
         float s[NT][4] = {};
         {
             const int t = (lane & 7) + ((lane >> 3) & 1) * 8;
-            const uint32_t row = krow + t * S::kRow;
+            const uint32_t row = krow + t * S::kPitch + (lane >> 4) * 16;
             if constexpr (!kNarrow) {
 #pragma unroll
                 for (int k = 0; k < kSteps; k++) {
                     uint32_t a[4];
-                    load_matrices(row + (((2 * k + (lane >> 4)) ^ S::swizzle(t)) * 16), a);
+                    load_matrices(row + k * 32, a);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) mma<M>(s[nt], a, qf[nt][k][0], qf[nt][k][1]);
                 }
@@ -363,7 +406,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
 #pragma unroll
                 for (int k = 0; k < kSteps; k += 2) {
                     uint32_t w[4];
-                    load_matrices(row + (((k + (lane >> 4)) ^ S::swizzle(t)) * 16), w);
+                    load_matrices(row + k * 16, w);
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         const uint32_t a[4] = {E4M3::halves(w[2 * i] & 0xffff), E4M3::halves(w[2 * i + 1] & 0xffff),
@@ -380,8 +423,8 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
         uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-            if (p.add_weight && at.base + at.tiles <= p.logit_tiles) {
-                float* row = p.logits + (at.base * p.n_heads + (int64_t)(kv * group + col0 + nt * 8) * at.tiles) * kTile +
+            if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles) {
+                float* row = p.logits + (at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + nt * 8) * at.tiles) * kTile +
                              at.j * kTile + warp * 16 + lane / 4;
 #pragma unroll
                 for (int i = 0; i < 2; i++)
@@ -402,13 +445,13 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
                 top = fmaxf(top, m[nt][i]);
-                const float base = top == -INFINITY ? 0.0f : top, u = unit[nt][i] * 1.4426950408889634f;
-                shrink[i] = m[nt][i] == -INFINITY ? 0.0f : exp2f((m[nt][i] - base) * u);
+                const float base = top == -INFINITY ? 0.0f : top, u = unit[nt][i] * kLog2e;
+                shrink[i] = m[nt][i] == -INFINITY ? 0.0f : power2((m[nt][i] - base) * u);
                 m[nt][i] = top;
                 float sum = 0;
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    const float e = dead[k] ? 0.0f : exp2f((s[nt][2 * k + i] - base) * u);
+                    const float e = dead[k] ? 0.0f : power2((s[nt][2 * k + i] - base) * u);
                     s[nt][2 * k + i] = e;
                     sum += e;
                 }
@@ -436,11 +479,11 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
         {
             const int which = lane >> 3;
             if constexpr (!kNarrow) {
-                const int t = (lane & 7) + (which >> 1) * 8;
+                const uint32_t row = vrow + ((lane & 7) + (which >> 1) * 8) * S::kPitch + (which & 1) * 16;
 #pragma unroll
                 for (int k = 0; k < kSteps; k++) {
                     uint32_t a[4];
-                    load_matrices_transposed(vrow + t * S::kRow + (((2 * k + (which & 1)) ^ S::swizzle(t)) * 16), a);
+                    load_matrices_transposed(row + k * 32, a);
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++) {
                         mma<M>(o[k][nt], a, hi[nt][0], hi[nt][1]);
@@ -448,12 +491,12 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                     }
                 }
             } else {
-                const int t = (lane & 7) + (which & 1) * 8;
+                const uint32_t row = vrow + ((lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
 #pragma unroll
                 for (int k = 0; k < kSteps; k += 2) {
                     // a lane gets bytes 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8
                     uint32_t w[4];
-                    load_matrices_transposed(vrow + t * S::kRow + (((k + (which >> 1)) ^ S::swizzle(t)) * 16), w);
+                    load_matrices_transposed(row + k * 16, w);
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         const uint32_t x = w[2 * i], y = w[2 * i + 1];
@@ -468,11 +511,12 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                 }
             }
         }
-        stage = stage == S::kStages - 1 ? 0 : stage + 1;
+        }
+        if (++stage == S::kStages) stage = 0;
 
-        const bool complete = at.j == at.tiles - 1, ends = complete || done + 1 == to_do;
-        if (!ends) {
+        if (at.j < at.tiles - 1 && at.left > 1) {
             at.j++;
+            at.left--;
             continue;
         }
         // ---------------------------------------------------------------- end of this CTA's part of (request, head tile)
@@ -501,7 +545,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                 const int col = nt * 8 + 2 * (lane & 3) + i;
                 const float top = fmaxf(fmaxf(warp_m[col], warp_m[kCols + col]), fmaxf(warp_m[2 * kCols + col], warp_m[3 * kCols + col]));
                 const float base = top == -INFINITY ? 0.0f : top;
-                const float f = m[nt][i] == -INFINITY ? 0.0f : exp2f((m[nt][i] - base) * unit[nt][i] * 1.4426950408889634f);
+                const float f = m[nt][i] == -INFINITY ? 0.0f : power2((m[nt][i] - base) * unit[nt][i] * kLog2e);
 #pragma unroll
                 for (int k = 0; k < kSteps; k++) {
                     o[k][nt][i] *= f;
@@ -510,7 +554,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
             }
         auto element = [&](int k, int nt, int i) {  // where o[k][nt][i] lies in a merge buffer
             const int d = kNarrow ? k * 16 + 2 * (lane / 4) + (i >> 1) : k * 16 + lane / 4 + 8 * (i >> 1);
-            return (warp & 1) * kCols * S::kPitch + (nt * 8 + 2 * (lane & 3) + (i & 1)) * S::kPitch + d;
+            return (warp & 1) * kCols * S::kOutPitch + (nt * 8 + 2 * (lane & 3) + (i & 1)) * S::kOutPitch + d;
         };
         if (warp >= 2) {
 #pragma unroll
@@ -531,9 +575,11 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
         }
         __syncthreads();
 
-        // where this (request, head tile) begins and ends in the work, and which CTAs share it
-        const int64_t group_first = sh.first + done - at.j, group_end = group_first + at.tiles;
-        const int first_cta = (int)(group_first / sh.share), last_cta = (int)((group_end - 1) / sh.share);
+        // the units of this group's tiles, and the CTAs that have them
+        const int64_t group_first = sh.end - at.left - at.j, group_end = group_first + at.tiles;
+        int first_cta = blockIdx.x, last_cta = blockIdx.x;
+        if (group_first < sh.first) first_cta = (int)(group_first / sh.share);
+        if (group_end > sh.end) last_cta = (int)((group_end - 1) / sh.share);
         const int parts = last_cta - first_cta + 1;
         const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
         const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
@@ -542,24 +588,24 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
             if (p.lse) p.lse[head0 + col] = sum == 0.0f ? -INFINITY : top * u + logf(sum);
             if (p.add_weight)
                 *reinterpret_cast<float4*>(p.stats + (head0 + col) * 4) =
-                    make_float4(top == -INFINITY ? 0.0f : top, u * 1.4426950408889634f, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
+                    make_float4(top == -INFINITY ? 0.0f : top, u * kLog2e, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
         };
         constexpr int kPartSize = kCols * (DP + 2);
         float* const my_part = p.parts + (2 * (int64_t)blockIdx.x + (first_cta == (int)blockIdx.x ? 1 : 0)) * kPartSize;
         const int per_row = D / 4;
         for (int i = tid; i < cols * per_row; i += kThreads) {
             const int col = i / per_row, d = (i - col * per_row) * 4;
-            const float4 x = *reinterpret_cast<const float4*>(merge + col * S::kPitch + d);
-            const float4 y = *reinterpret_cast<const float4*>(merge + (kCols + col) * S::kPitch + d);
+            const float4 x = *reinterpret_cast<const float4*>(merge + col * S::kOutPitch + d);
+            const float4 y = *reinterpret_cast<const float4*>(merge + (kCols + col) * S::kOutPitch + d);
             const float4 z = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
             float sum = 0, top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < 4; w++) top = fmaxf(top, warp_m[w * kCols + col]);
-            const float base = top == -INFINITY ? 0.0f : top, u = col_unit[col] * 1.4426950408889634f;
+            const float base = top == -INFINITY ? 0.0f : top, u = col_unit[col] * kLog2e;
 #pragma unroll
             for (int w = 0; w < 4; w++) {
                 const float x = warp_m[w * kCols + col];  // -infinity: the sum is 0, or NaN and stays so
-                sum += warp_l[w * kCols + col] * (x == -INFINITY ? 0.0f : exp2f((x - base) * u));
+                sum += warp_l[w * kCols + col] * (x == -INFINITY ? 0.0f : power2((x - base) * u));
             }
             if (parts == 1) {
                 const float f = sum == 0.0f ? 0.0f : vscale / sum;
@@ -587,7 +633,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                 };
                 for (int i = tid; i < cols * per_row; i += kThreads) {
                     const int col = i / per_row, d = (i - col * per_row) * 4;
-                    const float u = col_unit[col] * 1.4426950408889634f;
+                    const float u = col_unit[col] * kLog2e;
                     float top = -INFINITY, sum = 0;
                     for (int k = 0; k < parts; k++) top = fmaxf(top, __ldcg(part(k) + kCols * DP + col * 2));
                     const float base = top == -INFINITY ? 0.0f : top;
@@ -596,7 +642,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
                     for (int k = 0; k < parts; k++) {
                         const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(k) + kCols * DP + col * 2));
                         const float4 x = __ldcg(reinterpret_cast<const float4*>(part(k) + col * DP + d));
-                        const float f = ml.x == -INFINITY ? 0.0f : exp2f((ml.x - base) * u);
+                        const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * u);
                         sum += f * ml.y;
                         z.x += f * x.x, z.y += f * x.y, z.z += f * x.z, z.w += f * x.w;
                     }
@@ -608,12 +654,9 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_attend_kernel(const AttendP
             }
         }
         __syncthreads();  // the merge buffers and the columns' statistics are free again
-        if (done + 1 < to_do) {
-            advance(p, at, per);
-            fresh = true;
-        }
+        advance<kOverhead>(p, at, per);
+        fresh = true;
     }
-    wait_group<0>();
 }
 
 template <class T, class C, int DP, int NT>
@@ -666,28 +709,28 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 // per token and kv head; the sum over the heads in order.
 __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendParams p) {
     Place at;
-    const Shares sh = divide(p, 1, 1, at);
+    divide<0>(p, 1, 1, at);
     const int group = p.n_heads / p.pool.n_kv;
-    for (int64_t i = sh.first; i < sh.end; i++) {
+    while (at.left > 0) {
         const int in = at.j * kTile + (threadIdx.x & (kTile - 1)), t = at.start + in;
-        if (at.base + at.tiles > p.logit_tiles) {
+        if (at.tiles_before + at.tiles > p.logit_tiles) {
             if (threadIdx.x == 0) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
         } else if (t < at.len) {
-            const int page = p.table[at.b * p.table_row + t / p.pool.page_size];
+            const int page = p.table[at.b * p.table_row + page_of(p, t)];
             if (page >= 0 && page < p.pool.n_pages) {
-                const float* row = p.logits + at.base * p.n_heads * kTile + in;
+                const float* row = p.logits + at.tiles_before * p.n_heads * kTile + in;
                 const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads;
                 for (int kv = threadIdx.x / kTile; kv < p.pool.n_kv; kv += kThreads / kTile) {
                     float sum = 0;
                     for (int h = kv * group; h < (kv + 1) * group; h++) {
                         const float4 x = stats[h];
-                        sum += exp2f((row[(int64_t)h * at.tiles * kTile] - x.x) * x.y) * x.z;
+                        sum += power2((row[(int64_t)h * at.tiles * kTile] - x.x) * x.y) * x.z;
                     }
-                    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t % p.pool.page_size] += sum;
+                    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t - page_of(p, t) * p.pool.page_size] += sum;
                 }
             }
         }
-        if (i + 1 < sh.end) advance(p, at, 1);
+        advance<0>(p, at, 1);
     }
 }
 int launch_weights(const AttendParams& p, int grid, cudaStream_t stream) {
