@@ -474,7 +474,7 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
     p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length, p->window = a->window;
     p->add_weight = a->add_weight != 0, p->scale = a->scale;
-    p->page_magic = ((1ull << 62) + c->page_size - 1) / c->page_size;
+    p->page_magic = ((1ull << 63) + c->page_size - 1) / c->page_size;
     return FCSIM_OK;
 }
 
@@ -525,6 +525,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     const int64_t tiles = (seen + kTile - 1) / kTile, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
     l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most, p.n_requests)}));
+    if ((most + (int64_t)p.n_requests * 16 * p.n_heads) / l->grid >= 0x7fffffff) return FCSIM_EINVAL;  // a CTA counts in 32 bits
     l->counters = (size_t)l->grid * 4;
     l->parts = (l->counters + 15) / 16 * 16;
     l->stats = l->parts + (size_t)2 * l->grid * v.head_cols * (v.width + 2) * 4;

@@ -98,11 +98,11 @@ struct OperandOf<T, E4M3> { using type = F16; };
 constexpr int kOverhead = 4;
 constexpr int kLeast = kOverhead + 4;  // units of a CTA at least: below that, joining costs more than it spreads
 
-// A place in the work: request b, group r of its `per`, tile j of `tiles`.
+// A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
-    int b, r, j, tiles, start, len;
+    int b, kv, ht, j, tiles, start, len;
+    int left;              // units from this tile to the end of the CTA's stretch; none: the place is beyond it
     int64_t tiles_before;  // tiles of the requests before b
-    int64_t left;          // units from this tile to the end of the CTA's stretch; none: the place is beyond it
 };
 
 __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
@@ -123,14 +123,16 @@ __device__ __forceinline__ void enter(const AttendParams& p, Place& w, int b) {
 }
 // The next tile, if the stretch has one more.
 template <int OVERHEAD>
-__device__ __forceinline__ void advance(const AttendParams& p, Place& w, int per) {
+__device__ __forceinline__ void advance(const AttendParams& p, Place& w, int n_kv, int head_tiles) {
     w.left--;
     if (++w.j < w.tiles) return;
     w.left -= OVERHEAD;
     if (w.left <= 0) return;
     w.j = 0;
-    if (++w.r < per) return;
-    w.r = 0;
+    if (++w.ht < head_tiles) return;
+    w.ht = 0;
+    if (++w.kv < n_kv) return;
+    w.kv = 0;
     w.tiles_before += w.tiles;
     do enter(p, w, w.b + 1);
     while (w.tiles == 0);
@@ -140,13 +142,14 @@ struct Shares {
     int64_t first, end, share;  // this CTA's units [first, end); a CTA's share
 };
 
-// Divides the units of all requests among the CTAs and finds where this CTA's stretch begins.  `per`: groups of a request.
+// Divides the units of all requests among the CTAs and finds where this CTA's stretch begins.  A request has n_kv times
+// head_tiles groups.  (A share has less than 2^31 units: the host refuses more.)
 template <int OVERHEAD>
-__device__ __forceinline__ Shares divide(const AttendParams& p, int per, int least, Place& w) {
+__device__ __forceinline__ Shares divide(const AttendParams& p, int n_kv, int head_tiles, int least, Place& w) {
     __shared__ int64_t warp_tiles[kThreads / 32], warp_units[kThreads / 32];
     __shared__ int64_t found_tiles, found_units;
     __shared__ int found_request;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = n_kv * head_tiles;
     const int each = (p.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, p.n_requests), b1 = min(b0 + each, p.n_requests);
     int64_t tiles = 0, units = 0;
@@ -193,17 +196,20 @@ __device__ __forceinline__ Shares divide(const AttendParams& p, int per, int lea
         w.tiles_before = found_tiles;
         const int64_t in = s.first - found_units;
         const int cost = w.tiles + OVERHEAD;
-        w.r = (int)(in / cost);
-        const int x = (int)(in - (int64_t)w.r * cost);
+        const int r = (int)(in / cost), x = (int)(in - (int64_t)r * cost);
+        w.kv = r / head_tiles;
+        w.ht = r - w.kv * head_tiles;
         w.j = max(0, x - OVERHEAD);
-        w.left = s.end - s.first - max(0, OVERHEAD - x);
+        w.left = (int)(s.end - s.first) - max(0, OVERHEAD - x);
     }
     return s;
 }
 
-// t / page_size by a multiplication: page_magic = ceil(2^62 / page_size), exact for t < 2^31
+// t / page_size by a multiplication: page_magic = ceil(2^63 / page_size), exact for t < 2^31
 __device__ __forceinline__ int page_of(const AttendParams& p, int t) {
-    return (int)__umul64hi((uint64_t)(uint32_t)t << 2, p.page_magic);
+    const uint32_t x = (uint32_t)t << 1;
+    const uint64_t low = (uint64_t)x * (uint32_t)p.page_magic;
+    return (int)(((uint64_t)x * (uint32_t)(p.page_magic >> 32) + (low >> 32)) >> 32);
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int D = p.pool.head_dim, group = p.n_heads / p.pool.n_kv;
-    const int head_tiles = (group + kCols - 1) / kCols, per = p.pool.n_kv * head_tiles;
+    const int head_tiles = (group + kCols - 1) / kCols, n_kv = p.pool.n_kv;
 
     // requests without tokens
     for (int b = blockIdx.x; b < p.n_requests; b += gridDim.x) {
@@ -258,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     }
 
     Place in;  // the tile whose loads are issued next
-    const Shares sh = divide<kOverhead>(p, per, kLeast, in);
+    const Shares sh = divide<kOverhead>(p, n_kv, head_tiles, kLeast, in);
     if (in.left <= 0) return;
     Place at = in;  // the tile that is computed next
 
@@ -277,21 +283,20 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const bool copies = chunk < chunks;
     const int64_t v_from_k = p.pool.v - p.pool.k, slot_bytes = p.pool.stride_slot * C::bytes;
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
-    int page = -1;
+    int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15);
-        page = t < in.len ? p.table[in.b * p.table_row + page_of(p, t)] : -1;
+        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15), i = page_of(p, t);
+        place = t - i * p.pool.page_size;
+        page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
     };
     auto load_next = [&](int stage) {
         if (in.left > 0) {
-            const int t0 = in.start + in.j * kTile + warp * 16, t = t0 + (lane & 15);
-            const bool live = t < in.len, good = (unsigned)page < (unsigned)p.pool.n_pages;
-            if (live && !good) flag(p.status, FCSIM_KV_BAD_PAGE);
+            const bool good = (unsigned)page < (unsigned)p.pool.n_pages;
             const uint32_t mask = __ballot_sync(~0u, good) & 0xffff;
             if (lane == 0) masks[stage] = mask;  // for the computation of this tile
             const uint32_t dst = lane_dst + stage * S::kStage;
-            const int place0 = t0 - page_of(p, t0) * p.pool.page_size;
-            const int64_t head = (in.r / head_tiles) * p.pool.stride_head;
+            const int64_t head = in.kv * p.pool.stride_head;
+            const int place0 = __shfl_sync(~0u, place, 0);
             if (mask == 0xffff && place0 + 16 <= p.pool.page_size) {  // 16 tokens of one page: rows at equal distances
                 const char* src = p.pool.k + (page * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
                 if (copies) {
@@ -302,20 +307,22 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                         src += kRows * slot_bytes;
                     }
                 }
-            } else if (mask) {
-                const int64_t row = (page * p.pool.stride_page + (t - page_of(p, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes;
-                const int64_t mine = good ? row : -1;
+            } else {
+                if (!good && in.start + in.j * kTile + warp * 16 + (lane & 15) < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
+                if (mask) {
+                    const int64_t mine = good ? (page * p.pool.stride_page + place * p.pool.stride_slot + head) * C::bytes : -1;
 #pragma unroll
-                for (int i = 0; i < 16 / kRows; i++) {
-                    const int64_t x = __shfl_sync(~0u, mine, i * kRows + lane_row);
-                    const char* src = p.pool.k + (x < 0 ? 0 : x + chunk * 16);
-                    if (copies) {  // rows that do not exist: zeros, for weights of zero
-                        copy16(dst + i * kRows * S::kPitch, src, x < 0 ? 0 : 16);
-                        copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k, x < 0 ? 0 : 16);
+                    for (int i = 0; i < 16 / kRows; i++) {
+                        const int64_t x = __shfl_sync(~0u, mine, i * kRows + lane_row);
+                        const char* src = p.pool.k + (x < 0 ? 0 : x + chunk * 16);
+                        if (copies) {  // rows that do not exist: zeros, for weights of zero
+                            copy16(dst + i * kRows * S::kPitch, src, x < 0 ? 0 : 16);
+                            copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k, x < 0 ? 0 : 16);
+                        }
                     }
                 }
             }
-            advance<kOverhead>(p, in, per);
+            advance<kOverhead>(p, in, n_kv, head_tiles);
             if (in.left > 0) fetch_page();
         }
         commit();
@@ -325,15 +332,25 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     for (int s = 0; s < S::kStages - 1; s++) load_next(s);
 
     uint32_t qf[NT][kSteps][2];  // q^T as the second operand
-    float unit[NT][2], m[NT][2], l[NT][2], o[kSteps][NT][4];
+    // per head (two a lane): the logits' unit times log2 e, the reference of the exponentials (zero until there is a finite
+    // logit), the logit from which it has to move, the sum
+    float unit[NT][2], m[NT][2], limit[NT][2], l[NT][2], o[kSteps][NT][4];
+    int col0 = 0, cols = 0;
+    float* logits = nullptr;  // of this lane's first head and first token of a tile
     bool fresh = true;
     int stage = 0;
     const float flip = p.scale < 0 ? -1.0f : 1.0f;  // a negative scale turns the order around: turn q instead
 
     while (at.left > 0) {
-        const int kv = at.r / head_tiles, col0 = (at.r % head_tiles) * kCols, cols = min(kCols, group - col0);
+        const int kv = at.kv;
         if (fresh) {
             fresh = false;
+            col0 = at.ht * kCols;
+            cols = min(kCols, group - col0);
+            logits = nullptr;
+            if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles)
+                logits = p.logits + (at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * kTile +
+                         warp * 16 + lane / 4;
             const float kscale = kNarrow ? p.pool.k_scale[kv] : 1.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
@@ -368,12 +385,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                             qf[nt][k][i] = F16::pack(f.x * up, f.y * up);
                         }
                 }
-                const float u = fabsf(p.scale) * kscale * power;
+                // (never zero: a logit of -infinity must stay without weight)
+                const float u = fmaxf(fabsf(p.scale) * kscale * power * kLog2e, 1.2e-38f);
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     unit[nt][i] = __shfl_sync(~0u, u, (2 * (lane & 3) + i) * 4);
-                    m[nt][i] = -INFINITY;
-                    l[nt][i] = 0;
+                    m[nt][i] = l[nt][i] = 0;
+                    limit[nt][i] = -INFINITY;
                 }
 #pragma unroll
                 for (int k = 0; k < kSteps; k++)
@@ -385,9 +403,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         wait_group<S::kStages - 2>();
         __syncwarp();
         load_next(stage == 0 ? S::kStages - 1 : stage - 1);  // into what the last step has read
-        const bool some = masks[stage] != 0;
+        const uint32_t mask = masks[stage];
 
-        if (some) {  // (a warp may have no token of a request's last tile)
+        if (mask) {  // (a warp may have no token of a request's last tile)
         const uint32_t krow = ring + stage * S::kStage, vrow = krow + 16 * S::kPitch;
         // ---- s^T = K q^T: 16 tokens by 8 heads
         float s[NT][4] = {};
@@ -409,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     load_matrices(row + k * 16, w);
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
-                        const uint32_t a[4] = {E4M3::halves(w[2 * i] & 0xffff), E4M3::halves(w[2 * i + 1] & 0xffff),
+                        const uint32_t a[4] = {E4M3::halves(w[2 * i]), E4M3::halves(w[2 * i + 1]),
                                                E4M3::halves(w[2 * i] >> 16), E4M3::halves(w[2 * i + 1] >> 16)};
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++) mma<M>(s[nt], a, qf[nt][k + i][0], qf[nt][k + i][1]);
@@ -418,44 +436,50 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             }
         }
         // ---- softmax: this lane holds tokens lane / 4 and + 8 of heads 2 (lane % 4) and + 1
-        const uint32_t live = masks[stage] >> (lane / 4);
-        const bool dead[2] = {!(live & 1), !(live & 0x100)};
         uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
-            if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles) {
-                float* row = p.logits + (at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + nt * 8) * at.tiles) * kTile +
-                             at.j * kTile + warp * 16 + lane / 4;
+            if (logits) {
+                float* x = logits + at.j * kTile + (int64_t)(nt * 8) * at.tiles * kTile;
 #pragma unroll
                 for (int i = 0; i < 2; i++)
                     if (nt * 8 + 2 * (lane & 3) + i < cols) {
-                        float* x = row + (int64_t)(2 * (lane & 3) + i) * at.tiles * kTile;
-                        x[0] = s[nt][i];
-                        x[8] = s[nt][2 + i];
+                        x[(int64_t)i * at.tiles * kTile] = s[nt][i];
+                        x[(int64_t)i * at.tiles * kTile + 8] = s[nt][2 + i];
                     }
             }
+            if (mask != 0xffff) {
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (dead[i >> 1]) s[nt][i] = -INFINITY;
-            float shrink[2];
+                for (int i = 0; i < 4; i++)
+                    if (!(mask >> (lane / 4 + 8 * (i >> 1)) & 1)) s[nt][i] = -INFINITY;
+            }
+            // The reference moves only when a logit is 2^8 above it: the weights stay far from f16's and fp32's ends, and the
+            // maximum over the lanes is taken a few times in a request instead of in every tile.
+            const bool over = fmaxf(s[nt][0], s[nt][2]) > limit[nt][0] || fmaxf(s[nt][1], s[nt][3]) > limit[nt][1];
+            if (__any_sync(~0u, over)) {
+                float shrink[2];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                float top = fmaxf(s[nt][i], s[nt][2 + i]);
-                top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
-                top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
-                top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-                top = fmaxf(top, m[nt][i]);
-                const float base = top == -INFINITY ? 0.0f : top, u = unit[nt][i] * kLog2e;
-                shrink[i] = m[nt][i] == -INFINITY ? 0.0f : power2((m[nt][i] - base) * u);
-                m[nt][i] = top;
-                float sum = 0;
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    const float e = dead[k] ? 0.0f : power2((s[nt][2 * k + i] - base) * u);
-                    s[nt][2 * k + i] = e;
-                    sum += e;
+                for (int i = 0; i < 2; i++) {
+                    float top = fmaxf(s[nt][i], s[nt][2 + i]);
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                    const bool first = limit[nt][i] == -INFINITY;
+                    const float now = first ? top : fmaxf(top, m[nt][i]), base = now == -INFINITY ? 0.0f : now;
+                    shrink[i] = first ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
+                    m[nt][i] = base;
+                    limit[nt][i] = now + fminf(8.0f / unit[nt][i], 1e30f);
+                    l[nt][i] *= shrink[i];
                 }
-                l[nt][i] = l[nt][i] * shrink[i] + sum;
+#pragma unroll
+                for (int k = 0; k < kSteps; k++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) o[k][nt][i] *= shrink[i & 1];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                s[nt][i] = power2((s[nt][i] - m[nt][i & 1]) * unit[nt][i & 1]);
+                l[nt][i & 1] += s[nt][i];
             }
 #pragma unroll
             for (int k = 0; k < 2; k++) {
@@ -467,12 +491,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     lo[nt][k] = transpose8x8(M::pack(a - back.x, b - back.y));
                 } else
                     hi[nt][k] = transpose8x8(M::pack(a, b));
-            }
-            if (__any_sync(~0u, shrink[0] != 1.0f || shrink[1] != 1.0f)) {
-#pragma unroll
-                for (int k = 0; k < kSteps; k++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) o[k][nt][i] *= shrink[i & 1];
             }
         }
         // ---- o^T += V^T p^T: 16 elements of head_dim by 8 heads
@@ -531,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 l[nt][i] = x;
                 if (lane < 4) {
                     const int col = nt * 8 + 2 * lane + i;
-                    warp_m[warp * kCols + col] = m[nt][i];
+                    warp_m[warp * kCols + col] = limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i];
                     warp_l[warp * kCols + col] = x;
                     if (warp == 0) col_unit[col] = unit[nt][i];
                 }
@@ -545,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 const int col = nt * 8 + 2 * (lane & 3) + i;
                 const float top = fmaxf(fmaxf(warp_m[col], warp_m[kCols + col]), fmaxf(warp_m[2 * kCols + col], warp_m[3 * kCols + col]));
                 const float base = top == -INFINITY ? 0.0f : top;
-                const float f = m[nt][i] == -INFINITY ? 0.0f : power2((m[nt][i] - base) * unit[nt][i] * kLog2e);
+                const float f = limit[nt][i] == -INFINITY ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
 #pragma unroll
                 for (int k = 0; k < kSteps; k++) {
                     o[k][nt][i] *= f;
@@ -585,10 +603,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
         auto finish = [&](int col, float top, float sum) {  // one lane per head: log-sum-exp and statistics
             const float u = col_unit[col];
-            if (p.lse) p.lse[head0 + col] = sum == 0.0f ? -INFINITY : top * u + logf(sum);
+            if (p.lse) p.lse[head0 + col] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * (u * 0.6931471805599453f) + logf(sum);
             if (p.add_weight)
                 *reinterpret_cast<float4*>(p.stats + (head0 + col) * 4) =
-                    make_float4(top == -INFINITY ? 0.0f : top, u * kLog2e, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
+                    make_float4(top == -INFINITY ? 0.0f : top, u, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
         };
         constexpr int kPartSize = kCols * (DP + 2);
         float* const my_part = p.parts + (2 * (int64_t)blockIdx.x + (first_cta == (int)blockIdx.x ? 1 : 0)) * kPartSize;
@@ -601,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             float sum = 0, top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < 4; w++) top = fmaxf(top, warp_m[w * kCols + col]);
-            const float base = top == -INFINITY ? 0.0f : top, u = col_unit[col] * kLog2e;
+            const float base = top == -INFINITY ? 0.0f : top, u = col_unit[col];
 #pragma unroll
             for (int w = 0; w < 4; w++) {
                 const float x = warp_m[w * kCols + col];  // -infinity: the sum is 0, or NaN and stays so
@@ -633,7 +651,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 };
                 for (int i = tid; i < cols * per_row; i += kThreads) {
                     const int col = i / per_row, d = (i - col * per_row) * 4;
-                    const float u = col_unit[col] * kLog2e;
+                    const float u = col_unit[col];
                     float top = -INFINITY, sum = 0;
                     for (int k = 0; k < parts; k++) top = fmaxf(top, __ldcg(part(k) + kCols * DP + col * 2));
                     const float base = top == -INFINITY ? 0.0f : top;
@@ -654,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             }
         }
         __syncthreads();  // the merge buffers and the columns' statistics are free again
-        advance<kOverhead>(p, at, per);
+        advance<kOverhead>(p, at, n_kv, head_tiles);
         fresh = true;
     }
 }
@@ -709,7 +727,7 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 // per token and kv head; the sum over the heads in order.
 __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendParams p) {
     Place at;
-    divide<0>(p, 1, 1, at);
+    divide<0>(p, 1, 1, 1, at);
     const int group = p.n_heads / p.pool.n_kv;
     while (at.left > 0) {
         const int in = at.j * kTile + (threadIdx.x & (kTile - 1)), t = at.start + in;
@@ -730,7 +748,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendP
                 }
             }
         }
-        advance<0>(p, at, 1);
+        advance<0>(p, at, 1, 1);
     }
 }
 int launch_weights(const AttendParams& p, int grid, cudaStream_t stream) {

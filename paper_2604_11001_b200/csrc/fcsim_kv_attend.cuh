@@ -19,7 +19,7 @@ struct AttendParams {
     int64_t q_row, q_head, table_row;
     int n_requests, n_heads, max_length, window, add_weight;
     float scale;
-    uint64_t page_magic;  // ceil(2^62 / page_size)
+    uint64_t page_magic;  // ceil(2^63 / page_size)
     // workspace
     int* counters;       // [grid], zero between calls
     float* parts;        // [2 * grid][heads of a tile][head_dim + 2]

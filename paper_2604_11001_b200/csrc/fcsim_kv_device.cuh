@@ -47,8 +47,9 @@ struct E4M3 {
     static constexpr int bytes = 1;
     // two stored bytes (the low half of w) as two halves, exactly
     static __device__ __forceinline__ uint32_t halves(uint32_t w) {
-        __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3);
-        return (uint32_t)h.x | ((uint32_t)h.y << 16);
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)w));
+        return h;
     }
     // round to nearest even; beyond +-448 the largest value
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
