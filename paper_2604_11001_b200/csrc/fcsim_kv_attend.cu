@@ -94,15 +94,17 @@ struct OperandOf<T, E4M3> { using type = F16; };
 // ---------------------------------------------------------------------------------------------- the walk over the work
 // The work is counted in units: a tile is one, and every (request, kv head, head tile) group counts kOverhead more for its
 // start and its end (q, the warps' merge, the output), which is what they cost beside a tile.  The units before a
-// group's first tile stand for these.
-constexpr int kOverhead = 4;
-constexpr int kLeast = kOverhead + 4;  // units of a CTA at least: below that, joining costs more than it spreads
+// group's first tile stand for these.  When there are too few tiles to keep every CTA busy for long, the groups are cut
+// into equal pieces instead and each CTA gets one: fewer starts, ends and joins one after another.
+constexpr int kOverhead = 3;
+constexpr int kPieceLeast = 4;   // tiles of a piece at least: below that, joining costs more than it spreads
+constexpr int kPieceMost = 16;   // tiles of a piece from which equal shares are better
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
     int b, kv, ht, j, tiles, start, len;
     int left;              // units from this tile to the end of the CTA's stretch; none: the place is beyond it
-    int64_t tiles_before;  // tiles of the requests before b
+    int tiles_before;      // tiles of the requests before b
 };
 
 __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
@@ -138,71 +140,121 @@ __device__ __forceinline__ void advance(const AttendParams& p, Place& w, int n_k
     while (w.tiles == 0);
 }
 
-struct Shares {
-    int64_t first, end, share;  // this CTA's units [first, end); a CTA's share
+// The division of the units [0, total) among the CTAs: CTA i has [i * share, (i + 1) * share).  It depends on the lengths
+// and the grid alone, so the same call gives the same sums in the same order.
+// With `cut`, a unit is a piece of at most `cut` tiles of one group, and a share is one unit.
+struct Division {
+    int64_t total, share;
+    int cut;
+    __device__ __forceinline__ int64_t first() const { return min(total, blockIdx.x * share); }
+    __device__ __forceinline__ int64_t end() const { return min(total, (blockIdx.x + 1) * share); }
+    template <int OVERHEAD>
+    __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles ? tiles + OVERHEAD : 0; }
+};
+// What the threads' stretches of the requests add up to before each of them.
+struct Before {
+    int tiles[kThreads], units[kThreads + 1];  // (units: of one of a request's groups)
+    int warps[2][kThreads / 32];
 };
 
-// Divides the units of all requests among the CTAs and finds where this CTA's stretch begins.  A request has n_kv times
-// head_tiles groups.  (A share has less than 2^31 units: the host refuses more.)
+// Running sums over the threads (exclusive), and the totals.
+__device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_x, int& all_y) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int upto_x = x, upto_y = y;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(~0u, upto_x, d), v = __shfl_up_sync(~0u, upto_y, d);
+        if (lane >= d) upto_x += u, upto_y += v;
+    }
+    if (lane == 31) s.warps[0][warp] = upto_x, s.warps[1][warp] = upto_y;
+    __syncthreads();
+    x = upto_x - x, y = upto_y - y;
+    all_x = all_y = 0;
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; i++) {
+        if (i < warp) x += s.warps[0][i], y += s.warps[1][i];
+        all_x += s.warps[0][i], all_y += s.warps[1][i];
+    }
+}
+
+// Adds up the tiles of all requests (less than 2^31: the host refuses more; a request has `per` groups) and divides them; `plain`: equal shares and no more.
 template <int OVERHEAD>
-__device__ __forceinline__ Shares divide(const AttendParams& p, int n_kv, int head_tiles, int least, Place& w) {
-    __shared__ int64_t warp_tiles[kThreads / 32], warp_units[kThreads / 32];
-    __shared__ int64_t found_tiles, found_units;
-    __shared__ int found_request;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, per = n_kv * head_tiles;
+__device__ __forceinline__ Division divide(const AttendParams& p, int per, bool plain, Before& before) {
+    const int tid = threadIdx.x;
     const int each = (p.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, p.n_requests), b1 = min(b0 + each, p.n_requests);
-    int64_t tiles = 0, units = 0;
+    int tiles = 0, live = 0, all_tiles, all_live;
     for (int b = b0; b < b1; b++) {
         const int t = tiles_of(p, length_of(p, b));
         tiles += t;
-        units += t ? t + OVERHEAD : 0;
+        live += t > 0;
     }
-    int64_t tiles_upto = tiles, units_upto = units;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(~0u, tiles_upto, d), y = __shfl_up_sync(~0u, units_upto, d);
-        if (lane >= d) tiles_upto += x, units_upto += y;
+    sums_before(before, tiles, live, all_tiles, all_live);
+    Division d;
+    int all_units = all_tiles + OVERHEAD * all_live, units = tiles + OVERHEAD * live;
+    d.total = (int64_t)all_units * per;
+    d.share = max((int64_t)1, (d.total + gridDim.x - 1) / gridDim.x);
+    d.cut = 0;
+    const int64_t groups = (int64_t)all_live * per, spare = gridDim.x - groups;
+    if (!plain && spare > 0 && 4 * groups <= 3 * (int64_t)gridDim.x) {
+        const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
+        if (piece <= kPieceMost) {
+            d.cut = (int)piece;
+            int none = 0, all_none;
+            units = 0;
+            for (int b = b0; b < b1; b++) units += d.units<OVERHEAD>(tiles_of(p, length_of(p, b)));
+            __syncthreads();
+            sums_before(before, units, none, all_units, all_none);
+            d.total = (int64_t)all_units * per;
+            d.share = 1;
+        }
     }
-    if (lane == 31) warp_tiles[warp] = tiles_upto, warp_units[warp] = units_upto;
+    before.tiles[tid] = tiles;
+    before.units[tid] = units;
+    if (tid == 0) before.units[kThreads] = all_units;
     __syncthreads();
-    int64_t total = 0, tiles_at = tiles_upto - tiles, units_at = units_upto - units;
-#pragma unroll
-    for (int i = 0; i < kThreads / 32; i++) {
-        if (i < warp) tiles_at += warp_tiles[i], units_at += warp_units[i];
-        total += warp_units[i];
-    }
-    total *= per;
-    Shares s;
-    s.share = (total + gridDim.x - 1) / gridDim.x;
-    if (s.share < least) s.share = least;
-    s.first = min(s.share * (int64_t)blockIdx.x, total);
-    s.end = min(s.first + s.share, total);
-    if (s.first < s.end && units > 0 && s.first >= units_at * per && s.first < (units_at + units) * per) {
-        int b = b0;
-        for (; b < b1; b++) {
-            const int t = tiles_of(p, length_of(p, b)), u = t ? t + OVERHEAD : 0;
-            if ((units_at + u) * per > s.first) break;
-            tiles_at += t, units_at += u;
+    return d;
+}
+
+// The first tile of the units [first, end), first < end.  (They are less than 2^31: the host refuses more.)
+// Pieces that are cut to fit: which of the group's `cuts` this is.
+template <int OVERHEAD>
+__device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head_tiles, const Division& d, int64_t first, int64_t end,
+                                       const Before& before, Place& w, int& cut, int& cuts) {
+    __shared__ int64_t found_units;
+    __shared__ int found_request, found_tiles;
+    const int tid = threadIdx.x, per = n_kv * head_tiles;
+    int64_t units = (int64_t)before.units[tid] * per;
+    if (first >= units && first < (int64_t)before.units[tid + 1] * per) {
+        int tiles = before.tiles[tid];
+        int b = tid * ((p.n_requests + kThreads - 1) / kThreads);
+        for (;; b++) {
+            const int t = tiles_of(p, length_of(p, b));
+            const int64_t u = (int64_t)d.units<OVERHEAD>(t) * per;
+            if (units + u > first) break;
+            tiles += t, units += u;
         }
         found_request = b;
-        found_tiles = tiles_at;
-        found_units = units_at * per;
+        found_tiles = tiles;
+        found_units = units;
     }
     __syncthreads();
-    w.left = 0;
-    if (s.first < s.end) {
-        enter(p, w, found_request);
-        w.tiles_before = found_tiles;
-        const int64_t in = s.first - found_units;
-        const int cost = w.tiles + OVERHEAD;
-        const int r = (int)(in / cost), x = (int)(in - (int64_t)r * cost);
-        w.kv = r / head_tiles;
-        w.ht = r - w.kv * head_tiles;
+    enter(p, w, found_request);
+    w.tiles_before = found_tiles;
+    const int64_t in = first - found_units;
+    const int cost = d.units<OVERHEAD>(w.tiles);
+    const int r = (int)(in / cost), x = (int)(in - (int64_t)r * cost);
+    w.kv = r / head_tiles;
+    w.ht = r - w.kv * head_tiles;
+    if (d.cut) {
+        cut = x, cuts = cost;
+        w.j = (int)((int64_t)w.tiles * x / cost);
+        w.left = (int)((int64_t)w.tiles * (x + 1) / cost) - w.j;
+    } else {
         w.j = max(0, x - OVERHEAD);
-        w.left = (int)(s.end - s.first) - max(0, OVERHEAD - x);
+        w.left = (int)(end - first) - max(0, OVERHEAD - x);
     }
-    return s;
+    __syncthreads();  // what was found may be overwritten
 }
 
 // t / page_size by a multiplication: page_magic = ceil(2^63 / page_size), exact for t < 2^31
@@ -221,19 +273,85 @@ struct Shape {
     static constexpr int kStage = kTile * 2 * kPitch;           // K and V of a tile
     static constexpr int kOutPitch = DP + 4;                    // floats; 4 more: heads fall on different banks
     static constexpr int kMerge = 2 * 8 * NT * kOutPitch * 4;   // two warps' outputs
-    static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 512;     // statistics of the columns; barriers and masks of the rings, a flag
-    static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall) / kStage; }
-    // As many CTAs on an SM (four at most, and as registers allow) as leave each three stages, one in use and two under way;
-    // the largest tiles, one CTA on an SM, make do with two.
-    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 ? 3 : 2;
-    static constexpr int kCtas = kRegisterCtas >= 4 && stages(4) >= 3 ? 4 : kRegisterCtas >= 3 && stages(3) >= 3 ? 3 : stages(2) >= 3 ? 2 : 1;
-    static constexpr int kStages = stages(kCtas) > 6 ? 6 : stages(kCtas);
+    static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 128;     // statistics of the columns, masks of the rings, a flag
+    static constexpr int kStatic = sizeof(Before) + 64;
+    static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall - kStatic) / kStage; }
+    // As many CTAs on an SM as registers and two stages each allow, then as many stages (three at most) as keep 64 KB of an SM's
+    // loads under way.  More only queue: with three stages of 32 KB instead of two, SMs differ more in the rate they get,
+    // and a call ends with the slowest (131 072 tokens of one request 99 us, with two 96; 16 KB tiles 82 us, with two 87).
+    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 && (kRow <= 128) ? 3 : 2;
+    static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(2) >= 2 ? 2 : 1;
+    static constexpr int kStages = kCtas * kStage >= 64 * 1024 || stages(kCtas) < 3 ? 2 : 3;
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
     static_assert(kStages >= 2, "shared memory of a CTA");
 };
 
+// A head's log-sum-exp and what the weights need of it: reference, unit, 1 / sum.
+__device__ __forceinline__ void finish(const AttendParams& p, int64_t head, float top, float sum, float unit) {
+    const float reference = top == -INFINITY ? 0.0f : top;
+    if (p.lse) p.lse[head] = sum == 0.0f ? -INFINITY : reference * (unit * 0.6931471805599453f) + logf(sum);
+    if (p.add_weight) *reinterpret_cast<float4*>(p.stats + head * 4) = make_float4(reference, unit, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
+}
+
+// Adds up the parts of a group in their order.  They come from L2 while the rest of the GPU keeps memory busy, so every
+// dependent load costs a microsecond or two: as many whole parts as the buffer holds are copied at once.
+// (A function of its own, so that it takes no registers from the loop over the tiles.)
+template <class T, int DP, int NT>
+__device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffer_bytes, int first_cta, int parts, int cols,
+                                  int64_t head0, float vscale, const float* col_unit) {
+    constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2), kOutputs = kCols * (DP / 4) / kThreads;
+    static_assert(kPartSize % 4 == 0 && kCols * (DP / 4) % kThreads == 0, "part layout");
+    const int room = buffer_bytes / (kPartSize * 4), per_row = p.pool.head_dim / 4;
+    const float* const at = reinterpret_cast<const float*>(buffer);
+    float4 z[kOutputs];
+    float top[kOutputs], sum[kOutputs];
+#pragma unroll
+    for (int i = 0; i < kOutputs; i++) z[i] = make_float4(0, 0, 0, 0), top[i] = -INFINITY, sum[i] = 0;
+    for (int k0 = 0; k0 < parts; k0 += room) {
+        const int n = min(room, parts - k0);
+        const uint32_t dst = smem_address(buffer);
+        for (int k = 0; k < n; k++) {
+            const float* src = p.parts + (2 * (int64_t)(first_cta + k0 + k) + (k0 + k == 0 ? 1 : 0)) * kPartSize;
+            for (int i = threadIdx.x; i < kPartSize / 4; i += kThreads) copy16(dst + (k * kPartSize + i * 4) * 4, src + i * 4);
+        }
+        commit();
+        wait_group<0>();
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kOutputs; i++) {
+            const int x = threadIdx.x + i * kThreads, col = x / per_row, d = (x - col * per_row) * 4;
+            if (col < cols) {
+                const float u = col_unit[col];
+                float now = top[i];
+                for (int k = 0; k < n; k++) now = fmaxf(now, at[k * kPartSize + kCols * DP + col * 2]);
+                const float base = now == -INFINITY ? 0.0f : now, old = top[i] == -INFINITY ? 0.0f : power2((top[i] - base) * u);
+                z[i].x *= old, z[i].y *= old, z[i].z *= old, z[i].w *= old, sum[i] *= old;  // (NaN stays)
+                for (int k = 0; k < n; k++) {
+                    const float2 ml = *reinterpret_cast<const float2*>(at + k * kPartSize + kCols * DP + col * 2);
+                    const float4 v = *reinterpret_cast<const float4*>(at + k * kPartSize + col * DP + d);
+                    const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * u);
+                    sum[i] += f * ml.y;
+                    z[i].x += f * v.x, z[i].y += f * v.y, z[i].z += f * v.z, z[i].w += f * v.w;
+                }
+                top[i] = now;
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < kOutputs; i++) {
+        const int x = threadIdx.x + i * kThreads, col = x / per_row, d = (x - col * per_row) * 4;
+        if (col < cols) {
+            const float f = sum[i] == 0.0f ? 0.0f : vscale / sum[i];
+            *reinterpret_cast<uint2*>(p.out + ((head0 + col) * p.pool.head_dim + d) * 2) =
+                sum[i] == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z[i].x * f, z[i].y * f), T::pack(z[i].z * f, z[i].w * f));
+            if (d == 0) finish(p, head0 + col, top[i], sum[i], col_unit[col]);
+        }
+    }
+}
+
 template <class T, class C, int DP, int NT>
-__global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv_attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv_attend_kernel(const __grid_constant__ AttendParams p) {
     using S = Shape<T, C, DP, NT>;
     using M = typename OperandOf<T, C>::type;
     constexpr bool kNarrow = C::bytes == 1, kRescaled = kNarrow && std::is_same<T, BF16>::value;
@@ -263,18 +381,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             for (int i = tid; i < p.n_heads; i += kThreads) p.lse[(int64_t)b * p.n_heads + i] = -INFINITY;
     }
 
-    Place in;  // the tile whose loads are issued next
-    const Shares sh = divide<kOverhead>(p, n_kv, head_tiles, kLeast, in);
-    if (in.left <= 0) return;
-    Place at = in;  // the tile that is computed next
+    __shared__ Before before;
+    const Division work = divide<kOverhead>(p, n_kv * head_tiles, false, before);
+    Place in = {};  // the tile whose loads are issued next
+    Place at = {};  // the tile that is computed next
+    int cut = 0, cuts = 1;
 
     // stage s of this warp: + s * kStage; 16 rows of K, then 16 of V
     const uint32_t ring = smem_address(smem + warp * 32 * S::kPitch);
     const int chunks = D * C::bytes / 16;
-    if (chunks * 16 < S::kRow)  // elements beyond head_dim are never copied to: zero them once
-        for (int s = 0; s < S::kStages; s++)
-            for (int i = chunks * 16; i < S::kRow; i += 16)
-                *reinterpret_cast<uint4*>(smem + (warp * 32 + lane) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
 
     // ---- loads: a row is kLanes lanes' 16 bytes, kRows rows at once; the page numbers (of token lane % 16) are fetched
     // one tile ahead
@@ -288,6 +403,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         const int t = in.start + in.j * kTile + warp * 16 + (lane & 15), i = page_of(p, t);
         place = t - i * p.pool.page_size;
         page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
+    };
+    auto fetch_queries = [&]() {  // of a group that begins soon, into L2
+        const int first = in.ht * kCols, lines = (D + 63) / 64, n = min(kCols, group - first) * lines;
+        for (int i = lane; i < n; i += 32) {
+            const char* x = p.q + ((int64_t)in.b * p.q_row + (int64_t)(in.kv * group + first + i / lines) * p.q_head + i % lines * 64) * 2;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(x));
+        }
     };
     auto load_next = [&](int stage) {
         if (in.left > 0) {
@@ -323,13 +445,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 }
             }
             advance<kOverhead>(p, in, n_kv, head_tiles);
-            if (in.left > 0) fetch_page();
+            if (in.left > 0) {
+                fetch_page();
+                if (in.j == 0 && warp == 0) fetch_queries();
+            }
         }
         commit();
     };
-    fetch_page();
-#pragma unroll
-    for (int s = 0; s < S::kStages - 1; s++) load_next(s);
 
     uint32_t qf[NT][kSteps][2];  // q^T as the second operand
     // per head (two a lane): the logits' unit times log2 e, the reference of the exponentials (zero until there is a finite
@@ -337,10 +459,25 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     float unit[NT][2], m[NT][2], limit[NT][2], l[NT][2], o[kSteps][NT][4];
     int col0 = 0, cols = 0;
     float* logits = nullptr;  // of this lane's first head and first token of a tile
-    bool fresh = true;
-    int stage = 0;
     const float flip = p.scale < 0 ? -1.0f : 1.0f;  // a negative scale turns the order around: turn q instead
 
+    const int64_t first = work.first(), end = work.end();
+    if (first >= end) return;
+    locate<kOverhead>(p, n_kv, head_tiles, work, first, end, before, in, cut, cuts);
+    at = in;
+    bool fresh = true;
+    int stage = 0;
+    auto start_ring = [&]() {
+        if (chunks * 16 < S::kRow)  // elements beyond head_dim are never copied to: zeros
+            for (int s = 0; s < S::kStages; s++)
+                for (int i = chunks * 16; i < S::kRow; i += 16)
+                    *reinterpret_cast<uint4*>(smem + (warp * 32 + lane) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
+        stage = 0;
+        fetch_page();
+#pragma unroll 1
+        for (int s = 0; s < S::kStages - 1; s++) load_next(s);
+    };
+    if (in.left > 0) start_ring();
     while (at.left > 0) {
         const int kv = at.kv;
         if (fresh) {
@@ -349,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             cols = min(kCols, group - col0);
             logits = nullptr;
             if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles)
-                logits = p.logits + (at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * kTile +
+                logits = p.logits + ((int64_t)at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * kTile +
                          warp * 16 + lane / 4;
             const float kscale = kNarrow ? p.pool.k_scale[kv] : 1.0f;
 #pragma unroll
@@ -594,21 +731,21 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         __syncthreads();
 
         // the units of this group's tiles, and the CTAs that have them
-        const int64_t group_first = sh.end - at.left - at.j, group_end = group_first + at.tiles;
+        const int64_t group_first = end - at.left - at.j, group_end = group_first + at.tiles;
         int first_cta = blockIdx.x, last_cta = blockIdx.x;
-        if (group_first < sh.first) first_cta = (int)(group_first / sh.share);
-        if (group_end > sh.end) last_cta = (int)((group_end - 1) / sh.share);
+        if (work.cut) {
+            first_cta -= cut;
+            last_cta = first_cta + cuts - 1;
+        } else {
+            if (group_first < first) first_cta = (int)(group_first / work.share);
+            if (group_end > end) last_cta = (int)((group_end - 1) / work.share);
+        }
         const int parts = last_cta - first_cta + 1;
         const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
         const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
-        auto finish = [&](int col, float top, float sum) {  // one lane per head: log-sum-exp and statistics
-            const float u = col_unit[col];
-            if (p.lse) p.lse[head0 + col] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top) * (u * 0.6931471805599453f) + logf(sum);
-            if (p.add_weight)
-                *reinterpret_cast<float4*>(p.stats + (head0 + col) * 4) =
-                    make_float4(top == -INFINITY ? 0.0f : top, u, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
-        };
         constexpr int kPartSize = kCols * (DP + 2);
+        bool restart = false;
+        // a CTA leaves at most two parts: of a group that began before it (0), and of one that goes on behind it (1)
         float* const my_part = p.parts + (2 * (int64_t)blockIdx.x + (first_cta == (int)blockIdx.x ? 1 : 0)) * kPartSize;
         const int per_row = D / 4;
         for (int i = tid; i < cols * per_row; i += kThreads) {
@@ -629,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 const float f = sum == 0.0f ? 0.0f : vscale / sum;
                 *reinterpret_cast<uint2*>(p.out + ((head0 + col) * D + d) * 2) =
                     sum == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z.x * f, z.y * f), T::pack(z.z * f, z.w * f));
-                if (d == 0) finish(col, top, sum);
+                if (d == 0) finish(p, head0 + col, top, sum, u);
             } else {
                 *reinterpret_cast<float4*>(my_part + col * DP + d) = z;
                 if (d == 0) *reinterpret_cast<float2*>(my_part + kCols * DP + col * 2) = make_float2(top, sum);
@@ -639,41 +776,27 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                const int before = atomicAdd(p.counters + first_cta, 1);
-                *last_flag = before == parts - 1;
-                if (before == parts - 1) p.counters[first_cta] = 0;
+                int* const counter = p.counters + first_cta;
+                const bool last = atomicAdd(counter, 1) == parts - 1;
+                *last_flag = last;
+                if (last) *counter = 0;
             }
             __syncthreads();
             if (*last_flag) {
                 __threadfence();
-                auto part = [&](int i) {
-                    return p.parts + (2 * (int64_t)(first_cta + i) + (i == 0 ? 1 : 0)) * kPartSize;
-                };
-                for (int i = tid; i < cols * per_row; i += kThreads) {
-                    const int col = i / per_row, d = (i - col * per_row) * 4;
-                    const float u = col_unit[col];
-                    float top = -INFINITY, sum = 0;
-                    for (int k = 0; k < parts; k++) top = fmaxf(top, __ldcg(part(k) + kCols * DP + col * 2));
-                    const float base = top == -INFINITY ? 0.0f : top;
-                    float4 z = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-                    for (int k = 0; k < parts; k++) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(k) + kCols * DP + col * 2));
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(part(k) + col * DP + d));
-                        const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * u);
-                        sum += f * ml.y;
-                        z.x += f * x.x, z.y += f * x.y, z.z += f * x.z, z.w += f * x.w;
-                    }
-                    const float f = sum == 0.0f ? 0.0f : vscale / sum;
-                    *reinterpret_cast<uint2*>(p.out + ((head0 + col) * D + d) * 2) =
-                        sum == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z.x * f, z.y * f), T::pack(z.z * f, z.w * f));
-                    if (d == 0) finish(col, top, sum);
-                }
+                wait_group<0>();  // the ring is the buffer: what it holds of the next group is loaded again
+                __syncthreads();
+                join<T, DP, NT>(p, smem, S::kStages * S::kStage, first_cta, parts, cols, head0, vscale, col_unit);
+                restart = true;
             }
         }
         __syncthreads();  // the merge buffers and the columns' statistics are free again
         advance<kOverhead>(p, at, n_kv, head_tiles);
         fresh = true;
+        if (restart && at.left > 0) {
+            in = at;
+            start_ring();
+        }
     }
 }
 
@@ -700,9 +823,11 @@ int ctas_per_sm(int device, int* out) {
 }
 template <class T, class C, int DP>
 AttendVariant of_group(int group) {
-    // more than 8 heads: two column tiles share every load from shared memory; beyond 16 the rows are read again
-    if (group <= 8) return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP};
-    return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP};
+    // more than 8 heads: two column tiles share every load; beyond 16, and for the widest rows (whose registers do not
+    // suffice: 145 us, rows read twice 126), the rows are read again
+    if constexpr (DP <= 128)
+        if (group > 8) return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP};
+    return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP};
 }
 template <class T, class C>
 AttendVariant of(int head_dim, int group) {
@@ -726,8 +851,13 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 // maximum and sum of a head are known only when all of its parts are joined.  The same division of the work, a thread
 // per token and kv head; the sum over the heads in order.
 __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendParams p) {
-    Place at;
-    divide<0>(p, 1, 1, 1, at);
+    __shared__ Before before;
+    const Division work = divide<0>(p, 1, true, before);
+    const int64_t first = work.first(), end = work.end();
+    if (first >= end) return;
+    Place at = {};
+    int cut, cuts;
+    locate<0>(p, 1, 1, work, first, end, before, at, cut, cuts);
     const int group = p.n_heads / p.pool.n_kv;
     while (at.left > 0) {
         const int in = at.j * kTile + (threadIdx.x & (kTile - 1)), t = at.start + in;
@@ -736,7 +866,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendP
         } else if (t < at.len) {
             const int page = p.table[at.b * p.table_row + page_of(p, t)];
             if (page >= 0 && page < p.pool.n_pages) {
-                const float* row = p.logits + at.tiles_before * p.n_heads * kTile + in;
+                const float* row = p.logits + (int64_t)at.tiles_before * p.n_heads * kTile + in;
                 const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads;
                 for (int kv = threadIdx.x / kTile; kv < p.pool.n_kv; kv += kThreads / kTile) {
                     float sum = 0;

@@ -21,8 +21,8 @@ struct AttendParams {
     float scale;
     uint64_t page_magic;  // ceil(2^63 / page_size)
     // workspace
-    int* counters;       // [grid], zero between calls
-    float* parts;        // [2 * grid][heads of a tile][head_dim + 2]
+    int* counters;       // [grid], zero between calls: the parts that are done of the group that begins in a CTA
+    float* parts;        // [grid][2][heads of a tile][head_dim + 2]
     float* stats;        // add_weight: [n_requests][n_heads][4]: largest logit, its unit, 1 / sum, -
     float* logits;       // add_weight: per request [n_heads][tiles * kTile]
     int64_t logit_tiles; // what `logits` has room for, in tiles
