@@ -38,74 +38,68 @@ struct AppendParams {
     int32_t* status;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;
     int n_tokens, n_heads, rope_dim, n_positions, interleaved;
-    float eps;
+    float eps, one_over_dim;
 };
 
 // Lanes with work from which a group takes four heads instead of one.
 constexpr int64_t kAppendMany = 1 << 20;
 
-// 16 bytes of a lane as 8 elements.
+// 8 bytes as 4 elements and back.
 template <class T>
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
-    const float2 a = T::unpack(w.x), b = T::unpack(w.y), c = T::unpack(w.z), d = T::unpack(w.w);
-    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
+__device__ __forceinline__ void unpack4(const uint2& w, float* x) {
+    const float2 a = T::unpack(w.x), b = T::unpack(w.y);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+}
+template <class T>
+__device__ __forceinline__ void store4(char* p, const float* x) {
+    if constexpr (T::bytes == 2) *reinterpret_cast<uint2*>(p) = make_uint2(T::pack(x[0], x[1]), T::pack(x[2], x[3]));
+    else *reinterpret_cast<uint32_t*>(p) = T::pack(x[0], x[1]) | (T::pack(x[2], x[3]) << 16);
 }
 
-// A group of LPR lanes takes HPG heads of one token, 8 elements a lane; a CTA takes the same heads of 256 / LPR tokens, so
-// that all its branches on the kind of head are uniform.  The heads' loads are issued together, and the token's
-// cosines and sines are read once for all of them (they are twice a row's bytes).  Bound by the bytes of q, k and v
-// when there are many tokens, by latency when there are few.
+// A group of LPR lanes takes HPG heads of one token; a CTA takes the same heads of 256 / LPR tokens, so that all its
+// branches on the kind of head are uniform, and the CTAs of a token's other heads are its neighbours.  A lane holds 8
+// elements of a head, as two runs of 4 that are a rotation's pairs (i .. i + 3 and i + rope_dim / 2 ..): turning them
+// needs no other lane, and half as many cosines and sines as elements, read once for all of the group's heads.  The
+// heads' loads are issued together.  Bound by the bytes of q, k and v when there are many tokens, by latency when few.
 template <class T, class C, int LPR, int HPG>
 __global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams p) {
-    const int heads = p.n_heads + 2 * p.pool.n_kv, D = p.pool.head_dim, first = blockIdx.y * HPG;
+    const int heads = p.n_heads + 2 * p.pool.n_kv, D = p.pool.head_dim, chunks = (heads + HPG - 1) / HPG;
+    const int block = blockIdx.x / chunks, first = (blockIdx.x - block * chunks) * HPG;
     const int lane = threadIdx.x & (LPR - 1);
-    const int at = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const int at = block * (256 / LPR) + threadIdx.x / LPR;
     const bool there = at < p.n_tokens, mine = there && lane * 8 < D;
     const int64_t token = there ? at : 0;
-    uint4 raw[HPG];
+    const int half = p.rope_dim / 2;
+    const bool halves = p.rope != nullptr && !p.interleaved, pairs = halves && lane * 4 < half;
+    const int lo = pairs ? lane * 4 : lane * 8, hi = pairs ? half + lane * 4 : lo + 4;
+    uint2 raw[HPG][2];
 #pragma unroll
     for (int i = 0; i < HPG; i++) {
         const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
+        raw[i][0] = raw[i][1] = make_uint2(0, 0);
         if (mine && j < heads) {
             const char* src = k < 0 ? p.q + (token * p.q_row + j * p.q_head) * 2
                             : v < 0 ? p.k + (token * p.k_row + k * p.k_head) * 2
                                     : p.v + (token * p.v_row + v * p.v_head) * 2;
-            raw[i] = *reinterpret_cast<const uint4*>(src + lane * 16);
-        } else
-            raw[i] = make_uint4(0, 0, 0, 0);
+            raw[i][0] = *reinterpret_cast<const uint2*>(src + lo * 2);
+            raw[i][1] = *reinterpret_cast<const uint2*>(src + hi * 2);
+        }
     }
-    // the token's rotation: 8 cosines and sines a lane, or 4 of pairs that are neighbours
-    bool good = true, turned = false;
-    float cosine[8], sine[8];
-    const bool any_turned = p.rope != nullptr && first < p.n_heads + p.pool.n_kv;
-    const bool lower = lane * 16 < p.rope_dim;  // this lane's half of the pairs
+    // the token's rotation
+    bool good = true;
+    float cosine[4] = {1, 1, 1, 1}, sine[4] = {0, 0, 0, 0};
     if (p.rope != nullptr) {
         const int position = p.positions[token];
         good = position >= 0 && position < p.n_positions;
         if (!good && there && lane == 0 && first == 0) flag(p.status, FCSIM_KV_BAD_POSITION);
-        turned = lane * 8 < p.rope_dim;
-        if (any_turned && turned) {
-            const int half = p.rope_dim / 2;
-            const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim;
-            if (p.interleaved) {
+        const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim + lane * 4;
+        if (pairs) {
+            *reinterpret_cast<float4*>(cosine) = *reinterpret_cast<const float4*>(row);
+            *reinterpret_cast<float4*>(sine) = *reinterpret_cast<const float4*>(row + half);
+        } else if (p.interleaved) {
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const bool in = lane * 8 + 2 * i < p.rope_dim;
-                    cosine[i] = in ? row[lane * 4 + i] : 1.0f;
-                    sine[i] = in ? row[half + lane * 4 + i] : 0.0f;
-                }
-            } else {
-                row += lower ? lane * 8 : lane * 8 - half;
-#pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    *reinterpret_cast<float4*>(cosine + i) = *reinterpret_cast<const float4*>(row + i);
-                    *reinterpret_cast<float4*>(sine + i) = *reinterpret_cast<const float4*>(row + half + i);
-                }
-                if (lower) {
-#pragma unroll
-                    for (int i = 0; i < 8; i++) sine[i] = -sine[i];
-                }
-            }
+            for (int i = 0; i < 4; i++)
+                if (lane * 4 + i < half) cosine[i] = row[i], sine[i] = row[half + i];
         }
     }
     // the token's place in the cache
@@ -116,53 +110,50 @@ __global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams
         if (slot >= (int64_t)p.pool.n_pages * p.pool.page_size) {
             if (lane == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
         } else if (slot >= 0) {
-            page = (int)((uint32_t)slot / (uint32_t)p.pool.page_size);
-            in_page = (int)((uint32_t)slot - (uint32_t)page * (uint32_t)p.pool.page_size);
+            page = page_of(p.pool, (int)slot);
+            in_page = (int)slot - page * p.pool.page_size;
             place = page * p.pool.stride_page + in_page * p.pool.stride_slot;
         }
     }
+    float weight[8];  // of the norm
 #pragma unroll
     for (int i = 0; i < HPG; i++) {
         const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
         if (j >= heads) break;
         float x[8];
-        unpack8<T>(raw[i], x);
         if (v < 0) {
             const char* w = k < 0 ? p.q_norm : p.k_norm;
+            unpack4<T>(raw[i][0], x);
+            unpack4<T>(raw[i][1], x + 4);
             if (w) {
-                float sum = 0, y[8];
+                if ((i == 0 || k == 0) && mine) {
+                    unpack4<T>(*reinterpret_cast<const uint2*>(w + lo * 2), weight);
+                    unpack4<T>(*reinterpret_cast<const uint2*>(w + hi * 2), weight + 4);
+                }
+                float sum = 0;
 #pragma unroll
                 for (int e = 0; e < 8; e++) sum += x[e] * x[e];
 #pragma unroll
                 for (int m = LPR / 2; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
-                if (mine) {
-                    unpack8<T>(*reinterpret_cast<const uint4*>(w + lane * 16), y);
-                    const float r = 1.0f / sqrtf(sum / (float)D + p.eps);
+                const float r = rsqrtf(sum * p.one_over_dim + p.eps);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) x[e] = x[e] * r * y[e];
-                }
+                for (int e = 0; e < 8; e++) x[e] = x[e] * r * weight[e];
             }
-            if (p.rope != nullptr) {
-                if (p.interleaved) {
-                    if (turned) {
+            if (pairs) {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const float a = x[2 * e], b = x[2 * e + 1];
-                            if (lane * 8 + 2 * e < p.rope_dim) {
-                                x[2 * e] = a * cosine[e] - b * sine[e];
-                                x[2 * e + 1] = b * cosine[e] + a * sine[e];
-                            }
-                        }
-                    }
-                } else {
-                    // the other element of a pair sits rope_dim / 16 lanes away, at the same place
-                    const int other = (lower ? lane + p.rope_dim / 16 : lane - p.rope_dim / 16) & (LPR - 1);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        const float mate = __shfl_sync(~0u, x[e], other, LPR);
-                        if (turned) x[e] = x[e] * cosine[e] + mate * sine[e];
-                    }
+                for (int e = 0; e < 4; e++) {
+                    const float a = x[e], b = x[e + 4];
+                    x[e] = a * cosine[e] - b * sine[e];
+                    x[e + 4] = b * cosine[e] + a * sine[e];
                 }
+            } else if (p.interleaved) {
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (lane * 4 + e < half) {
+                        const float a = x[2 * e], b = x[2 * e + 1];
+                        x[2 * e] = a * cosine[e] - b * sine[e];
+                        x[2 * e + 1] = b * cosine[e] + a * sine[e];
+                    }
             }
         }
         if (k < 0) {
@@ -170,17 +161,36 @@ __global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams
 #pragma unroll
                 for (int e = 0; e < 8; e++) x[e] = 0;
             }
-            if (mine) store8<T>(p.q_out + ((token * p.n_heads + j) * D + lane * 8) * 2, x);
+            if (mine) {
+                char* dst = p.q_out + (token * p.n_heads + j) * D * 2;
+                store4<T>(dst + lo * 2, x);
+                store4<T>(dst + hi * 2, x + 4);
+            }
             continue;
         }
         if (place < 0) continue;
         const int h = v < 0 ? k : v;
+        char* dst = (v < 0 ? p.pool.k : p.pool.v) + (place + h * p.pool.stride_head) * C::bytes;
+        if (C::bytes == 2 && v >= 0) {  // as it came
+            if (mine) {
+                *reinterpret_cast<uint2*>(dst + lo * 2) = raw[i][0];
+                *reinterpret_cast<uint2*>(dst + hi * 2) = raw[i][1];
+            }
+            continue;
+        }
         if (C::bytes == 1) {
+            if (v >= 0) {
+                unpack4<T>(raw[i][0], x);
+                unpack4<T>(raw[i][1], x + 4);
+            }
             const float s = 1.0f / (v < 0 ? p.pool.k_scale[h] : p.pool.v_scale[h]);
 #pragma unroll
             for (int e = 0; e < 8; e++) x[e] *= s;
         }
-        if (mine) store8<C>((v < 0 ? p.pool.k : p.pool.v) + (place + h * p.pool.stride_head + lane * 8) * C::bytes, x);
+        if (mine) {
+            store4<C>(dst + lo * C::bytes, x);
+            store4<C>(dst + hi * C::bytes, x + 4);
+        }
         if (v < 0 && lane == 0 && p.pool.weight)
             p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + in_page] = 0.0f;
     }
@@ -188,9 +198,10 @@ __global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams
 
 template <class T, class C, int LPR, int HPG>
 int launch_append_as(const AppendParams& p, cudaStream_t stream) {
-    const int heads = p.n_heads + 2 * p.pool.n_kv, tokens = 256 / LPR;
-    const dim3 grid((p.n_tokens + tokens - 1) / tokens, (heads + HPG - 1) / HPG);
-    fcsim_kv_append_kernel<T, C, LPR, HPG><<<grid, 256, 0, stream>>>(p);
+    const int64_t heads = p.n_heads + 2 * p.pool.n_kv, tokens = 256 / LPR;
+    const int64_t blocks = (p.n_tokens + tokens - 1) / tokens * ((heads + HPG - 1) / HPG);
+    if (blocks > 0x7fffffff) return FCSIM_EINVAL;
+    fcsim_kv_append_kernel<T, C, LPR, HPG><<<(unsigned)blocks, 256, 0, stream>>>(p);
     return launched();
 }
 template <class T, class C, int LPR>
@@ -224,16 +235,16 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int r, int max_
     return n;
 }
 
-// A weight as an unsigned key of the same order: NaN lowest, -0 as 0.
+// A weight as an unsigned key of the same order: NaN lowest, -0 as 0.  No weight has key 0.
 __device__ __forceinline__ uint32_t order_key(float w) {
-    if (w != w) return 0;
+    if (w != w) return 1;
     const uint32_t b = __float_as_uint(w + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
 constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kMaxCluster = 8;            // CTAs that share a row: the portable size of a cluster
-constexpr int kMaxKeys = 48 * 1024;       // keys a CTA keeps in shared memory (192 KB)
+constexpr int kMaxFours = 12 * 1024;      // fours of keys a CTA keeps in shared memory (192 KB)
 
 // What request r keeps: `keep` tokens, of which [0, lo) and [hi, n) are sure and `places` go to the largest of [lo, hi).
 struct Cut {
@@ -260,13 +271,14 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* stat
 // keeps their keys in shared memory, so that the weights are read once; four counts by 8 bits each, from the top, give
 // the smallest key that is kept and how many of its equals are.  The counts of the CTAs meet over distributed shared
 // memory, one cluster barrier for each (every count has a buffer of its own).  Places then follow from running sums in
-// the order of the tokens.  Bound by the latency of these few passes: a slice is 16 to 32 KB.
+// the order of the tokens.  A thread holds four neighbouring tokens at a time: they share a page where its size allows,
+// and a sum over a warp covers 128 of them.  Bound by the latency of these few passes: a slice is 16 to 32 KB.
 __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const EvictParams p, const int capacity) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    extern __shared__ uint32_t keys[];
+    extern __shared__ uint4 keys[];
     __shared__ uint32_t counts[4][256], sums[256];
-    __shared__ int warp_above[kSelectWarps], warp_equal[kSelectWarps], mine[2], chosen[2];
+    __shared__ int warp_sums[kSelectWarps], warp_equals[kSelectWarps], mine, mine_equal, chosen[2];
     const int r = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x, ctas = gridDim.x;
     const Cut c = cut_of(p, r, h == 0 && rank == 0 && tid == 0 ? p.status : nullptr);
@@ -279,39 +291,67 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
     if (h == 0 && rank == 0 && tid == 0) p.new_lengths[r] = c.keep;
     if (c.places == 0) return;  // the same for the whole cluster
 
-    const int all = c.hi - c.lo, each = (all + ctas - 1) / ctas;
-    const int begin = min(all, rank * each), count = min(all, begin + each) - begin;
+    // tokens by fours; key 0 for those of the first and last four that are no candidates
+    const int four0 = c.lo / 4, fours = (c.hi + 3) / 4 - four0, each = (fours + ctas - 1) / ctas;
+    const int begin = four0 + min(fours, rank * each), count = four0 + min(fours, (rank + 1) * each) - begin;
     const bool resident = each <= capacity;
-    auto weight_key = [&](int i) {
-        const int t = c.lo + begin + i;
-        const int page = p.table[r * p.table_row + t / p.pool.page_size];
-        if (page < 0 || page >= p.pool.n_pages) {
+    const float* const weights = p.pool.weight + (int64_t)h * p.pool.page_size;
+    const int64_t page_weights = (int64_t)p.pool.n_kv * p.pool.page_size;
+    const int32_t* const table = p.table + r * p.table_row;
+    auto token_key = [&](int t, int page, float w) {
+        if (t < c.lo || t >= c.hi) return 0u;
+        if ((unsigned)page >= (unsigned)p.pool.n_pages) {
             flag(p.status, FCSIM_KV_BAD_PAGE);
-            return 0u;
+            return 1u;
         }
-        return order_key(p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + t % p.pool.page_size]);
+        return order_key(w);
     };
-    auto key = [&](int i) { return resident ? keys[i] : weight_key(i); };
+    auto read_keys = [&](int i) {
+        const int t = (begin + i) * 4;
+        uint4 k;
+        if (p.pool.page_size % 4 == 0) {  // one page, 16 aligned bytes
+            const int index = page_of(p.pool, t), page = table[index];
+            float4 w = make_float4(0, 0, 0, 0);
+            if ((unsigned)page < (unsigned)p.pool.n_pages)
+                w = *reinterpret_cast<const float4*>(weights + page * page_weights + t - index * p.pool.page_size);
+            k = make_uint4(token_key(t, page, w.x), token_key(t + 1, page, w.y), token_key(t + 2, page, w.z), token_key(t + 3, page, w.w));
+        } else {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                int page = 0;
+                float w = 0;
+                if (t + e >= c.lo && t + e < c.hi) {
+                    const int index = page_of(p.pool, t + e);
+                    page = table[index];
+                    if ((unsigned)page < (unsigned)p.pool.n_pages) w = weights[page * page_weights + t + e - index * p.pool.page_size];
+                }
+                x[e] = token_key(t + e, page, w);
+            }
+            k = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        return k;
+    };
+    auto key = [&](int i) { return resident ? keys[i] : read_keys(i); };
     for (int i = tid; i < 4 * 256; i += kSelectThreads) counts[0][i] = 0;
     __syncthreads();
     uint32_t threshold = 0;
     int need = c.places;  // how many of the keys with the digits found so far are kept
-#pragma unroll
+#pragma unroll 1
     for (int pass = 0; pass < 4; pass++) {
         const int shift = 24 - 8 * pass;
-        if (pass == 0) {
 #pragma unroll 4
-            for (int i = tid; i < count; i += kSelectThreads) {
-                const uint32_t k = weight_key(i);
+        for (int i = tid; i < count; i += kSelectThreads) {
+            uint4 k;
+            if (pass == 0) {
+                k = read_keys(i);
                 if (resident) keys[i] = k;
-                atomicAdd(&counts[0][k >> 24], 1u);
-            }
-        } else {
-#pragma unroll 4
-            for (int i = tid; i < count; i += kSelectThreads) {
-                const uint32_t k = key(i);
-                if ((k ^ threshold) >> (shift + 8) == 0) atomicAdd(&counts[pass][(k >> shift) & 255], 1u);
-            }
+            } else
+                k = key(i);
+            auto add = [&](uint32_t x) {
+                if (pass == 0 || (x ^ threshold) >> (shift + 8) == 0) atomicAdd(&counts[pass][(x >> shift) & 255], 1u);
+            };
+            add(k.x), add(k.y), add(k.z), add(k.w);
         }
         cluster.sync();
         if (tid < 256) {
@@ -348,38 +388,48 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
     const int from = min(count, warp * run), to = min(count, from + run);
     int above = 0, equal = 0;
     for (int i = from + lane; i < to; i += 32) {
-        const uint32_t k = key(i);
-        above += k > threshold;
-        equal += k == threshold;
+        const uint4 k = key(i);
+        above += (k.x > threshold) + (k.y > threshold) + (k.z > threshold) + (k.w > threshold);
+        equal += (k.x == threshold) + (k.y == threshold) + (k.z == threshold) + (k.w == threshold);
     }
     above = __reduce_add_sync(~0u, above);
     equal = __reduce_add_sync(~0u, equal);
-    if (lane == 0) warp_above[warp] = above, warp_equal[warp] = equal;
+    if (lane == 0) warp_sums[warp] = above, warp_equals[warp] = equal;
     __syncthreads();
     if (tid == 0) {
         int a = 0, e = 0;
         for (int w = 0; w < kSelectWarps; w++) {
-            const int x = warp_above[w], y = warp_equal[w];
-            warp_above[w] = a, warp_equal[w] = e;
+            const int x = warp_sums[w], y = warp_equals[w];
+            warp_sums[w] = a, warp_equals[w] = e;
             a += x, e += y;
         }
-        mine[0] = a, mine[1] = e;
+        mine = a, mine_equal = e;
     }
     cluster.sync();
-    above = warp_above[warp], equal = warp_equal[warp];
-    for (int i = 0; i < rank; i++) {
-        const int* other = cluster.map_shared_rank(mine, i);
-        above += other[0], equal += other[1];
-    }
-    const uint32_t earlier = (1u << lane) - 1;
+    above = warp_sums[warp], equal = warp_equals[warp];
+    for (int i = 0; i < rank; i++) above += *cluster.map_shared_rank(&mine, i), equal += *cluster.map_shared_rank(&mine_equal, i);
     for (int i0 = from; i0 < to; i0 += 32) {
         const int i = i0 + lane;
-        const uint32_t k = i < to ? key(i) : 0;
-        const bool a = i < to && k > threshold, e = i < to && k == threshold;
-        const uint32_t as = __ballot_sync(~0u, a), es = __ballot_sync(~0u, e);
-        const int equals = equal + __popc(es & earlier);
-        if (a || (e && equals < need)) kept[c.lo + above + __popc(as & earlier) + min(equals, need)] = c.lo + begin + i;
-        above += __popc(as), equal += __popc(es);
+        const uint4 k = i < to ? key(i) : make_uint4(0, 0, 0, 0);
+        const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+        uint32_t own = 0;  // above, and equal in the upper half
+#pragma unroll
+        for (int e = 0; e < 4; e++) own += (x[e] > threshold) + ((uint32_t)(x[e] == threshold) << 16);
+        uint32_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t y = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += y;
+        }
+        int a = above + (int)((upto - own) & 0xffff), q = equal + (int)((upto - own) >> 16);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const bool over = x[e] > threshold, same = x[e] == threshold;
+            if (over || (same && q < need)) kept[c.lo + a + min(q, need)] = (begin + i) * 4 + e;
+            a += over, q += same;
+        }
+        const uint32_t all = __shfl_sync(~0u, upto, 31);
+        above += (int)(all & 0xffff), equal += (int)(all >> 16);
     }
     cluster.sync();  // the others may still read this CTA's counts
 }
@@ -401,20 +451,21 @@ __global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p)
         dst[i] = -1;
         if (row >= c.keep) continue;
         const int t = kept[row];
-        const int page = p.table[r * p.table_row + t / size], to = p.new_table[r * p.new_row + row / size];
+        const int from = page_of(p.pool, t), into = page_of(p.pool, row);
+        const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
         if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
             flag(p.status, FCSIM_KV_BAD_PAGE);
             continue;
         }
         if (lane < chunks) {
-            const int64_t src = (page * p.pool.stride_page + (t % size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            dst[i] = (to * p.pool.stride_page + (row % size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            dst[i] = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
             k[i] = *reinterpret_cast<const uint4*>(p.pool.k + src);
             v[i] = *reinterpret_cast<const uint4*>(p.pool.v + src);
         }
         if (lane == 0)
-            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row % size] =
-                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t % size];
+            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
+                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
     }
 #pragma unroll
     for (int i = 0; i < kRows; i++)
@@ -443,10 +494,11 @@ int check_cache(const fcsim_kv_cache* c, Pool* pool) {
     if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim * bytes % 16) return FCSIM_EINVAL;
     if (!good_stride(c->stride_page, bytes) || !good_stride(c->stride_slot, bytes) || !good_stride(c->stride_head, bytes))
         return FCSIM_EINVAL;
-    if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v) || ((uintptr_t)c->weight & 3)) return FCSIM_ESIZE;
+    if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v) || !aligned16(c->weight)) return FCSIM_ESIZE;
     if (bytes == 1 ? !c->k_scale || !c->v_scale : c->k_scale || c->v_scale) return FCSIM_EINVAL;
     *pool = Pool{(char*)c->k, (char*)c->v, c->weight, c->k_scale, c->v_scale, c->stride_page, c->stride_slot,
-                 c->stride_head, c->n_pages, c->page_size, c->n_kv_heads, c->head_dim};
+                 c->stride_head, c->n_pages, c->page_size, c->n_kv_heads, c->head_dim,
+                 ((1ull << 63) + c->page_size - 1) / c->page_size};
     return FCSIM_OK;
 }
 
@@ -474,7 +526,6 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
     p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length, p->window = a->window;
     p->add_weight = a->add_weight != 0, p->scale = a->scale;
-    p->page_magic = ((1ull << 63) + c->page_size - 1) / c->page_size;
     return FCSIM_OK;
 }
 
@@ -583,7 +634,8 @@ extern "C" int fcsim_kv_append(const fcsim_kv_cache* c, const fcsim_kv_append_ar
     p.positions = a->positions, p.slots = a->slots, p.status = a->status;
     p.q_row = a->q_row, p.q_head = a->q_head, p.k_row = a->k_row, p.k_head = a->k_head, p.v_row = a->v_row, p.v_head = a->v_head;
     p.n_tokens = a->n_tokens, p.n_heads = a->n_heads, p.rope_dim = a->rope ? a->rope_dim : 0;
-    p.n_positions = a->n_positions, p.interleaved = a->interleaved != 0, p.eps = a->eps;
+    p.n_positions = a->n_positions, p.interleaved = a->rope && a->interleaved, p.eps = a->eps;
+    p.one_over_dim = 1.0f / (float)c->head_dim;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     if (c->dtype == FCSIM_KV_E4M3)
         return a->dtype == FCSIM_KV_F16 ? launch_append<F16, E4M3>(p, stream) : launch_append<BF16, E4M3>(p, stream);
@@ -645,18 +697,19 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     int ctas = 1;
     while (ctas < kMaxCluster && (int64_t)a->n_requests * p.pool.n_kv * ctas < sms && p.max_length / ctas > 2 * kSelectThreads) ctas *= 2;
     // (and so that the keys fit, whatever the number of rows)
-    while (ctas < kMaxCluster && (p.max_length + ctas - 1) / ctas > kMaxKeys) ctas *= 2;
-    const int capacity = std::min((p.max_length + ctas - 1) / ctas, kMaxKeys);
+    const int fours = p.max_length / 4 + 2;
+    while (ctas < kMaxCluster && (fours + ctas - 1) / ctas > kMaxFours) ctas *= 2;
+    const int capacity = std::min((fours + ctas - 1) / ctas, kMaxFours);
     static std::atomic<bool> raised[kMaxDevices];
     if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxKeys * 4);
+        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxFours * 16);
         if (e != cudaSuccess) return cuda_status(e);
         if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
     }
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(ctas, p.pool.n_kv, a->n_requests);
     config.blockDim = dim3(kSelectThreads);
-    config.dynamicSmemBytes = (size_t)capacity * 4;
+    config.dynamicSmemBytes = (size_t)capacity * 16;
     config.stream = stream;
     cudaLaunchAttribute cluster;
     cluster.id = cudaLaunchAttributeClusterDimension;

@@ -257,13 +257,6 @@ __device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head
     __syncthreads();  // what was found may be overwritten
 }
 
-// t / page_size by a multiplication: page_magic = ceil(2^63 / page_size), exact for t < 2^31
-__device__ __forceinline__ int page_of(const AttendParams& p, int t) {
-    const uint32_t x = (uint32_t)t << 1;
-    const uint64_t low = (uint64_t)x * (uint32_t)p.page_magic;
-    return (int)(((uint64_t)x * (uint32_t)(p.page_magic >> 32) + (low >> 32)) >> 32);
-}
-
 // ---------------------------------------------------------------------------------------------- the kernel
 // DP: head_dim rounded up to 64, 128 or 256.  NT: column tiles of 8 query heads.
 template <class T, class C, int DP, int NT>
@@ -400,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15), i = page_of(p, t);
+        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15), i = page_of(p.pool, t);
         place = t - i * p.pool.page_size;
         page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
     };
@@ -864,7 +857,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendP
         if (at.tiles_before + at.tiles > p.logit_tiles) {
             if (threadIdx.x == 0) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
         } else if (t < at.len) {
-            const int page = p.table[at.b * p.table_row + page_of(p, t)];
+            const int page = p.table[at.b * p.table_row + page_of(p.pool, t)];
             if (page >= 0 && page < p.pool.n_pages) {
                 const float* row = p.logits + (int64_t)at.tiles_before * p.n_heads * kTile + in;
                 const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads;
@@ -874,7 +867,7 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendP
                         const float4 x = stats[h];
                         sum += power2((row[(int64_t)h * at.tiles * kTile] - x.x) * x.y) * x.z;
                     }
-                    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t - page_of(p, t) * p.pool.page_size] += sum;
+                    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t - page_of(p.pool, t) * p.pool.page_size] += sum;
                 }
             }
         }

@@ -19,7 +19,6 @@ struct AttendParams {
     int64_t q_row, q_head, table_row;
     int n_requests, n_heads, max_length, window, add_weight;
     float scale;
-    uint64_t page_magic;  // ceil(2^63 / page_size)
     // workspace
     int* counters;       // [grid], zero between calls: the parts that are done of the group that begins in a CTA
     float* parts;        // [grid][2][heads of a tile][head_dim + 2]

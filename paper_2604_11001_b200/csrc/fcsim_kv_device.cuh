@@ -16,7 +16,15 @@ struct Pool {
     const float *k_scale, *v_scale;
     int64_t stride_page, stride_slot, stride_head;  // elements
     int n_pages, page_size, n_kv, head_dim;
+    uint64_t page_magic;  // ceil(2^63 / page_size)
 };
+
+// t / page_size by a multiplication, exact for t < 2^31.
+__device__ __forceinline__ int page_of(const Pool& pool, int t) {
+    const uint32_t x = (uint32_t)t << 1;
+    const uint64_t low = (uint64_t)x * (uint32_t)pool.page_magic;
+    return (int)(((uint64_t)x * (uint32_t)(pool.page_magic >> 32) + (low >> 32)) >> 32);
+}
 
 // Sets a bit of the caller's status word (if there is one).
 __device__ __forceinline__ void flag(int32_t* status, int bit) {
@@ -56,30 +64,5 @@ struct E4M3 {
         return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
     }
 };
-
-// 8 elements of a row, at a multiple of 8 elements.
-template <class T>
-__device__ __forceinline__ void load8(const char* p, float (&x)[8]) {
-    if constexpr (T::bytes == 2) {
-        uint4 w = *reinterpret_cast<const uint4*>(p);
-        float2 a = T::unpack(w.x), b = T::unpack(w.y), c = T::unpack(w.z), d = T::unpack(w.w);
-        x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
-    } else {
-        uint2 w = *reinterpret_cast<const uint2*>(p);
-        float2 a = F16::unpack(E4M3::halves(w.x & 0xffff)), b = F16::unpack(E4M3::halves(w.x >> 16));
-        float2 c = F16::unpack(E4M3::halves(w.y & 0xffff)), d = F16::unpack(E4M3::halves(w.y >> 16));
-        x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
-    }
-}
-template <class T>
-__device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
-    if constexpr (T::bytes == 2) {
-        *reinterpret_cast<uint4*>(p) =
-            make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
-    } else {
-        *reinterpret_cast<uint2*>(p) = make_uint2(T::pack(x[0], x[1]) | (T::pack(x[2], x[3]) << 16),
-                                                  T::pack(x[4], x[5]) | (T::pack(x[6], x[7]) << 16));
-    }
-}
 
 }  // namespace fcsim_kv_dev
