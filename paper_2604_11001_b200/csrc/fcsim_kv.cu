@@ -276,6 +276,7 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* stat
 __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const EvictParams p, const int capacity) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
+    cudaTriggerProgrammaticLaunchCompletion();  // the copies may line up; they wait for this grid's end
     extern __shared__ uint4 keys[];
     __shared__ uint32_t counts[4][256], sums[256];
     __shared__ int warp_sums[kSelectWarps], warp_equals[kSelectWarps], mine, mine_equal, chosen[2];
@@ -333,6 +334,10 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         return k;
     };
     auto key = [&](int i) { return resident ? keys[i] : read_keys(i); };
+    auto meet = [&]() {  // a barrier of the cluster costs 0.5 us, one of a CTA a tenth of it
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+    };
     for (int i = tid; i < 4 * 256; i += kSelectThreads) counts[0][i] = 0;
     __syncthreads();
     uint32_t threshold = 0;
@@ -340,20 +345,30 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
 #pragma unroll 1
     for (int pass = 0; pass < 4; pass++) {
         const int shift = 24 - 8 * pass;
-#pragma unroll 4
-        for (int i = tid; i < count; i += kSelectThreads) {
-            uint4 k;
-            if (pass == 0) {
-                k = read_keys(i);
-                if (resident) keys[i] = k;
-            } else
-                k = key(i);
-            auto add = [&](uint32_t x) {
-                if (pass == 0 || (x ^ threshold) >> (shift + 8) == 0) atomicAdd(&counts[pass][(x >> shift) & 255], 1u);
-            };
-            add(k.x), add(k.y), add(k.z), add(k.w);
+        if (pass == 0) {
+            for (int i0 = tid; i0 < count; i0 += 4 * kSelectThreads) {
+                uint4 k[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (i0 + e * kSelectThreads < count) k[e] = read_keys(i0 + e * kSelectThreads);
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (i0 + e * kSelectThreads < count) {
+                        if (resident) keys[i0 + e * kSelectThreads] = k[e];
+                        atomicAdd(&counts[0][k[e].x >> 24], 1u), atomicAdd(&counts[0][k[e].y >> 24], 1u);
+                        atomicAdd(&counts[0][k[e].z >> 24], 1u), atomicAdd(&counts[0][k[e].w >> 24], 1u);
+                    }
+            }
+        } else {
+            for (int i = tid; i < count; i += kSelectThreads) {
+                const uint4 k = key(i);
+                auto add = [&](uint32_t x) {
+                    if ((x ^ threshold) >> (shift + 8) == 0) atomicAdd(&counts[pass][(x >> shift) & 255], 1u);
+                };
+                add(k.x), add(k.y), add(k.z), add(k.w);
+            }
         }
-        cluster.sync();
+        meet();
         if (tid < 256) {
             uint32_t sum = 0;
             for (int i = 0; i < ctas; i++) sum += cluster.map_shared_rank(&counts[pass][0], i)[tid];
@@ -405,9 +420,11 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         }
         mine = a, mine_equal = e;
     }
-    cluster.sync();
-    above = warp_sums[warp], equal = warp_equals[warp];
-    for (int i = 0; i < rank; i++) above += *cluster.map_shared_rank(&mine, i), equal += *cluster.map_shared_rank(&mine_equal, i);
+    meet();
+    above = lane < rank ? *cluster.map_shared_rank(&mine, lane) : 0;  // of the CTAs before this one
+    equal = lane < rank ? *cluster.map_shared_rank(&mine_equal, lane) : 0;
+    above = __reduce_add_sync(~0u, above) + warp_sums[warp];
+    equal = __reduce_add_sync(~0u, equal) + warp_equals[warp];
     for (int i0 = from; i0 < to; i0 += 32) {
         const int i = i0 + lane;
         const uint4 k = i < to ? key(i) : make_uint4(0, 0, 0, 0);
@@ -431,14 +448,19 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         const uint32_t all = __shfl_sync(~0u, upto, 31);
         above += (int)(all & 0xffff), equal += (int)(all >> 16);
     }
-    cluster.sync();  // the others may still read this CTA's counts
+    if (ctas > 1) cluster.sync();  // the others may still read this CTA's counts
 }
 
-// Copies the kept rows: 16 bytes a lane, LPR lanes a row, four rows of K and V in flight per lane.  Bound by memory.
+// Rows of K and V that a lane of the copies has in flight.  A row waits for its index and its page before it is read, so
+// more threads hide more than more rows of each: 64 requests to 1 024 tokens, 1, 2, 4, 8 rows: 82, 81, 89, 124 us in all.
+constexpr int kMoveRows = 2;
+
+// Copies the kept rows: 16 bytes a lane, LPR lanes a row.  Bound by memory.
 template <int LPR>
 __global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p) {
-    constexpr int kAtOnce = 256 / LPR, kRows = 4;
+    constexpr int kAtOnce = 256 / LPR, kRows = kMoveRows;
     const int r = blockIdx.z, h = blockIdx.y, lane = threadIdx.x % LPR;
+    cudaGridDependencySynchronize();
     const Cut c = cut_of(p, r, nullptr);
     const int row0 = blockIdx.x * kAtOnce * kRows + threadIdx.x / LPR;
     const int chunks = p.pool.head_dim * p.bytes / 16, size = p.pool.page_size;
@@ -477,9 +499,17 @@ __global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p)
 
 template <int LPR>
 int launch_move(const EvictParams& p, int n_requests, cudaStream_t stream) {
-    const int rows = 256 / LPR * 4;
-    fcsim_kv_move_kernel<LPR><<<dim3((p.max_budget + rows - 1) / rows, p.pool.n_kv, n_requests), 256, 0, stream>>>(p);
-    return launched();
+    const int rows = 256 / LPR * kMoveRows;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3((p.max_budget + rows - 1) / rows, p.pool.n_kv, n_requests);
+    config.blockDim = dim3(256);
+    config.stream = stream;
+    cudaLaunchAttribute early;  // launched while the selection runs
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&config, fcsim_kv_move_kernel<LPR>, (EvictParams)p));
 }
 
 // ------------------------------------------------------------------------------------------------ validation

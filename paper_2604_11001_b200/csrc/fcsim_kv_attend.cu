@@ -363,6 +363,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const int D = p.pool.head_dim, group = p.n_heads / p.pool.n_kv;
     const int head_tiles = (group + kCols - 1) / kCols, n_kv = p.pool.n_kv;
 
+    if (p.add_weight) cudaTriggerProgrammaticLaunchCompletion();  // the weights' kernel may line up; it waits for this grid's end
     // requests without tokens
     for (int b = blockIdx.x; b < p.n_requests; b += gridDim.x) {
         const int n = p.lengths[b];
@@ -845,12 +846,12 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 // per token and kv head; the sum over the heads in order.
 __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendParams p) {
     __shared__ Before before;
-    const Division work = divide<0>(p, 1, true, before);
+    const Division work = divide<0>(p, 1, true, before);  // (of the lengths alone, which the first kernel does not write)
     const int64_t first = work.first(), end = work.end();
-    if (first >= end) return;
     Place at = {};
     int cut, cuts;
-    locate<0>(p, 1, 1, work, first, end, before, at, cut, cuts);
+    if (first < end) locate<0>(p, 1, 1, work, first, end, before, at, cut, cuts);
+    cudaGridDependencySynchronize();  // (by every CTA: the grid must not end before the first one)
     const int group = p.n_heads / p.pool.n_kv;
     while (at.left > 0) {
         const int in = at.j * kTile + (threadIdx.x & (kTile - 1)), t = at.start + in;
@@ -875,8 +876,16 @@ __global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendP
     }
 }
 int launch_weights(const AttendParams& p, int grid, cudaStream_t stream) {
-    fcsim_kv_weight_kernel<<<grid, kThreads, 0, stream>>>(p);
-    return (int)cudaGetLastError();
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(kThreads);
+    config.stream = stream;
+    cudaLaunchAttribute early;  // launched while the first kernel ends
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return (int)cudaLaunchKernelEx(&config, fcsim_kv_weight_kernel, p);
 }
 #endif
 
