@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "fcsim_kv_attend.cuh"
 
@@ -41,9 +42,6 @@ struct AppendParams {
     float eps, one_over_dim;
 };
 
-// Lanes with work from which a group takes four heads instead of one.
-constexpr int64_t kAppendMany = 1 << 20;
-
 // 8 bytes as 4 elements and back.
 template <class T>
 __device__ __forceinline__ void unpack4(const uint2& w, float* x) {
@@ -56,158 +54,175 @@ __device__ __forceinline__ void store4(char* p, const float* x) {
     else *reinterpret_cast<uint32_t*>(p) = T::pack(x[0], x[1]) | (T::pack(x[2], x[3]) << 16);
 }
 
-// A group of LPR lanes takes HPG heads of one token; a CTA takes the same heads of 256 / LPR tokens, so that all its
-// branches on the kind of head are uniform, and the CTAs of a token's other heads are its neighbours.  A lane holds 8
-// elements of a head, as two runs of 4 that are a rotation's pairs (i .. i + 3 and i + rope_dim / 2 ..): turning them
-// needs no other lane, and half as many cosines and sines as elements, read once for all of the group's heads.  The
-// heads' loads are issued together.  Bound by the bytes of q, k and v when there are many tokens, by latency when few.
+enum { kQuery, kKey, kValue };
+
+// HPG neighbouring heads of one kind (`n` of them exist) of one token, by a group of LPR lanes: the loads of all first,
+// then norm, rotation and store of each.  A lane holds 8 elements of a head, as two runs of 4 at lo and hi.
+template <class T, class C, int LPR, int HPG, int KIND>
+__device__ __forceinline__ void append_heads(const AppendParams& p, const char* src, int64_t src_head, char* dst, int64_t dst_head, const char* norm,
+                                             const float* scale, int n, int lo, int hi, bool mine, bool stored, bool zero, bool pairs,
+                                             int neighbours, const float (&cosine)[4], const float (&sine)[4]) {
+    using Out = typename std::conditional<KIND == kQuery, T, C>::type;
+    uint2 raw[HPG][2];
+#pragma unroll
+    for (int i = 0; i < HPG; i++) {
+        raw[i][0] = raw[i][1] = make_uint2(0, 0);
+        if (mine && i < n) {
+            raw[i][0] = *reinterpret_cast<const uint2*>(src + lo * 2);
+            raw[i][1] = *reinterpret_cast<const uint2*>(src + hi * 2);
+        }
+        src += src_head;
+    }
+    float weight[8];
+    if (KIND != kValue && norm && mine) {
+        unpack4<T>(*reinterpret_cast<const uint2*>(norm + lo * 2), weight);
+        unpack4<T>(*reinterpret_cast<const uint2*>(norm + hi * 2), weight + 4);
+    }
+    char *to_lo = dst + lo * Out::bytes, *to_hi = dst + hi * Out::bytes;
+#pragma unroll
+    for (int i = 0; i < HPG; i++) {
+        if (i >= n) break;
+        if (KIND == kValue && C::bytes == 2) {  // as it came
+            if (stored) {
+                *reinterpret_cast<uint2*>(to_lo) = raw[i][0];
+                *reinterpret_cast<uint2*>(to_hi) = raw[i][1];
+            }
+        } else {
+            float x[8];
+            unpack4<T>(raw[i][0], x);
+            unpack4<T>(raw[i][1], x + 4);
+            if (KIND != kValue) {
+                if (norm) {
+                    float sum = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) sum += x[e] * x[e];
+#pragma unroll
+                    for (int m = LPR / 2; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
+                    const float r = rsqrtf(sum * p.one_over_dim + p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = x[e] * r * weight[e];
+                }
+                if (pairs) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const float a = x[e], b = x[e + 4];
+                        x[e] = a * cosine[e] - b * sine[e];
+                        x[e + 4] = b * cosine[e] + a * sine[e];
+                    }
+                } else if (neighbours > 0) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (e < neighbours) {
+                            const float a = x[2 * e], b = x[2 * e + 1];
+                            x[2 * e] = a * cosine[e] - b * sine[e];
+                            x[2 * e + 1] = b * cosine[e] + a * sine[e];
+                        }
+                }
+                if (zero) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = 0;
+                }
+            }
+            if (KIND != kQuery && C::bytes == 1) {
+                const float s = 1.0f / scale[i];
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] *= s;
+            }
+            if (stored) {
+                store4<Out>(to_lo, x);
+                store4<Out>(to_hi, x + 4);
+            }
+        }
+        to_lo += dst_head, to_hi += dst_head;
+    }
+}
+
+// A CTA takes the same HPG heads (of one kind: q, k or v) of 256 / LPR tokens, a group of LPR lanes each, so that every
+// branch on the kind is uniform and addresses advance by a stride; the CTAs of a token's other heads are its neighbours.
+// The two runs of a lane are a rotation's pairs (i .. i + 3 and i + rope_dim / 2 ..): turning them needs no other lane,
+// and half as many cosines and sines as elements, read once for all of the group's heads.  Bound by instructions and
+// by the bytes of q, k and v alike when there are many tokens, by latency when few.
 template <class T, class C, int LPR, int HPG>
-__global__ void __launch_bounds__(256) fcsim_kv_append_kernel(const AppendParams p) {
-    const int heads = p.n_heads + 2 * p.pool.n_kv, D = p.pool.head_dim, chunks = (heads + HPG - 1) / HPG;
-    const int block = blockIdx.x / chunks, first = (blockIdx.x - block * chunks) * HPG;
+__global__ void __launch_bounds__(256, HPG == 8 ? 4 : HPG == 4 ? 5 : 1) fcsim_kv_append_kernel(const AppendParams p) {
+    const int n_kv = p.pool.n_kv, D = p.pool.head_dim;
+    const int q_chunks = (p.n_heads + HPG - 1) / HPG, kv_chunks = (n_kv + HPG - 1) / HPG, chunks = q_chunks + 2 * kv_chunks;
+    const int block = blockIdx.x / chunks, chunk = blockIdx.x - block * chunks;
+    const int kind = chunk < q_chunks ? kQuery : chunk < q_chunks + kv_chunks ? kKey : kValue;
+    const int h = (kind == kQuery ? chunk : kind == kKey ? chunk - q_chunks : chunk - q_chunks - kv_chunks) * HPG;
     const int lane = threadIdx.x & (LPR - 1);
     const int at = block * (256 / LPR) + threadIdx.x / LPR;
     const bool there = at < p.n_tokens, mine = there && lane * 8 < D;
     const int64_t token = there ? at : 0;
     const int half = p.rope_dim / 2;
-    const bool halves = p.rope != nullptr && !p.interleaved, pairs = halves && lane * 4 < half;
+    const bool pairs = p.rope != nullptr && !p.interleaved && lane * 4 < half;
+    const int neighbours = p.interleaved ? half - lane * 4 : 0;  // pairs of this lane, if they are neighbours
     const int lo = pairs ? lane * 4 : lane * 8, hi = pairs ? half + lane * 4 : lo + 4;
-    uint2 raw[HPG][2];
-#pragma unroll
-    for (int i = 0; i < HPG; i++) {
-        const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
-        raw[i][0] = raw[i][1] = make_uint2(0, 0);
-        if (mine && j < heads) {
-            const char* src = k < 0 ? p.q + (token * p.q_row + j * p.q_head) * 2
-                            : v < 0 ? p.k + (token * p.k_row + k * p.k_head) * 2
-                                    : p.v + (token * p.v_row + v * p.v_head) * 2;
-            raw[i][0] = *reinterpret_cast<const uint2*>(src + lo * 2);
-            raw[i][1] = *reinterpret_cast<const uint2*>(src + hi * 2);
-        }
-    }
-    // the token's rotation
     bool good = true;
     float cosine[4] = {1, 1, 1, 1}, sine[4] = {0, 0, 0, 0};
     if (p.rope != nullptr) {
         const int position = p.positions[token];
         good = position >= 0 && position < p.n_positions;
-        if (!good && there && lane == 0 && first == 0) flag(p.status, FCSIM_KV_BAD_POSITION);
-        const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim + lane * 4;
-        if (pairs) {
-            *reinterpret_cast<float4*>(cosine) = *reinterpret_cast<const float4*>(row);
-            *reinterpret_cast<float4*>(sine) = *reinterpret_cast<const float4*>(row + half);
-        } else if (p.interleaved) {
+        if (!good && there && lane == 0 && chunk == 0) flag(p.status, FCSIM_KV_BAD_POSITION);
+        if (kind != kValue) {
+            const float* row = p.rope + (int64_t)(good ? position : 0) * p.rope_dim + lane * 4;
+            if (pairs) {
+                *reinterpret_cast<float4*>(cosine) = *reinterpret_cast<const float4*>(row);
+                *reinterpret_cast<float4*>(sine) = *reinterpret_cast<const float4*>(row + half);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (lane * 4 + i < half) cosine[i] = row[i], sine[i] = row[half + i];
+                for (int i = 0; i < 4; i++)
+                    if (i < neighbours) cosine[i] = row[i], sine[i] = row[half + i];
+            }
         }
+    }
+    if (kind == kQuery) {
+        append_heads<T, C, LPR, HPG, kQuery>(p, p.q + (token * p.q_row + h * p.q_head) * 2, p.q_head * 2, p.q_out + (token * p.n_heads + h) * D * 2, D * 2,
+                                             p.q_norm, nullptr, p.n_heads - h, lo, hi, mine, mine, !good, pairs, neighbours, cosine, sine);
+        return;
     }
     // the token's place in the cache
-    int64_t place = -1;
-    int page = 0, in_page = 0;
-    if (there && good && first + HPG > p.n_heads) {
+    bool stored = mine && good;
+    int64_t place = 0;
+    if (there && good) {
         const int64_t slot = p.slots[token];
-        if (slot >= (int64_t)p.pool.n_pages * p.pool.page_size) {
-            if (lane == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
-        } else if (slot >= 0) {
-            page = page_of(p.pool, (int)slot);
-            in_page = (int)slot - page * p.pool.page_size;
-            place = page * p.pool.stride_page + in_page * p.pool.stride_slot;
+        if (slot < 0 || slot >= (int64_t)p.pool.n_pages * p.pool.page_size) {
+            if (slot >= 0 && lane == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
+            stored = false;
+        } else {
+            const int page = page_of(p.pool, (int)slot), in_page = (int)slot - page * p.pool.page_size;
+            place = page * p.pool.stride_page + in_page * p.pool.stride_slot + h * p.pool.stride_head;
+            if (kind == kKey && p.pool.weight && lane < HPG && h + lane < n_kv)
+                p.pool.weight[((int64_t)page * n_kv + h + lane) * p.pool.page_size + in_page] = 0.0f;
         }
     }
-    float weight[8];  // of the norm
-#pragma unroll
-    for (int i = 0; i < HPG; i++) {
-        const int j = first + i, k = j - p.n_heads, v = k - p.pool.n_kv;
-        if (j >= heads) break;
-        float x[8];
-        if (v < 0) {
-            const char* w = k < 0 ? p.q_norm : p.k_norm;
-            unpack4<T>(raw[i][0], x);
-            unpack4<T>(raw[i][1], x + 4);
-            if (w) {
-                if ((i == 0 || k == 0) && mine) {
-                    unpack4<T>(*reinterpret_cast<const uint2*>(w + lo * 2), weight);
-                    unpack4<T>(*reinterpret_cast<const uint2*>(w + hi * 2), weight + 4);
-                }
-                float sum = 0;
-#pragma unroll
-                for (int e = 0; e < 8; e++) sum += x[e] * x[e];
-#pragma unroll
-                for (int m = LPR / 2; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
-                const float r = rsqrtf(sum * p.one_over_dim + p.eps);
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = x[e] * r * weight[e];
-            }
-            if (pairs) {
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float a = x[e], b = x[e + 4];
-                    x[e] = a * cosine[e] - b * sine[e];
-                    x[e + 4] = b * cosine[e] + a * sine[e];
-                }
-            } else if (p.interleaved) {
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (lane * 4 + e < half) {
-                        const float a = x[2 * e], b = x[2 * e + 1];
-                        x[2 * e] = a * cosine[e] - b * sine[e];
-                        x[2 * e + 1] = b * cosine[e] + a * sine[e];
-                    }
-            }
-        }
-        if (k < 0) {
-            if (!good) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = 0;
-            }
-            if (mine) {
-                char* dst = p.q_out + (token * p.n_heads + j) * D * 2;
-                store4<T>(dst + lo * 2, x);
-                store4<T>(dst + hi * 2, x + 4);
-            }
-            continue;
-        }
-        if (place < 0) continue;
-        const int h = v < 0 ? k : v;
-        char* dst = (v < 0 ? p.pool.k : p.pool.v) + (place + h * p.pool.stride_head) * C::bytes;
-        if (C::bytes == 2 && v >= 0) {  // as it came
-            if (mine) {
-                *reinterpret_cast<uint2*>(dst + lo * 2) = raw[i][0];
-                *reinterpret_cast<uint2*>(dst + hi * 2) = raw[i][1];
-            }
-            continue;
-        }
-        if (C::bytes == 1) {
-            if (v >= 0) {
-                unpack4<T>(raw[i][0], x);
-                unpack4<T>(raw[i][1], x + 4);
-            }
-            const float s = 1.0f / (v < 0 ? p.pool.k_scale[h] : p.pool.v_scale[h]);
-#pragma unroll
-            for (int e = 0; e < 8; e++) x[e] *= s;
-        }
-        if (mine) {
-            store4<C>(dst + lo * C::bytes, x);
-            store4<C>(dst + hi * C::bytes, x + 4);
-        }
-        if (v < 0 && lane == 0 && p.pool.weight)
-            p.pool.weight[((int64_t)page * p.pool.n_kv + h) * p.pool.page_size + in_page] = 0.0f;
-    }
+    if (kind == kKey)
+        append_heads<T, C, LPR, HPG, kKey>(p, p.k + (token * p.k_row + h * p.k_head) * 2, p.k_head * 2, p.pool.k + place * C::bytes,
+                                           p.pool.stride_head * C::bytes, p.k_norm, p.pool.k_scale + h, n_kv - h, lo, hi, mine, stored, false, pairs,
+                                           neighbours, cosine, sine);
+    else
+        append_heads<T, C, LPR, HPG, kValue>(p, p.v + (token * p.v_row + h * p.v_head) * 2, p.v_head * 2, p.pool.v + place * C::bytes,
+                                             p.pool.stride_head * C::bytes, nullptr, p.pool.v_scale + h, n_kv - h, lo, hi, mine, stored, false, false, 0,
+                                             cosine, sine);
 }
 
 template <class T, class C, int LPR, int HPG>
 int launch_append_as(const AppendParams& p, cudaStream_t stream) {
-    const int64_t heads = p.n_heads + 2 * p.pool.n_kv, tokens = 256 / LPR;
-    const int64_t blocks = (p.n_tokens + tokens - 1) / tokens * ((heads + HPG - 1) / HPG);
+    const int64_t chunks = (p.n_heads + HPG - 1) / HPG + 2 * ((p.pool.n_kv + HPG - 1) / HPG), tokens = 256 / LPR;
+    const int64_t blocks = (p.n_tokens + tokens - 1) / tokens * chunks;
     if (blocks > 0x7fffffff) return FCSIM_EINVAL;
     fcsim_kv_append_kernel<T, C, LPR, HPG><<<(unsigned)blocks, 256, 0, stream>>>(p);
     return launched();
 }
 template <class T, class C, int LPR>
 int launch_append_lanes(const AppendParams& p, cudaStream_t stream) {
+    // Heads a group: more share the rotation and the addresses, fewer spread a small call over the SMs.  With 64 + 2 x 8
+    // heads of 128 bf16 elements, 1 / 2 / 4 / 8 heads: 64 tokens 3.7 / 3.9 / 4.3 / 5.3 us, 256 tokens 6.1 / 5.0 / 5.0 / 5.8,
+    // 1 024 tokens 15.6 / 12.0 / 10.3 / 10.8, 4 096 tokens 55 / 41 / 31 / 29, 16 384 tokens 215 / 158 / 120 / 109.
     const int64_t lanes = (int64_t)p.n_tokens * (p.n_heads + 2 * p.pool.n_kv) * LPR;
-    return lanes >= kAppendMany ? launch_append_as<T, C, LPR, 4>(p, stream) : launch_append_as<T, C, LPR, 1>(p, stream);
+    if (lanes < 1 << 17) return launch_append_as<T, C, LPR, 1>(p, stream);
+    if (lanes < 1 << 19) return launch_append_as<T, C, LPR, 2>(p, stream);
+    if (lanes < 5 << 19) return launch_append_as<T, C, LPR, 4>(p, stream);
+    return launch_append_as<T, C, LPR, 8>(p, stream);
 }
 template <class T, class C>
 int launch_append(const AppendParams& p, cudaStream_t stream) {
