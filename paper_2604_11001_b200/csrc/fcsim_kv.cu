@@ -629,7 +629,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     l->logit_tiles = logit_tiles(p);
     l->logits = l->stats + (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0);
     l->bytes = l->stats + attend_kept(p);
-    l->weight_grid = (int)std::max<int64_t>(1, std::min<int64_t>(sms * 8, l->logit_tiles));
+    l->weight_grid = (int)std::max<int64_t>(1, std::min<int64_t>(sms * kWeightCtas, (l->logit_tiles * p.pool.n_kv + 7) / 8));
     return FCSIM_OK;
 }
 

@@ -842,37 +842,82 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 
 #if FCSIM_KV_TYPES == 0
 // weight[token] += sum over a group's heads of the softmax weights, from the logits that the first kernel left: the final
-// maximum and sum of a head are known only when all of its parts are joined.  The same division of the work, a thread
-// per token and kv head; the sum over the heads in order.
-__global__ void __launch_bounds__(kThreads) fcsim_kv_weight_kernel(const AttendParams p) {
+// reference and sum of a head are known only when all of its parts are joined.  The same division of the work, without
+// overhead: a CTA takes eight tiles of (request, kv head) at a time, 16 threads and four tokens a thread for each, two
+// heads' logits at once and their sum in order.  Bound by the latency of a few dependent loads, so what matters is that
+// one round of the grid is all of it, and what does not need the logits is loaded before the first kernel has ended.
+__global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(const AttendParams p) {
+    constexpr int kTiles = kThreads / (kTile / 4), kAtOnce = 2;
+    const int n_kv = p.pool.n_kv, group = p.n_heads / n_kv, mine = threadIdx.x / (kTile / 4), size = p.pool.page_size;
     __shared__ Before before;
-    const Division work = divide<0>(p, 1, true, before);  // (of the lengths alone, which the first kernel does not write)
+    const Division work = divide<0>(p, n_kv, true, before);  // (of the lengths alone, which the first kernel does not write)
     const int64_t first = work.first(), end = work.end();
     Place at = {};
     int cut, cuts;
-    if (first < end) locate<0>(p, 1, 1, work, first, end, before, at, cut, cuts);
+    if (first < end) locate<0>(p, n_kv, 1, work, first, end, before, at, cut, cuts);
+    for (int i = 0; i < mine && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
+
+    int in, t;
+    bool aligned, room;
+    float* weight[4];  // of each token, or none; one page and 16 aligned bytes where the size of a page allows
+    float old[4];
+    auto load_weights = [&]() {
+        in = at.j * kTile + threadIdx.x % (kTile / 4) * 4;
+        t = at.start + in;
+        aligned = size % 4 == 0 && t % 4 == 0;
+        room = at.tiles_before + at.tiles <= p.logit_tiles;
+        if (!room) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
+        const int32_t* const table = p.table + at.b * p.table_row;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            weight[i] = nullptr;
+            if (room && t + i < at.len && (i == 0 || !aligned)) {
+                const int index = page_of(p.pool, t + i), page = table[index];
+                if ((unsigned)page < (unsigned)p.pool.n_pages) weight[i] = p.pool.weight + ((int64_t)page * n_kv + at.kv) * size + t + i - index * size;
+            }
+        }
+        if (aligned) {
+            if (weight[0]) *reinterpret_cast<float4*>(old) = *reinterpret_cast<const float4*>(weight[0]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (weight[i]) old[i] = *weight[i];
+        }
+    };
+    if (at.left > 0) load_weights();
     cudaGridDependencySynchronize();  // (by every CTA: the grid must not end before the first one)
-    const int group = p.n_heads / p.pool.n_kv;
     while (at.left > 0) {
-        const int in = at.j * kTile + (threadIdx.x & (kTile - 1)), t = at.start + in;
-        if (at.tiles_before + at.tiles > p.logit_tiles) {
-            if (threadIdx.x == 0) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
-        } else if (t < at.len) {
-            const int page = p.table[at.b * p.table_row + page_of(p.pool, t)];
-            if (page >= 0 && page < p.pool.n_pages) {
-                const float* row = p.logits + (int64_t)at.tiles_before * p.n_heads * kTile + in;
-                const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads;
-                for (int kv = threadIdx.x / kTile; kv < p.pool.n_kv; kv += kThreads / kTile) {
-                    float sum = 0;
-                    for (int h = kv * group; h < (kv + 1) * group; h++) {
-                        const float4 x = stats[h];
-                        sum += power2((row[(int64_t)h * at.tiles * kTile] - x.x) * x.y) * x.z;
+        if (room && t < at.len) {
+            float sum[4] = {0, 0, 0, 0};
+            const int64_t step = (int64_t)at.tiles * kTile;
+            const float* logit = p.logits + (int64_t)at.tiles_before * p.n_heads * kTile + at.kv * group * step + in;
+            const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads + at.kv * group;
+            for (int h = 0; h < group; h += kAtOnce, logit += kAtOnce * step, stats += kAtOnce) {
+                float4 s[kAtOnce], x[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; i++)
+                    if (h + i < group) s[i] = *reinterpret_cast<const float4*>(logit + i * step), x[i] = stats[i];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; i++)
+                    if (h + i < group) {
+                        sum[0] += power2((s[i].x - x[i].x) * x[i].y) * x[i].z;
+                        sum[1] += power2((s[i].y - x[i].x) * x[i].y) * x[i].z;
+                        sum[2] += power2((s[i].z - x[i].x) * x[i].y) * x[i].z;
+                        sum[3] += power2((s[i].w - x[i].x) * x[i].y) * x[i].z;
                     }
-                    p.pool.weight[((int64_t)page * p.pool.n_kv + kv) * p.pool.page_size + t - page_of(p.pool, t) * p.pool.page_size] += sum;
+            }
+            if (aligned && t + 3 < at.len) {
+                if (weight[0]) *reinterpret_cast<float4*>(weight[0]) = make_float4(old[0] + sum[0], old[1] + sum[1], old[2] + sum[2], old[3] + sum[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    float* const w = aligned ? (weight[0] && t + i < at.len ? weight[0] + i : nullptr) : weight[i];
+                    if (w) *w = old[i] + sum[i];
                 }
             }
         }
-        advance<0>(p, at, 1, 1);
+        for (int i = 0; i < kTiles && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
+        if (at.left > 0) load_weights();
     }
 }
 int launch_weights(const AttendParams& p, int grid, cudaStream_t stream) {

@@ -22,7 +22,7 @@ from . import binding as _fb
 F16, BF16, E4M3 = 0, 1, 2
 BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET = 1, 2, 4, 8
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
-_WIDE = (torch.float16, torch.bfloat16)
+_WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
 # the current device's number and a device's current stream as plain integers, without the objects around them
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -163,31 +163,27 @@ class PagedKV:
     # ------------------------------------------------------------------------------------------ helpers
     # A slot's calls take a few microseconds on the device: checks are plain comparisons, the argument struct is packed
     # in one go, and messages are only made when they are needed.
-    def _on_device(self, *tensors):
-        for t in tensors:
-            if t is not None and t.get_device() != self._index:
-                raise ValueError(f"tensors have to be on the cache's device {self.device}, got {t.device}")
-
-    def _rows(self, x, name, n, heads, dtype):
-        """Strides of [tokens, heads, head_dim]."""
-        if x.dim() != 3 or x.dtype != dtype or x.shape[0] != n or x.shape[1] != heads or x.shape[2] != self.head_dim:
-            raise ValueError(f"{name}: {dtype} [{n}, {heads}, {self.head_dim}], got {x.dtype} {list(x.shape)}")
+    def _rows(self, x, name, shape, dtype):
+        """Row and head strides of a [tokens, heads, head_dim] tensor."""
+        if x.shape != shape or x.dtype != dtype or x.get_device() != self._index:
+            raise ValueError(f"{name}: {dtype} {list(shape)} on {self.device}, got {x.dtype} {list(x.shape)} on {x.device}")
         row, head, one = x.stride()
         if one != 1:
             raise ValueError(f"{name}: head_dim has to be contiguous")
         return row, head
 
-    @staticmethod
-    def _table(table, name, n):
-        if (table.dim() != 2 or table.dtype != torch.int32 or table.shape[0] != n
-                or (table.stride(1) != 1 and table.shape[1] > 1)):
-            raise ValueError(f"{name}: int32 [{n}, pages], rows contiguous")
-        return table.shape[1]
+    def _table(self, table, name, n):
+        """Columns of a page table."""
+        shape = table.shape
+        if len(shape) != 2 or shape[0] != n or table.dtype != torch.int32 or table.get_device() != self._index:
+            raise ValueError(f"{name}: int32 [{n}, pages] on {self.device}, got {table.dtype} {list(shape)} on {table.device}")
+        if shape[1] > 1 and table.stride(1) != 1:
+            raise ValueError(f"{name}: rows have to be contiguous")
+        return shape[1]
 
-    @staticmethod
-    def _ints(x, name, n, dtype=torch.int32):
-        if x.dim() != 1 or x.dtype != dtype or x.shape[0] != n or (n > 1 and x.stride(0) != 1):
-            raise ValueError(f"{name}: contiguous {dtype} [{n}]")
+    def _flat(self, x, name, shape, dtype):
+        if x.shape != shape or x.dtype != dtype or x.get_device() != self._index or not x.is_contiguous():
+            raise ValueError(f"{name}: contiguous {dtype} {list(shape)} on {self.device}, got {x.dtype} {list(x.shape)} on {x.device}")
 
     def _call(self, entry, args, size=None):
         """Run an entry point on the current stream of the cache's device.  ``size``: the entry point that tells the size
@@ -230,33 +226,35 @@ class PagedKV:
         n, dtype = k.shape[0], k.dtype
         if dtype not in _WIDE:
             raise ValueError("k: float16 or bfloat16")
-        k_row, k_head = self._rows(k, "k", n, self.n_kv_heads, dtype)
-        v_row, v_head = self._rows(v, "v", n, self.n_kv_heads, dtype)
-        self._ints(slots, "slots", n, torch.int64)
-        out, heads, q_row, q_head = None, 0, 0, 0
+        shape = (n, self.n_kv_heads, self.head_dim)
+        k_row, k_head = self._rows(k, "k", shape, dtype)
+        v_row, v_head = self._rows(v, "v", shape, dtype)
+        self._flat(slots, "slots", (n,), torch.int64)
+        out, heads, q_row, q_head, q_at, out_at = None, 0, 0, 0, 0, 0
         if q is not None:
             heads = q.shape[1]
-            q_row, q_head = self._rows(q, "q", n, heads, dtype)
-        rope_dim = n_positions = 0
-        if rope is not None:
-            if rope.dim() != 2 or rope.dtype != torch.float32 or not rope.is_contiguous():
-                raise ValueError("rope: contiguous float32 [positions, rope_dim]")
-            if positions is None:
-                raise ValueError("positions: needed with rope")
-            self._ints(positions, "positions", n)
-            n_positions, rope_dim = rope.shape
-        else:
-            positions = None
-        for w in (q_norm, k_norm):
-            if w is not None and (w.dim() != 1 or w.shape[0] != self.head_dim or w.dtype != dtype or w.stride(0) != 1):
-                raise ValueError(f"q_norm, k_norm: contiguous {dtype} [{self.head_dim}]")
-        self._on_device(q, k, v, slots, rope, positions, q_norm, k_norm)
-        if q is not None:
+            q_row, q_head = self._rows(q, "q", (n, heads, self.head_dim), dtype)
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            q_at, out_at = q.data_ptr(), out.data_ptr()
+        rope_at = positions_at = rope_dim = n_positions = 0
+        if rope is not None:
+            if positions is None or rope.dim() != 2:
+                raise ValueError("rope: float32 [positions, rope_dim], with positions")
+            n_positions, rope_dim = rope.shape
+            self._flat(rope, "rope", (n_positions, rope_dim), torch.float32)
+            self._flat(positions, "positions", (n,), torch.int32)
+            rope_at, positions_at = rope.data_ptr(), positions.data_ptr()
+        q_norm_at = k_norm_at = 0
+        if q_norm is not None:
+            self._flat(q_norm, "q_norm", (self.head_dim,), dtype)
+            q_norm_at = q_norm.data_ptr()
+        if k_norm is not None:
+            self._flat(k_norm, "k_norm", (self.head_dim,), dtype)
+            k_norm_at = k_norm.data_ptr()
         self._call(_lib.fcsim_kv_append, _APPEND.pack(
-            _pointer(q), k.data_ptr(), v.data_ptr(), _pointer(out), _pointer(q_norm), _pointer(k_norm), _pointer(rope),
-            _pointer(positions), slots.data_ptr(), self._status, q_row, q_head, k_row, k_head, v_row, v_head, n, heads,
-            _TYPES[dtype], rope_dim, n_positions, 1 if interleaved else 0, eps, 0))
+            q_at, k.data_ptr(), v.data_ptr(), out_at, q_norm_at, k_norm_at, rope_at, positions_at, slots.data_ptr(),
+            self._status, q_row, q_head, k_row, k_head, v_row, v_head, n, heads, _TYPES[dtype], rope_dim, n_positions,
+            1 if interleaved else 0, eps, 0))
         return out
 
     def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, add_weight=False,
@@ -267,13 +265,13 @@ class PagedKV:
 
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
         only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
-        if q.dim() != 3 or q.dtype not in _WIDE:
+        dtype = q.dtype
+        if q.dim() != 3 or dtype not in _WIDE:
             raise ValueError("q: float16 or bfloat16 [requests, heads, head_dim]")
-        n, heads, dtype = q.shape[0], q.shape[1], q.dtype
-        q_row, q_head = self._rows(q, "q", n, heads, dtype)
+        n, heads, _ = q.shape
+        q_row, q_head = self._rows(q, "q", (n, heads, self.head_dim), dtype)
         cols = self._table(table, "table", n)
-        self._ints(lengths, "lengths", n)
-        self._on_device(q, table, lengths)
+        self._flat(lengths, "lengths", (n,), torch.int32)
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lse = q.new_empty((n, heads), dtype=torch.float32) if return_lse else None
         self._call(_lib.fcsim_kv_attend, _ATTEND.pack(
@@ -290,9 +288,8 @@ class PagedKV:
         [requests, n_kv_heads, max_budget], -1 beyond)."""
         n = lengths.shape[0]
         cols, new_cols = self._table(table, "table", n), self._table(new_table, "new_table", n)
-        self._ints(lengths, "lengths", n)
-        self._ints(budget, "budget", n)
-        self._on_device(table, lengths, budget, new_table)
+        self._flat(lengths, "lengths", (n,), torch.int32)
+        self._flat(budget, "budget", (n,), torch.int32)
         if max_budget is None:
             max_budget = new_cols * self.page_size
         if max_budget < 0:
