@@ -606,11 +606,12 @@ struct AttendLayout {
 int64_t logit_tiles(const AttendParams& p) {
     if (!p.add_weight) return 0;
     const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
-    return std::min((seen + kTile - 1) / kTile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / kTile + p.n_requests);
+    const int64_t tile = 1 << p.tile_bits;
+    return std::min((seen + tile - 1) / tile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / tile + p.n_requests);
 }
 // The part of the workspace that does not depend on the device.
 size_t attend_kept(const AttendParams& p) {
-    return (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0) + (size_t)logit_tiles(p) * kTile * p.n_heads * 4;
+    return (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0) + ((size_t)logit_tiles(p) << p.tile_bits) * p.n_heads * 4;
 }
 
 int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l) {
@@ -618,7 +619,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     if (rc != FCSIM_OK) return rc;
     if ((rc = v.ctas_per_sm(device, &per_sm)) != 0) return cuda_status((cudaError_t)rc);
     const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
-    const int64_t tiles = (seen + kTile - 1) / kTile, group = p.n_heads / p.pool.n_kv;
+    const int64_t tiles = (seen + (1 << p.tile_bits) - 1) >> p.tile_bits, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
     l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most, p.n_requests)}));
     // the kernel counts the tiles of all requests, and the work of a CTA, in 32 bits
@@ -629,7 +630,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     l->logit_tiles = logit_tiles(p);
     l->logits = l->stats + (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0);
     l->bytes = l->stats + attend_kept(p);
-    l->weight_grid = (int)std::max<int64_t>(1, std::min<int64_t>(sms * kWeightCtas, (l->logit_tiles * p.pool.n_kv + 7) / 8));
+    l->weight_grid = (int)std::max<int64_t>(1, std::min<int64_t>(sms * kWeightCtas, ((l->logit_tiles << p.tile_bits) * p.pool.n_kv + 4 * kThreads - 1) / (4 * kThreads)));
     return FCSIM_OK;
 }
 
@@ -694,8 +695,10 @@ extern "C" int fcsim_kv_attend_workspace(const fcsim_kv_cache* c, const fcsim_kv
     if (!out) return FCSIM_EINVAL;
     *out = {0, 0};
     if (p.n_requests == 0) return FCSIM_OK;
+    const AttendVariant v = attend_variant(c, a);
+    p.tile_bits = v.tile_bits;
     AttendLayout l;
-    if ((rc = attend_layout(p, attend_variant(c, a), &l)) != FCSIM_OK) return rc;
+    if ((rc = attend_layout(p, v, &l)) != FCSIM_OK) return rc;
     *out = {l.bytes, l.counters};
     return FCSIM_OK;
 }
@@ -706,8 +709,9 @@ extern "C" int fcsim_kv_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_ar
     int rc = check_attend(c, a, &p);
     if (rc != FCSIM_OK) return rc;
     if (p.n_requests == 0) return FCSIM_OK;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < attend_kept(p)) return FCSIM_ESIZE;
     const AttendVariant v = attend_variant(c, a);
+    p.tile_bits = v.tile_bits;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < attend_kept(p)) return FCSIM_ESIZE;
     AttendLayout l;
     if ((rc = attend_layout(p, v, &l)) != FCSIM_OK) return rc;
     if (workspace_bytes < l.bytes) return FCSIM_ESIZE;

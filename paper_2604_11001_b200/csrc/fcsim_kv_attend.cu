@@ -115,7 +115,7 @@ __device__ __forceinline__ int start_of(const AttendParams& p, int len) {
     return p.window > 0 && len > p.window ? len - p.window : 0;
 }
 __device__ __forceinline__ int tiles_of(const AttendParams& p, int len) {
-    return (len - start_of(p, len) + kTile - 1) / kTile;
+    return (len - start_of(p, len) + (1 << p.tile_bits) - 1) >> p.tile_bits;
 }
 __device__ __forceinline__ void enter(const AttendParams& p, Place& w, int b) {
     w.b = b;
@@ -263,17 +263,21 @@ template <class T, class C, int DP, int NT>
 struct Shape {
     static constexpr int kRow = DP * C::bytes;
     static constexpr int kPitch = kRow + 16;                    // bytes of a row in shared memory: 8 rows of a column cover all banks
+    // tokens of a warp: 8-bit rows want twice as many for each tile's fixed work (64 requests, 82 -> 78 us; 16-bit rows of 128
+    // bytes lose more by fewer CTAs on an SM: 47 -> 55)
+    static constexpr int kTokens = C::bytes == 1 && kRow == 128 ? 32 : 16;
+    static constexpr int kTile = 4 * kTokens, kTileBits = kTokens == 32 ? 7 : 6;
     static constexpr int kStage = kTile * 2 * kPitch;           // K and V of a tile
     static constexpr int kOutPitch = DP + 4;                    // floats; 4 more: heads fall on different banks
     static constexpr int kMerge = 2 * 8 * NT * kOutPitch * 4;   // two warps' outputs
     static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 128;     // statistics of the columns, masks of the rings, a flag
     static constexpr int kStatic = sizeof(Before) + 64;
     static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall - kStatic) / kStage; }
-    // As many CTAs on an SM as registers and two stages each allow, then as many stages (three at most) as keep 64 KB of an SM's
-    // loads under way.  More only queue: with three stages of 32 KB instead of two, SMs differ more in the rate they get,
-    // and a call ends with the slowest (131 072 tokens of one request 99 us, with two 96; 16 KB tiles 82 us, with two 87).
-    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 && (kRow <= 128) ? 3 : 2;
-    static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(2) >= 2 ? 2 : 1;
+    // As many CTAs on an SM as registers and two stages each allow.  More stages only queue: with three of 32 KB instead of
+    // two, SMs differ more in the rate they get, and a call ends with the slowest (131 072 tokens of one request 99 us,
+    // with two 96).
+    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 && kRow <= 128 ? 3 : 2;
+    static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(3) >= 2 && kRegisterCtas >= 3 ? 3 : stages(2) >= 2 ? 2 : 1;
     static constexpr int kStages = kCtas * kStage >= 64 * 1024 || stages(kCtas) < 3 ? 2 : 3;
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
     static_assert(kStages >= 2, "shared memory of a CTA");
@@ -349,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     using M = typename OperandOf<T, C>::type;
     constexpr bool kNarrow = C::bytes == 1, kRescaled = kNarrow && std::is_same<T, BF16>::value;
     constexpr bool kSplit = !kRescaled;  // f16 weights are 8 times finer than a bf16 output as they are
-    constexpr int kCols = 8 * NT, kSteps = DP / 16;
+    constexpr int kCols = 8 * NT, kSteps = DP / 16, kTokens = S::kTokens, kSub = kTokens / 16;
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
@@ -381,20 +385,21 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     Place at = {};  // the tile that is computed next
     int cut = 0, cuts = 1;
 
-    // stage s of this warp: + s * kStage; 16 rows of K, then 16 of V
-    const uint32_t ring = smem_address(smem + warp * 32 * S::kPitch);
+    // stage s of this warp: + s * kStage; its tokens' rows of K, then of V
+    const uint32_t ring = smem_address(smem + warp * 2 * kTokens * S::kPitch);
     const int chunks = D * C::bytes / 16;
 
-    // ---- loads: a row is kLanes lanes' 16 bytes, kRows rows at once; the page numbers (of token lane % 16) are fetched
-    // one tile ahead
+    // ---- loads: a row is kLanes lanes' 16 bytes, kRows rows at once; the page numbers (of token lane % kTokens) are
+    // fetched one tile ahead
     constexpr int kLanes = S::kRow / 16, kRows = 32 / kLanes;
+    constexpr uint32_t kAll = kTokens == 32 ? ~0u : 0xffffu;
     const int chunk = lane % kLanes, lane_row = lane / kLanes;
     const bool copies = chunk < chunks;
     const int64_t v_from_k = p.pool.v - p.pool.k, slot_bytes = p.pool.stride_slot * C::bytes;
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * kTile + warp * 16 + (lane & 15), i = page_of(p.pool, t);
+        const int t = in.start + in.j * S::kTile + warp * kTokens + lane % kTokens, i = page_of(p.pool, t);
         place = t - i * p.pool.page_size;
         page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
     };
@@ -408,33 +413,42 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     auto load_next = [&](int stage) {
         if (in.left > 0) {
             const bool good = (unsigned)page < (unsigned)p.pool.n_pages;
-            const uint32_t mask = __ballot_sync(~0u, good) & 0xffff;
+            const uint32_t mask = __ballot_sync(~0u, good) & kAll;
             if (lane == 0) masks[stage] = mask;  // for the computation of this tile
-            const uint32_t dst = lane_dst + stage * S::kStage;
+            if (mask != kAll && !good && in.start + in.j * S::kTile + warp * kTokens + lane % kTokens < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
             const int64_t head = in.kv * p.pool.stride_head;
-            const int place0 = __shfl_sync(~0u, place, 0);
-            if (mask == 0xffff && place0 + 16 <= p.pool.page_size) {  // 16 tokens of one page: rows at equal distances
-                const char* src = p.pool.k + (page * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
-                if (copies) {
 #pragma unroll
-                    for (int i = 0; i < 16 / kRows; i++) {
-                        copy16(dst + i * kRows * S::kPitch, src);
-                        copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k);
-                        src += kRows * slot_bytes;
+            for (int b = 0; b < kSub; b++) {
+                const uint32_t dst = lane_dst + stage * S::kStage + b * 16 * S::kPitch, half = mask >> (16 * b) & 0xffff;
+                const int page0 = __shfl_sync(~0u, page, 16 * b), place0 = __shfl_sync(~0u, place, 16 * b);
+                if (half == 0xffff && place0 + 16 <= p.pool.page_size) {  // 16 tokens of one page: rows at equal distances
+                    const char* src = p.pool.k + (page0 * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
+                    if (copies) {
+#pragma unroll
+                        for (int i = 0; i < 16 / kRows; i++) {
+                            copy16(dst + i * kRows * S::kPitch, src);
+                            copy16(dst + (kTokens + i * kRows) * S::kPitch, src + v_from_k);
+                            src += kRows * slot_bytes;
+                        }
                     }
-                }
-            } else {
-                if (!good && in.start + in.j * kTile + warp * 16 + (lane & 15) < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
-                if (mask) {
+                } else if (half) {
                     const int64_t mine = good ? (page * p.pool.stride_page + place * p.pool.stride_slot + head) * C::bytes : -1;
 #pragma unroll
                     for (int i = 0; i < 16 / kRows; i++) {
-                        const int64_t x = __shfl_sync(~0u, mine, i * kRows + lane_row);
+                        const int64_t x = __shfl_sync(~0u, mine, 16 * b + i * kRows + lane_row);
                         const char* src = p.pool.k + (x < 0 ? 0 : x + chunk * 16);
                         if (copies) {  // rows that do not exist: zeros, for weights of zero
                             copy16(dst + i * kRows * S::kPitch, src, x < 0 ? 0 : 16);
-                            copy16(dst + (16 + i * kRows) * S::kPitch, src + v_from_k, x < 0 ? 0 : 16);
+                            copy16(dst + (kTokens + i * kRows) * S::kPitch, src + v_from_k, x < 0 ? 0 : 16);
                         }
+                    }
+                } else if (copies) {  // none of the 16
+                    const uint4 none = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16 / kRows; i++) {
+                        char* const row = smem + warp * 2 * kTokens * S::kPitch + stage * S::kStage + (b * 16 + lane_row + i * kRows) * S::kPitch + chunk * 16;
+                        *reinterpret_cast<uint4*>(row) = none;
+                        *reinterpret_cast<uint4*>(row + kTokens * S::kPitch) = none;
                     }
                 }
             }
@@ -464,8 +478,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     auto start_ring = [&]() {
         if (chunks * 16 < S::kRow)  // elements beyond head_dim are never copied to: zeros
             for (int s = 0; s < S::kStages; s++)
-                for (int i = chunks * 16; i < S::kRow; i += 16)
-                    *reinterpret_cast<uint4*>(smem + (warp * 32 + lane) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
+                for (int t = lane; t < 2 * kTokens; t += 32)
+                    for (int i = chunks * 16; i < S::kRow; i += 16)
+                        *reinterpret_cast<uint4*>(smem + (warp * 2 * kTokens + t) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
         stage = 0;
         fetch_page();
 #pragma unroll 1
@@ -480,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             cols = min(kCols, group - col0);
             logits = nullptr;
             if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles)
-                logits = p.logits + ((int64_t)at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * kTile +
-                         warp * 16 + lane / 4;
+                logits = p.logits + ((int64_t)at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * S::kTile +
+                         warp * kTokens + lane / 4;
             const float kscale = kNarrow ? p.pool.k_scale[kv] : 1.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
@@ -537,129 +552,144 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         const uint32_t mask = masks[stage];
 
         if (mask) {  // (a warp may have no token of a request's last tile)
-        const uint32_t krow = ring + stage * S::kStage, vrow = krow + 16 * S::kPitch;
-        // ---- s^T = K q^T: 16 tokens by 8 heads
-        float s[NT][4] = {};
-        {
-            const int t = (lane & 7) + ((lane >> 3) & 1) * 8;
-            const uint32_t row = krow + t * S::kPitch + (lane >> 4) * 16;
-            if constexpr (!kNarrow) {
+            const uint32_t krow = ring + stage * S::kStage, vrow = krow + kTokens * S::kPitch;
+            // ---- s^T = K q^T: 16 tokens by 8 heads at a time
+            float s[kSub][NT][4] = {};
 #pragma unroll
-                for (int k = 0; k < kSteps; k++) {
-                    uint32_t a[4];
-                    load_matrices(row + k * 32, a);
+            for (int b = 0; b < kSub; b++) {
+                const uint32_t row = krow + (b * 16 + (lane & 7) + ((lane >> 3) & 1) * 8) * S::kPitch + (lane >> 4) * 16;
+                if constexpr (!kNarrow) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; nt++) mma<M>(s[nt], a, qf[nt][k][0], qf[nt][k][1]);
-                }
-            } else {
+                    for (int k = 0; k < kSteps; k++) {
+                        uint32_t a[4];
+                        load_matrices(row + k * 32, a);
 #pragma unroll
-                for (int k = 0; k < kSteps; k += 2) {
-                    uint32_t w[4];
-                    load_matrices(row + k * 16, w);
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const uint32_t a[4] = {E4M3::halves(w[2 * i]), E4M3::halves(w[2 * i + 1]),
-                                               E4M3::halves(w[2 * i] >> 16), E4M3::halves(w[2 * i + 1] >> 16)};
-#pragma unroll
-                        for (int nt = 0; nt < NT; nt++) mma<M>(s[nt], a, qf[nt][k + i][0], qf[nt][k + i][1]);
+                        for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k][0], qf[nt][k][1]);
                     }
-                }
-            }
-        }
-        // ---- softmax: this lane holds tokens lane / 4 and + 8 of heads 2 (lane % 4) and + 1
-        uint32_t hi[NT][2], lo[NT][2];
+                } else {
 #pragma unroll
-        for (int nt = 0; nt < NT; nt++) {
-            if (logits) {
-                float* x = logits + at.j * kTile + (int64_t)(nt * 8) * at.tiles * kTile;
+                    for (int k = 0; k < kSteps; k += 2) {
+                        uint32_t w[4];
+                        load_matrices(row + k * 16, w);
 #pragma unroll
-                for (int i = 0; i < 2; i++)
-                    if (nt * 8 + 2 * (lane & 3) + i < cols) {
-                        x[(int64_t)i * at.tiles * kTile] = s[nt][i];
-                        x[(int64_t)i * at.tiles * kTile + 8] = s[nt][2 + i];
-                    }
-            }
-            if (mask != 0xffff) {
+                        for (int i = 0; i < 2; i++) {
+                            const uint32_t a[4] = {E4M3::halves(w[2 * i]), E4M3::halves(w[2 * i + 1]),
+                                                   E4M3::halves(w[2 * i] >> 16), E4M3::halves(w[2 * i + 1] >> 16)};
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    if (!(mask >> (lane / 4 + 8 * (i >> 1)) & 1)) s[nt][i] = -INFINITY;
-            }
-            // The reference moves only when a logit is 2^8 above it: the weights stay far from f16's and fp32's ends, and the
-            // maximum over the lanes is taken a few times in a request instead of in every tile.
-            const bool over = fmaxf(s[nt][0], s[nt][2]) > limit[nt][0] || fmaxf(s[nt][1], s[nt][3]) > limit[nt][1];
-            if (__any_sync(~0u, over)) {
-                float shrink[2];
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    float top = fmaxf(s[nt][i], s[nt][2 + i]);
-                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-                    const bool first = limit[nt][i] == -INFINITY;
-                    const float now = first ? top : fmaxf(top, m[nt][i]), base = now == -INFINITY ? 0.0f : now;
-                    shrink[i] = first ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
-                    m[nt][i] = base;
-                    limit[nt][i] = now + fminf(8.0f / unit[nt][i], 1e30f);
-                    l[nt][i] *= shrink[i];
-                }
-#pragma unroll
-                for (int k = 0; k < kSteps; k++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) o[k][nt][i] *= shrink[i & 1];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                s[nt][i] = power2((s[nt][i] - m[nt][i & 1]) * unit[nt][i & 1]);
-                l[nt][i & 1] += s[nt][i];
-            }
-#pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const float a = s[nt][2 * k], b = s[nt][2 * k + 1];
-                if constexpr (kSplit) {
-                    const uint32_t h = below<M>(a, b);
-                    const float2 back = M::unpack(h);
-                    hi[nt][k] = transpose8x8(h);
-                    lo[nt][k] = transpose8x8(M::pack(a - back.x, b - back.y));
-                } else
-                    hi[nt][k] = transpose8x8(M::pack(a, b));
-            }
-        }
-        // ---- o^T += V^T p^T: 16 elements of head_dim by 8 heads
-        {
-            const int which = lane >> 3;
-            if constexpr (!kNarrow) {
-                const uint32_t row = vrow + ((lane & 7) + (which >> 1) * 8) * S::kPitch + (which & 1) * 16;
-#pragma unroll
-                for (int k = 0; k < kSteps; k++) {
-                    uint32_t a[4];
-                    load_matrices_transposed(row + k * 32, a);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++) {
-                        mma<M>(o[k][nt], a, hi[nt][0], hi[nt][1]);
-                        if constexpr (kSplit) mma<M>(o[k][nt], a, lo[nt][0], lo[nt][1]);
-                    }
-                }
-            } else {
-                const uint32_t row = vrow + ((lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
-#pragma unroll
-                for (int k = 0; k < kSteps; k += 2) {
-                    // a lane gets bytes 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8
-                    uint32_t w[4];
-                    load_matrices_transposed(row + k * 16, w);
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const uint32_t x = w[2 * i], y = w[2 * i + 1];
-                        const uint32_t a[4] = {E4M3::halves(__byte_perm(x, 0, 0x4420)), E4M3::halves(__byte_perm(x, 0, 0x4431)),
-                                               E4M3::halves(__byte_perm(y, 0, 0x4420)), E4M3::halves(__byte_perm(y, 0, 0x4431))};
-#pragma unroll
-                        for (int nt = 0; nt < NT; nt++) {
-                            mma<M>(o[k + i][nt], a, hi[nt][0], hi[nt][1]);
-                            if constexpr (kSplit) mma<M>(o[k + i][nt], a, lo[nt][0], lo[nt][1]);
+                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k + i][0], qf[nt][k + i][1]);
                         }
                     }
                 }
             }
-        }
+            // ---- softmax: this lane holds tokens lane / 4 and + 8 of every 16, of heads 2 (lane % 4) and + 1
+            uint32_t hi[kSub][NT][2], lo[kSub][NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                if (logits) {
+                    float* x = logits + at.j * S::kTile + (int64_t)(nt * 8) * at.tiles * S::kTile;
+#pragma unroll
+                    for (int i = 0; i < 2; i++)
+                        if (nt * 8 + 2 * (lane & 3) + i < cols) {
+#pragma unroll
+                            for (int b = 0; b < kSub; b++) {
+                                x[16 * b] = s[b][nt][i];
+                                x[16 * b + 8] = s[b][nt][2 + i];
+                            }
+                            x += (int64_t)at.tiles * S::kTile;
+                        }
+                }
+                if (mask != kAll) {
+#pragma unroll
+                    for (int b = 0; b < kSub; b++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            if (!(mask >> (16 * b + lane / 4 + 8 * (i >> 1)) & 1)) s[b][nt][i] = -INFINITY;
+                }
+                float most[2];
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    most[i] = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
+                    if (kSub == 2) most[i] = fmaxf(most[i], fmaxf(s[kSub - 1][nt][i], s[kSub - 1][nt][2 + i]));
+                }
+                // The reference moves only when a logit is 2^8 above it: the weights stay far from f16's and fp32's ends, and
+                // the maximum over the lanes is taken a few times in a request instead of in every tile.
+                if (__any_sync(~0u, most[0] > limit[nt][0] || most[1] > limit[nt][1])) {
+                    float shrink[2];
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        float top = most[i];
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                        const bool first_one = limit[nt][i] == -INFINITY;
+                        const float now = first_one ? top : fmaxf(top, m[nt][i]), base = now == -INFINITY ? 0.0f : now;
+                        shrink[i] = first_one ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
+                        m[nt][i] = base;
+                        limit[nt][i] = now + fminf(8.0f / unit[nt][i], 1e30f);
+                        l[nt][i] *= shrink[i];
+                    }
+#pragma unroll
+                    for (int k = 0; k < kSteps; k++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) o[k][nt][i] *= shrink[i & 1];
+                }
+#pragma unroll
+                for (int b = 0; b < kSub; b++) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        s[b][nt][i] = power2((s[b][nt][i] - m[nt][i & 1]) * unit[nt][i & 1]);
+                        l[nt][i & 1] += s[b][nt][i];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; k++) {
+                        const float x = s[b][nt][2 * k], y = s[b][nt][2 * k + 1];
+                        if constexpr (kSplit) {
+                            const uint32_t h = below<M>(x, y);
+                            const float2 back = M::unpack(h);
+                            hi[b][nt][k] = transpose8x8(h);
+                            lo[b][nt][k] = transpose8x8(M::pack(x - back.x, y - back.y));
+                        } else
+                            hi[b][nt][k] = transpose8x8(M::pack(x, y));
+                    }
+                }
+            }
+            // ---- o^T += V^T p^T: 16 elements of head_dim by 8 heads
+            const int which = lane >> 3;
+#pragma unroll
+            for (int b = 0; b < kSub; b++) {
+                if constexpr (!kNarrow) {
+                    const uint32_t row = vrow + (b * 16 + (lane & 7) + (which >> 1) * 8) * S::kPitch + (which & 1) * 16;
+#pragma unroll
+                    for (int k = 0; k < kSteps; k++) {
+                        uint32_t a[4];
+                        load_matrices_transposed(row + k * 32, a);
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++) {
+                            mma<M>(o[k][nt], a, hi[b][nt][0], hi[b][nt][1]);
+                            if constexpr (kSplit) mma<M>(o[k][nt], a, lo[b][nt][0], lo[b][nt][1]);
+                        }
+                    }
+                } else {
+                    const uint32_t row = vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
+#pragma unroll
+                    for (int k = 0; k < kSteps; k += 2) {
+                        // a lane gets bytes 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8
+                        uint32_t w[4];
+                        load_matrices_transposed(row + k * 16, w);
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            const uint32_t x = w[2 * i], y = w[2 * i + 1];
+                            const uint32_t a[4] = {E4M3::halves(__byte_perm(x, 0, 0x4420)), E4M3::halves(__byte_perm(x, 0, 0x4431)),
+                                                   E4M3::halves(__byte_perm(y, 0, 0x4420)), E4M3::halves(__byte_perm(y, 0, 0x4431))};
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++) {
+                                mma<M>(o[k + i][nt], a, hi[b][nt][0], hi[b][nt][1]);
+                                if constexpr (kSplit) mma<M>(o[k + i][nt], a, lo[b][nt][0], lo[b][nt][1]);
+                            }
+                        }
+                    }
+                }
+            }
         }
         if (++stage == S::kStages) stage = 0;
 
@@ -820,8 +850,8 @@ AttendVariant of_group(int group) {
     // more than 8 heads: two column tiles share every load; beyond 16, and for the widest rows (whose registers do not
     // suffice: 145 us, rows read twice 126), the rows are read again
     if constexpr (DP <= 128)
-        if (group > 8) return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP};
-    return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP};
+        if (group > 8) return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP, Shape<T, C, DP, 2>::kTileBits};
+    return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP, Shape<T, C, DP, 1>::kTileBits};
 }
 template <class T, class C>
 AttendVariant of(int head_dim, int group) {
@@ -843,12 +873,13 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 #if FCSIM_KV_TYPES == 0
 // weight[token] += sum over a group's heads of the softmax weights, from the logits that the first kernel left: the final
 // reference and sum of a head are known only when all of its parts are joined.  The same division of the work, without
-// overhead: a CTA takes eight tiles of (request, kv head) at a time, 16 threads and four tokens a thread for each, two
+// overhead: a CTA takes eight tiles (of 64 tokens) of (request, kv head) at a time, four tokens a thread, two
 // heads' logits at once and their sum in order.  Bound by the latency of a few dependent loads, so what matters is that
 // one round of the grid is all of it, and what does not need the logits is loaded before the first kernel has ended.
 __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(const AttendParams p) {
-    constexpr int kTiles = kThreads / (kTile / 4), kAtOnce = 2;
-    const int n_kv = p.pool.n_kv, group = p.n_heads / n_kv, mine = threadIdx.x / (kTile / 4), size = p.pool.page_size;
+    constexpr int kAtOnce = 2;
+    const int threads = 1 << (p.tile_bits - 2), tiles = kThreads / threads;  // of a tile; at a time
+    const int n_kv = p.pool.n_kv, group = p.n_heads / n_kv, mine = threadIdx.x / threads, size = p.pool.page_size;
     __shared__ Before before;
     const Division work = divide<0>(p, n_kv, true, before);  // (of the lengths alone, which the first kernel does not write)
     const int64_t first = work.first(), end = work.end();
@@ -862,7 +893,7 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     float* weight[4];  // of each token, or none; one page and 16 aligned bytes where the size of a page allows
     float old[4];
     auto load_weights = [&]() {
-        in = at.j * kTile + threadIdx.x % (kTile / 4) * 4;
+        in = (at.j << p.tile_bits) + threadIdx.x % threads * 4;
         t = at.start + in;
         aligned = size % 4 == 0 && t % 4 == 0;
         room = at.tiles_before + at.tiles <= p.logit_tiles;
@@ -889,8 +920,8 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     while (at.left > 0) {
         if (room && t < at.len) {
             float sum[4] = {0, 0, 0, 0};
-            const int64_t step = (int64_t)at.tiles * kTile;
-            const float* logit = p.logits + (int64_t)at.tiles_before * p.n_heads * kTile + at.kv * group * step + in;
+            const int64_t step = (int64_t)at.tiles << p.tile_bits;
+            const float* logit = p.logits + ((int64_t)at.tiles_before * p.n_heads << p.tile_bits) + at.kv * group * step + in;
             const float4* stats = reinterpret_cast<const float4*>(p.stats) + (int64_t)at.b * p.n_heads + at.kv * group;
             for (int h = 0; h < group; h += kAtOnce, logit += kAtOnce * step, stats += kAtOnce) {
                 float4 s[kAtOnce], x[kAtOnce];
@@ -916,7 +947,7 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
                 }
             }
         }
-        for (int i = 0; i < kTiles && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
+        for (int i = 0; i < tiles && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
         if (at.left > 0) load_weights();
     }
 }

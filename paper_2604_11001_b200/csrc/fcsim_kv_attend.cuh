@@ -4,7 +4,6 @@
 
 namespace fcsim_kv_dev {
 
-constexpr int kTile = 64;        // tokens a CTA takes at once: 16 by each of its four warps
 constexpr int kThreads = 128;
 constexpr int kWeightCtas = 6;    // CTAs of the weights' kernel on an SM (4, 6, 8, 12: 50.1, 47.1, 48.2, 51.7 us in all)
 constexpr int kMaxDevices = 64;   // devices for which answers of the runtime are remembered
@@ -20,11 +19,12 @@ struct AttendParams {
     int64_t q_row, q_head, table_row;
     int n_requests, n_heads, max_length, window, add_weight;
     float scale;
+    int tile_bits;       // tokens a CTA takes at once, of the variant
     // workspace
     int* counters;       // [grid], zero between calls: the parts that are done of the group that begins in a CTA
     float* parts;        // [grid][2][heads of a tile][head_dim + 2]
     float* stats;        // add_weight: [n_requests][n_heads][4]: largest logit, its unit, 1 / sum, -
-    float* logits;       // add_weight: per request [n_heads][tiles * kTile]
+    float* logits;       // add_weight: per request [n_heads][tiles * tokens of a tile]
     int64_t logit_tiles; // what `logits` has room for, in tiles
 };
 
@@ -33,6 +33,7 @@ struct AttendVariant {
     int (*launch)(const AttendParams&, int grid, cudaStream_t);
     int (*ctas_per_sm)(int device, int* out);  // asked once per device; also raises the kernel's limit of shared memory
     int head_cols, width;          // query heads and elements of its tile
+    int tile_bits;                 // its tokens: 64 or 128
 };
 
 // The variant for a type of q, a type of cache, a head width and a group of query heads per kv head.
