@@ -59,17 +59,17 @@ __device__ __forceinline__ void load_matrices_transposed(uint32_t a, uint32_t (&
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 template <class M>  // M: the type of the tensor-core operands
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (std::is_same<M, F16>::value)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -273,12 +273,14 @@ struct Shape {
     static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 128;     // statistics of the columns, masks of the rings, a flag
     static constexpr int kStatic = sizeof(Before) + 64;
     static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall - kStatic) / kStage; }
-    // As many CTAs on an SM as registers and two stages each allow.  More stages only queue: with three of 32 KB instead of
-    // two, SMs differ more in the rate they get, and a call ends with the slowest (131 072 tokens of one request 99 us,
-    // with two 96).
+    // As many CTAs on an SM as registers and two stages each allow, then as many stages as there is room for.  When every SM
+    // has work for long, only kFair of them are used: more only queue, SMs differ more in the rate they get, and a call
+    // ends with the slowest (131 072 tokens of one request, three stages of 32 KB 99 us, two 96).  When each CTA has one
+    // short piece, all: nothing but the loads' latency counts (16 requests of 1 024 tokens 22 -> 18 us).
     static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 && kRow <= 128 ? 3 : 2;
     static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(3) >= 2 && kRegisterCtas >= 3 ? 3 : stages(2) >= 2 ? 2 : 1;
-    static constexpr int kStages = kCtas * kStage >= 64 * 1024 || stages(kCtas) < 3 ? 2 : 3;
+    static constexpr int kStages = stages(kCtas) < 4 ? stages(kCtas) : 4;
+    static constexpr int kFair = kCtas * kStage >= 64 * 1024 || kStages < 3 ? 2 : 3;
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
     static_assert(kStages >= 2, "shared memory of a CTA");
 };
@@ -381,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 
     __shared__ Before before;
     const Division work = divide<kOverhead>(p, n_kv * head_tiles, false, before);
+    const int depth = work.cut ? S::kStages : S::kFair;  // stages in use
     Place in = {};  // the tile whose loads are issued next
     Place at = {};  // the tile that is computed next
     int cut = 0, cuts = 1;
@@ -477,14 +480,14 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     int stage = 0;
     auto start_ring = [&]() {
         if (chunks * 16 < S::kRow)  // elements beyond head_dim are never copied to: zeros
-            for (int s = 0; s < S::kStages; s++)
+            for (int s = 0; s < depth; s++)
                 for (int t = lane; t < 2 * kTokens; t += 32)
                     for (int i = chunks * 16; i < S::kRow; i += 16)
                         *reinterpret_cast<uint4*>(smem + (warp * 2 * kTokens + t) * S::kPitch + s * S::kStage + i) = make_uint4(0, 0, 0, 0);
         stage = 0;
         fetch_page();
 #pragma unroll 1
-        for (int s = 0; s < S::kStages - 1; s++) load_next(s);
+        for (int s = 0; s < depth - 1; s++) load_next(s);
     };
     if (in.left > 0) start_ring();
     while (at.left > 0) {
@@ -546,9 +549,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             }
         }
 
-        wait_group<S::kStages - 2>();
+        if (depth == 2) wait_group<0>();
+        else if (depth == 3) wait_group<1>();
+        else wait_group<2>();
         __syncwarp();
-        load_next(stage == 0 ? S::kStages - 1 : stage - 1);  // into what the last step has read
+        load_next(stage == 0 ? depth - 1 : stage - 1);  // into what the last step has read
         const uint32_t mask = masks[stage];
 
         if (mask) {  // (a warp may have no token of a request's last tile)
@@ -560,23 +565,27 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 const uint32_t row = krow + (b * 16 + (lane & 7) + ((lane >> 3) & 1) * 8) * S::kPitch + (lane >> 4) * 16;
                 if constexpr (!kNarrow) {
 #pragma unroll
-                    for (int k = 0; k < kSteps; k++) {
-                        uint32_t a[4];
-                        load_matrices(row + k * 32, a);
+                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                        uint32_t a[4][4];
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k][0], qf[nt][k][1]);
+                        for (int k = 0; k < 4; k++) load_matrices(row + (k0 + k) * 32, a[k]);
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a[k], qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
                     }
                 } else {
 #pragma unroll
-                    for (int k = 0; k < kSteps; k += 2) {
-                        uint32_t w[4];
-                        load_matrices(row + k * 16, w);
+                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                        uint32_t w[2][4];
+                        load_matrices(row + k0 * 16, w[0]);
+                        load_matrices(row + k0 * 16 + 32, w[1]);
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint32_t a[4] = {E4M3::halves(w[2 * i]), E4M3::halves(w[2 * i + 1]),
-                                                   E4M3::halves(w[2 * i] >> 16), E4M3::halves(w[2 * i + 1] >> 16)};
+                        for (int k = 0; k < 4; k++) {
+                            const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
+                            const uint32_t a[4] = {E4M3::halves(x), E4M3::halves(y), E4M3::halves(x >> 16), E4M3::halves(y >> 16)};
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k + i][0], qf[nt][k + i][1]);
+                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
                         }
                     }
                 }
@@ -660,38 +669,45 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 if constexpr (!kNarrow) {
                     const uint32_t row = vrow + (b * 16 + (lane & 7) + (which >> 1) * 8) * S::kPitch + (which & 1) * 16;
 #pragma unroll
-                    for (int k = 0; k < kSteps; k++) {
-                        uint32_t a[4];
-                        load_matrices_transposed(row + k * 32, a);
+                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                        uint32_t a[4][4];
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) {
-                            mma<M>(o[k][nt], a, hi[b][nt][0], hi[b][nt][1]);
-                            if constexpr (kSplit) mma<M>(o[k][nt], a, lo[b][nt][0], lo[b][nt][1]);
+                        for (int k = 0; k < 4; k++) load_matrices_transposed(row + (k0 + k) * 32, a[k]);
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++) mma<M>(o[k0 + k][nt], a[k], hi[b][nt][0], hi[b][nt][1]);
+                        if constexpr (kSplit) {
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+#pragma unroll
+                                for (int nt = 0; nt < NT; nt++) mma<M>(o[k0 + k][nt], a[k], lo[b][nt][0], lo[b][nt][1]);
                         }
                     }
                 } else {
                     const uint32_t row = vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
 #pragma unroll
-                    for (int k = 0; k < kSteps; k += 2) {
+                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
                         // a lane gets bytes 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8
-                        uint32_t w[4];
-                        load_matrices_transposed(row + k * 16, w);
+                        uint32_t w[2][4];
+                        load_matrices_transposed(row + k0 * 16, w[0]);
+                        load_matrices_transposed(row + k0 * 16 + 32, w[1]);
 #pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint32_t x = w[2 * i], y = w[2 * i + 1];
+                        for (int k = 0; k < 4; k++) {
+                            const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
                             const uint32_t a[4] = {E4M3::halves(__byte_perm(x, 0, 0x4420)), E4M3::halves(__byte_perm(x, 0, 0x4431)),
                                                    E4M3::halves(__byte_perm(y, 0, 0x4420)), E4M3::halves(__byte_perm(y, 0, 0x4431))};
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++) {
-                                mma<M>(o[k + i][nt], a, hi[b][nt][0], hi[b][nt][1]);
-                                if constexpr (kSplit) mma<M>(o[k + i][nt], a, lo[b][nt][0], lo[b][nt][1]);
+                                mma<M>(o[k0 + k][nt], a, hi[b][nt][0], hi[b][nt][1]);
+                                if constexpr (kSplit) mma<M>(o[k0 + k][nt], a, lo[b][nt][0], lo[b][nt][1]);
                             }
                         }
                     }
                 }
             }
         }
-        if (++stage == S::kStages) stage = 0;
+        if (++stage == depth) stage = 0;
 
         if (at.j < at.tiles - 1 && at.left > 1) {
             at.j++;
