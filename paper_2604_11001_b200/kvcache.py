@@ -22,6 +22,7 @@ from . import binding as _fb
 F16, BF16, E4M3 = 0, 1, 2
 BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET = 1, 2, 4, 8
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+_I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
 # the current device's number and a device's current stream as plain integers, without the objects around them
@@ -163,27 +164,16 @@ class PagedKV:
     # ------------------------------------------------------------------------------------------ helpers
     # A slot's calls take a few microseconds on the device: checks are plain comparisons, the argument struct is packed
     # in one go, and messages are only made when they are needed.
-    def _rows(self, x, name, shape, dtype):
-        """Row and head strides of a [tokens, heads, head_dim] tensor."""
-        if x.shape != shape or x.dtype != dtype or x.get_device() != self._index:
-            raise ValueError(f"{name}: {dtype} {list(shape)} on {self.device}, got {x.dtype} {list(x.shape)} on {x.device}")
-        row, head, one = x.stride()
-        if one != 1:
-            raise ValueError(f"{name}: head_dim has to be contiguous")
-        return row, head
+    def _refuse(self, name, what, x):
+        raise ValueError(f"{name}: {what} on {self.device}, got {x.dtype} {list(x.shape)} on {x.device}")
 
     def _table(self, table, name, n):
         """Columns of a page table."""
         shape = table.shape
-        if len(shape) != 2 or shape[0] != n or table.dtype != torch.int32 or table.get_device() != self._index:
-            raise ValueError(f"{name}: int32 [{n}, pages] on {self.device}, got {table.dtype} {list(shape)} on {table.device}")
-        if shape[1] > 1 and table.stride(1) != 1:
-            raise ValueError(f"{name}: rows have to be contiguous")
+        if len(shape) != 2 or shape[0] != n or table.dtype != _I32 or table.get_device() != self._index \
+                or not (shape[1] <= 1 or table.stride(1) == 1):
+            self._refuse(name, f"int32 [{n}, pages], rows contiguous", table)
         return shape[1]
-
-    def _flat(self, x, name, shape, dtype):
-        if x.shape != shape or x.dtype != dtype or x.get_device() != self._index or not x.is_contiguous():
-            raise ValueError(f"{name}: contiguous {dtype} {list(shape)} on {self.device}, got {x.dtype} {list(x.shape)} on {x.device}")
 
     def _call(self, entry, args, size=None):
         """Run an entry point on the current stream of the cache's device.  ``size``: the entry point that tells the size
@@ -223,33 +213,45 @@ class PagedKV:
 
         ``rope``: float32 [positions, rope_dim], cosines then sines; ``positions``: int32 [n].  ``q_norm``,
         ``k_norm``: [head_dim] weights of the norms over each head.  ``q`` may be None (nothing is returned)."""
-        n, dtype = k.shape[0], k.dtype
-        if dtype not in _WIDE:
-            raise ValueError("k: float16 or bfloat16")
-        shape = (n, self.n_kv_heads, self.head_dim)
-        k_row, k_head = self._rows(k, "k", shape, dtype)
-        v_row, v_head = self._rows(v, "v", shape, dtype)
-        self._flat(slots, "slots", (n,), torch.int64)
-        out, heads, q_row, q_head, q_at, out_at = None, 0, 0, 0, 0, 0
+        dtype, shape, index = k.dtype, k.shape, self._index
+        if dtype not in _WIDE or len(shape) != 3 or shape[1] != self.n_kv_heads or shape[2] != self.head_dim \
+                or k.get_device() != index:
+            self._refuse("k", f"float16 or bfloat16 [tokens, {self.n_kv_heads}, {self.head_dim}]", k)
+        if v.shape != shape or v.dtype != dtype or v.get_device() != index:
+            self._refuse("v", f"{dtype} {list(shape)}", v)
+        n = shape[0]
+        k_row, k_head, k_one = k.stride()
+        v_row, v_head, v_one = v.stride()
+        if slots.dtype != _I64 or slots.numel() != n or slots.get_device() != index or not slots.is_contiguous():
+            self._refuse("slots", f"contiguous int64 [{n}]", slots)
+        out, heads, q_row, q_head, q_one, q_at, out_at = None, 0, 0, 0, 1, 0, 0
         if q is not None:
-            heads = q.shape[1]
-            q_row, q_head = self._rows(q, "q", (n, heads, self.head_dim), dtype)
+            q_shape = q.shape
+            if len(q_shape) != 3 or q_shape[0] != n or q_shape[2] != self.head_dim or q.dtype != dtype or q.get_device() != index:
+                self._refuse("q", f"{dtype} [{n}, heads, {self.head_dim}]", q)
+            heads = q_shape[1]
+            q_row, q_head, q_one = q.stride()
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
             q_at, out_at = q.data_ptr(), out.data_ptr()
+        if k_one != 1 or v_one != 1 or q_one != 1:
+            raise ValueError("q, k, v: head_dim has to be contiguous")
         rope_at = positions_at = rope_dim = n_positions = 0
         if rope is not None:
-            if positions is None or rope.dim() != 2:
-                raise ValueError("rope: float32 [positions, rope_dim], with positions")
+            if rope.dim() != 2 or rope.dtype != torch.float32 or rope.get_device() != index or not rope.is_contiguous():
+                self._refuse("rope", "contiguous float32 [positions, rope_dim]", rope)
+            if positions is None or positions.dtype != _I32 or positions.numel() != n or positions.get_device() != index \
+                    or not positions.is_contiguous():
+                raise ValueError(f"positions: contiguous int32 [{n}] on {self.device}")
             n_positions, rope_dim = rope.shape
-            self._flat(rope, "rope", (n_positions, rope_dim), torch.float32)
-            self._flat(positions, "positions", (n,), torch.int32)
             rope_at, positions_at = rope.data_ptr(), positions.data_ptr()
         q_norm_at = k_norm_at = 0
         if q_norm is not None:
-            self._flat(q_norm, "q_norm", (self.head_dim,), dtype)
+            if q_norm.dtype != dtype or q_norm.numel() != self.head_dim or q_norm.get_device() != index or not q_norm.is_contiguous():
+                self._refuse("q_norm", f"contiguous {dtype} [{self.head_dim}]", q_norm)
             q_norm_at = q_norm.data_ptr()
         if k_norm is not None:
-            self._flat(k_norm, "k_norm", (self.head_dim,), dtype)
+            if k_norm.dtype != dtype or k_norm.numel() != self.head_dim or k_norm.get_device() != index or not k_norm.is_contiguous():
+                self._refuse("k_norm", f"contiguous {dtype} [{self.head_dim}]", k_norm)
             k_norm_at = k_norm.data_ptr()
         self._call(_lib.fcsim_kv_append, _APPEND.pack(
             q_at, k.data_ptr(), v.data_ptr(), out_at, q_norm_at, k_norm_at, rope_at, positions_at, slots.data_ptr(),
@@ -265,13 +267,16 @@ class PagedKV:
 
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
         only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
-        dtype = q.dtype
-        if q.dim() != 3 or dtype not in _WIDE:
-            raise ValueError("q: float16 or bfloat16 [requests, heads, head_dim]")
-        n, heads, _ = q.shape
-        q_row, q_head = self._rows(q, "q", (n, heads, self.head_dim), dtype)
+        dtype, shape, index = q.dtype, q.shape, self._index
+        if dtype not in _WIDE or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
+            self._refuse("q", f"float16 or bfloat16 [requests, heads, {self.head_dim}]", q)
+        n, heads, _ = shape
+        q_row, q_head, q_one = q.stride()
+        if q_one != 1:
+            raise ValueError("q: head_dim has to be contiguous")
         cols = self._table(table, "table", n)
-        self._flat(lengths, "lengths", (n,), torch.int32)
+        if lengths.dtype != _I32 or lengths.numel() != n or lengths.get_device() != index or not lengths.is_contiguous():
+            self._refuse("lengths", f"contiguous int32 [{n}]", lengths)
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lse = q.new_empty((n, heads), dtype=torch.float32) if return_lse else None
         self._call(_lib.fcsim_kv_attend, _ATTEND.pack(
@@ -286,10 +291,12 @@ class PagedKV:
         ``first`` oldest and the largest weights, copied in order to the pages of ``new_table`` (none of which the
         call may read).  Returns the new lengths (int32 [requests]) and the old index of every kept token (int32
         [requests, n_kv_heads, max_budget], -1 beyond)."""
-        n = lengths.shape[0]
+        n, index = lengths.numel(), self._index
         cols, new_cols = self._table(table, "table", n), self._table(new_table, "new_table", n)
-        self._flat(lengths, "lengths", (n,), torch.int32)
-        self._flat(budget, "budget", (n,), torch.int32)
+        if lengths.dtype != _I32 or lengths.get_device() != index or not lengths.is_contiguous():
+            self._refuse("lengths", "contiguous int32", lengths)
+        if budget.dtype != _I32 or budget.numel() != n or budget.get_device() != index or not budget.is_contiguous():
+            self._refuse("budget", f"contiguous int32 [{n}]", budget)
         if max_budget is None:
             max_budget = new_cols * self.page_size
         if max_budget < 0:
