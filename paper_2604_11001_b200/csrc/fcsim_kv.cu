@@ -259,6 +259,7 @@ __device__ __forceinline__ uint32_t order_key(float w) {
 
 constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kMaxCluster = 8;            // CTAs that share a row: the portable size of a cluster
+constexpr int64_t kFusedBytes = 128 * 1024;  // what a CTA of the selection copies itself
 constexpr int kMaxFours = 12 * 1024;      // fours of keys a CTA keeps in shared memory (192 KB)
 
 // What request r keeps: `keep` tokens, of which [0, lo) and [hi, n) are sure and `places` go to the largest of [lo, hi).
@@ -282,16 +283,61 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* stat
     return c;
 }
 
+// Rows of K and V that a lane of the copies has in flight.  A row waits for its index and its page before it is read, so
+// more threads hide more than more rows of each: 64 requests to 1 024 tokens, 1, 2, 4, 8 rows: 82, 81, 89, 124 us in all.
+constexpr int kMoveRows = 2;
+
+// Copies kept rows [row0, row0 + THREADS / LPR * kMoveRows) of one kv head of request r: 16 bytes a lane, LPR lanes a row.
+template <int LPR, int THREADS>
+__device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, int keep, int row0) {
+    constexpr int kAtOnce = THREADS / LPR;
+    const int lane = threadIdx.x % LPR, chunks = p.pool.head_dim * p.bytes / 16, size = p.pool.page_size;
+    const int32_t* kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
+    row0 += threadIdx.x / LPR;
+    int64_t dst[kMoveRows];
+    uint4 k[kMoveRows], v[kMoveRows];
+#pragma unroll
+    for (int i = 0; i < kMoveRows; i++) {
+        const int row = row0 + i * kAtOnce;
+        dst[i] = -1;
+        if (row >= keep) continue;
+        const int t = kept[row];
+        const int from = page_of(p.pool, t), into = page_of(p.pool, row);
+        const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
+        if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
+            flag(p.status, FCSIM_KV_BAD_PAGE);
+            continue;
+        }
+        if (lane < chunks) {
+            const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            dst[i] = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+            k[i] = *reinterpret_cast<const uint4*>(p.pool.k + src);
+            v[i] = *reinterpret_cast<const uint4*>(p.pool.v + src);
+        }
+        if (lane == 0)
+            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
+                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveRows; i++)
+        if (dst[i] >= 0) {
+            *reinterpret_cast<uint4*>(p.pool.k + dst[i]) = k[i];
+            *reinterpret_cast<uint4*>(p.pool.v + dst[i]) = v[i];
+        }
+}
+
 // Which tokens one kv head of one request keeps, by one cluster.  Every CTA takes an equal slice of the candidates and
 // keeps their keys in shared memory, so that the weights are read once; four counts by 8 bits each, from the top, give
 // the smallest key that is kept and how many of its equals are.  The counts of the CTAs meet over distributed shared
 // memory, one cluster barrier for each (every count has a buffer of its own).  Places then follow from running sums in
 // the order of the tokens.  A thread holds four neighbouring tokens at a time: they share a page where its size allows,
 // and a sum over a warp covers 128 of them.  Bound by the latency of these few passes: a slice is 16 to 32 KB.
-__global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const EvictParams p, const int capacity) {
+// With LPR the same cluster copies what it has selected (its CTAs in turn); without, a second kernel does.
+template <int LPR>
+__global__ void __launch_bounds__(kSelectThreads, 2) fcsim_kv_select_kernel(const EvictParams p, const int capacity) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    cudaTriggerProgrammaticLaunchCompletion();  // the copies may line up; they wait for this grid's end
+    if (LPR == 0) cudaTriggerProgrammaticLaunchCompletion();  // the copies may line up; they wait for this grid's end
     extern __shared__ uint4 keys[];
     __shared__ uint32_t counts[4][256], sums[256];
     __shared__ int warp_sums[kSelectWarps], warp_equals[kSelectWarps], mine, mine_equal, chosen[2];
@@ -305,7 +351,20 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         else if (i >= c.lo + c.places) kept[i] = c.n - c.keep + i;
     }
     if (h == 0 && rank == 0 && tid == 0) p.new_lengths[r] = c.keep;
-    if (c.places == 0) return;  // the same for the whole cluster
+    auto copy = [&]() {
+        if constexpr (LPR > 0)
+            for (int row = rank * (kSelectThreads / LPR * kMoveRows); row < c.keep; row += ctas * (kSelectThreads / LPR * kMoveRows))
+                move_rows<LPR, kSelectThreads>(p, r, h, c.keep, row);
+    };
+    auto meet = [&]() {  // a barrier of the cluster costs 0.5 us, one of a CTA a tenth of it
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+    };
+    if (c.places == 0) {  // the same for the whole cluster
+        meet();
+        copy();
+        return;
+    }
 
     // tokens by fours; key 0 for those of the first and last four that are no candidates
     const int four0 = c.lo / 4, fours = (c.hi + 3) / 4 - four0, each = (fours + ctas - 1) / ctas;
@@ -349,10 +408,6 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         return k;
     };
     auto key = [&](int i) { return resident ? keys[i] : read_keys(i); };
-    auto meet = [&]() {  // a barrier of the cluster costs 0.5 us, one of a CTA a tenth of it
-        if (ctas > 1) cluster.sync();
-        else __syncthreads();
-    };
     for (int i = tid; i < 4 * 256; i += kSelectThreads) counts[0][i] = 0;
     __syncthreads();
     uint32_t threshold = 0;
@@ -463,57 +518,41 @@ __global__ void __launch_bounds__(kSelectThreads) fcsim_kv_select_kernel(const E
         const uint32_t all = __shfl_sync(~0u, upto, 31);
         above += (int)(all & 0xffff), equal += (int)(all >> 16);
     }
-    if (ctas > 1) cluster.sync();  // the others may still read this CTA's counts
+    meet();  // the others may still read this CTA's counts; all of the row's indexes are written
+    copy();
 }
 
-// Rows of K and V that a lane of the copies has in flight.  A row waits for its index and its page before it is read, so
-// more threads hide more than more rows of each: 64 requests to 1 024 tokens, 1, 2, 4, 8 rows: 82, 81, 89, 124 us in all.
-constexpr int kMoveRows = 2;
-
-// Copies the kept rows: 16 bytes a lane, LPR lanes a row.  Bound by memory.
+// The copies as a kernel of their own, bound by memory.
 template <int LPR>
 __global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p) {
-    constexpr int kAtOnce = 256 / LPR, kRows = kMoveRows;
-    const int r = blockIdx.z, h = blockIdx.y, lane = threadIdx.x % LPR;
     cudaGridDependencySynchronize();
-    const Cut c = cut_of(p, r, nullptr);
-    const int row0 = blockIdx.x * kAtOnce * kRows + threadIdx.x / LPR;
-    const int chunks = p.pool.head_dim * p.bytes / 16, size = p.pool.page_size;
-    const int32_t* kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
-    int64_t dst[kRows];
-    uint4 k[kRows], v[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; i++) {
-        const int row = row0 + i * kAtOnce;
-        dst[i] = -1;
-        if (row >= c.keep) continue;
-        const int t = kept[row];
-        const int from = page_of(p.pool, t), into = page_of(p.pool, row);
-        const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
-        if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
-            flag(p.status, FCSIM_KV_BAD_PAGE);
-            continue;
-        }
-        if (lane < chunks) {
-            const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            dst[i] = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            k[i] = *reinterpret_cast<const uint4*>(p.pool.k + src);
-            v[i] = *reinterpret_cast<const uint4*>(p.pool.v + src);
-        }
-        if (lane == 0)
-            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
-                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
-    }
-#pragma unroll
-    for (int i = 0; i < kRows; i++)
-        if (dst[i] >= 0) {
-            *reinterpret_cast<uint4*>(p.pool.k + dst[i]) = k[i];
-            *reinterpret_cast<uint4*>(p.pool.v + dst[i]) = v[i];
-        }
+    const int r = blockIdx.z, h = blockIdx.y;
+    move_rows<LPR, 256>(p, r, h, cut_of(p, r, nullptr).keep, blockIdx.x * (256 / LPR * kMoveRows));
 }
 
 template <int LPR>
+int launch_select(const EvictParams& p, dim3 grid, int capacity, int device, cudaStream_t stream) {
+    static std::atomic<bool> raised[kMaxDevices];
+    if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_select_kernel<LPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxFours * 16);
+        if (e != cudaSuccess) return cuda_status(e);
+        if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = dim3(kSelectThreads);
+    config.dynamicSmemBytes = (size_t)capacity * 16;
+    config.stream = stream;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = grid.x, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&config, fcsim_kv_select_kernel<LPR>, (EvictParams)p, (int)capacity));
+}
+template <int LPR>
 int launch_move(const EvictParams& p, int n_requests, cudaStream_t stream) {
+    if (p.max_budget == 0) return FCSIM_OK;
     const int rows = 256 / LPR * kMoveRows;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((p.max_budget + rows - 1) / rows, p.pool.n_kv, n_requests);
@@ -749,25 +788,18 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     const int fours = p.max_length / 4 + 2;
     while (ctas < kMaxCluster && (fours + ctas - 1) / ctas > kMaxFours) ctas *= 2;
     const int capacity = std::min((fours + ctas - 1) / ctas, kMaxFours);
-    static std::atomic<bool> raised[kMaxDevices];
-    if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxFours * 16);
-        if (e != cudaSuccess) return cuda_status(e);
-        if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
-    }
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(ctas, p.pool.n_kv, a->n_requests);
-    config.blockDim = dim3(kSelectThreads);
-    config.dynamicSmemBytes = (size_t)capacity * 16;
-    config.stream = stream;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = ctas, cluster.val.clusterDim.y = 1, cluster.val.clusterDim.z = 1;
-    config.attrs = &cluster;
-    config.numAttrs = 1;
-    if ((rc = cuda_status(cudaLaunchKernelEx(&config, fcsim_kv_select_kernel, (const EvictParams)p, capacity))) != FCSIM_OK) return rc;
-    if (p.max_budget == 0) return FCSIM_OK;
+    const dim3 grid(ctas, p.pool.n_kv, a->n_requests);
     const int chunks = p.pool.head_dim * p.bytes / 16;
+    // One kernel when there is little to copy (4 requests of 515 tokens to 256: 12.1 us a call, with two 13.9); else a second
+    // one spreads the copies better (64 requests to 1 024 tokens of 128 elements: 82 us, with one 93).
+    const int64_t row_bytes = (int64_t)p.max_budget * p.pool.head_dim * p.bytes * 2;
+    if (row_bytes <= kFusedBytes * ctas) {
+        if (chunks <= 4) return launch_select<4>(p, grid, capacity, device, stream);
+        if (chunks <= 8) return launch_select<8>(p, grid, capacity, device, stream);
+        if (chunks <= 16) return launch_select<16>(p, grid, capacity, device, stream);
+        return launch_select<32>(p, grid, capacity, device, stream);
+    }
+    if ((rc = launch_select<0>(p, grid, capacity, device, stream)) != FCSIM_OK) return rc;
     if (chunks <= 4) return launch_move<4>(p, a->n_requests, stream);
     if (chunks <= 8) return launch_move<8>(p, a->n_requests, stream);
     if (chunks <= 16) return launch_move<16>(p, a->n_requests, stream);
