@@ -660,12 +660,13 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
     const int64_t tiles = (seen + (1 << p.tile_bits) - 1) >> p.tile_bits, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
-    l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most, p.n_requests)}));
+    l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most + most / 3 + 1, p.n_requests)}));
     // the kernel counts the tiles of all requests, and the work of a CTA, in 32 bits
     if ((tiles + 16) * p.n_requests > 0x7fffffff || (most + (int64_t)p.n_requests * 16 * p.n_heads) / l->grid >= 0x7fffffff) return FCSIM_EINVAL;
-    l->counters = (size_t)l->grid * 4;
+    const size_t workers = (size_t)l->grid * (kThreads / 32);
+    l->counters = workers * 4;
     l->parts = (l->counters + 15) / 16 * 16;
-    l->stats = l->parts + (size_t)2 * l->grid * v.head_cols * (v.width + 2) * 4;
+    l->stats = l->parts + 2 * workers * v.head_cols * (v.width + 2) * 4;
     l->logit_tiles = logit_tiles(p);
     l->logits = l->stats + (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0);
     l->bytes = l->stats + attend_kept(p);

@@ -92,19 +92,27 @@ template <class T>
 struct OperandOf<T, E4M3> { using type = F16; };
 
 // ---------------------------------------------------------------------------------------------- the walk over the work
-// The work is counted in units: a tile is one, and every (request, kv head, head tile) group counts kOverhead more for its
-// start and its end (q, the warps' merge, the output), which is what they cost beside a tile.  The units before a
-// group's first tile stand for these.  When there are too few tiles to keep every CTA busy for long, the groups are cut
-// into equal pieces instead and each CTA gets one: fewer starts, ends and joins one after another.
-constexpr int kOverhead = 3;
-constexpr int kPieceLeast = 4;   // tiles of a piece at least: below that, joining costs more than it spreads
-constexpr int kPieceMost = 16;   // tiles of a piece from which equal shares are better
+// The work is counted in units: a tile is one, and every (request, kv head, head tile) group counts some more for its start
+// and its end (q, the warps' merge, the output), which is what they cost beside a tile.  The units before a group's
+// first tile stand for these.  Three ways to divide them, by what the lengths add up to:
+//   shares  every CTA an equal stretch of units, a tile at a time by its four warps;
+//   cut     few tiles: the groups are cut into equal pieces and each CTA gets one, so that starts, ends and joins do not follow
+//           one another (16 requests of 1 024 tokens);
+//   alone   short requests in number: every warp an equal stretch, a tile being its own 16 or 32 tokens: a group of one or two
+//           tiles is nearly all start and end, and four at a time hide what one waits for (400 requests of up to 70 tokens,
+//           64 heads on 8: 56 -> 32 us; 512 of 300: 130 -> 115; with less than two groups a warp most are cut and joined, and
+//           shares are better: 400 x 5 kv heads of 64 elements 20 us, alone 28).
+constexpr int kOverhead = 3;       // units of a group's start and end: shares
+constexpr int kOverheadAlone = 3;  // alone
+constexpr int kPieceLeast = 4;     // tiles of a piece at least: below that, joining costs more than it spreads
+constexpr int kPieceMost = 16;     // tiles of a piece from which equal shares are better
+constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
     int b, kv, ht, j, tiles, start, len;
-    int left;              // units from this tile to the end of the CTA's stretch; none: the place is beyond it
-    int tiles_before;      // tiles of the requests before b
+    int left;              // units from this tile to the end of the worker's stretch; none: the place is beyond it
+    int tiles_before;      // tiles (of a CTA) of the requests before b
 };
 
 __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
@@ -114,46 +122,48 @@ __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
 __device__ __forceinline__ int start_of(const AttendParams& p, int len) {
     return p.window > 0 && len > p.window ? len - p.window : 0;
 }
-__device__ __forceinline__ int tiles_of(const AttendParams& p, int len) {
-    return (len - start_of(p, len) + (1 << p.tile_bits) - 1) >> p.tile_bits;
+__device__ __forceinline__ int tiles_of(const AttendParams& p, int len, int bits) {
+    return (len - start_of(p, len) + (1 << bits) - 1) >> bits;
 }
-__device__ __forceinline__ void enter(const AttendParams& p, Place& w, int b) {
+
+// The division of the units [0, total) among the workers (CTAs or warps): worker i has [i * share, (i + 1) * share).  It
+// depends on the lengths and the grid alone, so the same call gives the same sums in the same order.
+// With `cut`, a unit is a piece of at most `cut` tiles of one group, and a share is one unit.
+struct Division {
+    int64_t total, share;
+    int cut, over, bits;  // bits: of the tokens of a tile
+    bool alone;
+    __device__ __forceinline__ int worker(int warp) const { return alone ? blockIdx.x * (kThreads / 32) + warp : blockIdx.x; }
+    __device__ __forceinline__ int64_t first(int worker) const { return min(total, worker * share); }
+    __device__ __forceinline__ int64_t end(int worker) const { return min(total, (worker + 1) * share); }
+    __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles ? tiles + over : 0; }
+};
+
+__device__ __forceinline__ void enter(const AttendParams& p, const Division& d, Place& w, int b) {
     w.b = b;
     w.len = length_of(p, b);
     w.start = start_of(p, w.len);
-    w.tiles = tiles_of(p, w.len);
+    w.tiles = tiles_of(p, w.len, d.bits);
 }
 // The next tile, if the stretch has one more.
-template <int OVERHEAD>
-__device__ __forceinline__ void advance(const AttendParams& p, Place& w, int n_kv, int head_tiles) {
+__device__ __forceinline__ void advance(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
     w.left--;
     if (++w.j < w.tiles) return;
-    w.left -= OVERHEAD;
+    w.left -= d.over;
     if (w.left <= 0) return;
     w.j = 0;
     if (++w.ht < head_tiles) return;
     w.ht = 0;
     if (++w.kv < n_kv) return;
     w.kv = 0;
-    w.tiles_before += w.tiles;
-    do enter(p, w, w.b + 1);
+    w.tiles_before += tiles_of(p, w.len, p.tile_bits);
+    do enter(p, d, w, w.b + 1);
     while (w.tiles == 0);
 }
 
-// The division of the units [0, total) among the CTAs: CTA i has [i * share, (i + 1) * share).  It depends on the lengths
-// and the grid alone, so the same call gives the same sums in the same order.
-// With `cut`, a unit is a piece of at most `cut` tiles of one group, and a share is one unit.
-struct Division {
-    int64_t total, share;
-    int cut;
-    __device__ __forceinline__ int64_t first() const { return min(total, blockIdx.x * share); }
-    __device__ __forceinline__ int64_t end() const { return min(total, (blockIdx.x + 1) * share); }
-    template <int OVERHEAD>
-    __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles ? tiles + OVERHEAD : 0; }
-};
 // What the threads' stretches of the requests add up to before each of them.
 struct Before {
-    int tiles[kThreads], units[kThreads + 1];  // (units: of one of a request's groups)
+    int tiles[kThreads], units[kThreads + 1];  // (tiles of a CTA; units of one of a request's groups)
     int warps[2][kThreads / 32];
 };
 
@@ -177,38 +187,46 @@ __device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_
     }
 }
 
-// Adds up the tiles of all requests (less than 2^31: the host refuses more; a request has `per` groups) and divides them; `plain`: equal shares and no more.
-template <int OVERHEAD>
-__device__ __forceinline__ Division divide(const AttendParams& p, int per, bool plain, Before& before) {
+// Adds up the tiles of all requests (less than 2^31: the host refuses more; a request has `per` groups) and divides them.
+// `warp_bits`: of a warp's tokens; 0 = equal shares without overhead and no other way.
+__device__ __forceinline__ Division divide(const AttendParams& p, int per, int warp_bits, Before& before) {
     const int tid = threadIdx.x;
     const int each = (p.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, p.n_requests), b1 = min(b0 + each, p.n_requests);
     int tiles = 0, live = 0, all_tiles, all_live;
     for (int b = b0; b < b1; b++) {
-        const int t = tiles_of(p, length_of(p, b));
+        const int t = tiles_of(p, length_of(p, b), p.tile_bits);
         tiles += t;
         live += t > 0;
     }
     sums_before(before, tiles, live, all_tiles, all_live);
     Division d;
-    int all_units = all_tiles + OVERHEAD * all_live, units = tiles + OVERHEAD * live;
-    d.total = (int64_t)all_units * per;
-    d.share = max((int64_t)1, (d.total + gridDim.x - 1) / gridDim.x);
     d.cut = 0;
+    d.over = warp_bits ? kOverhead : 0;
+    d.bits = p.tile_bits;
+    d.alone = false;
     const int64_t groups = (int64_t)all_live * per, spare = gridDim.x - groups;
-    if (!plain && spare > 0 && 4 * groups <= 3 * (int64_t)gridDim.x) {
-        const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
-        if (piece <= kPieceMost) {
-            d.cut = (int)piece;
-            int none = 0, all_none;
-            units = 0;
-            for (int b = b0; b < b1; b++) units += d.units<OVERHEAD>(tiles_of(p, length_of(p, b)));
-            __syncthreads();
-            sums_before(before, units, none, all_units, all_none);
-            d.total = (int64_t)all_units * per;
-            d.share = 1;
+    if (warp_bits) {
+        if (4 * groups <= 3 * (int64_t)gridDim.x) {
+            const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
+            if (piece <= kPieceMost) d.cut = (int)piece;
+        } else if (all_tiles <= (int64_t)kAloneMost * all_live && groups >= 2 * (int64_t)gridDim.x * (kThreads / 32)) {
+            d.alone = true;
+            d.over = kOverheadAlone;
+            d.bits = warp_bits;
         }
     }
+    int all_units = all_tiles + d.over * all_live, units = tiles + d.over * live;
+    if (d.cut || d.alone) {
+        int none = 0, all_none;
+        units = 0;
+        for (int b = b0; b < b1; b++) units += d.units(tiles_of(p, length_of(p, b), d.bits));
+        __syncthreads();
+        sums_before(before, units, none, all_units, all_none);
+    }
+    const int workers = d.alone ? gridDim.x * (kThreads / 32) : gridDim.x;
+    d.total = (int64_t)all_units * per;
+    d.share = d.cut ? 1 : max((int64_t)1, (d.total + workers - 1) / workers);
     before.tiles[tid] = tiles;
     before.units[tid] = units;
     if (tid == 0) before.units[kThreads] = all_units;
@@ -216,33 +234,39 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, bool 
     return d;
 }
 
-// The first tile of the units [first, end), first < end.  (They are less than 2^31: the host refuses more.)
+// The first tile of a warp's worker, if it has units (less than 2^31: the host refuses more).
 // Pieces that are cut to fit: which of the group's `cuts` this is.
-template <int OVERHEAD>
-__device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head_tiles, const Division& d, int64_t first, int64_t end,
-                                       const Before& before, Place& w, int& cut, int& cuts) {
-    __shared__ int64_t found_units;
-    __shared__ int found_request, found_tiles;
-    const int tid = threadIdx.x, per = n_kv * head_tiles;
-    int64_t units = (int64_t)before.units[tid] * per;
-    if (first >= units && first < (int64_t)before.units[tid + 1] * per) {
-        int tiles = before.tiles[tid];
-        int b = tid * ((p.n_requests + kThreads - 1) / kThreads);
+__device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head_tiles, const Division& d, const Before& before, Place& w,
+                                       int& cut, int& cuts) {
+    constexpr int kWarps = kThreads / 32;
+    __shared__ int64_t found_units[kWarps];
+    __shared__ int found_request[kWarps], found_tiles[kWarps];
+    const int tid = threadIdx.x, warp = tid >> 5, per = n_kv * head_tiles, each = (p.n_requests + kThreads - 1) / kThreads;
+    const int64_t units0 = (int64_t)before.units[tid] * per, units1 = (int64_t)before.units[tid + 1] * per;
+    for (int i = 0; i < (d.alone ? kWarps : 1); i++) {
+        const int64_t first = d.first(d.worker(i));
+        if (first < units0 || first >= units1) continue;
+        int64_t units = units0;
+        int tiles = before.tiles[tid], b = tid * each;
         for (;; b++) {
-            const int t = tiles_of(p, length_of(p, b));
-            const int64_t u = (int64_t)d.units<OVERHEAD>(t) * per;
+            const int n = length_of(p, b);
+            const int64_t u = (int64_t)d.units(tiles_of(p, n, d.bits)) * per;
             if (units + u > first) break;
-            tiles += t, units += u;
+            tiles += tiles_of(p, n, p.tile_bits), units += u;
         }
-        found_request = b;
-        found_tiles = tiles;
-        found_units = units;
+        found_request[i] = b;
+        found_tiles[i] = tiles;
+        found_units[i] = units;
     }
     __syncthreads();
-    enter(p, w, found_request);
-    w.tiles_before = found_tiles;
-    const int64_t in = first - found_units;
-    const int cost = d.units<OVERHEAD>(w.tiles);
+    const int mine = d.alone ? warp : 0;
+    const int64_t first = d.first(d.worker(warp)), end = d.end(d.worker(warp));
+    w.left = 0;
+    if (first >= end) return;
+    enter(p, d, w, found_request[mine]);
+    w.tiles_before = found_tiles[mine];
+    const int64_t in = first - found_units[mine];
+    const int cost = d.units(w.tiles);
     const int r = (int)(in / cost), x = (int)(in - (int64_t)r * cost);
     w.kv = r / head_tiles;
     w.ht = r - w.kv * head_tiles;
@@ -251,10 +275,9 @@ __device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head
         w.j = (int)((int64_t)w.tiles * x / cost);
         w.left = (int)((int64_t)w.tiles * (x + 1) / cost) - w.j;
     } else {
-        w.j = max(0, x - OVERHEAD);
-        w.left = (int)(end - first) - max(0, OVERHEAD - x);
+        w.j = max(0, x - d.over);
+        w.left = (int)(end - first) - max(0, d.over - x);
     }
-    __syncthreads();  // what was found may be overwritten
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
@@ -273,12 +296,12 @@ struct Shape {
     static constexpr int kSmall = 3 * 4 * 8 * NT * 4 + 128;     // statistics of the columns, masks of the rings, a flag
     static constexpr int kStatic = sizeof(Before) + 64;
     static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall - kStatic) / kStage; }
-    // As many CTAs on an SM as registers and two stages each allow, then as many stages as there is room for.  When every SM
+    // As many CTAs on an SM (three at most) as registers and two stages each allow, then as many stages as there is room for.  When every SM
     // has work for long, only kFair of them are used: more only queue, SMs differ more in the rate they get, and a call
     // ends with the slowest (131 072 tokens of one request, three stages of 32 KB 99 us, two 96).  When each CTA has one
     // short piece, all: nothing but the loads' latency counts (16 requests of 1 024 tokens 22 -> 18 us).
-    static constexpr int kRegisterCtas = DP * NT <= 64 ? 4 : DP * NT <= 128 && kRow <= 128 ? 3 : 2;
-    static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(3) >= 2 && kRegisterCtas >= 3 ? 3 : stages(2) >= 2 ? 2 : 1;
+    static constexpr int kRegisterCtas = DP * NT <= 128 && kRow <= 128 ? 3 : 2;
+    static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(2) >= 2 ? 2 : 1;
     static constexpr int kStages = stages(kCtas) < 4 ? stages(kCtas) : 4;
     static constexpr int kFair = kCtas * kStage >= 64 * 1024 || kStages < 3 ? 2 : 3;
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
@@ -296,7 +319,7 @@ __device__ __forceinline__ void finish(const AttendParams& p, int64_t head, floa
 // dependent load costs a microsecond or two: as many whole parts as the buffer holds are copied at once.
 // (A function of its own, so that it takes no registers from the loop over the tiles.)
 template <class T, int DP, int NT>
-__device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffer_bytes, int first_cta, int parts, int cols,
+__device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffer_bytes, int first_worker, int parts, int cols,
                                   int64_t head0, float vscale, const float* col_unit) {
     constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2), kOutputs = kCols * (DP / 4) / kThreads;
     static_assert(kPartSize % 4 == 0 && kCols * (DP / 4) % kThreads == 0, "part layout");
@@ -310,7 +333,7 @@ __device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffe
         const int n = min(room, parts - k0);
         const uint32_t dst = smem_address(buffer);
         for (int k = 0; k < n; k++) {
-            const float* src = p.parts + (2 * (int64_t)(first_cta + k0 + k) + (k0 + k == 0 ? 1 : 0)) * kPartSize;
+            const float* src = p.parts + (2 * (int64_t)(first_worker + k0 + k) + (k0 + k == 0 ? 1 : 0)) * kPartSize;
             for (int i = threadIdx.x; i < kPartSize / 4; i += kThreads) copy16(dst + (k * kPartSize + i * 4) * 4, src + i * 4);
         }
         commit();
@@ -349,6 +372,32 @@ __device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffe
     }
 }
 
+// The same for one head by one warp: the few groups that lie across the stretches of warps that work alone.
+template <class T, int DP, int NT>
+__device__ __noinline__ void join_alone(const AttendParams& p, int first_worker, int parts, int col, int64_t head0, float vscale, float unit) {
+    constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2);
+    const int lane = threadIdx.x & 31, D = p.pool.head_dim;
+    auto part = [&](int k) { return p.parts + (2 * (int64_t)(first_worker + k) + (k == 0 ? 1 : 0)) * kPartSize; };
+    float top = -INFINITY;
+    for (int k = 0; k < parts; k++) top = fmaxf(top, __ldcg(part(k) + kCols * DP + col * 2));
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int d = lane * 4; d < D; d += 128) {
+        float4 z = make_float4(0, 0, 0, 0);
+        float sum = 0;
+        for (int k = 0; k < parts; k++) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(k) + kCols * DP + col * 2));
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(part(k) + col * DP + d));
+            const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * unit);
+            sum += f * ml.y;
+            z.x += f * v.x, z.y += f * v.y, z.z += f * v.z, z.w += f * v.w;
+        }
+        const float f = sum == 0.0f ? 0.0f : vscale / sum;
+        *reinterpret_cast<uint2*>(p.out + ((head0 + col) * D + d) * 2) =
+            sum == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z.x * f, z.y * f), T::pack(z.z * f, z.w * f));
+        if (d == 0) finish(p, head0 + col, top, sum, unit);
+    }
+}
+
 template <class T, class C, int DP, int NT>
 __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv_attend_kernel(const __grid_constant__ AttendParams p) {
     using S = Shape<T, C, DP, NT>;
@@ -382,7 +431,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     }
 
     __shared__ Before before;
-    const Division work = divide<kOverhead>(p, n_kv * head_tiles, false, before);
+    const Division work = divide(p, n_kv * head_tiles, kTokens == 32 ? 5 : 4, before);
+    const int worker = work.worker(warp), step = 1 << work.bits, offset = work.alone ? 0 : warp * kTokens;  // tokens: of a tile; of this warp's first
     const int depth = work.cut ? S::kStages : S::kFair;  // stages in use
     Place in = {};  // the tile whose loads are issued next
     Place at = {};  // the tile that is computed next
@@ -402,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * S::kTile + warp * kTokens + lane % kTokens, i = page_of(p.pool, t);
+        const int t = in.start + in.j * step + offset + lane % kTokens, i = page_of(p.pool, t);
         place = t - i * p.pool.page_size;
         page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
     };
@@ -418,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             const bool good = (unsigned)page < (unsigned)p.pool.n_pages;
             const uint32_t mask = __ballot_sync(~0u, good) & kAll;
             if (lane == 0) masks[stage] = mask;  // for the computation of this tile
-            if (mask != kAll && !good && in.start + in.j * S::kTile + warp * kTokens + lane % kTokens < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
+            if (mask != kAll && !good && in.start + in.j * step + offset + lane % kTokens < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
             const int64_t head = in.kv * p.pool.stride_head;
 #pragma unroll
             for (int b = 0; b < kSub; b++) {
@@ -455,10 +505,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     }
                 }
             }
-            advance<kOverhead>(p, in, n_kv, head_tiles);
+            advance(p, work, in, n_kv, head_tiles);
             if (in.left > 0) {
                 fetch_page();
-                if (in.j == 0 && warp == 0) fetch_queries();
+                if (in.j == 0 && (warp == 0 || work.alone)) fetch_queries();
             }
         }
         commit();
@@ -470,11 +520,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     float unit[NT][2], m[NT][2], limit[NT][2], l[NT][2], o[kSteps][NT][4];
     int col0 = 0, cols = 0;
     float* logits = nullptr;  // of this lane's first head and first token of a tile
+    int64_t logit_row = 0;
     const float flip = p.scale < 0 ? -1.0f : 1.0f;  // a negative scale turns the order around: turn q instead
 
-    const int64_t first = work.first(), end = work.end();
-    if (first >= end) return;
-    locate<kOverhead>(p, n_kv, head_tiles, work, first, end, before, in, cut, cuts);
+    const int64_t first = work.first(worker), end = work.end(worker);
+    locate(p, n_kv, head_tiles, work, before, in, cut, cuts);
+    if (in.left <= 0) return;  // a CTA whole, or a warp that works alone and meets no barrier
     at = in;
     bool fresh = true;
     int stage = 0;
@@ -497,9 +548,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             col0 = at.ht * kCols;
             cols = min(kCols, group - col0);
             logits = nullptr;
-            if (p.add_weight && at.tiles_before + at.tiles <= p.logit_tiles)
-                logits = p.logits + ((int64_t)at.tiles_before * p.n_heads + (int64_t)(kv * group + col0 + 2 * (lane & 3)) * at.tiles) * S::kTile +
-                         warp * kTokens + lane / 4;
+            const int cta_tiles = tiles_of(p, at.len, S::kTileBits);
+            logit_row = (int64_t)cta_tiles * S::kTile;
+            if (p.add_weight && at.tiles_before + cta_tiles <= p.logit_tiles)
+                logits = p.logits + (int64_t)at.tiles_before * S::kTile * p.n_heads + (kv * group + col0 + 2 * (lane & 3)) * logit_row + offset + lane / 4;
             const float kscale = kNarrow ? p.pool.k_scale[kv] : 1.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
@@ -595,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
                 if (logits) {
-                    float* x = logits + at.j * S::kTile + (int64_t)(nt * 8) * at.tiles * S::kTile;
+                    float* x = logits + at.j * step + nt * 8 * logit_row;
 #pragma unroll
                     for (int i = 0; i < 2; i++)
                         if (nt * 8 + 2 * (lane & 3) + i < cols) {
@@ -604,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                                 x[16 * b] = s[b][nt][i];
                                 x[16 * b + 8] = s[b][nt][2 + i];
                             }
-                            x += (int64_t)at.tiles * S::kTile;
+                            x += logit_row;
                         }
                 }
                 if (mask != kAll) {
@@ -714,23 +766,109 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             at.left--;
             continue;
         }
-        // ---------------------------------------------------------------- end of this CTA's part of (request, head tile)
+        // ---------------------------------------------------------------- end of this worker's part of a group
+        // the units of the group's tiles, and the workers that have them
+        const int64_t group_first = end - at.left - at.j, group_end = group_first + at.tiles;
+        int first_worker = worker, last_worker = worker;
+        if (work.cut) {
+            first_worker -= cut;
+            last_worker = first_worker + cuts - 1;
+        } else {
+            if (group_first < first) first_worker = (int)(group_first / work.share);
+            if (group_end > end) last_worker = (int)((group_end - 1) / work.share);
+        }
+        const int parts = last_worker - first_worker + 1;
+        const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
+        const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
+        constexpr int kPartSize = kCols * (DP + 2);
+        // a worker leaves at most two parts: of a group that began before it (0), and of one that goes on behind it (1)
+        float* const my_part = p.parts + (2 * (int64_t)worker + (first_worker == worker ? 1 : 0)) * kPartSize;
+        int* const counter = p.counters + first_worker;
 #pragma unroll
         for (int nt = 0; nt < NT; nt++)
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                float x = l[nt][i];
-                x += __shfl_xor_sync(~0u, x, 4);
-                x += __shfl_xor_sync(~0u, x, 8);
-                x += __shfl_xor_sync(~0u, x, 16);
-                l[nt][i] = x;
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 4);
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 8);
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 16);
+            }
+        if (work.alone) {
+            if (parts == 1) {
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    float f[2];
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const int col = nt * 8 + 2 * (lane & 3) + i;
+                        f[i] = l[nt][i] == 0.0f ? 0.0f : vscale / l[nt][i];
+                        if (lane < 4 && col < cols) finish(p, head0 + col, limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i], l[nt][i], unit[nt][i]);
+                    }
+                    // two heads a lane become two or four neighbouring elements of one head: lane / 4
+                    const bool real = nt * 8 + lane / 4 < cols;
+                    char* const row = p.out + (head0 + nt * 8 + lane / 4) * D * 2;
+#pragma unroll
+                    for (int k = 0; k < kSteps; k++) {
+                        const uint32_t x = transpose8x8(T::pack(o[k][nt][0] * f[0], o[k][nt][1] * f[1]));
+                        const uint32_t y = transpose8x8(T::pack(o[k][nt][2] * f[0], o[k][nt][3] * f[1]));
+                        if constexpr (kNarrow) {
+                            const int d = k * 16 + 4 * (lane & 3);
+                            if (real && d < D) *reinterpret_cast<uint2*>(row + d * 2) = make_uint2(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+                        } else {
+                            const int d = k * 16 + 2 * (lane & 3);
+                            if (real && d < D) *reinterpret_cast<uint32_t*>(row + d * 2) = x;
+                            if (real && d + 8 < D) *reinterpret_cast<uint32_t*>(row + (d + 8) * 2) = y;
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int col = nt * 8 + 2 * (lane & 3) + (i & 1);
+                        if (i < 2 && lane < 4)
+                            *reinterpret_cast<float2*>(my_part + kCols * DP + col * 2) =
+                                make_float2(limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i], l[nt][i]);
+#pragma unroll
+                        for (int k = 0; k < kSteps; k++)
+                            my_part[col * DP + (kNarrow ? k * 16 + 2 * (lane / 4) + (i >> 1) : k * 16 + lane / 4 + 8 * (i >> 1))] = o[k][nt][i];
+                    }
+                __threadfence();
+                __syncwarp();
+                int before = 0;
+                if (lane == 0) before = atomicAdd(counter, 1);
+                if (__shfl_sync(~0u, before, 0) == parts - 1) {
+                    if (lane == 0) *counter = 0;
+                    __threadfence();
+#pragma unroll 1
+                    for (int col = 0; col < cols; col++) {
+                        float u = 0;
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                const float x = __shfl_sync(~0u, unit[nt][i], (col & 7) / 2);
+                                if (col / 8 == nt && (col & 1) == i) u = x;
+                            }
+                        join_alone<T, DP, NT>(p, first_worker, parts, col, head0, vscale, u);
+                    }
+                }
+            }
+            advance(p, work, at, n_kv, head_tiles);
+            fresh = true;
+            continue;
+        }
+        bool restart = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int i = 0; i < 2; i++)
                 if (lane < 4) {
                     const int col = nt * 8 + 2 * lane + i;
                     warp_m[warp * kCols + col] = limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i];
-                    warp_l[warp * kCols + col] = x;
+                    warp_l[warp * kCols + col] = l[nt][i];
                     if (warp == 0) col_unit[col] = unit[nt][i];
                 }
-            }
         __syncthreads();
         // bring the four warps to one maximum, then add their outputs: 2 and 3 write, 0 and 1 add, all finish
 #pragma unroll
@@ -770,23 +908,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         }
         __syncthreads();
 
-        // the units of this group's tiles, and the CTAs that have them
-        const int64_t group_first = end - at.left - at.j, group_end = group_first + at.tiles;
-        int first_cta = blockIdx.x, last_cta = blockIdx.x;
-        if (work.cut) {
-            first_cta -= cut;
-            last_cta = first_cta + cuts - 1;
-        } else {
-            if (group_first < first) first_cta = (int)(group_first / work.share);
-            if (group_end > end) last_cta = (int)((group_end - 1) / work.share);
-        }
-        const int parts = last_cta - first_cta + 1;
-        const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
-        const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
-        constexpr int kPartSize = kCols * (DP + 2);
-        bool restart = false;
-        // a CTA leaves at most two parts: of a group that began before it (0), and of one that goes on behind it (1)
-        float* const my_part = p.parts + (2 * (int64_t)blockIdx.x + (first_cta == (int)blockIdx.x ? 1 : 0)) * kPartSize;
         const int per_row = D / 4;
         for (int i = tid; i < cols * per_row; i += kThreads) {
             const int col = i / per_row, d = (i - col * per_row) * 4;
@@ -816,7 +937,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             __threadfence();
             __syncthreads();
             if (tid == 0) {
-                int* const counter = p.counters + first_cta;
                 const bool last = atomicAdd(counter, 1) == parts - 1;
                 *last_flag = last;
                 if (last) *counter = 0;
@@ -826,12 +946,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 __threadfence();
                 wait_group<0>();  // the ring is the buffer: what it holds of the next group is loaded again
                 __syncthreads();
-                join<T, DP, NT>(p, smem, S::kStages * S::kStage, first_cta, parts, cols, head0, vscale, col_unit);
+                join<T, DP, NT>(p, smem, S::kStages * S::kStage, first_worker, parts, cols, head0, vscale, col_unit);
                 restart = true;
             }
         }
         __syncthreads();  // the merge buffers and the columns' statistics are free again
-        advance<kOverhead>(p, at, n_kv, head_tiles);
+        advance(p, work, at, n_kv, head_tiles);
         fresh = true;
         if (restart && at.left > 0) {
             in = at;
@@ -897,12 +1017,11 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     const int threads = 1 << (p.tile_bits - 2), tiles = kThreads / threads;  // of a tile; at a time
     const int n_kv = p.pool.n_kv, group = p.n_heads / n_kv, mine = threadIdx.x / threads, size = p.pool.page_size;
     __shared__ Before before;
-    const Division work = divide<0>(p, n_kv, true, before);  // (of the lengths alone, which the first kernel does not write)
-    const int64_t first = work.first(), end = work.end();
+    const Division work = divide(p, n_kv, 0, before);  // (of the lengths alone, which the first kernel does not write)
     Place at = {};
     int cut, cuts;
-    if (first < end) locate<0>(p, n_kv, 1, work, first, end, before, at, cut, cuts);
-    for (int i = 0; i < mine && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
+    locate(p, n_kv, 1, work, before, at, cut, cuts);
+    for (int i = 0; i < mine && at.left > 0; i++) advance(p, work, at, n_kv, 1);
 
     int in, t;
     bool aligned, room;
@@ -963,7 +1082,7 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
                 }
             }
         }
-        for (int i = 0; i < tiles && at.left > 0; i++) advance<0>(p, at, n_kv, 1);
+        for (int i = 0; i < tiles && at.left > 0; i++) advance(p, work, at, n_kv, 1);
         if (at.left > 0) load_weights();
     }
 }

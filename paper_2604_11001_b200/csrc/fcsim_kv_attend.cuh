@@ -21,8 +21,8 @@ struct AttendParams {
     float scale;
     int tile_bits;       // tokens a CTA takes at once, of the variant
     // workspace
-    int* counters;       // [grid], zero between calls: the parts that are done of the group that begins in a CTA
-    float* parts;        // [grid][2][heads of a tile][head_dim + 2]
+    int* counters;       // [workers], zero between calls: the parts that are done of the group that begins in a worker's stretch
+    float* parts;        // [workers][2][heads of a tile][head_dim + 2]; a worker is a CTA or one of its four warps
     float* stats;        // add_weight: [n_requests][n_heads][4]: largest logit, its unit, 1 / sum, -
     float* logits;       // add_weight: per request [n_heads][tiles * tokens of a tile]
     int64_t logit_tiles; // what `logits` has room for, in tiles
