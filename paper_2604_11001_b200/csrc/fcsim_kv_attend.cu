@@ -100,13 +100,15 @@ struct OperandOf<T, E4M3> { using type = F16; };
 //           one another (16 requests of 1 024 tokens);
 //   alone   short requests in number: every warp an equal stretch, a tile being its own 16 or 32 tokens: a group of one or two
 //           tiles is nearly all start and end, and four at a time hide what one waits for (400 requests of up to 70 tokens,
-//           64 heads on 8: 56 -> 32 us; 512 of 300: 130 -> 115; with less than two groups a warp most are cut and joined, and
-//           shares are better: 400 x 5 kv heads of 64 elements 20 us, alone 28).
+//           64 heads on 8: 56 -> 32 us; 512 of 300: 130 -> 115).  A short group is the work of the warp in whose stretch its
+//           first tile lies, so that it need not be joined.
 constexpr int kOverhead = 3;       // units of a group's start and end: shares
 constexpr int kOverheadAlone = 3;  // alone
 constexpr int kPieceLeast = 4;     // tiles of a piece at least: below that, joining costs more than it spreads
 constexpr int kPieceMost = 16;     // tiles of a piece from which equal shares are better
-constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone
+constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone if each gets two groups
+constexpr int kAloneAlways = 2;    // and up to which they do in any case
+constexpr int kWhole = 8;          // tiles (of a warp) up to which a group is not cut for a warp that works alone
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
@@ -136,6 +138,7 @@ struct Division {
     __device__ __forceinline__ int worker(int warp) const { return alone ? blockIdx.x * (kThreads / 32) + warp : blockIdx.x; }
     __device__ __forceinline__ int64_t first(int worker) const { return min(total, worker * share); }
     __device__ __forceinline__ int64_t end(int worker) const { return min(total, (worker + 1) * share); }
+    __device__ __forceinline__ bool whole(int tiles) const { return alone && tiles <= kWhole; }
     __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles ? tiles + over : 0; }
 };
 
@@ -145,12 +148,8 @@ __device__ __forceinline__ void enter(const AttendParams& p, const Division& d, 
     w.start = start_of(p, w.len);
     w.tiles = tiles_of(p, w.len, d.bits);
 }
-// The next tile, if the stretch has one more.
-__device__ __forceinline__ void advance(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
-    w.left--;
-    if (++w.j < w.tiles) return;
-    w.left -= d.over;
-    if (w.left <= 0) return;
+// The next group of the work; the caller knows that there is one.
+__device__ __forceinline__ void next_group(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
     w.j = 0;
     if (++w.ht < head_tiles) return;
     w.ht = 0;
@@ -159,6 +158,14 @@ __device__ __forceinline__ void advance(const AttendParams& p, const Division& d
     w.tiles_before += tiles_of(p, w.len, p.tile_bits);
     do enter(p, d, w, w.b + 1);
     while (w.tiles == 0);
+}
+// The next tile, if the stretch has one more.  (In a group that is not cut, `left` stays at its first tile.)
+__device__ __forceinline__ void advance(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
+    const bool whole = d.whole(w.tiles);
+    if (!whole) w.left--;
+    if (++w.j < w.tiles) return;
+    w.left -= d.over + (whole ? w.tiles : 0);
+    if (w.left > 0) next_group(p, d, w, n_kv, head_tiles);
 }
 
 // What the threads' stretches of the requests add up to before each of them.
@@ -210,7 +217,7 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, int w
         if (4 * groups <= 3 * (int64_t)gridDim.x) {
             const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
             if (piece <= kPieceMost) d.cut = (int)piece;
-        } else if (all_tiles <= (int64_t)kAloneMost * all_live && groups >= 2 * (int64_t)gridDim.x * (kThreads / 32)) {
+        } else if (all_tiles <= (int64_t)kAloneMost * all_live && (groups >= 2 * (int64_t)gridDim.x * (kThreads / 32) || all_tiles <= kAloneAlways * (int64_t)all_live)) {
             d.alone = true;
             d.over = kOverheadAlone;
             d.bits = warp_bits;
@@ -277,6 +284,10 @@ __device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head
     } else {
         w.j = max(0, x - d.over);
         w.left = (int)(end - first) - max(0, d.over - x);
+        if (d.whole(w.tiles) && w.j > 0) {  // the worker before has it all
+            w.left = (int)(end - first) - (cost - x) - d.over;
+            if (w.left > 0) next_group(p, d, w, n_kv, head_tiles);
+        }
     }
 }
 
@@ -761,9 +772,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         }
         if (++stage == depth) stage = 0;
 
-        if (at.j < at.tiles - 1 && at.left > 1) {
+        const bool whole = work.whole(at.tiles);
+        if (at.j < at.tiles - 1 && (whole || at.left > 1)) {
             at.j++;
-            at.left--;
+            at.left -= !whole;
             continue;
         }
         // ---------------------------------------------------------------- end of this worker's part of a group
@@ -773,7 +785,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         if (work.cut) {
             first_worker -= cut;
             last_worker = first_worker + cuts - 1;
-        } else {
+        } else if (!whole) {
             if (group_first < first) first_worker = (int)(group_first / work.share);
             if (group_end > end) last_worker = (int)((group_end - 1) / work.share);
         }
