@@ -550,3 +550,49 @@ def test_a_call_on_the_wrong_device_or_type_is_refused():
                 dict(lengths=n.cpu()), dict(max_length=17), dict(window=-1), dict(q=q.float()), dict(table=table[0])):
         with pytest.raises((ValueError, fb.FcsimError)):
             c.attend(**{**dict(q=q, table=table, lengths=n), **bad})
+
+
+@pytest.mark.parametrize("cache,head_dim,heads,n_kv", [("bf16", 128, 64, 8), ("f16", 64, 16, 8), ("e4m3", 128, 64, 8), ("e4m3", 64, 24, 2),
+                                                       ("bf16", 192, 48, 8), ("f16", 112, 96, 8)])
+@pytest.mark.parametrize("window", [0, 37])
+def test_attend_many_short_requests_and_a_few_long_ones(cache, head_dim, heads, n_kv, window):
+    """More groups than warps on the GPU, most of one or two tiles, some cut among many."""
+    import random
+    rng = random.Random(head_dim + window)
+    lengths = [rng.randint(0, 90) for _ in range(500)] + [2500, 1] + [rng.randint(100, 400) for _ in range(60)] + [0, 1300]
+    run_attend(head_dim, lengths, heads, n_kv, head_dim, 16, "f16" if cache == "f16" else "bf16", cache, window=window, spoil=window > 0)
+
+
+@pytest.mark.parametrize("requests,n_kv", [(1, 8), (3, 2), (37, 8), (220, 1), (300, 2)])
+@pytest.mark.parametrize("length", [1, 64, 65, 300, 1024, 1025])
+def test_attend_equal_lengths(requests, n_kv, length):
+    """Every way of dividing the work: pieces of groups, whole groups, shares of units, warps alone."""
+    run_attend(requests + length, [length] * requests, 4 * n_kv, n_kv, 64, 16, spoil=False)
+
+
+@pytest.mark.parametrize("preset,cache,budget", [(1, "bf16", None), (1, "e4m3", 48), (6, "f16", 32)])
+def test_slots_of_a_preset_in_seconds(preset, cache, budget):
+    from paper_2604_11001_b200 import slot_time as st
+    got = st.run(preset, slots=300, replicas=4, points=3, grow=80 if budget else 3, budget=budget, heads=8, kv_heads=2, head_dim=64, cache=cache)
+    assert len(got["rows"]) >= 2 and all(r["us"] > 0 for r in got["rows"])
+    if budget:
+        assert all(r["longest"] <= budget for r in got["rows"])
+    for g in got["groups"]:
+        assert g["slot_us"] > 0 and math.isfinite(g["mean_latency_ms"]) and g["tokens_per_second"] > 0
+
+
+def test_a_layer_grows_as_its_parts_do():
+    """The example's slots against the same steps in 64 bits: lengths, places and the last slot's attention."""
+    from paper_2604_11001_b200 import slot_time as st
+    layer = st.Layer([5, 33, 16], heads=4, kv_heads=2, head_dim=64, cache="f16", budget=40, seed=3)
+    for i in range(90):
+        before = layer.cache.weight.clone()
+        layer.grow()
+    assert layer.positions.tolist() == [95, 123, 106]
+    assert all(40 <= n < 40 + st.SLACK for n in layer.lengths.tolist())
+    lengths = layer.lengths.tolist()
+    q = randn(gen(1), 3, 4, 64, dtype=torch.float16)
+    before = layer.cache.weight.clone()
+    out, lse = layer.cache.attend(q, layer.table, layer.lengths, add_weight=True, return_lse=True)
+    assert_attend(layer.cache, q, layer.table, lengths, out, lse, before)
+    layer.cache.check()

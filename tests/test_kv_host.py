@@ -134,3 +134,17 @@ def test_the_binding_refuses_cpu_tensors():
     k = torch.zeros(2, 16, 1, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         kv.PagedKV(k, k)
+
+
+def test_active_sets_hold_the_usage_they_are_drawn_for():
+    import numpy as np
+
+    from paper_2604_11001_b200 import slot_time as st
+    from paper_2604_11001_b200 import workloads as wl
+    for cfg, usage in ((wl.config1(), 3000), (wl.config6(), 16492), (wl.config2(), 65536)):
+        lengths = st.active_set(cfg, usage, np.random.default_rng(1))
+        assert min(lengths) >= 1 and len(lengths) <= cfg.Acap
+        assert sum(lengths) == usage or len(lengths) == cfg.Acap
+        most = max(t.vmax for t in cfg.prompt) + max(t.vmax for t in cfg.decode)
+        assert max(lengths) < most
+        assert max(st.active_set(cfg, usage, np.random.default_rng(1), limit=40)) <= 40
