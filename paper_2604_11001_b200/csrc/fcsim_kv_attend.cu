@@ -148,7 +148,8 @@ __device__ __forceinline__ void enter(const AttendParams& p, const Division& d, 
     w.start = start_of(p, w.len);
     w.tiles = tiles_of(p, w.len, d.bits);
 }
-// The next group of the work; the caller knows that there is one.
+// The next group of the work; the caller knows that there is one (the lengths stay as they are during a call; if they do not,
+// the results are wrong, but nothing beyond the last request is read).
 __device__ __forceinline__ void next_group(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
     w.j = 0;
     if (++w.ht < head_tiles) return;
@@ -156,8 +157,13 @@ __device__ __forceinline__ void next_group(const AttendParams& p, const Division
     if (++w.kv < n_kv) return;
     w.kv = 0;
     w.tiles_before += tiles_of(p, w.len, p.tile_bits);
-    do enter(p, d, w, w.b + 1);
-    while (w.tiles == 0);
+    do {
+        if (w.b + 1 >= p.n_requests) {
+            w.left = 0;
+            return;
+        }
+        enter(p, d, w, w.b + 1);
+    } while (w.tiles == 0);
 }
 // The next tile, if the stretch has one more.  (In a group that is not cut, `left` stays at its first tile.)
 __device__ __forceinline__ void advance(const AttendParams& p, const Division& d, Place& w, int n_kv, int head_tiles) {
@@ -255,7 +261,7 @@ __device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head
         if (first < units0 || first >= units1) continue;
         int64_t units = units0;
         int tiles = before.tiles[tid], b = tid * each;
-        for (;; b++) {
+        for (const int last = min(b + each, p.n_requests) - 1; b < last; b++) {
             const int n = length_of(p, b);
             const int64_t u = (int64_t)d.units(tiles_of(p, n, d.bits)) * per;
             if (units + u > first) break;
@@ -270,11 +276,12 @@ __device__ __forceinline__ void locate(const AttendParams& p, int n_kv, int head
     const int64_t first = d.first(d.worker(warp)), end = d.end(d.worker(warp));
     w.left = 0;
     if (first >= end) return;
-    enter(p, d, w, found_request[mine]);
+    enter(p, d, w, min(max(found_request[mine], 0), p.n_requests - 1));
     w.tiles_before = found_tiles[mine];
     const int64_t in = first - found_units[mine];
     const int cost = d.units(w.tiles);
-    const int r = (int)(in / cost), x = (int)(in - (int64_t)r * cost);
+    const int r = cost > 0 ? (int)(in / cost) : -1, x = (int)(in - (int64_t)r * cost);
+    if (r < 0 || r >= per) return;  // (lengths that changed since they were added up: see next_group)
     w.kv = r / head_tiles;
     w.ht = r - w.kv * head_tiles;
     if (d.cut) {
@@ -315,6 +322,9 @@ struct Shape {
     static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(2) >= 2 ? 2 : 1;
     static constexpr int kStages = stages(kCtas) < 4 ? stages(kCtas) : 4;
     static constexpr int kFair = kCtas * kStage >= 64 * 1024 || kStages < 3 ? 2 : 3;
+    // parts that a join takes at once: as many as the ring holds, and their factors the merge buffers
+    static constexpr int kInRing = kStages * kStage / (8 * NT * (DP + 2) * 4), kInMerge = kMerge / (8 * NT * 8);
+    static constexpr int kJoined = kInRing < kInMerge ? kInRing : kInMerge;
     static constexpr int kBytes = kStages * kStage + kMerge + kSmall;
     static_assert(kStages >= 2, "shared memory of a CTA");
 };
@@ -327,60 +337,84 @@ __device__ __forceinline__ void finish(const AttendParams& p, int64_t head, floa
 }
 
 // Adds up the parts of a group in their order.  They come from L2 while the rest of the GPU keeps memory busy, so every
-// dependent load costs a microsecond or two: as many whole parts as the buffer holds are copied at once.
+// dependent load costs a microsecond or two: as many whole parts as the buffer holds are copied at once.  A lone CTA waits
+// for its own instructions too, so addresses are constants off one pointer and each factor is computed once.
+// `factors`: room for two floats per head of each of those parts.
 // (A function of its own, so that it takes no registers from the loop over the tiles.)
 template <class T, int DP, int NT>
-__device__ __noinline__ void join(const AttendParams& p, char* buffer, int buffer_bytes, int first_worker, int parts, int cols,
+__device__ __noinline__ void join(const AttendParams& p, char* buffer, int room, float2* factors, int first_worker, int parts, int cols,
                                   int64_t head0, float vscale, const float* col_unit) {
-    constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2), kOutputs = kCols * (DP / 4) / kThreads;
+    constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2), kOutputs = kCols * (DP / 4) / kThreads, kStats = kCols / 2;
     static_assert(kPartSize % 4 == 0 && kCols * (DP / 4) % kThreads == 0, "part layout");
-    const int room = buffer_bytes / (kPartSize * 4), per_row = p.pool.head_dim / 4;
+    const int tid = threadIdx.x, per_row = p.pool.head_dim / 4, my_col = tid % kCols;
     const float* const at = reinterpret_cast<const float*>(buffer);
     float4 z[kOutputs];
     float top[kOutputs], sum[kOutputs];
+    int col[kOutputs], d[kOutputs];
 #pragma unroll
-    for (int i = 0; i < kOutputs; i++) z[i] = make_float4(0, 0, 0, 0), top[i] = -INFINITY, sum[i] = 0;
+    for (int i = 0; i < kOutputs; i++) {
+        const int x = tid + i * kThreads;
+        z[i] = make_float4(0, 0, 0, 0), top[i] = -INFINITY, sum[i] = 0;
+        col[i] = x / per_row, d[i] = (x - col[i] * per_row) * 4;
+    }
     for (int k0 = 0; k0 < parts; k0 += room) {
         const int n = min(room, parts - k0);
-        const uint32_t dst = smem_address(buffer);
+        const uint32_t dst = smem_address(buffer) + tid * 16;
+        const float* const src = p.parts + 2 * (int64_t)(first_worker + k0) * kPartSize + tid * 4;  // part k: + 2 k kPartSize
+#pragma unroll 8
         for (int k = 0; k < n; k++) {
-            const float* src = p.parts + (2 * (int64_t)(first_worker + k0 + k) + (k0 + k == 0 ? 1 : 0)) * kPartSize;
-            for (int i = threadIdx.x; i < kPartSize / 4; i += kThreads) copy16(dst + (k * kPartSize + i * 4) * 4, src + i * 4);
+            const float* const from = src + 2 * k * kPartSize + (k0 + k == 0 ? kPartSize : 0);
+#pragma unroll
+            for (int i = 0; i < kOutputs; i++) copy16(dst + (k * kPartSize + i * 4 * kThreads) * 4, from + i * 4 * kThreads);
+        }
+        for (int x = tid; x < n * kStats; x += kThreads) {  // references and sums: the end of each part
+            const int k = x / kStats, i = kCols * DP + (x % kStats) * 4;
+            copy16(smem_address(buffer) + (k * kPartSize + i) * 4, src - tid * 4 + 2 * k * kPartSize + (k0 + k == 0 ? kPartSize : 0) + i);
         }
         commit();
         wait_group<0>();
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kOutputs; i++) {
-            const int x = threadIdx.x + i * kThreads, col = x / per_row, d = (x - col * per_row) * 4;
-            if (col < cols) {
-                const float u = col_unit[col];
-                float now = top[i];
-                for (int k = 0; k < n; k++) now = fmaxf(now, at[k * kPartSize + kCols * DP + col * 2]);
-                const float base = now == -INFINITY ? 0.0f : now, old = top[i] == -INFINITY ? 0.0f : power2((top[i] - base) * u);
-                z[i].x *= old, z[i].y *= old, z[i].z *= old, z[i].w *= old, sum[i] *= old;  // (NaN stays)
-                for (int k = 0; k < n; k++) {
-                    const float2 ml = *reinterpret_cast<const float2*>(at + k * kPartSize + kCols * DP + col * 2);
-                    const float4 v = *reinterpret_cast<const float4*>(at + k * kPartSize + col * DP + d);
-                    const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * u);
-                    sum[i] += f * ml.y;
-                    z[i].x += f * v.x, z[i].y += f * v.y, z[i].z += f * v.z, z[i].w += f * v.w;
-                }
-                top[i] = now;
-            }
+        float now = -INFINITY;
+        for (int k = 0; k < n; k++) now = fmaxf(now, at[k * kPartSize + kCols * DP + my_col * 2]);
+        const float base = now == -INFINITY ? 0.0f : now;
+        for (int k = tid / kCols; k < n; k += kThreads / kCols) {
+            const float2 ml = *reinterpret_cast<const float2*>(at + k * kPartSize + kCols * DP + my_col * 2);
+            const float f = ml.x == -INFINITY ? 0.0f : power2((ml.x - base) * col_unit[my_col]);
+            factors[k * kCols + my_col] = make_float2(f, f * ml.y);  // (a NaN without a reference stays)
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kOutputs; i++)
+            if (col[i] < cols) {
+                // this round's own reference, then the rounds' in turn
+                float here = -INFINITY;
+                for (int k = 0; k < n; k++) here = fmaxf(here, at[k * kPartSize + kCols * DP + col[i] * 2]);
+                float4 y = make_float4(0, 0, 0, 0);
+                float all = 0;
+#pragma unroll 4
+                for (int k = 0; k < n; k++) {
+                    const float2 fl = factors[k * kCols + col[i]];
+                    const float4 v = *reinterpret_cast<const float4*>(at + k * kPartSize + col[i] * DP + d[i]);
+                    all += fl.y;
+                    y.x += fl.x * v.x, y.y += fl.x * v.y, y.z += fl.x * v.z, y.w += fl.x * v.w;
+                }
+                const float most = fmaxf(top[i], here), u = col_unit[col[i]];
+                const float old = top[i] == -INFINITY ? 0.0f : power2((top[i] - most) * u), young = here == -INFINITY ? 0.0f : power2((here - most) * u);
+                z[i].x = z[i].x * old + y.x * young, z[i].y = z[i].y * old + y.y * young;
+                z[i].z = z[i].z * old + y.z * young, z[i].w = z[i].w * old + y.w * young;
+                sum[i] = sum[i] * old + all * young;
+                top[i] = most;
+            }
         __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < kOutputs; i++) {
-        const int x = threadIdx.x + i * kThreads, col = x / per_row, d = (x - col * per_row) * 4;
-        if (col < cols) {
+    for (int i = 0; i < kOutputs; i++)
+        if (col[i] < cols) {
             const float f = sum[i] == 0.0f ? 0.0f : vscale / sum[i];
-            *reinterpret_cast<uint2*>(p.out + ((head0 + col) * p.pool.head_dim + d) * 2) =
+            *reinterpret_cast<uint2*>(p.out + ((head0 + col[i]) * p.pool.head_dim + d[i]) * 2) =
                 sum[i] == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z[i].x * f, z[i].y * f), T::pack(z[i].z * f, z[i].w * f));
-            if (d == 0) finish(p, head0 + col, top[i], sum[i], col_unit[col]);
+            if (d[i] == 0) finish(p, head0 + col[i], top[i], sum[i], col_unit[col[i]]);
         }
-    }
 }
 
 // The same for one head by one warp: the few groups that lie across the stretches of warps that work alone.
@@ -958,7 +992,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 __threadfence();
                 wait_group<0>();  // the ring is the buffer: what it holds of the next group is loaded again
                 __syncthreads();
-                join<T, DP, NT>(p, smem, S::kStages * S::kStage, first_worker, parts, cols, head0, vscale, col_unit);
+                join<T, DP, NT>(p, smem, S::kJoined, reinterpret_cast<float2*>(merge), first_worker, parts, cols, head0, vscale, col_unit);
                 restart = true;
             }
         }

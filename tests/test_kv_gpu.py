@@ -481,6 +481,11 @@ def test_evict_sizes(lengths, budgets, values):
     run_evict(len(lengths), lengths, budgets, 0 if budgets[0] < 2 else 33, 0, 1 if lengths[0] > 300 else 2, 16, 16, values=values)
 
 
+def test_evict_more_keys_than_shared_memory_holds():
+    """Eight CTAs hold 393 216 keys; beyond that the weights are read again for every digit."""
+    run_evict(9, [450001], [5000], 100, 3, 1, 16, 16)
+
+
 def test_evict_wider_output_than_any_budget():
     run_evict(1, [40, 70], [16, 70], 4, 1, max_budget=300)
 
