@@ -44,6 +44,7 @@ enum { /* bits of *status */
 };
 
 /* head_dim: a multiple of 8 (16-bit caches) or 16 (E4M3), at most 256.  k and v have the same strides.
+ * n_pages * page_size is below 2^31, n_kv_heads at most 65535.
  * weight: [n_pages][n_kv_heads][page_size] fp32, contiguous, 16-byte aligned, or NULL.
  * k_scale, v_scale: [n_kv_heads] fp32, E4M3 only (else NULL): a stored value x stands for x * scale. */
 typedef struct {
@@ -93,8 +94,10 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
  *   logarithm of the softmax sums, or NULL.  A request without tokens gives zeros and -infinity.
  * add_weight: cache->weight[token] += the softmax weights, summed over the heads of its group.  The requests of such
  *   a call must not share pages.
- * workspace: 16-byte aligned, of the size fcsim_kv_attend_workspace reports; its first `zeroed` bytes must be zero
- *   before the first call and are zero again after every call.  Calls that share it must be ordered. */
+ * workspace: 16-byte aligned, of the size fcsim_kv_attend_workspace reports; its first `zeroed` bytes (the same for all
+ *   calls) must be zero before the first call and are zero again after every call.  Calls that share it must be ordered;
+ *   they may differ in everything else.
+ * At most 65535 requests, and n_requests * max_length below 2^36 (FCSIM_EINVAL). */
 typedef struct {
     const void* q;
     void* out;

@@ -664,8 +664,8 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     // the kernel counts the tiles of all requests, and the work of a CTA, in 32 bits
     if ((tiles + 16) * p.n_requests > 0x7fffffff || (most + (int64_t)p.n_requests * 16 * p.n_heads) / l->grid >= 0x7fffffff) return FCSIM_EINVAL;
     const size_t workers = (size_t)l->grid * (kThreads / 32);
-    l->counters = workers * 4;
-    l->parts = (l->counters + 15) / 16 * 16;
+    l->counters = kMaxCtas * (kThreads / 32) * 4;  // the same for every call, so that none finds another's parts there
+    l->parts = l->counters;
     l->stats = l->parts + 2 * workers * v.head_cols * (v.width + 2) * 4;
     l->logit_tiles = logit_tiles(p);
     l->logits = l->stats + (p.add_weight ? (size_t)p.n_requests * p.n_heads * 16 : 0);

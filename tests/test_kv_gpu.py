@@ -189,6 +189,52 @@ def test_attend_minus_infinity_logits_count_as_nothing():
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())   # nothing left: as without tokens
 
 
+def test_attend_calls_of_different_shapes_share_a_workspace():
+    """One cache, one stream: calls whose grids, parts and joins differ, each after another kind."""
+    g = gen(17)
+    c = make_cache(g, 2000, 16, 4, 64, "bf16")
+    kinds = [([9000], 16), ([40] * 300, 4), ([700] * 20, 32), ([1], 4), ([16000], 4), ([300, 5, 2000], 64), ([18] * 900, 16), ([4000] * 4, 8)]
+    for turn in range(3):
+        for lengths, heads in kinds[turn:] + kinds[:turn]:
+            table, _ = make_table(g, lengths, 16, 2000)
+            q = randn(g, len(lengths), heads, 64, dtype=torch.bfloat16)
+            before = c.weight.clone()
+            add = (turn + heads) % 3 == 0
+            out, lse = c.attend(q, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), add_weight=add, return_lse=True)
+            assert_attend(c, q, table, lengths, out, lse, before if add else None)
+    zeroed = next(iter(c._workspaces.values()))[:64 * 1024]
+    assert not bool(zeroed.any())
+    c.check()
+
+
+def test_append_and_evict_in_a_graph():
+    g = gen(18)
+    c = make_cache(g, 64, 16, 2, 64, "bf16")
+    to_int = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table, new = to_int([list(range(20)), list(range(20, 40))]), to_int([[40, 41, 42, 43], [44, 45, 46, 47]])
+    lengths, budget = to_int([300, 77]), to_int([50, 64])
+    x = randn(g, 2, 2, 64, dtype=torch.bfloat16)
+    slots = torch.tensor([5, 20 * 16 + 3], device="cuda")
+    want_n, want_kept = c.evict(table, lengths, budget, new, recent=5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        q = c.append(x, x, x, None, slots)
+        n, kept = c.evict(table, lengths, budget, new, recent=5)
+    c.weight.copy_(torch.rand(c.weight.shape, generator=g, device="cuda") + 1)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(q, x) and torch.equal(c.k[0, 5], x[0]) and torch.equal(n, want_n)
+    weight = c.weight.clone()
+    weight[0, :, 5] = 0        # the appended tokens have no weight yet
+    for r, (length, b) in enumerate(((300, 50), (77, 64))):
+        t = torch.arange(length, device="cuda")
+        w = weight[table[r].long()[t // 16], :, t % 16].cpu()
+        for h in range(2):
+            assert kept[r, h, :b].tolist() == ref_evict(w[:, h].tolist(), length, b, 5, 0)
+    c.check()
+
+
 def test_attend_beyond_32_bit_offsets():
     """A pool of more than 2^32 elements: the pages that a request holds lie at its two ends."""
     page, n_kv, D = 16, 8, 128
