@@ -221,7 +221,7 @@ int launch_append_lanes(const AppendParams& p, cudaStream_t stream) {
     const int64_t lanes = (int64_t)p.n_tokens * (p.n_heads + 2 * p.pool.n_kv) * LPR;
     if (lanes < 1 << 17) return launch_append_as<T, C, LPR, 1>(p, stream);
     if (lanes < 1 << 19) return launch_append_as<T, C, LPR, 2>(p, stream);
-    if (lanes < 5 << 19) return launch_append_as<T, C, LPR, 4>(p, stream);
+    if (lanes < 3 << 19) return launch_append_as<T, C, LPR, 4>(p, stream);
     return launch_append_as<T, C, LPR, 8>(p, stream);
 }
 template <class T, class C>
@@ -288,6 +288,8 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* stat
 constexpr int kMoveRows = 2;
 
 // Copies kept rows [row0, row0 + THREADS / LPR * kMoveRows) of one kv head of request r: 16 bytes a lane, LPR lanes a row.
+// Nothing is read twice, so both sides go through the caches as streams (64 requests to 1 024 tokens, a call among others 86.0
+// -> 82.4 us).
 template <int LPR, int THREADS>
 __device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, int keep, int row0) {
     constexpr int kAtOnce = THREADS / LPR;
@@ -311,8 +313,8 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, in
         if (lane < chunks) {
             const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
             dst[i] = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            k[i] = *reinterpret_cast<const uint4*>(p.pool.k + src);
-            v[i] = *reinterpret_cast<const uint4*>(p.pool.v + src);
+            k[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + src));
+            v[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + src));
         }
         if (lane == 0)
             p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
@@ -321,8 +323,8 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, in
 #pragma unroll
     for (int i = 0; i < kMoveRows; i++)
         if (dst[i] >= 0) {
-            *reinterpret_cast<uint4*>(p.pool.k + dst[i]) = k[i];
-            *reinterpret_cast<uint4*>(p.pool.v + dst[i]) = v[i];
+            __stcs(reinterpret_cast<uint4*>(p.pool.k + dst[i]), k[i]);
+            __stcs(reinterpret_cast<uint4*>(p.pool.v + dst[i]), v[i]);
         }
 }
 
