@@ -106,9 +106,10 @@ constexpr int kOverhead = 3;       // units of a group's start and end: shares
 constexpr int kOverheadAlone = 3;  // alone
 constexpr int kPieceLeast = 4;     // tiles of a piece at least: below that, joining costs more than it spreads
 constexpr int kPieceMost = 16;     // tiles of a piece from which equal shares are better
-constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone if each gets two groups
+constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone if half of them get a group
 constexpr int kAloneAlways = 2;    // and up to which they do in any case
-constexpr int kWhole = 8;          // tiles (of a warp) up to which a group is not cut for a warp that works alone
+constexpr int kWhole = 16;         // tiles (of a warp) up to which a group is not cut for a warp that works alone (128 requests of
+                                   // 256 tokens, 8, 12, 16 tiles: 38, 36, 29 us; 32 lose where lengths differ: 512 of 600, 81 -> 95)
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
@@ -223,7 +224,7 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, int w
         if (4 * groups <= 3 * (int64_t)gridDim.x) {
             const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
             if (piece <= kPieceMost) d.cut = (int)piece;
-        } else if (all_tiles <= (int64_t)kAloneMost * all_live && (groups >= 2 * (int64_t)gridDim.x * (kThreads / 32) || all_tiles <= kAloneAlways * (int64_t)all_live)) {
+        } else if (all_tiles <= (int64_t)kAloneMost * all_live && (groups * 2 >= (int64_t)gridDim.x * (kThreads / 32) || all_tiles <= kAloneAlways * (int64_t)all_live)) {
             d.alone = true;
             d.over = kOverheadAlone;
             d.bits = warp_bits;
