@@ -283,49 +283,32 @@ __device__ __forceinline__ Cut cut_of(const EvictParams& p, int r, int32_t* stat
     return c;
 }
 
-// Rows of K and V that a lane of the copies has in flight.  A row waits for its index and its page before it is read, so
-// more threads hide more than more rows of each: 64 requests to 1 024 tokens, 1, 2, 4, 8 rows: 82, 81, 89, 124 us in all.
-constexpr int kMoveRows = 2;
-
-// Copies kept rows [row0, row0 + THREADS / LPR * kMoveRows) of one kv head of request r: 16 bytes a lane, LPR lanes a row.
-// Nothing is read twice, so both sides go through the caches as streams (64 requests to 1 024 tokens, a call among others 86.0
-// -> 82.4 us).
+// Copies kept rows [row0, row0 + THREADS / LPR) of one kv head of request r: 16 bytes a lane, LPR lanes a row.  A row waits for
+// its index and its page before it is read, so more threads hide more than more rows of each (4 requests of 65 536 to 8 192
+// tokens, 1, 2, 4, 8 rows a thread: 43, 43, 48, 63 us in all).  Nothing is read twice, so both sides go through the caches
+// as streams (64 requests to 1 024 tokens, a call among others 86 -> 82 us).
 template <int LPR, int THREADS>
 __device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, int keep, int row0) {
-    constexpr int kAtOnce = THREADS / LPR;
     const int lane = threadIdx.x % LPR, chunks = p.pool.head_dim * p.bytes / 16, size = p.pool.page_size;
-    const int32_t* kept = p.kept + ((int64_t)r * p.pool.n_kv + h) * p.max_budget;
-    row0 += threadIdx.x / LPR;
-    int64_t dst[kMoveRows];
-    uint4 k[kMoveRows], v[kMoveRows];
-#pragma unroll
-    for (int i = 0; i < kMoveRows; i++) {
-        const int row = row0 + i * kAtOnce;
-        dst[i] = -1;
-        if (row >= keep) continue;
-        const int t = kept[row];
-        const int from = page_of(p.pool, t), into = page_of(p.pool, row);
-        const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
-        if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
-            flag(p.status, FCSIM_KV_BAD_PAGE);
-            continue;
-        }
-        if (lane < chunks) {
-            const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            dst[i] = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-            k[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + src));
-            v[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + src));
-        }
-        if (lane == 0)
-            p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
-                p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
+    const int row = row0 + threadIdx.x / LPR;
+    if (row >= keep) return;
+    const int t = p.kept[((int64_t)r * p.pool.n_kv + h) * p.max_budget + row];
+    const int from = page_of(p.pool, t), into = page_of(p.pool, row);
+    const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
+    if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
+        flag(p.status, FCSIM_KV_BAD_PAGE);
+        return;
     }
-#pragma unroll
-    for (int i = 0; i < kMoveRows; i++)
-        if (dst[i] >= 0) {
-            __stcs(reinterpret_cast<uint4*>(p.pool.k + dst[i]), k[i]);
-            __stcs(reinterpret_cast<uint4*>(p.pool.v + dst[i]), v[i]);
-        }
+    if (lane < chunks) {
+        const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+        const int64_t dst = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
+        const uint4 k = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + src)), v = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + src));
+        __stcs(reinterpret_cast<uint4*>(p.pool.k + dst), k);
+        __stcs(reinterpret_cast<uint4*>(p.pool.v + dst), v);
+    }
+    if (lane == 0)
+        p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
+            p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
 }
 
 // Which tokens one kv head of one request keeps, by one cluster.  Every CTA takes an equal slice of the candidates and
@@ -355,7 +338,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) fcsim_kv_select_kernel(cons
     if (h == 0 && rank == 0 && tid == 0) p.new_lengths[r] = c.keep;
     auto copy = [&]() {
         if constexpr (LPR > 0)
-            for (int row = rank * (kSelectThreads / LPR * kMoveRows); row < c.keep; row += ctas * (kSelectThreads / LPR * kMoveRows))
+            for (int row = rank * (kSelectThreads / LPR); row < c.keep; row += ctas * (kSelectThreads / LPR))
                 move_rows<LPR, kSelectThreads>(p, r, h, c.keep, row);
     };
     auto meet = [&]() {  // a barrier of the cluster costs 0.5 us, one of a CTA a tenth of it
@@ -529,7 +512,7 @@ template <int LPR>
 __global__ void __launch_bounds__(256) fcsim_kv_move_kernel(const EvictParams p) {
     cudaGridDependencySynchronize();
     const int r = blockIdx.z, h = blockIdx.y;
-    move_rows<LPR, 256>(p, r, h, cut_of(p, r, nullptr).keep, blockIdx.x * (256 / LPR * kMoveRows));
+    move_rows<LPR, 256>(p, r, h, cut_of(p, r, nullptr).keep, blockIdx.x * (256 / LPR));
 }
 
 template <int LPR>
@@ -555,7 +538,7 @@ int launch_select(const EvictParams& p, dim3 grid, int capacity, int device, cud
 template <int LPR>
 int launch_move(const EvictParams& p, int n_requests, cudaStream_t stream) {
     if (p.max_budget == 0) return FCSIM_OK;
-    const int rows = 256 / LPR * kMoveRows;
+    const int rows = 256 / LPR;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((p.max_budget + rows - 1) / rows, p.pool.n_kv, n_requests);
     config.blockDim = dim3(256);
@@ -794,7 +777,7 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     const dim3 grid(ctas, p.pool.n_kv, a->n_requests);
     const int chunks = p.pool.head_dim * p.bytes / 16;
     // One kernel when there is little to copy (4 requests of 515 tokens to 256: 12.1 us a call, with two 13.9); else a second
-    // one spreads the copies better (64 requests to 1 024 tokens of 128 elements: 82 us, with one 93).
+    // one spreads the copies better (64 requests to 1 024 tokens of 128 elements: 79 us, with one 85).
     const int64_t row_bytes = (int64_t)p.max_budget * p.pool.head_dim * p.bytes * 2;
     if (row_bytes <= kFusedBytes * ctas) {
         if (chunks <= 4) return launch_select<4>(p, grid, capacity, device, stream);

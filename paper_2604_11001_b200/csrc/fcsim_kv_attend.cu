@@ -5,20 +5,21 @@
 // Every cached byte is used for 2 * group multiplications (k.q and p.v), so the kernel is bound by the bytes of K and V;
 // everything below serves to keep loads in flight on all SMs whatever the lengths are.
 //
-// * Work is counted in tiles of 64 tokens of one kv head and laid out end to end over all requests; every CTA takes an
-//   equal stretch of it (and finds its start by a scan of the lengths), so one request of 131 072 tokens and 500 of a
-//   few hundred load the GPU alike and nothing is planned on the host.  A stretch that covers only part of a
-//   (request, kv head) leaves its maximum, sum and unnormalised output; the CTA that comes last joins them in a fixed
+// * Work is counted in tiles of one kv head and laid out end to end over all requests; every CTA (every warp, where requests
+//   are short) takes an equal stretch of it and finds its start by a scan of the lengths, so one request of 131 072 tokens
+//   and 500 of a few hundred load the GPU alike and nothing is planned on the host.  A stretch that covers only part of a
+//   (request, kv head) leaves its maximum, sum and unnormalised output; the one that comes last joins them in a fixed
 //   order (no atomics on values: the same call gives the same bits).
-// * Each warp copies its own 16 tokens of a tile with cp.async into a ring of its own, and runs ahead over the borders of
+// * Each warp copies its own 16 or 32 tokens of a tile with cp.async into a ring of its own, and runs ahead over the borders of
 //   requests, so the ring never drains at the end of a short one.
 // * Both products run on the tensor cores as transposes, tokens (or head_dim) as the 16 rows and the group's query heads
 //   as the 8 columns: s^T = K q^T and o^T = V^T p^T, m16n8k16.  A group of 8 heads fills the tile (the other way around
 //   half of its 16 rows would be padding), K and V are both read once with ldmatrix, and a column's maximum and sum stay
 //   in the lanes that hold it.  The rate needed is two orders below what these instructions give.
 // * s, m, the sums and o are 32-bit.  p goes to 16 bits in two parts (p = hi + lo; one where it is f16 and the output
-//   bf16), so that rounding it is far below the output's own rounding: one part alone would be as large.  8-bit rows become f16 exactly; a bf16 query beside them is scaled by a
-//   power of two per head to lie in f16's range, with at least 38 bits below its largest element.
+//   bf16), so that rounding it is far below the output's own rounding: one part alone would be as large.  8-bit rows
+//   become f16 exactly; a bf16 query beside them is scaled by a power of two per head to lie in f16's range, with at least
+//   38 bits below its largest element.
 #include <math.h>
 
 #include <atomic>
@@ -106,10 +107,15 @@ constexpr int kOverhead = 3;       // units of a group's start and end: shares
 constexpr int kOverheadAlone = 3;  // alone
 constexpr int kPieceLeast = 4;     // tiles of a piece at least: below that, joining costs more than it spreads
 constexpr int kPieceMost = 16;     // tiles of a piece from which equal shares are better
-constexpr int kAloneMost = 16;     // tiles of a group, on average, up to which the warps work alone if half of them get a group
-constexpr int kAloneAlways = 2;    // and up to which they do in any case
-constexpr int kWhole = 16;         // tiles (of a warp) up to which a group is not cut for a warp that works alone (128 requests of
-                                   // 256 tokens, 8, 12, 16 tiles: 38, 36, 29 us; 32 lose where lengths differ: 512 of 600, 81 -> 95)
+// Warps work alone if they get two groups each of up to kAloneMost tiles on average; if half of them get a group and none is
+// longer than kWhole (128 requests of 256 tokens: 38 -> 29 us, 256 of 256: 62 -> 53; with longer ones among them equal shares
+// win: 114 requests of 1 to 2 500 tokens, 574 on average, with their append 71 us, alone 85); and if groups have kAloneAlways on average.
+constexpr int kAloneMost = 16;
+constexpr int kAloneAlways = 2;
+// Tiles of a warp up to which a group is not cut for a warp that works alone: all groups whole, or those that change little
+// (512 of 600 on average, 8, 16, 32 tiles: 81, 84, 95 us).
+constexpr int kWhole = 16;
+constexpr int kWholeAmongLonger = 8;
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
@@ -135,11 +141,12 @@ __device__ __forceinline__ int tiles_of(const AttendParams& p, int len, int bits
 struct Division {
     int64_t total, share;
     int cut, over, bits;  // bits: of the tokens of a tile
+    int most;             // tiles of a group that is not cut (alone; else none)
     bool alone;
     __device__ __forceinline__ int worker(int warp) const { return alone ? blockIdx.x * (kThreads / 32) + warp : blockIdx.x; }
     __device__ __forceinline__ int64_t first(int worker) const { return min(total, worker * share); }
     __device__ __forceinline__ int64_t end(int worker) const { return min(total, (worker + 1) * share); }
-    __device__ __forceinline__ bool whole(int tiles) const { return alone && tiles <= kWhole; }
+    __device__ __forceinline__ bool whole(int tiles) const { return tiles <= most; }
     __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles ? tiles + over : 0; }
 };
 
@@ -181,8 +188,8 @@ struct Before {
     int warps[2][kThreads / 32];
 };
 
-// Running sums over the threads (exclusive), and the totals.
-__device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_x, int& all_y) {
+// Running sums over the threads (exclusive), and the totals; whether any thread says so.
+__device__ __forceinline__ bool sums_before(Before& s, int& x, int& y, int& all_x, int& all_y, bool says = false) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int upto_x = x, upto_y = y;
 #pragma unroll
@@ -191,7 +198,7 @@ __device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_
         if (lane >= d) upto_x += u, upto_y += v;
     }
     if (lane == 31) s.warps[0][warp] = upto_x, s.warps[1][warp] = upto_y;
-    __syncthreads();
+    const bool any = __syncthreads_or(says);
     x = upto_x - x, y = upto_y - y;
     all_x = all_y = 0;
 #pragma unroll
@@ -199,6 +206,7 @@ __device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_
         if (i < warp) x += s.warps[0][i], y += s.warps[1][i];
         all_x += s.warps[0][i], all_y += s.warps[1][i];
     }
+    return any;
 }
 
 // Adds up the tiles of all requests (less than 2^31: the host refuses more; a request has `per` groups) and divides them.
@@ -207,25 +215,30 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, int w
     const int tid = threadIdx.x;
     const int each = (p.n_requests + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, p.n_requests), b1 = min(b0 + each, p.n_requests);
-    int tiles = 0, live = 0, all_tiles, all_live;
+    int tiles = 0, live = 0, longest = 0, all_tiles, all_live;
     for (int b = b0; b < b1; b++) {
         const int t = tiles_of(p, length_of(p, b), p.tile_bits);
         tiles += t;
         live += t > 0;
+        longest = max(longest, t);
     }
-    sums_before(before, tiles, live, all_tiles, all_live);
+    const bool longer = sums_before(before, tiles, live, all_tiles, all_live, longest > kWhole / (kThreads / 32));
     Division d;
     d.cut = 0;
     d.over = warp_bits ? kOverhead : 0;
     d.bits = p.tile_bits;
     d.alone = false;
+    d.most = 0;
     const int64_t groups = (int64_t)all_live * per, spare = gridDim.x - groups;
+    const int64_t warps = (int64_t)gridDim.x * (kThreads / 32);
     if (warp_bits) {
         if (4 * groups <= 3 * (int64_t)gridDim.x) {
             const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
             if (piece <= kPieceMost) d.cut = (int)piece;
-        } else if (all_tiles <= (int64_t)kAloneMost * all_live && (groups * 2 >= (int64_t)gridDim.x * (kThreads / 32) || all_tiles <= kAloneAlways * (int64_t)all_live)) {
+        } else if ((groups >= 2 * warps && all_tiles <= (int64_t)kAloneMost * all_live) || (2 * groups >= warps && !longer) ||
+                   all_tiles <= (int64_t)kAloneAlways * all_live) {
             d.alone = true;
+            d.most = longer ? kWholeAmongLonger : kWhole;
             d.over = kOverheadAlone;
             d.bits = warp_bits;
         }
