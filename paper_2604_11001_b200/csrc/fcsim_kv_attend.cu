@@ -98,7 +98,7 @@ struct OperandOf<T, E4M3> { using type = F16; };
 // first tile stand for these.  Three ways to divide them, by what the lengths add up to:
 //   shares  every CTA an equal stretch of units, a tile at a time by its four warps;
 //   cut     few tiles: the groups are cut into equal pieces and each CTA gets one, so that starts, ends and joins do not follow
-//           one another (16 requests of 1 024 tokens);
+//           one another (16 requests of 1 024 tokens; 30 of 90 to 300, whole, with their append 22 us, by shares 36);
 //   alone   short requests in number: every warp an equal stretch, a tile being its own 16 or 32 tokens: a group of one or two
 //           tiles is nearly all start and end, and four at a time hide what one waits for (400 requests of up to 70 tokens,
 //           64 heads on 8: 56 -> 32 us; 512 of 300: 130 -> 115).  A short group is the work of the warp in whose stretch its
@@ -186,10 +186,11 @@ __device__ __forceinline__ void advance(const AttendParams& p, const Division& d
 struct Before {
     int tiles[kThreads], units[kThreads + 1];  // (tiles of a CTA; units of one of a request's groups)
     int warps[2][kThreads / 32];
+    int longest[kThreads / 32];  // tiles of a CTA
 };
 
-// Running sums over the threads (exclusive), and the totals; whether any thread says so.
-__device__ __forceinline__ bool sums_before(Before& s, int& x, int& y, int& all_x, int& all_y, bool says = false) {
+// Running sums over the threads (exclusive), and the totals.
+__device__ __forceinline__ void sums_before(Before& s, int& x, int& y, int& all_x, int& all_y) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int upto_x = x, upto_y = y;
 #pragma unroll
@@ -198,7 +199,7 @@ __device__ __forceinline__ bool sums_before(Before& s, int& x, int& y, int& all_
         if (lane >= d) upto_x += u, upto_y += v;
     }
     if (lane == 31) s.warps[0][warp] = upto_x, s.warps[1][warp] = upto_y;
-    const bool any = __syncthreads_or(says);
+    __syncthreads();
     x = upto_x - x, y = upto_y - y;
     all_x = all_y = 0;
 #pragma unroll
@@ -206,7 +207,6 @@ __device__ __forceinline__ bool sums_before(Before& s, int& x, int& y, int& all_
         if (i < warp) x += s.warps[0][i], y += s.warps[1][i];
         all_x += s.warps[0][i], all_y += s.warps[1][i];
     }
-    return any;
 }
 
 // Adds up the tiles of all requests (less than 2^31: the host refuses more; a request has `per` groups) and divides them.
@@ -222,7 +222,12 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, int w
         live += t > 0;
         longest = max(longest, t);
     }
-    const bool longer = sums_before(before, tiles, live, all_tiles, all_live, longest > kWhole / (kThreads / 32));
+    longest = __reduce_max_sync(~0u, longest);
+    if ((tid & 31) == 0) before.longest[tid >> 5] = longest;
+    sums_before(before, tiles, live, all_tiles, all_live);
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; i++) longest = max(longest, before.longest[i]);
+    const bool longer = longest > kWhole / (kThreads / 32);
     Division d;
     d.cut = 0;
     d.over = warp_bits ? kOverhead : 0;
@@ -232,9 +237,10 @@ __device__ __forceinline__ Division divide(const AttendParams& p, int per, int w
     const int64_t groups = (int64_t)all_live * per, spare = gridDim.x - groups;
     const int64_t warps = (int64_t)gridDim.x * (kThreads / 32);
     if (warp_bits) {
-        if (4 * groups <= 3 * (int64_t)gridDim.x) {
-            const int64_t piece = max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare);  // so that the pieces fit the grid
-            if (piece <= kPieceMost) d.cut = (int)piece;
+        if (spare >= 0) {  // so that the pieces fit the grid
+            int64_t piece = longest;
+            if (spare > 0) piece = min(piece, max((int64_t)kPieceLeast, ((int64_t)all_tiles * per + spare - 1) / spare));
+            if (piece <= kPieceMost) d.cut = (int)max((int64_t)kPieceLeast, piece);
         } else if ((groups >= 2 * warps && all_tiles <= (int64_t)kAloneMost * all_live) || (2 * groups >= warps && !longer) ||
                    all_tiles <= (int64_t)kAloneAlways * all_live) {
             d.alone = true;

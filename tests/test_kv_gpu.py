@@ -621,6 +621,17 @@ def test_attend_equal_lengths(requests, n_kv, length):
     run_attend(requests + length, [length] * requests, 4 * n_kv, n_kv, 64, 16, spoil=False)
 
 
+@pytest.mark.parametrize("requests", [27, 28, 36, 37, 38, 55, 56, 74, 75, 160])
+@pytest.mark.parametrize("longest", [64, 256, 257, 1100])
+def test_attend_about_as_many_groups_as_workers(requests, longest):
+    """One group more or less than the GPU holds CTAs or warps, all short or one among them long."""
+    import random
+    rng = random.Random(requests * longest)
+    lengths = [rng.randint(0, min(longest, 256)) for _ in range(requests)]
+    lengths[requests // 2] = longest
+    run_attend(requests + longest, lengths, 16, 8, 128, 16, spoil=False)
+
+
 @pytest.mark.parametrize("preset,cache,budget", [(1, "bf16", None), (1, "e4m3", 48), (6, "f16", 32)])
 def test_slots_of_a_preset_in_seconds(preset, cache, budget):
     from paper_2604_11001_b200 import slot_time as st
