@@ -1,0 +1,80 @@
+"""Values and calls at which the paged cache's operators can lose precision or go wrong, against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+from kv_common import DT, TINY, UNIT, assert_attend, ref_attend
+from paper_2604_11001_b200 import kvcache as kv
+
+pytestmark = pytest.mark.gpu
+
+PAGE = 16
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def to_int(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def stored(x, cache):
+    """A pool of the cache's type that holds `x`."""
+    return x.to(DT[cache])
+
+
+def one_hot(logits, v, dtype, cache, heads=None, q0=1.0, **scales):
+    """A cache in which token t of request r has the logit logits[r, t, h] (its key's first element; the others are zero, so that
+    the product is exact) and the value v[r, t, h], queries that read them with scale 1, table and lengths."""
+    B, n, H = logits.shape
+    D, pages = v.shape[-1], -(-n // PAGE)
+    k = torch.zeros(B * pages, PAGE, H, D, device="cuda")
+    values = torch.zeros_like(k)
+    t = torch.arange(n, device="cuda")
+    at = torch.arange(B, device="cuda")[:, None] * pages + (t // PAGE)[None, :]
+    k[at, (t % PAGE).expand(B, n), :, 0] = logits
+    values[at, (t % PAGE).expand(B, n)] = v
+    if cache == "e4m3":
+        scales = {name: scales.get(name, torch.ones(H, device="cuda")) for name in ("k_scale", "v_scale")}
+    c = kv.PagedKV(stored(k, cache), stored(values, cache), **scales)
+    q = torch.zeros(B, heads or H, D, dtype=DT[dtype], device="cuda")
+    q[..., 0] = q0
+    table = torch.arange(B * pages, dtype=torch.int32, device="cuda").view(B, pages)
+    return c, q, table, [n] * B
+
+
+def attend_within(c, q, table, lengths, slack, **kw):
+    """Attention within half a step of the output's type and `slack` of sum p |v|."""
+    out, lse = c.attend(q, table, to_int(lengths), return_lse=True, **kw)
+    c.check()
+    ref, rlse, _, mag, _ = ref_attend(c, q, table, lengths, **kw)
+    err = (out.double() - ref).abs()
+    half_step = torch.ldexp(torch.full_like(ref, UNIT[q.dtype]), torch.frexp(ref).exponent - 1)
+    tol = torch.where(ref == 0, 0, half_step) + slack * mag + TINY[q.dtype]
+    assert bool((err <= tol).all()), f"off by {float((err / tol.clamp(min=1e-300)).max()):.3g} of the bound, {int((err > tol).sum())} of {err.numel()}"
+    assert bool(((lse.double() - rlse).abs() <= 2.0 ** -20 * (1 + rlse.abs()) + slack).all())
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("requests", [3, 400])
+def test_weights_meet_values_unrounded(dtype, cache, requests):
+    check_weights(dtype, cache, requests)
+
+
+def check_weights(dtype, cache, requests):
+    """Two tokens, the first one's value zero: the output is the second one's weight times its value.  Logits are exact, so the weight
+    is within 2^-20 (an exponent of up to 16 rounded twice, the exponential, for both tokens: 2 (2^-21 ln 2 + 2^-22.5)); its
+    parts, the sum, the quotient and the product add 2^-21 at most."""
+    g = gen(requests)
+    H, D = 8, 64
+    x = torch.zeros(requests, 2, H, device="cuda")
+    x[:, 1] = (1.5 * torch.randn(requests, H, generator=g, device="cuda")).clamp(-4, 4)
+    v = torch.randn(requests, 2, H, D, generator=g, device="cuda") + 2
+    v[:, 0] = 0
+    c, q, table, lengths = one_hot(x, v, dtype, cache)
+    attend_within(c, q, table, lengths, 2.0 ** -19, scale=1.0)
