@@ -16,10 +16,11 @@
 //   as the 8 columns: s^T = K q^T and o^T = V^T p^T, m16n8k16.  A group of 8 heads fills the tile (the other way around
 //   half of its 16 rows would be padding), K and V are both read once with ldmatrix, and a column's maximum and sum stay
 //   in the lanes that hold it.  The rate needed is two orders below what these instructions give.
-// * s, m, the sums and o are 32-bit.  p goes to 16 bits in two parts (p = hi + lo), so that rounding it is far below the
-//   output's own rounding; one part alone is not (f16 beside a bf16 output: 8.5e-4 of the output's norm from the same sums in
-//   32 bits, in two parts 7e-5, for 64 requests over e4m3 78.5 -> 80.4 us).  8-bit rows become f16 exactly; a bf16
-//   query beside them is scaled by a power of two per head to lie in f16's range, with at least 38 bits below its largest element.
+// * s, m, the sums and o are 32-bit.  p meets v in 16-bit parts that add up to it, two of f16 (11 bits each) or three of bf16 (8
+//   each), so that nothing is lost beside the 32-bit sums: with one part less the output is 1.6e-4 (bf16) or 8.5e-4 (f16 weights of
+//   a bf16 output) of its norm from the same sums in 32 bits, with all 4e-5 and 7e-5.  The products cost nothing for bf16 (128
+//   requests 189.7 -> 190.0 us), 2 us of 80 over e4m3.  8-bit rows become f16 exactly; a bf16 query beside them is scaled by a
+//   power of two per head to lie in f16's range, with at least 38 bits below its largest element.
 #include <math.h>
 
 #include <atomic>
@@ -75,8 +76,8 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Two weights in 0 .. 1 as one operand word, and what is left of them as a second.  The first is rounded down and one more
-// step below, so that neither is zero unless the weight is nearly (2^-23 for f16): an infinite v then stays infinite.
+// Two weights as one operand word, rounded down and one more step below: what is left of them for the next part is above zero
+// then, and no part is zero unless the weight is nearly (2^-23 for f16), so that an infinite v stays infinite.
 template <class M>
 __device__ __forceinline__ uint32_t below(float a, float b) {
     uint32_t h;
@@ -469,6 +470,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     using M = typename OperandOf<T, C>::type;
     constexpr bool kNarrow = C::bytes == 1, kRescaled = kNarrow && std::is_same<T, BF16>::value;
     constexpr int kCols = 8 * NT, kSteps = DP / 16, kTokens = S::kTokens, kSub = kTokens / 16;
+    constexpr int kParts = std::is_same<M, F16>::value ? 2 : 3;  // 11 bits each, or 8: of the softmax weights
     constexpr float kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
@@ -707,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 }
             }
             // ---- softmax: this lane holds tokens lane / 4 and + 8 of every 16, of heads 2 (lane % 4) and + 1
-            uint32_t hi[kSub][NT][2], lo[kSub][NT][2];
+            uint32_t part[kParts][kSub][NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
                 if (logits) {
@@ -768,10 +770,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
                         const float x = s[b][nt][2 * k], y = s[b][nt][2 * k + 1];
-                        const uint32_t h = below<M>(x, y);
-                        const float2 back = M::unpack(h);
-                        hi[b][nt][k] = transpose8x8(h);
-                        lo[b][nt][k] = transpose8x8(M::pack(x - back.x, y - back.y));
+                        float restx = x, resty = y;
+#pragma unroll
+                        for (int i = 0; i < kParts - 1; i++) {
+                            const uint32_t h = below<M>(restx, resty);
+                            const float2 back = M::unpack(h);
+                            part[i][b][nt][k] = transpose8x8(h);
+                            restx -= back.x, resty -= back.y;
+                        }
+                        part[kParts - 1][b][nt][k] = transpose8x8(M::pack(restx, resty));
                     }
                 }
             }
@@ -787,13 +794,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
                         for (int k = 0; k < 4; k++) load_matrices_transposed(row + (k0 + k) * 32, a[k]);
 #pragma unroll
-                        for (int k = 0; k < 4; k++)
+                        for (int i = 0; i < kParts; i++)
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma<M>(o[k0 + k][nt], a[k], hi[b][nt][0], hi[b][nt][1]);
+                            for (int k = 0; k < 4; k++)
 #pragma unroll
-                        for (int k = 0; k < 4; k++)
-#pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma<M>(o[k0 + k][nt], a[k], lo[b][nt][0], lo[b][nt][1]);
+                                for (int nt = 0; nt < NT; nt++) mma<M>(o[k0 + k][nt], a[k], part[i][b][nt][0], part[i][b][nt][1]);
                     }
                 } else {
                     const uint32_t row = vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
@@ -809,10 +814,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                             const uint32_t a[4] = {E4M3::halves(__byte_perm(x, 0, 0x4420)), E4M3::halves(__byte_perm(x, 0, 0x4431)),
                                                    E4M3::halves(__byte_perm(y, 0, 0x4420)), E4M3::halves(__byte_perm(y, 0, 0x4431))};
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) {
-                                mma<M>(o[k0 + k][nt], a, hi[b][nt][0], hi[b][nt][1]);
-                                mma<M>(o[k0 + k][nt], a, lo[b][nt][0], lo[b][nt][1]);
-                            }
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int i = 0; i < kParts; i++) mma<M>(o[k0 + k][nt], a, part[i][b][nt][0], part[i][b][nt][1]);
                         }
                     }
                 }

@@ -78,3 +78,8 @@ def check_weights(dtype, cache, requests):
     v[:, 0] = 0
     c, q, table, lengths = one_hot(x, v, dtype, cache)
     attend_within(c, q, table, lengths, 2.0 ** -19, scale=1.0)
+
+
+@pytest.mark.parametrize("requests", [3, 400])
+def test_weights_meet_bf16_values_unrounded(requests):
+    check_weights("bf16", "bf16", requests)
