@@ -45,7 +45,7 @@ template <int N>
 __device__ __forceinline__ void wait_group() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// 2^x for x <= 0; results below 2^-126 are 0
+// 2^x; results below 2^-126 are 0
 __device__ __forceinline__ float power2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -350,8 +350,14 @@ struct Shape {
     static_assert(kStages >= 2, "shared memory of a CTA");
 };
 
+// The exponent of a softmax weight at the reference: those that meet v in f16 use its range up to 2^15, since its steps below are coarse.
+template <class M>
+constexpr int kRaiseOf = std::is_same<M, F16>::value ? 14 : 0;
+
 // A head's log-sum-exp and what the weights need of it: reference, unit, 1 / sum.
+template <class M>
 __device__ __forceinline__ void finish(const AttendParams& p, int64_t head, float top, float sum, float unit) {
+    sum *= 1.0f / (1 << kRaiseOf<M>);
     const float reference = top == -INFINITY ? 0.0f : top;
     if (p.lse) p.lse[head] = sum == 0.0f ? -INFINITY : reference * (unit * 0.6931471805599453f) + logf(sum);
     if (p.add_weight) *reinterpret_cast<float4*>(p.stats + head * 4) = make_float4(reference, unit, sum == 0.0f ? 0.0f : 1.0f / sum, 0.0f);
@@ -362,7 +368,7 @@ __device__ __forceinline__ void finish(const AttendParams& p, int64_t head, floa
 // for its own instructions too, so addresses are constants off one pointer and each factor is computed once.
 // `factors`: room for two floats per head of each of those parts.
 // (A function of its own, so that it takes no registers from the loop over the tiles.)
-template <class T, int DP, int NT>
+template <class T, class M, int DP, int NT>
 __device__ __noinline__ void join(const AttendParams& p, char* buffer, int room, float2* factors, int first_worker, int parts, int cols,
                                   int64_t head0, float vscale, const float* col_unit) {
     constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2), kOutputs = kCols * (DP / 4) / kThreads, kStats = kCols / 2;
@@ -434,12 +440,12 @@ __device__ __noinline__ void join(const AttendParams& p, char* buffer, int room,
             const float f = sum[i] == 0.0f ? 0.0f : vscale / sum[i];
             *reinterpret_cast<uint2*>(p.out + ((head0 + col[i]) * p.pool.head_dim + d[i]) * 2) =
                 sum[i] == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z[i].x * f, z[i].y * f), T::pack(z[i].z * f, z[i].w * f));
-            if (d[i] == 0) finish(p, head0 + col[i], top[i], sum[i], col_unit[col[i]]);
+            if (d[i] == 0) finish<M>(p, head0 + col[i], top[i], sum[i], col_unit[col[i]]);
         }
 }
 
 // The same for one head by one warp: the few groups that lie across the stretches of warps that work alone.
-template <class T, int DP, int NT>
+template <class T, class M, int DP, int NT>
 __device__ __noinline__ void join_alone(const AttendParams& p, int first_worker, int parts, int col, int64_t head0, float vscale, float unit) {
     constexpr int kCols = 8 * NT, kPartSize = kCols * (DP + 2);
     const int lane = threadIdx.x & 31, D = p.pool.head_dim;
@@ -460,7 +466,7 @@ __device__ __noinline__ void join_alone(const AttendParams& p, int first_worker,
         const float f = sum == 0.0f ? 0.0f : vscale / sum;
         *reinterpret_cast<uint2*>(p.out + ((head0 + col) * D + d) * 2) =
             sum == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z.x * f, z.y * f), T::pack(z.z * f, z.w * f));
-        if (d == 0) finish(p, head0 + col, top, sum, unit);
+        if (d == 0) finish<M>(p, head0 + col, top, sum, unit);
     }
 }
 
@@ -472,6 +478,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     constexpr int kCols = 8 * NT, kSteps = DP / 16, kTokens = S::kTokens, kSub = kTokens / 16;
     constexpr int kParts = std::is_same<M, F16>::value ? 2 : 3;  // 11 bits each, or 8: of the softmax weights
     constexpr float kLog2e = 1.4426950408889634f;
+    // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
+    constexpr bool kFollow = std::is_same<M, F16>::value;
+    constexpr float kRaise = kRaiseOf<M>, kLag = kFollow ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
     float* const warp_m = merge + 2 * kCols * S::kOutPitch;  // [4][kCols]
@@ -738,21 +747,54 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     most[i] = fmaxf(s[0][nt][i], s[0][nt][2 + i]);
                     if (kSub == 2) most[i] = fmaxf(most[i], fmaxf(s[kSub - 1][nt][i], s[kSub - 1][nt][2 + i]));
                 }
-                // The reference moves only when a logit is 2^8 above it: the weights stay far from f16's and fp32's ends, and
-                // the maximum over the lanes is taken a few times in a request instead of in every tile.
-                if (__any_sync(~0u, most[0] > limit[nt][0] || most[1] > limit[nt][1])) {
+                // The reference moves only when a logit is 2^kLag above it: the weights stay far from f16's and fp32's ends, and
+                // the maximum over the lanes is taken a few times in a request instead of in every tile.  f16 has steps of
+                // 2^-24, so beside it the reference also moves down where all of a tile's tokens lie 2^-kDeep below it (one
+                // token may hold nearly all of the sum and have a v of nothing); the 32-bit sums grow by as much.  A weight's
+                // rounding is then 2^-17 of its tile's largest at most, 2^-39 of it in that one token's own tile.  (100 requests
+                // in f16 41.1 -> 42.6 us, 64 over e4m3 80.3 -> 83.0; with a reach of 2^8 up, 42.2 and 2^-32 in its own tile.)
+                bool moves;
+                if constexpr (kFollow) {
+                    bool low[2];
+                    moves = false;
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const float above = (most[i] - limit[nt][i]) * unit[nt][i];
+                        moves |= above > 0.0f;
+                        low[i] = above < -(kLag + kDeep);
+                    }
+                    if (__any_sync(~0u, moves || low[0] || low[1])) {
+                        moves = __any_sync(~0u, moves);
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {  // all of a head's eight lanes
+                            uint32_t all = __ballot_sync(~0u, low[i]);
+                            all &= all >> 16, all &= all >> 8, all &= all >> 4;
+                            moves |= (all & 15) != 0;
+                        }
+                    }
+                } else
+                    moves = __any_sync(~0u, most[0] > limit[nt][0] || most[1] > limit[nt][1]);
+                if (moves) {
                     float shrink[2];
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
-                        float top = most[i];
-                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
-                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
-                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                        float top = most[i], most_l = l[nt][i];
+#pragma unroll
+                        for (int d = 4; d < 32; d *= 2) {
+                            top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+                            if constexpr (kFollow) most_l = fmaxf(most_l, __shfl_xor_sync(~0u, most_l, d));
+                        }
                         const bool first_one = limit[nt][i] == -INFINITY;
-                        const float now = first_one ? top : fmaxf(top, m[nt][i]), base = now == -INFINITY ? 0.0f : now;
+                        float now = first_one ? top : fmaxf(top, m[nt][i]);
+                        if constexpr (kFollow) {
+                            const float under = (m[nt][i] - top) * unit[nt][i];
+                            const float room = kMost + 126 - (float)(__float_as_uint(most_l) >> 23);  // so that l stays below 2^kMost
+                            if (!first_one && under > kDeep && top > -INFINITY) now = m[nt][i] - fmaxf(fminf(under, room), 0.0f) / unit[nt][i];
+                        }
+                        const float base = now == -INFINITY ? 0.0f : now;
                         shrink[i] = first_one ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
                         m[nt][i] = base;
-                        limit[nt][i] = now + fminf(8.0f / unit[nt][i], 1e30f);
+                        limit[nt][i] = now + fminf(kLag / unit[nt][i], 1e30f);
                         l[nt][i] *= shrink[i];
                     }
 #pragma unroll
@@ -764,7 +806,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 for (int b = 0; b < kSub; b++) {
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        s[b][nt][i] = power2((s[b][nt][i] - m[nt][i & 1]) * unit[nt][i & 1]);
+                        s[b][nt][i] = power2(fmaf(s[b][nt][i] - m[nt][i & 1], unit[nt][i & 1], kRaise));
                         l[nt][i & 1] += s[b][nt][i];
                     }
 #pragma unroll
@@ -865,7 +907,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     for (int i = 0; i < 2; i++) {
                         const int col = nt * 8 + 2 * (lane & 3) + i;
                         f[i] = l[nt][i] == 0.0f ? 0.0f : vscale / l[nt][i];
-                        if (lane < 4 && col < cols) finish(p, head0 + col, limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i], l[nt][i], unit[nt][i]);
+                        if (lane < 4 && col < cols) finish<M>(p, head0 + col, limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i], l[nt][i], unit[nt][i]);
                     }
                     // two heads a lane become two or four neighbouring elements of one head: lane / 4
                     const bool real = nt * 8 + lane / 4 < cols;
@@ -914,7 +956,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                                 const float x = __shfl_sync(~0u, unit[nt][i], (col & 7) / 2);
                                 if (col / 8 == nt && (col & 1) == i) u = x;
                             }
-                        join_alone<T, DP, NT>(p, first_worker, parts, col, head0, vscale, u);
+                        join_alone<T, M, DP, NT>(p, first_worker, parts, col, head0, vscale, u);
                     }
                 }
             }
@@ -991,7 +1033,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 const float f = sum == 0.0f ? 0.0f : vscale / sum;
                 *reinterpret_cast<uint2*>(p.out + ((head0 + col) * D + d) * 2) =
                     sum == 0.0f ? make_uint2(0, 0) : make_uint2(T::pack(z.x * f, z.y * f), T::pack(z.z * f, z.w * f));
-                if (d == 0) finish(p, head0 + col, top, sum, u);
+                if (d == 0) finish<M>(p, head0 + col, top, sum, u);
             } else {
                 *reinterpret_cast<float4*>(my_part + col * DP + d) = z;
                 if (d == 0) *reinterpret_cast<float2*>(my_part + kCols * DP + col * 2) = make_float2(top, sum);
@@ -1010,7 +1052,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 __threadfence();
                 wait_group<0>();  // the ring is the buffer: what it holds of the next group is loaded again
                 __syncthreads();
-                join<T, DP, NT>(p, smem, S::kJoined, reinterpret_cast<float2*>(merge), first_worker, parts, cols, head0, vscale, col_unit);
+                join<T, M, DP, NT>(p, smem, S::kJoined, reinterpret_cast<float2*>(merge), first_worker, parts, cols, head0, vscale, col_unit);
                 restart = true;
             }
         }

@@ -60,6 +60,26 @@ def attend_within(c, q, table, lengths, slack, **kw):
     return out, lse
 
 
+# ------------------------------------------------------------------------------------------ precision of attend
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3")])
+@pytest.mark.parametrize("gap", [6, 12, 18, 30])
+@pytest.mark.parametrize("requests,n,at", [(1, 40, 0), (1, 5000, 0), (1, 5000, 2500), (2, 700, 699), (300, 40, 7)])
+def test_one_token_far_above_the_rest(dtype, cache, gap, requests, n, at):
+    """A token that draws nearly all of the attention and whose value is zero: the output is what the others add up to, e^-gap
+    of its weight each.  A weight meets v in two parts of f16 whose smallest step is 2^-24; the reference of the exponentials
+    follows a tile's largest weight down to 2^-8, so the step is 2^-16 of it and a rounding 2^-17.  The logits of the others
+    spread by 0.25, eight of these within a tile: 2^-14.1 of the smallest.  Exponentials: 2^-22 of their argument at most, gap
+    and reference (23 bits) together."""
+    g = gen(gap + n)
+    H, D = 2, 64
+    x = 0.25 * torch.randn(requests, n, H, generator=g, device="cuda")
+    x[:, at] = gap
+    v = 200 * (0.5 + torch.rand(requests, n, H, D, generator=g, device="cuda"))
+    v[:, at] = 0
+    c, q, table, lengths = one_hot(x, v, dtype, cache, 4)
+    attend_within(c, q, table, lengths, 2.0 ** -14 + 2.0 ** -21 * (gap + 16), scale=1.0)
+
+
 @pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3")])
 @pytest.mark.parametrize("requests", [3, 400])
 def test_weights_meet_values_unrounded(dtype, cache, requests):
