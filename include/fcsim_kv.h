@@ -46,7 +46,7 @@ enum { /* bits of *status */
 /* head_dim: a multiple of 8 (16-bit caches) or 16 (E4M3), at most 256.  k and v have the same strides.
  * n_pages * page_size is below 2^31, n_kv_heads at most 65535.
  * weight: [n_pages][n_kv_heads][page_size] fp32, contiguous, 16-byte aligned, or NULL.
- * k_scale, v_scale: [n_kv_heads] fp32, E4M3 only (else NULL): a stored value x stands for x * scale. */
+ * k_scale, v_scale: [n_kv_heads] fp32 of either sign, E4M3 only (else NULL): a stored value x stands for x * scale. */
 typedef struct {
     void* k;
     void* v;

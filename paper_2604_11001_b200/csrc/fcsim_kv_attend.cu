@@ -596,8 +596,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     int col0 = 0, cols = 0;
     float* logits = nullptr;  // of this lane's first head and first token of a tile
     int64_t logit_row = 0;
-    const float flip = p.scale < 0 ? -1.0f : 1.0f;  // a negative scale turns the order around: turn q instead
-
     const int64_t first = work.first(worker), end = work.end(worker);
     locate(p, n_kv, head_tiles, work, before, in, cut, cuts);
     if (in.left <= 0) return;  // a CTA whole, or a warp that works alone and meets no barrier
@@ -627,7 +625,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             logit_row = (int64_t)cta_tiles * S::kTile;
             if (p.add_weight && at.tiles_before + cta_tiles <= p.logit_tiles)
                 logits = p.logits + (int64_t)at.tiles_before * S::kTile * p.n_heads + (kv * group + col0 + 2 * (lane & 3)) * logit_row + offset + lane / 4;
-            const float kscale = kNarrow ? p.pool.k_scale[kv] : 1.0f;
+            const float scale = kNarrow ? p.scale * p.pool.k_scale[kv] : p.scale;
+            const uint32_t flip = scale < 0 ? 0x80008000u : 0u;  // a negative scale turns the order around: turn q instead
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
                 const int col = nt * 8 + lane / 4;
@@ -640,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                         // 8-bit rows come as four neighbours per lane: the same order for q
                         const int d = kNarrow ? k * 16 + 4 * (lane & 3) + 2 * i : k * 16 + 2 * (lane & 3) + 8 * i;
                         uint32_t x = col < cols && d < D ? *reinterpret_cast<const uint32_t*>(row + d * 2) : 0u;
-                        if (flip < 0) x ^= 0x80008000u;
+                        x ^= flip;
                         qf[nt][k][i] = x;
                         if constexpr (kRescaled) {
                             const float2 f = BF16::unpack(x);
@@ -661,8 +660,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                             qf[nt][k][i] = F16::pack(f.x * up, f.y * up);
                         }
                 }
-                // (never zero: a logit of -infinity must stay without weight)
-                const float u = fmaxf(fabsf(p.scale) * kscale * power * kLog2e, 1.2e-38f);
+                // (never zero: a logit of -infinity must stay without weight; and a scale that is no number stays none)
+                float u = fabsf(scale) * power * kLog2e;
+                if (u < 1.2e-38f) u = 1.2e-38f;
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     unit[nt][i] = __shfl_sync(~0u, u, (2 * (lane & 3) + i) * 4);

@@ -103,3 +103,39 @@ def check_weights(dtype, cache, requests):
 @pytest.mark.parametrize("requests", [3, 400])
 def test_weights_meet_bf16_values_unrounded(requests):
     check_weights("bf16", "bf16", requests)
+
+
+# ------------------------------------------------------------------------------------------ scales
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("scale", [None, -0.3, 0.0])
+@pytest.mark.parametrize("requests", [1, 60])
+def test_scales_of_either_sign(dtype, scale, requests):
+    """A stored x stands for x * scale, whatever the scale's sign: logits, log-sum-exp and added weights follow."""
+    g = gen(requests)
+    H, D, n = 5, 64, 90
+    shape = (requests * 6, PAGE, H, D)
+    k_scale = torch.tensor([0.7, -0.4, 1.5, -2.0, 0.0], device="cuda")
+    v_scale = torch.tensor([-1.0, 0.5, 0.25, -0.75, 3.0], device="cuda")
+    c = kv.PagedKV(stored(torch.randn(shape, generator=g, device="cuda"), "e4m3"), stored(torch.randn(shape, generator=g, device="cuda"), "e4m3"),
+                   torch.rand(shape[0], H, PAGE, generator=g, device="cuda"), k_scale, v_scale)
+    q = torch.randn(requests, 3 * H, D, generator=g, device="cuda").to(DT[dtype])
+    table = torch.arange(shape[0], dtype=torch.int32, device="cuda").view(requests, 6)
+    before = c.weight.clone()
+    out, lse = c.attend(q, table, to_int([n] * requests), add_weight=True, return_lse=True, scale=scale)
+    c.check()
+    assert_attend(c, q, table, [n] * requests, out, lse, before, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("requests", [1, 400])
+def test_a_scale_that_is_no_number_shows(dtype, requests):
+    H, D = 2, 64
+    shape = (requests, PAGE, H, D)
+    c = kv.PagedKV(stored(torch.ones(shape, device="cuda"), "e4m3"), stored(torch.ones(shape, device="cuda"), "e4m3"),
+                   torch.zeros(requests, H, PAGE, device="cuda"), torch.tensor([float("nan"), 1.0], device="cuda"), torch.ones(H, device="cuda"))
+    q = torch.ones(requests, 4, D, device="cuda").to(DT[dtype])
+    table = torch.arange(requests, dtype=torch.int32, device="cuda").view(requests, 1)
+    out, lse = c.attend(q, table, to_int([9] * requests), add_weight=True, return_lse=True)
+    for x in (out[:, :2], lse[:, :2], c.weight[:, 0, :9]):
+        assert bool(torch.isnan(x).all())
+    assert bool((out[:, 2:] == 1).all()) and bool(torch.isfinite(lse[:, 2:]).all()) and bool(torch.isfinite(c.weight[:, 1]).all())
