@@ -627,6 +627,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 logits = p.logits + (int64_t)at.tiles_before * S::kTile * p.n_heads + (kv * group + col0 + 2 * (lane & 3)) * logit_row + offset + lane / 4;
             const float scale = kNarrow ? p.scale * p.pool.k_scale[kv] : p.scale;
             const uint32_t flip = scale < 0 ? 0x80008000u : 0u;  // a negative scale turns the order around: turn q instead
+            // logits of bf16 reach the end of fp32, where their differences do not fit: below a scale that makes those vanish
+            // as -infinity would, q is halved
+            const float half = std::is_same<M, BF16>::value && fabsf(scale) < 1e-36f ? 0.5f : 1.0f;
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
                 const int col = nt * 8 + lane / 4;
@@ -640,6 +643,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                         const int d = kNarrow ? k * 16 + 4 * (lane & 3) + 2 * i : k * 16 + 2 * (lane & 3) + 8 * i;
                         uint32_t x = col < cols && d < D ? *reinterpret_cast<const uint32_t*>(row + d * 2) : 0u;
                         x ^= flip;
+                        if constexpr (std::is_same<M, BF16>::value)
+                            if (half < 1.0f) x = BF16::pack(BF16::unpack(x).x * half, BF16::unpack(x).y * half);
                         qf[nt][k][i] = x;
                         if constexpr (kRescaled) {
                             const float2 f = BF16::unpack(x);
@@ -660,9 +665,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                             qf[nt][k][i] = F16::pack(f.x * up, f.y * up);
                         }
                 }
-                // (never zero: a logit of -infinity must stay without weight; and a scale that is no number stays none)
-                float u = fabsf(scale) * power * kLog2e;
-                if (u < 1.2e-38f) u = 1.2e-38f;
+                // (never zero: a logit of -infinity must stay without weight.  2^-149 times the largest logit is 5e-7.  A scale that
+                // is no number stays none.)
+                float u = fabsf(scale) / half * power * kLog2e;
+                if (u < 1.4e-45f) u = 1.4e-45f;
 #pragma unroll
                 for (int i = 0; i < 2; i++) {
                     unit[nt][i] = __shfl_sync(~0u, u, (2 * (lane & 3) + i) * 4);

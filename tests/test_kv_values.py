@@ -139,3 +139,13 @@ def test_a_scale_that_is_no_number_shows(dtype, requests):
     for x in (out[:, :2], lse[:, :2], c.weight[:, 0, :9]):
         assert bool(torch.isnan(x).all())
     assert bool((out[:, 2:] == 1).all()) and bool(torch.isfinite(lse[:, 2:]).all()) and bool(torch.isfinite(c.weight[:, 1]).all())
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-39, -1e-39, 1e-38, 3e-42])
+def test_scales_near_zero_over_keys_at_the_end_of_bf16(scale):
+    """Keys of +-3e38: their products with a scale of nearly nothing are small, their differences are not finite."""
+    g = gen(3)
+    x = 3e38 * torch.sign(torch.randn(3, 90, 2, generator=g, device="cuda"))
+    c, q, table, lengths = one_hot(x, torch.randn(3, 90, 2, 64, generator=g, device="cuda"), "bf16", "bf16")
+    # a scale of 1e-39 has 20 bits, one of 3e-42 11, and logits of 0.3 and 0.001; the smallest unit is 2^-149, 5e-7 of a logit here
+    attend_within(c, q, table, lengths, 2.0 ** -16, scale=scale)
