@@ -481,6 +481,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
     constexpr bool kFollow = std::is_same<M, F16>::value;
     constexpr float kRaise = kRaiseOf<M>, kLag = kFollow ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
+    constexpr float kLowered = 4294967296.0f;  // 2^32: bf16 weights meet v that much smaller, so that 2^24 values at the type's end add up
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
     float* const warp_m = merge + 2 * kCols * S::kOutPitch;  // [4][kCols]
@@ -814,6 +815,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     for (int i = 0; i < 4; i++) {
                         s[b][nt][i] = power2(fmaf(s[b][nt][i] - m[nt][i & 1], unit[nt][i & 1], kRaise));
                         l[nt][i & 1] += s[b][nt][i];
+                        if constexpr (!kFollow) s[b][nt][i] *= 1 / kLowered;
                     }
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
@@ -891,7 +893,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         }
         const int parts = last_worker - first_worker + 1;
         const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
-        const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
+        const float vscale = kNarrow ? p.pool.v_scale[kv] : kFollow ? 1.0f : kLowered;
         constexpr int kPartSize = kCols * (DP + 2);
         // a worker leaves at most two parts: of a group that began before it (0), and of one that goes on behind it (1)
         float* const my_part = p.parts + (2 * (int64_t)worker + (first_worker == worker ? 1 : 0)) * kPartSize;

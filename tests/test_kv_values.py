@@ -105,6 +105,17 @@ def test_weights_meet_bf16_values_unrounded(requests):
     check_weights("bf16", "bf16", requests)
 
 
+@pytest.mark.parametrize("n", [2, 33, 1000, 20000])
+@pytest.mark.parametrize("rise", [0.0, 5.0])
+def test_values_at_the_end_of_bf16(n, rise):
+    """Values of 3e38: their mean is as large, and a sum of two of them is not finite."""
+    g = gen(n)
+    x = rise * torch.arange(n, device="cuda")[None, :, None] / n + torch.zeros(2, n, 2, device="cuda")
+    v = 3e38 * (0.75 + 0.25 * torch.rand(2, n, 2, 64, generator=g, device="cuda"))
+    c, q, table, lengths = one_hot(x, v, "bf16", "bf16")
+    attend_within(c, q, table, lengths, 2.0 ** -16, scale=1.0)
+
+
 # ------------------------------------------------------------------------------------------ scales
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("scale", [None, -0.3, 0.0])
