@@ -89,7 +89,8 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
 /* table: [n_requests] rows of table_cols int32, row r at table + r * table_row; only the entries that a request's
  *   length reaches are read.  lengths: [n_requests] int32 tokens held, 0 .. max_length <= table_cols * page_size.
  * window > 0: only the newest `window` tokens are seen.  n_heads: a multiple of n_kv_heads; head h reads kv head
- *   h / (n_heads / n_kv_heads).  q: request r at q + r * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.
+ *   h / (n_heads / n_kv_heads).  q: request r at q + r * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.  (Of a BF16
+ *   query over E4M3, elements below 2^-31 of the head's largest finite one are rounded to 2^-38 of it.)
  * out: [n_requests][n_heads][head_dim] contiguous, in q's type.  lse: [n_requests][n_heads] fp32, the natural
  *   logarithm of the softmax sums, or NULL.  A request without tokens gives zeros and -infinity.
  * add_weight: cache->weight[token] += the softmax weights, summed over the heads of its group.  The requests of such

@@ -20,7 +20,8 @@
 //   each), so that nothing is lost beside the 32-bit sums: with one part less the output is 1.6e-4 (bf16) or 8.5e-4 (f16 weights of
 //   a bf16 output) of its norm from the same sums in 32 bits, with all 4e-5 and 7e-5.  The products cost nothing for bf16 (128
 //   requests 189.7 -> 190.0 us), 2 us of 80 over e4m3.  8-bit rows become f16 exactly; a bf16 query beside them is scaled by a
-//   power of two per head to lie in f16's range, with at least 38 bits below its largest element.
+//   power of two per head to lie in f16's range: exact down to 2^-31 of its largest finite element, nothing below 2^-38.  (A
+//   second path for such queries, by bands of 30 bits, took 83 -> 90 us from all of them.)
 #include <math.h>
 
 #include <atomic>
@@ -655,8 +656,20 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 if constexpr (kRescaled) {
                     big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
                     big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
-                    const int e = max((int)(__float_as_uint(big) >> 23), 27);  // biased; infinities stay what they are
-                    const float up = e >= 255 ? 1.0f : __uint_as_float((uint32_t)min(127 + 14 + 127 - e, 254) << 23);
+                    if (__any_sync(~0u, big == INFINITY)) {  // infinities stay what they are: the largest of the rest
+                        big = 0;
+#pragma unroll
+                        for (int k = 0; k < kSteps; k++)
+#pragma unroll
+                            for (int i = 0; i < 2; i++) {
+                                const float2 f = BF16::unpack(qf[nt][k][i]);
+                                big = fmaxf(big, fmaxf(fabsf(f.x) < INFINITY ? fabsf(f.x) : 0.0f, fabsf(f.y) < INFINITY ? fabsf(f.y) : 0.0f));
+                            }
+                        big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
+                        big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
+                    }
+                    const int e = max((int)(__float_as_uint(big) >> 23), 27);  // biased
+                    const float up = __uint_as_float((uint32_t)(127 + 14 + 127 - e) << 23);
                     power = 1.0f / up;  // a power of two: exact
 #pragma unroll
                     for (int k = 0; k < kSteps; k++)

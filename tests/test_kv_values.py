@@ -116,6 +116,46 @@ def test_values_at_the_end_of_bf16(n, rise):
     attend_within(c, q, table, lengths, 2.0 ** -16, scale=1.0)
 
 
+@pytest.mark.parametrize("large", [[2.0 ** 8], [2.0 ** 20, -2.0 ** 10]])
+@pytest.mark.parametrize("small", [1.0, 2.0 ** -20, 2.0 ** -100, 2.0 ** 100])
+def test_bf16_queries_of_a_wide_range_over_8_bits(large, small):
+    """Elements of q far below the head's largest decide the logits where the keys are zero beside the large ones."""
+    g = gen(len(large))
+    B, n, H, D = 5, 70, 2, 64
+    k = torch.randn(B * 5, PAGE, H, D, generator=g, device="cuda")
+    k[..., :len(large)] = 0
+    v = torch.randn(B * 5, PAGE, H, D, generator=g, device="cuda")
+    one = torch.ones(H, device="cuda")
+    c = kv.PagedKV(stored(k, "e4m3"), stored(v, "e4m3"), k_scale=one, v_scale=one)
+    q = (small * torch.randn(B, 6, D, generator=g, device="cuda")).bfloat16()
+    q[..., :len(large)] = (small * torch.tensor(large, device="cuda")).bfloat16()
+    q[0, 1] = 0                                       # a head without any
+    q[1, :, :len(large)] = 0                          # and one without large ones
+    table = torch.arange(B * 5, dtype=torch.int32, device="cuda").view(B, 5)
+    # sums of 64 products in 32 bits: 64 * 2^-23 of sum |q k|, which is below 100 here; twice, for the weight and for the sum
+    attend_within(c, q, table, [n] * B, 2.0 ** -9, scale=1.0 / small)
+
+
+def test_infinite_queries_over_8_bits():
+    """An infinite element of q: logits of -infinity where the key has the other sign, whatever the finite elements are."""
+    H, D = 1, 64
+    k = torch.zeros(5, PAGE, H, D, device="cuda")
+    k[..., 0] = -1
+    k[..., 1] = -1
+    k[2, :, :, 0] = 1
+    v = torch.randn(5, PAGE, H, D, generator=gen(1), device="cuda")
+    one = torch.ones(H, device="cuda")
+    c = kv.PagedKV(stored(k, "e4m3"), stored(v, "e4m3"), k_scale=one, v_scale=one)
+    q = torch.zeros(2, 2, D, dtype=torch.bfloat16, device="cuda")
+    q[0, :, 0] = float("inf")
+    q[0, :, 1] = -1e30
+    q[1, :, 1] = 1
+    out, lse = c.attend(q, torch.arange(5, dtype=torch.int32, device="cuda").expand(2, 5), to_int([32, 80]), return_lse=True, scale=1.0)
+    assert bool((out[0] == 0).all()) and bool((lse[0] == -math.inf).all())      # all of the 32 tokens' logits are -infinity
+    ref = c.v.float().double().reshape(80, D).mean(0)
+    assert bool(((out[1].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -18).all())
+
+
 # ------------------------------------------------------------------------------------------ scales
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("scale", [None, -0.3, 0.0])
