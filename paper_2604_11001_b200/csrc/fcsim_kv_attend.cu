@@ -927,7 +927,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
                         const int col = nt * 8 + 2 * (lane & 3) + i;
-                        f[i] = l[nt][i] == 0.0f ? 0.0f : vscale / l[nt][i];
+                        f[i] = vscale / l[nt][i];
+                        if (l[nt][i] == 0.0f) {  // zeros, also where a v is infinite
+                            f[i] = 0;
+#pragma unroll
+                            for (int k = 0; k < kSteps; k++) o[k][nt][i] = o[k][nt][2 + i] = 0;
+                        }
                         if (lane < 4 && col < cols) finish<M>(p, head0 + col, limit[nt][i] == -INFINITY ? -INFINITY : m[nt][i], l[nt][i], unit[nt][i]);
                     }
                     // two heads a lane become two or four neighbouring elements of one head: lane / 4

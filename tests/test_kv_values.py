@@ -200,3 +200,26 @@ def test_scales_near_zero_over_keys_at_the_end_of_bf16(scale):
     c, q, table, lengths = one_hot(x, torch.randn(3, 90, 2, 64, generator=g, device="cuda"), "bf16", "bf16")
     # a scale of 1e-39 has 20 bits, one of 3e-42 11, and logits of 0.3 and 0.001; the smallest unit is 2^-149, 5e-7 of a logit here
     attend_within(c, q, table, lengths, 2.0 ** -16, scale=scale)
+
+
+# ------------------------------------------------------------------------------------------ nothing left, by every division
+@pytest.mark.parametrize("cache", ["bf16", "f16", "e4m3"])
+@pytest.mark.parametrize("requests,n", [(1, 3), (1, 9000), (20, 100), (60, 700), (150, 200), (700, 3), (700, 40), (300, 400)])
+def test_requests_whose_logits_are_all_minus_infinity(cache, requests, n):
+    """Zeros and -infinity, as without tokens, whatever the values are and however the work is divided."""
+    H, D = 2, 64
+    pages = -(-n // PAGE)
+    k = torch.zeros(pages, PAGE, H, D, device="cuda")
+    k[..., 0] = 1
+    v = torch.randn(pages, PAGE, H, D, generator=gen(n), device="cuda")
+    v[..., 3], v[..., 5] = float("inf"), float("nan")
+    if cache == "e4m3":
+        v[..., 3] = float("nan")                        # (it has no infinity)
+    scales = [torch.ones(H, device="cuda")] * 2 if cache == "e4m3" else [None, None]
+    c = kv.PagedKV(stored(k, cache), stored(v, cache), None, *scales)
+    q = torch.zeros(requests, 4, D, dtype=torch.float16 if cache == "f16" else torch.bfloat16, device="cuda")
+    q[..., 0] = float("-inf")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").expand(requests, pages).contiguous()   # (pages are only read)
+    out, lse = c.attend(q, table, to_int([n] * requests), return_lse=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    c.check()
