@@ -37,7 +37,7 @@ extern "C" {
 enum { FCSIM_KV_F16 = 0, FCSIM_KV_BF16 = 1, FCSIM_KV_E4M3 = 2 };
 
 enum { /* bits of *status */
-    FCSIM_KV_BAD_PAGE = 1,     /* page or slot outside the pool: its tokens are left out */
+    FCSIM_KV_BAD_PAGE = 1,     /* page or slot outside the pool: its tokens are left out (evict: see there) */
     FCSIM_KV_BAD_LENGTH = 2,   /* length < 0 (taken as 0) or > max_length (taken as max_length) */
     FCSIM_KV_BAD_POSITION = 4, /* position outside the rope table: q_out row zero, nothing stored */
     FCSIM_KV_BAD_BUDGET = 8    /* budget < 0 (taken as 0) or > max_budget (taken as max_budget) */
@@ -122,7 +122,8 @@ int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* arg
 /* Request r keeps n' = min(length, budget[r]) tokens: the newest min(recent, budget), of what is left the oldest
  * min(first, budget - recent), then the largest weights (equal weights: the oldest first; NaN counts as the lowest,
  * and -0 as 0).  Kept tokens stay in order: token i of the new request is row kept[r][h][i] of the old one.  They are
- * copied with their weights to new_table's pages, which must not be among the pages read by the call.
+ * copied with their weights to new_table's pages, which must not be among the pages read by the call.  Tokens of a page
+ * outside the pool rank as NaN does; those that are kept become zeros of weight 0, and rows for one are not written.
  * new_lengths: [n_requests] int32.  kept: [n_requests][n_kv_heads][max_budget] int32, -1 beyond n'.
  * budget: [n_requests] int32, 0 .. max_budget <= new_cols * page_size.  Needs cache->weight.
  * workspace: 16-byte aligned, of the size fcsim_kv_evict_workspace reports (zeroed as above). */

@@ -295,20 +295,20 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, int r, int h, in
     const int t = p.kept[((int64_t)r * p.pool.n_kv + h) * p.max_budget + row];
     const int from = page_of(p.pool, t), into = page_of(p.pool, row);
     const int page = p.table[r * p.table_row + from], to = p.new_table[r * p.new_row + into];
-    if (page < 0 || page >= p.pool.n_pages || to < 0 || to >= p.pool.n_pages) {
-        flag(p.status, FCSIM_KV_BAD_PAGE);
-        return;
-    }
+    const bool there = (unsigned)page < (unsigned)p.pool.n_pages, room = (unsigned)to < (unsigned)p.pool.n_pages;
+    if (!there || !room) flag(p.status, FCSIM_KV_BAD_PAGE);
+    if (!room) return;
     if (lane < chunks) {
         const int64_t src = (page * p.pool.stride_page + (t - from * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
         const int64_t dst = (to * p.pool.stride_page + (row - into * size) * p.pool.stride_slot + h * p.pool.stride_head) * p.bytes + lane * 16;
-        const uint4 k = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + src)), v = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + src));
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;  // of a page that does not exist
+        if (there) k = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + src)), v = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + src));
         __stcs(reinterpret_cast<uint4*>(p.pool.k + dst), k);
         __stcs(reinterpret_cast<uint4*>(p.pool.v + dst), v);
     }
     if (lane == 0)
         p.pool.weight[((int64_t)to * p.pool.n_kv + h) * size + row - into * size] =
-            p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size];
+            there ? p.pool.weight[((int64_t)page * p.pool.n_kv + h) * size + t - from * size] : 0.0f;
 }
 
 // Which tokens one kv head of one request keeps, by one cluster.  Every CTA takes an equal slice of the candidates and

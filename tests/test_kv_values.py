@@ -223,3 +223,41 @@ def test_requests_whose_logits_are_all_minus_infinity(cache, requests, n):
     out, lse = c.attend(q, table, to_int([n] * requests), return_lse=True)
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
     c.check()
+
+
+# ------------------------------------------------------------------------------------------ evict
+@pytest.mark.parametrize("n,budget", [(40, 24), (1500, 900)])
+@pytest.mark.parametrize("recent,first", [(0, 0), (10, 10)])
+def test_evicted_rows_of_a_bad_page_are_zero(n, budget, recent, first):
+    """Tokens of a page outside the pool rank as NaN does; those that are kept become rows of zeros, not what the page held before."""
+    g = gen(n)
+    pages, cols, new_cols = 200, -(-n // PAGE), -(-budget // PAGE)
+    c = kv.PagedKV(torch.randn(pages, PAGE, 2, 64, generator=g, device="cuda").half(), torch.randn(pages, PAGE, 2, 64, generator=g, device="cuda").half(),
+                   torch.rand(pages, 2, PAGE, generator=g, device="cuda") + 1)
+    table = torch.arange(cols, dtype=torch.int32, device="cuda")[None].clone()
+    new = torch.arange(pages - new_cols, pages, dtype=torch.int32, device="cuda")[None].clone()
+    for wild in range(0, cols, 2):                     # half of the pages, the first among them: some must be kept
+        table[0, wild] = pages + wild
+    if cols % 2 == 0:
+        table[0, -1] = -1
+    k0, v0, w0 = c.k.clone(), c.v.clone(), c.weight.clone()
+    got, kept = c.evict(table, to_int([n]), to_int([budget]), new, recent=recent, first=first)
+    with pytest.raises(ValueError, match="page"):
+        c.check()
+    assert got.tolist() == [budget]
+    row = torch.arange(budget, device="cuda")
+    a, b = new[0].long()[row // PAGE], row % PAGE
+    bad = 0
+    for h in range(2):
+        old = kept[0, h, :budget].long()
+        assert bool((old[1:] > old[:-1]).all()) and int(old[0]) >= 0 and int(old[-1]) < n
+        page, place = table[0].long()[old // PAGE], old % PAGE
+        good = (page >= 0) & (page < pages)
+        bad += int((~good).sum())
+        page = page.clamp(0, pages - 1)
+        for pool, before in ((c.k, k0), (c.v, v0)):
+            want = torch.where(good[:, None], before[page, place, h], torch.zeros(64, device="cuda").half())
+            assert torch.equal(pool[a, b, h], want)
+        assert torch.equal(c.weight[a, h, b], torch.where(good, w0[page, h, place], torch.zeros((), device="cuda")))
+    assert bad > 0
+    assert torch.equal(c.k[:pages - new_cols], k0[:pages - new_cols]) and torch.equal(c.weight[:pages - new_cols], w0[:pages - new_cols])
