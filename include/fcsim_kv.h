@@ -69,7 +69,7 @@ typedef struct {
  *   of a call may have the same slot.
  * q_out: [n][n_heads][head_dim] contiguous.  n_heads = 0: q, q_norm, q_out are not used.
  * The weights of the slots written are set to 0.  All arithmetic in fp32, one rounding at the end; values beyond
- * E4M3's range are stored as +-448. */
+ * E4M3's range are stored as +-448.  n_tokens is at most 2^31 - 2^16. */
 typedef struct {
     const void *q, *k, *v;
     void* q_out;
@@ -98,7 +98,8 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
  * workspace: 16-byte aligned, of the size fcsim_kv_attend_workspace reports; its first `zeroed` bytes (the same for all
  *   calls) must be zero before the first call and are zero again after every call.  Calls that share it must be ordered;
  *   they may differ in everything else.
- * At most 65535 requests, and n_requests * max_length below 2^36 (FCSIM_EINVAL). */
+ * At most 65535 requests, n_requests * max_length below 2^36, max_length at most 2^31 - 2^16 and n_heads * head_dim below 2^31
+ * (FCSIM_EINVAL). */
 typedef struct {
     const void* q;
     void* out;
@@ -125,7 +126,8 @@ int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* arg
  * copied with their weights to new_table's pages, which must not be among the pages read by the call.  Tokens of a page
  * outside the pool rank as NaN does; those that are kept become zeros of weight 0, and rows for one are not written.
  * new_lengths: [n_requests] int32.  kept: [n_requests][n_kv_heads][max_budget] int32, -1 beyond n'.
- * budget: [n_requests] int32, 0 .. max_budget <= new_cols * page_size.  Needs cache->weight.
+ * budget: [n_requests] int32, 0 .. max_budget <= new_cols * page_size.  Needs cache->weight.  At most 65535 requests; max_length
+ * and max_budget are at most 2^31 - 2^16.
  * workspace: 16-byte aligned, of the size fcsim_kv_evict_workspace reports (zeroed as above). */
 typedef struct {
     const int32_t* table;

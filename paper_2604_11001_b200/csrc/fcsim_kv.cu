@@ -552,6 +552,9 @@ int launch_move(const EvictParams& p, int n_requests, cudaStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------------ validation
+// Tokens of a call, a request or a budget at most: the kernels count on past the end, by less than 2^16, in 32 bits.
+constexpr int kMaxTokens = 0x7fffffff - 0xffff;
+
 int cache_bytes(const fcsim_kv_cache* c) { return c->dtype == FCSIM_KV_E4M3 ? 1 : 2; }
 
 int check_cache(const fcsim_kv_cache* c, Pool* pool) {
@@ -584,6 +587,7 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     if ((rc = check_type(c, a->dtype)) != FCSIM_OK) return rc;
     if (a->n_requests < 0 || a->n_requests > 65535 || a->n_heads < 1 || a->n_heads % c->n_kv_heads) return FCSIM_EINVAL;
     if (a->table_cols < 0 || a->max_length < 0 || a->max_length > (int64_t)a->table_cols * c->page_size) return FCSIM_EINVAL;
+    if (a->max_length > kMaxTokens || (int64_t)a->n_heads * c->head_dim > 0x7fffffff) return FCSIM_EINVAL;
     if (a->window < 0 || a->table_row < 0 || !isfinite(a->scale)) return FCSIM_EINVAL;
     if (!good_stride(a->q_row, 2) || !good_stride(a->q_head, 2)) return FCSIM_EINVAL;
     if (a->n_requests > 0) {
@@ -665,6 +669,7 @@ int check_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args* a, EvictPara
     if (!a || a->n_requests < 0 || a->n_requests > 65535) return FCSIM_EINVAL;
     if (a->table_cols < 0 || a->max_length < 0 || a->max_length > (int64_t)a->table_cols * c->page_size) return FCSIM_EINVAL;
     if (a->new_cols < 0 || a->max_budget < 0 || a->max_budget > (int64_t)a->new_cols * c->page_size) return FCSIM_EINVAL;
+    if (a->max_length > kMaxTokens || a->max_budget > kMaxTokens) return FCSIM_EINVAL;
     if (a->recent < 0 || a->first < 0 || a->table_row < 0 || a->new_row < 0) return FCSIM_EINVAL;
     if (!c->weight) return FCSIM_ESIZE;
     if (a->n_requests > 0) {
@@ -686,7 +691,7 @@ extern "C" int fcsim_kv_append(const fcsim_kv_cache* c, const fcsim_kv_append_ar
     if (rc != FCSIM_OK) return rc;
     if (!a) return FCSIM_EINVAL;
     if ((rc = check_type(c, a->dtype)) != FCSIM_OK) return rc;
-    if (a->n_tokens < 0 || a->n_heads < 0 || !(a->eps >= 0) || !isfinite(a->eps)) return FCSIM_EINVAL;
+    if (a->n_tokens < 0 || a->n_tokens > kMaxTokens || a->n_heads < 0 || !(a->eps >= 0) || !isfinite(a->eps)) return FCSIM_EINVAL;
     if ((int64_t)a->n_heads + 2 * c->n_kv_heads > 65535) return FCSIM_EINVAL;
     if (!good_stride(a->q_row, 2) || !good_stride(a->q_head, 2) || !good_stride(a->k_row, 2) ||
         !good_stride(a->k_head, 2) || !good_stride(a->v_row, 2) || !good_stride(a->v_head, 2))

@@ -25,6 +25,7 @@ _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 _I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
+_MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
 # the current device's number and a device's current stream as plain integers, without the objects around them
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
@@ -282,7 +283,7 @@ class PagedKV:
         self._call(_lib.fcsim_kv_attend, _ATTEND.pack(
             q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self._status, q_row,
             q_head, table.stride(0), n, heads, _TYPES[dtype], cols,
-            cols * self.page_size if max_length is None else max_length, window, 1 if add_weight else 0,
+            min(cols * self.page_size, _MOST) if max_length is None else max_length, window, 1 if add_weight else 0,
             1.0 / math.sqrt(self.head_dim) if scale is None else scale), _lib.fcsim_kv_attend_workspace)
         return (out, lse) if return_lse else out
 
@@ -298,7 +299,7 @@ class PagedKV:
         if budget.dtype != _I32 or budget.numel() != n or budget.get_device() != index or not budget.is_contiguous():
             self._refuse("budget", f"contiguous int32 [{n}]", budget)
         if max_budget is None:
-            max_budget = new_cols * self.page_size
+            max_budget = min(new_cols * self.page_size, _MOST)
         if max_budget < 0:
             raise ValueError("max_budget: 0 or more")
         new_lengths = torch.empty_like(lengths)
@@ -306,7 +307,7 @@ class PagedKV:
         self._call(_lib.fcsim_kv_evict, _EVICT.pack(
             table.data_ptr(), lengths.data_ptr(), budget.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(),
             kept.data_ptr(), self._status, table.stride(0), new_table.stride(0), n, cols, new_cols,
-            cols * self.page_size if max_length is None else max_length, max_budget, recent, first, 0),
+            min(cols * self.page_size, _MOST) if max_length is None else max_length, max_budget, recent, first, 0),
             _lib.fcsim_kv_evict_workspace)
         return new_lengths, kept
 
