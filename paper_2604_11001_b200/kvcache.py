@@ -25,6 +25,7 @@ _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 _I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
+_NO_FIT = (struct.error, OverflowError)   # of a number that an argument struct has no room for
 _MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
 # the current device's number and a device's current stream as plain integers, without the objects around them
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -254,10 +255,14 @@ class PagedKV:
             if k_norm.dtype != dtype or k_norm.numel() != self.head_dim or k_norm.get_device() != index or not k_norm.is_contiguous():
                 self._refuse("k_norm", f"contiguous {dtype} [{self.head_dim}]", k_norm)
             k_norm_at = k_norm.data_ptr()
-        self._call(_lib.fcsim_kv_append, _APPEND.pack(
-            q_at, k.data_ptr(), v.data_ptr(), out_at, q_norm_at, k_norm_at, rope_at, positions_at, slots.data_ptr(),
-            self._status, q_row, q_head, k_row, k_head, v_row, v_head, n, heads, _TYPES[dtype], rope_dim, n_positions,
-            1 if interleaved else 0, eps, 0))
+        try:
+            args = _APPEND.pack(
+                q_at, k.data_ptr(), v.data_ptr(), out_at, q_norm_at, k_norm_at, rope_at, positions_at, slots.data_ptr(),
+                self._status, q_row, q_head, k_row, k_head, v_row, v_head, n, heads, _TYPES[dtype], rope_dim, n_positions,
+                1 if interleaved else 0, eps, 0)
+        except _NO_FIT as e:
+            raise ValueError(f"append: {e}") from None
+        self._call(_lib.fcsim_kv_append, args)
         return out
 
     def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, add_weight=False,
@@ -280,11 +285,15 @@ class PagedKV:
             self._refuse("lengths", f"contiguous int32 [{n}]", lengths)
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         lse = q.new_empty((n, heads), dtype=torch.float32) if return_lse else None
-        self._call(_lib.fcsim_kv_attend, _ATTEND.pack(
-            q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self._status, q_row,
-            q_head, table.stride(0), n, heads, _TYPES[dtype], cols,
-            min(cols * self.page_size, _MOST) if max_length is None else max_length, window, 1 if add_weight else 0,
-            1.0 / math.sqrt(self.head_dim) if scale is None else scale), _lib.fcsim_kv_attend_workspace)
+        try:
+            args = _ATTEND.pack(
+                q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self._status, q_row,
+                q_head, table.stride(0), n, heads, _TYPES[dtype], cols,
+                min(cols * self.page_size, _MOST) if max_length is None else max_length, window, 1 if add_weight else 0,
+                1.0 / math.sqrt(self.head_dim) if scale is None else scale)
+        except _NO_FIT as e:
+            raise ValueError(f"attend: {e}") from None
+        self._call(_lib.fcsim_kv_attend, args, _lib.fcsim_kv_attend_workspace)
         return (out, lse) if return_lse else out
 
     def evict(self, table, lengths, budget, new_table, *, max_budget=None, recent=0, first=0, max_length=None):
@@ -304,11 +313,14 @@ class PagedKV:
             raise ValueError("max_budget: 0 or more")
         new_lengths = torch.empty_like(lengths)
         kept = lengths.new_empty((n, self.n_kv_heads, max_budget))
-        self._call(_lib.fcsim_kv_evict, _EVICT.pack(
-            table.data_ptr(), lengths.data_ptr(), budget.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(),
-            kept.data_ptr(), self._status, table.stride(0), new_table.stride(0), n, cols, new_cols,
-            min(cols * self.page_size, _MOST) if max_length is None else max_length, max_budget, recent, first, 0),
-            _lib.fcsim_kv_evict_workspace)
+        try:
+            args = _EVICT.pack(
+                table.data_ptr(), lengths.data_ptr(), budget.data_ptr(), new_table.data_ptr(), new_lengths.data_ptr(),
+                kept.data_ptr(), self._status, table.stride(0), new_table.stride(0), n, cols, new_cols,
+                min(cols * self.page_size, _MOST) if max_length is None else max_length, max_budget, recent, first, 0)
+        except _NO_FIT as e:
+            raise ValueError(f"evict: {e}") from None
+        self._call(_lib.fcsim_kv_evict, args, _lib.fcsim_kv_evict_workspace)
         return new_lengths, kept
 
     def check(self):
