@@ -25,7 +25,7 @@ _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 _I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
-_NO_FIT = (struct.error, OverflowError)   # of a number that an argument struct has no room for
+_NO_FIT = struct.error   # of a number that an argument struct has no room for
 _MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
 # the current device's number and a device's current stream as plain integers, without the objects around them
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream

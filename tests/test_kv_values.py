@@ -6,6 +6,7 @@ import torch
 
 from kv_common import DT, TINY, UNIT, assert_attend, ref_attend
 from paper_2604_11001_b200 import kvcache as kv
+from paper_2604_11001_b200.binding import FcsimError
 
 pytestmark = pytest.mark.gpu
 
@@ -266,12 +267,14 @@ def test_evicted_rows_of_a_bad_page_are_zero(n, budget, recent, first):
 def test_numbers_that_do_not_fit_are_refused():
     c = kv.PagedKV.allocate(8, PAGE, 1, 64, torch.float16, weight=True)
     x, table, n = torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda"), to_int([[0]]), to_int([1])
-    for bad in (dict(max_length=2 ** 40), dict(window=2 ** 33), dict(window=-2 ** 40), dict(scale=1e300), dict(window=0.5)):
+    for bad in (dict(max_length=2 ** 40), dict(window=2 ** 33), dict(window=-2 ** 40), dict(window=0.5)):
         with pytest.raises(ValueError):
             c.attend(x, table, n, **bad)
     for bad in (dict(recent=2 ** 31), dict(first=-2 ** 31 - 1), dict(max_length=2 ** 40)):
         with pytest.raises(ValueError):
             c.evict(table, n, n, to_int([[1]]), **bad)
-    with pytest.raises(ValueError):
+    with pytest.raises(FcsimError):                    # (infinity in 32 bits)
+        c.attend(x, table, n, scale=1e300)
+    with pytest.raises(FcsimError):
         c.append(x, x, x, None, torch.tensor([0], device="cuda"), eps=1e300)
     c.check()
