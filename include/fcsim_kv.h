@@ -128,7 +128,7 @@ int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* arg
  * new_lengths: [n_requests] int32.  kept: [n_requests][n_kv_heads][max_budget] int32, -1 beyond n'.
  * budget: [n_requests] int32, 0 .. max_budget <= new_cols * page_size.  Needs cache->weight.  At most 65535 requests; max_length
  * and max_budget are at most 2^31 - 2^16.
- * workspace: 16-byte aligned, of the size fcsim_kv_evict_workspace reports (zeroed as above). */
+ * workspace: none is needed at present; fcsim_kv_evict_workspace reports {0, 0}, and NULL will do. */
 typedef struct {
     const int32_t* table;
     const int32_t* lengths;

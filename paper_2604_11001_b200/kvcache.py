@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import struct
+import threading
 
 import torch
 
@@ -25,6 +26,10 @@ _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 _I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
 _ESIZE = -3
+# device -> stream -> workspace of that stream's calls, whichever cache they are of (a stream's calls follow one another; the lock
+# keeps the launches of one call together where threads share a stream)
+_WORKSPACES = {}
+_LOCK = threading.Lock()
 _NO_FIT = struct.error   # of a number that an argument struct has no room for
 _MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
 # the current device's number and a device's current stream as plain integers, without the objects around them
@@ -118,6 +123,7 @@ class PagedKV:
     ``k_scale``, ``v_scale``: [n_kv_heads] float32 for 8-bit caches: a stored x stands for x * scale.
 
     Calls run on the current stream; calls on different streams that touch the same pages are the caller's to order.
+    All caches of a device share one workspace per stream, kept for good.
     The object is not thread-safe."""
 
     def __init__(self, k, v, weight=None, k_scale=None, v_scale=None):
@@ -141,7 +147,7 @@ class PagedKV:
         self.device, self._index = k.device, k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._status = self.status.data_ptr()
-        self._workspaces = {}   # stream -> zero-initialised workspace, so that streams never share one
+        self._workspaces = _WORKSPACES.setdefault(self._index, {})   # of the device
         self._c = fcsim_kv_cache(k.data_ptr(), v.data_ptr(), _pointer(weight), _pointer(k_scale), _pointer(v_scale),
                                  k.stride(0), k.stride(1), k.stride(2), _TYPES[k.dtype], n_pages, page_size, n_kv,
                                  head_dim, 0)
@@ -187,24 +193,32 @@ class PagedKV:
         if size is None:
             code = entry(self._c_ref, args, stream)
         else:
-            buf = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream)
-            code = _ESIZE
-            if buf is not None:
-                code = entry(self._c_ref, args, buf.data_ptr(), buf.numel(), stream)
-            if code == _ESIZE:
-                need = fcsim_kv_workspace()
-                code = size(self._c_ref, args, C.byref(need))
-                if code == 0:
-                    buf = self._workspace(stream, need.bytes)
+            with _LOCK:
+                buf = None if torch.cuda.is_current_stream_capturing() else self._workspaces.get(stream)
+                if buf is None:  # (enough for the calls that need none)
+                    code = entry(self._c_ref, args, None, 0, stream)
+                else:
                     code = entry(self._c_ref, args, buf.data_ptr(), buf.numel(), stream)
+                if code == _ESIZE:
+                    need = fcsim_kv_workspace()
+                    code = size(self._c_ref, args, C.byref(need))
+                    if code == 0:
+                        buf = self._workspace(stream, need.bytes, need.zeroed)
+                        code = entry(self._c_ref, args, buf.data_ptr(), buf.numel(), stream)
         if code != 0:
             _raise(code, entry.__name__)
 
-    def _workspace(self, stream, size):
-        """Zeroed when new; every call leaves the part that has to be zero as it found it.  A graph under capture
-        gets its own, whose zeroing is part of the graph."""
-        buf = torch.zeros(max(size, 16), dtype=torch.uint8, device=self.device)
-        if not torch.cuda.is_current_stream_capturing():
+    def _workspace(self, stream, size, zeroed):
+        """A new workspace, kept for the stream's later calls.  Its first `zeroed` bytes are cleared; every call leaves them
+        as it found them, and the rest does not matter.  One that replaces a smaller one grows by half of it at least.  A graph
+        under capture gets its own for each call, whose clearing is part of the graph."""
+        capturing = torch.cuda.is_current_stream_capturing()
+        old = None if capturing else self._workspaces.get(stream)
+        if old is not None:
+            size = max(size, old.numel() * 3 // 2)
+        buf = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+        buf[:zeroed].zero_()
+        if not capturing:
             self._workspaces[stream] = buf
         return buf
 

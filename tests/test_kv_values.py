@@ -278,3 +278,88 @@ def test_numbers_that_do_not_fit_are_refused():
     with pytest.raises(FcsimError):
         c.append(x, x, x, None, torch.tensor([0], device="cuda"), eps=1e300)
     c.check()
+
+
+# ------------------------------------------------------------------------------------------ calls
+def test_layers_share_a_workspace_and_only_its_counters_are_cleared():
+    """One workspace per stream whatever the number of caches; of a new one the part that has to be zero is cleared, no more."""
+    g = gen(1)
+    make = lambda: kv.PagedKV.allocate(600, PAGE, 2, 64, torch.float16, weight=True)  # noqa: E731
+    a, b = make(), make()
+    for c in (a, b):
+        c.k.normal_(generator=g), c.v.normal_(generator=g)
+    table = torch.arange(600, dtype=torch.int32, device="cuda").view(2, 300)
+    q = torch.randn(2, 16, 64, generator=g, device="cuda").half()
+    ln = to_int([4800, 4701])
+    with torch.cuda.stream(torch.cuda.Stream()):
+        old = torch.full((96 << 20,), 255, dtype=torch.uint8, device="cuda")   # what the allocator hands out next
+        del old
+        first = a.attend(q, table, ln, add_weight=True, return_lse=True)
+        stream = torch.cuda.current_stream().cuda_stream
+        work = a._workspaces[stream]
+        assert b.attend(q, table, ln) is not None and b._workspaces[stream] is work
+        assert not bool(work[:64 * 1024].any())
+        torch.cuda.synchronize()
+        before = a.weight.clone()
+        a.weight.zero_()
+        again = a.attend(q, table, ln, add_weight=True, return_lse=True)
+        assert all(torch.equal(x, y) for x, y in zip(first, again)) and torch.equal(before, a.weight)
+    # under capture: a call's own workspace, of which the graph clears the counters
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out = a.attend(q, table, ln, return_lse=True)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
+
+
+def test_a_fresh_workspace_is_not_cleared_whole():
+    c = kv.PagedKV.allocate(64, PAGE, 2, 64, torch.float16)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        size = 8 << 20
+        old = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        del old
+        buf = c._workspace(torch.cuda.current_stream().cuda_stream, size, 64 * 1024)
+        assert buf.numel() >= size and not bool(buf[:64 * 1024].any()) and bool((buf[64 * 1024:size] == 255).all())
+        assert c._workspace(0, 128, 0).numel() >= 128
+
+
+def test_an_eviction_keeps_no_workspace():
+    c = kv.PagedKV.allocate(8, PAGE, 1, 64, torch.float16, weight=True)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        c.evict(to_int([[0, 1]]), to_int([32]), to_int([16]), to_int([[2]]))
+        assert torch.cuda.current_stream().cuda_stream not in c._workspaces
+    c.check()
+
+
+def test_threads_with_caches_of_their_own_share_a_stream():
+    import threading
+    g = gen(2)
+    stream, got, want = torch.cuda.Stream(), {}, {}
+    caches = []
+    for i in range(4):
+        c = kv.PagedKV.allocate(300, PAGE, 2, 64, torch.float16, weight=True)
+        c.k.normal_(generator=g), c.v.normal_(generator=g)
+        table = torch.arange(300, dtype=torch.int32, device="cuda").view(3, 100)
+        caches.append((c, torch.randn(3, 8, 64, generator=g, device="cuda").half(), table, to_int([1600, 1500 - i, 40 * i])))
+    for i, (c, q, table, n) in enumerate(caches):
+        want[i] = c.attend(q, table, n, add_weight=True), c.weight.clone()
+        c.weight.zero_()
+    torch.cuda.synchronize()
+
+    def work(i):
+        c, q, table, n = caches[i]
+        with torch.cuda.stream(stream):
+            for _ in range(50):
+                c.weight.zero_()
+                got[i] = c.attend(q, table, n, add_weight=True)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i, (c, *_) in enumerate(caches):
+        assert torch.equal(got[i], want[i][0]) and torch.equal(c.weight, want[i][1])
+        c.check()
