@@ -147,6 +147,7 @@ class PagedKV:
         self.device, self._index = k.device, k.get_device()
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._status = self.status.data_ptr()
+        torch.cuda.current_stream(k.device).synchronize()   # cleared, whatever stream the calls come on
         self._workspaces = _WORKSPACES.setdefault(self._index, {})   # of the device
         self._c = fcsim_kv_cache(k.data_ptr(), v.data_ptr(), _pointer(weight), _pointer(k_scale), _pointer(v_scale),
                                  k.stride(0), k.stride(1), k.stride(2), _TYPES[k.dtype], n_pages, page_size, n_kv,
@@ -338,7 +339,9 @@ class PagedKV:
         return new_lengths, kept
 
     def check(self):
-        """Read and clear the device status; raise when a call met a bad page, length, position or budget."""
+        """Wait for all calls, on every stream, read and clear the device status; raise when a call met a bad page, length, position
+        or budget."""
+        torch.cuda.synchronize(self.device)
         bits = int(self.status.item())
         if bits:
             self.status.zero_()

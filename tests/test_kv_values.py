@@ -363,3 +363,34 @@ def test_threads_with_caches_of_their_own_share_a_stream():
     for i, (c, *_) in enumerate(caches):
         assert torch.equal(got[i], want[i][0]) and torch.equal(c.weight, want[i][1])
         c.check()
+
+
+def test_check_waits_for_calls_on_every_stream():
+    c = kv.PagedKV.allocate(8, PAGE, 1, 64, torch.float16)
+    q, table, n = torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda"), to_int([[99]]), to_int([5])
+    x = torch.randn(8192, 8192, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(10):
+            x = x @ x                                   # long work before the call
+        c.attend(q, table, n)
+    with pytest.raises(ValueError, match="page"):
+        c.check()
+    torch.cuda.synchronize()
+    c.check()
+
+
+def test_a_cache_made_behind_long_work_is_ready_for_other_streams():
+    k, v = (torch.zeros(8, PAGE, 1, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    q, table, n = torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda"), to_int([[99]]), to_int([5])
+    x = torch.randn(8192, 8192, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(10):
+            x = x @ x
+        c = kv.PagedKV(k, v)                            # its status word is cleared behind that
+    with torch.cuda.stream(torch.cuda.Stream()):
+        c.attend(q, table, n)
+    torch.cuda.synchronize()
+    with pytest.raises(ValueError, match="page"):
+        c.check()
