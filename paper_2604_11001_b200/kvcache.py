@@ -32,6 +32,7 @@ _WORKSPACES = {}
 _LOCK = threading.Lock()
 _NO_FIT = struct.error   # of a number that an argument struct has no room for
 _MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
+_grad_enabled = torch.is_grad_enabled
 # the current device's number and a device's current stream as plain integers, without the objects around them
 _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
@@ -111,6 +112,12 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _no_gradient(*tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError("a tensor requires a gradient, and there is no backward pass: detach it, or call under no_grad()")
+
+
 def _pointer(t):
     return 0 if t is None else t.data_ptr()
 
@@ -122,6 +129,7 @@ class PagedKV:
     ``weight``: [n_pages, n_kv_heads, page_size] float32, the attention each cached token has received.
     ``k_scale``, ``v_scale``: [n_kv_heads] float32 for 8-bit caches: a stored x stands for x * scale.
 
+    There is no backward pass: tensors that require a gradient are refused, unless gradients are off.
     Calls run on the current stream; calls on different streams that touch the same pages are the caller's to order.
     All caches of a device share one workspace per stream, kept for good.
     The object is not thread-safe."""
@@ -230,6 +238,8 @@ class PagedKV:
 
         ``rope``: float32 [positions, rope_dim], cosines then sines; ``positions``: int32 [n].  ``q_norm``,
         ``k_norm``: [head_dim] weights of the norms over each head.  ``q`` may be None (nothing is returned)."""
+        if _grad_enabled():
+            _no_gradient(q, k, v, rope, q_norm, k_norm)
         dtype, shape, index = k.dtype, k.shape, self._index
         if dtype not in _WIDE or len(shape) != 3 or shape[1] != self.n_kv_heads or shape[2] != self.head_dim \
                 or k.get_device() != index:
@@ -288,6 +298,8 @@ class PagedKV:
 
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
         only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
+        if q.requires_grad and _grad_enabled():
+            _no_gradient(q)
         dtype, shape, index = q.dtype, q.shape, self._index
         if dtype not in _WIDE or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
             self._refuse("q", f"float16 or bfloat16 [requests, heads, {self.head_dim}]", q)

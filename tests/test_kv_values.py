@@ -394,3 +394,26 @@ def test_a_cache_made_behind_long_work_is_ready_for_other_streams():
     torch.cuda.synchronize()
     with pytest.raises(ValueError, match="page"):
         c.check()
+
+
+def test_tensors_that_want_a_gradient_are_refused():
+    """There is no backward pass: results without one must not be taken for results with it."""
+    c = kv.PagedKV.allocate(8, PAGE, 1, 64, torch.float16)
+    x = torch.randn(1, 1, 64, device="cuda").half()
+    slot, table, n = torch.tensor([0], device="cuda"), to_int([[0]]), to_int([1])
+    w, rope = torch.ones(64, dtype=torch.float16, device="cuda"), torch.rand(4, 64, device="cuda")
+    g = lambda t: t.detach().clone().requires_grad_()  # noqa: E731
+    for bad in (dict(q=g(x)), dict(k=g(x)), dict(v=g(x)), dict(q_norm=g(w)), dict(k_norm=g(w)), dict(rope=g(rope))):
+        args = {**dict(q=x, k=x, v=x, positions=to_int([0]), slots=slot, rope=rope, q_norm=w, k_norm=w), **bad}
+        with pytest.raises(ValueError, match="gradient"):
+            c.append(**args)
+        with torch.no_grad():
+            c.append(**args)
+    with pytest.raises(ValueError, match="gradient"):
+        c.attend(g(x), table, n)
+    with torch.inference_mode():
+        c.attend(x, table, n)
+    with torch.no_grad():
+        out = c.attend(g(x), table, n)
+    assert not out.requires_grad
+    c.check()
