@@ -53,13 +53,14 @@ def active_set(cfg: wl.SimConfig, usage: int, rng, limit: Optional[int] = None) 
 
 
 class Layer:
-    """One layer's cache with room for `lengths` and for what they grow to, and the slots on it."""
+    """One layer's cache with room for `lengths` and for what they grow to in `spare` slots, and the slots on it."""
 
     def __init__(self, lengths, heads=64, kv_heads=8, head_dim=128, cache="bf16", budget=None, spare=256, device="cuda:0", seed=0):
         import torch
 
         from .kvcache import PagedKV
         self.torch, self.budget, self.device = torch, budget, torch.device(device)
+        self.spare_slots = spare
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         self.dtype = torch.float16 if cache == "f16" else torch.bfloat16
         store = {"f16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[cache]
@@ -75,7 +76,7 @@ class Layer:
         self.spare = None if budget is None else order[n * self.columns:].view(n, self.columns).contiguous()
         self.lengths = torch.zeros(n, dtype=torch.int32, device=self.device)
         self.positions = torch.zeros(n, dtype=torch.int32, device=self.device)   # of the next token; cut requests go on counting
-        angle = torch.arange(max(lengths) + 4096, device=self.device, dtype=torch.float64)[:, None] \
+        angle = torch.arange(max(lengths) + spare + 1, device=self.device, dtype=torch.float64)[:, None] \
             * 10000.0 ** (-torch.arange(0, head_dim, 2, device=self.device, dtype=torch.float64) / head_dim)
         self.rope = torch.cat((angle.cos(), angle.sin()), 1).float()
         self.norm = torch.ones(head_dim, dtype=self.dtype, device=self.device)
@@ -109,6 +110,9 @@ class Layer:
     def grow(self):
         """One whole slot: a new token per request, then the cut of those that have outgrown their budget."""
         torch = self.torch
+        if self.spare_slots == 0:
+            raise ValueError("the layer has no room (pages, positions) for another slot: make it with more `spare`")
+        self.spare_slots -= 1
         n = self.lengths.numel()
         slots = self._slots(torch.arange(n, device=self.device), self.lengths)
         self.lengths += 1
@@ -162,7 +166,7 @@ def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6,
     rows = []
     for u in np.unique(np.quantile(busy, np.linspace(0.05, 1.0, points)).astype(int)):
         lengths = active_set(cfg, int(u), rng, budget)
-        layer = Layer(lengths, heads, kv_heads, head_dim, cache, budget, device=device, seed=seed)
+        layer = Layer(lengths, heads, kv_heads, head_dim, cache, budget, spare=grow, device=device, seed=seed)
         us = layer.time()
         for _ in range(grow):
             layer.grow()
