@@ -66,7 +66,7 @@ class Layer:
         store = {"f16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[cache]
         self.generator = torch.Generator(device=self.device)
         self.generator.manual_seed(seed)
-        grown = max(lengths) + spare if budget is None else budget + SLACK
+        grown = max(lengths) + spare + 1 if budget is None else budget + SLACK   # (one more: time() after the last)
         self.columns = -(-max(grown, max(lengths) + 1) // PAGE)
         pages = len(lengths) * self.columns * (1 if budget is None else 2)
         self.cache = PagedKV.allocate(pages, PAGE, kv_heads, head_dim, store, weight=budget is not None, device=self.device)
@@ -129,12 +129,9 @@ class Layer:
                 self.table[over], self.spare[over] = new, old
         return out
 
-    def time(self, repeats=20):
-        """Microseconds of one slot at the present lengths (median, on the device)."""
+    def _timed(self, call, repeats):
+        """Microseconds of a call (median, on the device), the L2 cache filled with other data before each."""
         torch = self.torch
-        n = self.lengths.numel()
-        inputs = (self._rows(n, self.heads), self._rows(n, self.kv_heads), self._rows(n, self.kv_heads),
-                  self._slots(torch.arange(n, device=self.device), self.lengths - 1))
         times = []
         with torch.cuda.device(self.device):
             flush = torch.empty(64 << 20, dtype=torch.float32, device=self.device)   # twice the L2 cache
@@ -142,13 +139,28 @@ class Layer:
                 flush.sum()
                 a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
                 a.record()
-                self.step(*inputs)
+                call()
                 b.record()
                 b.synchronize()
                 if i >= 3:
                     times.append(a.elapsed_time(b) * 1e3)
         self.cache.check()
         return float(np.median(times))
+
+    def time(self, repeats=20):
+        """Microseconds of the next slot.  The layer is left as it was: the slot's tokens lie behind its requests' last ones, and
+        the weights are put back."""
+        torch = self.torch
+        n = self.lengths.numel()
+        inputs = (self._rows(n, self.heads), self._rows(n, self.kv_heads), self._rows(n, self.kv_heads),
+                  self._slots(torch.arange(n, device=self.device), self.lengths))
+        weight = None if self.budget is None else self.cache.weight.clone()
+        self.lengths += 1
+        us = self._timed(lambda: self.step(*inputs), repeats)
+        self.lengths -= 1
+        if weight is not None:
+            self.cache.weight.copy_(weight)
+        return us
 
 
 def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6, grow: int = 0, budget: Optional[int] = None,
