@@ -7,9 +7,10 @@ of the preset goes through, one append and one attend per slot, timed on the dev
     microseconds(U) = a + b U
 
 through the times, and with it the simulated run's results in seconds per layer instead of slots (the run's own trace
-gives every slot's U_t).  With ``--budget`` requests are also cut to that many tokens by accumulated attention weight,
-whenever one has grown ``SLACK`` tokens past it: the eviction of tokens that the slotted model, which evicts whole
-requests, has no form of.
+gives every slot's U_t).  With ``--budget`` each request's cache is also cut to that many tokens by accumulated attention
+weight, whenever it has grown ``SLACK`` tokens past it: the eviction of tokens that the slotted model, which evicts whole
+requests, has no form of.  The requests of a slot stay those of the simulated run (admission counts whole requests, and U is
+their usage); what the budget changes is what they hold on the GPU, and the time of a slot, to which the cuts add.
 
     python -m paper_2604_11001_b200.slot_time [--preset 2] [--slots 2000] [--cache e4m3] [--budget 256]
 """
@@ -36,7 +37,7 @@ def _draw(table: wl.Table, rng) -> int:
 def active_set(cfg: wl.SimConfig, usage: int, rng, limit: Optional[int] = None) -> List[int]:
     """Lengths of requests that hold `usage` tokens together: classes and lengths from the preset's laws, generated
     tokens as in a slot picked at random (an output of o tokens is met o times as often, at a uniform point of it).
-    At most ``cfg.Acap`` requests; ``limit`` cuts every one (a token budget)."""
+    At most ``cfg.Acap`` requests.  ``limit`` (a token budget) then cuts every one: the requests stay the same."""
     lengths: List[int] = []
     held = 0
     longest = [t.vmax for t in cfg.decode]
@@ -45,11 +46,10 @@ def active_set(cfg: wl.SimConfig, usage: int, rng, limit: Optional[int] = None) 
         prompt, out = _draw(cfg.prompt[k], rng), _draw(cfg.decode[k], rng)
         if rng.random() * max(longest) > out:
             continue
-        n = prompt + int(rng.integers(0, out))
-        n = min(n, usage - held, n if limit is None else limit)
+        n = min(prompt + int(rng.integers(0, out)), usage - held)
         lengths.append(n)
         held += n
-    return lengths
+    return lengths if limit is None else [min(n, limit) for n in lengths]
 
 
 class Layer:
@@ -121,13 +121,15 @@ class Layer:
         if self.budget is not None:
             over = (self.lengths >= self.budget + SLACK).nonzero()[:, 0]
             if over.numel():
-                budget = torch.full((over.numel(),), self.budget, dtype=torch.int32, device=self.device)
                 old, new = self.table[over].contiguous(), self.spare[over].contiguous()
-                kept, _ = self.cache.evict(old, self.lengths[over].contiguous(), budget, new, max_budget=self.budget,
-                                           recent=self.budget // 4, first=FIRST)
+                kept, _ = self._cut(old, self.lengths[over].contiguous(), new)
                 self.lengths[over] = kept
                 self.table[over], self.spare[over] = new, old
         return out
+
+    def _cut(self, old, lengths, new):
+        budget = self.torch.full_like(lengths, self.budget)
+        return self.cache.evict(old, lengths, budget, new, max_budget=self.budget, recent=self.budget // 4, first=FIRST)
 
     def _timed(self, call, repeats):
         """Microseconds of a call (median, on the device), the L2 cache filled with other data before each."""
@@ -162,6 +164,19 @@ class Layer:
             self.cache.weight.copy_(weight)
         return us
 
+    def time_cuts(self, repeats=20):
+        """Microseconds that cuts add to a slot on average.  A request past its budget is cut once in SLACK slots, so `due` of them
+        are in a slot: one call for these, or, where they are less than one, a call for one in so many slots.  (The rows
+        move to the pages that wait for the next cut; the layer is left as it was.)"""
+        over = (self.lengths >= self.budget).nonzero()[:, 0]
+        due = over.numel() / SLACK
+        if due == 0:
+            return 0.0
+        over = over[:max(1, round(due))]
+        old, new = self.table[over].contiguous(), self.spare[over].contiguous()
+        lengths = self.torch.full((over.numel(),), self.budget + SLACK, dtype=self.torch.int32, device=self.device)
+        return min(1.0, due) * self._timed(lambda: self._cut(old, lengths, new), repeats)
+
 
 def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6, grow: int = 0, budget: Optional[int] = None,
         heads: int = 64, kv_heads: int = 8, head_dim: int = 128, cache: str = "bf16", device: str = "cuda:0", seed: int = 0) -> dict:
@@ -173,17 +188,21 @@ def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6,
     _, summary = sim.stats(want_counters=False)
     usage = sim.trace()[:, :, 0].cpu().numpy()   # [replicas of all groups, slots]
     sim.close()
-    rng = np.random.default_rng(seed)
+    rng, since_cut = np.random.default_rng(seed), np.random.default_rng([seed, 1])   # (the sets do not depend on the budget)
     busy = usage[usage > 0]
     rows = []
     for u in np.unique(np.quantile(busy, np.linspace(0.05, 1.0, points)).astype(int)):
-        lengths = active_set(cfg, int(u), rng, budget)
-        layer = Layer(lengths, heads, kv_heads, head_dim, cache, budget, spare=grow, device=device, seed=seed)
-        us = layer.time()
+        whole = active_set(cfg, int(u), rng)
+        # with a budget: the same requests, each that has outgrown it somewhere between two cuts
+        held = whole if budget is None else [n if n < budget else budget + int(since_cut.integers(0, SLACK)) for n in whole]
+        layer = Layer(held, heads, kv_heads, head_dim, cache, budget, spare=grow, device=device, seed=seed)
+        cuts = 0.0 if budget is None else layer.time_cuts()
+        us = layer.time() + cuts
         for _ in range(grow):
             layer.grow()
         layer.cache.check()
-        rows.append(dict(usage=int(sum(lengths)), requests=len(lengths), longest=max(lengths), us=us))
+        rows.append(dict(usage=int(sum(whole)), requests=len(whole), longest=max(whole) if budget is None else min(max(whole), budget),
+                         held=int(sum(held)), us=us, cuts_us=cuts))
         del layer
     x = np.array([[1.0, r["usage"]] for r in rows])
     a, b = np.linalg.lstsq(x, np.array([r["us"] for r in rows]), rcond=None)[0] if len(rows) > 1 else (rows[0]["us"], 0.0)
@@ -209,15 +228,15 @@ def main():
     ap.add_argument("--kv-heads", type=int, default=8)
     ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--cache", default="bf16", choices=("bf16", "f16", "e4m3"))
-    ap.add_argument("--budget", type=int, default=None, help="tokens a request may keep")
-    ap.add_argument("--grow", type=int, default=0, help="slots to run on from each timed set (with --budget: and cut)")
+    ap.add_argument("--budget", type=int, default=None, help="tokens a request's cache is cut to")
+    ap.add_argument("--grow", type=int, default=0, help="slots to run on from each timed set, cuts among them")
     args = ap.parse_args()
     got = run(args.preset, args.slots, args.replicas, grow=args.grow, budget=args.budget, heads=args.heads, kv_heads=args.kv_heads,
               head_dim=args.head_dim, cache=args.cache)
     print("%s, one layer, %d heads on %d of %d, %s cache" % (got["preset"], args.heads, args.kv_heads, args.head_dim, args.cache))
-    print("%10s %10s %10s %12s" % ("tokens", "requests", "longest", "us per slot"))
+    print("%10s %10s %10s %10s %12s %12s" % ("tokens", "requests", "longest", "held", "us per slot", "of it cuts"))
     for r in got["rows"]:
-        print("%10d %10d %10d %12.2f" % (r["usage"], r["requests"], r["longest"], r["us"]))
+        print("%10d %10d %10d %10d %12.2f %12.2f" % (r["usage"], r["requests"], r["longest"], r["held"], r["us"], r["cuts_us"]))
     print("us(U) = %.2f + %.6f U" % (got["a_us"], got["b_us"]))
     for g in got["groups"]:
         print("policy %d: %.2f us a slot, mean latency %.1f slots = %.3f ms a layer, %.0f tokens/s a layer" % (

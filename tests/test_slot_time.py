@@ -40,3 +40,46 @@ def test_timing_a_slot_leaves_the_layer_as_it_was(budget):
     assert all(torch.equal(a, b) for a, b in zip(before, held()))
     layer.grow()                                       # the pages have room for the next slot all the same
     layer.cache.check()
+
+
+def test_a_budget_cuts_the_requests_that_there_are():
+    """It takes no others in: the number of requests and their order are those of the uncut set."""
+    import numpy as np
+
+    from paper_2604_11001_b200 import workloads as wl
+    for cfg, usage in ((wl.config2(), 8000), (wl.config2(), 65536), (wl.config5(), 100000), (wl.config6(), 16492)):
+        whole = st.active_set(cfg, usage, np.random.default_rng(1))
+        cut = st.active_set(cfg, usage, np.random.default_rng(1), limit=40)
+        assert cut == [min(n, 40) for n in whole]
+        assert sum(whole) == usage or len(whole) == cfg.Acap
+
+
+@pytest.mark.gpu
+def test_a_smaller_budget_takes_less_time():
+    """Predicted from the same simulated run: its usages, its requests, less of each on the GPU; the cuts are in the time."""
+    got = [st.run(2, slots=600, replicas=2, points=4, budget=b) for b in (None, 512, 64)]
+    for g, budget in zip(got[1:], (512, 64)):
+        assert [(r["usage"], r["requests"]) for r in g["rows"]] == [(r["usage"], r["requests"]) for r in got[0]["rows"]]
+        assert all(r["held"] < r["requests"] * (budget + st.SLACK) for r in g["rows"])
+        assert any(r["cuts_us"] > 0 for r in g["rows"]) and all(r["us"] > r["cuts_us"] for r in g["rows"])
+        assert [x["mean_latency_slots"] for x in g["groups"]] == [x["mean_latency_slots"] for x in got[0]["groups"]]
+    times = [[x["slot_us"] for x in g["groups"]] for g in got]
+    for i in range(2):
+        assert times[2][i] < times[0][i]
+    assert got[2]["rows"][-1]["us"] < got[0]["rows"][-1]["us"]
+
+
+@pytest.mark.gpu
+def test_timing_cuts_leaves_the_layer_as_it_was():
+    import torch
+    layer = st.Layer([5, 40, 70] + [60] * 130, heads=4, kv_heads=2, head_dim=64, cache="f16", budget=40, spare=2)
+    t = torch.cat([torch.arange(n) for n in layer.lengths.tolist()]).cuda()
+    r = torch.repeat_interleave(torch.arange(layer.lengths.numel(), device="cuda"), layer.lengths.long())
+    held = lambda: [x.view(-1, 2, 64)[layer._slots(r, t)].clone() for x in (layer.cache.k, layer.cache.v)] \
+        + [layer.cache.weight.transpose(1, 2).reshape(-1, 2)[layer._slots(r, t)].clone(), layer.lengths.clone(), layer.table.clone()]  # noqa: E731
+    before = held()
+    assert layer.time_cuts(3) > 0
+    assert all(torch.equal(a, b) for a, b in zip(before, held()))
+    layer.grow()
+    layer.cache.check()
+    assert st.Layer([5, 6], heads=4, kv_heads=2, head_dim=64, cache="f16", budget=40).time_cuts() == 0.0
