@@ -6,8 +6,10 @@ of the preset goes through, one append and one attend per slot, timed on the dev
 
     microseconds(U) = a + b U
 
-through the times, and with it the simulated run's results in seconds per layer instead of slots (the run's own trace
-gives every slot's U_t).  With ``--budget`` each request's cache is also cut to that many tokens by accumulated attention
+through the times, and with it the simulated run's results in seconds per layer instead of slots: the run's own trace gives
+every slot's U_t and so its time (a slot without requests takes that of an empty one, a), its log every request's first and last
+slot, whose times add up to its latency.  In a slot's time are the new tokens of its requests, not the prompts of those that
+begin in it: nothing here attends over a prompt.  With ``--budget`` each request's cache is also cut to that many tokens by accumulated attention
 weight, whenever it has grown ``SLACK`` tokens past it: the eviction of tokens that the slotted model, which evicts whole
 requests, has no form of.  The requests of a slot stay those of the simulated run (admission counts whole requests, and U is
 their usage); what the budget changes is what they hold on the GPU, and the time of a slot, to which the cuts add.
@@ -178,15 +180,26 @@ class Layer:
         return min(1.0, due) * self._timed(lambda: self._cut(old, lengths, new), repeats)
 
 
+def latency_seconds(seconds, done, latency):
+    """Seconds from the first to the last slot of requests that completed in slot `done` (1, 2, ..) after `latency` slots, that one
+    and the first included; `seconds` of every slot."""
+    clock = np.concatenate(([0.0], np.cumsum(seconds)))
+    return clock[done] - clock[done - latency]
+
+
 def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6, grow: int = 0, budget: Optional[int] = None,
         heads: int = 64, kv_heads: int = 8, head_dim: int = 128, cache: str = "bf16", device: str = "cuda:0", seed: int = 0) -> dict:
     """Simulate the preset, time slots at usages its trace goes through, and turn the run's slots into seconds."""
     from . import binding as fb
-    cfg = PRESETS[preset](replicas=replicas, T=slots).with_(trace_stride=1)
+    cfg = PRESETS[preset](replicas=replicas, T=slots)
+    arrivals = max(t.vmax for a in cfg.arrivals for t in a.count)
+    cfg = cfg.with_(trace_stride=1, complog_cap=slots * arrivals)   # (no more than that can complete)
     sim = fb.Simulation(cfg, device=device)
     sim.run(slots)
-    _, summary = sim.stats(want_counters=False)
+    counters, summary = sim.stats()
     usage = sim.trace()[:, :, 0].cpu().numpy()   # [replicas of all groups, slots]
+    logged = counters[:, fb.COUNTER_NAMES.index("n_logged")]
+    log = sim.complog()[:, :max(1, int(logged.max()))].cpu().numpy()
     sim.close()
     rng, since_cut = np.random.default_rng(seed), np.random.default_rng([seed, 1])   # (the sets do not depend on the budget)
     busy = usage[usage > 0]
@@ -206,16 +219,17 @@ def run(preset: int = 2, slots: int = 2000, replicas: int = 16, points: int = 6,
         del layer
     x = np.array([[1.0, r["usage"]] for r in rows])
     a, b = np.linalg.lstsq(x, np.array([r["us"] for r in rows]), rcond=None)[0] if len(rows) > 1 else (rows[0]["us"], 0.0)
-    seconds = (a * (usage > 0) + b * usage) * 1e-6   # of every slot of every replica
+    seconds = (a + b * usage) * 1e-6   # of every slot of every replica
     out = dict(preset=cfg.name, rows=rows, a_us=float(a), b_us=float(b), groups=[])
     start = 0
     for g, s in zip(cfg.groups, summary):
-        mine = seconds[start:start + g.n_replicas]
+        mine = range(start, start + g.n_replicas)
         start += g.n_replicas
-        slot = float(mine.sum() / (g.n_replicas * slots))
+        slot = float(seconds[mine].mean())
+        waits = np.concatenate([latency_seconds(seconds[r], *log[r, :logged[r]].T) for r in mine])
         out["groups"].append(dict(policy=g.policy, slot_us=slot * 1e6, mean_latency_slots=s["mean_latency"],
-                                  mean_latency_ms=s["mean_latency"] * slot * 1e3,
-                                  tokens_per_second=s["token_throughput"] / slot if slot > 0 else 0.0))
+                                  mean_latency_ms=float(waits.mean()) * 1e3 if waits.size else float("nan"),
+                                  tokens_per_second=s["token_throughput"] / slot))
     return out
 
 
@@ -233,7 +247,7 @@ def main():
     args = ap.parse_args()
     got = run(args.preset, args.slots, args.replicas, grow=args.grow, budget=args.budget, heads=args.heads, kv_heads=args.kv_heads,
               head_dim=args.head_dim, cache=args.cache)
-    print("%s, one layer, %d heads on %d of %d, %s cache" % (got["preset"], args.heads, args.kv_heads, args.head_dim, args.cache))
+    print("%s, one layer, %d heads on %d of %d, %s cache (no prompts in the times)" % (got["preset"], args.heads, args.kv_heads, args.head_dim, args.cache))
     print("%10s %10s %10s %10s %12s %12s" % ("tokens", "requests", "longest", "held", "us per slot", "of it cuts"))
     for r in got["rows"]:
         print("%10d %10d %10d %10d %12.2f %12.2f" % (r["usage"], r["requests"], r["longest"], r["held"], r["us"], r["cuts_us"]))

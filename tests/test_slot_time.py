@@ -83,3 +83,47 @@ def test_timing_cuts_leaves_the_layer_as_it_was():
     layer.grow()
     layer.cache.check()
     assert st.Layer([5, 6], heads=4, kv_heads=2, head_dim=64, cache="f16", budget=40).time_cuts() == 0.0
+
+
+def test_latencies_are_the_times_of_a_requests_own_slots():
+    """Idle slots before and after a request are none of its latency, full ones in it are."""
+    import numpy as np
+    seconds = np.array([1.0, 1.0, 7.0, 7.0, 1.0, 1.0, 2.0, 1.0])
+    done, latency = np.array([4, 7, 3, 8]), np.array([2, 1, 1, 8])
+    assert st.latency_seconds(seconds, done, latency).tolist() == [14.0, 2.0, 7.0, 21.0]
+    assert st.latency_seconds(seconds, done[:0], latency[:0]).size == 0
+
+
+@pytest.mark.gpu
+def test_results_in_seconds_follow_from_the_runs_own_slots():
+    """A system that is idle half of the time, replayed request by request from its trace and log."""
+    import numpy as np
+
+    from paper_2604_11001_b200 import binding as fb
+    from paper_2604_11001_b200 import workloads as wl
+    preset = lambda replicas, T: wl.config6(replicas=replicas, T=T, total_rate=0.02)  # noqa: E731
+    old = st.PRESETS.get(6)
+    st.PRESETS[6] = preset
+    try:
+        got = st.run(6, slots=3000, replicas=4, points=3, heads=4, kv_heads=2, head_dim=64, cache="f16")
+    finally:
+        st.PRESETS[6] = old
+    cfg = preset(4, 3000).with_(complog_cap=3000)
+    sim = fb.Simulation(cfg)
+    sim.run(3000)
+    counters, _ = sim.stats()
+    usage, log = sim.trace()[:, :, 0].cpu().numpy(), sim.complog().cpu().numpy()
+    sim.close()
+    assert 0.1 < (usage == 0).mean() < 0.9
+    for g, mine in enumerate(np.split(np.arange(cfg.n_replicas), len(cfg.groups))):
+        waits, total = [], 0.0
+        for r in mine:
+            us = got["a_us"] + got["b_us"] * usage[r]
+            total += us.sum()
+            for done, latency in log[r, :counters[r, fb.COUNTER_NAMES.index("n_logged")]]:
+                waits.append(sum(us[done - latency:done]))
+        one = got["groups"][g]
+        assert one["mean_latency_ms"] == pytest.approx(np.mean(waits) * 1e-3, rel=1e-9)
+        assert one["slot_us"] == pytest.approx(total / (len(mine) * 3000), rel=1e-9)
+        tokens = counters[mine, fb.COUNTER_NAMES.index("tokens_generated")].sum()
+        assert one["tokens_per_second"] == pytest.approx(tokens / (total * 1e-6), rel=0.1)
