@@ -125,8 +125,13 @@ __device__ __forceinline__ void append_heads(const AppendParams& p, const char* 
             }
             if (KIND != kQuery && C::bytes == 1) {
                 const float s = 1.0f / scale[i];
+                if (fabsf(s) < INFINITY) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] *= s;
+                    for (int e = 0; e < 8; e++) x[e] *= s;
+                } else {  // a scale below 2^-128, or none
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] /= scale[i];
+                }
             }
             if (stored) {
                 store4<Out>(to_lo, x);

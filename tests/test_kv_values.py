@@ -417,3 +417,19 @@ def test_tensors_that_want_a_gradient_are_refused():
         out = c.attend(g(x), table, n)
     assert not out.requires_grad
     c.check()
+
+
+# ------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("scale", [1e-39, -1e-39, 1e-44, 2.0 ** -127])
+def test_append_by_scales_whose_reciprocal_is_not_finite(scale):
+    """What is stored is x / scale: zero stays zero, the rest reaches the type's end, or less where x is as small."""
+    c = kv.PagedKV.allocate(2, PAGE, 1, 64, torch.float8_e4m3fn, k_scale=torch.tensor([scale], device="cuda"), v_scale=torch.tensor([scale], device="cuda"))
+    x = torch.zeros(1, 1, 64, device="cuda")
+    x[..., 0], x[..., 1], x[..., 2], x[..., 3] = 1.0, -1.0, scale, 2 * scale
+    x = x.bfloat16()
+    c.append(None, x, x, None, torch.tensor([3], device="cuda"))
+    c.check()
+    want = (x.double() / torch.tensor(scale, device="cuda").float().double()).clamp(-448, 448)[0, 0]
+    for pool in (c.k, c.v):
+        got = pool[0, 3, 0].float().double()
+        assert bool(((got - want).abs() <= UNIT[torch.float8_e4m3fn] * want.abs()).all()), got[:4]
