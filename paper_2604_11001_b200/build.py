@@ -55,16 +55,21 @@ def _compile(lib: str, verbose: bool, extra) -> str:
               "-Xcompiler", "-fPIC,-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
         common += ["-Xptxas", "-v"]
-    common += list(extra)
-    jobs = [(HOST_SOURCE, [], os.path.join(OBJ_DIR, f"{tag}_host.o"))]
+    extra = list(extra)
+    jobs = [(HOST_SOURCE, extra, os.path.join(OBJ_DIR, f"{tag}_host.o"))]
     for pol in range(N_KERNEL_POLICIES):
-        jobs.append((KERNEL_SOURCE, [f"-DFCSIM_KERNEL_POLICY={pol}"], os.path.join(OBJ_DIR, f"{tag}_policy{pol}.o")))
-    jobs.append((KV_SOURCE, [], os.path.join(OBJ_DIR, f"{tag}_kv.o")))
+        jobs.append((KERNEL_SOURCE, extra + [f"-DFCSIM_KERNEL_POLICY={pol}"], os.path.join(OBJ_DIR, f"{tag}_policy{pol}.o")))
+    # the cache's objects are the same in both builds: the checked one takes those that are there
+    kv = [(KV_SOURCE, [], os.path.join(OBJ_DIR, "kv.o"))]
     for types in range(N_KV_TYPES):
-        jobs.append((KV_ATTEND_SOURCE, [f"-DFCSIM_KV_TYPES={types}"], os.path.join(OBJ_DIR, f"{tag}_kv_attend{types}.o")))
+        kv.append((KV_ATTEND_SOURCE, [f"-DFCSIM_KV_TYPES={types}"], os.path.join(OBJ_DIR, f"kv_attend{types}.o")))
+    jobs += kv
+    there = {obj for _, _, obj in kv if extra and not _stale(obj)}
 
     def one(job):
         src, defs, obj = job
+        if obj in there:
+            return subprocess.CompletedProcess([], 0, "", "")
         return subprocess.run(common + defs + ["-c", src, "-o", obj], capture_output=True, text=True)
 
     with ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 1)) as pool:
