@@ -112,10 +112,8 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _no_gradient(*tensors):
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            raise ValueError("a tensor requires a gradient, and there is no backward pass: detach it, or call under no_grad()")
+def _refuse_gradient():
+    raise ValueError("a tensor requires a gradient, and there is no backward pass: detach it, or call under no_grad()")
 
 
 def _pointer(t):
@@ -238,8 +236,9 @@ class PagedKV:
 
         ``rope``: float32 [positions, rope_dim], cosines then sines; ``positions``: int32 [n].  ``q_norm``,
         ``k_norm``: [head_dim] weights of the norms over each head.  ``q`` may be None (nothing is returned)."""
-        if _grad_enabled():
-            _no_gradient(q, k, v, rope, q_norm, k_norm)
+        if (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) or (rope is not None and rope.requires_grad)
+                or (q_norm is not None and q_norm.requires_grad) or (k_norm is not None and k_norm.requires_grad)) and _grad_enabled():
+            _refuse_gradient()
         dtype, shape, index = k.dtype, k.shape, self._index
         if dtype not in _WIDE or len(shape) != 3 or shape[1] != self.n_kv_heads or shape[2] != self.head_dim \
                 or k.get_device() != index:
@@ -299,7 +298,7 @@ class PagedKV:
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
         only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
         if q.requires_grad and _grad_enabled():
-            _no_gradient(q)
+            _refuse_gradient()
         dtype, shape, index = q.dtype, q.shape, self._index
         if dtype not in _WIDE or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
             self._refuse("q", f"float16 or bfloat16 [requests, heads, {self.head_dim}]", q)
