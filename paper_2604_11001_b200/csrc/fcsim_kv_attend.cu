@@ -482,7 +482,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
     constexpr bool kFollow = std::is_same<M, F16>::value;
     constexpr float kRaise = kRaiseOf<M>, kLag = kFollow ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
-    constexpr float kLowered = 4294967296.0f;  // 2^32: bf16 weights meet v that much smaller, so that 2^24 values at the type's end add up
+    // bf16 weights meet v times 2^-24, so that 2^16 values at the type's end add up whatever their weights are.  (Values below
+    // 2^-94 lose bits by it.)
+    constexpr float kLowered = 16777216.0f;
     extern __shared__ __align__(128) char smem[];
     float* const merge = reinterpret_cast<float*>(smem + S::kStages * S::kStage);
     float* const warp_m = merge + 2 * kCols * S::kOutPitch;  // [4][kCols]

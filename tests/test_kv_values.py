@@ -117,6 +117,15 @@ def test_values_at_the_end_of_bf16(n, rise):
     attend_within(c, q, table, lengths, 2.0 ** -16, scale=1.0)
 
 
+@pytest.mark.parametrize("small", [1e-20, 1e-28])
+def test_small_bf16_values_keep_their_precision(small):
+    g = gen(4)
+    x = torch.randn(3, 500, 2, generator=g, device="cuda")
+    v = small * (1 + torch.rand(3, 500, 2, 64, generator=g, device="cuda"))
+    c, q, table, lengths = one_hot(x, v, "bf16", "bf16")
+    attend_within(c, q, table, lengths, 2.0 ** -16, scale=1.0)
+
+
 @pytest.mark.parametrize("large", [[2.0 ** 8], [2.0 ** 20, -2.0 ** 10]])
 @pytest.mark.parametrize("small", [1.0, 2.0 ** -20, 2.0 ** -100, 2.0 ** 100])
 def test_bf16_queries_of_a_wide_range_over_8_bits(large, small):
