@@ -326,8 +326,8 @@ template <class T, class C, int DP, int NT>
 struct Shape {
     static constexpr int kRow = DP * C::bytes;
     static constexpr int kPitch = kRow + 16;                    // bytes of a row in shared memory: 8 rows of a column cover all banks
-    // tokens of a warp: 8-bit rows want twice as many for each tile's fixed work (64 requests, 82 -> 78 us; 16-bit rows of 128
-    // bytes lose more by fewer CTAs on an SM: 47 -> 55)
+    // tokens of a warp: 8-bit rows want twice as many for each tile's fixed work (64 requests over e4m3, 94 -> 83 us; 16-bit rows of
+    // 128 bytes lose more by fewer CTAs on an SM: 100 requests in f16, 40.0 -> 42.6)
     static constexpr int kTokens = C::bytes == 1 && kRow == 128 ? 32 : 16;
     static constexpr int kTile = 4 * kTokens, kTileBits = kTokens == 32 ? 7 : 6;
     static constexpr int kStage = kTile * 2 * kPitch;           // K and V of a tile
@@ -338,7 +338,7 @@ struct Shape {
     static constexpr int stages(int ctas) { return ((228 / ctas - 1) * 1024 - kMerge - kSmall - kStatic) / kStage; }
     // As many CTAs on an SM (three at most) as registers and two stages each allow, then as many stages as there is room for.  When every SM
     // has work for long, only kFair of them are used: more only queue, SMs differ more in the rate they get, and a call
-    // ends with the slowest (131 072 tokens of one request, three stages of 32 KB 99 us, two 96).  When each CTA has one
+    // ends with the slowest (131 072 tokens of one request, three stages of 32 KB 100 us, two 96; 128 heavy-tailed requests 196, 190).  When each CTA has one
     // short piece, all: nothing but the loads' latency counts (16 requests of 1 024 tokens 22 -> 18 us).
     static constexpr int kRegisterCtas = DP * NT <= 128 && kRow <= 128 ? 3 : 2;
     static constexpr int kCtas = stages(kRegisterCtas) >= 2 ? kRegisterCtas : stages(2) >= 2 ? 2 : 1;
@@ -1118,7 +1118,7 @@ int ctas_per_sm(int device, int* out) {
 template <class T, class C, int DP>
 AttendVariant of_group(int group) {
     // more than 8 heads: two column tiles share every load; beyond 16, and for the widest rows (whose registers do not
-    // suffice: 145 us, rows read twice 126), the rows are read again
+    // suffice: 32 requests, 16 heads on each kv head of 256, 172 us, rows read twice 136), the rows are read again
     if constexpr (DP <= 128)
         if (group > 8) return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP, Shape<T, C, DP, 2>::kTileBits};
     return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP, Shape<T, C, DP, 1>::kTileBits};

@@ -5,7 +5,7 @@
 namespace fcsim_kv_dev {
 
 constexpr int kThreads = 128;
-constexpr int kWeightCtas = 6;    // CTAs of the weights' kernel on an SM (4, 6, 8, 12: 50.1, 47.1, 48.2, 51.7 us in all)
+constexpr int kWeightCtas = 6;    // CTAs of the weights' kernel on an SM (100 requests in f16, 4, 6, 8, 12: 53.6, 50.5, 50.5, 54.2 us in all)
 constexpr int kMaxDevices = 64;   // devices for which answers of the runtime are remembered
 constexpr int kMaxCtas = 4096;   // bound of the grid (the work is divided among the CTAs at run time)
 
