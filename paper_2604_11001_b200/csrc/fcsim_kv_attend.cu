@@ -77,6 +77,20 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// 64 8-bit elements at `row` (per lane) + 0 .. 63 of 16 tokens, transposed, as the first operand of four products.  A lane gets bytes
+// 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8.
+__device__ __forceinline__ void load_narrow_transposed(uint32_t row, uint32_t (&a)[4][4]) {
+    uint32_t w[2][4];
+    load_matrices_transposed(row, w[0]);
+    load_matrices_transposed(row + 32, w[1]);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
+        a[k][0] = E4M3::halves(__byte_perm(x, 0, 0x4420)), a[k][1] = E4M3::halves(__byte_perm(x, 0, 0x4431));
+        a[k][2] = E4M3::halves(__byte_perm(y, 0, 0x4420)), a[k][3] = E4M3::halves(__byte_perm(y, 0, 0x4431));
+    }
+}
+
 // Two weights as one operand word, rounded down and one more step below: what is left of them for the next part is above zero
 // then, and no part is zero unless the weight is nearly (2^-23 for f16), so that an infinite v stays infinite.
 template <class M>
@@ -480,8 +494,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     constexpr int kParts = std::is_same<M, F16>::value ? 2 : 3;  // 11 bits each, or 8: of the softmax weights
     constexpr float kLog2e = 1.4426950408889634f;
     // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
-    constexpr bool kFollow = std::is_same<M, F16>::value;
-    constexpr float kRaise = kRaiseOf<M>, kLag = kFollow ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
+    constexpr bool kHalf = std::is_same<M, F16>::value, kFollow = kHalf && !kNarrow;
+    constexpr float kRaise = kRaiseOf<M>, kLag = kHalf ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
+    constexpr float kStep = 1.0f / 256, kFiner = 274877906944.0f, kFew = 0.125f, kSlight = 1.0f / 32;  // 2^-8, 2^38, 2^-3, 2^-5: see the end of a tile
+    constexpr int kPasses = 3;
     // bf16 weights meet v times 2^-24, so that 2^16 values at the type's end add up whatever their weights are.  (Values below
     // 2^-94 lose bits by it.)
     constexpr float kLowered = 16777216.0f;
@@ -707,40 +723,48 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 
         if (mask) {  // (a warp may have no token of a request's last tile)
             const uint32_t krow = ring + stage * S::kStage, vrow = krow + kTokens * S::kPitch;
-            // ---- s^T = K q^T: 16 tokens by 8 heads at a time
-            float s[kSub][NT][4] = {};
+            auto score = [&](float (&s)[kSub][NT][4]) {  // s^T = K q^T: 16 tokens by 8 heads at a time
 #pragma unroll
-            for (int b = 0; b < kSub; b++) {
-                const uint32_t row = krow + (b * 16 + (lane & 7) + ((lane >> 3) & 1) * 8) * S::kPitch + (lane >> 4) * 16;
-                if constexpr (!kNarrow) {
+                for (int b = 0; b < kSub; b++) {
+                    const uint32_t row = krow + (b * 16 + (lane & 7) + ((lane >> 3) & 1) * 8) * S::kPitch + (lane >> 4) * 16;
+                    if constexpr (!kNarrow) {
 #pragma unroll
-                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
-                        uint32_t a[4][4];
+                        for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                            uint32_t a[4][4];
 #pragma unroll
-                        for (int k = 0; k < 4; k++) load_matrices(row + (k0 + k) * 32, a[k]);
+                            for (int k = 0; k < 4; k++) load_matrices(row + (k0 + k) * 32, a[k]);
 #pragma unroll
-                        for (int k = 0; k < 4; k++)
+                            for (int k = 0; k < 4; k++)
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a[k], qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
-                    }
-                } else {
+                                for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a[k], qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
+                        }
+                    } else {
 #pragma unroll
-                    for (int k0 = 0; k0 < kSteps; k0 += 4) {
-                        uint32_t w[2][4];
-                        load_matrices(row + k0 * 16, w[0]);
-                        load_matrices(row + k0 * 16 + 32, w[1]);
+                        for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                            uint32_t w[2][4];
+                            load_matrices(row + k0 * 16, w[0]);
+                            load_matrices(row + k0 * 16 + 32, w[1]);
 #pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
-                            const uint32_t a[4] = {E4M3::halves(x), E4M3::halves(y), E4M3::halves(x >> 16), E4M3::halves(y >> 16)};
+                            for (int k = 0; k < 4; k++) {
+                                const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
+                                const uint32_t a[4] = {E4M3::halves(x), E4M3::halves(y), E4M3::halves(x >> 16), E4M3::halves(y >> 16)};
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
+                                for (int nt = 0; nt < NT; nt++) mma<M>(s[b][nt], a, qf[nt][k0 + k][0], qf[nt][k0 + k][1]);
+                            }
                         }
                     }
                 }
-            }
-            // ---- softmax: this lane holds tokens lane / 4 and + 8 of every 16, of heads 2 (lane % 4) and + 1
+            };
+            auto forget = [&](float (&s)[NT][4], int b, int nt) {  // tokens that do not exist
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (!(mask >> (16 * b + lane / 4 + 8 * (i >> 1)) & 1)) s[nt][i] = -INFINITY;
+            };
             uint32_t part[kParts][kSub][NT][2];
+            float s[kSub][NT][4] = {};
+            score(s);
+            uint32_t least = ~0u;  // of the weights above zero, as bits, less one
+            // ---- softmax: this lane holds tokens lane / 4 and + 8 of every 16, of heads 2 (lane % 4) and + 1
 #pragma unroll
             for (int nt = 0; nt < NT; nt++) {
                 if (logits) {
@@ -758,10 +782,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 }
                 if (mask != kAll) {
 #pragma unroll
-                    for (int b = 0; b < kSub; b++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            if (!(mask >> (16 * b + lane / 4 + 8 * (i >> 1)) & 1)) s[b][nt][i] = -INFINITY;
+                    for (int b = 0; b < kSub; b++) forget(s[b], b, nt);
                 }
                 float most[2];
 #pragma unroll
@@ -772,9 +793,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 // The reference moves only when a logit is 2^kLag above it: the weights stay far from f16's and fp32's ends, and
                 // the maximum over the lanes is taken a few times in a request instead of in every tile.  f16 has steps of
                 // 2^-24, so beside it the reference also moves down where all of a tile's tokens lie 2^-kDeep below it (one
-                // token may hold nearly all of the sum and have a v of nothing); the 32-bit sums grow by as much.  A weight's
-                // rounding is then 2^-17 of its tile's largest at most, 2^-39 of it in that one token's own tile.  (100 requests
-                // in f16 41.1 -> 42.6 us, 64 over e4m3 80.3 -> 83.0; with a reach of 2^8 up, 42.2 and 2^-32 in its own tile.)
+                // token may hold nearly all of the sum and have a v of nothing); the 32-bit sums grow by as much.  (For 8-bit rows
+                // see the end of the tile.)  A weight's rounding is then 2^-17 of its tile's largest at most, 2^-39 of it in that
+                // one token's own tile, which is below f16's own steps for values up to 2^10.  (100 requests in f16, attention alone,
+                // 41.1 -> 42.6 us; with a reach of 2^8 up, 42.2, and 2^-32 in its own tile.)
                 bool moves;
                 if constexpr (kFollow) {
                     bool low[2];
@@ -830,7 +852,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     for (int i = 0; i < 4; i++) {
                         s[b][nt][i] = power2(fmaf(s[b][nt][i] - m[nt][i & 1], unit[nt][i & 1], kRaise));
                         l[nt][i & 1] += s[b][nt][i];
-                        if constexpr (!kFollow) s[b][nt][i] *= 1 / kLowered;
+                        if constexpr (kNarrow) least = __viaddmin_u32(__float_as_uint(s[b][nt][i]), ~0u, least);
+                        if constexpr (!kHalf) s[b][nt][i] *= 1 / kLowered;
                     }
 #pragma unroll
                     for (int k = 0; k < 2; k++) {
@@ -869,20 +892,140 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     const uint32_t row = vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16;
 #pragma unroll
                     for (int k0 = 0; k0 < kSteps; k0 += 4) {
-                        // a lane gets bytes 2n, 2n + 1 of two tokens: even and odd elements become rows n and n + 8
-                        uint32_t w[2][4];
-                        load_matrices_transposed(row + k0 * 16, w[0]);
-                        load_matrices_transposed(row + k0 * 16 + 32, w[1]);
+                        uint32_t a[4][4];
+                        load_narrow_transposed(row + k0 * 16, a);
 #pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            const uint32_t x = w[k / 2][2 * (k & 1)], y = w[k / 2][2 * (k & 1) + 1];
-                            const uint32_t a[4] = {E4M3::halves(__byte_perm(x, 0, 0x4420)), E4M3::halves(__byte_perm(x, 0, 0x4431)),
-                                                   E4M3::halves(__byte_perm(y, 0, 0x4420)), E4M3::halves(__byte_perm(y, 0, 0x4431))};
+                        for (int k = 0; k < 4; k++)
 #pragma unroll
                             for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                                for (int i = 0; i < kParts; i++) mma<M>(o[k0 + k][nt], a, part[i][b][nt][0], part[i][b][nt][1]);
+                                for (int i = 0; i < kParts; i++) mma<M>(o[k0 + k][nt], a[k], part[i][b][nt][0], part[i][b][nt][1]);
+                    }
+                }
+            }
+            // Weights below kStep are few of f16's steps, too few where those above meet a v of nothing and the output is bf16.  So where
+            // there are any and an element of the sums is still slight (below kSlight, of weights of 2^14 at the reference), what their
+            // rounding has lost follows in up to three passes, kFiner times as large in each and added up apart: 22 bits of weights of any
+            // size.  If a head has no others here, its reference moves down for the tiles to come.  (No 8-bit value is infinite, so a part may
+            // be zero or negative.  It stands behind the products so that nothing comes between these and the weights.  64 requests over
+            // e4m3: without any of it 81.3 us, with it 82.9; with logits four times as wide 86.9, without the test of the sums 124.)
+            if constexpr (kNarrow) {
+                bool lost = __any_sync(~0u, least < __float_as_uint(kStep) - 1);
+                if (lost) {
+                    float slight = INFINITY;
+#pragma unroll
+                    for (int k = 0; k < kSteps; k++)
+                        if (k * 16 < D) {
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int i = 0; i < 4; i++) slight = fminf(slight, fabsf(o[k][nt][i]));
                         }
+                    lost = __any_sync(~0u, slight < kSlight);
+                }
+                if (lost) {
+                    float w[kSub][NT][4] = {};
+                    score(w);
+                    float top[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) {
+                        top[nt][0] = top[nt][1] = 0;
+#pragma unroll
+                        for (int b = 0; b < kSub; b++) {
+                            if (mask != kAll) forget(w[b], b, nt);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                float& x = w[b][nt][i];
+                                x = power2(fmaf(x - m[nt][i & 1], unit[nt][i & 1], kRaise));
+                                top[nt][i & 1] = fmaxf(top[nt][i & 1], x);
+                                x = x < kStep ? x : 0.0f;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < kSub; b++)  // what the two parts have left of them
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                            for (int k = 0; k < 2; k++) {
+                                float &x = w[b][nt][2 * k], &y = w[b][nt][2 * k + 1];
+                                float2 f = M::unpack(below<M>(x, y));
+                                x -= f.x, y -= f.y;
+                                f = M::unpack(M::pack(x, y));
+                                x -= f.x, y -= f.y;
+                            }
+                    float lower = 1;
+#pragma unroll 1
+                    for (int pass = 0; pass < kPasses; pass++) {
+                        bool more = false;
+#pragma unroll
+                        for (int b = 0; b < kSub; b++)
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int k = 0; k < 2; k++) {
+                                    float &x = w[b][nt][2 * k], &y = w[b][nt][2 * k + 1];
+                                    x *= kFiner, y *= kFiner;
+                                    const bool few_x = fabsf(x) < kFew, few_y = fabsf(y) < kFew;  // (and few bits again)
+                                    more |= (few_x && x != 0.0f) || (few_y && y != 0.0f);
+                                    const uint32_t h = M::pack(x, y);
+                                    float2 f = M::unpack(h);
+                                    x -= f.x, y -= f.y;
+                                    const uint32_t g = M::pack(x, y);
+                                    f = M::unpack(g);
+                                    x = few_x ? x - f.x : 0.0f, y = few_y ? y - f.y : 0.0f;
+                                    part[0][b][nt][k] = transpose8x8(h);
+                                    part[1][b][nt][k] = transpose8x8(g);
+                                }
+                        lower /= kFiner;
+#pragma unroll
+                        for (int k0 = 0; k0 < kSteps; k0 += 4) {
+                            float apart[4][NT][4] = {};
+#pragma unroll
+                            for (int b = 0; b < kSub; b++) {
+                                uint32_t a[4][4];
+                                load_narrow_transposed(vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16 + k0 * 16, a);
+#pragma unroll
+                                for (int k = 0; k < 4; k++)
+#pragma unroll
+                                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                        for (int i = 0; i < kParts; i++) mma<M>(apart[k][nt], a[k], part[i][b][nt][0], part[i][b][nt][1]);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+#pragma unroll
+                                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                    for (int i = 0; i < 4; i++) o[k0 + k][nt][i] += apart[k][nt][i] * lower;
+                        }
+                        if (!__any_sync(~0u, more)) break;
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++) {
+                        float grow[2];
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            float highest = top[nt][i], most_l = l[nt][i];
+#pragma unroll
+                            for (int d = 4; d < 32; d *= 2) {
+                                highest = fmaxf(highest, __shfl_xor_sync(~0u, highest, d));
+                                most_l = fmaxf(most_l, __shfl_xor_sync(~0u, most_l, d));
+                            }
+                            grow[i] = 1;
+                            if (highest > 0.0f && highest < kStep) {
+                                const float room = kMost + 126 - (float)(__float_as_uint(most_l) >> 23);  // so that l stays below 2^kMost
+                                const float now = m[nt][i] - fmaxf(fminf(kRaise - log2f(highest), room), 0.0f) / unit[nt][i];
+                                grow[i] = power2((m[nt][i] - now) * unit[nt][i]);
+                                m[nt][i] = now;
+                                limit[nt][i] = now + fminf(kLag / unit[nt][i], 1e30f);
+                                l[nt][i] *= grow[i];
+                            }
+                        }
+#pragma unroll
+                        for (int k = 0; k < kSteps; k++)
+#pragma unroll
+                            for (int i = 0; i < 4; i++) o[k][nt][i] *= grow[i & 1];
                     }
                 }
             }
@@ -908,7 +1051,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
         }
         const int parts = last_worker - first_worker + 1;
         const int64_t head0 = (int64_t)at.b * p.n_heads + kv * group + col0;
-        const float vscale = kNarrow ? p.pool.v_scale[kv] : kFollow ? 1.0f : kLowered;
+        const float vscale = kNarrow ? p.pool.v_scale[kv] : kHalf ? 1.0f : kLowered;
         constexpr int kPartSize = kCols * (DP + 2);
         // a worker leaves at most two parts: of a group that began before it (0), and of one that goes on behind it (1)
         float* const my_part = p.parts + (2 * (int64_t)worker + (first_worker == worker ? 1 : 0)) * kPartSize;

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from kv_common import DT, TINY, UNIT, assert_attend, ref_attend
+from kv_common import DT, TINY, UNIT, assert_attend, make_table, ref_attend
 from paper_2604_11001_b200 import kvcache as kv
 from paper_2604_11001_b200.binding import FcsimError
 
@@ -79,6 +79,42 @@ def test_one_token_far_above_the_rest(dtype, cache, gap, requests, n, at):
     v[:, at] = 0
     c, q, table, lengths = one_hot(x, v, dtype, cache, 4)
     attend_within(c, q, table, lengths, 2.0 ** -14 + 2.0 ** -21 * (gap + 16), scale=1.0)
+
+
+@pytest.mark.parametrize("gap", [6, 12, 18, 30])
+@pytest.mark.parametrize("requests,n,at", [(1, 40, 0), (1, 5000, 0), (1, 5000, 2500), (2, 700, 699), (300, 40, 7)])
+def test_one_token_far_above_the_rest_in_bf16(gap, requests, n, at):
+    """The same where the output has bf16's range: the others' weights are exact to 2^-18 whatever their size."""
+    g = gen(gap + n)
+    H, D = 2, 64
+    x = 0.25 * torch.randn(requests, n, H, generator=g, device="cuda")
+    x[:, at] = gap
+    v = 0.5 + torch.rand(requests, n, H, D, generator=g, device="cuda")
+    v[:, at] = 0
+    c, q, table, lengths = one_hot(x, v, "bf16", "e4m3", 4)
+    attend_within(c, q, table, lengths, 2.0 ** -17 + 2.0 ** -21 * (gap + 16), scale=1.0)
+
+
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3"), ("bf16", "bf16")])
+@pytest.mark.parametrize("D", [96, 128, 256])
+@pytest.mark.parametrize("longest", [20, 1500])
+def test_logits_that_spread_over_many_powers_of_e(dtype, cache, D, longest):
+    """Random rows with scale 1: weights from one down to e^-80, and elements of v that are zero beside the largest."""
+    g = gen(D + longest)
+    H, requests = 4, 30
+    lengths = torch.randint(0, longest + 1, (requests,), generator=g, device="cuda").tolist()
+    pages = sum(-(-n // PAGE) for n in lengths) + 2
+    shape = (pages, PAGE, H, D)
+    scales = [0.5 + torch.rand(H, generator=g, device="cuda") if cache == "e4m3" else None for _ in range(2)]
+    c = kv.PagedKV(stored(torch.randn(shape, generator=g, device="cuda"), cache),
+                   stored(torch.randn(shape, generator=g, device="cuda").mul(torch.rand(shape, generator=g, device="cuda") > 0.3), cache),
+                   torch.rand(pages, H, PAGE, generator=g, device="cuda"), *scales)
+    table, _ = make_table(g, lengths, PAGE, pages)
+    q = torch.randn(requests, 2 * H, D, generator=g, device="cuda").to(DT[dtype])
+    before = c.weight.clone()
+    out, lse = c.attend(q, table, to_int(lengths), add_weight=True, return_lse=True, scale=1.0)
+    c.check()
+    assert_attend(c, q, table, lengths, out, lse, before, scale=1.0)
 
 
 @pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3")])
