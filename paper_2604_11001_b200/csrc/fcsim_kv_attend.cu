@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     constexpr float kLog2e = 1.4426950408889634f;
     // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
     constexpr bool kHalf = std::is_same<M, F16>::value, kFollow = kHalf && !kNarrow;
-    constexpr float kRaise = kRaiseOf<M>, kLag = kHalf ? 1.9f : 8, kDeep = kRaise + 8, kMost = 76;
+    constexpr float kRaise = kRaiseOf<M>, kLag = kHalf ? 1.9f : 8, kDeep = kRaise + 8, kMost = kNarrow ? 36 : 76;
     constexpr float kStep = 1.0f / 256, kFiner = 274877906944.0f, kFew = 0.125f, kSlight = 1.0f / 32;  // 2^-8, 2^38, 2^-3, 2^-5: see the end of a tile
     constexpr int kPasses = 3;
     // bf16 weights meet v times 2^-24, so that 2^16 values at the type's end add up whatever their weights are.  (Values below
@@ -905,10 +905,11 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             }
             // Weights below kStep are few of f16's steps, too few where those above meet a v of nothing and the output is bf16.  So where
             // there are any and an element of the sums is still slight (below kSlight, of weights of 2^14 at the reference), what their
-            // rounding has lost follows in up to three passes, kFiner times as large in each and added up apart: 22 bits of weights of any
-            // size.  If a head has no others here, its reference moves down for the tiles to come.  (No 8-bit value is infinite, so a part may
-            // be zero or negative.  It stands behind the products so that nothing comes between these and the weights.  64 requests over
-            // e4m3: without any of it 81.3 us, with it 82.9; with logits four times as wide 86.9, without the test of the sums 124.)
+            // rounding has lost follows in up to three passes, kFiner times as large in each and added up apart: 22 bits of weights down
+            // to 2^-100.  If a head has no others here, its reference moves down for the tiles to come (by 2^22 at most: it has to come back up
+            // in one factor).  (No 8-bit value is infinite, so a part may be zero or negative.  It stands behind the products so that nothing
+            // comes between these and the weights.  64 requests over e4m3: without any of it 81.3 us, with it 82.9; with logits four times as
+            // wide 86.9, without the test of the sums 124.)
             if constexpr (kNarrow) {
                 bool lost = __any_sync(~0u, least < __float_as_uint(kStep) - 1);
                 if (lost) {

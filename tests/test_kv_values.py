@@ -84,7 +84,7 @@ def test_one_token_far_above_the_rest(dtype, cache, gap, requests, n, at):
 @pytest.mark.parametrize("gap", [6, 12, 18, 30])
 @pytest.mark.parametrize("requests,n,at", [(1, 40, 0), (1, 5000, 0), (1, 5000, 2500), (2, 700, 699), (300, 40, 7)])
 def test_one_token_far_above_the_rest_in_bf16(gap, requests, n, at):
-    """The same where the output has bf16's range: the others' weights are exact to 2^-18 whatever their size."""
+    """The same where the output has bf16's range: the others' weights are exact to 2^-18 down to 2^-100 of it."""
     g = gen(gap + n)
     H, D = 2, 64
     x = 0.25 * torch.randn(requests, n, H, generator=g, device="cuda")
@@ -115,6 +115,22 @@ def test_logits_that_spread_over_many_powers_of_e(dtype, cache, D, longest):
     out, lse = c.attend(q, table, to_int(lengths), add_weight=True, return_lse=True, scale=1.0)
     c.check()
     assert_attend(c, q, table, lengths, out, lse, before, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "e4m3"), ("bf16", "bf16")])
+@pytest.mark.parametrize("n", [40, 600, 4000])
+def test_a_weight_before_one_far_above_it(dtype, cache, n):
+    """A token at e^40, the only one whose value is not zero, many at e^0, where the reference follows them down, then one at e^88: the
+    output is e^-48 of the first one's value."""
+    g = gen(7)
+    H, D = 2, 64
+    x = 0.25 * torch.randn(20, n, H, generator=g, device="cuda")
+    v = torch.zeros(20, n, H, D, device="cuda")
+    x[:, 9], x[:, n - 5] = 40, 88
+    v[:, 9] = 0.5 + torch.rand(20, H, D, generator=g, device="cuda")
+    v[:, 9, :, ::2] = 0                                # (what is nothing yet makes the sums slight)
+    c, q, table, lengths = one_hot(x, v, dtype, cache, 4)
+    attend_within(c, q, table, lengths, 2.0 ** -16 + 2.0 ** -21 * 104, scale=1.0)
 
 
 @pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3")])
