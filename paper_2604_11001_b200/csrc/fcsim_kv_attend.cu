@@ -494,9 +494,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     constexpr int kParts = std::is_same<M, F16>::value ? 2 : 3;  // 11 bits each, or 8: of the softmax weights
     constexpr float kLog2e = 1.4426950408889634f;
     // a weight is 2^kRaise at the reference of the exponentials and 2^(kRaise + kLag) at most; see where the reference moves
-    constexpr bool kHalf = std::is_same<M, F16>::value, kFollow = kHalf && !kNarrow;
-    constexpr float kRaise = kRaiseOf<M>, kLag = kHalf ? 1.9f : 8, kDeep = kRaise + 8, kMost = kNarrow ? 36 : 76;
+    constexpr bool kHalf = std::is_same<M, F16>::value;
+    constexpr float kRaise = kRaiseOf<M>, kLag = kHalf ? 1.9f : 8, kMost = 36;
     constexpr float kStep = 1.0f / 256, kFiner = 274877906944.0f, kFew = 0.125f, kSlight = 1.0f / 32;  // 2^-8, 2^38, 2^-3, 2^-5: see the end of a tile
+    constexpr float kLargest = kNarrow ? 448 : 65504;
     constexpr int kPasses = 3;
     // bf16 weights meet v times 2^-24, so that 2^16 values at the type's end add up whatever their weights are.  (Values below
     // 2^-94 lose bits by it.)
@@ -791,50 +792,16 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     if (kSub == 2) most[i] = fmaxf(most[i], fmaxf(s[kSub - 1][nt][i], s[kSub - 1][nt][2 + i]));
                 }
                 // The reference moves only when a logit is 2^kLag above it: the weights stay far from f16's and fp32's ends, and
-                // the maximum over the lanes is taken a few times in a request instead of in every tile.  f16 has steps of
-                // 2^-24, so beside it the reference also moves down where all of a tile's tokens lie 2^-kDeep below it (one
-                // token may hold nearly all of the sum and have a v of nothing); the 32-bit sums grow by as much.  (For 8-bit rows
-                // see the end of the tile.)  A weight's rounding is then 2^-17 of its tile's largest at most, 2^-39 of it in that
-                // one token's own tile, which is below f16's own steps for values up to 2^10.  (100 requests in f16, attention alone,
-                // 41.1 -> 42.6 us; with a reach of 2^8 up, 42.2, and 2^-32 in its own tile.)
-                bool moves;
-                if constexpr (kFollow) {
-                    bool low[2];
-                    moves = false;
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const float above = (most[i] - limit[nt][i]) * unit[nt][i];
-                        moves |= above > 0.0f;
-                        low[i] = above < -(kLag + kDeep);
-                    }
-                    if (__any_sync(~0u, moves || low[0] || low[1])) {
-                        moves = __any_sync(~0u, moves);
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {  // all of a head's eight lanes
-                            uint32_t all = __ballot_sync(~0u, low[i]);
-                            all &= all >> 16, all &= all >> 8, all &= all >> 4;
-                            moves |= (all & 15) != 0;
-                        }
-                    }
-                } else
-                    moves = __any_sync(~0u, most[0] > limit[nt][0] || most[1] > limit[nt][1]);
-                if (moves) {
+                // the maximum over the lanes is taken a few times in a request instead of in every tile.
+                if (__any_sync(~0u, most[0] > limit[nt][0] || most[1] > limit[nt][1])) {
                     float shrink[2];
 #pragma unroll
                     for (int i = 0; i < 2; i++) {
-                        float top = most[i], most_l = l[nt][i];
+                        float top = most[i];
 #pragma unroll
-                        for (int d = 4; d < 32; d *= 2) {
-                            top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-                            if constexpr (kFollow) most_l = fmaxf(most_l, __shfl_xor_sync(~0u, most_l, d));
-                        }
+                        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
                         const bool first_one = limit[nt][i] == -INFINITY;
-                        float now = first_one ? top : fmaxf(top, m[nt][i]);
-                        if constexpr (kFollow) {
-                            const float under = (m[nt][i] - top) * unit[nt][i];
-                            const float room = kMost + 126 - (float)(__float_as_uint(most_l) >> 23);  // so that l stays below 2^kMost
-                            if (!first_one && under > kDeep && top > -INFINITY) now = m[nt][i] - fmaxf(fminf(under, room), 0.0f) / unit[nt][i];
-                        }
+                        const float now = first_one ? top : fmaxf(top, m[nt][i]);
                         const float base = now == -INFINITY ? 0.0f : now;
                         shrink[i] = first_one ? 0.0f : power2((m[nt][i] - base) * unit[nt][i]);
                         m[nt][i] = base;
@@ -852,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     for (int i = 0; i < 4; i++) {
                         s[b][nt][i] = power2(fmaf(s[b][nt][i] - m[nt][i & 1], unit[nt][i & 1], kRaise));
                         l[nt][i & 1] += s[b][nt][i];
-                        if constexpr (kNarrow) least = __viaddmin_u32(__float_as_uint(s[b][nt][i]), ~0u, least);
+                        if constexpr (kHalf) least = __viaddmin_u32(__float_as_uint(s[b][nt][i]), ~0u, least);
                         if constexpr (!kHalf) s[b][nt][i] *= 1 / kLowered;
                     }
 #pragma unroll
@@ -903,14 +870,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     }
                 }
             }
-            // Weights below kStep are few of f16's steps, too few where those above meet a v of nothing and the output is bf16.  So where
-            // there are any and an element of the sums is still slight (below kSlight, of weights of 2^14 at the reference), what their
-            // rounding has lost follows in up to three passes, kFiner times as large in each and added up apart: 22 bits of weights down
-            // to 2^-100.  If a head has no others here, its reference moves down for the tiles to come (by 2^22 at most: it has to come back up
-            // in one factor).  (No 8-bit value is infinite, so a part may be zero or negative.  It stands behind the products so that nothing
-            // comes between these and the weights.  64 requests over e4m3: without any of it 81.3 us, with it 82.9; with logits four times as
-            // wide 86.9, without the test of the sums 124.)
-            if constexpr (kNarrow) {
+            // Weights below kStep are few of f16's steps, too few where those above meet a v of nothing.  So where there are any and an
+            // element of the sums is still slight (below kSlight of the tile's largest v, of weights of 2^14 at the reference), what their
+            // rounding has lost follows in up to three passes, kFiner times as large in each and added up apart: 22 bits of weights down to
+            // 2^-100.  If a head has no others here, its reference moves down for the tiles to come (by 2^22 at most: it has to come back
+            // up in one factor).  The parts may be zero or negative, so a tile with a v that is infinite or NaN goes without.  It stands
+            // behind the products so that nothing comes between these and the weights.  (Attention alone: 64 requests over e4m3, without
+            // any of it 81.3 us, with it 82.8, with logits four times as wide 91, and without the test of the sums 124; 100 requests in f16
+            // 41.1, 41.8, and 46.)
+            if constexpr (kHalf) {
                 bool lost = __any_sync(~0u, least < __float_as_uint(kStep) - 1);
                 if (lost) {
                     float slight = INFINITY;
@@ -922,7 +890,26 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
                                 for (int i = 0; i < 4; i++) slight = fminf(slight, fabsf(o[k][nt][i]));
                         }
-                    lost = __any_sync(~0u, slight < kSlight);
+                    lost = __any_sync(~0u, slight < kSlight * kLargest);
+                    if (lost) {  // beside the tile's own largest v
+                        uint32_t large = 0;
+                        const char* const rows = smem + warp * 2 * kTokens * S::kPitch + stage * S::kStage + kTokens * S::kPitch;
+#pragma unroll 4
+                        for (int t = lane_row; t < kTokens; t += kRows) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(rows + t * S::kPitch + chunk * 16);
+                            const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                if constexpr (kNarrow) large = __vmaxu2(large, __vmaxu2(word[i] << 8 & 0x7f007f00u, word[i] & 0x7f007f00u));
+                                else large = __vmaxu2(large, word[i] & 0x7fff7fffu);
+                            }
+                        }
+                        large = __reduce_max_sync(~0u, max(large & 0xffff, large >> 16));
+                        float most_v;
+                        if constexpr (kNarrow) most_v = M::unpack(E4M3::halves(large >> 8)).x;
+                        else most_v = M::unpack(large).x;
+                        lost = __any_sync(~0u, slight <= kSlight * most_v) && most_v < INFINITY;  // (NaN: not)
+                    }
                 }
                 if (lost) {
                     float w[kSub][NT][4] = {};
@@ -985,7 +972,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
 #pragma unroll
                             for (int b = 0; b < kSub; b++) {
                                 uint32_t a[4][4];
-                                load_narrow_transposed(vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16 + k0 * 16, a);
+                                if constexpr (kNarrow)
+                                    load_narrow_transposed(vrow + (b * 16 + (lane & 7) + (which & 1) * 8) * S::kPitch + (which >> 1) * 16 + k0 * 16, a);
+                                else {
+#pragma unroll
+                                    for (int k = 0; k < 4; k++)
+                                        load_matrices_transposed(vrow + (b * 16 + (lane & 7) + (which >> 1) * 8) * S::kPitch + (which & 1) * 16 + (k0 + k) * 32, a[k]);
+                                }
 #pragma unroll
                                 for (int k = 0; k < 4; k++)
 #pragma unroll

@@ -133,6 +133,40 @@ def test_a_weight_before_one_far_above_it(dtype, cache, n):
     attend_within(c, q, table, lengths, 2.0 ** -16 + 2.0 ** -21 * 104, scale=1.0)
 
 
+@pytest.mark.parametrize("gap", [6, 12, 18, 22])
+@pytest.mark.parametrize("n,at", [(12, 3), (40, 0), (900, 450)])
+def test_large_f16_values_below_one_token_far_above(gap, n, at):
+    """f16 rows of values about 30 000: what the others add up to is well within the output's range, in that token's own tile too."""
+    g = gen(gap + n)
+    H, D = 2, 64
+    x = 0.25 * torch.randn(8, n, H, generator=g, device="cuda")
+    x[:, at] = gap
+    v = 20000 * (1 + torch.rand(8, n, H, D, generator=g, device="cuda"))
+    v[:, at] = 0
+    c, q, table, lengths = one_hot(x, v, "f16", "f16", 4)
+    attend_within(c, q, table, lengths, 2.0 ** -17 + 2.0 ** -21 * (gap + 16), scale=1.0)
+
+
+def test_an_infinite_f16_value_among_small_weights():
+    """The passes for small weights leave out a tile that has one, or a NaN: it stays in its element, the rest is as exact as without them."""
+    H, D, n = 1, 64, 40
+    x = torch.zeros(3, n, H, device="cuda")
+    x[:, 5] = 12
+    v = torch.ones(3, n, H, D, device="cuda")
+    v[:, 5] = 0
+    v[1, 9, 0, 7] = float("inf")
+    v[2, 9, 0, 7] = float("nan")
+    c, q, table, lengths = one_hot(x, v, "f16", "f16")
+    out = c.attend(q, table, to_int(lengths), scale=1.0)
+    want = 39 * math.exp(-12) / (1 + 39 * math.exp(-12))
+    assert float(out[1, 0, 7]) == math.inf and bool(torch.isnan(out[2, 0, 7]))
+    rest = [i for i in range(64) if i != 7]
+    for r in range(3):
+        # (without the passes: 2^-25 of a weight that is 2^-17.3 of 2^14, on 15 of 39)
+        assert bool(((out[r, 0, rest].double() - want).abs() <= 2.0 ** -11 * want + 2.0 ** -21 * want * 29).all())
+    assert bool(((out[0, 0].double() - want).abs() <= 2.0 ** -11 * want + 2.0 ** -21 * want * 29).all())
+
+
 @pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("f16", "e4m3"), ("bf16", "e4m3")])
 @pytest.mark.parametrize("requests", [3, 400])
 def test_weights_meet_values_unrounded(dtype, cache, requests):
