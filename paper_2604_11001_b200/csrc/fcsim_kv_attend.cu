@@ -884,12 +884,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                     float slight = INFINITY;
 #pragma unroll
                     for (int k = 0; k < kSteps; k++)
-                        if (k * 16 < D) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++)
+                        for (int i = 0; i < 4; i++)
+                            if (k * 16 + (kNarrow ? 0 : 8 * (i >> 1)) < D) {  // (head_dim is a multiple of 16, or of 8)
 #pragma unroll
-                                for (int i = 0; i < 4; i++) slight = fminf(slight, fabsf(o[k][nt][i]));
-                        }
+                                for (int nt = 0; nt < NT; nt++) slight = fminf(slight, fabsf(o[k][nt][i]));
+                            }
                     lost = __any_sync(~0u, slight < kSlight * kLargest);
                     if (lost) {  // beside the tile's own largest v
                         uint32_t large = 0;
