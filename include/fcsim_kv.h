@@ -1,7 +1,7 @@
 /*
- * fcsim_kv -- the paged key-value cache of one layer on the device: append, attend, evict.
+ * fcsim_kv -- the paged key-value cache of one layer on the device: append, attend, evict, read.
  *
- * The simulator (fcsim.h) counts tokens of KV cache per slot; these three operators are what a slot does to a real
+ * The simulator (fcsim.h) counts tokens of KV cache per slot; these operators are what a slot does to a real
  * cache.  A cache is a pool of n_pages pages of page_size tokens; a request owns pages through a row of a table
  * (entry i holds tokens i * page_size ..).  Token rows are [n_kv_heads][head_dim].
  *
@@ -11,6 +11,7 @@
  *            share its kv head).
  *   evict    per request and kv head: the oldest `first`, the newest `recent` and, of the rest, the largest
  *            weights are kept up to a budget; the kept rows move in order, with their weights, to other pages.
+ *   read     the values that stand at given slots, as 16-bit rows: what append has stored, for another cache or for the eye.
  *
  * (The paper of fcsim.h has no counterpart: it counts tokens and evicts whole requests.)
  *
@@ -88,7 +89,7 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
 
 /* table: [n_requests] rows of table_cols int32, row r at table + r * table_row; only the entries that a request's
  *   length reaches are read.  lengths: [n_requests] int32 tokens held, 0 .. max_length <= table_cols * page_size.
- * window > 0: only the newest `window` tokens are seen.  n_heads: a multiple of n_kv_heads; head h reads kv head
+ * window > 0: only the newest `window` tokens are seen, and the oldest `first` (without a window `first` has no effect).  n_heads: a multiple of n_kv_heads; head h reads kv head
  *   h / (n_heads / n_kv_heads).  q: request r at q + r * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.  (Of a BF16
  *   query over E4M3, elements below 2^-31 of the head's largest finite one are rounded to 2^-38 of it.)
  * out: [n_requests][n_heads][head_dim] contiguous, in q's type.  lse: [n_requests][n_heads] fp32, the natural
@@ -110,6 +111,7 @@ typedef struct {
     int64_t q_row, q_head, table_row;
     int32_t n_requests, n_heads, dtype, table_cols, max_length, window, add_weight;
     float scale;
+    int32_t first, reserved;
 } fcsim_kv_attend_args;
 
 typedef struct {
@@ -145,6 +147,18 @@ typedef struct {
 int fcsim_kv_evict_workspace(const fcsim_kv_cache* cache, const fcsim_kv_evict_args* args, fcsim_kv_workspace* out);
 int fcsim_kv_evict(const fcsim_kv_cache* cache, const fcsim_kv_evict_args* args, void* workspace,
                    size_t workspace_bytes, void* cuda_stream);
+
+/* k_out, v_out: [n_tokens][n_kv_heads][head_dim] contiguous in `dtype` (F16 or BF16, whatever the cache's type), 16-byte aligned.  Row i
+ * is what stands at slots[i] (int64, page * page_size + place), an E4M3 value times its scale, rounded once; negative: zeros.
+ * A slot outside the pool gives zeros (FCSIM_KV_BAD_PAGE).  A slot may come more than once.  n_tokens is at most 2^31 - 2^16. */
+typedef struct {
+    const int64_t* slots;
+    void *k_out, *v_out;
+    int32_t* status;
+    int32_t n_tokens, dtype;
+} fcsim_kv_read_args;
+
+int fcsim_kv_read(const fcsim_kv_cache* cache, const fcsim_kv_read_args* args, void* cuda_stream);
 
 /* cudaError_t behind the last FCSIM_ECUDA of these functions on the calling thread, else 0. */
 int fcsim_kv_last_cuda_error(void);

@@ -237,6 +237,105 @@ int launch_append(const AppendParams& p, cudaStream_t stream) {
     return launch_append_lanes<T, C, 32>(p, stream);
 }
 
+// ------------------------------------------------------------------------------------------------ read
+struct ReadParams {
+    Pool pool;
+    const int64_t* slots;
+    char *k_out, *v_out;
+    int32_t* status;
+    int64_t pieces;               // of all tokens: 16 cached bytes each, of k and of v
+    int token_pieces, row_pieces; // of a token; of a head
+    uint64_t token_magic, row_magic;
+};
+
+// x / d for x < 2^31, of magic = ceil(2^63 / d)
+__device__ __forceinline__ int divide_by(uint64_t magic, int x) {
+    return (int)__umul64hi(magic, (uint64_t)x << 1);
+}
+
+// 16 cached bytes as 8 or 16 elements of type T, times `scale` where the cache has scales
+template <class T, class C>
+__device__ __forceinline__ void convert_piece(const uint4& raw, float scale, char* out) {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    uint32_t y[8];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (C::bytes == 1) {
+            const float2 a = F16::unpack(E4M3::halves(w[i])), b = F16::unpack(E4M3::halves(w[i] >> 16));
+            y[2 * i] = T::pack(a.x * scale, a.y * scale), y[2 * i + 1] = T::pack(b.x * scale, b.y * scale);
+        } else if constexpr (std::is_same<T, C>::value) {
+            y[i] = w[i];
+        } else {
+            const float2 a = C::unpack(w[i]);
+            y[i] = T::pack(a.x, a.y);
+        }
+    }
+    __stcs(reinterpret_cast<uint4*>(out), make_uint4(y[0], y[1], y[2], y[3]));
+    if constexpr (C::bytes == 1) __stcs(reinterpret_cast<uint4*>(out) + 1, make_uint4(y[4], y[5], y[6], y[7]));
+}
+
+// The tokens' rows are cut into pieces of 16 cached bytes, end to end over all tokens, and a thread takes PIECES of them, 256 apart:
+// neighbouring lanes read and write neighbouring bytes whatever the width of a head, and the slots and then the rows of all
+// are asked for before any is used.  Bound by memory when there are many tokens, by two dependent loads when few.
+template <class T, class C, int PIECES>
+__global__ void __launch_bounds__(256) fcsim_kv_read_kernel(const ReadParams p) {
+    const int64_t base = (int64_t)blockIdx.x * (PIECES * 256);
+    const int64_t token0 = base / p.token_pieces;  // the same for the CTA
+    const int offset = (int)(base - token0 * p.token_pieces) + threadIdx.x;
+    int64_t slot[PIECES], to[PIECES];
+    int h[PIECES], piece[PIECES];
+    bool mine[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        const int x = offset + i * 256, ahead = divide_by(p.token_magic, x), rest = x - ahead * p.token_pieces;
+        mine[i] = base + threadIdx.x + i * 256 < p.pieces;
+        to[i] = base + threadIdx.x + i * 256;
+        h[i] = divide_by(p.row_magic, rest);
+        piece[i] = rest - h[i] * p.row_pieces;
+        slot[i] = mine[i] ? p.slots[token0 + ahead] : -1;
+    }
+    uint4 k[PIECES], v[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        k[i] = v[i] = make_uint4(0, 0, 0, 0);
+        if (slot[i] >= (int64_t)p.pool.n_pages * p.pool.page_size) {
+            if (h[i] == 0 && piece[i] == 0) flag(p.status, FCSIM_KV_BAD_PAGE);
+        } else if (slot[i] >= 0) {
+            const int page = page_of(p.pool, (int)slot[i]), place = (int)slot[i] - page * p.pool.page_size;
+            const int64_t at = (page * p.pool.stride_page + place * p.pool.stride_slot + h[i] * p.pool.stride_head) * C::bytes + piece[i] * 16;
+            k[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.k + at));
+            v[i] = __ldcs(reinterpret_cast<const uint4*>(p.pool.v + at));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; i++)
+        if (mine[i]) {
+            const bool none = slot[i] < 0 || slot[i] >= (int64_t)p.pool.n_pages * p.pool.page_size;  // zeros, whatever the scale is
+            const float ks = C::bytes == 1 && !none ? p.pool.k_scale[h[i]] : 1.0f, vs = C::bytes == 1 && !none ? p.pool.v_scale[h[i]] : 1.0f;
+            const int64_t at = to[i] * (16 / C::bytes * 2);
+            convert_piece<T, C>(k[i], ks, p.k_out + at);
+            convert_piece<T, C>(v[i], vs, p.v_out + at);
+        }
+}
+
+template <class T, class C, int PIECES>
+int launch_read_as(const ReadParams& p, cudaStream_t stream) {
+    const int64_t blocks = (p.pieces + PIECES * 256 - 1) / (PIECES * 256);
+    if (blocks > 0x7fffffff) return FCSIM_EINVAL;
+    fcsim_kv_read_kernel<T, C, PIECES><<<(unsigned)blocks, 256, 0, stream>>>(p);
+    return launched();
+}
+template <class T, class C>
+int launch_read(const ReadParams& p, cudaStream_t stream) {
+    if (p.pieces < 1 << 18) return launch_read_as<T, C, 1>(p, stream);
+    return launch_read_as<T, C, 4>(p, stream);
+}
+template <class T>
+int launch_read_from(int cache_type, const ReadParams& p, cudaStream_t stream) {
+    if (cache_type == FCSIM_KV_E4M3) return launch_read<T, E4M3>(p, stream);
+    return cache_type == FCSIM_KV_F16 ? launch_read<T, F16>(p, stream) : launch_read<T, BF16>(p, stream);
+}
+
 // ------------------------------------------------------------------------------------------------ evict
 struct EvictParams {
     Pool pool;
@@ -593,7 +692,7 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     if (a->n_requests < 0 || a->n_requests > 65535 || a->n_heads < 1 || a->n_heads % c->n_kv_heads) return FCSIM_EINVAL;
     if (a->table_cols < 0 || a->max_length < 0 || a->max_length > (int64_t)a->table_cols * c->page_size) return FCSIM_EINVAL;
     if (a->max_length > kMaxTokens || (int64_t)a->n_heads * c->head_dim > 0x7fffffff) return FCSIM_EINVAL;
-    if (a->window < 0 || a->table_row < 0 || !isfinite(a->scale)) return FCSIM_EINVAL;
+    if (a->window < 0 || a->first < 0 || a->table_row < 0 || !isfinite(a->scale)) return FCSIM_EINVAL;
     if (!good_stride(a->q_row, 2) || !good_stride(a->q_head, 2)) return FCSIM_EINVAL;
     if (a->n_requests > 0) {
         if (!a->q || !a->out || !a->lengths || !aligned16(a->q) || !aligned16(a->out)) return FCSIM_ESIZE;
@@ -602,7 +701,9 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     }
     p->q = (const char*)a->q, p->out = (char*)a->out, p->lse = a->lse, p->table = a->table, p->lengths = a->lengths;
     p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
-    p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length, p->window = a->window;
+    p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length;
+    const bool all = (int64_t)a->window + a->first >= a->max_length || a->window == 0;  // (of the longest request, and so of all)
+    p->window = all ? 0 : a->window, p->first = all ? 0 : a->first;
     p->add_weight = a->add_weight != 0, p->scale = a->scale;
     return FCSIM_OK;
 }
@@ -638,7 +739,7 @@ struct AttendLayout {
 // requests that share no page hold at most the pool's tokens, and each at most one tile that is not full
 int64_t logit_tiles(const AttendParams& p) {
     if (!p.add_weight) return 0;
-    const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
+    const int64_t seen = p.window > 0 ? p.window + p.first : p.max_length;
     const int64_t tile = 1 << p.tile_bits;
     return std::min((seen + tile - 1) / tile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / tile + p.n_requests);
 }
@@ -651,7 +752,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     int device = 0, sms = 0, per_sm = 0, rc = device_and_sms(&device, &sms);
     if (rc != FCSIM_OK) return rc;
     if ((rc = v.ctas_per_sm(device, &per_sm)) != 0) return cuda_status((cudaError_t)rc);
-    const int64_t seen = p.window > 0 ? std::min(p.window, p.max_length) : p.max_length;
+    const int64_t seen = p.window > 0 ? p.window + p.first : p.max_length;
     const int64_t tiles = (seen + (1 << p.tile_bits) - 1) >> p.tile_bits, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
     l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most + most / 3 + 1, p.n_requests)}));
@@ -800,6 +901,23 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     if (chunks <= 8) return launch_move<8>(p, a->n_requests, stream);
     if (chunks <= 16) return launch_move<16>(p, a->n_requests, stream);
     return launch_move<32>(p, a->n_requests, stream);
+}
+
+extern "C" int fcsim_kv_read(const fcsim_kv_cache* c, const fcsim_kv_read_args* a, void* cuda_stream) {
+    ReadParams p;
+    int rc = check_cache(c, &p.pool);
+    if (rc != FCSIM_OK) return rc;
+    if (!a || (a->dtype != FCSIM_KV_F16 && a->dtype != FCSIM_KV_BF16) || a->n_tokens < 0 || a->n_tokens > kMaxTokens) return FCSIM_EINVAL;
+    p.row_pieces = c->head_dim * cache_bytes(c) / 16;
+    p.token_pieces = p.row_pieces * c->n_kv_heads;
+    p.pieces = (int64_t)p.token_pieces * a->n_tokens;
+    if (a->n_tokens == 0) return FCSIM_OK;
+    if (!a->slots || !a->k_out || !a->v_out || !aligned16(a->k_out) || !aligned16(a->v_out)) return FCSIM_ESIZE;
+    p.slots = a->slots, p.k_out = (char*)a->k_out, p.v_out = (char*)a->v_out, p.status = a->status;
+    p.token_magic = ((1ull << 63) + p.token_pieces - 1) / p.token_pieces;
+    p.row_magic = ((1ull << 63) + p.row_pieces - 1) / p.row_pieces;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    return a->dtype == FCSIM_KV_F16 ? launch_read_from<F16>(c->dtype, p, stream) : launch_read_from<BF16>(c->dtype, p, stream);
 }
 
 extern "C" int fcsim_kv_last_cuda_error(void) { return g_last_cuda_error; }

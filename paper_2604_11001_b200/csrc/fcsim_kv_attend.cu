@@ -135,7 +135,7 @@ constexpr int kWholeAmongLonger = 8;
 
 // A place in the work: request b, its group (kv head, head tile), tile j of `tiles`.
 struct Place {
-    int b, kv, ht, j, tiles, start, len;
+    int b, kv, ht, j, tiles, gap, seen;
     int left;              // units from this tile to the end of the worker's stretch; none: the place is beyond it
     int tiles_before;      // tiles (of a CTA) of the requests before b
 };
@@ -144,11 +144,14 @@ __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
     const int n = p.lengths[b];
     return n < 0 ? 0 : n > p.max_length ? p.max_length : n;
 }
-__device__ __forceinline__ int start_of(const AttendParams& p, int len) {
-    return p.window > 0 && len > p.window ? len - p.window : 0;
+// Tokens between the first ones and the window, which are not seen.  What is seen is counted without them: seen token u is token
+// u, or behind the first ones u + gap.
+__device__ __forceinline__ int gap_of(const AttendParams& p, int len) {
+    return p.window > 0 && len > p.window + p.first ? len - p.window - p.first : 0;
 }
+__device__ __forceinline__ int token_of(const AttendParams& p, int gap, int u) { return u + (u >= p.first ? gap : 0); }
 __device__ __forceinline__ int tiles_of(const AttendParams& p, int len, int bits) {
-    return (len - start_of(p, len) + (1 << bits) - 1) >> bits;
+    return (len - gap_of(p, len) + (1 << bits) - 1) >> bits;
 }
 
 // The division of the units [0, total) among the workers (CTAs or warps): worker i has [i * share, (i + 1) * share).  It
@@ -168,9 +171,10 @@ struct Division {
 
 __device__ __forceinline__ void enter(const AttendParams& p, const Division& d, Place& w, int b) {
     w.b = b;
-    w.len = length_of(p, b);
-    w.start = start_of(p, w.len);
-    w.tiles = tiles_of(p, w.len, d.bits);
+    const int len = length_of(p, b);
+    w.gap = gap_of(p, len);
+    w.seen = len - w.gap;
+    w.tiles = (w.seen + (1 << d.bits) - 1) >> d.bits;
 }
 // The next group of the work; the caller knows that there is one (the lengths stay as they are during a call; if they do not,
 // the results are wrong, but nothing beyond the last request is read).
@@ -180,7 +184,7 @@ __device__ __forceinline__ void next_group(const AttendParams& p, const Division
     w.ht = 0;
     if (++w.kv < n_kv) return;
     w.kv = 0;
-    w.tiles_before += tiles_of(p, w.len, p.tile_bits);
+    w.tiles_before += (w.seen + (1 << p.tile_bits) - 1) >> p.tile_bits;
     do {
         if (w.b + 1 >= p.n_requests) {
             w.left = 0;
@@ -548,9 +552,9 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int t = in.start + in.j * step + offset + lane % kTokens, i = page_of(p.pool, t);
+        const int u = in.j * step + offset + lane % kTokens, t = token_of(p, in.gap, u), i = page_of(p.pool, t);
         place = t - i * p.pool.page_size;
-        page = t < in.len ? p.table[in.b * p.table_row + i] : -1;
+        page = u < in.seen ? p.table[in.b * p.table_row + i] : -1;
     };
     auto fetch_queries = [&]() {  // of a group that begins soon, into L2
         const int first = in.ht * kCols, lines = (D + 63) / 64, n = min(kCols, group - first) * lines;
@@ -564,13 +568,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             const bool good = (unsigned)page < (unsigned)p.pool.n_pages;
             const uint32_t mask = __ballot_sync(~0u, good) & kAll;
             if (lane == 0) masks[stage] = mask;  // for the computation of this tile
-            if (mask != kAll && !good && in.start + in.j * step + offset + lane % kTokens < in.len) flag(p.status, FCSIM_KV_BAD_PAGE);
+            if (mask != kAll && !good && in.j * step + offset + lane % kTokens < in.seen) flag(p.status, FCSIM_KV_BAD_PAGE);
             const int64_t head = in.kv * p.pool.stride_head;
 #pragma unroll
             for (int b = 0; b < kSub; b++) {
                 const uint32_t dst = lane_dst + stage * S::kStage + b * 16 * S::kPitch, half = mask >> (16 * b) & 0xffff;
                 const int page0 = __shfl_sync(~0u, page, 16 * b), place0 = __shfl_sync(~0u, place, 16 * b);
-                if (half == 0xffff && place0 + 16 <= p.pool.page_size) {  // 16 tokens of one page: rows at equal distances
+                const int before = p.first - (in.j * step + offset + 16 * b);  // first tokens among the 16
+                const bool split = before > 0 && before < 16 && in.gap > 0;
+                if (half == 0xffff && place0 + 16 <= p.pool.page_size && !split) {  // 16 tokens of one page: rows at equal distances
                     const char* src = p.pool.k + (page0 * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
                     if (copies) {
 #pragma unroll
@@ -642,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
             col0 = at.ht * kCols;
             cols = min(kCols, group - col0);
             logits = nullptr;
-            const int cta_tiles = tiles_of(p, at.len, S::kTileBits);
+            const int cta_tiles = (at.seen + S::kTile - 1) >> S::kTileBits;
             logit_row = (int64_t)cta_tiles * S::kTile;
             if (p.add_weight && at.tiles_before + cta_tiles <= p.logit_tiles)
                 logits = p.logits + (int64_t)at.tiles_before * S::kTile * p.n_heads + (kv * group + col0 + 2 * (lane & 3)) * logit_row + offset + lane / 4;
@@ -1294,23 +1300,23 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     locate(p, n_kv, 1, work, before, at, cut, cuts);
     for (int i = 0; i < mine && at.left > 0; i++) advance(p, work, at, n_kv, 1);
 
-    int in, t;
+    int in;
     bool aligned, room;
     float* weight[4];  // of each token, or none; one page and 16 aligned bytes where the size of a page allows
     float old[4];
     auto load_weights = [&]() {
         in = (at.j << p.tile_bits) + threadIdx.x % threads * 4;
-        t = at.start + in;
-        aligned = size % 4 == 0 && t % 4 == 0;
+        const int t0 = token_of(p, at.gap, in);
+        aligned = size % 4 == 0 && t0 % 4 == 0 && token_of(p, at.gap, in + 3) == t0 + 3;
         room = at.tiles_before + at.tiles <= p.logit_tiles;
         if (!room) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
         const int32_t* const table = p.table + at.b * p.table_row;
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             weight[i] = nullptr;
-            if (room && t + i < at.len && (i == 0 || !aligned)) {
-                const int index = page_of(p.pool, t + i), page = table[index];
-                if ((unsigned)page < (unsigned)p.pool.n_pages) weight[i] = p.pool.weight + ((int64_t)page * n_kv + at.kv) * size + t + i - index * size;
+            if (room && in + i < at.seen && (i == 0 || !aligned)) {
+                const int t = token_of(p, at.gap, in + i), index = page_of(p.pool, t), page = table[index];
+                if ((unsigned)page < (unsigned)p.pool.n_pages) weight[i] = p.pool.weight + ((int64_t)page * n_kv + at.kv) * size + t - index * size;
             }
         }
         if (aligned) {
@@ -1324,7 +1330,7 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     if (at.left > 0) load_weights();
     cudaGridDependencySynchronize();  // (by every CTA: the grid must not end before the first one)
     while (at.left > 0) {
-        if (room && t < at.len) {
+        if (room && in < at.seen) {
             float sum[4] = {0, 0, 0, 0};
             const int64_t step = (int64_t)at.tiles << p.tile_bits;
             const float* logit = p.logits + ((int64_t)at.tiles_before * p.n_heads << p.tile_bits) + at.kv * group * step + in;
@@ -1343,12 +1349,12 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
                         sum[3] += power2((s[i].w - x[i].x) * x[i].y) * x[i].z;
                     }
             }
-            if (aligned && t + 3 < at.len) {
+            if (aligned && in + 3 < at.seen) {
                 if (weight[0]) *reinterpret_cast<float4*>(weight[0]) = make_float4(old[0] + sum[0], old[1] + sum[1], old[2] + sum[2], old[3] + sum[3]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    float* const w = aligned ? (weight[0] && t + i < at.len ? weight[0] + i : nullptr) : weight[i];
+                    float* const w = aligned ? (weight[0] && in + i < at.seen ? weight[0] + i : nullptr) : weight[i];
                     if (w) *w = old[i] + sum[i];
                 }
             }

@@ -17,7 +17,8 @@ struct AttendParams {
     const int32_t *table, *lengths;
     int32_t* status;
     int64_t q_row, q_head, table_row;
-    int n_requests, n_heads, max_length, window, add_weight;
+    int n_requests, n_heads, max_length, add_weight;
+    int window, first;   // both 0 where everything is seen; their sum is below max_length
     float scale;
     int tile_bits;       // tokens a CTA takes at once, of the variant
     // workspace

@@ -1,4 +1,4 @@
-"""ctypes binding of the paged key-value cache (include/fcsim_kv.h): append, attend, evict.
+"""ctypes binding of the paged key-value cache (include/fcsim_kv.h): append, attend, evict, read.
 
 Argument checks and marshalling only -- the work is done by the CUDA library, on the current stream of the cache's
 device.  PyTorch provides device memory and streams; there is no CPU fallback.
@@ -7,6 +7,7 @@ device.  PyTorch provides device memory and streams; there is no CPU fallback.
     q = cache.append(q, k, v, positions, slots, rope=table, q_norm=w_q, k_norm=w_k)   # a slot's new tokens
     out = cache.attend(q, table, lengths, add_weight=True)                            # one query per request
     new_lengths, kept = cache.evict(table, lengths, budget, new_table, max_budget=512, recent=64, first=4)
+    k, v = cache.read(slots)                                                          # what stands there
     cache.check()                                                                     # synchronises
 """
 from __future__ import annotations
@@ -57,7 +58,7 @@ class fcsim_kv_attend_args(C.Structure):
                 + [(n, C.c_int64) for n in ("q_row", "q_head", "table_row")]
                 + [(n, C.c_int32) for n in ("n_requests", "n_heads", "dtype", "table_cols", "max_length", "window",
                                             "add_weight")]
-                + [("scale", C.c_float)])
+                + [("scale", C.c_float), ("first", C.c_int32), ("reserved", C.c_int32)])
 
 
 class fcsim_kv_evict_args(C.Structure):
@@ -68,17 +69,23 @@ class fcsim_kv_evict_args(C.Structure):
                                             "recent", "first", "reserved")])
 
 
+class fcsim_kv_read_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("slots", "k_out", "v_out", "status")] + [("n_tokens", C.c_int32), ("dtype", C.c_int32)]
+
+
 class fcsim_kv_workspace(C.Structure):
     _fields_ = [("bytes", C.c_size_t), ("zeroed", C.c_size_t)]
 
 
 # the argument structs as one packing each (native sizes and alignment, as the compiler's)
-_APPEND, _ATTEND, _EVICT = struct.Struct("10P6q6ifi"), struct.Struct("6P3q7if"), struct.Struct("7P2q8i")
+_APPEND, _ATTEND, _EVICT = struct.Struct("10P6q6ifi"), struct.Struct("6P3q7if2i"), struct.Struct("7P2q8i")
+_READ = struct.Struct("4P2i")
 assert (_APPEND.size, _ATTEND.size, _EVICT.size) == (C.sizeof(fcsim_kv_append_args), C.sizeof(fcsim_kv_attend_args),
                                                      C.sizeof(fcsim_kv_evict_args))
+assert _READ.size == C.sizeof(fcsim_kv_read_args)
 
 EXPORTS = ("fcsim_kv_append", "fcsim_kv_attend_workspace", "fcsim_kv_attend", "fcsim_kv_evict_workspace",
-           "fcsim_kv_evict", "fcsim_kv_last_cuda_error")
+           "fcsim_kv_evict", "fcsim_kv_read", "fcsim_kv_last_cuda_error")
 
 _lib = None
 
@@ -89,7 +96,7 @@ def load():
     if _lib is None:
         lib = _fb.load()
         vp = C.c_void_p
-        lib.fcsim_kv_append.argtypes = [vp, vp, vp]
+        lib.fcsim_kv_append.argtypes = lib.fcsim_kv_read.argtypes = [vp, vp, vp]
         for name in ("attend", "evict"):
             getattr(lib, f"fcsim_kv_{name}_workspace").argtypes = [vp, vp, C.POINTER(fcsim_kv_workspace)]
             getattr(lib, f"fcsim_kv_{name}").argtypes = [vp, vp, vp, C.c_size_t, vp]
@@ -289,14 +296,14 @@ class PagedKV:
         self._call(_lib.fcsim_kv_append, args)
         return out
 
-    def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, add_weight=False,
+    def attend(self, q, table, lengths, *, max_length=None, scale=None, window=0, first=0, add_weight=False,
                return_lse=False):
         """Attention of one token per request: ``q`` [requests, heads, head_dim] over the ``lengths`` (int32) tokens
         that the rows of ``table`` (int32 [requests, pages]) hold; returns [requests, heads, head_dim], with
         ``return_lse`` also the float32 [requests, heads] log-sum-exp.
 
         ``max_length`` bounds the lengths (default: what the table's width holds).  ``window`` > 0: the newest tokens
-        only.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
+        only, and the ``first`` oldest.  ``add_weight``: the cache's weights grow by each token's share (requests must not share pages)."""
         if q.requires_grad and _grad_enabled():
             _refuse_gradient()
         dtype, shape, index = q.dtype, q.shape, self._index
@@ -316,7 +323,7 @@ class PagedKV:
                 q.data_ptr(), out.data_ptr(), _pointer(lse), table.data_ptr(), lengths.data_ptr(), self._status, q_row,
                 q_head, table.stride(0), n, heads, _TYPES[dtype], cols,
                 min(cols * self.page_size, _MOST) if max_length is None else max_length, window, 1 if add_weight else 0,
-                1.0 / math.sqrt(self.head_dim) if scale is None else scale)
+                1.0 / math.sqrt(self.head_dim) if scale is None else scale, first, 0)
         except _NO_FIT as e:
             raise ValueError(f"attend: {e}") from None
         self._call(_lib.fcsim_kv_attend, args, _lib.fcsim_kv_attend_workspace)
@@ -348,6 +355,25 @@ class PagedKV:
             raise ValueError(f"evict: {e}") from None
         self._call(_lib.fcsim_kv_evict, args, _lib.fcsim_kv_evict_workspace)
         return new_lengths, kept
+
+    def read(self, slots, *, dtype=None):
+        """What stands at ``slots`` (int64 [n], page * page_size + place, negative = zeros): k and v as [n, n_kv_heads, head_dim]
+        of ``dtype`` (float16 or bfloat16; default: the cache's own, of an 8-bit cache bfloat16), 8-bit values times their scales."""
+        if dtype is None:
+            dtype = torch.bfloat16 if self.k_scale is not None else self.k.dtype
+        if dtype not in _WIDE:
+            raise ValueError(f"dtype: float16 or bfloat16, got {dtype}")
+        n = slots.numel()
+        if slots.dtype != _I64 or slots.get_device() != self._index or not slots.is_contiguous():
+            self._refuse("slots", "contiguous int64", slots)
+        k = slots.new_empty((n, self.n_kv_heads, self.head_dim), dtype=dtype)
+        v = torch.empty_like(k)
+        try:
+            args = _READ.pack(slots.data_ptr(), k.data_ptr(), v.data_ptr(), self._status, n, _TYPES[dtype])
+        except _NO_FIT as e:
+            raise ValueError(f"read: {e}") from None
+        self._call(_lib.fcsim_kv_read, args)
+        return k, v
 
     def check(self):
         """Wait for all calls, on every stream, read and clear the device status; raise when a call met a bad page, length, position
