@@ -1,5 +1,5 @@
 /*
- * fcsim_kv -- the paged key-value cache of one layer on the device: append, attend, evict, read.
+ * fcsim_kv -- the paged key-value cache of one layer on the device: append, attend, prefill, evict, read.
  *
  * The simulator (fcsim.h) counts tokens of KV cache per slot; these operators are what a slot does to a real
  * cache.  A cache is a pool of n_pages pages of page_size tokens; a request owns pages through a row of a table
@@ -9,6 +9,7 @@
  *   attend   one query token per request: o = sum_t softmax_t(scale q . k_t) v_t over the request's cached tokens;
  *            optionally each token's weight grows by the attention it received (summed over the query heads that
  *            share its kv head).
+ *   prefill  the same for several query tokens per request, each of which sees the tokens up to its own: a prompt, or a chunk of one.
  *   evict    per request and kv head: the oldest `first`, the newest `recent` and, of the rest, the largest
  *            weights are kept up to a budget; the kept rows move in order, with their weights, to other pages.
  *   read     the values that stand at given slots, as 16-bit rows: what append has stored, for another cache or for the eye.
@@ -41,7 +42,8 @@ enum { /* bits of *status */
     FCSIM_KV_BAD_PAGE = 1,     /* page or slot outside the pool: its tokens are left out (evict: see there) */
     FCSIM_KV_BAD_LENGTH = 2,   /* length < 0 (taken as 0) or > max_length (taken as max_length) */
     FCSIM_KV_BAD_POSITION = 4, /* position outside the rope table: q_out row zero, nothing stored */
-    FCSIM_KV_BAD_BUDGET = 8    /* budget < 0 (taken as 0) or > max_budget (taken as max_budget) */
+    FCSIM_KV_BAD_BUDGET = 8,   /* budget < 0 (taken as 0) or > max_budget (taken as max_budget) */
+    FCSIM_KV_STUCK = 16        /* a wait inside a kernel took seconds and was given up: the call's results are wrong */
 };
 
 /* head_dim: a multiple of 8 (16-bit caches) or 16 (E4M3), at most 256.  k and v have the same strides.
@@ -121,6 +123,34 @@ typedef struct {
 int fcsim_kv_attend_workspace(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* args, fcsim_kv_workspace* out);
 int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* args, void* workspace,
                     size_t workspace_bytes, void* cuda_stream);
+
+/* q: n_rows rows, row i at q + i * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.  Request r has the rows starts[r] ..
+ * starts[r + 1] - 1 (starts: [n_requests + 1] int32, not falling, 0 .. n_rows): the newest of its lengths[r] tokens, which are all in
+ * the cache already.  A row whose token is number p sees the tokens t <= p, with window > 0 only those of t > p - window or t < first (without
+ * a window `first` has no effect).  n_heads: a multiple of n_kv_heads; head h reads kv head h / (n_heads / n_kv_heads).
+ * table, lengths, max_length, workspace: as for attend (one workspace serves both).
+ * out: [n_rows][n_heads][head_dim] contiguous, in q's type.  lse: [n_rows][n_heads] fp32, or NULL.  A row that sees nothing, or belongs to no
+ * request, gives zeros and -infinity.  What a row does not see may hold anything, infinities and NaN too.
+ * Softmax weights of F16 queries are multiples of 2^-38 of the row's largest; of BF16 queries and a 16-bit cache, values below 2^-94 lose bits.
+ * starts beyond 0 .. n_rows are taken as these ends, a request of more rows than tokens has rows that see nothing (FCSIM_KV_BAD_LENGTH
+ * for either).  n_rows and max_length are at most 2^31 - 2^16, n_requests 65535, n_heads * head_dim below 2^31. */
+typedef struct {
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t* starts;
+    const int32_t* table;
+    const int32_t* lengths;
+    int32_t* status;
+    int64_t q_row, q_head, table_row;
+    int32_t n_rows, n_requests, n_heads, dtype, table_cols, max_length, window, first;
+    float scale;
+    int32_t reserved;
+} fcsim_kv_prefill_args;
+
+int fcsim_kv_prefill_workspace(const fcsim_kv_cache* cache, const fcsim_kv_prefill_args* args, fcsim_kv_workspace* out);
+int fcsim_kv_prefill(const fcsim_kv_cache* cache, const fcsim_kv_prefill_args* args, void* workspace,
+                     size_t workspace_bytes, void* cuda_stream);
 
 /* Request r keeps n' = min(length, budget[r]) tokens: the newest min(recent, budget), of what is left the oldest
  * min(first, budget - recent), then the largest weights (equal weights: the oldest first; NaN counts as the lowest,

@@ -15,10 +15,12 @@ KERNEL_SOURCE = os.path.join(CSRC, "fcsim_step_kernels.cu")   # compiled once pe
 N_KERNEL_POLICIES = 7
 KV_SOURCE = os.path.join(CSRC, "fcsim_kv.cu")                  # the paged key-value cache
 KV_ATTEND_SOURCE = os.path.join(CSRC, "fcsim_kv_attend.cu")    # its attention, compiled once per pair of types
-N_KV_TYPES = 4
-SOURCES = [HOST_SOURCE, KERNEL_SOURCE, KV_SOURCE, KV_ATTEND_SOURCE]
+KV_PREFILL_SOURCE = os.path.join(CSRC, "fcsim_kv_prefill.cu")  # and of several tokens, the same
+N_KV_TYPES = 2 * 4                                             # objects of the two
+SOURCES = [HOST_SOURCE, KERNEL_SOURCE, KV_SOURCE, KV_ATTEND_SOURCE, KV_PREFILL_SOURCE]
 HEADERS = [os.path.join(CSRC, "fcsim_device.cuh"), os.path.join(ROOT, "include", "fcsim.h"),
            os.path.join(CSRC, "fcsim_kv_device.cuh"), os.path.join(CSRC, "fcsim_kv_attend.cuh"),
+           os.path.join(CSRC, "fcsim_kv_prefill.cuh"),
            os.path.join(ROOT, "include", "fcsim_kv.h")]
 OBJ_DIR = os.path.join(HERE, "_build")
 
@@ -61,8 +63,9 @@ def _compile(lib: str, verbose: bool, extra) -> str:
         jobs.append((KERNEL_SOURCE, extra + [f"-DFCSIM_KERNEL_POLICY={pol}"], os.path.join(OBJ_DIR, f"{tag}_policy{pol}.o")))
     # the cache's objects are the same in both builds: the checked one takes those that are there
     kv = [(KV_SOURCE, [], os.path.join(OBJ_DIR, "kv.o"))]
-    for types in range(N_KV_TYPES):
-        kv.append((KV_ATTEND_SOURCE, [f"-DFCSIM_KV_TYPES={types}"], os.path.join(OBJ_DIR, f"kv_attend{types}.o")))
+    for source, name in ((KV_ATTEND_SOURCE, "kv_attend"), (KV_PREFILL_SOURCE, "kv_prefill")):
+        for types in range(N_KV_TYPES // 2):
+            kv.append((source, [f"-DFCSIM_KV_TYPES={types}"], os.path.join(OBJ_DIR, f"{name}{types}.o")))
     jobs += kv
     there = {obj for _, _, obj in kv if extra and not _stale(obj)}
 

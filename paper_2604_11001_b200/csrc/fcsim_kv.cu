@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "fcsim_kv_attend.cuh"
+#include "fcsim_kv_prefill.cuh"
 
 using namespace fcsim_kv_dev;
 
@@ -769,6 +770,55 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     return FCSIM_OK;
 }
 
+// ------------------------------------------------------------------------------------------------ prefill
+PrefillVariant prefill_variant(const fcsim_kv_cache* c, int dtype) {
+    if (c->dtype == FCSIM_KV_E4M3) return dtype == FCSIM_KV_F16 ? prefill_variant_f16_e4m3(c->head_dim) : prefill_variant_bf16_e4m3(c->head_dim);
+    return dtype == FCSIM_KV_F16 ? prefill_variant_f16(c->head_dim) : prefill_variant_bf16(c->head_dim);
+}
+
+int check_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, PrefillParams* p, PrefillVariant* v) {
+    int rc = check_cache(c, &p->pool);
+    if (rc != FCSIM_OK) return rc;
+    if (!a) return FCSIM_EINVAL;
+    if ((rc = check_type(c, a->dtype)) != FCSIM_OK) return rc;
+    if (a->n_rows < 0 || a->n_rows > kMaxTokens || a->n_requests < 0 || a->n_requests > 65535) return FCSIM_EINVAL;
+    if (a->n_heads < 1 || a->n_heads % c->n_kv_heads || (int64_t)a->n_heads * c->head_dim > 0x7fffffff) return FCSIM_EINVAL;
+    if (a->table_cols < 0 || a->max_length < 0 || a->max_length > (int64_t)a->table_cols * c->page_size || a->max_length > kMaxTokens)
+        return FCSIM_EINVAL;
+    if (a->window < 0 || a->first < 0 || a->table_row < 0 || !isfinite(a->scale)) return FCSIM_EINVAL;
+    if (!good_stride(a->q_row, 2) || !good_stride(a->q_head, 2)) return FCSIM_EINVAL;
+    if (a->n_rows > 0) {
+        if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out)) return FCSIM_ESIZE;
+        if (a->n_requests > 0 && (!a->starts || !a->lengths || (a->max_length > 0 && !a->table))) return FCSIM_ESIZE;
+    }
+    p->q = (const char*)a->q, p->out = (char*)a->out, p->lse = a->lse, p->starts = a->starts, p->table = a->table;
+    p->lengths = a->lengths, p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
+    p->n_rows = a->n_rows, p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length;
+    const bool all = (int64_t)a->window + a->first >= a->max_length || a->window == 0;  // (of the longest request, and so of all)
+    p->window = all ? 0 : a->window, p->first = all ? 0 : a->first;
+    p->scale = a->scale;
+    // the rows of a block: all heads of a group and as many tokens as there is room for
+    *v = prefill_variant(c, a->dtype);
+    const int group = a->n_heads / c->n_kv_heads;
+    p->head_tiles = (group + v->rows - 1) / v->rows;
+    p->heads_a_tile = (group + p->head_tiles - 1) / p->head_tiles;
+    p->tokens_a_block = v->rows / p->heads_a_tile;
+    return FCSIM_OK;
+}
+
+constexpr size_t kPrefillCounters = kMaxCtas * (kThreads / 32) * 4;  // those of attend: one workspace serves both
+
+int prefill_layout(const PrefillParams& p, const PrefillVariant& v, int* device, int* grid, size_t* bytes) {
+    int sms = 0, rc = device_and_sms(device, &sms);
+    if (rc != FCSIM_OK) return rc;
+    // a CTA has an SM to itself; no more of them than tiles that there may be
+    const int64_t blocks = (int64_t)p.n_rows / p.tokens_a_block + std::min(p.n_requests, p.n_rows), tiles = (p.max_length + (int64_t)v.keys - 1) / v.keys;
+    const int64_t most = std::min<int64_t>(blocks * p.pool.n_kv, 1 << 20) * p.head_tiles * std::max<int64_t>(tiles, 1);
+    *grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms, (int64_t)kMaxCtas, most}));
+    *bytes = kPrefillCounters + (size_t)*grid * 2 * (v.rows / 128) * (v.width + 2) * 128 * 4;
+    return FCSIM_OK;
+}
+
 int check_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args* a, EvictParams* p) {
     int rc = check_cache(c, &p->pool);
     if (rc != FCSIM_OK) return rc;
@@ -901,6 +951,37 @@ extern "C" int fcsim_kv_evict(const fcsim_kv_cache* c, const fcsim_kv_evict_args
     if (chunks <= 8) return launch_move<8>(p, a->n_requests, stream);
     if (chunks <= 16) return launch_move<16>(p, a->n_requests, stream);
     return launch_move<32>(p, a->n_requests, stream);
+}
+
+extern "C" int fcsim_kv_prefill_workspace(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, fcsim_kv_workspace* out) {
+    PrefillParams p;
+    PrefillVariant v;
+    int rc = check_prefill(c, a, &p, &v);
+    if (rc != FCSIM_OK) return rc;
+    if (!out) return FCSIM_EINVAL;
+    *out = {0, 0};
+    if (p.n_rows == 0) return FCSIM_OK;
+    int device, grid;
+    size_t bytes;
+    if ((rc = prefill_layout(p, v, &device, &grid, &bytes)) != FCSIM_OK) return rc;
+    *out = {bytes, kPrefillCounters};
+    return FCSIM_OK;
+}
+
+extern "C" int fcsim_kv_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, void* workspace,
+                                size_t workspace_bytes, void* cuda_stream) {
+    PrefillParams p;
+    PrefillVariant v;
+    int rc = check_prefill(c, a, &p, &v);
+    if (rc != FCSIM_OK) return rc;
+    if (p.n_rows == 0) return FCSIM_OK;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < kPrefillCounters) return FCSIM_ESIZE;
+    int device, grid;
+    size_t bytes;
+    if ((rc = prefill_layout(p, v, &device, &grid, &bytes)) != FCSIM_OK) return rc;
+    if (workspace_bytes < bytes) return FCSIM_ESIZE;
+    p.counters = (int*)workspace, p.parts = (float*)((char*)workspace + kPrefillCounters);
+    return cuda_status((cudaError_t)v.launch(p, grid, device, (cudaStream_t)cuda_stream));
 }
 
 extern "C" int fcsim_kv_read(const fcsim_kv_cache* c, const fcsim_kv_read_args* a, void* cuda_stream) {

@@ -1,4 +1,4 @@
-"""ctypes binding of the paged key-value cache (include/fcsim_kv.h): append, attend, evict, read.
+"""ctypes binding of the paged key-value cache (include/fcsim_kv.h): append, attend, prefill, evict, read.
 
 Argument checks and marshalling only -- the work is done by the CUDA library, on the current stream of the cache's
 device.  PyTorch provides device memory and streams; there is no CPU fallback.
@@ -6,6 +6,7 @@ device.  PyTorch provides device memory and streams; there is no CPU fallback.
     cache = PagedKV.allocate(n_pages=1024, page_size=16, n_kv_heads=8, head_dim=128, weight=True)
     q = cache.append(q, k, v, positions, slots, rope=table, q_norm=w_q, k_norm=w_k)   # a slot's new tokens
     out = cache.attend(q, table, lengths, add_weight=True)                            # one query per request
+    out = cache.prefill(q, starts, table, lengths)                                    # several, as of a prompt
     new_lengths, kept = cache.evict(table, lengths, budget, new_table, max_budget=512, recent=64, first=4)
     k, v = cache.read(slots)                                                          # what stands there
     cache.check()                                                                     # synchronises
@@ -22,7 +23,7 @@ import torch
 from . import binding as _fb
 
 F16, BF16, E4M3 = 0, 1, 2
-BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET = 1, 2, 4, 8
+BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_BUDGET, STUCK = 1, 2, 4, 8, 16
 _TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
 _I32, _I64 = torch.int32, torch.int64
 _WIDE = frozenset((torch.float16, torch.bfloat16))
@@ -61,6 +62,14 @@ class fcsim_kv_attend_args(C.Structure):
                 + [("scale", C.c_float), ("first", C.c_int32), ("reserved", C.c_int32)])
 
 
+class fcsim_kv_prefill_args(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "out", "lse", "starts", "table", "lengths", "status")]
+                + [(n, C.c_int64) for n in ("q_row", "q_head", "table_row")]
+                + [(n, C.c_int32) for n in ("n_rows", "n_requests", "n_heads", "dtype", "table_cols", "max_length", "window",
+                                            "first")]
+                + [("scale", C.c_float), ("reserved", C.c_int32)])
+
+
 class fcsim_kv_evict_args(C.Structure):
     _fields_ = ([(n, C.c_void_p) for n in ("table", "lengths", "budget", "new_table", "new_lengths", "kept",
                                            "status")]
@@ -79,12 +88,13 @@ class fcsim_kv_workspace(C.Structure):
 
 # the argument structs as one packing each (native sizes and alignment, as the compiler's)
 _APPEND, _ATTEND, _EVICT = struct.Struct("10P6q6ifi"), struct.Struct("6P3q7if2i"), struct.Struct("7P2q8i")
-_READ = struct.Struct("4P2i")
+_READ, _PREFILL = struct.Struct("4P2i"), struct.Struct("7P3q8ifi")
 assert (_APPEND.size, _ATTEND.size, _EVICT.size) == (C.sizeof(fcsim_kv_append_args), C.sizeof(fcsim_kv_attend_args),
                                                      C.sizeof(fcsim_kv_evict_args))
-assert _READ.size == C.sizeof(fcsim_kv_read_args)
+assert (_READ.size, _PREFILL.size) == (C.sizeof(fcsim_kv_read_args), C.sizeof(fcsim_kv_prefill_args))
 
-EXPORTS = ("fcsim_kv_append", "fcsim_kv_attend_workspace", "fcsim_kv_attend", "fcsim_kv_evict_workspace",
+EXPORTS = ("fcsim_kv_append", "fcsim_kv_attend_workspace", "fcsim_kv_attend", "fcsim_kv_prefill_workspace", "fcsim_kv_prefill",
+           "fcsim_kv_evict_workspace",
            "fcsim_kv_evict", "fcsim_kv_read", "fcsim_kv_last_cuda_error")
 
 _lib = None
@@ -97,7 +107,7 @@ def load():
         lib = _fb.load()
         vp = C.c_void_p
         lib.fcsim_kv_append.argtypes = lib.fcsim_kv_read.argtypes = [vp, vp, vp]
-        for name in ("attend", "evict"):
+        for name in ("attend", "prefill", "evict"):
             getattr(lib, f"fcsim_kv_{name}_workspace").argtypes = [vp, vp, C.POINTER(fcsim_kv_workspace)]
             getattr(lib, f"fcsim_kv_{name}").argtypes = [vp, vp, vp, C.c_size_t, vp]
         lib.fcsim_kv_last_cuda_error.argtypes = []
@@ -329,6 +339,40 @@ class PagedKV:
         self._call(_lib.fcsim_kv_attend, args, _lib.fcsim_kv_attend_workspace)
         return (out, lse) if return_lse else out
 
+    def prefill(self, q, starts, table, lengths, *, max_length=None, scale=None, window=0, first=0, return_lse=False):
+        """Attention of several tokens per request, such as those of a prompt or of a chunk of one: the rows ``starts[r]`` ..
+        ``starts[r + 1] - 1`` (``starts``: int32 [requests + 1]) of ``q`` [n, heads, head_dim] are the newest of the ``lengths`` (int32)
+        tokens of request r, which the rows of ``table`` (int32 [requests, pages]) hold already.  Each sees the tokens up to its own, with
+        ``window`` > 0 only the newest so many of these and the ``first`` oldest.  Returns [n, heads, head_dim], with ``return_lse``
+        also the float32 [n, heads] log-sum-exp; rows of no request are zeros."""
+        if q.requires_grad and _grad_enabled():
+            _refuse_gradient()
+        dtype, shape, index = q.dtype, q.shape, self._index
+        if dtype not in _WIDE or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
+            self._refuse("q", f"float16 or bfloat16 [tokens, heads, {self.head_dim}]", q)
+        n, heads, _ = shape
+        q_row, q_head, q_one = q.stride()
+        if q_one != 1:
+            raise ValueError("q: head_dim has to be contiguous")
+        requests = lengths.numel()
+        cols = self._table(table, "table", requests)
+        if lengths.dtype != _I32 or lengths.get_device() != index or not lengths.is_contiguous():
+            self._refuse("lengths", "contiguous int32 [requests]", lengths)
+        if starts.dtype != _I32 or starts.numel() != requests + 1 or starts.get_device() != index or not starts.is_contiguous():
+            self._refuse("starts", f"contiguous int32 [{requests + 1}]", starts)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = q.new_empty((n, heads), dtype=torch.float32) if return_lse else None
+        try:
+            args = _PREFILL.pack(
+                q.data_ptr(), out.data_ptr(), _pointer(lse), starts.data_ptr(), table.data_ptr(), lengths.data_ptr(), self._status,
+                q_row, q_head, table.stride(0), n, requests, heads, _TYPES[dtype], cols,
+                min(cols * self.page_size, _MOST) if max_length is None else max_length, window, first,
+                1.0 / math.sqrt(self.head_dim) if scale is None else scale, 0)
+        except _NO_FIT as e:
+            raise ValueError(f"prefill: {e}") from None
+        self._call(_lib.fcsim_kv_prefill, args, _lib.fcsim_kv_prefill_workspace)
+        return (out, lse) if return_lse else out
+
     def evict(self, table, lengths, budget, new_table, *, max_budget=None, recent=0, first=0, max_length=None):
         """Cut every request to its ``budget`` (int32 [requests]) of tokens per kv head: the ``recent`` newest, the
         ``first`` oldest and the largest weights, copied in order to the pages of ``new_table`` (none of which the
@@ -382,6 +426,8 @@ class PagedKV:
         bits = int(self.status.item())
         if bits:
             self.status.zero_()
+            if bits & STUCK:
+                raise RuntimeError("a wait inside a kernel was given up: results are wrong")
             names = [s for b, s in ((BAD_PAGE, "page or slot outside the pool"),
                                     (BAD_LENGTH, "length outside 0 .. max_length"),
                                     (BAD_POSITION, "position outside the rope table"),
