@@ -93,6 +93,27 @@ __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&x)[32])
           "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31])
         : "memory");
 }
+// two 32-bit values at once
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+    return x;
+}
+__device__ __forceinline__ float2 unpair(uint64_t x) {
+    float2 y;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
+    return y;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // 2^x; results below 2^-126 are 0
 __device__ __forceinline__ float power2(float x) {
     float y;
@@ -110,6 +131,14 @@ __device__ __forceinline__ uint32_t instruction(uint32_t type, bool b_across, ui
     return 1u << 4 | type << 7 | type << 10 | (uint32_t)b_across << 16 | (n >> 3) << 17 | (m >> 4) << 24;
 }
 
+// whichever of the warp's lanes, for numbers that are the same in all: in a register of the warp, as what issues products needs them
+__device__ __forceinline__ uint32_t uni(uint32_t x) { return __reduce_max_sync(~0u, x); }
+__device__ __forceinline__ bool elected() {
+    uint32_t x;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(x));
+    return x != 0;
+}
+
 // ---------------------------------------------------------------------------------------------- shape
 template <class T, class C, int DP>
 struct Shape {
@@ -121,8 +150,14 @@ struct Shape {
     static constexpr int kRoom = (227 * 1024 - 2048 - 1024 - kQuery) / kStage;
     static constexpr int kStages = kRoom < 8 ? kRoom : 8;
     static constexpr int kBytes = kQuery + kStages * kStage + 1024;
-    static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 3;
+    static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 7;
     static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 1, kThreads = 32 * kWarps;
+    // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's.
+    static constexpr int kSoftmaxRegisters = 160, kOtherRegisters = 96;
+    // A warp loads half a tile at a time.  It waits for the place of a tile by the parity of one barrier, so the tile that was there two rounds before
+    // has to be gone: it is, as what the warp has loaded last waited for a later one.
+    static_assert(kLoadWarps <= 2 * kStages, "parities");
+    static_assert(kTiles == 1 || 256 * kSoftmaxRegisters + 256 * kOtherRegisters <= 128 * kThreads, "a split beyond the launch's total waits for good");
     // tensor memory: two areas of kKeys columns for S and P, then O of each tile
     static constexpr int kScore = 0, kOutput = 2 * kKeys, kColumns = 512;
     static_assert(kOutput + kTiles * DP <= kColumns && kStages >= 4, "room");
@@ -132,10 +167,13 @@ struct Shape {
 // Cost of a block's start and end beside one tile of keys.
 constexpr int kOverhead = 2;
 constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are cut
+// A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and
+// their outputs are joined as those of different CTAs are.
+constexpr int kSharedLeast = 6;
 
-// A block of rows: tokens [at, at + tokens) of the new ones of a request, heads of one head tile.
+// A block of rows: tokens [b * tokens_a_block, + tokens) of the new ones of a request, heads of one head tile.
 struct Block {
-    int r, head, b;              // request, kv head * head tiles + head tile, block
+    int r, kv, ht, b;
     int row0, rows, position0;   // the request's rows in q; position of the first of them
     int tokens, gap, seen, tiles;
 };
@@ -149,37 +187,43 @@ __device__ __forceinline__ int request_length(const PrefillParams& p, int r) { r
 // What a block of tokens sees: all tokens up to its last one, or the first ones and, without the gap behind these, those from the start of
 // its first token's window.  Counted without the gap: seen key u is token u, or behind the first ones u + gap.
 __device__ __forceinline__ int seen_by(const PrefillParams& p, int position0, int tokens, int& gap) {
-    const int64_t low = (int64_t)position0 - p.window + 1;  // (a request of more rows than tokens has positions below 0)
-    gap = p.window > 0 && low > p.first ? (int)(low - p.first) : 0;
+    gap = 0;
+    if (p.window > 0) {
+        const int64_t low = (int64_t)position0 - p.window + 1;  // (a request of more rows than tokens has positions below 0)
+        if (low > p.first) gap = (int)(low - p.first);
+    }
     return max(position0 + tokens - gap, 0);
 }
 template <int KEYS>
 __device__ __forceinline__ int tiles_of(const PrefillParams& p, int position0, int rows, int b) {
     int gap;
     const int at = b * p.tokens_a_block;
-    return max(1, (seen_by(p, position0 + at, min(p.tokens_a_block, rows - at), gap) + KEYS - 1) / KEYS);
+    return max(1, (int)((unsigned)(seen_by(p, position0 + at, min(p.tokens_a_block, rows - at), gap) + KEYS - 1) / KEYS));
 }
-__device__ __forceinline__ int blocks_of(const PrefillParams& p, int rows) { return (int)(((int64_t)rows + p.tokens_a_block - 1) / p.tokens_a_block); }
+__device__ __forceinline__ int blocks_of(const PrefillParams& p, int rows) { return (unsigned)(rows + p.tokens_a_block - 1) / (unsigned)p.tokens_a_block; }
 
 template <int KEYS>
 __device__ __forceinline__ void enter_block(const PrefillParams& p, Block& x) {
     const int at = x.b * p.tokens_a_block;
     x.tokens = min(p.tokens_a_block, x.rows - at);
     x.seen = seen_by(p, x.position0 + at, x.tokens, x.gap);
-    x.tiles = max(1, (x.seen + KEYS - 1) / KEYS);
+    x.tiles = max(1, (int)((unsigned)(x.seen + KEYS - 1) / KEYS));
 }
-template <int KEYS>
 __device__ __forceinline__ void enter_request(const PrefillParams& p, Block& x) {
     x.rows = request_rows(p, x.r, x.row0);
     x.position0 = request_length(p, x.r) - x.rows;
 }
 
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // neither below 0
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // The division of the units among the CTAs, which depends on the lengths and the grid alone.  A unit is a tile of keys (and kOverhead of them
 // stand before a block's first tile), or, with `cut`, a piece of a block of at most `cut` tiles.
 struct Division {
-    int64_t total, share;
+    int64_t first, end, share;  // of this CTA
     int cut;
-    __device__ __forceinline__ int units(int tiles) const { return cut ? (tiles + cut - 1) / cut : tiles + kOverhead; }
+    __device__ __forceinline__ int units(int tiles) const { return cut ? (unsigned)(tiles + cut - 1) / (unsigned)cut : tiles + kOverhead; }
 };
 
 // Where a CTA's stretch begins.
@@ -197,18 +241,11 @@ __device__ __forceinline__ int64_t warp_sum(int64_t x) {
     return x;
 }
 
-// Units (or tiles, with `tiles_only`) of one of the heads of request base + lane, and its blocks.  The blocks of long requests are added up by the warp.
+// Tiles of one of the heads of a lane's request (`rows` of them from position0 on), or units of the division.  Long requests are added up by the warp.
 template <int KEYS>
-__device__ __forceinline__ int64_t units_of_requests(const PrefillParams& p, int r, bool mine, const Division* d, int& blocks) {
-    constexpr int kAlone = 4;
+__device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, int position0, int blocks, const Division* d) {
+    constexpr int kAlone = 2;
     const int lane = threadIdx.x & 31;
-    int rows = 0, position0 = 0;
-    if (mine) {
-        int row0;
-        rows = request_rows(p, r, row0);
-        position0 = request_length(p, r) - rows;
-    }
-    blocks = blocks_of(p, rows);
     int64_t own = 0;
     auto cost = [&](int position, int n, int b) {
         const int t = tiles_of<KEYS>(p, position, n, b);
@@ -217,6 +254,7 @@ __device__ __forceinline__ int64_t units_of_requests(const PrefillParams& p, int
     if (blocks <= kAlone)
         for (int b = 0; b < blocks; b++) own += cost(position0, rows, b);
     uint32_t together = __ballot_sync(~0u, blocks > kAlone);
+#pragma unroll 1
     while (together) {
         const int src = __ffs(together) - 1;
         together &= together - 1;
@@ -228,74 +266,88 @@ __device__ __forceinline__ int64_t units_of_requests(const PrefillParams& p, int
     }
     return own;
 }
+template <int KEYS>
+__device__ __forceinline__ int64_t add_request(const PrefillParams& p, int r, bool mine, const Division* d, int& blocks) {
+    int rows = 0, position0 = 0, row0;
+    if (mine) {
+        rows = request_rows(p, r, row0);
+        position0 = request_length(p, r) - rows;
+    }
+    blocks = blocks_of(p, rows);
+    return add_blocks<KEYS>(p, rows, position0, blocks, d);
+}
 
 template <int KEYS, int WARPS>
 __device__ __forceinline__ Division plan(const PrefillParams& p, Start& start) {
     __shared__ int64_t sums[2][WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int heads = p.pool.n_kv * p.head_tiles, each = (p.n_requests + WARPS - 1) / WARPS;
+    const int heads = p.pool.n_kv * p.head_tiles, each = (unsigned)(p.n_requests + WARPS - 1) / WARPS;
     const int r0 = min(warp * each, p.n_requests), r1 = min(r0 + each, p.n_requests);
-    auto add_up = [&](const Division* d) {
+    auto add_up = [&](const Division* d, bool again) {
         int64_t units = 0, blocks = 0;
+#pragma unroll 1
         for (int base = r0; base < r1; base += 32) {
             int n;
-            units += units_of_requests<KEYS>(p, base + lane, base + lane < r1, d, n);
+            units += add_request<KEYS>(p, base + lane, base + lane < r1, d, n);
             blocks += n;
         }
         units = warp_sum(units), blocks = warp_sum(blocks);
-        __syncthreads();
+        if (again) __syncthreads();
         if (lane == 0) sums[0][warp] = units, sums[1][warp] = blocks;
         __syncthreads();
     };
-    add_up(nullptr);
+    if (threadIdx.x == 0) start.left = 0;
+    add_up(nullptr, false);
     int64_t tiles = 0, blocks = 0;
     for (int w = 0; w < WARPS; w++) tiles += sums[0][w], blocks += sums[1][w];
     Division d;
     d.cut = 0;
+    int64_t total;
     if (blocks * heads <= gridDim.x) {  // so that the pieces fit the grid
         const int64_t spare = max((int64_t)1, gridDim.x - blocks * heads);
-        d.cut = (int)max((int64_t)kPieceLeast, (tiles * heads + spare - 1) / spare);
-        add_up(&d);
+        d.cut = (int)max((int64_t)kPieceLeast, divide(tiles * heads + spare - 1, spare));
+        add_up(&d, true);
         tiles = 0;
         for (int w = 0; w < WARPS; w++) tiles += sums[0][w];
-        d.total = tiles * heads;
+        total = tiles * heads;
         d.share = 1;
     } else {
-        d.total = (tiles + kOverhead * blocks) * heads;
-        d.share = max((int64_t)1, (d.total + gridDim.x - 1) / gridDim.x);
+        total = (tiles + kOverhead * blocks) * heads;
+        d.share = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x));
     }
-    const int64_t first = min(d.total, (int64_t)blockIdx.x * d.share), end = min(d.total, first + d.share);
-    if (threadIdx.x == 0) start.left = 0;
-    __syncthreads();
-    if (first >= end) return d;
+    d.first = min(total, (int64_t)blockIdx.x * d.share), d.end = min(total, d.first + d.share);
+    if (d.first >= d.end) return d;
     // the warp whose requests hold the first unit looks for it
     int64_t before = 0;
     for (int w = 0; w < warp; w++) before += (sums[0][w] + (d.cut ? 0 : kOverhead * sums[1][w])) * heads;
     const int64_t mine = (sums[0][warp] + (d.cut ? 0 : kOverhead * sums[1][warp])) * heads;
-    if (first >= before && first < before + mine) {
+    if (d.first >= before && d.first < before + mine) {
+#pragma unroll 1
         for (int base = r0; base < r1; base += 32) {
             int n;
-            const int64_t own = units_of_requests<KEYS>(p, base + lane, base + lane < r1, &d, n) * heads;
+            const int64_t own = add_request<KEYS>(p, base + lane, base + lane < r1, &d, n) * heads;
             int64_t upto = own;
 #pragma unroll
             for (int i = 1; i < 32; i <<= 1) {
                 const int64_t x = __shfl_up_sync(~0u, upto, i);
                 if (lane >= i) upto += x;
             }
-            const uint32_t found = __ballot_sync(~0u, before + upto > first);
+            const uint32_t found = __ballot_sync(~0u, before + upto > d.first);
             if (found == 0) {
                 before += __shfl_sync(~0u, upto, 31);
                 continue;
             }
             const int src = __ffs(found) - 1;
-            const int64_t per_head = __shfl_sync(~0u, own, src) / heads;
-            int64_t x = first - before - __shfl_sync(~0u, upto - own, src);
+            const int64_t per_head = divide(__shfl_sync(~0u, own, src), heads);
+            int64_t x = d.first - before - __shfl_sync(~0u, upto - own, src);
             Block k;
             k.r = base + src;
-            k.head = (int)(x / per_head);
-            x -= k.head * per_head;
-            enter_request<KEYS>(p, k);
+            const int head = (int)divide(x, per_head);
+            k.kv = (unsigned)head / (unsigned)p.head_tiles, k.ht = head - k.kv * p.head_tiles;
+            x -= head * per_head;
+            enter_request(p, k);
             const int all = blocks_of(p, k.rows);
+#pragma unroll 1
             for (int b0 = 0; b0 < all; b0 += 32) {
                 const int cost = b0 + lane < all ? d.units(tiles_of<KEYS>(p, k.position0, k.rows, b0 + lane)) : 0;
                 int64_t sum = cost;
@@ -318,12 +370,13 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Start& start) {
                     start.block = k;
                     if (d.cut) {
                         start.piece = (int)x, start.pieces = units;
-                        start.j = (int)((int64_t)k.tiles * x / units);
-                        start.left = (int64_t)k.tiles * (x + 1) / units - start.j;
+                        start.j = (int)divide((int64_t)k.tiles * x, units);
+                        start.left = divide((int64_t)k.tiles * (x + 1), units) - start.j;
+                        start.first_unit = 0;
                     } else {
                         start.j = (int)max((int64_t)0, x - kOverhead);
-                        start.left = end - first - max((int64_t)0, kOverhead - x);
-                        start.first_unit = first - x + kOverhead;
+                        start.left = d.end - d.first - max((int64_t)0, kOverhead - x);
+                        start.first_unit = d.first - x + kOverhead;
                         start.piece = 0, start.pieces = 1;
                     }
                 }
@@ -340,9 +393,9 @@ struct Walk {
     Block block;
     int j, j_end;        // tiles
     int64_t left, first_unit;
+    __device__ __forceinline__ bool whole() const { return j == 0 && j_end == block.tiles; }
 };
 
-template <int KEYS>
 __device__ __forceinline__ bool begin_walk(const Start& s, Walk& w) {
     w.block = s.block, w.j = s.j, w.left = s.left, w.first_unit = s.first_unit;
     if (w.left <= 0) return false;
@@ -357,14 +410,17 @@ __device__ __forceinline__ bool next_block(const PrefillParams& p, const Divisio
     if (d.cut || w.left <= 0) return false;
     w.first_unit += w.block.tiles + kOverhead;
     Block& k = w.block;
-    if (++k.b >= blocks_of(p, k.rows)) {
+    if (++k.b * (int64_t)p.tokens_a_block >= k.rows) {
         k.b = 0;
-        if (++k.head >= p.pool.n_kv * p.head_tiles) {
-            k.head = 0;
-            do {
-                if (++k.r >= p.n_requests) return false;
-                enter_request<KEYS>(p, k);
-            } while (k.rows == 0);
+        if (++k.ht >= p.head_tiles) {
+            k.ht = 0;
+            if (++k.kv >= p.pool.n_kv) {
+                k.kv = 0;
+                do {
+                    if (++k.r >= p.n_requests) return false;
+                    enter_request(p, k);
+                } while (k.rows == 0);
+            }
         }
     }
     enter_block<KEYS>(p, k);
@@ -402,7 +458,8 @@ __device__ __forceinline__ void split(float a, float b, uint32_t& high, uint32_t
     h = __viaddmax_s16x2(h, 0xffffffffu, 0u);
     const float2 back = M::unpack(h);
     high = h;
-    low = M::pack(a - back.x, b - back.y);
+    const float2 rest = unpair(add2(pair(a, b), pair(-back.x, -back.y)));
+    low = M::pack(rest.x, rest.y);
 }
 
 // 16 elements of 8 bits as 16 of type T
@@ -439,13 +496,134 @@ __device__ __forceinline__ bool make_finite(uint4& x) {
     return a || b || c || d;
 }
 
+// ---------------------------------------------------------------------------------------------- the end of a block
+// What a row's thread needs to leave its output: 32 columns of tensor memory at a time, to the output or to a part.
+struct Row {
+    uint32_t at;       // tensor memory: O of the row
+    int row;           // of its tile
+    int64_t out;       // row of the output (token and head)
+    bool real;         // it is one
+    int kv, position, from;  // the kv head; the last seen key, the first of the window (counted without the gap)
+};
+
+template <class T>
+__device__ __forceinline__ void store_columns(const PrefillParams& p, int64_t out_row, int c, const float (&o)[32], float f, bool none) {
+    const int D = p.pool.head_dim;
+    char* const to = p.out + (out_row * D + c * 32) * 2;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (c * 32 + e * 8 < D)
+            *reinterpret_cast<uint4*>(to + e * 16) = none ? make_uint4(0, 0, 0, 0)
+                : make_uint4(T::pack(o[8 * e] * f, o[8 * e + 1] * f), T::pack(o[8 * e + 2] * f, o[8 * e + 3] * f),
+                             T::pack(o[8 * e + 4] * f, o[8 * e + 5] * f), T::pack(o[8 * e + 6] * f, o[8 * e + 7] * f));
+}
+
+template <class T>
+__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, float* part, float f, bool none) {
+#pragma unroll 1
+    for (int c = 0; c * 32 < p.pool.head_dim; c++) {
+        float o[32];
+        tmem_load(x.at + 32 * c, o);
+        wait_loads();
+        if (part) {
+#pragma unroll
+            for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + x.row] = o[e];
+        } else if (x.real)
+            store_columns<T>(p, x.out, c, o, f, none);
+    }
+}
+// The same where tiles that are not seen whole had infinite or NaN elements of v, which were left out of the products: those that this row
+// sees are added.  Tiles j0, j0 + step, .. of the block.
+template <class T, class C, int KEYS>
+__device__ __noinline__ void leave_with_infinite(const PrefillParams& p, const Row& x, const Block& k, int j0, int j1, int step, float* part, float f, bool none) {
+    const int D = p.pool.head_dim;
+#pragma unroll 1
+    for (int c = 0; c * 32 < D; c++) {
+        float o[32];
+        tmem_load(x.at + 32 * c, o);
+        wait_loads();
+        if (x.real)
+            for (int j = j0; j < j1; j += step) {
+                if (!partly_seen(p, k, j * KEYS, KEYS)) continue;
+                for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
+                    if (u > x.position || (u < x.from && u >= p.first)) continue;
+                    const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                    if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
+                    const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + x.kv * p.pool.stride_head + c * 32) * C::bytes;
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        if (c * 32 + 2 * e < D) {
+                            float2 y;
+                            if constexpr (C::bytes == 1) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
+                            else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
+                            if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
+                            if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
+                        }
+                }
+            }
+        if (part) {
+#pragma unroll
+            for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + x.row] = o[e];
+        } else if (x.real)
+            store_columns<T>(p, x.out, c, o, f, none);
+    }
+}
+
+// A row's log-sum-exp from the sum of its weights 2^(logit + add).
+__device__ __forceinline__ void leave_lse(const PrefillParams& p, int64_t out, float sum, float add) {
+    if (p.lse) p.lse[out] = sum == 0.0f ? -INFINITY : logf(sum) - add * 0.6931471805599453f;
+}
+
+// Parts of a row, `n` of them, in their order: the first at `first`, the others from `rest` on, `stride` floats apart.
+struct Parts {
+    const float *first, *rest;
+    int64_t stride;
+    int n;
+    __device__ __forceinline__ const float* at(int x) const { return x == 0 ? first : rest + (x - 1) * stride; }
+};
+// Adds up the parts of a block's tile: references, sums and outputs of each, a row a thread.  With `shared` a part is a pair of tiles' parts.
+template <class T, int DP>
+__device__ __noinline__ void join(const PrefillParams& p, const Row& row, const Parts& parts, bool shared, float vscale) {
+    constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
+    const int pairs = shared ? 2 : 1, n = parts.n * pairs;
+    auto part = [&](int x) { return shared ? parts.at(x >> 1) + (x & 1) * kPart : parts.at(x); };
+    float least = INFINITY;  // of add: the highest reference
+#pragma unroll 4
+    for (int x = 0; x < n; x++) least = fminf(least, __ldcg(part(x) + DP * 128 + row.row));
+    float all = 0;
+#pragma unroll 4
+    for (int x = 0; x < n; x++) {
+        const float a = __ldcg(part(x) + DP * 128 + row.row);
+        all += (a == INFINITY ? 0.0f : power2(least - a)) * __ldcg(part(x) + (DP + 1) * 128 + row.row);
+    }
+    const float f = all == 0.0f ? 0.0f : vscale / all;
+#pragma unroll 1
+    for (int c = 0; c * 32 < p.pool.head_dim; c++) {
+        float o[32] = {};
+#pragma unroll 1
+        for (int x = 0; x < n; x++) {
+            const float* const from = part(x);
+            const float a = __ldcg(from + DP * 128 + row.row);
+            if (__all_sync(~0u, a == INFINITY)) continue;  // (a part without a tile has no output)
+            const float y = a == INFINITY ? 0.0f : power2(least - a);
+            float z[32];
+#pragma unroll
+            for (int e = 0; e < 32; e++) z[e] = __ldcg(from + (c * 32 + e) * 128 + row.row);
+#pragma unroll
+            for (int e = 0; e < 32; e++) o[e] += y * z[e];
+        }
+        if (row.real) store_columns<T>(p, row.out, c, o, f, all == 0.0f);
+    }
+    if (row.real) leave_lse(p, row.out, all, least);
+}
+
 // ---------------------------------------------------------------------------------------------- the kernel
 template <class T, class C, int DP>
 __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill_kernel(const __grid_constant__ PrefillParams p) {
     using S = Shape<T, C, DP>;
     constexpr int kTiles = S::kTiles, kKeys = S::kKeys, kStages = S::kStages;
     constexpr bool kNarrow = C::bytes == 1;
-    constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+    constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f;
     constexpr int64_t kPatience = 4000000000ll;  // cycles that a wait may take: seconds, where microseconds are usual
     extern __shared__ char raw_smem[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 13];
@@ -465,46 +643,31 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     const uint32_t query_full = bar0 + (2 * kStages + 6) * 8, query_empty = query_full + 8, added = query_full + 16, drained = query_full + 24, both = query_full + 32;
     auto meeting = [&](int i) { return query_full + 40 + i * 8; };
 
-    // A wait that ends: false when the time is up, and then for every other wait of the CTA too.
+    // A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (bar_try(bar, parity)) return true;
+        bool done = bar_try(bar, parity);
+        if (__all_sync(~0u, done)) return true;
         const int64_t began = clock64();
-        while (!bar_try(bar, parity)) {
-            if (*(volatile int*)&stuck) return false;
+        while (!done && !(done = bar_try(bar, parity))) {
+            if (*(volatile int*)&stuck) break;
             if (clock64() - began > kPatience) {
                 *(volatile int*)&stuck = 1;
                 flag(p.status, FCSIM_KV_STUCK);
-                return false;
+                break;
             }
         }
-        return true;
+        return (bool)__all_sync(~0u, done);
     };
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; s++) bar_init(full(s), 32), bar_init(empty(s), 1);
+        for (int s = 0; s < kStages; s++) bar_init(full(s), 64), bar_init(empty(s), 1);
         for (int s = 0; s < 2; s++) bar_init(score_full(s), 1), bar_init(weights_ready(s), 128), bar_init(output_full(s), 1);
         bar_init(query_full, 32 * S::kLoadWarps), bar_init(query_empty, 1), bar_init(added, 1), bar_init(drained, 1);
         bar_init(both, 256), bar_init(meeting(0), 128), bar_init(meeting(1), 128);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         stuck = 0;
     }
-    // rows that belong to no request, and what is wrong with the requests
-    {
-        const int n0 = p.n_requests > 0 ? min(max(p.starts[0], 0), p.n_rows) : p.n_rows;
-        const int n1 = p.n_requests > 0 ? min(max(p.starts[p.n_requests], n0), p.n_rows) : p.n_rows;
-        const int64_t per_row = (int64_t)p.n_heads * (D / 8), none = ((int64_t)p.n_rows - n1 + n0) * per_row;
-        for (int64_t i = (int64_t)blockIdx.x * S::kThreads + tid; i < none; i += (int64_t)gridDim.x * S::kThreads)
-            reinterpret_cast<uint4*>(p.out)[i < n0 * per_row ? i : i + (n1 - n0) * per_row] = make_uint4(0, 0, 0, 0);
-        if (p.lse)
-            for (int64_t i = (int64_t)blockIdx.x * S::kThreads + tid; i < ((int64_t)p.n_rows - n1 + n0) * p.n_heads; i += (int64_t)gridDim.x * S::kThreads)
-                p.lse[i < (int64_t)n0 * p.n_heads ? i : i + (int64_t)(n1 - n0) * p.n_heads] = -INFINITY;
-        for (int r = blockIdx.x * S::kThreads + tid; r < p.n_requests; r += gridDim.x * S::kThreads) {
-            const int a = p.starts[r], b = p.starts[r + 1], n = p.lengths[r];
-            if (n < 0 || n > p.max_length || a < 0 || b < a || b > p.n_rows || b - a > n) flag(p.status, FCSIM_KV_BAD_LENGTH);
-        }
-    }
-    const Division work = plan<kKeys, S::kWarps>(p, start);
-    if (warp == 0) {
+    if (warp == S::kWarps - 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)), "r"(S::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -521,45 +684,46 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         clear(ring, kStages * kKeys, kKeys);
         fence_for_products();
     }
+    const Division work = plan<kKeys, S::kWarps>(p, start);
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = tmem_at;
 
     Walk w;
-    bool more = begin_walk<kKeys>(start, w);
+    bool more = begin_walk(start, w);
     const int heads_a_tile = p.heads_a_tile;
     auto tiles_in_use = [&](const Block& k) { return kTiles == 2 && k.tokens * heads_a_tile > 128 ? 2 : 1; };
+    // one tile of rows, of which the groups of warps take every other tile of keys
+    auto shared_block = [&](const Walk& w) { return kTiles == 2 && tiles_in_use(w.block) == 1 && (!w.whole() || w.j_end >= kSharedLeast); };
 
-    if (warp >= S::kSoftmaxWarps && warp < S::kSoftmaxWarps + S::kLoadWarps) {
+    if constexpr (kTiles == 2) {
+        if (warp >= S::kSoftmaxWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegisters));
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegisters));
+    }
+    if (warp >= S::kSoftmaxWarps && warp < S::kWarps - 1) {
         // ------------------------------------------------------------------------------------------ loads
-        // Tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own copies
-        // while the others' are on their way.
+        // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own
+        // copies while the others' are on their way.
         const int me = warp - S::kSoftmaxWarps;
-        constexpr int kLanes = DP * C::bytes / 16, kAtOnce = 32 / kLanes, kRounds = kKeys / kAtOnce;  // lanes of a row, rows at once
-        constexpr int kOffs = kKeys / 32, kBatch = kRounds < 16 ? kRounds : 16;
+        constexpr int kLanes = DP * C::bytes / 16, kAtOnce = 32 / kLanes, kHalf = kKeys / 2, kRounds = kHalf / kAtOnce;  // lanes of a row, rows at once
+        constexpr int kOffs = kHalf / 32, kBatch = kRounds < 8 ? kRounds : 8;
         const int chunk = lane % kLanes, lane_row = lane / kLanes, chunks = D * C::bytes / 16;
         const bool copies = chunk < chunks;
+        const uint32_t token_magic = (65536 + heads_a_tile - 1) / heads_a_tile;  // row / heads_a_tile for rows below 256
         int tile0 = 0, step0 = 0, segment = 0;  // tiles and steps of the segments before this one
-        bool query_waits = false;               // copies of Q that are not yet told of
-        auto tell_query = [&]() {
-            if (!query_waits) return;
-            fence_for_products();
-            bar_arrive(query_full);
-            query_waits = false;
-        };
-        int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the tile that is loaded next, or -1
+        int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
         uint32_t next_bad = 0;     // which of them are in a page outside the pool
-        auto fetch_pages = [&](const Block& k, int j) {
+        auto fetch_pages = [&](const Block& k, int j, int half) {
             next_bad = 0;
 #pragma unroll
             for (int c = 0; c < kOffs; c++) {
-                const int u = j * kKeys + c * 32 + lane;
+                const int u = j * kKeys + half * kHalf + c * 32 + lane;
                 next_off[c] = -1;
                 if (u < k.seen) {
                     const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
                     if ((unsigned)page < (unsigned)p.pool.n_pages)
-                        next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.head / p.head_tiles * p.pool.stride_head) * C::bytes;
+                        next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
                     else
                         next_bad |= 1u << c;
                 }
@@ -571,38 +735,14 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         while (more && fine) {
             const Block& k = w.block;
             const int steps = w.j_end - w.j;
-            // tile x of the segment: which it is (with one tile of rows the scores run a step ahead)
-            auto is_key = [&](int x) { return kTiles == 2 ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
-            auto step_of = [&](int x) { return kTiles == 2 || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
-            int x = (me + S::kLoadWarps - tile0 % S::kLoadWarps) % S::kLoadWarps;  // this warp's first
-            if (x < 2 * steps) fetch_pages(k, w.j + step_of(x));
-            if (lane == 0) infinite[segment & 3][me] = 0;
-            // this warp's share of the rows of Q
-            if (segment > 0 && !wait(query_empty, (segment - 1) & 1)) break;
-            {
-                constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
-                const int at = lane % kQueryLanes, head0 = k.head / p.head_tiles * group, part0 = k.head % p.head_tiles * heads_a_tile;
-                const int part = min(heads_a_tile, group - part0);
-                for (int r0 = me * 32; r0 < tiles_in_use(k) * 128; r0 += 32 * S::kLoadWarps) {
-                    const int row = r0 + lane, token = row / heads_a_tile, g = row - token * heads_a_tile;
-                    int64_t off = -1;
-                    if (token < k.tokens && g < part)
-                        off = ((int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.q_row + (int64_t)(head0 + part0 + g) * p.q_head) * 2;
-#pragma unroll
-                    for (int i = 0; i < 32 / kQueryRows; i++) {
-                        const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
-                        const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                        if (at < D / 8)
-                            copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
-                                   p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
-                    }
-                }
-                commit_copies();
-                query_waits = true;
-            }
-            for (; x < 2 * steps; x += S::kLoadWarps) {
-                const int tile = tile0 + x, s = tile % kStages, j = w.j + step_of(x);
-                const bool key = is_key(x), edge = !key && partly_seen(p, k, j * kKeys, kKeys);
+            // tile x of the segment: with two tiles of rows K and V of a step, then of the next; with one, the scores run a step ahead
+            const bool ahead = kTiles == 1 || shared_block(w);
+            auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
+            auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
+            // copies of half h of the segment (8-bit rows: all of it)
+            auto begin_half = [&](int h) {
+                const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = w.j + step_of(x);
+                const bool key = is_key(x);
                 const char* const pool = key ? p.pool.k : p.pool.v;
                 int64_t off[kOffs];
 #pragma unroll
@@ -611,41 +751,40 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     if (key) {
                         const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
                         if (lane == 0) {
-                            valid[(step0 + step_of(x)) & 7][c] = ~bad;  // (what lies behind the last token is no row's)
+                            valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
                             if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
                         }
                     }
                 }
-                if (x + S::kLoadWarps < 2 * steps) fetch_pages(k, w.j + step_of(x + S::kLoadWarps));
-                if (tile >= kStages && !bar_try(empty(s), (tile / kStages - 1) & 1)) {
-                    if (query_waits) {
-                        wait_copies<0>();
-                        tell_query();
-                    }
-                    if (!(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
-                }
-                const uint32_t to = ring + s * S::kStage;
-                bool found = false;
+                if (h + S::kLoadWarps < 4 * steps) fetch_pages(k, w.j + step_of((h + S::kLoadWarps) / 2), (h + S::kLoadWarps) % 2);
+                if (tile >= kStages && !wait(empty(s), (tile / kStages - 1) & 1)) return false;
+                const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
                 if constexpr (kNarrow) {
+                    const bool edge = !key && partly_seen(p, k, j * kKeys, kKeys);
+                    bool found = false;
 #pragma unroll 1
                     for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
                         uint4 raw[kBatch];
+                        const int row0 = i0 * kAtOnce + lane_row;
+                        constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
+                        int64_t mine[kHere];
+#pragma unroll
+                        for (int y = 0; y < kHere; y++) {
+                            mine[y] = off[y];
+#pragma unroll
+                            for (int c = 1; c < kOffs; c++)
+                                if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
+                        }
 #pragma unroll
                         for (int i = 0; i < kBatch; i++) {
-                            const int row = (i0 + i) * kAtOnce + lane_row;
-                            int64_t o = __shfl_sync(~0u, off[0], row % 32);
-#pragma unroll
-                            for (int c = 1; c < kOffs; c++) {
-                                const int64_t other = __shfl_sync(~0u, off[c], row % 32);
-                                if (row / 32 == c) o = other;
-                            }
+                            const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
                             raw[i] = make_uint4(0, 0, 0, 0);
                             if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
                         }
                         if (copies) {
 #pragma unroll
                             for (int i = 0; i < kBatch; i++) {
-                                const int row = (i0 + i) * kAtOnce + lane_row;
+                                const int row = row0 + i * kAtOnce;
                                 uint4 a, b;
                                 widen<T>(raw[i], a, b);
                                 if (edge) found |= make_finite<T>(a) | make_finite<T>(b);
@@ -654,146 +793,228 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                             }
                         }
                     }
-                    if (query_waits) {
-                        wait_copies<0>();
-                        tell_query();
-                    }
+                    if (__any_sync(~0u, found) && lane == 0) infinite[segment & 3][me] = 1;
+                    fence_for_products();
+                    bar_arrive(full(s));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kRounds; i++) {
-                        const int row = i * kAtOnce + lane_row;
-                        const int64_t o = __shfl_sync(~0u, off[i * kAtOnce / 32], row % 32);
-                        if (copies) copy16(to + place(row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
-                    }
-                    commit_copies();
-                    if (query_waits) {
-                        wait_copies<1>();
-                        tell_query();
-                    }
-                    wait_copies<0>();
-                    if (edge && copies) {
-                        // what some row does not see must not meet its weight of zero as an infinity or NaN
-#pragma unroll 4
-                        for (int i = 0; i < kRounds; i++) {
-                            const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
-                            uint4 y = load16(at);
-                            if (make_finite<T>(y)) {
-                                store16(at, y);
-                                found = true;
-                            }
+                    for (int c = 0; c < kOffs; c++) {
+#pragma unroll 8
+                        for (int i = 0; i < kRounds / kOffs; i++) {
+                            const int row = i * kAtOnce + lane_row;
+                            const int64_t o = __shfl_sync(~0u, off[c], row);
+                            if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
                         }
                     }
+                    commit_copies();
                 }
-                if (__any_sync(~0u, found) && lane == 0) infinite[segment & 3][me] = 1;
-                fence_for_products();
-                bar_arrive(full(s));
+                return true;
+            };
+            auto end_half = [&](int h) {  // its copies have arrived
+                if constexpr (!kNarrow) {
+                    const int x = h / 2, s = (tile0 + x) % kStages, j = w.j + step_of(x);
+                    if (!is_key(x) && partly_seen(p, k, j * kKeys, kKeys)) {
+                        // what some row does not see must not meet its weight of zero as an infinity or NaN
+                        bool found = false;
+                        if (copies) {
+#pragma unroll 8
+                            for (int i = 0; i < kRounds; i++) {
+                                const uint32_t at = ring + s * S::kStage + h % 2 * kHalf * 128 + place(i * kAtOnce + lane_row, chunk);
+                                uint4 y = load16(at);
+                                if (make_finite<T>(y)) {
+                                    store16(at, y);
+                                    found = true;
+                                }
+                            }
+                        }
+                        if (__any_sync(~0u, found) && lane == 0) infinite[segment & 3][me] = 1;
+                    }
+                    fence_for_products();
+                    bar_arrive(full(s));
+                }
+            };
+            int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps;  // this warp's first
+            if (h < 4 * steps) fetch_pages(k, w.j + step_of(h / 2), h % 2);
+            if (lane == 0) infinite[segment & 3][me] = 0;
+            // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
+            // are left by tiles of blocks before.)
+            const bool early = h < 4;
+            if (early && !(fine = begin_half(h))) break;
+            if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
+            {
+                constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
+                const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
+                for (int r0 = me * 16; r0 < tiles_in_use(k) * 128; r0 += 16 * S::kLoadWarps) {
+                    const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
+                    int64_t off = -1;
+                    if (token < k.tokens && g < part)
+                        off = ((int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
+#pragma unroll
+                    for (int i = 0; i < 16 / kQueryRows; i++) {
+                        const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
+                        const int y = r0 + i * kQueryRows + lane / kQueryLanes;
+                        if (at < D / 8)
+                            copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
+                                   p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
+                    }
+                }
+                commit_copies();
             }
-            if (query_waits) {
+            if (early) {
+                wait_copies<1>();
+                end_half(h);
+                h += S::kLoadWarps;
+            }
+            wait_copies<0>();
+            fence_for_products();
+            bar_arrive(query_full);
+            for (; h < 4 * steps; h += S::kLoadWarps) {
+                if (!(fine = begin_half(h))) break;
                 wait_copies<0>();
-                tell_query();
+                end_half(h);
             }
             tile0 += 2 * steps, step0 += steps, segment++;
             more = next_block<kKeys>(p, work, w);
         }
         wait_copies<0>();
-    } else if (warp == S::kSoftmaxWarps + S::kLoadWarps) {
+    } else if (warp == S::kWarps - 1) {
         // ------------------------------------------------------------------------------------------ products
-        if (lane == 0) {
-            constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
-            const uint32_t how_score = instruction(kType, false, 128, kKeys), how_output = instruction(kType, true, 128, (D + 15) / 16 * 16);
-            const int depth = (D + 15) / 16;
-            int tile = 0, segment = 0, step = 0;
-            uint32_t ready[2] = {0, 0};  // parities of the weights
-            auto score = [&](int slot, int i, int s) {  // S of row tile i, with K in stage s
-                const uint64_t a = operand(query + i * (128 * DP * 2), 16, 1024), b = operand(ring + s * S::kStage, 16, 1024);
-                for (int k = 0; k < depth; k++)
-                    product(tmem + S::kScore + slot * kKeys, a + ((k / 4 * (128 * 128) + k % 4 * 32) >> 4), b + ((k / 4 * (kKeys * 128) + k % 4 * 32) >> 4),
-                            how_score, k > 0);
+        constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
+        const uint32_t depth = uni((D + 15) / 16), base = uni(tmem), how_score = instruction(kType, false, 128, kKeys);
+        const uint32_t how_output = instruction(kType, true, 128, depth * 16);
+        const uint64_t query_operand = operand(uni(query), 16, 1024), key_operand = operand(uni(ring), 16, 1024), value_operand = operand(uni(ring), kKeys * 128, 1024);
+        int tile = 0, segment = 0;
+        uint32_t ready[2] = {0, 0};  // parities of the weights
+        auto score = [&](int slot, int i, int t) {  // S of row tile i, with K in tile t of the ring
+            const uint32_t s = uni(t % kStages);
+            const uint64_t a = query_operand + i * (128 * DP * 2 >> 4), b = key_operand + s * (S::kStage >> 4);
+            if (elected()) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; k++)
+                    if (k < depth)
+                        product(base + S::kScore + slot * kKeys, a + ((k / 4 * (128 * 128) + k % 4 * 32) >> 4), b + ((k / 4 * (kKeys * 128) + k % 4 * 32) >> 4),
+                                how_score, k > 0);
                 commit_products(score_full(slot));
-            };
-            auto output = [&](int slot, int i, int s, bool add) {  // O of row tile i, with V in stage s
-                const uint64_t b = operand(ring + s * S::kStage, kKeys * 128, 1024);
-                const uint32_t to = tmem + S::kOutput + i * DP, from = tmem + S::kScore + slot * kKeys;
+            }
+        };
+        auto output = [&](int slot, int i, int t, bool add) {  // O of tile i, with V in tile t of the ring
+            const uint32_t s = uni(t % kStages), more_of = uni(add);
+            const uint64_t b = value_operand + s * (S::kStage >> 4);
+            const uint32_t to = base + S::kOutput + i * DP, from = base + S::kScore + slot * kKeys;
+            if (elected()) {
 #pragma unroll
                 for (int part = 0; part < 2; part++)
 #pragma unroll
                     for (int k = 0; k < kKeys / 16; k++)
-                        product_from_tmem(to, from + k / 2 * 32 + part * 16 + k % 2 * 8, b + (k * 2048 >> 4), how_output, add || part > 0 || k > 0);
-            };
-            auto wait_full = [&](int t) {
-                if (!wait(full(t % kStages), (t / kStages) & 1)) return false;
-                fence_after_sync();
-                return true;
-            };
-            bool fine = true;
-            while (more && fine) {
-                const int n = tiles_in_use(w.block), steps = w.j_end - w.j;
-                fine = wait(query_full, segment & 1) && wait_full(tile);
-                if (!fine) break;
-                for (int i = 0; i < n; i++) score(kTiles == 2 ? i : step & 1, i, tile % kStages);
-                commit_products(empty(tile % kStages));
-                tile++;
-                if (steps == 1) commit_products(query_empty);
-                for (int j = 0; j < steps && fine; j++) {
-                    const bool another = j + 1 < steps;
-                    if constexpr (kTiles == 1) {
-                        // the next step's scores, then this one's output
-                        if (another) {
-                            if (!(fine = wait_full(tile))) break;
-                            score((step + 1) & 1, 0, tile % kStages);
-                            commit_products(empty(tile % kStages));
-                            tile++;
-                            if (j + 2 == steps) commit_products(query_empty);
-                        }
-                        const int slot = step & 1;
-                        fine = wait_full(tile) && wait(weights_ready(slot), ready[slot]);
-                        if (!fine) break;
-                        ready[slot] ^= 1;
-                        fence_after_sync();
-                        output(slot, 0, tile % kStages, j > 0);
-                        commit_products(empty(tile % kStages));
-                        commit_products(added);
-                        if (!another) commit_products(output_full(0));
-                        tile++;
-                    } else {
-                        // tile after tile: the output of this step, then the scores of the next
-                        const int v = tile, k = tile + 1;
-                        fine = wait_full(v);
-                        for (int i = 0; i < n && fine; i++) {
-                            if (!(fine = wait(weights_ready(i), ready[i]))) break;
-                            ready[i] ^= 1;
-                            fence_after_sync();
-                            output(i, i, v % kStages, j > 0);
-                            if (i == n - 1) commit_products(empty(v % kStages));
-                            if (another) {
-                                if (i == 0 && !(fine = wait_full(k))) break;
-                                score(i, i, k % kStages);
-                                if (i == n - 1) {
-                                    commit_products(empty(k % kStages));
-                                    if (j + 2 == steps) commit_products(query_empty);
-                                }
-                            } else
-                                commit_products(output_full(i));
-                        }
-                        tile += another ? 2 : 1;
-                    }
-                    step++;
-                }
-                segment++;
-                more = next_block<kKeys>(p, work, w);
+                        product_from_tmem(to, from + k / 2 * 32 + part * 16 + k % 2 * 8, b + (k * 2048 >> 4), how_output, part > 0 || k > 0 ? 1u : more_of);
             }
-            commit_products(drained);  // nothing is in flight when the CTA ends
-            const int64_t began = clock64();
-            while (!bar_try(drained, 0) && clock64() - began < kPatience) {}
+        };
+        auto told = [&](uint32_t bar) {  // all products so far
+            if (elected()) commit_products(bar);
+        };
+        auto wait_full = [&](int t) {
+            if (!wait(full(t % kStages), (t / kStages) & 1)) return false;
+            fence_after_sync();
+            return true;
+        };
+        auto wait_weights = [&](int slot) {
+            if (!wait(weights_ready(slot), ready[slot])) return false;
+            ready[slot] ^= 1;
+            fence_after_sync();
+            return true;
+        };
+        bool fine = true;
+        while (more && fine) {
+            const int n = tiles_in_use(w.block), steps = w.j_end - w.j;
+            const bool shared = shared_block(w);
+            if (!(fine = wait(query_full, segment & 1) && wait_full(tile))) break;
+            if (kTiles == 1 || shared) {
+                // scores run a step ahead, in the two areas in turn: K0 K1 V0 K2 V1 ..
+                score(0, 0, tile);
+                told(empty(tile % kStages));
+                tile++;
+                if (steps > 1) {
+                    if (!(fine = wait_full(tile))) break;
+                    score(1, 0, tile);
+                    told(empty(tile % kStages));
+                    tile++;
+                }
+                if (steps <= 2) told(query_empty);
+                for (int j = 0; j < steps && fine; j++) {
+                    const int slot = j & 1;
+                    if (!(fine = wait_full(tile) && wait_weights(slot))) break;
+                    output(slot, kTiles == 1 ? 0 : slot, tile, j >= (kTiles == 1 ? 1 : 2));
+                    told(empty(tile % kStages));
+                    if (kTiles == 1) told(added);
+                    tile++;
+                    if (j + 2 < steps) {
+                        if (!(fine = wait_full(tile))) break;
+                        score(slot, 0, tile);
+                        told(empty(tile % kStages));
+                        if (j + 3 == steps) told(query_empty);
+                        tile++;
+                    }
+                    if (kTiles == 1 ? j + 1 == steps : j + 2 >= steps) told(output_full(kTiles == 1 ? 0 : slot));
+                }
+            } else {
+                for (int i = 0; i < n; i++) score(i, i, tile);
+                told(empty(tile % kStages));
+                if (steps == 1) told(query_empty);
+                tile++;
+                for (int j = 0; j < steps && fine; j++) {
+                    // tile after tile: the output of this step, then the scores of the next
+                    const bool another = j + 1 < steps;
+                    if (!(fine = wait_full(tile))) break;
+                    for (int i = 0; i < n; i++) {
+                        if (!(fine = wait_weights(i))) break;
+                        output(i, i, tile, j > 0);
+                        if (i == n - 1) told(empty(tile % kStages));
+                        if (another) {
+                            if (i == 0 && !(fine = wait_full(tile + 1))) break;
+                            score(i, i, tile + 1);
+                            if (i == n - 1) {
+                                told(empty((tile + 1) % kStages));
+                                if (j + 2 == steps) told(query_empty);
+                            }
+                        } else
+                            told(output_full(i));
+                    }
+                    tile += another ? 2 : 1;
+                }
+            }
+            segment++;
+            more = next_block<kKeys>(p, work, w);
         }
-        __syncwarp();
-    } else if (warp < S::kSoftmaxWarps) {
+        told(drained);  // nothing is in flight when the CTA ends
+        const int64_t began = clock64();
+        while (!bar_try(drained, 0) && clock64() - began < kPatience) {}
+    } else {
         // ------------------------------------------------------------------------------------------ softmax
-        const int i = warp >> 2, row = tid & 127;  // tile; its row
+        // rows that belong to no request, and what is wrong with the requests
+        {
+            constexpr int kHere = 32 * S::kSoftmaxWarps;
+            const int n0 = p.n_requests > 0 ? min(max(p.starts[0], 0), p.n_rows) : p.n_rows;
+            const int n1 = p.n_requests > 0 ? min(max(p.starts[p.n_requests], n0), p.n_rows) : p.n_rows, none = p.n_rows - n1 + n0;
+            if (none > 0) {
+                const int64_t per_row = (int64_t)p.n_heads * (D / 8);
+                for (int64_t i = (int64_t)blockIdx.x * kHere + tid; i < none * per_row; i += (int64_t)gridDim.x * kHere)
+                    reinterpret_cast<uint4*>(p.out)[i < n0 * per_row ? i : i + (n1 - n0) * per_row] = make_uint4(0, 0, 0, 0);
+                if (p.lse)
+                    for (int64_t i = (int64_t)blockIdx.x * kHere + tid; i < (int64_t)none * p.n_heads; i += (int64_t)gridDim.x * kHere)
+                        p.lse[i < (int64_t)n0 * p.n_heads ? i : i + (int64_t)(n1 - n0) * p.n_heads] = -INFINITY;
+            }
+            for (int r = blockIdx.x * kHere + tid; r < p.n_requests; r += gridDim.x * kHere) {
+                const int a = p.starts[r], b = p.starts[r + 1], n = p.lengths[r];
+                if (n < 0 || n > p.max_length || a < 0 || b < a || b > p.n_rows || b - a > n) flag(p.status, FCSIM_KV_BAD_LENGTH);
+            }
+        }
+        const int i = warp >> 2;  // tile
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's lanes of tensor memory: 32 (warp % 4) << 16
-        const uint32_t mine = tmem + S::kOutput + i * DP + lanes;
-        const int token = (i * 128 + row) / heads_a_tile, g = i * 128 + row - token * heads_a_tile;
-        int step = 0, segment = 0, before_tiles = 0;
+        Row x;
+        x.row = tid & 127;
+        x.at = tmem + S::kOutput + i * DP + lanes;
+        int step0 = 0, segment = 0;
+        bool was_here = false;
         uint32_t score_parity[2] = {0, 0}, output_parity = 0, both_parity = 0, meeting_parity = 0;
         bool fine = true;
         auto meet = [&](uint32_t bar, uint32_t& parity) {
@@ -805,230 +1026,191 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         while (more && fine) {
             const Block& k = w.block;
             const int n = tiles_in_use(k), steps = w.j_end - w.j;
+            const bool shared = shared_block(w), whole = w.whole();
             if (kTiles == 2) {
-                // (a group that sits out does not run ahead of one that is at work: flags of a few segments are kept)
-                if (before_tiles == 2 && n == 1 && !meet(both, both_parity)) break;
-                before_tiles = n;
-                if (i >= n) {
-                    step += steps, segment++;
-                    more = next_block<kKeys>(p, work, w);
-                    continue;
-                }
+                // (the second group does not fall behind while it is not needed: flags of a few segments are kept)
+                const bool here = n == 2 || (shared && steps > 1);
+                if (was_here && !here && !meet(both, both_parity)) break;
+                was_here = here;
             }
-            const int kv = k.head / p.head_tiles, head = k.head % p.head_tiles * heads_a_tile + g;
-            const bool real = token < k.tokens && head < group && g < heads_a_tile;
-            const float unit = (kNarrow ? p.scale * p.pool.k_scale[kv] : p.scale) * kLog2e;
+            const int row = (kTiles == 1 || shared ? 0 : i * 128) + x.row, token = (uint32_t)row / (uint32_t)heads_a_tile, g = row - token * heads_a_tile;
+            const int head = k.ht * heads_a_tile + g;
+            x.real = token < k.tokens && head < group;
+            x.kv = k.kv;
+            x.out = (int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.n_heads + k.kv * group + head;
+            const float unit = (kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale) * kLog2e;
             const bool turned = unit < 0;
             // the last seen key of this row and the first of its window; nothing for rows that are none
             const int position = k.position0 + k.b * p.tokens_a_block + token - k.gap;
-            const int last = real ? position : -1, from = p.window > 0 && position >= p.window ? position - p.window + 1 : 0;
+            x.position = x.real ? position : -1, x.from = p.window > 0 && position >= p.window ? position - p.window + 1 : 0;
             float add = INFINITY, limit = -INFINITY, sum = 0;  // weights are 2^(unit s + add); add is infinite until there is a finite logit
-            for (int j = w.j; j < w.j_end; j++, step++) {
-                const int slot = kTiles == 2 ? i : step & 1, base = j * kKeys;
+            const int step_first = shared ? i : kTiles == 2 && i >= n ? steps : 0, step_by = shared ? 2 : 1;
+            for (int t = step_first; t < steps; t += step_by) {
+                const int slot = kTiles == 2 ? i : t & 1, tile_base = (w.j + t) * kKeys, flags = (step0 + t) & 7;
                 const uint32_t at = tmem + S::kScore + slot * kKeys + lanes;
                 if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
                 score_parity[slot] ^= 1;
                 fence_after_sync();
                 uint32_t there = ~0u;
 #pragma unroll
-                for (int c = 0; c < kKeys / 32; c++) there &= valid[step & 7][c];
-                const bool masked = there != ~0u || partly_seen(p, k, base, kKeys);
-                uint32_t mask[kKeys / 32];
-                if (masked) {
-#pragma unroll
-                    for (int c = 0; c < kKeys / 32; c++)
-                        mask[c] = lowest(last + 1 - base - 32 * c) & (~lowest(from - base - 32 * c) | lowest(p.first - base - 32 * c)) & valid[step & 7][c];
-                }
+                for (int c = 0; c < kKeys / 32; c++) there &= valid[flags][c];
+                const bool masked = there != ~0u || partly_seen(p, k, tile_base, kKeys);
+                auto mask_of = [&](int c) {  // of 32 keys
+                    const int b = tile_base + 32 * c;
+                    return lowest(x.position + 1 - b) & (~lowest(x.from - b) | lowest(p.first - b)) & valid[flags][c];
+                };
                 // the largest logit (with a negative scale: the lowest)
                 const float none = turned ? INFINITY : -INFINITY;
                 float top = none;
-#pragma unroll
-                for (int c = 0; c < kKeys / 32; c++) {
-                    float s[32];
-                    tmem_load(at + 32 * c, s);
+#pragma unroll 1
+                for (int c = 0; c < kKeys / 32; c += 2) {
+                    float s[2][32];
+                    tmem_load(at + 32 * c, s[0]);
+                    tmem_load(at + 32 * c + 32, s[1]);
                     wait_loads();
                     if (masked) {
+                        const uint32_t mask[2] = {mask_of(c), mask_of(c + 1)};
 #pragma unroll
-                        for (int e = 0; e < 32; e++) s[e] = mask[c] >> e & 1 ? s[e] : none;
+                        for (int e = 0; e < 64; e++) s[e / 32][e % 32] = mask[e / 32] >> e % 32 & 1 ? s[e / 32][e % 32] : none;
                     }
+                    float tops[4] = {top, none, none, none};
                     if (turned) {
 #pragma unroll
-                        for (int e = 0; e < 32; e++) top = fminf(top, s[e]);
+                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fminf(fminf(tops[e / 2 % 4], s[e / 32][e % 32]), s[e / 32][e % 32 + 1]);
+                        top = fminf(fminf(tops[0], tops[1]), fminf(tops[2], tops[3]));
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 32; e++) top = fmaxf(top, s[e]);
+                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fmaxf(fmaxf(tops[e / 2 % 4], s[e / 32][e % 32]), s[e / 32][e % 32 + 1]);
+                        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     }
                 }
                 const float most = top == none ? -INFINITY : top * unit;
                 // The reference moves only when a logit is 2^kLag above it, so that the output is seldom taken through registers.
-                bool moves = most > limit;
+                const bool moves = most > limit;
                 float shrink = 1;
                 if (moves) {
-                    const bool first_one = limit == -INFINITY;
                     const float now = kRaise - most;
-                    shrink = first_one ? 0.0f : power2(now - add);
+                    shrink = limit == -INFINITY ? 0.0f : power2(now - add);
                     add = now;
                     limit = most + kLag;
                     sum *= shrink;
                 }
-                if (j > w.j && __any_sync(~0u, moves)) {
-                    if (kTiles == 1 && !(fine = wait(added, (step - 1) & 1))) break;
+                if (t > step_first && __any_sync(~0u, moves)) {
+                    if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
                     fence_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c * 32 < D; c++) {
+                        float o[32];
+                        uint32_t y[32];
+                        tmem_load(x.at + 32 * c, o);
+                        wait_loads();
 #pragma unroll
-                    for (int c = 0; c < DP / 32; c++)
-                        if (c * 32 < D) {
-                            float o[32];
-                            uint32_t x[32];
-                            tmem_load(mine + 32 * c, o);
-                            wait_loads();
-#pragma unroll
-                            for (int e = 0; e < 32; e++) x[e] = __float_as_uint(o[e] * shrink);
-                            tmem_store(mine + 32 * c, x);
-                        }
+                        for (int e = 0; e < 32; e++) y[e] = __float_as_uint(o[e] * shrink);
+                        tmem_store(x.at + 32 * c, y);
+                    }
                 }
                 const float plus = limit == -INFINITY ? 0.0f : add;
-                float sums[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < kKeys / 32; c++) {
-                    float s[32];
-                    uint32_t x[32];
-                    tmem_load(at + 32 * c, s);
+                const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
+                uint64_t sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll 1
+                for (int c = 0; c < kKeys / 32; c += 2) {
+                    float s[2][32];
+                    tmem_load(at + 32 * c, s[0]);
+                    tmem_load(at + 32 * c + 32, s[1]);
                     wait_loads();
 #pragma unroll
-                    for (int e = 0; e < 32; e++) {
-                        s[e] = power2(fmaf(s[e], unit, plus));
+                    for (int h = 0; h < 2; h++) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float2 y = unpair(fma2(pair(s[h][e], s[h][e + 1]), unit2, plus2));
+                            s[h][e] = power2(y.x), s[h][e + 1] = power2(y.y);
+                        }
+                        if (masked) {
+                            const uint32_t mask = mask_of(c + h);
+#pragma unroll
+                            for (int e = 0; e < 32; e++) s[h][e] = mask >> e & 1 ? s[h][e] : 0.0f;
+                        }
+                        uint32_t y[32];
+#pragma unroll
+                        for (int e = 0; e < 16; e++) {
+                            sums[e & 1] = add2(sums[e & 1], pair(s[h][2 * e], s[h][2 * e + 1]));
+                            split<T>(s[h][2 * e], s[h][2 * e + 1], y[e], y[16 + e]);
+                        }
+                        tmem_store(at + 32 * (c + h), y);
                     }
-                    if (masked) {
-#pragma unroll
-                        for (int e = 0; e < 32; e++) s[e] = mask[c] >> e & 1 ? s[e] : 0.0f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; e++) sums[e & 3] += s[e];
-#pragma unroll
-                    for (int e = 0; e < 16; e++) split<T>(s[2 * e], s[2 * e + 1], x[e], x[16 + e]);
-                    tmem_store(at + 32 * c, x);
                 }
-                sum += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                {
+                    const float2 y = unpair(add2(sums[0], sums[1]));
+                    sum += y.x + y.y;
+                }
                 wait_stores();
                 fence_before_sync();
                 bar_arrive(weights_ready(slot));
             }
             if (!fine) break;
             // -------------------------------------------------------------- end of this CTA's part of a block
-            if (!(fine = wait(output_full(i), output_parity))) break;
-            output_parity ^= 1;
-            fence_after_sync();
-            bool poisoned = false;
+            const bool worked = step_first < steps, has_part = !whole || shared;
+            if (worked || (shared && has_part)) {
+                bool poisoned = false;
+                if (worked) {
+                    if (!(fine = wait(output_full(i), output_parity))) break;
+                    output_parity ^= 1;
+                    fence_after_sync();
 #pragma unroll
-            for (int x = 0; x < S::kLoadWarps; x++) poisoned |= infinite[segment & 3][x] != 0;
-            int first_part = blockIdx.x, final_part = blockIdx.x;  // CTAs that have parts of the block
-            if (work.cut) {
-                first_part -= start.piece;
-                final_part = first_part + start.pieces - 1;
-            } else {
-                first_part = (int)(w.first_unit / work.share);
-                final_part = (int)((w.first_unit + k.tiles - 1) / work.share);
-            }
-            const bool whole = first_part == final_part;
-            constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
-            auto part_of = [&](int cta) { return p.parts + ((2 * (int64_t)cta + (cta == first_part ? 1 : 0)) * kTiles + i) * kPart; };
-            const int64_t out_row = (int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.n_heads + kv * group + head;
-            const float vscale = kNarrow ? p.pool.v_scale[kv] : 1.0f;
-            auto store_row = [&](const float (&o)[32], int c, float f, bool none) {  // elements 32 c ..
-                char* const to = p.out + (out_row * D + c * 32) * 2;
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (c * 32 + e * 8 < D)
-                        *reinterpret_cast<uint4*>(to + e * 16) = none ? make_uint4(0, 0, 0, 0)
-                            : make_uint4(T::pack(o[8 * e] * f, o[8 * e + 1] * f), T::pack(o[8 * e + 2] * f, o[8 * e + 3] * f),
-                                         T::pack(o[8 * e + 4] * f, o[8 * e + 5] * f), T::pack(o[8 * e + 6] * f, o[8 * e + 7] * f));
-            };
-            auto finish = [&](float all, float plus) {
-                if (p.lse) p.lse[out_row] = all == 0.0f ? -INFINITY : logf(all) - plus * kLn2;
-            };
-            float* const part = part_of(blockIdx.x);
-            const float f = sum == 0.0f ? 0.0f : vscale / sum;
-#pragma unroll 1
-            for (int c = 0; c < DP / 32; c++) {
-                if (c * 32 >= D) break;
-                float o[32];
-                tmem_load(mine + 32 * c, o);
-                wait_loads();
-                if (poisoned && real) {
-                    // infinite and NaN elements of v in tiles that are not seen whole were left out of the products: those this row sees
-                    for (int j = w.j; j < w.j_end; j++) {
-                        if (!partly_seen(p, k, j * kKeys, kKeys)) continue;
-                        for (int u = j * kKeys; u < min(k.seen, (j + 1) * kKeys); u++) {
-                            if (u > position || (u < from && u >= p.first)) continue;
-                            const int t = u + (u >= p.first ? k.gap : 0), x = page_of(p.pool, t), page = p.table[k.r * p.table_row + x];
-                            if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
-                            const char* const v = p.pool.v + (page * p.pool.stride_page + (t - x * p.pool.page_size) * p.pool.stride_slot + kv * p.pool.stride_head + c * 32) * C::bytes;
-#pragma unroll
-                            for (int e = 0; e < 16; e++)
-                                if (c * 32 + 2 * e < D) {
-                                    float2 y;
-                                    if constexpr (kNarrow) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
-                                    else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
-                                    if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
-                                    if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
-                                }
-                        }
-                    }
+                    for (int y = 0; y < S::kLoadWarps; y++) poisoned |= infinite[segment & 3][y] != 0;
                 }
+                constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
+                const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
+                // CTAs that have parts of the block; this one's: the first of its two, unless the block begins here
+                int first_part = blockIdx.x, final_part = blockIdx.x;
                 if (!whole) {
-#pragma unroll
-                    for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + row] = o[e];
-                } else if (real)
-                    store_row(o, c, f, sum == 0.0f);
-            }
-            fence_before_sync();
-            if (whole) {
-                if (real) finish(sum, add);
-            } else {
-                part[DP * 128 + row] = add;
-                part[(DP + 1) * 128 + row] = sum;
-                __threadfence();
-                if (!(fine = meet(meeting(i), meeting_parity))) break;
-                if (row == 0) {
-                    int* const counter = p.counters + first_part * 2 + i;
-                    const bool last_one = atomicAdd(counter, 1) == final_part - first_part;
-                    joins[i] = last_one;
-                    if (last_one) *counter = 0;
+                    if (work.cut) {
+                        first_part -= start.piece;
+                        final_part = first_part + start.pieces - 1;
+                    } else {
+                        if (w.first_unit < work.first) first_part = (int)divide(w.first_unit, work.share);
+                        if (w.first_unit + k.tiles > work.end) final_part = (int)divide(w.first_unit + k.tiles - 1, work.share);
+                    }
                 }
-                if (!(fine = meet(meeting(i), meeting_parity))) break;
-                if (joins[i]) {
+                float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
+                if (worked) {
+                    if (poisoned) leave_with_infinite<T, C, kKeys>(p, x, k, w.j + step_first, w.j_end, step_by, part, f, sum == 0.0f);
+                    else leave<T>(p, x, part, f, sum == 0.0f);
+                    fence_before_sync();
+                }
+                if (!has_part) {
+                    if (x.real) leave_lse(p, x.out, sum, add);
+                } else {
+                    part[DP * 128 + x.row] = add;
+                    part[(DP + 1) * 128 + x.row] = sum;
                     __threadfence();
-                    float least = INFINITY;  // of add: the highest reference
-                    for (int x = first_part; x <= final_part; x++) least = fminf(least, __ldcg(part_of(x) + DP * 128 + row));
-                    float all = 0;
-                    for (int x = first_part; x <= final_part; x++) {
-                        const float* const from_part = part_of(x);
-                        const float a = __ldcg(from_part + DP * 128 + row), y = a == INFINITY ? 0.0f : power2(least - a);
-                        all += y * __ldcg(from_part + (DP + 1) * 128 + row);
+                    if (!(fine = meet(meeting(i), meeting_parity))) break;
+                    if (x.row == 0) {
+                        int* const counter = p.counters + first_part * 2 + (shared ? 0 : i);
+                        const bool last = atomicAdd(counter, 1) == (final_part - first_part + 1) * (shared ? 2 : 1) - 1;
+                        joins[i] = last;
+                        if (last) *counter = 0;
                     }
-                    const float g = all == 0.0f ? 0.0f : vscale / all;
-#pragma unroll 1
-                    for (int c = 0; c < DP / 32; c++) {
-                        if (c * 32 >= D) break;
-                        float o[32] = {};
-                        for (int x = first_part; x <= final_part; x++) {
-                            const float* const from_part = part_of(x);
-                            const float a = __ldcg(from_part + DP * 128 + row), y = a == INFINITY ? 0.0f : power2(least - a);
-#pragma unroll
-                            for (int e = 0; e < 32; e++) o[e] += y * __ldcg(from_part + (c * 32 + e) * 128 + row);
-                        }
-                        if (real) store_row(o, c, g, all == 0.0f);
+                    if (!(fine = meet(meeting(i), meeting_parity))) break;
+                    if (joins[i]) {
+                        __threadfence();
+                        const int tile = shared ? 0 : i;
+                        Parts parts;
+                        parts.first = p.parts + ((2 * (int64_t)first_part + 1) * kTiles + tile) * kPart;
+                        parts.rest = p.parts + ((2 * (int64_t)first_part + 2) * kTiles + tile) * kPart;
+                        parts.stride = 2 * kTiles * kPart;
+                        parts.n = final_part - first_part + 1;
+                        join<T, DP>(p, x, parts, shared, vscale);
                     }
-                    if (real) finish(all, least);
                 }
             }
-            segment++;
+            step0 += steps, segment++;
             more = next_block<kKeys>(p, work, w);
         }
     }
     fence_before_sync();
     __syncthreads();
-    if (warp == 0) {
+    if (warp == S::kWarps - 1) {
         fence_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns) : "memory");
     }
@@ -1039,8 +1221,12 @@ int launch(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
     using S = Shape<T, C, DP>;
     static std::atomic<bool> raised[kMaxDevices];
     if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(fcsim_kv_prefill_kernel<T, C, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+        auto* kernel = fcsim_kv_prefill_kernel<T, C, DP>;
+        cudaFuncAttributes a;
+        cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
         if (e != cudaSuccess) return (int)e;
+        if (S::kTiles == 2 && a.numRegs * S::kThreads < 256 * (S::kSoftmaxRegisters + S::kOtherRegisters)) return (int)cudaErrorLaunchOutOfResources;
         if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
     }
     fcsim_kv_prefill_kernel<T, C, DP><<<grid, S::kThreads, S::kBytes, stream>>>(p);
