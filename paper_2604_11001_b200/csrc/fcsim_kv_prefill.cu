@@ -85,13 +85,25 @@ __device__ __forceinline__ void tmem_load(uint32_t at, float (&x)[32]) {
           "=f"(x[31])
         : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&x)[32]) {
+__device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&x)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&x)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&x)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]),
-          "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]),
-          "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31])
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]),
+          "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15])
+        : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&x)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]),
+                   "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
 }
 // two 32-bit values at once
 __device__ __forceinline__ uint64_t pair(float a, float b) {
@@ -150,8 +162,8 @@ struct Shape {
     static constexpr int kRoom = (227 * 1024 - 2048 - 1024 - kQuery) / kStage;
     static constexpr int kStages = kRoom < 8 ? kRoom : 8;
     static constexpr int kBytes = kQuery + kStages * kStage + 1024;
-    static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 7;
-    static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 1, kThreads = 32 * kWarps;
+    static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 6;
+    static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 2, kThreads = 32 * kWarps;
     // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's.
     static constexpr int kSoftmaxRegisters = 160, kOtherRegisters = 96;
     // A warp loads half a tile at a time.  It waits for the place of a tile by the parity of one barrier, so the tile that was there two rounds before
@@ -214,8 +226,9 @@ __device__ __forceinline__ void enter_request(const PrefillParams& p, Block& x) 
     x.position0 = request_length(p, x.r) - x.rows;
 }
 
+__device__ __noinline__ int64_t divide_wide(int64_t a, int64_t b) { return a / b; }
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {  // neither below 0
-    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : divide_wide(a, b);
 }
 
 // The division of the units among the CTAs, which depends on the lengths and the grid alone.  A unit is a tile of keys (and kOverhead of them
@@ -226,11 +239,11 @@ struct Division {
     __device__ __forceinline__ int units(int tiles) const { return cut ? (unsigned)(tiles + cut - 1) / (unsigned)cut : tiles + kOverhead; }
 };
 
-// Where a CTA's stretch begins.
-struct Start {
+// The work of one warp's walk: a block and tiles j .. j_end of it.
+struct Walk {
     Block block;
-    int j;               // first tile
-    int64_t left;        // units from it to the end of the stretch, or the piece's tiles; none: no work
+    int j, j_end;
+    int64_t left;        // units from j to the end of the stretch, or the piece's tiles; none: no work
     int64_t first_unit;  // of the block's first tile (without `cut`)
     int piece, pieces;   // with `cut`
 };
@@ -241,17 +254,18 @@ __device__ __forceinline__ int64_t warp_sum(int64_t x) {
     return x;
 }
 
-// Tiles of one of the heads of a lane's request (`rows` of them from position0 on), or units of the division.  Long requests are added up by the warp.
+// Tiles of one of the heads of a lane's request (`rows` of them from position0 on), or, with `d`, its units.  Long requests are added up by the warp.
 template <int KEYS>
-__device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, int position0, int blocks, const Division* d) {
+__device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, int position0, int cut, int over) {
     constexpr int kAlone = 2;
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, blocks = blocks_of(p, rows);
     int64_t own = 0;
     auto cost = [&](int position, int n, int b) {
         const int t = tiles_of<KEYS>(p, position, n, b);
-        return d ? d->units(t) : t;
+        return cut ? (unsigned)(t + cut - 1) / (unsigned)cut : t + over;
     };
     if (blocks <= kAlone)
+#pragma unroll 1
         for (int b = 0; b < blocks; b++) own += cost(position0, rows, b);
     uint32_t together = __ballot_sync(~0u, blocks > kAlone);
 #pragma unroll 1
@@ -260,148 +274,139 @@ __device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, 
         together &= together - 1;
         const int n = __shfl_sync(~0u, rows, src), position = __shfl_sync(~0u, position0, src), all = __shfl_sync(~0u, blocks, src);
         int64_t sum = 0;
+#pragma unroll 1
         for (int b = lane; b < all; b += 32) sum += cost(position, n, b);
         sum = warp_sum(sum);
         if (lane == src) own = sum;
     }
     return own;
 }
-template <int KEYS>
-__device__ __forceinline__ int64_t add_request(const PrefillParams& p, int r, bool mine, const Division* d, int& blocks) {
-    int rows = 0, position0 = 0, row0;
-    if (mine) {
-        rows = request_rows(p, r, row0);
-        position0 = request_length(p, r) - rows;
-    }
-    blocks = blocks_of(p, rows);
-    return add_blocks<KEYS>(p, rows, position0, blocks, d);
-}
 
-template <int KEYS, int WARPS>
-__device__ __forceinline__ Division plan(const PrefillParams& p, Start& start) {
-    __shared__ int64_t sums[2][WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int heads = p.pool.n_kv * p.head_tiles, each = (unsigned)(p.n_requests + WARPS - 1) / WARPS;
-    const int r0 = min(warp * each, p.n_requests), r1 = min(r0 + each, p.n_requests);
-    auto add_up = [&](const Division* d, bool again) {
+// The division of the work, and where this CTA's part begins.  Warps 0 .. warps - 1 take part, each with a stretch of the requests; one of them
+// finds the start and leaves it in `start`.
+template <int KEYS>
+__device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, int64_t (*sums)[16], int me, int warps) {
+    const int lane = threadIdx.x & 31;
+    const int heads = p.pool.n_kv * p.head_tiles, each = (unsigned)(p.n_requests + warps - 1) / (unsigned)warps;
+    const int r0 = min(me * each, p.n_requests), r1 = min(r0 + each, p.n_requests);
+    int rows = 0, position0 = 0;
+    auto enter = [&](int r) {  // this lane's request
+        int row0;
+        rows = position0 = 0;
+        if (r < r1) {
+            rows = request_rows(p, r, row0);
+            position0 = request_length(p, r) - rows;
+        }
+    };
+    Division d;
+    d.cut = 0, d.share = 1;
+    int64_t all[2], total = 0;  // tiles and blocks, of one head
+#pragma unroll 1
+    for (int pass = 0; pass < 2; pass++) {  // tiles; with `cut` also pieces
         int64_t units = 0, blocks = 0;
 #pragma unroll 1
         for (int base = r0; base < r1; base += 32) {
-            int n;
-            units += add_request<KEYS>(p, base + lane, base + lane < r1, d, n);
-            blocks += n;
+            enter(base + lane);
+            units += add_blocks<KEYS>(p, rows, position0, pass ? d.cut : 0, 0);
+            blocks += blocks_of(p, rows);
         }
         units = warp_sum(units), blocks = warp_sum(blocks);
-        if (again) __syncthreads();
-        if (lane == 0) sums[0][warp] = units, sums[1][warp] = blocks;
-        __syncthreads();
-    };
-    if (threadIdx.x == 0) start.left = 0;
-    add_up(nullptr, false);
-    int64_t tiles = 0, blocks = 0;
-    for (int w = 0; w < WARPS; w++) tiles += sums[0][w], blocks += sums[1][w];
-    Division d;
-    d.cut = 0;
-    int64_t total;
-    if (blocks * heads <= gridDim.x) {  // so that the pieces fit the grid
-        const int64_t spare = max((int64_t)1, gridDim.x - blocks * heads);
-        d.cut = (int)max((int64_t)kPieceLeast, divide(tiles * heads + spare - 1, spare));
-        add_up(&d, true);
-        tiles = 0;
-        for (int w = 0; w < WARPS; w++) tiles += sums[0][w];
-        total = tiles * heads;
-        d.share = 1;
-    } else {
-        total = (tiles + kOverhead * blocks) * heads;
-        d.share = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x));
+        all[0] = units, all[1] = blocks;
+        if (warps > 1) {
+            __syncthreads();
+            if (lane == 0) sums[0][me] = units, sums[1][me] = blocks;
+            __syncthreads();
+            all[0] = all[1] = 0;
+#pragma unroll 1
+            for (int w = 0; w < warps; w++) all[0] += sums[0][w], all[1] += sums[1][w];
+        }
+        if (pass) {
+            total = all[0] * heads;
+            break;
+        }
+        if (all[1] * heads > gridDim.x) {
+            total = (all[0] + kOverhead * all[1]) * heads;
+            d.share = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x));
+            break;
+        }
+        const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);  // so that the pieces fit the grid
+        d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
     }
+    const int over = d.cut ? 0 : kOverhead;
     d.first = min(total, (int64_t)blockIdx.x * d.share), d.end = min(total, d.first + d.share);
     if (d.first >= d.end) return d;
     // the warp whose requests hold the first unit looks for it
     int64_t before = 0;
-    for (int w = 0; w < warp; w++) before += (sums[0][w] + (d.cut ? 0 : kOverhead * sums[1][w])) * heads;
-    const int64_t mine = (sums[0][warp] + (d.cut ? 0 : kOverhead * sums[1][warp])) * heads;
-    if (d.first >= before && d.first < before + mine) {
+    if (warps > 1) {
 #pragma unroll 1
-        for (int base = r0; base < r1; base += 32) {
-            int n;
-            const int64_t own = add_request<KEYS>(p, base + lane, base + lane < r1, &d, n) * heads;
-            int64_t upto = own;
-#pragma unroll
+        for (int w = 0; w < me; w++) before += (sums[0][w] + over * sums[1][w]) * heads;
+        if (d.first < before || d.first >= before + (sums[0][me] + over * sums[1][me]) * heads) return d;
+    }
+#pragma unroll 1
+    for (int base = r0; base < r1; base += 32) {
+        enter(base + lane);
+        const int64_t own = add_blocks<KEYS>(p, rows, position0, d.cut, over) * heads;
+        int64_t upto = own;
+#pragma unroll 1
+        for (int i = 1; i < 32; i <<= 1) {
+            const int64_t x = __shfl_up_sync(~0u, upto, i);
+            if (lane >= i) upto += x;
+        }
+        const uint32_t found = __ballot_sync(~0u, before + upto > d.first);
+        if (found == 0) {
+            before += __shfl_sync(~0u, upto, 31);
+            continue;
+        }
+        const int src = __ffs(found) - 1;
+        const int64_t per_head = divide(__shfl_sync(~0u, own, src), heads);
+        int64_t x = d.first - before - __shfl_sync(~0u, upto - own, src);
+        Block k;
+        k.r = base + src;
+        const int head = (int)divide(x, per_head);
+        k.kv = (unsigned)head / (unsigned)p.head_tiles, k.ht = head - k.kv * p.head_tiles;
+        x -= head * per_head;
+        enter_request(p, k);
+        const int blocks = blocks_of(p, k.rows);
+#pragma unroll 1
+        for (int b0 = 0; b0 < blocks; b0 += 32) {
+            const int cost = b0 + lane < blocks ? d.units(tiles_of<KEYS>(p, k.position0, k.rows, b0 + lane)) : 0;
+            int64_t sum = cost;
+#pragma unroll 1
             for (int i = 1; i < 32; i <<= 1) {
-                const int64_t x = __shfl_up_sync(~0u, upto, i);
-                if (lane >= i) upto += x;
+                const int64_t y = __shfl_up_sync(~0u, sum, i);
+                if (lane >= i) sum += y;
             }
-            const uint32_t found = __ballot_sync(~0u, before + upto > d.first);
-            if (found == 0) {
-                before += __shfl_sync(~0u, upto, 31);
+            const uint32_t here = __ballot_sync(~0u, sum > x);
+            if (here == 0) {
+                x -= __shfl_sync(~0u, sum, 31);
                 continue;
             }
-            const int src = __ffs(found) - 1;
-            const int64_t per_head = divide(__shfl_sync(~0u, own, src), heads);
-            int64_t x = d.first - before - __shfl_sync(~0u, upto - own, src);
-            Block k;
-            k.r = base + src;
-            const int head = (int)divide(x, per_head);
-            k.kv = (unsigned)head / (unsigned)p.head_tiles, k.ht = head - k.kv * p.head_tiles;
-            x -= head * per_head;
-            enter_request(p, k);
-            const int all = blocks_of(p, k.rows);
-#pragma unroll 1
-            for (int b0 = 0; b0 < all; b0 += 32) {
-                const int cost = b0 + lane < all ? d.units(tiles_of<KEYS>(p, k.position0, k.rows, b0 + lane)) : 0;
-                int64_t sum = cost;
-#pragma unroll
-                for (int i = 1; i < 32; i <<= 1) {
-                    const int64_t y = __shfl_up_sync(~0u, sum, i);
-                    if (lane >= i) sum += y;
+            const int at = __ffs(here) - 1;
+            x -= __shfl_sync(~0u, sum - cost, at);
+            const int units = __shfl_sync(~0u, cost, at);
+            k.b = b0 + at;
+            enter_block<KEYS>(p, k);
+            if (lane == 0) {
+                start.block = k;
+                start.piece = 0, start.pieces = 1;
+                if (d.cut) {
+                    start.piece = (int)x, start.pieces = units;
+                    start.j = (int)divide((int64_t)k.tiles * x, units);
+                    start.left = divide((int64_t)k.tiles * (x + 1), units) - start.j;
+                    start.first_unit = 0;
+                } else {
+                    start.j = (int)max((int64_t)0, x - kOverhead);
+                    start.left = d.end - d.first - max((int64_t)0, kOverhead - x);
+                    start.first_unit = d.first - x + kOverhead;
                 }
-                const uint32_t here = __ballot_sync(~0u, sum > x);
-                if (here == 0) {
-                    x -= __shfl_sync(~0u, sum, 31);
-                    continue;
-                }
-                const int at = __ffs(here) - 1;
-                x -= __shfl_sync(~0u, sum - cost, at);
-                const int units = __shfl_sync(~0u, cost, at);
-                k.b = b0 + at;
-                enter_block<KEYS>(p, k);
-                if (lane == 0) {
-                    start.block = k;
-                    if (d.cut) {
-                        start.piece = (int)x, start.pieces = units;
-                        start.j = (int)divide((int64_t)k.tiles * x, units);
-                        start.left = divide((int64_t)k.tiles * (x + 1), units) - start.j;
-                        start.first_unit = 0;
-                    } else {
-                        start.j = (int)max((int64_t)0, x - kOverhead);
-                        start.left = d.end - d.first - max((int64_t)0, kOverhead - x);
-                        start.first_unit = d.first - x + kOverhead;
-                        start.piece = 0, start.pieces = 1;
-                    }
-                }
-                break;
             }
-            break;
+            return d;
         }
+        return d;
     }
     return d;
 }
 
-// A run of tiles of one block.
-struct Walk {
-    Block block;
-    int j, j_end;        // tiles
-    int64_t left, first_unit;
-    __device__ __forceinline__ bool whole() const { return j == 0 && j_end == block.tiles; }
-};
-
-__device__ __forceinline__ bool begin_walk(const Start& s, Walk& w) {
-    w.block = s.block, w.j = s.j, w.left = s.left, w.first_unit = s.first_unit;
-    if (w.left <= 0) return false;
-    w.j_end = (int)min((int64_t)w.block.tiles, w.j + w.left);
-    return true;
-}
 // The next block of the stretch.  (The lengths stay as they are during a call; if they do not, the results are wrong, but nothing beyond the last
 // request is read.)
 template <int KEYS>
@@ -429,10 +434,20 @@ __device__ __forceinline__ bool next_block(const PrefillParams& p, const Divisio
     return true;
 }
 
+// What the warps are told of a run of tiles of one block.
+struct Segment {
+    int r, kv, ht, row, tokens;      // request, heads, first row in q and how many tokens follow it
+    int position, gap, seen;         // of the first row, counted without the gap; the gap; keys
+    int j, steps;                    // the first tile, and how many; no steps: the end
+    int tiles_in_use;                // tiles of rows
+    bool shared, whole;              // one tile of rows, whose tiles of keys the groups of warps take in turn; no other CTA has a part
+    int first_part, final_part;      // the CTAs that have
+};
+
 // Whether some row of the block does not see some key of a tile: those at or behind `base`.
-__device__ __forceinline__ bool partly_seen(const PrefillParams& p, const Block& k, int base, int keys) {
-    const int position0 = k.position0 + k.b * p.tokens_a_block - k.gap, position1 = position0 + k.tokens - 1;
-    return base + keys - 1 > position0 || (p.window > 0 && max(base, p.first) < min((int64_t)base + keys, (int64_t)position1 - p.window + 1));
+__device__ __forceinline__ bool partly_seen(const PrefillParams& p, const Segment& k, int base, int keys) {
+    const int last = k.position + k.tokens - 1;
+    return base + keys - 1 > k.position || (p.window > 0 && max(base, p.first) < min((int64_t)base + keys, (int64_t)last - p.window + 1));
 }
 
 // the lowest n bits, n of any size
@@ -497,76 +512,82 @@ __device__ __forceinline__ bool make_finite(uint4& x) {
 }
 
 // ---------------------------------------------------------------------------------------------- the end of a block
-// What a row's thread needs to leave its output: 32 columns of tensor memory at a time, to the output or to a part.
+// What a row's thread needs to leave its output.
 struct Row {
     uint32_t at;       // tensor memory: O of the row
     int row;           // of its tile
     int64_t out;       // row of the output (token and head)
     bool real;         // it is one
-    int kv, position, from;  // the kv head; the last seen key, the first of the window (counted without the gap)
+    int position, from;  // the last seen key, the first of the window (counted without the gap)
 };
 
+// 32 bytes at once where the rows of the output lie so
+__device__ __forceinline__ void store32(char* to, const uint32_t (&y)[8], bool aligned) {
+    if (aligned)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7]) : "memory");
+    else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+    }
+}
 template <class T>
 __device__ __forceinline__ void store_columns(const PrefillParams& p, int64_t out_row, int c, const float (&o)[32], float f, bool none) {
     const int D = p.pool.head_dim;
     char* const to = p.out + (out_row * D + c * 32) * 2;
+    const bool aligned = D % 16 == 0 && ((uintptr_t)p.out & 31) == 0;
 #pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (c * 32 + e * 8 < D)
-            *reinterpret_cast<uint4*>(to + e * 16) = none ? make_uint4(0, 0, 0, 0)
-                : make_uint4(T::pack(o[8 * e] * f, o[8 * e + 1] * f), T::pack(o[8 * e + 2] * f, o[8 * e + 3] * f),
-                             T::pack(o[8 * e + 4] * f, o[8 * e + 5] * f), T::pack(o[8 * e + 6] * f, o[8 * e + 7] * f));
-}
-
-template <class T>
-__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, float* part, float f, bool none) {
-#pragma unroll 1
-    for (int c = 0; c * 32 < p.pool.head_dim; c++) {
-        float o[32];
-        tmem_load(x.at + 32 * c, o);
-        wait_loads();
-        if (part) {
+    for (int e = 0; e < 2; e++) {
+        uint32_t y[8];
 #pragma unroll
-            for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + x.row] = o[e];
-        } else if (x.real)
-            store_columns<T>(p, x.out, c, o, f, none);
+        for (int i = 0; i < 8; i++) y[i] = none ? 0u : T::pack(o[16 * e + 2 * i] * f, o[16 * e + 2 * i + 1] * f);
+        if (c * 32 + e * 16 + 8 < D) store32(to + e * 32, y, aligned);
+        else if (c * 32 + e * 16 < D) *reinterpret_cast<uint4*>(to + e * 32) = make_uint4(y[0], y[1], y[2], y[3]);
     }
 }
-// The same where tiles that are not seen whole had infinite or NaN elements of v, which were left out of the products: those that this row
-// sees are added.  Tiles j0, j0 + step, .. of the block.
-template <class T, class C, int KEYS>
-__device__ __noinline__ void leave_with_infinite(const PrefillParams& p, const Row& x, const Block& k, int j0, int j1, int step, float* part, float f, bool none) {
+
+// O of a row, 32 columns of tensor memory at a time, to the output or to a part.  INFINITE: tiles that are not seen whole had infinite or NaN
+// elements of v, which were left out of the products: those that this row sees are added (tiles t0, t0 + by, .. of the segment).
+template <class T, class C, int KEYS, bool INFINITE>
+__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by, float* part, float f, bool none) {
     const int D = p.pool.head_dim;
 #pragma unroll 1
     for (int c = 0; c * 32 < D; c++) {
         float o[32];
         tmem_load(x.at + 32 * c, o);
         wait_loads();
-        if (x.real)
-            for (int j = j0; j < j1; j += step) {
-                if (!partly_seen(p, k, j * KEYS, KEYS)) continue;
-                for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
-                    if (u > x.position || (u < x.from && u >= p.first)) continue;
-                    const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
-                    if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
-                    const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + x.kv * p.pool.stride_head + c * 32) * C::bytes;
+        if constexpr (INFINITE) {
+            if (x.real)
+#pragma unroll 1
+                for (int j = k.j + t0; j < k.j + k.steps; j += by) {
+                    if (!partly_seen(p, k, j * KEYS, KEYS)) continue;
+#pragma unroll 1
+                    for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
+                        if (u > x.position || (u < x.from && u >= p.first)) continue;
+                        const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                        if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
+                        const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head + c * 32) * C::bytes;
 #pragma unroll
-                    for (int e = 0; e < 16; e++)
-                        if (c * 32 + 2 * e < D) {
-                            float2 y;
-                            if constexpr (C::bytes == 1) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
-                            else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
-                            if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
-                            if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
-                        }
+                        for (int e = 0; e < 16; e++)
+                            if (c * 32 + 2 * e < D) {
+                                float2 y;
+                                if constexpr (C::bytes == 1) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
+                                else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
+                                if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
+                                if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
+                            }
+                    }
                 }
-            }
+        }
         if (part) {
 #pragma unroll
             for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + x.row] = o[e];
         } else if (x.real)
             store_columns<T>(p, x.out, c, o, f, none);
     }
+}
+template <class T, class C, int KEYS>
+__device__ __noinline__ void leave_with_infinite(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by, float* part, float f, bool none) {
+    leave<T, C, KEYS, true>(p, x, k, t0, by, part, f, none);
 }
 
 // A row's log-sum-exp from the sum of its weights 2^(logit + add).
@@ -617,19 +638,36 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
     if (row.real) leave_lse(p, row.out, all, least);
 }
 
+// A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int* stuck, int32_t* status) {
+    constexpr int64_t kPatience = 4000000000ll;  // cycles: seconds, where microseconds are usual
+    const int64_t began = clock64();
+    bool done = false;
+    while (!(done = bar_try(bar, parity))) {
+        if (*stuck) break;
+        if (clock64() - began > kPatience) {
+            *stuck = 1;
+            flag(status, FCSIM_KV_STUCK);
+            break;
+        }
+    }
+    return (bool)__all_sync(~0u, done);
+}
+
 // ---------------------------------------------------------------------------------------------- the kernel
 template <class T, class C, int DP>
 __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill_kernel(const __grid_constant__ PrefillParams p) {
     using S = Shape<T, C, DP>;
-    constexpr int kTiles = S::kTiles, kKeys = S::kKeys, kStages = S::kStages;
+    constexpr int kTiles = S::kTiles, kKeys = S::kKeys, kStages = S::kStages, kSegments = 4;
     constexpr bool kNarrow = C::bytes == 1;
     constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f;
-    constexpr int64_t kPatience = 4000000000ll;  // cycles that a wait may take: seconds, where microseconds are usual
     extern __shared__ char raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 13];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 12];
     __shared__ uint32_t tmem_at, valid[8][4];
-    __shared__ int stuck, infinite[4][S::kLoadWarps], joins[kTiles];
-    __shared__ Start start;
+    __shared__ int stuck, infinite[kSegments], joins[kTiles];
+    __shared__ Walk start;
+    __shared__ Segment segments[kSegments];
+    __shared__ int64_t sums[2][16];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int D = p.pool.head_dim, group = p.n_heads / p.pool.n_kv;
@@ -637,43 +675,37 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     const uint32_t bar0 = smem_address(bars);
     auto full = [&](int s) { return bar0 + s * 8; };
     auto empty = [&](int s) { return bar0 + (kStages + s) * 8; };
-    auto score_full = [&](int s) { return bar0 + (2 * kStages + s) * 8; };
-    auto weights_ready = [&](int s) { return bar0 + (2 * kStages + 2 + s) * 8; };
-    auto output_full = [&](int s) { return bar0 + (2 * kStages + 4 + s) * 8; };
-    const uint32_t query_full = bar0 + (2 * kStages + 6) * 8, query_empty = query_full + 8, added = query_full + 16, drained = query_full + 24, both = query_full + 32;
-    auto meeting = [&](int i) { return query_full + 40 + i * 8; };
+    auto told_of = [&](int s) { return bar0 + (2 * kStages + s) * 8; };               // of a segment
+    auto done_with = [&](int s) { return bar0 + (2 * kStages + kSegments + s) * 8; };
+    const uint32_t rest = bar0 + (2 * kStages + 2 * kSegments) * 8;
+    auto score_full = [&](int s) { return rest + s * 8; };
+    auto weights_ready = [&](int s) { return rest + 16 + s * 8; };
+    auto output_full = [&](int s) { return rest + 32 + s * 8; };
+    auto meeting = [&](int i) { return rest + 48 + i * 8; };
+    const uint32_t query_full = rest + 64, query_empty = rest + 72, added = rest + 80, drained = rest + 88;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, bar_try(bar, parity)) || wait_long(bar, parity, &stuck, p.status); };
 
-    // A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        bool done = bar_try(bar, parity);
-        if (__all_sync(~0u, done)) return true;
-        const int64_t began = clock64();
-        while (!done && !(done = bar_try(bar, parity))) {
-            if (*(volatile int*)&stuck) break;
-            if (clock64() - began > kPatience) {
-                *(volatile int*)&stuck = 1;
-                flag(p.status, FCSIM_KV_STUCK);
-                break;
-            }
-        }
-        return (bool)__all_sync(~0u, done);
-    };
-
+    constexpr int kProductWarp = S::kWarps - 2, kPlanWarp = S::kWarps - 1;
     if (tid == 0) {
+#pragma unroll 1
         for (int s = 0; s < kStages; s++) bar_init(full(s), 64), bar_init(empty(s), 1);
-        for (int s = 0; s < 2; s++) bar_init(score_full(s), 1), bar_init(weights_ready(s), 128), bar_init(output_full(s), 1);
+#pragma unroll 1
+        for (int s = 0; s < kSegments; s++) bar_init(told_of(s), 1), bar_init(done_with(s), S::kWarps - 1);
+#pragma unroll 1
+        for (int s = 0; s < 2; s++) bar_init(score_full(s), 1), bar_init(weights_ready(s), 128), bar_init(output_full(s), 1), bar_init(meeting(s), 128);
         bar_init(query_full, 32 * S::kLoadWarps), bar_init(query_empty, 1), bar_init(added, 1), bar_init(drained, 1);
-        bar_init(both, 256), bar_init(meeting(0), 128), bar_init(meeting(1), 128);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         stuck = 0;
+        start.left = 0;
     }
-    if (warp == S::kWarps - 1) {
+    if (warp == kProductWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)), "r"(S::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (D % 16 != 0) {  // the products read elements by 16: what is beyond head_dim is zero, and stays so
         const int chunk = D / 8;
         auto clear = [&](uint32_t at, int rows, int tall) {
+#pragma unroll 1
             for (int i = tid; i < rows; i += S::kThreads) {
                 const uint32_t tile = at + i / tall * (tall * DP * 2);
                 const int row = i % tall;
@@ -684,24 +716,148 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         clear(ring, kStages * kKeys, kKeys);
         fence_for_products();
     }
-    const Division work = plan<kKeys, S::kWarps>(p, start);
+    Division work;
+    if (p.n_requests > 32) {
+        __syncthreads();  // (start.left)
+        work = plan<kKeys>(p, start, sums, warp, S::kWarps);
+    }
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = tmem_at;
-
-    Walk w;
-    bool more = begin_walk(start, w);
-    const int heads_a_tile = p.heads_a_tile;
-    auto tiles_in_use = [&](const Block& k) { return kTiles == 2 && k.tokens * heads_a_tile > 128 ? 2 : 1; };
-    // one tile of rows, of which the groups of warps take every other tile of keys
-    auto shared_block = [&](const Walk& w) { return kTiles == 2 && tiles_in_use(w.block) == 1 && (!w.whole() || w.j_end >= kSharedLeast); };
-
     if constexpr (kTiles == 2) {
         if (warp >= S::kSoftmaxWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegisters));
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegisters));
     }
-    if (warp >= S::kSoftmaxWarps && warp < S::kWarps - 1) {
+
+    const int heads_a_tile = p.heads_a_tile;
+    int segment = 0;
+    bool fine = true;
+    // the next segment; false at the end
+    auto next_segment = [&]() {
+        if (!(fine = wait(told_of(segment % kSegments), segment / kSegments & 1))) return false;
+        return segments[segment % kSegments].steps > 0;
+    };
+    auto leave_segment = [&]() {
+        __syncwarp();
+        if (lane == 0) bar_arrive(done_with(segment % kSegments));
+        segment++;
+    };
+
+    if (warp == kPlanWarp) {
+        // ------------------------------------------------------------------------------------------ the walk
+        if (p.n_requests <= 32) work = plan<kKeys>(p, start, sums, 0, 1);
+        __syncwarp();
+        Walk w = start;
+        bool more = w.left > 0;
+        if (more) w.j_end = (int)min((int64_t)w.block.tiles, w.j + w.left);
+        while (true) {
+            const int s = segment % kSegments;
+            if (segment >= kSegments && !wait(done_with(s), (segment / kSegments - 1) & 1)) break;
+            if (lane == 0) {
+                Segment& k = segments[s];
+                k.steps = 0;
+                if (more) {
+                    const Block& b = w.block;
+                    const int at = b.b * p.tokens_a_block;
+                    k.r = b.r, k.kv = b.kv, k.ht = b.ht, k.row = b.row0 + at, k.tokens = b.tokens;
+                    k.position = b.position0 + at - b.gap, k.gap = b.gap, k.seen = b.seen;
+                    k.j = w.j, k.steps = w.j_end - w.j;
+                    k.tiles_in_use = kTiles == 2 && b.tokens * heads_a_tile > 128 ? 2 : 1;
+                    k.whole = w.j == 0 && w.j_end == b.tiles;
+                    k.shared = kTiles == 2 && k.tiles_in_use == 1 && (!k.whole || k.steps >= kSharedLeast);
+                    k.first_part = k.final_part = blockIdx.x;
+                    if (!k.whole) {
+                        if (work.cut) {
+                            k.first_part -= w.piece;
+                            k.final_part = k.first_part + w.pieces - 1;
+                        } else {
+                            if (w.first_unit < work.first) k.first_part = (int)divide(w.first_unit, work.share);
+                            if (w.first_unit + b.tiles > work.end) k.final_part = (int)divide(w.first_unit + b.tiles - 1, work.share);
+                        }
+                    }
+                }
+                infinite[s] = 0;
+                bar_arrive(told_of(s));
+            }
+            segment++;
+            if (!more) break;
+            more = next_block<kKeys>(p, work, w);
+        }
+    } else if (warp == kProductWarp) {
+        // ------------------------------------------------------------------------------------------ products
+        constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
+        const uint32_t depth = uni((D + 15) / 16), base = uni(tmem);
+        const uint32_t how_output = instruction(kType, true, 128, depth * 16);
+        const uint64_t query_operand = operand(uni(query), 16, 1024), key_operand = operand(uni(ring), 16, 1024), value_operand = operand(uni(ring), kKeys * 128, 1024);
+        int tile0 = 0;
+        uint32_t ready[2] = {0, 0};  // parities of the weights
+        while (next_segment()) {
+            const Segment& k = segments[segment % kSegments];
+            const int n = k.tiles_in_use, steps = k.steps;
+            // With two tiles of rows, tile after tile: the output of a step, then the scores of the next (K0 V0 K1 V1 ..).  With one, the scores
+            // run a step ahead, in the two areas in turn (K0 K1 V0 K2 V1 ..).  Both are a row of outputs, each followed by the scores of the
+            // output `lead` later.
+            const bool ahead = kTiles == 1 || k.shared;
+            const int outputs = ahead ? steps : steps * n, lead = ahead ? min(2, steps) : n, wide = ahead ? 0 : n - 1;
+            // a negative scale turns the order of the logits around: Q is taken as -Q instead
+            const float scale = kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale;
+            const uint32_t how_score = instruction(kType, false, 128, kKeys) | uni(scale < 0) << 13;
+            if (!(fine = wait(query_full, segment & 1))) break;
+            auto wait_tile = [&](int x) {  // tile x of the segment is there
+                const int t = tile0 + x;
+                if (!wait(full(t % kStages), (t / kStages) & 1)) return false;
+                fence_after_sync();
+                return true;
+            };
+#pragma unroll 1
+            for (int q = -lead; q < outputs; q++) {
+                if (q >= 0) {
+                    const int j = q >> wide, i = ahead ? q & 1 : q & wide, x = !ahead ? 2 * j + 1 : j + 1 < steps ? 2 * j + 2 : 2 * j + 1;
+                    if ((ahead || i == 0) && !(fine = wait_tile(x))) break;
+                    if (!(fine = wait(weights_ready(i), ready[i]))) break;
+                    ready[i] ^= 1;
+                    fence_after_sync();
+                    const int o = kTiles == 1 ? 0 : i, first = kTiles == 2 && ahead ? 2 : 1;
+                    const uint32_t s = uni((tile0 + x) % kStages), more_of = uni(j >= first), to = uni(base + S::kOutput + o * DP), from = uni(base + S::kScore + i * kKeys);
+                    const uint64_t b = value_operand + s * (S::kStage >> 4);
+                    const bool releases = ahead || i == n - 1, ends = kTiles == 1 ? j + 1 == steps : ahead ? j + 2 >= steps : j + 1 == steps;
+                    if (elected()) {
+#pragma unroll
+                        for (int part = 0; part < 2; part++)
+#pragma unroll
+                            for (int y = 0; y < kKeys / 16; y++)
+                                product_from_tmem(to, from + y * 16 + part * 8, b + (y * 2048 >> 4), how_output, part > 0 || y > 0 ? 1u : more_of);
+                        if (releases) commit_products(empty(s));
+                        if (kTiles == 1) commit_products(added);
+                        if (ends) commit_products(output_full(o));
+                    }
+                }
+                const int next = q + lead;
+                if (next < outputs) {
+                    const int j = next >> wide, i = ahead ? next & 1 : next & wide, x = !ahead ? 2 * j : j == 0 ? 0 : 2 * j - 1;
+                    if ((ahead || i == 0) && !(fine = wait_tile(x))) break;
+                    const uint32_t s = uni((tile0 + x) % kStages), to = uni(base + S::kScore + i * kKeys), rows = uni(ahead ? 0 : i);
+                    const uint64_t a = query_operand + rows * (128 * DP * 2 >> 4), b = key_operand + s * (S::kStage >> 4);
+                    const bool releases = ahead || i == n - 1;
+                    if (elected()) {
+#pragma unroll
+                        for (int y = 0; y < DP / 16; y++)
+                            if (y < depth) product(to, a + ((y / 4 * (128 * 128) + y % 4 * 32) >> 4), b + ((y / 4 * (kKeys * 128) + y % 4 * 32) >> 4), how_score, y > 0);
+                        commit_products(score_full(i));
+                        if (releases) commit_products(empty(s));
+                        if (next + 1 == outputs) commit_products(query_empty);
+                    }
+                }
+            }
+            if (!fine) break;
+            tile0 += 2 * steps;
+            leave_segment();
+        }
+        if (elected()) commit_products(drained);  // nothing is in flight when the CTA ends
+        const int64_t began = clock64();
+        while (!bar_try(drained, 0) && clock64() - began < 4000000000ll) {}
+    } else if (warp >= S::kSoftmaxWarps) {
         // ------------------------------------------------------------------------------------------ loads
         // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own
         // copies while the others' are on their way.
@@ -711,283 +867,162 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         const int chunk = lane % kLanes, lane_row = lane / kLanes, chunks = D * C::bytes / 16;
         const bool copies = chunk < chunks;
         const uint32_t token_magic = (65536 + heads_a_tile - 1) / heads_a_tile;  // row / heads_a_tile for rows below 256
-        int tile0 = 0, step0 = 0, segment = 0;  // tiles and steps of the segments before this one
-        int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
-        uint32_t next_bad = 0;     // which of them are in a page outside the pool
-        auto fetch_pages = [&](const Block& k, int j, int half) {
-            next_bad = 0;
-#pragma unroll
-            for (int c = 0; c < kOffs; c++) {
-                const int u = j * kKeys + half * kHalf + c * 32 + lane;
-                next_off[c] = -1;
-                if (u < k.seen) {
-                    const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
-                    if ((unsigned)page < (unsigned)p.pool.n_pages)
-                        next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
-                    else
-                        next_bad |= 1u << c;
-                }
-            }
-        };
+        int tile0 = 0, step0 = 0;  // tiles and steps of the segments before this one
         // place in a stage of 16 bytes of a row
         auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
-        bool fine = true;
-        while (more && fine) {
-            const Block& k = w.block;
-            const int steps = w.j_end - w.j;
-            // tile x of the segment: with two tiles of rows K and V of a step, then of the next; with one, the scores run a step ahead
-            const bool ahead = kTiles == 1 || shared_block(w);
+        while (next_segment()) {
+            const Segment& k = segments[segment % kSegments];
+            const int steps = k.steps, halves = 4 * steps;
+            // tile x of the segment
+            const bool ahead = kTiles == 1 || k.shared;
             auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
             auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
-            // copies of half h of the segment (8-bit rows: all of it)
-            auto begin_half = [&](int h) {
-                const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = w.j + step_of(x);
-                const bool key = is_key(x);
-                const char* const pool = key ? p.pool.k : p.pool.v;
-                int64_t off[kOffs];
-#pragma unroll
-                for (int c = 0; c < kOffs; c++) {
-                    off[c] = next_off[c];
-                    if (key) {
-                        const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
-                        if (lane == 0) {
-                            valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
-                            if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
-                        }
-                    }
-                }
-                if (h + S::kLoadWarps < 4 * steps) fetch_pages(k, w.j + step_of((h + S::kLoadWarps) / 2), (h + S::kLoadWarps) % 2);
-                if (tile >= kStages && !wait(empty(s), (tile / kStages - 1) & 1)) return false;
-                const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
-                if constexpr (kNarrow) {
-                    const bool edge = !key && partly_seen(p, k, j * kKeys, kKeys);
-                    bool found = false;
+            int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
+            uint32_t next_bad = 0;     // which of them are in a page outside the pool
+            int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps, fetched = -1;  // this warp's first half
+            // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
+            // are left by tiles of blocks before.)
+            bool query_due = true;
 #pragma unroll 1
-                    for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
-                        uint4 raw[kBatch];
-                        const int row0 = i0 * kAtOnce + lane_row;
-                        constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
-                        int64_t mine[kHere];
+            while (query_due || h < halves) {
+                const bool loads = h < (query_due ? min(4, halves) : halves);
+                const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = k.j + step_of(x);
+                const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
+                const bool key = is_key(x), edge = !key && partly_seen(p, k, j * kKeys, kKeys);
+                const char* const pool = key ? p.pool.k : p.pool.v;
+                bool found = false;
+                if (loads) {
+                    int64_t off[kOffs];
+#pragma unroll 1
+                    for (int again = 0; again < 2; again++) {  // the pages of this half, if they are not at hand, and of the next
+                        const int y = again ? h + S::kLoadWarps : h;
+                        if (again) {
 #pragma unroll
-                        for (int y = 0; y < kHere; y++) {
-                            mine[y] = off[y];
+                            for (int c = 0; c < kOffs; c++) off[c] = next_off[c];
+                            if (key) {
 #pragma unroll
-                            for (int c = 1; c < kOffs; c++)
-                                if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
-                        }
-#pragma unroll
-                        for (int i = 0; i < kBatch; i++) {
-                            const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
-                            raw[i] = make_uint4(0, 0, 0, 0);
-                            if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
-                        }
-                        if (copies) {
-#pragma unroll
-                            for (int i = 0; i < kBatch; i++) {
-                                const int row = row0 + i * kAtOnce;
-                                uint4 a, b;
-                                widen<T>(raw[i], a, b);
-                                if (edge) found |= make_finite<T>(a) | make_finite<T>(b);
-                                store16(to + place(row, 2 * chunk), a);
-                                store16(to + place(row, 2 * chunk + 1), b);
-                            }
-                        }
-                    }
-                    if (__any_sync(~0u, found) && lane == 0) infinite[segment & 3][me] = 1;
-                    fence_for_products();
-                    bar_arrive(full(s));
-                } else {
-#pragma unroll
-                    for (int c = 0; c < kOffs; c++) {
-#pragma unroll 8
-                        for (int i = 0; i < kRounds / kOffs; i++) {
-                            const int row = i * kAtOnce + lane_row;
-                            const int64_t o = __shfl_sync(~0u, off[c], row);
-                            if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
-                        }
-                    }
-                    commit_copies();
-                }
-                return true;
-            };
-            auto end_half = [&](int h) {  // its copies have arrived
-                if constexpr (!kNarrow) {
-                    const int x = h / 2, s = (tile0 + x) % kStages, j = w.j + step_of(x);
-                    if (!is_key(x) && partly_seen(p, k, j * kKeys, kKeys)) {
-                        // what some row does not see must not meet its weight of zero as an infinity or NaN
-                        bool found = false;
-                        if (copies) {
-#pragma unroll 8
-                            for (int i = 0; i < kRounds; i++) {
-                                const uint32_t at = ring + s * S::kStage + h % 2 * kHalf * 128 + place(i * kAtOnce + lane_row, chunk);
-                                uint4 y = load16(at);
-                                if (make_finite<T>(y)) {
-                                    store16(at, y);
-                                    found = true;
+                                for (int c = 0; c < kOffs; c++) {
+                                    const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
+                                    if (lane == 0) {
+                                        valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
+                                        if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
+                                    }
                                 }
                             }
                         }
-                        if (__any_sync(~0u, found) && lane == 0) infinite[segment & 3][me] = 1;
-                    }
-                    fence_for_products();
-                    bar_arrive(full(s));
-                }
-            };
-            int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps;  // this warp's first
-            if (h < 4 * steps) fetch_pages(k, w.j + step_of(h / 2), h % 2);
-            if (lane == 0) infinite[segment & 3][me] = 0;
-            // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
-            // are left by tiles of blocks before.)
-            const bool early = h < 4;
-            if (early && !(fine = begin_half(h))) break;
-            if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
-            {
-                constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
-                const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
-                for (int r0 = me * 16; r0 < tiles_in_use(k) * 128; r0 += 16 * S::kLoadWarps) {
-                    const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
-                    int64_t off = -1;
-                    if (token < k.tokens && g < part)
-                        off = ((int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
+                        if (fetched >= y || y >= halves) continue;
+                        fetched = y;
+                        next_bad = 0;
 #pragma unroll
-                    for (int i = 0; i < 16 / kQueryRows; i++) {
-                        const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
-                        const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                        if (at < D / 8)
-                            copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
-                                   p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
+                        for (int c = 0; c < kOffs; c++) {
+                            const int u = (k.j + step_of(y / 2)) * kKeys + y % 2 * kHalf + c * 32 + lane;
+                            next_off[c] = -1;
+                            if (u < k.seen) {
+                                const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                                if ((unsigned)page < (unsigned)p.pool.n_pages)
+                                    next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
+                                else
+                                    next_bad |= 1u << c;
+                            }
+                        }
+                    }
+                    if (tile >= kStages && !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
+                    if constexpr (kNarrow) {
+#pragma unroll 1
+                        for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
+                            uint4 raw[kBatch];
+                            const int row0 = i0 * kAtOnce + lane_row;
+                            constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
+                            int64_t mine[kHere];
+#pragma unroll
+                            for (int y = 0; y < kHere; y++) {
+                                mine[y] = off[y];
+#pragma unroll
+                                for (int c = 1; c < kOffs; c++)
+                                    if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
+                            }
+#pragma unroll
+                            for (int i = 0; i < kBatch; i++) {
+                                const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
+                                raw[i] = make_uint4(0, 0, 0, 0);
+                                if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
+                            }
+                            if (copies) {
+#pragma unroll
+                                for (int i = 0; i < kBatch; i++) {
+                                    const int row = row0 + i * kAtOnce;
+                                    uint4 a, b;
+                                    widen<T>(raw[i], a, b);
+                                    store16(to + place(row, 2 * chunk), a);
+                                    store16(to + place(row, 2 * chunk + 1), b);
+                                }
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kOffs; c++) {
+#pragma unroll 8
+                            for (int i = 0; i < kRounds / kOffs; i++) {
+                                const int row = i * kAtOnce + lane_row;
+                                const int64_t o = __shfl_sync(~0u, off[c], row);
+                                if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
+                            }
+                        }
                     }
                 }
                 commit_copies();
+                if (query_due) {
+                    if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
+                    constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
+                    const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
+#pragma unroll 1
+                    for (int r0 = me * 16; r0 < k.tiles_in_use * 128; r0 += 16 * S::kLoadWarps) {
+                        const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
+                        int64_t off = -1;
+                        if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
+#pragma unroll
+                        for (int i = 0; i < 16 / kQueryRows; i++) {
+                            const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
+                            const int y = r0 + i * kQueryRows + lane / kQueryLanes;
+                            if (at < D / 8)
+                                copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
+                                       p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
+                        }
+                    }
+                    commit_copies();
+                    wait_copies<1>();
+                } else
+                    wait_copies<0>();
+                if (loads) {
+                    if (edge && (kNarrow ? 2 * chunk < D / 8 : copies)) {
+                        // what some row does not see must not meet its weight of zero as an infinity or NaN
+#pragma unroll 4
+                        for (int i = 0; i < kRounds * (kNarrow ? 2 : 1); i++) {
+                            const uint32_t at = to + (kNarrow ? place(i / 2 * kAtOnce + lane_row, 2 * chunk + i % 2) : place(i * kAtOnce + lane_row, chunk));
+                            uint4 y = load16(at);
+                            if (make_finite<T>(y)) {
+                                store16(at, y);
+                                found = true;
+                            }
+                        }
+                    }
+                    if (found) infinite[segment % kSegments] = 1;
+                    fence_for_products();
+                    bar_arrive(full(s));
+                    h += S::kLoadWarps;
+                }
+                if (query_due) {
+                    wait_copies<0>();
+                    fence_for_products();
+                    bar_arrive(query_full);
+                    query_due = false;
+                }
             }
-            if (early) {
-                wait_copies<1>();
-                end_half(h);
-                h += S::kLoadWarps;
-            }
-            wait_copies<0>();
-            fence_for_products();
-            bar_arrive(query_full);
-            for (; h < 4 * steps; h += S::kLoadWarps) {
-                if (!(fine = begin_half(h))) break;
-                wait_copies<0>();
-                end_half(h);
-            }
-            tile0 += 2 * steps, step0 += steps, segment++;
-            more = next_block<kKeys>(p, work, w);
+            if (!fine) break;
+            tile0 += 2 * steps, step0 += steps;
+            leave_segment();
         }
         wait_copies<0>();
-    } else if (warp == S::kWarps - 1) {
-        // ------------------------------------------------------------------------------------------ products
-        constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
-        const uint32_t depth = uni((D + 15) / 16), base = uni(tmem), how_score = instruction(kType, false, 128, kKeys);
-        const uint32_t how_output = instruction(kType, true, 128, depth * 16);
-        const uint64_t query_operand = operand(uni(query), 16, 1024), key_operand = operand(uni(ring), 16, 1024), value_operand = operand(uni(ring), kKeys * 128, 1024);
-        int tile = 0, segment = 0;
-        uint32_t ready[2] = {0, 0};  // parities of the weights
-        auto score = [&](int slot, int i, int t) {  // S of row tile i, with K in tile t of the ring
-            const uint32_t s = uni(t % kStages);
-            const uint64_t a = query_operand + i * (128 * DP * 2 >> 4), b = key_operand + s * (S::kStage >> 4);
-            if (elected()) {
-#pragma unroll
-                for (int k = 0; k < DP / 16; k++)
-                    if (k < depth)
-                        product(base + S::kScore + slot * kKeys, a + ((k / 4 * (128 * 128) + k % 4 * 32) >> 4), b + ((k / 4 * (kKeys * 128) + k % 4 * 32) >> 4),
-                                how_score, k > 0);
-                commit_products(score_full(slot));
-            }
-        };
-        auto output = [&](int slot, int i, int t, bool add) {  // O of tile i, with V in tile t of the ring
-            const uint32_t s = uni(t % kStages), more_of = uni(add);
-            const uint64_t b = value_operand + s * (S::kStage >> 4);
-            const uint32_t to = base + S::kOutput + i * DP, from = base + S::kScore + slot * kKeys;
-            if (elected()) {
-#pragma unroll
-                for (int part = 0; part < 2; part++)
-#pragma unroll
-                    for (int k = 0; k < kKeys / 16; k++)
-                        product_from_tmem(to, from + k / 2 * 32 + part * 16 + k % 2 * 8, b + (k * 2048 >> 4), how_output, part > 0 || k > 0 ? 1u : more_of);
-            }
-        };
-        auto told = [&](uint32_t bar) {  // all products so far
-            if (elected()) commit_products(bar);
-        };
-        auto wait_full = [&](int t) {
-            if (!wait(full(t % kStages), (t / kStages) & 1)) return false;
-            fence_after_sync();
-            return true;
-        };
-        auto wait_weights = [&](int slot) {
-            if (!wait(weights_ready(slot), ready[slot])) return false;
-            ready[slot] ^= 1;
-            fence_after_sync();
-            return true;
-        };
-        bool fine = true;
-        while (more && fine) {
-            const int n = tiles_in_use(w.block), steps = w.j_end - w.j;
-            const bool shared = shared_block(w);
-            if (!(fine = wait(query_full, segment & 1) && wait_full(tile))) break;
-            if (kTiles == 1 || shared) {
-                // scores run a step ahead, in the two areas in turn: K0 K1 V0 K2 V1 ..
-                score(0, 0, tile);
-                told(empty(tile % kStages));
-                tile++;
-                if (steps > 1) {
-                    if (!(fine = wait_full(tile))) break;
-                    score(1, 0, tile);
-                    told(empty(tile % kStages));
-                    tile++;
-                }
-                if (steps <= 2) told(query_empty);
-                for (int j = 0; j < steps && fine; j++) {
-                    const int slot = j & 1;
-                    if (!(fine = wait_full(tile) && wait_weights(slot))) break;
-                    output(slot, kTiles == 1 ? 0 : slot, tile, j >= (kTiles == 1 ? 1 : 2));
-                    told(empty(tile % kStages));
-                    if (kTiles == 1) told(added);
-                    tile++;
-                    if (j + 2 < steps) {
-                        if (!(fine = wait_full(tile))) break;
-                        score(slot, 0, tile);
-                        told(empty(tile % kStages));
-                        if (j + 3 == steps) told(query_empty);
-                        tile++;
-                    }
-                    if (kTiles == 1 ? j + 1 == steps : j + 2 >= steps) told(output_full(kTiles == 1 ? 0 : slot));
-                }
-            } else {
-                for (int i = 0; i < n; i++) score(i, i, tile);
-                told(empty(tile % kStages));
-                if (steps == 1) told(query_empty);
-                tile++;
-                for (int j = 0; j < steps && fine; j++) {
-                    // tile after tile: the output of this step, then the scores of the next
-                    const bool another = j + 1 < steps;
-                    if (!(fine = wait_full(tile))) break;
-                    for (int i = 0; i < n; i++) {
-                        if (!(fine = wait_weights(i))) break;
-                        output(i, i, tile, j > 0);
-                        if (i == n - 1) told(empty(tile % kStages));
-                        if (another) {
-                            if (i == 0 && !(fine = wait_full(tile + 1))) break;
-                            score(i, i, tile + 1);
-                            if (i == n - 1) {
-                                told(empty((tile + 1) % kStages));
-                                if (j + 2 == steps) told(query_empty);
-                            }
-                        } else
-                            told(output_full(i));
-                    }
-                    tile += another ? 2 : 1;
-                }
-            }
-            segment++;
-            more = next_block<kKeys>(p, work, w);
-        }
-        told(drained);  // nothing is in flight when the CTA ends
-        const int64_t began = clock64();
-        while (!bar_try(drained, 0) && clock64() - began < kPatience) {}
     } else {
         // ------------------------------------------------------------------------------------------ softmax
         // rows that belong to no request, and what is wrong with the requests
@@ -997,12 +1032,15 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             const int n1 = p.n_requests > 0 ? min(max(p.starts[p.n_requests], n0), p.n_rows) : p.n_rows, none = p.n_rows - n1 + n0;
             if (none > 0) {
                 const int64_t per_row = (int64_t)p.n_heads * (D / 8);
+#pragma unroll 1
                 for (int64_t i = (int64_t)blockIdx.x * kHere + tid; i < none * per_row; i += (int64_t)gridDim.x * kHere)
                     reinterpret_cast<uint4*>(p.out)[i < n0 * per_row ? i : i + (n1 - n0) * per_row] = make_uint4(0, 0, 0, 0);
                 if (p.lse)
+#pragma unroll 1
                     for (int64_t i = (int64_t)blockIdx.x * kHere + tid; i < (int64_t)none * p.n_heads; i += (int64_t)gridDim.x * kHere)
                         p.lse[i < (int64_t)n0 * p.n_heads ? i : i + (int64_t)(n1 - n0) * p.n_heads] = -INFINITY;
             }
+#pragma unroll 1
             for (int r = blockIdx.x * kHere + tid; r < p.n_requests; r += gridDim.x * kHere) {
                 const int a = p.starts[r], b = p.starts[r + 1], n = p.lengths[r];
                 if (n < 0 || n > p.max_length || a < 0 || b < a || b > p.n_rows || b - a > n) flag(p.status, FCSIM_KV_BAD_LENGTH);
@@ -1013,169 +1051,137 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         Row x;
         x.row = tid & 127;
         x.at = tmem + S::kOutput + i * DP + lanes;
-        int step0 = 0, segment = 0;
-        bool was_here = false;
-        uint32_t score_parity[2] = {0, 0}, output_parity = 0, both_parity = 0, meeting_parity = 0;
-        bool fine = true;
-        auto meet = [&](uint32_t bar, uint32_t& parity) {
-            bar_arrive(bar);
-            const bool ok = wait(bar, parity);
-            parity ^= 1;
+        // token and head of the row, in a tile of its own or where both groups have the first
+        const int token_own = (uint32_t)tid / (uint32_t)heads_a_tile, g_own = tid - token_own * heads_a_tile;
+        const int token_first = (uint32_t)x.row / (uint32_t)heads_a_tile, g_first = x.row - token_first * heads_a_tile;
+        int step0 = 0;
+        uint32_t score_parity[2] = {0, 0}, output_parity = 0, meeting_parity = 0;
+        auto meet = [&]() {
+            bar_arrive(meeting(i));
+            const bool ok = wait(meeting(i), meeting_parity);
+            meeting_parity ^= 1;
             return ok;
         };
-        while (more && fine) {
-            const Block& k = w.block;
-            const int n = tiles_in_use(k), steps = w.j_end - w.j;
-            const bool shared = shared_block(w), whole = w.whole();
-            if (kTiles == 2) {
-                // (the second group does not fall behind while it is not needed: flags of a few segments are kept)
-                const bool here = n == 2 || (shared && steps > 1);
-                if (was_here && !here && !meet(both, both_parity)) break;
-                was_here = here;
-            }
-            const int row = (kTiles == 1 || shared ? 0 : i * 128) + x.row, token = (uint32_t)row / (uint32_t)heads_a_tile, g = row - token * heads_a_tile;
-            const int head = k.ht * heads_a_tile + g;
-            x.real = token < k.tokens && head < group;
-            x.kv = k.kv;
-            x.out = (int64_t)(k.row0 + k.b * p.tokens_a_block + token) * p.n_heads + k.kv * group + head;
-            const float unit = (kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale) * kLog2e;
-            const bool turned = unit < 0;
-            // the last seen key of this row and the first of its window; nothing for rows that are none
-            const int position = k.position0 + k.b * p.tokens_a_block + token - k.gap;
-            x.position = x.real ? position : -1, x.from = p.window > 0 && position >= p.window ? position - p.window + 1 : 0;
-            float add = INFINITY, limit = -INFINITY, sum = 0;  // weights are 2^(unit s + add); add is infinite until there is a finite logit
-            const int step_first = shared ? i : kTiles == 2 && i >= n ? steps : 0, step_by = shared ? 2 : 1;
-            for (int t = step_first; t < steps; t += step_by) {
-                const int slot = kTiles == 2 ? i : t & 1, tile_base = (w.j + t) * kKeys, flags = (step0 + t) & 7;
-                const uint32_t at = tmem + S::kScore + slot * kKeys + lanes;
-                if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
-                score_parity[slot] ^= 1;
-                fence_after_sync();
-                uint32_t there = ~0u;
-#pragma unroll
-                for (int c = 0; c < kKeys / 32; c++) there &= valid[flags][c];
-                const bool masked = there != ~0u || partly_seen(p, k, tile_base, kKeys);
-                auto mask_of = [&](int c) {  // of 32 keys
-                    const int b = tile_base + 32 * c;
-                    return lowest(x.position + 1 - b) & (~lowest(x.from - b) | lowest(p.first - b)) & valid[flags][c];
-                };
-                // the largest logit (with a negative scale: the lowest)
-                const float none = turned ? INFINITY : -INFINITY;
-                float top = none;
+        while (next_segment()) {
+            const Segment& k = segments[segment % kSegments];
+            const int steps = k.steps;
+            const bool shared = k.shared, whole = k.whole;
+            const int step_first = shared ? i : i >= k.tiles_in_use ? steps : 0, step_by = shared ? 2 : 1;
+            const bool worked = step_first < steps, has_part = !whole || shared;
+            if (worked || shared) {
+                const int token = shared ? token_first : token_own, head = k.ht * heads_a_tile + (shared ? g_first : g_own);
+                x.real = token < k.tokens && head < group;
+                x.out = (int64_t)(k.row + token) * p.n_heads + k.kv * group + head;
+                // (never zero, so that what is not seen, a logit of -infinity, stays without weight: 2^-149 times the largest logit is 5e-7)
+                float unit = fabsf(kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale) * kLog2e;
+                if (unit < 1.4e-45f) unit = 1.4e-45f;
+                // the last seen key of this row and the first of its window; nothing for rows that are none
+                x.position = x.real ? k.position + token : -1;
+                x.from = p.window > 0 && x.position >= p.window ? x.position - p.window + 1 : 0;
+                float add = INFINITY, limit = -INFINITY, sum = 0;  // weights are 2^(unit s + add); add is infinite until there is a finite logit
 #pragma unroll 1
-                for (int c = 0; c < kKeys / 32; c += 2) {
-                    float s[2][32];
-                    tmem_load(at + 32 * c, s[0]);
-                    tmem_load(at + 32 * c + 32, s[1]);
-                    wait_loads();
-                    if (masked) {
-                        const uint32_t mask[2] = {mask_of(c), mask_of(c + 1)};
+                for (int t = step_first; t < steps; t += step_by) {
+                    const int slot = kTiles == 2 ? i : t & 1, tile_base = (k.j + t) * kKeys;
+                    const uint32_t at = tmem + S::kScore + slot * kKeys + lanes;
+                    const bool edge = partly_seen(p, k, tile_base, kKeys);
+                    if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
+                    score_parity[slot] ^= 1;
+                    fence_after_sync();
+                    const uint32_t* const there = valid[(step0 + t) & 7];
+                    uint32_t some = ~0u;
 #pragma unroll
-                        for (int e = 0; e < 64; e++) s[e / 32][e % 32] = mask[e / 32] >> e % 32 & 1 ? s[e / 32][e % 32] : none;
-                    }
-                    float tops[4] = {top, none, none, none};
-                    if (turned) {
+                    for (int c = 0; c < kKeys / 32; c++) some &= there[c];
+                    const bool masked = edge || some != ~0u;
+                    auto load = [&](int c, float (&s)[4][16]) {  // 64 logits; those that are not seen are -infinity
 #pragma unroll
-                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fminf(fminf(tops[e / 2 % 4], s[e / 32][e % 32]), s[e / 32][e % 32 + 1]);
-                        top = fminf(fminf(tops[0], tops[1]), fminf(tops[2], tops[3]));
-                    } else {
+                        for (int e = 0; e < 4; e++) tmem_load16(at + c * 64 + 16 * e, s[e]);
+                        wait_loads();
+                        if (masked) {
 #pragma unroll
-                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fmaxf(fmaxf(tops[e / 2 % 4], s[e / 32][e % 32]), s[e / 32][e % 32 + 1]);
+                            for (int y = 0; y < 2; y++) {
+                                const int b = tile_base + 64 * c + 32 * y;
+                                const uint32_t mask = lowest(x.position + 1 - b) & (~lowest(x.from - b) | lowest(p.first - b)) & there[2 * c + y];
+#pragma unroll
+                                for (int e = 0; e < 32; e++) s[2 * y + e / 16][e % 16] = mask >> e & 1 ? s[2 * y + e / 16][e % 16] : -INFINITY;
+                            }
+                        }
+                    };
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kKeys / 64; c++) {
+                        float s[4][16];
+                        load(c, s);
+                        float tops[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fmaxf(fmaxf(tops[e / 2 % 4], s[e / 16][e % 16]), s[e / 16][e % 16 + 1]);
                         top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     }
-                }
-                const float most = top == none ? -INFINITY : top * unit;
-                // The reference moves only when a logit is 2^kLag above it, so that the output is seldom taken through registers.
-                const bool moves = most > limit;
-                float shrink = 1;
-                if (moves) {
-                    const float now = kRaise - most;
-                    shrink = limit == -INFINITY ? 0.0f : power2(now - add);
-                    add = now;
-                    limit = most + kLag;
-                    sum *= shrink;
-                }
-                if (t > step_first && __any_sync(~0u, moves)) {
-                    if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
-                    fence_after_sync();
+                    const float most = top * unit;
+                    // The reference moves only when a logit is 2^kLag above it, so that the output is seldom taken through registers.
+                    const bool moves = most > limit;
+                    if (__any_sync(~0u, moves)) {
+                        float shrink = 1;
+                        if (moves) {
+                            const float now = kRaise - most;
+                            shrink = limit == -INFINITY ? 0.0f : power2(now - add);
+                            add = now;
+                            limit = most + kLag;
+                            sum *= shrink;
+                        }
+                        if (t > step_first) {
+                            if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
+                            fence_after_sync();
 #pragma unroll 1
-                    for (int c = 0; c * 32 < D; c++) {
-                        float o[32];
-                        uint32_t y[32];
-                        tmem_load(x.at + 32 * c, o);
-                        wait_loads();
+                            for (int c = 0; c * 8 < D; c++) {
+                                uint32_t y[8];
+                                tmem_load8(x.at + 8 * c, y);
+                                wait_loads();
 #pragma unroll
-                        for (int e = 0; e < 32; e++) y[e] = __float_as_uint(o[e] * shrink);
-                        tmem_store(x.at + 32 * c, y);
+                                for (int e = 0; e < 8; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * shrink);
+                                tmem_store8(x.at + 8 * c, y);
+                            }
+                        }
                     }
-                }
-                const float plus = limit == -INFINITY ? 0.0f : add;
-                const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
-                uint64_t sums[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+                    const float plus = limit == -INFINITY ? 0.0f : add;
+                    const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
+                    uint64_t sums2[2] = {pair(sum, 0.0f), pair(0.0f, 0.0f)};
 #pragma unroll 1
-                for (int c = 0; c < kKeys / 32; c += 2) {
-                    float s[2][32];
-                    tmem_load(at + 32 * c, s[0]);
-                    tmem_load(at + 32 * c + 32, s[1]);
-                    wait_loads();
+                    for (int c = 0; c < kKeys / 64; c++) {
+                        float s[4][16];
+                        load(c, s);
 #pragma unroll
-                    for (int h = 0; h < 2; h++) {
+                        for (int h = 0; h < 4; h++) {
+                            uint32_t y[16];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float2 y = unpair(fma2(pair(s[h][e], s[h][e + 1]), unit2, plus2));
-                            s[h][e] = power2(y.x), s[h][e + 1] = power2(y.y);
+                            for (int e = 0; e < 8; e++) {
+                                const float2 z = unpair(fma2(pair(s[h][2 * e], s[h][2 * e + 1]), unit2, plus2));
+                                const float a = power2(z.x), b = power2(z.y);
+                                sums2[e & 1] = add2(sums2[e & 1], pair(a, b));
+                                split<T>(a, b, y[e], y[8 + e]);
+                            }
+                            tmem_store16(at + c * 64 + 16 * h, y);
                         }
-                        if (masked) {
-                            const uint32_t mask = mask_of(c + h);
-#pragma unroll
-                            for (int e = 0; e < 32; e++) s[h][e] = mask >> e & 1 ? s[h][e] : 0.0f;
-                        }
-                        uint32_t y[32];
-#pragma unroll
-                        for (int e = 0; e < 16; e++) {
-                            sums[e & 1] = add2(sums[e & 1], pair(s[h][2 * e], s[h][2 * e + 1]));
-                            split<T>(s[h][2 * e], s[h][2 * e + 1], y[e], y[16 + e]);
-                        }
-                        tmem_store(at + 32 * (c + h), y);
                     }
+                    const float2 z = unpair(add2(sums2[0], sums2[1]));
+                    sum = z.x + z.y;
+                    wait_stores();
+                    fence_before_sync();
+                    bar_arrive(weights_ready(slot));
                 }
-                {
-                    const float2 y = unpair(add2(sums[0], sums[1]));
-                    sum += y.x + y.y;
-                }
-                wait_stores();
-                fence_before_sync();
-                bar_arrive(weights_ready(slot));
-            }
-            if (!fine) break;
-            // -------------------------------------------------------------- end of this CTA's part of a block
-            const bool worked = step_first < steps, has_part = !whole || shared;
-            if (worked || (shared && has_part)) {
-                bool poisoned = false;
+                if (!fine) break;
+                // -------------------------------------------------------------- end of this CTA's part of a block
                 if (worked) {
                     if (!(fine = wait(output_full(i), output_parity))) break;
                     output_parity ^= 1;
                     fence_after_sync();
-#pragma unroll
-                    for (int y = 0; y < S::kLoadWarps; y++) poisoned |= infinite[segment & 3][y] != 0;
                 }
                 constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
                 const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
-                // CTAs that have parts of the block; this one's: the first of its two, unless the block begins here
-                int first_part = blockIdx.x, final_part = blockIdx.x;
-                if (!whole) {
-                    if (work.cut) {
-                        first_part -= start.piece;
-                        final_part = first_part + start.pieces - 1;
-                    } else {
-                        if (w.first_unit < work.first) first_part = (int)divide(w.first_unit, work.share);
-                        if (w.first_unit + k.tiles > work.end) final_part = (int)divide(w.first_unit + k.tiles - 1, work.share);
-                    }
-                }
-                float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
+                // this CTA's part is the first of its two, unless the block begins here
+                float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
                 if (worked) {
-                    if (poisoned) leave_with_infinite<T, C, kKeys>(p, x, k, w.j + step_first, w.j_end, step_by, part, f, sum == 0.0f);
-                    else leave<T>(p, x, part, f, sum == 0.0f);
+                    if (infinite[segment % kSegments]) leave_with_infinite<T, C, kKeys>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
+                    else leave<T, C, kKeys, false>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
                     fence_before_sync();
                 }
                 if (!has_part) {
@@ -1184,33 +1190,33 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     part[DP * 128 + x.row] = add;
                     part[(DP + 1) * 128 + x.row] = sum;
                     __threadfence();
-                    if (!(fine = meet(meeting(i), meeting_parity))) break;
+                    if (!(fine = meet())) break;
                     if (x.row == 0) {
-                        int* const counter = p.counters + first_part * 2 + (shared ? 0 : i);
-                        const bool last = atomicAdd(counter, 1) == (final_part - first_part + 1) * (shared ? 2 : 1) - 1;
+                        int* const counter = p.counters + k.first_part * 2 + (shared ? 0 : i);
+                        const bool last = atomicAdd(counter, 1) == (k.final_part - k.first_part + 1) * (shared ? 2 : 1) - 1;
                         joins[i] = last;
                         if (last) *counter = 0;
                     }
-                    if (!(fine = meet(meeting(i), meeting_parity))) break;
+                    if (!(fine = meet())) break;
                     if (joins[i]) {
                         __threadfence();
                         const int tile = shared ? 0 : i;
                         Parts parts;
-                        parts.first = p.parts + ((2 * (int64_t)first_part + 1) * kTiles + tile) * kPart;
-                        parts.rest = p.parts + ((2 * (int64_t)first_part + 2) * kTiles + tile) * kPart;
+                        parts.first = p.parts + ((2 * (int64_t)k.first_part + 1) * kTiles + tile) * kPart;
+                        parts.rest = p.parts + ((2 * (int64_t)k.first_part + 2) * kTiles + tile) * kPart;
                         parts.stride = 2 * kTiles * kPart;
-                        parts.n = final_part - first_part + 1;
+                        parts.n = k.final_part - k.first_part + 1;
                         join<T, DP>(p, x, parts, shared, vscale);
                     }
                 }
             }
-            step0 += steps, segment++;
-            more = next_block<kKeys>(p, work, w);
+            step0 += steps;
+            leave_segment();
         }
     }
     fence_before_sync();
     __syncthreads();
-    if (warp == S::kWarps - 1) {
+    if (warp == kProductWarp) {
         fence_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kColumns) : "memory");
     }
