@@ -638,7 +638,9 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
     if (row.real) leave_lse(p, row.out, all, least);
 }
 
-// A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.
+// A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.  (One function for each side of the kernel:
+// they have different numbers of registers.)
+template <int SIDE>
 __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile int* stuck, int32_t* status) {
     constexpr int64_t kPatience = 4000000000ll;  // cycles: seconds, where microseconds are usual
     const int64_t began = clock64();
@@ -683,7 +685,9 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     auto output_full = [&](int s) { return rest + 32 + s * 8; };
     auto meeting = [&](int i) { return rest + 48 + i * 8; };
     const uint32_t query_full = rest + 64, query_empty = rest + 72, added = rest + 80, drained = rest + 88;
-    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(~0u, bar_try(bar, parity)) || wait_long(bar, parity, &stuck, p.status); };
+    auto wait_on = [&](auto side, uint32_t bar, uint32_t parity) {
+        return __all_sync(~0u, bar_try(bar, parity)) || wait_long<decltype(side)::value>(bar, parity, &stuck, p.status);
+    };
 
     constexpr int kProductWarp = S::kWarps - 2, kPlanWarp = S::kWarps - 1;
     if (tid == 0) {
@@ -725,16 +729,11 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     __syncthreads();
     fence_after_sync();
     const uint32_t tmem = tmem_at;
-    if constexpr (kTiles == 2) {
-        if (warp >= S::kSoftmaxWarps) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegisters));
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegisters));
-    }
-
     const int heads_a_tile = p.heads_a_tile;
     int segment = 0;
     bool fine = true;
     // the next segment; false at the end
-    auto next_segment = [&]() {
+    auto next_segment = [&](auto& wait) {
         if (!(fine = wait(told_of(segment % kSegments), segment / kSegments & 1))) return false;
         return segments[segment % kSegments].steps > 0;
     };
@@ -744,286 +743,10 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         segment++;
     };
 
-    if (warp == kPlanWarp) {
-        // ------------------------------------------------------------------------------------------ the walk
-        if (p.n_requests <= 32) work = plan<kKeys>(p, start, sums, 0, 1);
-        __syncwarp();
-        Walk w = start;
-        bool more = w.left > 0;
-        if (more) w.j_end = (int)min((int64_t)w.block.tiles, w.j + w.left);
-        while (true) {
-            const int s = segment % kSegments;
-            if (segment >= kSegments && !wait(done_with(s), (segment / kSegments - 1) & 1)) break;
-            if (lane == 0) {
-                Segment& k = segments[s];
-                k.steps = 0;
-                if (more) {
-                    const Block& b = w.block;
-                    const int at = b.b * p.tokens_a_block;
-                    k.r = b.r, k.kv = b.kv, k.ht = b.ht, k.row = b.row0 + at, k.tokens = b.tokens;
-                    k.position = b.position0 + at - b.gap, k.gap = b.gap, k.seen = b.seen;
-                    k.j = w.j, k.steps = w.j_end - w.j;
-                    k.tiles_in_use = kTiles == 2 && b.tokens * heads_a_tile > 128 ? 2 : 1;
-                    k.whole = w.j == 0 && w.j_end == b.tiles;
-                    k.shared = kTiles == 2 && k.tiles_in_use == 1 && (!k.whole || k.steps >= kSharedLeast);
-                    k.first_part = k.final_part = blockIdx.x;
-                    if (!k.whole) {
-                        if (work.cut) {
-                            k.first_part -= w.piece;
-                            k.final_part = k.first_part + w.pieces - 1;
-                        } else {
-                            if (w.first_unit < work.first) k.first_part = (int)divide(w.first_unit, work.share);
-                            if (w.first_unit + b.tiles > work.end) k.final_part = (int)divide(w.first_unit + b.tiles - 1, work.share);
-                        }
-                    }
-                }
-                infinite[s] = 0;
-                bar_arrive(told_of(s));
-            }
-            segment++;
-            if (!more) break;
-            more = next_block<kKeys>(p, work, w);
-        }
-    } else if (warp == kProductWarp) {
-        // ------------------------------------------------------------------------------------------ products
-        constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
-        const uint32_t depth = uni((D + 15) / 16), base = uni(tmem);
-        const uint32_t how_output = instruction(kType, true, 128, depth * 16);
-        const uint64_t query_operand = operand(uni(query), 16, 1024), key_operand = operand(uni(ring), 16, 1024), value_operand = operand(uni(ring), kKeys * 128, 1024);
-        int tile0 = 0;
-        uint32_t ready[2] = {0, 0};  // parities of the weights
-        while (next_segment()) {
-            const Segment& k = segments[segment % kSegments];
-            const int n = k.tiles_in_use, steps = k.steps;
-            // With two tiles of rows, tile after tile: the output of a step, then the scores of the next (K0 V0 K1 V1 ..).  With one, the scores
-            // run a step ahead, in the two areas in turn (K0 K1 V0 K2 V1 ..).  Both are a row of outputs, each followed by the scores of the
-            // output `lead` later.
-            const bool ahead = kTiles == 1 || k.shared;
-            const int outputs = ahead ? steps : steps * n, lead = ahead ? min(2, steps) : n, wide = ahead ? 0 : n - 1;
-            // a negative scale turns the order of the logits around: Q is taken as -Q instead
-            const float scale = kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale;
-            const uint32_t how_score = instruction(kType, false, 128, kKeys) | uni(scale < 0) << 13;
-            if (!(fine = wait(query_full, segment & 1))) break;
-            auto wait_tile = [&](int x) {  // tile x of the segment is there
-                const int t = tile0 + x;
-                if (!wait(full(t % kStages), (t / kStages) & 1)) return false;
-                fence_after_sync();
-                return true;
-            };
-#pragma unroll 1
-            for (int q = -lead; q < outputs; q++) {
-                if (q >= 0) {
-                    const int j = q >> wide, i = ahead ? q & 1 : q & wide, x = !ahead ? 2 * j + 1 : j + 1 < steps ? 2 * j + 2 : 2 * j + 1;
-                    if ((ahead || i == 0) && !(fine = wait_tile(x))) break;
-                    if (!(fine = wait(weights_ready(i), ready[i]))) break;
-                    ready[i] ^= 1;
-                    fence_after_sync();
-                    const int o = kTiles == 1 ? 0 : i, first = kTiles == 2 && ahead ? 2 : 1;
-                    const uint32_t s = uni((tile0 + x) % kStages), more_of = uni(j >= first), to = uni(base + S::kOutput + o * DP), from = uni(base + S::kScore + i * kKeys);
-                    const uint64_t b = value_operand + s * (S::kStage >> 4);
-                    const bool releases = ahead || i == n - 1, ends = kTiles == 1 ? j + 1 == steps : ahead ? j + 2 >= steps : j + 1 == steps;
-                    if (elected()) {
-#pragma unroll
-                        for (int part = 0; part < 2; part++)
-#pragma unroll
-                            for (int y = 0; y < kKeys / 16; y++)
-                                product_from_tmem(to, from + y * 16 + part * 8, b + (y * 2048 >> 4), how_output, part > 0 || y > 0 ? 1u : more_of);
-                        if (releases) commit_products(empty(s));
-                        if (kTiles == 1) commit_products(added);
-                        if (ends) commit_products(output_full(o));
-                    }
-                }
-                const int next = q + lead;
-                if (next < outputs) {
-                    const int j = next >> wide, i = ahead ? next & 1 : next & wide, x = !ahead ? 2 * j : j == 0 ? 0 : 2 * j - 1;
-                    if ((ahead || i == 0) && !(fine = wait_tile(x))) break;
-                    const uint32_t s = uni((tile0 + x) % kStages), to = uni(base + S::kScore + i * kKeys), rows = uni(ahead ? 0 : i);
-                    const uint64_t a = query_operand + rows * (128 * DP * 2 >> 4), b = key_operand + s * (S::kStage >> 4);
-                    const bool releases = ahead || i == n - 1;
-                    if (elected()) {
-#pragma unroll
-                        for (int y = 0; y < DP / 16; y++)
-                            if (y < depth) product(to, a + ((y / 4 * (128 * 128) + y % 4 * 32) >> 4), b + ((y / 4 * (kKeys * 128) + y % 4 * 32) >> 4), how_score, y > 0);
-                        commit_products(score_full(i));
-                        if (releases) commit_products(empty(s));
-                        if (next + 1 == outputs) commit_products(query_empty);
-                    }
-                }
-            }
-            if (!fine) break;
-            tile0 += 2 * steps;
-            leave_segment();
-        }
-        if (elected()) commit_products(drained);  // nothing is in flight when the CTA ends
-        const int64_t began = clock64();
-        while (!bar_try(drained, 0) && clock64() - began < 4000000000ll) {}
-    } else if (warp >= S::kSoftmaxWarps) {
-        // ------------------------------------------------------------------------------------------ loads
-        // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own
-        // copies while the others' are on their way.
-        const int me = warp - S::kSoftmaxWarps;
-        constexpr int kLanes = DP * C::bytes / 16, kAtOnce = 32 / kLanes, kHalf = kKeys / 2, kRounds = kHalf / kAtOnce;  // lanes of a row, rows at once
-        constexpr int kOffs = kHalf / 32, kBatch = kRounds < 8 ? kRounds : 8;
-        const int chunk = lane % kLanes, lane_row = lane / kLanes, chunks = D * C::bytes / 16;
-        const bool copies = chunk < chunks;
-        const uint32_t token_magic = (65536 + heads_a_tile - 1) / heads_a_tile;  // row / heads_a_tile for rows below 256
-        int tile0 = 0, step0 = 0;  // tiles and steps of the segments before this one
-        // place in a stage of 16 bytes of a row
-        auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
-        while (next_segment()) {
-            const Segment& k = segments[segment % kSegments];
-            const int steps = k.steps, halves = 4 * steps;
-            // tile x of the segment
-            const bool ahead = kTiles == 1 || k.shared;
-            auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
-            auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
-            int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
-            uint32_t next_bad = 0;     // which of them are in a page outside the pool
-            int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps, fetched = -1;  // this warp's first half
-            // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
-            // are left by tiles of blocks before.)
-            bool query_due = true;
-#pragma unroll 1
-            while (query_due || h < halves) {
-                const bool loads = h < (query_due ? min(4, halves) : halves);
-                const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = k.j + step_of(x);
-                const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
-                const bool key = is_key(x), edge = !key && partly_seen(p, k, j * kKeys, kKeys);
-                const char* const pool = key ? p.pool.k : p.pool.v;
-                bool found = false;
-                if (loads) {
-                    int64_t off[kOffs];
-#pragma unroll 1
-                    for (int again = 0; again < 2; again++) {  // the pages of this half, if they are not at hand, and of the next
-                        const int y = again ? h + S::kLoadWarps : h;
-                        if (again) {
-#pragma unroll
-                            for (int c = 0; c < kOffs; c++) off[c] = next_off[c];
-                            if (key) {
-#pragma unroll
-                                for (int c = 0; c < kOffs; c++) {
-                                    const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
-                                    if (lane == 0) {
-                                        valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
-                                        if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
-                                    }
-                                }
-                            }
-                        }
-                        if (fetched >= y || y >= halves) continue;
-                        fetched = y;
-                        next_bad = 0;
-#pragma unroll
-                        for (int c = 0; c < kOffs; c++) {
-                            const int u = (k.j + step_of(y / 2)) * kKeys + y % 2 * kHalf + c * 32 + lane;
-                            next_off[c] = -1;
-                            if (u < k.seen) {
-                                const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
-                                if ((unsigned)page < (unsigned)p.pool.n_pages)
-                                    next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
-                                else
-                                    next_bad |= 1u << c;
-                            }
-                        }
-                    }
-                    if (tile >= kStages && !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
-                    if constexpr (kNarrow) {
-#pragma unroll 1
-                        for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
-                            uint4 raw[kBatch];
-                            const int row0 = i0 * kAtOnce + lane_row;
-                            constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
-                            int64_t mine[kHere];
-#pragma unroll
-                            for (int y = 0; y < kHere; y++) {
-                                mine[y] = off[y];
-#pragma unroll
-                                for (int c = 1; c < kOffs; c++)
-                                    if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
-                            }
-#pragma unroll
-                            for (int i = 0; i < kBatch; i++) {
-                                const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
-                                raw[i] = make_uint4(0, 0, 0, 0);
-                                if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
-                            }
-                            if (copies) {
-#pragma unroll
-                                for (int i = 0; i < kBatch; i++) {
-                                    const int row = row0 + i * kAtOnce;
-                                    uint4 a, b;
-                                    widen<T>(raw[i], a, b);
-                                    store16(to + place(row, 2 * chunk), a);
-                                    store16(to + place(row, 2 * chunk + 1), b);
-                                }
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < kOffs; c++) {
-#pragma unroll 8
-                            for (int i = 0; i < kRounds / kOffs; i++) {
-                                const int row = i * kAtOnce + lane_row;
-                                const int64_t o = __shfl_sync(~0u, off[c], row);
-                                if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
-                            }
-                        }
-                    }
-                }
-                commit_copies();
-                if (query_due) {
-                    if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
-                    constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
-                    const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
-#pragma unroll 1
-                    for (int r0 = me * 16; r0 < k.tiles_in_use * 128; r0 += 16 * S::kLoadWarps) {
-                        const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
-                        int64_t off = -1;
-                        if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
-#pragma unroll
-                        for (int i = 0; i < 16 / kQueryRows; i++) {
-                            const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
-                            const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                            if (at < D / 8)
-                                copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
-                                       p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
-                        }
-                    }
-                    commit_copies();
-                    wait_copies<1>();
-                } else
-                    wait_copies<0>();
-                if (loads) {
-                    if (edge && (kNarrow ? 2 * chunk < D / 8 : copies)) {
-                        // what some row does not see must not meet its weight of zero as an infinity or NaN
-#pragma unroll 4
-                        for (int i = 0; i < kRounds * (kNarrow ? 2 : 1); i++) {
-                            const uint32_t at = to + (kNarrow ? place(i / 2 * kAtOnce + lane_row, 2 * chunk + i % 2) : place(i * kAtOnce + lane_row, chunk));
-                            uint4 y = load16(at);
-                            if (make_finite<T>(y)) {
-                                store16(at, y);
-                                found = true;
-                            }
-                        }
-                    }
-                    if (found) infinite[segment % kSegments] = 1;
-                    fence_for_products();
-                    bar_arrive(full(s));
-                    h += S::kLoadWarps;
-                }
-                if (query_due) {
-                    wait_copies<0>();
-                    fence_for_products();
-                    bar_arrive(query_full);
-                    query_due = false;
-                }
-            }
-            if (!fine) break;
-            tile0 += 2 * steps, step0 += steps;
-            leave_segment();
-        }
-        wait_copies<0>();
-    } else {
+    // (each side leaves or takes its registers in a branch of its own: what comes before both is compiled for the fewer)
+    if (warp < S::kSoftmaxWarps) {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegisters));
+        auto wait = [&](uint32_t bar, uint32_t parity) { return wait_on(std::integral_constant<int, 0>(), bar, parity); };
         // ------------------------------------------------------------------------------------------ softmax
         // rows that belong to no request, and what is wrong with the requests
         {
@@ -1062,7 +785,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             meeting_parity ^= 1;
             return ok;
         };
-        while (next_segment()) {
+        while (next_segment(wait)) {
             const Segment& k = segments[segment % kSegments];
             const int steps = k.steps;
             const bool shared = k.shared, whole = k.whole;
@@ -1212,6 +935,288 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             }
             step0 += steps;
             leave_segment();
+        }
+    } else {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kOtherRegisters));
+        auto wait = [&](uint32_t bar, uint32_t parity) { return wait_on(std::integral_constant<int, 1>(), bar, parity); };
+        if (warp == kPlanWarp) {
+            // ------------------------------------------------------------------------------------------ the walk
+            if (p.n_requests <= 32) work = plan<kKeys>(p, start, sums, 0, 1);
+            __syncwarp();
+            Walk w = start;
+            bool more = w.left > 0;
+            if (more) w.j_end = (int)min((int64_t)w.block.tiles, w.j + w.left);
+            while (true) {
+                const int s = segment % kSegments;
+                if (segment >= kSegments && !wait(done_with(s), (segment / kSegments - 1) & 1)) break;
+                if (lane == 0) {
+                    Segment& k = segments[s];
+                    k.steps = 0;
+                    if (more) {
+                        const Block& b = w.block;
+                        const int at = b.b * p.tokens_a_block;
+                        k.r = b.r, k.kv = b.kv, k.ht = b.ht, k.row = b.row0 + at, k.tokens = b.tokens;
+                        k.position = b.position0 + at - b.gap, k.gap = b.gap, k.seen = b.seen;
+                        k.j = w.j, k.steps = w.j_end - w.j;
+                        k.tiles_in_use = kTiles == 2 && b.tokens * heads_a_tile > 128 ? 2 : 1;
+                        k.whole = w.j == 0 && w.j_end == b.tiles;
+                        k.shared = kTiles == 2 && k.tiles_in_use == 1 && (!k.whole || k.steps >= kSharedLeast);
+                        k.first_part = k.final_part = blockIdx.x;
+                        if (!k.whole) {
+                            if (work.cut) {
+                                k.first_part -= w.piece;
+                                k.final_part = k.first_part + w.pieces - 1;
+                            } else {
+                                if (w.first_unit < work.first) k.first_part = (int)divide(w.first_unit, work.share);
+                                if (w.first_unit + b.tiles > work.end) k.final_part = (int)divide(w.first_unit + b.tiles - 1, work.share);
+                            }
+                        }
+                    }
+                    infinite[s] = 0;
+                    bar_arrive(told_of(s));
+                }
+                segment++;
+                if (!more) break;
+                more = next_block<kKeys>(p, work, w);
+            }
+        } else if (warp == kProductWarp) {
+            // ------------------------------------------------------------------------------------------ products
+            constexpr uint32_t kType = std::is_same<T, F16>::value ? 0 : 1;
+            const uint32_t depth = uni((D + 15) / 16), base = uni(tmem);
+            const uint32_t how_output = instruction(kType, true, 128, depth * 16);
+            const uint64_t query_operand = operand(uni(query), 16, 1024), key_operand = operand(uni(ring), 16, 1024), value_operand = operand(uni(ring), kKeys * 128, 1024);
+            // What decides the way through the loop is in registers of the warp, and few instructions stand between a wait and the products that
+            // it lets go: with 200 clocks of them for each tile the tensor core stood idle 40 % of the time.
+            uint32_t stage = 0, phase = 0, ready = 0;  // of the ring: the next tile; parities of the weights, a bit each
+            uint32_t key_stage = 0, value_stage = 0;
+            auto next_tile = [&](uint32_t& at) {  // the next tile of the ring is there
+                if (!wait(full(stage), phase)) return false;
+                fence_after_sync();
+                at = stage;
+                if (++stage == kStages) stage = 0, phase ^= 1;
+                return true;
+            };
+            while (next_segment(wait)) {
+                const Segment& k = segments[segment % kSegments];
+                const uint32_t steps = uni(k.steps), n = uni(k.tiles_in_use);
+                // With two tiles of rows, tile after tile: the output of a step, then the scores of the next (K0 V0 K1 V1 ..).  With one, the scores
+                // run a step ahead, in the two areas in turn (K0 K1 V0 K2 V1 ..).  Both are a row of outputs, each followed by the scores of the
+                // output `lead` later.
+                const uint32_t ahead = kTiles == 1 ? 1u : uni(k.shared), both = 1 - ahead & n - 1;
+                const uint32_t outputs = steps << both, lead = ahead ? min(2u, steps) : n;
+                // a negative scale turns the order of the logits around: Q is taken as -Q instead
+                const float scale = kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale;
+                const uint32_t how_score = instruction(kType, false, 128, kKeys) | uni(scale < 0) << 13;
+                if (!(fine = wait(query_full, segment & 1))) break;
+#pragma unroll 1
+                for (uint32_t q = 0; q < outputs + lead; q++) {  // scores of output q, behind the products of output q - lead
+                    if (q >= lead) {
+                        const uint32_t w = q - lead, i = ahead ? w & 1 : w & both;
+                        if ((!both || i == 0) && !(fine = next_tile(value_stage))) break;
+                        const uint32_t o = kTiles == 1 ? 0 : i, j = w >> both, more_of = j >= (kTiles == 2 && ahead ? 2 : 1);
+                        const uint32_t to = base + S::kOutput + o * DP, from = base + S::kScore + i * kKeys;
+                        const uint64_t b = value_operand + value_stage * (S::kStage >> 4);
+                        if (!(fine = wait(weights_ready(i), ready >> i & 1))) break;
+                        ready ^= 1u << i;
+                        fence_after_sync();
+                        if (elected()) {
+#pragma unroll
+                            for (int y = 0; y < kKeys / 16; y++)
+#pragma unroll
+                                for (int part = 0; part < 2; part++)
+                                    product_from_tmem(to, from + y * 16 + part * 8, b + (y * 2048 >> 4), how_output, part > 0 || y > 0 ? 1u : more_of);
+                            if (!both || i == 1) commit_products(empty(value_stage));
+                            if (kTiles == 1) commit_products(added);
+                            if (kTiles == 2 && ahead ? w + 2 >= outputs : j + 1 == steps) commit_products(output_full(o));
+                        }
+                    }
+                    if (q < outputs) {
+                        const uint32_t i = ahead ? q & 1 : q & both;
+                        if ((!both || i == 0) && !(fine = next_tile(key_stage))) break;
+                        const uint32_t to = base + S::kScore + i * kKeys;
+                        const uint64_t a = query_operand + (ahead ? 0 : i) * (128 * DP * 2 >> 4), b = key_operand + key_stage * (S::kStage >> 4);
+                        if (elected()) {
+#pragma unroll
+                            for (int y = 0; y < DP / 16; y++)
+                                if (y < depth) product(to, a + ((y / 4 * (128 * 128) + y % 4 * 32) >> 4), b + ((y / 4 * (kKeys * 128) + y % 4 * 32) >> 4), how_score, y > 0);
+                            commit_products(score_full(i));
+                            if (!both || i == 1) commit_products(empty(key_stage));
+                            if (q + 1 == outputs) commit_products(query_empty);
+                        }
+                    }
+                }
+                if (!fine) break;
+                leave_segment();
+            }
+            if (elected()) commit_products(drained);  // nothing is in flight when the CTA ends
+            const int64_t began = clock64();
+            while (!bar_try(drained, 0) && clock64() - began < 4000000000ll) {}
+        } else if (warp >= S::kSoftmaxWarps) {
+            // ------------------------------------------------------------------------------------------ loads
+            // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own
+            // copies while the others' are on their way.
+            const int me = warp - S::kSoftmaxWarps;
+            constexpr int kLanes = DP * C::bytes / 16, kAtOnce = 32 / kLanes, kHalf = kKeys / 2, kRounds = kHalf / kAtOnce;  // lanes of a row, rows at once
+            constexpr int kOffs = kHalf / 32, kBatch = kRounds < 8 ? kRounds : 8;
+            const int chunk = lane % kLanes, lane_row = lane / kLanes, chunks = D * C::bytes / 16;
+            const bool copies = chunk < chunks;
+            const uint32_t token_magic = (65536 + heads_a_tile - 1) / heads_a_tile;  // row / heads_a_tile for rows below 256
+            int tile0 = 0, step0 = 0;  // tiles and steps of the segments before this one
+            // place in a stage of 16 bytes of a row
+            auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
+            while (next_segment(wait)) {
+                const Segment& k = segments[segment % kSegments];
+                const int steps = k.steps, halves = 4 * steps;
+                // tile x of the segment
+                const bool ahead = kTiles == 1 || k.shared;
+                auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
+                auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
+                int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
+                uint32_t next_bad = 0;     // which of them are in a page outside the pool
+                int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps, fetched = -1;  // this warp's first half
+                // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
+                // are left by tiles of blocks before.)
+                bool query_due = true;
+#pragma unroll 1
+                while (query_due || h < halves) {
+                    const bool loads = h < (query_due ? min(4, halves) : halves);
+                    const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = k.j + step_of(x);
+                    const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
+                    const bool key = is_key(x), edge = !key && partly_seen(p, k, j * kKeys, kKeys);
+                    const char* const pool = key ? p.pool.k : p.pool.v;
+                    bool found = false;
+                    if (loads) {
+                        int64_t off[kOffs];
+#pragma unroll 1
+                        for (int again = 0; again < 2; again++) {  // the pages of this half, if they are not at hand, and of the next
+                            const int y = again ? h + S::kLoadWarps : h;
+                            if (again) {
+#pragma unroll
+                                for (int c = 0; c < kOffs; c++) off[c] = next_off[c];
+                                if (key) {
+#pragma unroll
+                                    for (int c = 0; c < kOffs; c++) {
+                                        const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
+                                        if (lane == 0) {
+                                            valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
+                                            if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
+                                        }
+                                    }
+                                }
+                            }
+                            if (fetched >= y || y >= halves) continue;
+                            fetched = y;
+                            next_bad = 0;
+#pragma unroll
+                            for (int c = 0; c < kOffs; c++) {
+                                const int u = (k.j + step_of(y / 2)) * kKeys + y % 2 * kHalf + c * 32 + lane;
+                                next_off[c] = -1;
+                                if (u < k.seen) {
+                                    const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                                    if ((unsigned)page < (unsigned)p.pool.n_pages)
+                                        next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
+                                    else
+                                        next_bad |= 1u << c;
+                                }
+                            }
+                        }
+                        if (tile >= kStages && !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
+                        if constexpr (kNarrow) {
+#pragma unroll 1
+                            for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
+                                uint4 raw[kBatch];
+                                const int row0 = i0 * kAtOnce + lane_row;
+                                constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
+                                int64_t mine[kHere];
+#pragma unroll
+                                for (int y = 0; y < kHere; y++) {
+                                    mine[y] = off[y];
+#pragma unroll
+                                    for (int c = 1; c < kOffs; c++)
+                                        if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
+                                }
+#pragma unroll
+                                for (int i = 0; i < kBatch; i++) {
+                                    const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
+                                    raw[i] = make_uint4(0, 0, 0, 0);
+                                    if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
+                                }
+                                if (copies) {
+#pragma unroll
+                                    for (int i = 0; i < kBatch; i++) {
+                                        const int row = row0 + i * kAtOnce;
+                                        uint4 a, b;
+                                        widen<T>(raw[i], a, b);
+                                        store16(to + place(row, 2 * chunk), a);
+                                        store16(to + place(row, 2 * chunk + 1), b);
+                                    }
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < kOffs; c++) {
+#pragma unroll 8
+                                for (int i = 0; i < kRounds / kOffs; i++) {
+                                    const int row = i * kAtOnce + lane_row;
+                                    const int64_t o = __shfl_sync(~0u, off[c], row);
+                                    if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
+                                }
+                            }
+                        }
+                    }
+                    commit_copies();
+                    if (query_due) {
+                        if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
+                        constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
+                        const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
+#pragma unroll 1
+                        for (int r0 = me * 16; r0 < k.tiles_in_use * 128; r0 += 16 * S::kLoadWarps) {
+                            const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
+                            int64_t off = -1;
+                            if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
+#pragma unroll
+                            for (int i = 0; i < 16 / kQueryRows; i++) {
+                                const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
+                                const int y = r0 + i * kQueryRows + lane / kQueryLanes;
+                                if (at < D / 8)
+                                    copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
+                                           p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
+                            }
+                        }
+                        commit_copies();
+                        wait_copies<1>();
+                    } else
+                        wait_copies<0>();
+                    if (loads) {
+                        if (edge && (kNarrow ? 2 * chunk < D / 8 : copies)) {
+                            // what some row does not see must not meet its weight of zero as an infinity or NaN
+#pragma unroll 4
+                            for (int i = 0; i < kRounds * (kNarrow ? 2 : 1); i++) {
+                                const uint32_t at = to + (kNarrow ? place(i / 2 * kAtOnce + lane_row, 2 * chunk + i % 2) : place(i * kAtOnce + lane_row, chunk));
+                                uint4 y = load16(at);
+                                if (make_finite<T>(y)) {
+                                    store16(at, y);
+                                    found = true;
+                                }
+                            }
+                        }
+                        if (found) infinite[segment % kSegments] = 1;
+                        fence_for_products();
+                        bar_arrive(full(s));
+                        h += S::kLoadWarps;
+                    }
+                    if (query_due) {
+                        wait_copies<0>();
+                        fence_for_products();
+                        bar_arrive(query_full);
+                        query_due = false;
+                    }
+                }
+                if (!fine) break;
+                tile0 += 2 * steps, step0 += steps;
+                leave_segment();
+            }
+            wait_copies<0>();
         }
     }
     fence_before_sync();
