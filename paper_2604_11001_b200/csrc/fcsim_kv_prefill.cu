@@ -85,14 +85,6 @@ __device__ __forceinline__ void tmem_load(uint32_t at, float (&x)[32]) {
           "=f"(x[31])
         : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&x)[8]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&x)[8]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
-}
 __device__ __forceinline__ void tmem_load16(uint32_t at, float (&x)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -159,9 +151,9 @@ struct Shape {
     static constexpr int kKeys = DP <= 128 ? 128 : 64;  // of a tile
     static constexpr int kQuery = kRows * DP * 2;       // bytes
     static constexpr int kStage = kKeys * DP * 2;       // of K or V
-    static constexpr int kRoom = (227 * 1024 - 2048 - 1024 - kQuery) / kStage;
+    static constexpr int kRoom = (227 * 1024 - 3072 - kQuery) / kStage;  // (beside what the kernel keeps itself)
     static constexpr int kStages = kRoom < 8 ? kRoom : 8;
-    static constexpr int kBytes = kQuery + kStages * kStage + 1024;
+    static constexpr int kBytes = kQuery + kStages * kStage;
     static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 6;
     static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 2, kThreads = 32 * kWarps;
     // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's.
@@ -179,6 +171,8 @@ struct Shape {
 // Cost of a block's start and end beside one tile of keys.
 constexpr int kOverhead = 2;
 constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are cut
+// Tiles by which the longest piece may exceed an equal share: what the joins of shares cost.
+constexpr int kShareCost = 4;
 // A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and
 // their outputs are joined as those of different CTAs are.
 constexpr int kSharedLeast = 6;
@@ -304,33 +298,39 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, in
 #pragma unroll 1
     for (int pass = 0; pass < 2; pass++) {  // tiles; with `cut` also pieces
         int64_t units = 0, blocks = 0;
+        int longest = 0;
 #pragma unroll 1
         for (int base = r0; base < r1; base += 32) {
             enter(base + lane);
             units += add_blocks<KEYS>(p, rows, position0, pass ? d.cut : 0, 0);
-            blocks += blocks_of(p, rows);
+            const int n = blocks_of(p, rows);
+            blocks += n;
+            if (n > 0) longest = max(longest, tiles_of<KEYS>(p, position0, rows, n - 1));
         }
-        units = warp_sum(units), blocks = warp_sum(blocks);
+        units = warp_sum(units), blocks = warp_sum(blocks), longest = __reduce_max_sync(~0u, longest);
         all[0] = units, all[1] = blocks;
         if (warps > 1) {
             __syncthreads();
-            if (lane == 0) sums[0][me] = units, sums[1][me] = blocks;
+            if (lane == 0) sums[0][me] = units, sums[1][me] = blocks, sums[2][me] = longest;
             __syncthreads();
             all[0] = all[1] = 0;
 #pragma unroll 1
-            for (int w = 0; w < warps; w++) all[0] += sums[0][w], all[1] += sums[1][w];
+            for (int w = 0; w < warps; w++) all[0] += sums[0][w], all[1] += sums[1][w], longest = max(longest, (int)sums[2][w]);
         }
         if (pass) {
             total = all[0] * heads;
             break;
         }
-        if (all[1] * heads > gridDim.x) {
-            total = (all[0] + kOverhead * all[1]) * heads;
-            d.share = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x));
-            break;
+        // Pieces that fit the grid, if there are as few blocks and that leaves none much longer than an equal share.
+        if (all[1] * heads <= gridDim.x) {
+            const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);
+            d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
+            if (min(d.cut, longest) <= divide(all[0] * heads, gridDim.x) + kShareCost) continue;
+            d.cut = 0;
         }
-        const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);  // so that the pieces fit the grid
-        d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
+        total = (all[0] + kOverhead * all[1]) * heads;
+        d.share = max((int64_t)1, divide(total + gridDim.x - 1, gridDim.x));
+        break;
     }
     const int over = d.cut ? 0 : kOverhead;
     d.first = min(total, (int64_t)blockIdx.x * d.share), d.end = min(total, d.first + d.share);
@@ -578,9 +578,9 @@ __device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, cons
                     }
                 }
         }
-        if (part) {
+        if (part) {  // fours of columns
 #pragma unroll
-            for (int e = 0; e < 32; e++) part[(c * 32 + e) * 128 + x.row] = o[e];
+            for (int e = 0; e < 32; e += 4) reinterpret_cast<float4*>(part)[(c * 8 + e / 4) * 128 + x.row] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         } else if (x.real)
             store_columns<T>(p, x.out, c, o, f, none);
     }
@@ -618,20 +618,34 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
         all += (a == INFINITY ? 0.0f : power2(least - a)) * __ldcg(part(x) + (DP + 1) * 128 + row.row);
     }
     const float f = all == 0.0f ? 0.0f : vscale / all;
+    // They come from L2 at a microsecond each, so four parts are asked for at once.
 #pragma unroll 1
     for (int c = 0; c * 32 < p.pool.head_dim; c++) {
         float o[32] = {};
 #pragma unroll 1
-        for (int x = 0; x < n; x++) {
-            const float* const from = part(x);
-            const float a = __ldcg(from + DP * 128 + row.row);
-            if (__all_sync(~0u, a == INFINITY)) continue;  // (a part without a tile has no output)
-            const float y = a == INFINITY ? 0.0f : power2(least - a);
-            float z[32];
+        for (int x0 = 0; x0 < n; x0 += 4) {
+            float4 z[4][4];
+            float y[4];
 #pragma unroll
-            for (int e = 0; e < 32; e++) z[e] = __ldcg(from + (c * 32 + e) * 128 + row.row);
+            for (int h = 0; h < 2; h++) {
 #pragma unroll
-            for (int e = 0; e < 32; e++) o[e] += y * z[e];
+                for (int x = 0; x < 4; x++) {
+                    const bool there = x0 + x < n;
+                    const float* const from = part(there ? x0 + x : x0);
+                    const float a = there ? __ldcg(from + DP * 128 + row.row) : INFINITY;
+                    y[x] = a == INFINITY ? 0.0f : power2(least - a);
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        z[x][e] = a == INFINITY ? make_float4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const float4*>(from) + (c * 8 + h * 4 + e) * 128 + row.row);  // (a part without a tile has no output)
+                }
+#pragma unroll
+                for (int x = 0; x < 4; x++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        float* const to = o + 16 * h + 4 * e;
+                        to[0] += y[x] * z[x][e].x, to[1] += y[x] * z[x][e].y, to[2] += y[x] * z[x][e].z, to[3] += y[x] * z[x][e].w;
+                    }
+            }
         }
         if (row.real) store_columns<T>(p, row.out, c, o, f, all == 0.0f);
     }
@@ -663,17 +677,17 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     constexpr int kTiles = S::kTiles, kKeys = S::kKeys, kStages = S::kStages, kSegments = 4;
     constexpr bool kNarrow = C::bytes == 1;
     constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f;
-    extern __shared__ char raw_smem[];
+    extern __shared__ __align__(1024) char raw_smem[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 12];
     __shared__ uint32_t tmem_at, valid[8][4];
     __shared__ int stuck, infinite[kSegments], joins[kTiles];
     __shared__ Walk start;
     __shared__ Segment segments[kSegments];
-    __shared__ int64_t sums[2][16];
+    __shared__ int64_t sums[3][16];
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int D = p.pool.head_dim, group = p.n_heads / p.pool.n_kv;
-    const uint32_t smem = (smem_address(raw_smem) + 1023) & ~1023u, query = smem, ring = smem + S::kQuery;
+    const uint32_t smem = smem_address(raw_smem), query = smem, ring = smem + S::kQuery;
     const uint32_t bar0 = smem_address(bars);
     auto full = [&](int s) { return bar0 + s * 8; };
     auto empty = [&](int s) { return bar0 + (kStages + s) * 8; };
@@ -855,13 +869,18 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                             if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
                             fence_after_sync();
 #pragma unroll 1
-                            for (int c = 0; c * 8 < D; c++) {
-                                uint32_t y[8];
-                                tmem_load8(x.at + 8 * c, y);
+                            for (int c = 0; c * 32 < D; c++) {
+                                float o[2][16];
+                                tmem_load16(x.at + 32 * c, o[0]);
+                                tmem_load16(x.at + 32 * c + 16, o[1]);
                                 wait_loads();
 #pragma unroll
-                                for (int e = 0; e < 8; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * shrink);
-                                tmem_store8(x.at + 8 * c, y);
+                                for (int h = 0; h < 2; h++) {
+                                    uint32_t y[16];
+#pragma unroll
+                                    for (int e = 0; e < 16; e++) y[e] = __float_as_uint(o[h][e] * shrink);
+                                    tmem_store16(x.at + 32 * c + 16 * h, y);
+                                }
                             }
                         }
                     }
@@ -1053,120 +1072,152 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             while (!bar_try(drained, 0) && clock64() - began < 4000000000ll) {}
         } else if (warp >= S::kSoftmaxWarps) {
             // ------------------------------------------------------------------------------------------ loads
-            // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps: a warp waits for its own
-            // copies while the others' are on their way.
+            // Halves of the tiles of K and V in the order in which they are used, one after the other to these warps.  A warp keeps two on their
+            // way: it waits for the copies of one when those of the next are asked for, unless there is no place yet for the next.
             const int me = warp - S::kSoftmaxWarps;
             constexpr int kLanes = DP * C::bytes / 16, kAtOnce = 32 / kLanes, kHalf = kKeys / 2, kRounds = kHalf / kAtOnce;  // lanes of a row, rows at once
-            constexpr int kOffs = kHalf / 32, kBatch = kRounds < 8 ? kRounds : 8;
+            constexpr int kOffs = kHalf / 32;
             const int chunk = lane % kLanes, lane_row = lane / kLanes, chunks = D * C::bytes / 16;
             const bool copies = chunk < chunks;
             const uint32_t token_magic = (65536 + heads_a_tile - 1) / heads_a_tile;  // row / heads_a_tile for rows below 256
             int tile0 = 0, step0 = 0;  // tiles and steps of the segments before this one
-            // place in a stage of 16 bytes of a row
+            // Place in a stage of 16 bytes of a row.  8-bit rows come into the upper half of the place of a row, 16 bytes to where 8 elements will be, and become
+            // 16-bit ones from there.
             auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
+            constexpr int kRaw = kNarrow ? DP / 16 : 0;
             while (next_segment(wait)) {
                 const Segment& k = segments[segment % kSegments];
-                const int steps = k.steps, halves = 4 * steps;
+                const int steps = k.steps, halves = 4 * steps, gap = k.gap, seen = k.seen;
+                const int32_t* const table = p.table + k.r * p.table_row;
+                const int64_t head = k.kv * p.pool.stride_head;
                 // tile x of the segment
                 const bool ahead = kTiles == 1 || k.shared;
                 auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
                 auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
-                int64_t next_off[kOffs];   // of the rows of this lane's tokens (lane, lane + 32, ..) in the half that is loaded next, or -1
-                uint32_t next_bad = 0;     // which of them are in a page outside the pool
-                int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps, fetched = -1;  // this warp's first half
+                // pages of this lane's tokens (lane, lane + 32) of a half: asked for long before they are used
+                int pages[kOffs];
+                auto fetch_pages = [&](int h) {
+#pragma unroll
+                    for (int c = 0; c < kOffs; c++) {
+                        const int u = (k.j + step_of(h / 2)) * kKeys + h % 2 * kHalf + c * 32 + lane;
+                        pages[c] = 0;
+                        if (u < seen) pages[c] = table[page_of(p.pool, u + (u >= p.first ? gap : 0))];
+                    }
+                };
+                int pending = -1;  // the half whose copies are on their way
+                auto finish = [&]() {  // they have arrived
+                    const int s = (tile0 + pending / 2) % kStages, x = pending / 2;
+                    const uint32_t to = ring + s * S::kStage + pending % 2 * kHalf * 128;
+                    const bool edge = !is_key(x) && partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys);
+                    bool found = false;
+                    if constexpr (kNarrow) {
+                        constexpr int kBatch = 4;  // rows a lane reads before the first is written over
+#pragma unroll 1
+                        for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
+                            uint4 raw[kBatch];
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < kBatch; i++) {
+                                raw[i] = make_uint4(0, 0, 0, 0);
+                                if (copies) raw[i] = load16(to + place((i0 + i) * kAtOnce + lane_row, kRaw + chunk));
+                            }
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < kBatch; i++) {
+                                const int row = (i0 + i) * kAtOnce + lane_row;
+                                uint4 a, b;
+                                widen<T>(raw[i], a, b);
+                                // what some row does not see must not meet its weight of zero as an infinity or NaN
+                                if (edge) found |= make_finite<T>(a) | make_finite<T>(b);
+                                if (copies) {
+                                    store16(to + place(row, 2 * chunk), a);
+                                    store16(to + place(row, 2 * chunk + 1), b);
+                                }
+                            }
+                        }
+                    } else if (edge && copies) {
+#pragma unroll 4
+                        for (int i = 0; i < kRounds; i++) {
+                            const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
+                            uint4 y = load16(at);
+                            if (make_finite<T>(y)) {
+                                store16(at, y);
+                                found = true;
+                            }
+                        }
+                    }
+                    if (found) infinite[segment % kSegments] = 1;
+                    fence_for_products();
+                    bar_arrive(full(s));
+                    pending = -1;
+                };
+                auto finish_all = [&]() {
+                    if (pending >= 0) {
+                        wait_copies<0>();
+                        finish();
+                    }
+                };
+                int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps;  // this warp's first half
+                if (h < halves) fetch_pages(h);
                 // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
                 // are left by tiles of blocks before.)
                 bool query_due = true;
 #pragma unroll 1
                 while (query_due || h < halves) {
-                    const bool loads = h < (query_due ? min(4, halves) : halves);
-                    const int x = h / 2, half = h % 2, tile = tile0 + x, s = tile % kStages, j = k.j + step_of(x);
-                    const uint32_t to = ring + s * S::kStage + half * kHalf * 128;
-                    const bool key = is_key(x), edge = !key && partly_seen(p, k, j * kKeys, kKeys);
-                    const char* const pool = key ? p.pool.k : p.pool.v;
-                    bool found = false;
-                    if (loads) {
-                        int64_t off[kOffs];
-#pragma unroll 1
-                        for (int again = 0; again < 2; again++) {  // the pages of this half, if they are not at hand, and of the next
-                            const int y = again ? h + S::kLoadWarps : h;
-                            if (again) {
+                    if (h < (query_due ? min(4, halves) : halves)) {
+                        const int x = h / 2, tile = tile0 + x, s = tile % kStages;
+                        const bool key = is_key(x);
+                        int64_t off[kOffs];  // of the rows of this lane's tokens, or -1
 #pragma unroll
-                                for (int c = 0; c < kOffs; c++) off[c] = next_off[c];
-                                if (key) {
-#pragma unroll
-                                    for (int c = 0; c < kOffs; c++) {
-                                        const uint32_t bad = __ballot_sync(~0u, next_bad >> c & 1);
-                                        if (lane == 0) {
-                                            valid[(step0 + step_of(x)) & 7][half * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
-                                            if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
-                                        }
-                                    }
-                                }
-                            }
-                            if (fetched >= y || y >= halves) continue;
-                            fetched = y;
-                            next_bad = 0;
-#pragma unroll
-                            for (int c = 0; c < kOffs; c++) {
-                                const int u = (k.j + step_of(y / 2)) * kKeys + y % 2 * kHalf + c * 32 + lane;
-                                next_off[c] = -1;
-                                if (u < k.seen) {
-                                    const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
-                                    if ((unsigned)page < (unsigned)p.pool.n_pages)
-                                        next_off[c] = (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head) * C::bytes;
-                                    else
-                                        next_bad |= 1u << c;
+                        for (int c = 0; c < kOffs; c++) {
+                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + c * 32 + lane, t = u + (u >= p.first ? gap : 0);
+                            const bool there = (unsigned)pages[c] < (unsigned)p.pool.n_pages;
+                            off[c] = u < seen && there ? (pages[c] * p.pool.stride_page + (t - page_of(p.pool, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes : -1;
+                            if (key) {
+                                const uint32_t bad = __ballot_sync(~0u, u < seen && !there);
+                                if (lane == 0) {
+                                    valid[(step0 + step_of(x)) & 7][h % 2 * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
+                                    if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
                                 }
                             }
                         }
-                        if (tile >= kStages && !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
-                        if constexpr (kNarrow) {
+                        if (h + S::kLoadWarps < halves) fetch_pages(h + S::kLoadWarps);
+                        if (tile >= kStages && !__all_sync(~0u, bar_try(empty(s), (tile / kStages - 1) & 1))) {
+                            finish_all();
+                            if (!(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
+                        }
+                        const uint32_t to = ring + s * S::kStage + h % 2 * kHalf * 128;
+                        const char* const pool = (key ? p.pool.k : p.pool.v) + chunk * 16;
+                        // (the lanes ask each other for eight offsets before the first is used: one by one a copy took 76 clocks)
+                        constexpr int kBatch = kRounds / kOffs < 8 ? kRounds / kOffs : 8;
+#pragma unroll
+                        for (int c = 0; c < kOffs; c++) {
 #pragma unroll 1
-                            for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
-                                uint4 raw[kBatch];
-                                const int row0 = i0 * kAtOnce + lane_row;
-                                constexpr int kHere = kBatch * kAtOnce <= 32 ? 1 : kBatch * kAtOnce / 32;  // runs of 32 rows in a batch
-                                int64_t mine[kHere];
+                            for (int i0 = 0; i0 < kRounds / kOffs; i0 += kBatch) {
+                                int64_t o[kBatch];
 #pragma unroll
-                                for (int y = 0; y < kHere; y++) {
-                                    mine[y] = off[y];
-#pragma unroll
-                                    for (int c = 1; c < kOffs; c++)
-                                        if (i0 * kAtOnce / 32 + y == c) mine[y] = off[c];
-                                }
-#pragma unroll
-                                for (int i = 0; i < kBatch; i++) {
-                                    const int64_t o = __shfl_sync(~0u, mine[kHere == 1 ? 0 : i * kAtOnce / 32], (row0 + i * kAtOnce) % 32);
-                                    raw[i] = make_uint4(0, 0, 0, 0);
-                                    if (copies && o >= 0) raw[i] = *reinterpret_cast<const uint4*>(pool + o + chunk * 16);
-                                }
+                                for (int i = 0; i < kBatch; i++) o[i] = __shfl_sync(~0u, off[c], (i0 + i) * kAtOnce + lane_row);
                                 if (copies) {
 #pragma unroll
-                                    for (int i = 0; i < kBatch; i++) {
-                                        const int row = row0 + i * kAtOnce;
-                                        uint4 a, b;
-                                        widen<T>(raw[i], a, b);
-                                        store16(to + place(row, 2 * chunk), a);
-                                        store16(to + place(row, 2 * chunk + 1), b);
-                                    }
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < kOffs; c++) {
-#pragma unroll 8
-                                for (int i = 0; i < kRounds / kOffs; i++) {
-                                    const int row = i * kAtOnce + lane_row;
-                                    const int64_t o = __shfl_sync(~0u, off[c], row);
-                                    if (copies) copy16(to + place(c * 32 + row, chunk), pool + (o < 0 ? 0 : o + chunk * 16), o < 0 ? 0 : 16);
+                                    for (int i = 0; i < kBatch; i++)
+                                        copy16(to + place(c * 32 + (i0 + i) * kAtOnce + lane_row, kRaw + chunk), pool + (o[i] < 0 ? 0 : o[i]), o[i] < 0 ? 0 : 16);
                                 }
                             }
                         }
+                        commit_copies();
+                        if (kNarrow && pending >= 0) {
+                            wait_copies<1>();
+                            finish();
+                        }
+                        pending = h;
+                        h += S::kLoadWarps;
+                        if (!kNarrow && !query_due) finish_all();
                     }
-                    commit_copies();
                     if (query_due) {
-                        if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
+                        if (segment > 0 && !__all_sync(~0u, bar_try(query_empty, (segment - 1) & 1))) {
+                            finish_all();
+                            if (!(fine = wait(query_empty, (segment - 1) & 1))) break;
+                        }
                         constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
                         const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
 #pragma unroll 1
@@ -1174,44 +1225,27 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                             const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
                             int64_t off = -1;
                             if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
+                            int64_t o[16 / kQueryRows];
 #pragma unroll
-                            for (int i = 0; i < 16 / kQueryRows; i++) {
-                                const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
-                                const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                                if (at < D / 8)
+                            for (int i = 0; i < 16 / kQueryRows; i++) o[i] = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
+                            if (at < D / 8) {
+#pragma unroll
+                                for (int i = 0; i < 16 / kQueryRows; i++) {
+                                    const int y = r0 + i * kQueryRows + lane / kQueryLanes;
                                     copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
-                                           p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
-                            }
-                        }
-                        commit_copies();
-                        wait_copies<1>();
-                    } else
-                        wait_copies<0>();
-                    if (loads) {
-                        if (edge && (kNarrow ? 2 * chunk < D / 8 : copies)) {
-                            // what some row does not see must not meet its weight of zero as an infinity or NaN
-#pragma unroll 4
-                            for (int i = 0; i < kRounds * (kNarrow ? 2 : 1); i++) {
-                                const uint32_t at = to + (kNarrow ? place(i / 2 * kAtOnce + lane_row, 2 * chunk + i % 2) : place(i * kAtOnce + lane_row, chunk));
-                                uint4 y = load16(at);
-                                if (make_finite<T>(y)) {
-                                    store16(at, y);
-                                    found = true;
+                                           p.q + (o[i] < 0 ? 0 : o[i] + at * 16), o[i] < 0 ? 0 : 16);
                                 }
                             }
                         }
-                        if (found) infinite[segment % kSegments] = 1;
-                        fence_for_products();
-                        bar_arrive(full(s));
-                        h += S::kLoadWarps;
-                    }
-                    if (query_due) {
+                        commit_copies();
                         wait_copies<0>();
+                        if (pending >= 0) finish();
                         fence_for_products();
                         bar_arrive(query_full);
                         query_due = false;
                     }
                 }
+                finish_all();
                 if (!fine) break;
                 tile0 += 2 * steps, step0 += steps;
                 leave_segment();
