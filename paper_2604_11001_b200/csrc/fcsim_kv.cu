@@ -806,6 +806,55 @@ int check_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, Prefi
     return FCSIM_OK;
 }
 
+// Tensor maps of the cache and of q, for bulk copies, where pages hold whole boxes of 8 tokens or more.  (Other pages and strides are copied row by row.)
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static std::atomic<void*> known;
+    void* f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return nullptr;
+        }
+        known.store(f, std::memory_order_relaxed);
+    }
+    return (EncodeTiled)f;
+}
+struct MapDim {
+    int64_t size, stride;  // stride in elements; of the first 1
+    int box;
+};
+bool encode(CUtensorMap* map, const void* base, int bytes, int dims, const MapDim* d) {
+    const EncodeTiled f = encode_tiled();
+    cuuint64_t size[4], stride[4];
+    cuuint32_t box[4], ones[4] = {1, 1, 1, 1};
+    for (int i = 0; i < dims; i++) {
+        size[i] = d[i].size, box[i] = d[i].box;
+        if (i == 0) continue;
+        stride[i - 1] = (cuuint64_t)d[i].stride * bytes;
+        if (d[i].size == 1) stride[i - 1] = std::max<cuuint64_t>(stride[i - 1], 16);  // never taken
+        if (stride[i - 1] == 0 || stride[i - 1] >= 1ull << 40) return false;
+    }
+    return f && f(map, bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, dims, const_cast<void*>(base), size, stride, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+void prefill_maps(PrefillParams* p, const PrefillVariant& v, int bytes) {
+    const Pool& c = p->pool;
+    p->box = 0, p->kept = p->first;
+    if (!v.raw_rows || c.page_size % 8 != 0) return;
+    int box = 8;
+    while (box * 2 <= v.keys / 2 && c.page_size % (box * 2) == 0) box *= 2;
+    p->key_dim = c.stride_slot <= c.stride_head;
+    const MapDim slots = {c.page_size, c.stride_slot, box}, heads = {c.n_kv, c.stride_head, 1};
+    const MapDim d[4] = {{c.head_dim, 1, 128 / bytes}, p->key_dim ? slots : heads, p->key_dim ? heads : slots, {c.n_pages, c.stride_page, 1}};
+    p->query_tokens = 128 % p->heads_a_tile == 0 ? std::min(128 / p->heads_a_tile, p->tokens_a_block) : p->tokens_a_block;
+    const MapDim q[3] = {{c.head_dim, 1, 64}, {p->n_heads, p->q_head, p->heads_a_tile}, {p->n_rows, p->q_row, p->query_tokens}};
+    if (!encode(&p->k_map, c.k, bytes, 4, d) || !encode(&p->v_map, c.v, bytes, 4, d) || !encode(&p->q_map, p->q, 2, 3, q)) return;
+    p->box = box, p->kept = (p->first + box - 1) / box * box;
+}
+
 constexpr size_t kPrefillCounters = kMaxCtas * (kThreads / 32) * 4;  // those of attend: one workspace serves both
 
 int prefill_layout(const PrefillParams& p, const PrefillVariant& v, int* device, int* grid, size_t* bytes) {
@@ -981,6 +1030,7 @@ extern "C" int fcsim_kv_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_
     if ((rc = prefill_layout(p, v, &device, &grid, &bytes)) != FCSIM_OK) return rc;
     if (workspace_bytes < bytes) return FCSIM_ESIZE;
     p.counters = (int*)workspace, p.parts = (float*)((char*)workspace + kPrefillCounters);
+    prefill_maps(&p, v, cache_bytes(c));
     return cuda_status((cudaError_t)v.launch(p, grid, device, (cudaStream_t)cuda_stream));
 }
 

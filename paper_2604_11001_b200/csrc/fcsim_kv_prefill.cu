@@ -52,6 +52,19 @@ __device__ __forceinline__ void fence_for_products() { asm volatile("fence.proxy
 
 __device__ __forceinline__ void bar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// and with as many bytes of bulk copies to come
+__device__ __forceinline__ void bar_expect(uint32_t bar, int bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// a box of a tensor of 4 or 3 dimensions into shared memory, rows of 128 bytes swizzled by 128 bytes
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
@@ -191,12 +204,13 @@ __device__ __forceinline__ int request_rows(const PrefillParams& p, int r, int& 
 __device__ __forceinline__ int request_length(const PrefillParams& p, int r) { return min(max(p.lengths[r], 0), p.max_length); }
 
 // What a block of tokens sees: all tokens up to its last one, or the first ones and, without the gap behind these, those from the start of
-// its first token's window.  Counted without the gap: seen key u is token u, or behind the first ones u + gap.
+// its first token's window.  Counted without the gap: seen key u is token u, or behind the first ones u + gap.  (Both ends of the gap are rounded
+// so that what one bulk copy brings lies on one side of it.)
 __device__ __forceinline__ int seen_by(const PrefillParams& p, int position0, int tokens, int& gap) {
     gap = 0;
     if (p.window > 0) {
         const int64_t low = (int64_t)position0 - p.window + 1;  // (a request of more rows than tokens has positions below 0)
-        if (low > p.first) gap = (int)(low - p.first);
+        if (low > p.kept) gap = (int)(low - p.kept) & -max(p.box, 1);
     }
     return max(position0 + tokens - gap, 0);
 }
@@ -563,7 +577,7 @@ __device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, cons
 #pragma unroll 1
                     for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
                         if (u > x.position || (u < x.from && u >= p.first)) continue;
-                        const int t = u + (u >= p.first ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                        const int t = u + (u >= p.kept ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
                         if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
                         const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head + c * 32) * C::bytes;
 #pragma unroll
@@ -678,7 +692,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     constexpr bool kNarrow = C::bytes == 1;
     constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(1024) char raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 12];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 12 + 2 * S::kLoadWarps];
     __shared__ uint32_t tmem_at, valid[8][4];
     __shared__ int stuck, infinite[kSegments], joins[kTiles];
     __shared__ Walk start;
@@ -698,6 +712,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     auto weights_ready = [&](int s) { return rest + 16 + s * 8; };
     auto output_full = [&](int s) { return rest + 32 + s * 8; };
     auto meeting = [&](int i) { return rest + 48 + i * 8; };
+    auto landed = [&](int me, int turn) { return rest + 96 + (me * 2 + turn) * 8; };  // a warp's bulk copies that it looks over
     const uint32_t query_full = rest + 64, query_empty = rest + 72, added = rest + 80, drained = rest + 88;
     auto wait_on = [&](auto side, uint32_t bar, uint32_t parity) {
         return __all_sync(~0u, bar_try(bar, parity)) || wait_long<decltype(side)::value>(bar, parity, &stuck, p.status);
@@ -711,7 +726,9 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         for (int s = 0; s < kSegments; s++) bar_init(told_of(s), 1), bar_init(done_with(s), S::kWarps - 1);
 #pragma unroll 1
         for (int s = 0; s < 2; s++) bar_init(score_full(s), 1), bar_init(weights_ready(s), 128), bar_init(output_full(s), 1), bar_init(meeting(s), 128);
-        bar_init(query_full, 32 * S::kLoadWarps), bar_init(query_empty, 1), bar_init(added, 1), bar_init(drained, 1);
+#pragma unroll 1
+        for (int s = 0; s < S::kLoadWarps; s++) bar_init(landed(s, 0), 1), bar_init(landed(s, 1), 1);
+        bar_init(query_full, p.box ? 1 : 32 * S::kLoadWarps), bar_init(query_empty, 1), bar_init(added, 1), bar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         stuck = 0;
         start.left = 0;
@@ -730,7 +747,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 store16(tile + chunk / 8 * (tall * 128) + row * 128 + ((chunk % 8) ^ (row % 8)) * 16, make_uint4(0, 0, 0, 0));
             }
         };
-        clear(query, S::kRows, 128);
+        clear(query, S::kRows, S::kRows);
         clear(ring, kStages * kKeys, kKeys);
         fence_for_products();
     }
@@ -1053,11 +1070,11 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         const uint32_t i = ahead ? q & 1 : q & both;
                         if ((!both || i == 0) && !(fine = next_tile(key_stage))) break;
                         const uint32_t to = base + S::kScore + i * kKeys;
-                        const uint64_t a = query_operand + (ahead ? 0 : i) * (128 * DP * 2 >> 4), b = key_operand + key_stage * (S::kStage >> 4);
+                        const uint64_t a = query_operand + (ahead ? 0 : i) * (128 * 128 >> 4), b = key_operand + key_stage * (S::kStage >> 4);
                         if (elected()) {
 #pragma unroll
                             for (int y = 0; y < DP / 16; y++)
-                                if (y < depth) product(to, a + ((y / 4 * (128 * 128) + y % 4 * 32) >> 4), b + ((y / 4 * (kKeys * 128) + y % 4 * 32) >> 4), how_score, y > 0);
+                                if (y < depth) product(to, a + ((y / 4 * (S::kRows * 128) + y % 4 * 32) >> 4), b + ((y / 4 * (kKeys * 128) + y % 4 * 32) >> 4), how_score, y > 0);
                             commit_products(score_full(i));
                             if (!both || i == 1) commit_products(empty(key_stage));
                             if (q + 1 == outputs) commit_products(query_empty);
@@ -1085,6 +1102,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             // 16-bit ones from there.
             auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
             constexpr int kRaw = kNarrow ? DP / 16 : 0;
+            uint32_t landed_parity = 0, turn = 0;  // of the two barriers, a bit each; the next
             while (next_segment(wait)) {
                 const Segment& k = segments[segment % kSegments];
                 const int steps = k.steps, halves = 4 * steps, gap = k.gap, seen = k.seen;
@@ -1094,22 +1112,41 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 const bool ahead = kTiles == 1 || k.shared;
                 auto is_key = [&](int x) { return !ahead ? x % 2 == 0 : x == 0 || (x % 2 == 1 && x < 2 * steps - 1); };
                 auto step_of = [&](int x) { return !ahead || x == 2 * steps - 1 ? x / 2 : is_key(x) ? (x + 1) / 2 : x / 2 - 1; };
-                // pages of this lane's tokens (lane, lane + 32) of a half: asked for long before they are used
+                // Bulk copies: a lane has a box of `box` tokens by 128 bytes of a half.  Otherwise a lane has tokens lane and lane + 32.
+                constexpr int kAcross = kNarrow ? (DP + 127) / 128 : DP / 64;
+                const int across = kNarrow ? (D + 127) / 128 : (D + 63) / 64, my_box = lane / kAcross * p.box, my_part = lane % kAcross;
+                const bool in_boxes = p.box > 0, has_box = in_boxes && my_box < kHalf && my_part < across;
+                // pages of this lane's tokens: asked for long before they are used
                 int pages[kOffs];
                 auto fetch_pages = [&](int h) {
+                    if (in_boxes) {
+                        const int u = (k.j + step_of(h / 2)) * kKeys + h % 2 * kHalf + my_box;
+                        pages[0] = 0;
+                        if (has_box && u < seen) pages[0] = table[page_of(p.pool, u + (u >= p.kept ? gap : 0))];
+                        return;
+                    }
 #pragma unroll
                     for (int c = 0; c < kOffs; c++) {
                         const int u = (k.j + step_of(h / 2)) * kKeys + h % 2 * kHalf + c * 32 + lane;
                         pages[c] = 0;
-                        if (u < seen) pages[c] = table[page_of(p.pool, u + (u >= p.first ? gap : 0))];
+                        if (u < seen) pages[c] = table[page_of(p.pool, u + (u >= p.kept ? gap : 0))];
                     }
                 };
-                int pending = -1;  // the half whose copies are on their way
+                uint32_t holes_of[kOffs];  // of a half that is looked over: rows whose page is there
+                int pending = -1;      // the half whose copies are on their way and are looked over when they are there
+                bool holes = false;    // some of its boxes were not copied
                 auto finish = [&]() {  // they have arrived
                     const int s = (tile0 + pending / 2) % kStages, x = pending / 2;
                     const uint32_t to = ring + s * S::kStage + pending % 2 * kHalf * 128;
-                    const bool edge = !is_key(x) && partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys);
+                    const bool edge = !is_key(x) && (holes || partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys));
                     bool found = false;
+                    // of bulk copies: rows of places without a token, and of pages outside the pool
+                    uint32_t gone[kOffs] = {};
+                    if (in_boxes && edge) {
+#pragma unroll
+                        for (int c = 0; c < kOffs; c++) gone[c] = ~lowest(seen - ((k.j + step_of(x)) * kKeys + pending % 2 * kHalf + c * 32)) | ~holes_of[c];
+                    }
+                    auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
                     if constexpr (kNarrow) {
                         constexpr int kBatch = 4;  // rows a lane reads before the first is written over
 #pragma unroll 1
@@ -1119,7 +1156,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
 #pragma unroll
                             for (int i = 0; i < kBatch; i++) {
                                 raw[i] = make_uint4(0, 0, 0, 0);
-                                if (copies) raw[i] = load16(to + place((i0 + i) * kAtOnce + lane_row, kRaw + chunk));
+                                const int row = (i0 + i) * kAtOnce + lane_row;
+                                if (copies && !is_gone(row)) raw[i] = load16(to + place(row, kRaw + chunk));
                             }
                             __syncwarp();
 #pragma unroll
@@ -1140,7 +1178,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         for (int i = 0; i < kRounds; i++) {
                             const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
                             uint4 y = load16(at);
-                            if (make_finite<T>(y)) {
+                            if (is_gone(i * kAtOnce + lane_row)) store16(at, make_uint4(0, 0, 0, 0));
+                            else if (make_finite<T>(y)) {
                                 store16(at, y);
                                 found = true;
                             }
@@ -1153,7 +1192,14 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 };
                 auto finish_all = [&]() {
                     if (pending >= 0) {
-                        wait_copies<0>();
+                        if (in_boxes) {
+                            turn ^= 1;
+                            fine = wait(landed(me, turn), landed_parity >> turn & 1);
+                            landed_parity ^= 1u << turn;
+                            turn ^= 1;
+                            if (!fine) return;
+                        } else
+                            wait_copies<0>();
                         finish();
                     }
                 };
@@ -1167,10 +1213,50 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     if (h < (query_due ? min(4, halves) : halves)) {
                         const int x = h / 2, tile = tile0 + x, s = tile % kStages;
                         const bool key = is_key(x);
+                        if (in_boxes) {
+                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + my_box, t = u + (u >= p.kept ? gap : 0), page = pages[0];
+                            const bool bad = has_box && u < seen && (unsigned)page >= (unsigned)p.pool.n_pages, issue = has_box && u < seen && !bad;
+                            const int slot = t - page_of(p.pool, t) * p.pool.page_size;
+                            const uint32_t any_bad = __ballot_sync(~0u, bad), issues = __ballot_sync(~0u, issue);
+                            uint32_t there[kOffs];
+#pragma unroll
+                            for (int c = 0; c < kOffs; c++)
+                                there[c] = any_bad ? ~__reduce_or_sync(~0u, bad ? lowest(my_box + p.box - c * 32) & ~lowest(my_box - c * 32) : 0u) : ~0u;
+                            if (lane == 0) {
+                                if (key) {
+#pragma unroll
+                                    for (int c = 0; c < kOffs; c++) valid[(step0 + step_of(x)) & 7][h % 2 * kOffs + c] = there[c];  // (what lies behind the last token is no row's)
+                                }
+                                if (any_bad) flag(p.status, FCSIM_KV_BAD_PAGE);
+                            }
+                            if (h + S::kLoadWarps < halves) fetch_pages(h + S::kLoadWarps);
+                            if (tile >= kStages && !__all_sync(~0u, bar_try(empty(s), (tile / kStages - 1) & 1))) {
+                                finish_all();
+                                if (!fine || !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
+                            }
+                            const bool looks = kNarrow || (!key && (any_bad || partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys)));
+                            const uint32_t bar = looks ? landed(me, turn) : full(s);
+                            if (lane == 0) bar_expect(bar, __popc(issues) * p.box * 128);
+                            __syncwarp();
+                            if (issue)
+                                copy_box(ring + s * S::kStage + (my_part + (kNarrow ? kAcross : 0)) * (kKeys * 128) + (h % 2 * kHalf + my_box) * 128, key ? &p.k_map : &p.v_map,
+                                         my_part * (kNarrow ? 128 : 64), p.key_dim ? slot : k.kv, p.key_dim ? k.kv : slot, page, bar);
+                            if (looks) {
+                                if (pending >= 0) finish_all();  // (the one before)
+                                if (!fine) break;
+                                pending = h, holes = any_bad != 0, turn ^= 1;
+#pragma unroll
+                                for (int c = 0; c < kOffs; c++) holes_of[c] = there[c];
+                                if (!kNarrow) finish_all();
+                                if (!fine) break;
+                            } else if (lane != 0)
+                                bar_arrive(full(s));
+                            h += S::kLoadWarps;
+                        } else {
                         int64_t off[kOffs];  // of the rows of this lane's tokens, or -1
 #pragma unroll
                         for (int c = 0; c < kOffs; c++) {
-                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + c * 32 + lane, t = u + (u >= p.first ? gap : 0);
+                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + c * 32 + lane, t = u + (u >= p.kept ? gap : 0);
                             const bool there = (unsigned)pages[c] < (unsigned)p.pool.n_pages;
                             off[c] = u < seen && there ? (pages[c] * p.pool.stride_page + (t - page_of(p.pool, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes : -1;
                             if (key) {
@@ -1212,11 +1298,27 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         pending = h;
                         h += S::kLoadWarps;
                         if (!kNarrow && !query_due) finish_all();
+                        }
+                    }
+                    if (query_due && in_boxes && me != 0) {  // (the first warp brings Q)
+                        query_due = false;
+                        continue;
                     }
                     if (query_due) {
                         if (segment > 0 && !__all_sync(~0u, bar_try(query_empty, (segment - 1) & 1))) {
                             finish_all();
-                            if (!(fine = wait(query_empty, (segment - 1) & 1))) break;
+                            if (!fine || !(fine = wait(query_empty, (segment - 1) & 1))) break;
+                        }
+                        if (in_boxes) {
+                            // all rows of the block, or tile after tile; what lies behind the request's rows is no row of the block
+                            const int boxes = p.query_tokens == p.tokens_a_block ? 1 : k.tiles_in_use, rows = p.query_tokens * heads_a_tile;
+                            if (lane == 0) bar_expect(query_full, boxes * (DP / 64) * rows * 128);
+                            __syncwarp();
+                            if (lane < boxes * (DP / 64))
+                                copy_box(query + lane / (DP / 64) * (128 * 128) + lane % (DP / 64) * (S::kRows * 128), &p.q_map, lane % (DP / 64) * 64,
+                                         k.kv * group + k.ht * heads_a_tile, k.row + lane / (DP / 64) * p.query_tokens, query_full);
+                            query_due = false;
+                            continue;
                         }
                         constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
                         const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
@@ -1232,7 +1334,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
 #pragma unroll
                                 for (int i = 0; i < 16 / kQueryRows; i++) {
                                     const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                                    copy16(query + y / 128 * (128 * DP * 2) + at / 8 * (128 * 128) + y % 128 * 128 + ((at % 8) ^ (y % 8)) * 16,
+                                    copy16(query + at / 8 * (S::kRows * 128) + y * 128 + ((at % 8) ^ (y % 8)) * 16,
                                            p.q + (o[i] < 0 ? 0 : o[i] + at * 16), o[i] < 0 ? 0 : 16);
                                 }
                             }
@@ -1245,8 +1347,12 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         query_due = false;
                     }
                 }
-                finish_all();
-                if (!fine) break;
+                if (fine) finish_all();
+                if (!fine) {  // what is on its way arrives before the CTA ends
+                    const int64_t began = clock64();
+                    while (clock64() - began < 4000000) {}
+                    break;
+                }
                 tile0 += 2 * steps, step0 += steps;
                 leave_segment();
             }
@@ -1279,7 +1385,7 @@ int launch(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
 }
 template <class T, class C, int DP>
 PrefillVariant variant() {
-    return {launch<T, C, DP>, Shape<T, C, DP>::kRows, Shape<T, C, DP>::kKeys, DP};
+    return {launch<T, C, DP>, Shape<T, C, DP>::kRows, Shape<T, C, DP>::kKeys, DP, C::bytes == 2 || DP > 64};
 }
 template <class T, class C>
 PrefillVariant of(int head_dim) {
