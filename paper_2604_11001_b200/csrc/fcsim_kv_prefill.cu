@@ -622,42 +622,62 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
     constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
     const int pairs = shared ? 2 : 1, n = parts.n * pairs;
     auto part = [&](int x) { return shared ? parts.at(x >> 1) + (x & 1) * kPart : parts.at(x); };
-    float least = INFINITY;  // of add: the highest reference
-#pragma unroll 4
-    for (int x = 0; x < n; x++) least = fminf(least, __ldcg(part(x) + DP * 128 + row.row));
-    float all = 0;
-#pragma unroll 4
-    for (int x = 0; x < n; x++) {
-        const float a = __ldcg(part(x) + DP * 128 + row.row);
-        all += (a == INFINITY ? 0.0f : power2(least - a)) * __ldcg(part(x) + (DP + 1) * 128 + row.row);
+    // They come from L2 at a microsecond each: what can be asked for at once is.
+    constexpr int kMost = 8;
+    float add[kMost], least = INFINITY, all = 0;  // references as numbers to add; the least is the highest reference
+#pragma unroll 1
+    for (int x0 = 0; x0 < n; x0 += kMost) {
+        float sum[kMost];
+#pragma unroll
+        for (int x = 0; x < kMost; x++) {
+            const float* const from = part(min(x0 + x, n - 1)) + DP * 128 + row.row;
+            add[x] = __ldcg(from), sum[x] = __ldcg(from + 128);
+        }
+        const float before = least;
+#pragma unroll
+        for (int x = 0; x < kMost; x++) {
+            if (x0 + x >= n) add[x] = INFINITY, sum[x] = 0;
+            least = fminf(least, add[x]);
+        }
+        all *= before == INFINITY ? 0.0f : power2(least - before);
+#pragma unroll
+        for (int x = 0; x < kMost; x++) all += (add[x] == INFINITY ? 0.0f : power2(least - add[x])) * sum[x];
     }
     const float f = all == 0.0f ? 0.0f : vscale / all;
-    // They come from L2 at a microsecond each, so four parts are asked for at once.
+    if (n <= kMost) {
+#pragma unroll
+        for (int x = 0; x < kMost; x++) add[x] = add[x] == INFINITY ? 0.0f : power2(least - add[x]);  // now factors
+    }
 #pragma unroll 1
     for (int c = 0; c * 32 < p.pool.head_dim; c++) {
         float o[32] = {};
 #pragma unroll 1
-        for (int x0 = 0; x0 < n; x0 += 4) {
-            float4 z[4][4];
-            float y[4];
+        for (int x0 = 0; x0 < n; x0 += kMost) {
+            if (n > kMost) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
+                for (int x = 0; x < kMost; x++) {
+                    const float a = x0 + x < n ? __ldcg(part(x0 + x) + DP * 128 + row.row) : INFINITY;
+                    add[x] = a == INFINITY ? 0.0f : power2(least - a);
+                }
+            }
 #pragma unroll
-                for (int x = 0; x < 4; x++) {
-                    const bool there = x0 + x < n;
-                    const float* const from = part(there ? x0 + x : x0);
-                    const float a = there ? __ldcg(from + DP * 128 + row.row) : INFINITY;
-                    y[x] = a == INFINITY ? 0.0f : power2(least - a);
+            for (int x1 = 0; x1 < kMost; x1 += 2) {
+                if (x0 + x1 >= n) break;
+                float4 z[2][8];
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        z[x][e] = a == INFINITY ? make_float4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const float4*>(from) + (c * 8 + h * 4 + e) * 128 + row.row);  // (a part without a tile has no output)
+                for (int x = 0; x < 2; x++) {
+                    const bool there = __any_sync(~0u, add[x1 + x] != 0.0f);  // (a part without a tile has no output)
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        z[x][e] = there ? __ldcg(reinterpret_cast<const float4*>(part(x0 + x1 + x)) + (c * 8 + e) * 128 + row.row) : make_float4(0, 0, 0, 0);
                 }
 #pragma unroll
-                for (int x = 0; x < 4; x++)
+                for (int x = 0; x < 2; x++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        float* const to = o + 16 * h + 4 * e;
-                        to[0] += y[x] * z[x][e].x, to[1] += y[x] * z[x][e].y, to[2] += y[x] * z[x][e].z, to[3] += y[x] * z[x][e].w;
+                    for (int e = 0; e < 8; e++) {
+                        float* const to = o + 4 * e;
+                        const float y = add[x1 + x];
+                        to[0] += y * z[x][e].x, to[1] += y * z[x][e].y, to[2] += y * z[x][e].z, to[3] += y * z[x][e].w;
                     }
             }
         }
@@ -1148,31 +1168,36 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     }
                     auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
                     if constexpr (kNarrow) {
-                        constexpr int kBatch = 4;  // rows a lane reads before the first is written over
+                        auto turn_rows = [&](auto at_once, auto careful) {
+                            constexpr int kBatch = decltype(at_once)::value;  // rows a lane reads before the first is written over
 #pragma unroll 1
-                        for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
-                            uint4 raw[kBatch];
-                            __syncwarp();
+                            for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
+                                uint4 raw[kBatch];
+                                __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < kBatch; i++) {
-                                raw[i] = make_uint4(0, 0, 0, 0);
-                                const int row = (i0 + i) * kAtOnce + lane_row;
-                                if (copies && !is_gone(row)) raw[i] = load16(to + place(row, kRaw + chunk));
-                            }
-                            __syncwarp();
+                                for (int i = 0; i < kBatch; i++) {
+                                    const int row = (i0 + i) * kAtOnce + lane_row;
+                                    raw[i] = make_uint4(0, 0, 0, 0);
+                                    if (copies && !(decltype(careful)::value && is_gone(row))) raw[i] = load16(to + place(row, kRaw + chunk));
+                                }
+                                __syncwarp();
 #pragma unroll
-                            for (int i = 0; i < kBatch; i++) {
-                                const int row = (i0 + i) * kAtOnce + lane_row;
-                                uint4 a, b;
-                                widen<T>(raw[i], a, b);
-                                // what some row does not see must not meet its weight of zero as an infinity or NaN
-                                if (edge) found |= make_finite<T>(a) | make_finite<T>(b);
-                                if (copies) {
-                                    store16(to + place(row, 2 * chunk), a);
-                                    store16(to + place(row, 2 * chunk + 1), b);
+                                for (int i = 0; i < kBatch; i++) {
+                                    const int row = (i0 + i) * kAtOnce + lane_row;
+                                    uint4 a, b;
+                                    widen<T>(raw[i], a, b);
+                                    // what some row does not see must not meet its weight of zero as an infinity or NaN
+                                    if constexpr (decltype(careful)::value) found |= make_finite<T>(a) | make_finite<T>(b);
+                                    if (copies) {  // (of every eight lanes half begin with the odd place: all banks at once)
+                                        const bool odd = kLanes > 4 && (chunk & 4);
+                                        store16(to + place(row, 2 * chunk + odd), odd ? b : a);
+                                        store16(to + place(row, 2 * chunk + !odd), odd ? a : b);
+                                    }
                                 }
                             }
-                        }
+                        };
+                        if (edge) turn_rows(std::integral_constant<int, 1>(), std::true_type());
+                        else turn_rows(std::integral_constant<int, 4>(), std::false_type());
                     } else if (edge && copies) {
 #pragma unroll 4
                         for (int i = 0; i < kRounds; i++) {
