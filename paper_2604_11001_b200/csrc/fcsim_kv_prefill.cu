@@ -1168,6 +1168,14 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     }
                     auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
                     if constexpr (kNarrow) {
+                        // Eight lanes take four pieces each of rows r and r ^ 5: so both what they read and what they write lies in all banks.
+                        constexpr int kGroups = kLanes / 4, kPairs = 4 / kGroups;
+                        const int turned_chunk = (lane >> 3) % kGroups * 4 + (lane & 3), swap = lane & 4 ? 5 : 0;
+                        const bool turns = turned_chunk < chunks;
+                        auto turned_row = [&](int i) {
+                            const int pair = i * kPairs + (lane >> 3) / kGroups;
+                            return pair / 4 * 8 + (pair % 4 ^ swap);
+                        };
                         auto turn_rows = [&](auto at_once, auto careful) {
                             constexpr int kBatch = decltype(at_once)::value;  // rows a lane reads before the first is written over
 #pragma unroll 1
@@ -1176,22 +1184,19 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                 __syncwarp();
 #pragma unroll
                                 for (int i = 0; i < kBatch; i++) {
-                                    const int row = (i0 + i) * kAtOnce + lane_row;
                                     raw[i] = make_uint4(0, 0, 0, 0);
-                                    if (copies && !(decltype(careful)::value && is_gone(row))) raw[i] = load16(to + place(row, kRaw + chunk));
+                                    if (turns && !(decltype(careful)::value && is_gone(turned_row(i0 + i)))) raw[i] = load16(to + place(turned_row(i0 + i), kRaw + turned_chunk));
                                 }
                                 __syncwarp();
 #pragma unroll
                                 for (int i = 0; i < kBatch; i++) {
-                                    const int row = (i0 + i) * kAtOnce + lane_row;
                                     uint4 a, b;
                                     widen<T>(raw[i], a, b);
                                     // what some row does not see must not meet its weight of zero as an infinity or NaN
                                     if constexpr (decltype(careful)::value) found |= make_finite<T>(a) | make_finite<T>(b);
-                                    if (copies) {  // (of every eight lanes half begin with the odd place: all banks at once)
-                                        const bool odd = kLanes > 4 && (chunk & 4);
-                                        store16(to + place(row, 2 * chunk + odd), odd ? b : a);
-                                        store16(to + place(row, 2 * chunk + !odd), odd ? a : b);
+                                    if (turns) {
+                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk), a);
+                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk + 1), b);
                                     }
                                 }
                             }
