@@ -56,6 +56,14 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrie
 __device__ __forceinline__ void bar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// the same, the thread asleep for up to so many nanoseconds
+__device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity, uint32_t ns) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done) : "r"(bar), "r"(parity), "r"(ns) : "memory");
+    return done != 0;
+}
 // a box of a tensor of 4 or 3 dimensions into shared memory, rows of 128 bytes swizzled by 128 bytes
 __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -693,7 +701,7 @@ __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile i
     constexpr int64_t kPatience = 4000000000ll;  // cycles: seconds, where microseconds are usual
     const int64_t began = clock64();
     bool done = false;
-    while (!(done = bar_try(bar, parity))) {
+    while (!(done = bar_sleep(bar, parity, 100000))) {
         if (*stuck) break;
         if (clock64() - began > kPatience) {
             *stuck = 1;
