@@ -533,6 +533,19 @@ __device__ __forceinline__ bool make_finite(uint4& x) {
     return a || b || c || d;
 }
 
+// The same for NaN among sixteen 8-bit elements.
+__device__ __forceinline__ bool make_finite8(uint4& x) {
+    uint32_t* const w = &x.x;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t nan = __vcmpeq4(w[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+        w[i] &= ~nan;
+        any |= nan;
+    }
+    return any != 0;
+}
+
 // ---------------------------------------------------------------------------------------------- the end of a block
 // What a row's thread needs to leave its output.
 struct Row {
@@ -1160,193 +1173,89 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         if (u < seen) pages[c] = table[page_of(p.pool, u + (u >= p.kept ? gap : 0))];
                     }
                 };
-                uint32_t holes_of[kOffs];  // of a half that is looked over: rows whose page is there
-                int pending = -1;      // the half whose copies are on their way and are looked over when they are there
-                bool holes = false;    // some of its boxes were not copied
-                auto finish = [&]() {  // they have arrived
-                    const int s = (tile0 + pending / 2) % kStages, x = pending / 2;
-                    const uint32_t to = ring + s * S::kStage + pending % 2 * kHalf * 128;
-                    const bool edge = !is_key(x) && (holes || partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys));
-                    bool found = false;
-                    // of bulk copies: rows of places without a token, and of pages outside the pool
-                    uint32_t gone[kOffs] = {};
-                    if (in_boxes && edge) {
-#pragma unroll
-                        for (int c = 0; c < kOffs; c++) gone[c] = ~lowest(seen - ((k.j + step_of(x)) * kKeys + pending % 2 * kHalf + c * 32)) | ~holes_of[c];
-                    }
-                    auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
-                    if constexpr (kNarrow) {
-                        // Eight lanes take four pieces each of rows r and r ^ 5: so both what they read and what they write lies in all banks.
-                        constexpr int kGroups = kLanes / 4, kPairs = 4 / kGroups;
-                        const int turned_chunk = (lane >> 3) % kGroups * 4 + (lane & 3), swap = lane & 4 ? 5 : 0;
-                        const bool turns = turned_chunk < chunks;
-                        auto turned_row = [&](int i) {
-                            const int pair = i * kPairs + (lane >> 3) / kGroups;
-                            return pair / 4 * 8 + (pair % 4 ^ swap);
-                        };
-                        auto turn_rows = [&](auto at_once, auto careful) {
-                            constexpr int kBatch = decltype(at_once)::value;  // rows a lane reads before the first is written over
-#pragma unroll 1
-                            for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
-                                uint4 raw[kBatch];
-                                __syncwarp();
-#pragma unroll
-                                for (int i = 0; i < kBatch; i++) {
-                                    raw[i] = make_uint4(0, 0, 0, 0);
-                                    if (turns && !(decltype(careful)::value && is_gone(turned_row(i0 + i)))) raw[i] = load16(to + place(turned_row(i0 + i), kRaw + turned_chunk));
-                                }
-                                __syncwarp();
-#pragma unroll
-                                for (int i = 0; i < kBatch; i++) {
-                                    uint4 a, b;
-                                    widen<T>(raw[i], a, b);
-                                    // what some row does not see must not meet its weight of zero as an infinity or NaN
-                                    if constexpr (decltype(careful)::value) found |= make_finite<T>(a) | make_finite<T>(b);
-                                    if (turns) {
-                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk), a);
-                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk + 1), b);
-                                    }
-                                }
-                            }
-                        };
-                        if (edge) turn_rows(std::integral_constant<int, 1>(), std::true_type());
-                        else turn_rows(std::integral_constant<int, 4>(), std::false_type());
-                    } else if (edge && copies) {
-#pragma unroll 4
-                        for (int i = 0; i < kRounds; i++) {
-                            const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
-                            uint4 y = load16(at);
-                            if (is_gone(i * kAtOnce + lane_row)) store16(at, make_uint4(0, 0, 0, 0));
-                            else if (make_finite<T>(y)) {
-                                store16(at, y);
-                                found = true;
-                            }
-                        }
-                    }
-                    if (found) infinite[segment % kSegments] = 1;
-                    fence_for_products();
-                    bar_arrive(full(s));
-                    pending = -1;
-                };
-                auto finish_all = [&]() {
-                    if (pending >= 0) {
-                        if (in_boxes) {
-                            turn ^= 1;
-                            fine = wait(landed(me, turn), landed_parity >> turn & 1);
-                            landed_parity ^= 1u << turn;
-                            turn ^= 1;
-                            if (!fine) return;
-                        } else
-                            wait_copies<0>();
-                        finish();
-                    }
-                };
+                // A half whose copies are on their way and which is looked over, or turned into 16 bits, when they are there: which, on what barrier, and
+                // rows whose page is in the pool.
+                int pending = -1, pending_turn = 0;
+                uint32_t pending_rows[kOffs];
                 int h = (me + S::kLoadWarps - 2 * tile0 % S::kLoadWarps) % S::kLoadWarps;  // this warp's first half
                 if (h < halves) fetch_pages(h);
                 // The first two tiles do not wait for the rows of Q, which wait for the end of the last block's scores.  (The places of these two
-                // are left by tiles of blocks before.)
-                bool query_due = true;
+                // are left by tiles of blocks before.)  The first warp brings them in bulk; else each brings some.
+                bool query_due = !in_boxes || me == 0;
+                // (Each step stands here once: the instructions of all roles have to come through one cache.)
 #pragma unroll 1
-                while (query_due || h < halves) {
+                while (query_due || h < halves || pending >= 0) {
+                    int issued = -1, issued_turn = 0;
+                    uint32_t rows_there[kOffs];
                     if (h < (query_due ? min(4, halves) : halves)) {
-                        const int x = h / 2, tile = tile0 + x, s = tile % kStages;
-                        const bool key = is_key(x);
-                        if (in_boxes) {
-                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + my_box, t = u + (u >= p.kept ? gap : 0), page = pages[0];
-                            const bool bad = has_box && u < seen && (unsigned)page >= (unsigned)p.pool.n_pages, issue = has_box && u < seen && !bad;
-                            const int slot = t - page_of(p.pool, t) * p.pool.page_size;
-                            const uint32_t any_bad = __ballot_sync(~0u, bad), issues = __ballot_sync(~0u, issue);
-                            uint32_t there[kOffs];
+                        const int x = h / 2, tile = tile0 + x, s = tile % kStages, u0 = (k.j + step_of(x)) * kKeys + h % 2 * kHalf;
+                        bool room = tile < kStages || __all_sync(~0u, bar_try(empty(s), (tile / kStages - 1) & 1));
+                        if (!room && pending < 0 && !query_due) {  // (nothing else to do)
+                            if (!(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
+                            room = true;
+                        }
+                        if (room) {
+                            const bool key = is_key(x);
+                            const uint32_t to = ring + s * S::kStage + h % 2 * kHalf * 128;
+                            if (in_boxes) {
+                                const int u = u0 + my_box, t = u + (u >= p.kept ? gap : 0), page = pages[0];
+                                const bool bad = has_box && u < seen && (unsigned)page >= (unsigned)p.pool.n_pages, issue = has_box && u < seen && !bad;
+                                const int slot = t - page_of(p.pool, t) * p.pool.page_size;
+                                const uint32_t any_bad = __ballot_sync(~0u, bad), issues = __ballot_sync(~0u, issue);
 #pragma unroll
-                            for (int c = 0; c < kOffs; c++)
-                                there[c] = any_bad ? ~__reduce_or_sync(~0u, bad ? lowest(my_box + p.box - c * 32) & ~lowest(my_box - c * 32) : 0u) : ~0u;
+                                for (int c = 0; c < kOffs; c++)
+                                    rows_there[c] = any_bad ? ~__reduce_or_sync(~0u, bad ? lowest(my_box + p.box - c * 32) & ~lowest(my_box - c * 32) : 0u) : ~0u;
+                                const bool looks = kNarrow || (!key && (any_bad || partly_seen(p, k, u0 - h % 2 * kHalf, kKeys)));
+                                const uint32_t bar = looks ? landed(me, turn) : full(s);
+                                if (lane == 0) bar_expect(bar, __popc(issues) * p.box * 128);
+                                __syncwarp();
+                                if (issue)
+                                    copy_box(to + (my_part + (kNarrow ? kAcross : 0)) * (kKeys * 128) + my_box * 128, key ? &p.k_map : &p.v_map, my_part * (kNarrow ? 128 : 64),
+                                             p.key_dim ? slot : k.kv, p.key_dim ? k.kv : slot, page, bar);
+                                if (looks) issued = h, issued_turn = turn, turn ^= 1;
+                                else if (lane != 0) bar_arrive(full(s));
+                            } else {
+                                int64_t off[kOffs];  // of the rows of this lane's tokens, or -1
+#pragma unroll
+                                for (int c = 0; c < kOffs; c++) {
+                                    const int u = u0 + c * 32 + lane, t = u + (u >= p.kept ? gap : 0);
+                                    const bool there = (unsigned)pages[c] < (unsigned)p.pool.n_pages;
+                                    off[c] = u < seen && there ? (pages[c] * p.pool.stride_page + (t - page_of(p.pool, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes : -1;
+                                    rows_there[c] = ~__ballot_sync(~0u, u < seen && !there);
+                                }
+                                const char* const pool = (key ? p.pool.k : p.pool.v) + chunk * 16;
+                                constexpr int kBatch = kRounds / kOffs < 8 ? kRounds / kOffs : 8;
+#pragma unroll
+                                for (int c = 0; c < kOffs; c++) {
+#pragma unroll 1
+                                    for (int i0 = 0; i0 < kRounds / kOffs; i0 += kBatch) {
+#pragma unroll
+                                        for (int i = 0; i < kBatch; i++) {
+                                            const int row = (i0 + i) * kAtOnce + lane_row;
+                                            const int64_t o = __shfl_sync(~0u, off[c], row);
+                                            if (copies) copy16(to + place(c * 32 + row, kRaw + chunk), pool + (o < 0 ? 0 : o), o < 0 ? 0 : 16);
+                                        }
+                                    }
+                                }
+                                commit_copies();
+                                issued = h;
+                            }
                             if (lane == 0) {
-                                if (key) {
+                                bool any_bad = false;
 #pragma unroll
-                                    for (int c = 0; c < kOffs; c++) valid[(step0 + step_of(x)) & 7][h % 2 * kOffs + c] = there[c];  // (what lies behind the last token is no row's)
+                                for (int c = 0; c < kOffs; c++) {
+                                    if (key) valid[(step0 + step_of(x)) & 7][h % 2 * kOffs + c] = rows_there[c];  // (what lies behind the last token is no row's)
+                                    any_bad |= rows_there[c] != ~0u;
                                 }
                                 if (any_bad) flag(p.status, FCSIM_KV_BAD_PAGE);
                             }
-                            if (h + S::kLoadWarps < halves) fetch_pages(h + S::kLoadWarps);
-                            if (tile >= kStages && !__all_sync(~0u, bar_try(empty(s), (tile / kStages - 1) & 1))) {
-                                finish_all();
-                                if (!fine || !(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
-                            }
-                            const bool looks = kNarrow || (!key && (any_bad || partly_seen(p, k, (k.j + step_of(x)) * kKeys, kKeys)));
-                            const uint32_t bar = looks ? landed(me, turn) : full(s);
-                            if (lane == 0) bar_expect(bar, __popc(issues) * p.box * 128);
                             __syncwarp();
-                            if (issue)
-                                copy_box(ring + s * S::kStage + (my_part + (kNarrow ? kAcross : 0)) * (kKeys * 128) + (h % 2 * kHalf + my_box) * 128, key ? &p.k_map : &p.v_map,
-                                         my_part * (kNarrow ? 128 : 64), p.key_dim ? slot : k.kv, p.key_dim ? k.kv : slot, page, bar);
-                            if (looks) {
-                                if (pending >= 0) finish_all();  // (the one before)
-                                if (!fine) break;
-                                pending = h, holes = any_bad != 0, turn ^= 1;
-#pragma unroll
-                                for (int c = 0; c < kOffs; c++) holes_of[c] = there[c];
-                                if (!kNarrow) finish_all();
-                                if (!fine) break;
-                            } else if (lane != 0)
-                                bar_arrive(full(s));
                             h += S::kLoadWarps;
-                        } else {
-                        int64_t off[kOffs];  // of the rows of this lane's tokens, or -1
-#pragma unroll
-                        for (int c = 0; c < kOffs; c++) {
-                            const int u = (k.j + step_of(x)) * kKeys + h % 2 * kHalf + c * 32 + lane, t = u + (u >= p.kept ? gap : 0);
-                            const bool there = (unsigned)pages[c] < (unsigned)p.pool.n_pages;
-                            off[c] = u < seen && there ? (pages[c] * p.pool.stride_page + (t - page_of(p.pool, t) * p.pool.page_size) * p.pool.stride_slot + head) * C::bytes : -1;
-                            if (key) {
-                                const uint32_t bad = __ballot_sync(~0u, u < seen && !there);
-                                if (lane == 0) {
-                                    valid[(step0 + step_of(x)) & 7][h % 2 * kOffs + c] = ~bad;  // (what lies behind the last token is no row's)
-                                    if (bad) flag(p.status, FCSIM_KV_BAD_PAGE);
-                                }
-                            }
+                            if (h < halves) fetch_pages(h);
                         }
-                        if (h + S::kLoadWarps < halves) fetch_pages(h + S::kLoadWarps);
-                        if (tile >= kStages && !__all_sync(~0u, bar_try(empty(s), (tile / kStages - 1) & 1))) {
-                            finish_all();
-                            if (!(fine = wait(empty(s), (tile / kStages - 1) & 1))) break;
-                        }
-                        const uint32_t to = ring + s * S::kStage + h % 2 * kHalf * 128;
-                        const char* const pool = (key ? p.pool.k : p.pool.v) + chunk * 16;
-                        // (the lanes ask each other for eight offsets before the first is used: one by one a copy took 76 clocks)
-                        constexpr int kBatch = kRounds / kOffs < 8 ? kRounds / kOffs : 8;
-#pragma unroll
-                        for (int c = 0; c < kOffs; c++) {
-#pragma unroll 1
-                            for (int i0 = 0; i0 < kRounds / kOffs; i0 += kBatch) {
-                                int64_t o[kBatch];
-#pragma unroll
-                                for (int i = 0; i < kBatch; i++) o[i] = __shfl_sync(~0u, off[c], (i0 + i) * kAtOnce + lane_row);
-                                if (copies) {
-#pragma unroll
-                                    for (int i = 0; i < kBatch; i++)
-                                        copy16(to + place(c * 32 + (i0 + i) * kAtOnce + lane_row, kRaw + chunk), pool + (o[i] < 0 ? 0 : o[i]), o[i] < 0 ? 0 : 16);
-                                }
-                            }
-                        }
-                        commit_copies();
-                        if (kNarrow && pending >= 0) {
-                            wait_copies<1>();
-                            finish();
-                        }
-                        pending = h;
-                        h += S::kLoadWarps;
-                        if (!kNarrow && !query_due) finish_all();
-                        }
-                    }
-                    if (query_due && in_boxes && me != 0) {  // (the first warp brings Q)
-                        query_due = false;
-                        continue;
                     }
                     if (query_due) {
-                        if (segment > 0 && !__all_sync(~0u, bar_try(query_empty, (segment - 1) & 1))) {
-                            finish_all();
-                            if (!fine || !(fine = wait(query_empty, (segment - 1) & 1))) break;
-                        }
+                        if (segment > 0 && !(fine = wait(query_empty, (segment - 1) & 1))) break;
                         if (in_boxes) {
                             // all rows of the block, or tile after tile; what lies behind the request's rows is no row of the block
                             const int boxes = p.query_tokens == p.tokens_a_block ? 1 : k.tiles_in_use, rows = p.query_tokens * heads_a_tile;
@@ -1355,37 +1264,121 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                             if (lane < boxes * (DP / 64))
                                 copy_box(query + lane / (DP / 64) * (128 * 128) + lane % (DP / 64) * (S::kRows * 128), &p.q_map, lane % (DP / 64) * 64,
                                          k.kv * group + k.ht * heads_a_tile, k.row + lane / (DP / 64) * p.query_tokens, query_full);
-                            query_due = false;
-                            continue;
-                        }
-                        constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
-                        const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
+                        } else {
+                            constexpr int kQueryLanes = DP / 8, kQueryRows = 32 / kQueryLanes;
+                            const int at = lane % kQueryLanes, head0 = k.kv * group + k.ht * heads_a_tile, part = min(heads_a_tile, group - k.ht * heads_a_tile);
 #pragma unroll 1
-                        for (int r0 = me * 16; r0 < k.tiles_in_use * 128; r0 += 16 * S::kLoadWarps) {
-                            const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
-                            int64_t off = -1;
-                            if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
-                            int64_t o[16 / kQueryRows];
-#pragma unroll
-                            for (int i = 0; i < 16 / kQueryRows; i++) o[i] = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
-                            if (at < D / 8) {
+                            for (int r0 = me * 16; r0 < k.tiles_in_use * 128; r0 += 16 * S::kLoadWarps) {
+                                const int row = r0 + lane % 16, token = row * token_magic >> 16, g = row - token * heads_a_tile;
+                                int64_t off = -1;
+                                if (token < k.tokens && g < part) off = ((int64_t)(k.row + token) * p.q_row + (int64_t)(head0 + g) * p.q_head) * 2;
 #pragma unroll
                                 for (int i = 0; i < 16 / kQueryRows; i++) {
+                                    const int64_t o = __shfl_sync(~0u, off, i * kQueryRows + lane / kQueryLanes);
                                     const int y = r0 + i * kQueryRows + lane / kQueryLanes;
-                                    copy16(query + at / 8 * (S::kRows * 128) + y * 128 + ((at % 8) ^ (y % 8)) * 16,
-                                           p.q + (o[i] < 0 ? 0 : o[i] + at * 16), o[i] < 0 ? 0 : 16);
+                                    if (at < D / 8)
+                                        copy16(query + at / 8 * (S::kRows * 128) + y * 128 + ((at % 8) ^ (y % 8)) * 16, p.q + (o < 0 ? 0 : o + at * 16), o < 0 ? 0 : 16);
+                                }
+                            }
+                            commit_copies();
+                            wait_copies<0>();
+                            fence_for_products();
+                            bar_arrive(query_full);
+                        }
+                        query_due = false;
+                    }
+                    // The half before this one, whose copies had the time of this one's.  (One by one they take longer than to arrive: then it is this one.)
+                    bool pending_now = pending >= 0;
+                    if (!in_boxes && !kNarrow && issued >= 0) {
+                        pending_now = true, pending = issued, issued = -1;
+#pragma unroll
+                        for (int c = 0; c < kOffs; c++) pending_rows[c] = rows_there[c];
+                    }
+                    if (pending_now) {
+                        if (in_boxes) {
+                            if (!(fine = wait(landed(me, pending_turn), landed_parity >> pending_turn & 1))) break;
+                            landed_parity ^= 1u << pending_turn;
+                        } else if (issued >= 0)
+                            wait_copies<1>();
+                        else
+                            wait_copies<0>();
+                        const int x = pending / 2, s = (tile0 + x) % kStages, u0 = (k.j + step_of(x)) * kKeys + pending % 2 * kHalf;
+                        const uint32_t to = ring + s * S::kStage + pending % 2 * kHalf * 128;
+                        uint32_t gone[kOffs];  // rows without a token, or of pages outside the pool
+                        bool edge = partly_seen(p, k, u0 - pending % 2 * kHalf, kKeys);
+#pragma unroll
+                        for (int c = 0; c < kOffs; c++) {
+                            gone[c] = ~lowest(seen - u0 - c * 32) | ~pending_rows[c];
+                            edge |= gone[c] != 0;
+                        }
+                        // What some row does not see must not meet its weight of zero as an infinity or NaN.
+                        edge = edge && !is_key(x);
+                        auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
+                        bool found = false;
+                        if constexpr (kNarrow) {
+                            // Eight lanes take four pieces each of rows r and r ^ 5: so both what they read and what they write lies in all banks.
+                            constexpr int kGroups = kLanes / 4, kPairs = 4 / kGroups, kBatch = 4;  // rows a lane reads before the first is written over
+                            const int turned_chunk = (lane >> 3) % kGroups * 4 + (lane & 3), swap = lane & 4 ? 5 : 0;
+                            const bool turns = turned_chunk < chunks;
+                            auto turned_row = [&](int i) {
+                                const int pair = i * kPairs + (lane >> 3) / kGroups;
+                                return pair / 4 * 8 + (pair % 4 ^ swap);
+                            };
+#pragma unroll 1
+                            for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
+                                uint4 raw[kBatch];
+                                __syncwarp();
+#pragma unroll
+                                for (int i = 0; i < kBatch; i++) {
+                                    raw[i] = make_uint4(0, 0, 0, 0);
+                                    if (turns) raw[i] = load16(to + place(turned_row(i0 + i), kRaw + turned_chunk));
+                                }
+                                if (edge) {
+#pragma unroll 1
+                                    for (int i = 0; i < kBatch; i++) {
+                                        uint4 y = raw[0];
+                                        if (i == 1) y = raw[1];
+                                        if (i == 2) y = raw[2];
+                                        if (i == 3) y = raw[3];
+                                        if (is_gone(turned_row(i0 + i))) y = make_uint4(0, 0, 0, 0);
+                                        else found |= make_finite8(y);
+                                        if (i == 0) raw[0] = y;
+                                        if (i == 1) raw[1] = y;
+                                        if (i == 2) raw[2] = y;
+                                        if (i == 3) raw[3] = y;
+                                    }
+                                }
+                                __syncwarp();
+#pragma unroll
+                                for (int i = 0; i < kBatch; i++) {
+                                    uint4 a, b;
+                                    widen<T>(raw[i], a, b);
+                                    if (turns) {
+                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk), a);
+                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk + 1), b);
+                                    }
+                                }
+                            }
+                        } else if (edge && copies) {
+#pragma unroll 4
+                            for (int i = 0; i < kRounds; i++) {
+                                const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
+                                uint4 y = load16(at);
+                                if (is_gone(i * kAtOnce + lane_row)) store16(at, make_uint4(0, 0, 0, 0));
+                                else if (make_finite<T>(y)) {
+                                    store16(at, y);
+                                    found = true;
                                 }
                             }
                         }
-                        commit_copies();
-                        wait_copies<0>();
-                        if (pending >= 0) finish();
+                        if (found) infinite[segment % kSegments] = 1;
                         fence_for_products();
-                        bar_arrive(query_full);
-                        query_due = false;
+                        bar_arrive(full(s));
                     }
+                    pending = issued, pending_turn = issued_turn;
+#pragma unroll
+                    for (int c = 0; c < kOffs; c++) pending_rows[c] = rows_there[c];
                 }
-                if (fine) finish_all();
                 if (!fine) {  // what is on its way arrives before the CTA ends
                     const int64_t began = clock64();
                     while (clock64() - began < 4000000) {}
