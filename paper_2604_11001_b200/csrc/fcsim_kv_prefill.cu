@@ -347,6 +347,30 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, in
         if (all[1] * heads <= gridDim.x) {
             const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);
             d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
+            if (warps == 1 && d.cut >= longest) {
+                // Every block whole, one a CTA: few numbers, all small.  (The general way takes 4 us, as long as the rest of a small call.)
+                const int own = blocks_of(p, rows) * heads;
+                int upto = own;
+#pragma unroll
+                for (int i = 1; i < 32; i <<= 1) {
+                    const int x = __shfl_up_sync(~0u, upto, i);
+                    if (lane >= i) upto += x;
+                }
+                const int me_first = blockIdx.x;
+                const uint32_t found = __ballot_sync(~0u, upto > me_first);
+                d.first = d.end = 0;
+                if (found && lane == __ffs(found) - 1) {
+                    Block k;
+                    const int x = me_first - (upto - own), n = blocks_of(p, rows), head = (unsigned)x / (unsigned)n;
+                    k.r = lane, k.b = x - head * n;
+                    k.kv = (unsigned)head / (unsigned)p.head_tiles, k.ht = head - k.kv * p.head_tiles;
+                    k.rows = request_rows(p, lane, k.row0), k.position0 = position0;
+                    enter_block<KEYS>(p, k);
+                    start.block = k;
+                    start.j = 0, start.left = k.tiles, start.first_unit = 0, start.piece = 0, start.pieces = 1;
+                }
+                return d;
+            }
             if (min(d.cut, longest) <= divide(all[0] * heads, gridDim.x) + kShareCost) continue;
             d.cut = 0;
         }
@@ -533,7 +557,13 @@ __device__ __forceinline__ bool make_finite(uint4& x) {
     return a || b || c || d;
 }
 
-// The same for NaN among sixteen 8-bit elements.
+// Whether there are any among eight: bits of the result.
+template <class T>
+__device__ __forceinline__ uint32_t infinite_among(const uint4& x) {
+    constexpr uint32_t kStep = std::is_same<T, F16>::value ? 0x04000400u : 0x00800080u;  // carries into the sign where the exponent is all ones
+    return (((x.x & 0x7fff7fffu) + kStep) | ((x.y & 0x7fff7fffu) + kStep) | ((x.z & 0x7fff7fffu) + kStep) | ((x.w & 0x7fff7fffu) + kStep)) & 0x80008000u;
+}
+// The same as the first for NaN among sixteen 8-bit elements.
 __device__ __forceinline__ bool make_finite8(uint4& x) {
     uint32_t* const w = &x.x;
     uint32_t any = 0;
@@ -760,19 +790,20 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     };
 
     constexpr int kProductWarp = S::kWarps - 2, kPlanWarp = S::kWarps - 1;
-    if (tid == 0) {
-#pragma unroll 1
-        for (int s = 0; s < kStages; s++) bar_init(full(s), 64), bar_init(empty(s), 1);
-#pragma unroll 1
-        for (int s = 0; s < kSegments; s++) bar_init(told_of(s), 1), bar_init(done_with(s), S::kWarps - 1);
-#pragma unroll 1
-        for (int s = 0; s < 2; s++) bar_init(score_full(s), 1), bar_init(weights_ready(s), 128), bar_init(output_full(s), 1), bar_init(meeting(s), 128);
-#pragma unroll 1
-        for (int s = 0; s < S::kLoadWarps; s++) bar_init(landed(s, 0), 1), bar_init(landed(s, 1), 1);
-        bar_init(query_full, p.box ? 1 : 32 * S::kLoadWarps), bar_init(query_empty, 1), bar_init(added, 1), bar_init(drained, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        stuck = 0;
-        start.left = 0;
+    {
+        // how many arrivals each of the barriers, in the order in which they lie, waits for
+        constexpr int kBars = 2 * kStages + 2 * kSegments + 12 + 2 * S::kLoadWarps;
+        if (tid < kBars) {
+            const int i = tid - 2 * kStages - 2 * kSegments;
+            int count = 1;
+            if (tid < kStages) count = 64;                                                        // full
+            else if (tid >= 2 * kStages + kSegments && i < 0) count = S::kWarps - 1;              // done_with
+            else if ((i >= 2 && i < 4) || (i >= 6 && i < 8)) count = 128;                         // weights_ready, meeting
+            else if (i == 8) count = p.box ? 1 : 32 * S::kLoadWarps;                              // query_full
+            bar_init(bar0 + tid * 8, count);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        if (tid == 0) stuck = 0, start.left = 0;
     }
     if (warp == kProductWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)), "r"(S::kColumns) : "memory");
@@ -1360,14 +1391,22 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                 }
                             }
                         } else if (edge && copies) {
-#pragma unroll 4
-                            for (int i = 0; i < kRounds; i++) {
-                                const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
-                                uint4 y = load16(at);
-                                if (is_gone(i * kAtOnce + lane_row)) store16(at, make_uint4(0, 0, 0, 0));
-                                else if (make_finite<T>(y)) {
-                                    store16(at, y);
-                                    found = true;
+                            uint32_t any = 0;
+#pragma unroll 8
+                            for (int i = 0; i < kRounds; i++) any |= infinite_among<T>(load16(to + place(i * kAtOnce + lane_row, chunk)));
+                            uint32_t none = 0;
+#pragma unroll
+                            for (int c = 0; c < kOffs; c++) none |= gone[c];
+                            if (any | none) {
+#pragma unroll 1
+                                for (int i = 0; i < kRounds; i++) {
+                                    const uint32_t at = to + place(i * kAtOnce + lane_row, chunk);
+                                    uint4 y = load16(at);
+                                    if (is_gone(i * kAtOnce + lane_row)) store16(at, make_uint4(0, 0, 0, 0));
+                                    else if (any && make_finite<T>(y)) {
+                                        store16(at, y);
+                                        found = true;
+                                    }
                                 }
                             }
                         }
