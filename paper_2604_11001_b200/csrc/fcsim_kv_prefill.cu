@@ -898,6 +898,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 const int token = shared ? token_first : token_own, head = k.ht * heads_a_tile + (shared ? g_first : g_own);
                 x.real = token < k.tokens && head < group;
                 x.out = (int64_t)(k.row + token) * p.n_heads + k.kv * group + head;
+                // A warp without a real row leaves the scores as they are for its weights: what becomes of them is nobody's output.
+                const bool idle = !__any_sync(~0u, x.real);
                 // (never zero, so that what is not seen, a logit of -infinity, stays without weight: 2^-149 times the largest logit is 5e-7)
                 float unit = fabsf(kNarrow ? p.scale * p.pool.k_scale[k.kv] : p.scale) * kLog2e;
                 if (unit < 1.4e-45f) unit = 1.4e-45f;
@@ -913,6 +915,11 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
                     score_parity[slot] ^= 1;
                     fence_after_sync();
+                    if (idle) {
+                        fence_before_sync();
+                        bar_arrive(weights_ready(slot));
+                        continue;
+                    }
                     const uint32_t* const there = valid[(step0 + t) & 7];
                     uint32_t some = ~0u;
 #pragma unroll
@@ -1010,7 +1017,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
                 // this CTA's part is the first of its two, unless the block begins here
                 float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
-                if (worked) {
+                if (worked && !idle) {
                     if (infinite[segment % kSegments]) leave_with_infinite<T, C, kKeys>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
                     else leave<T, C, kKeys, false>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
                     fence_before_sync();
@@ -1018,9 +1025,11 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 if (!has_part) {
                     if (x.real) leave_lse(p, x.out, sum, add);
                 } else {
-                    part[DP * 128 + x.row] = add;
-                    part[(DP + 1) * 128 + x.row] = sum;
-                    __threadfence();
+                    if (!idle) {
+                        part[DP * 128 + x.row] = add;
+                        part[(DP + 1) * 128 + x.row] = sum;
+                        __threadfence();
+                    }
                     if (!(fine = meet())) break;
                     if (x.row == 0) {
                         int* const counter = p.counters + k.first_part * 2 + (shared ? 0 : i);
@@ -1029,7 +1038,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         if (last) *counter = 0;
                     }
                     if (!(fine = meet())) break;
-                    if (joins[i]) {
+                    if (joins[i] && !idle) {
                         __threadfence();
                         const int tile = shared ? 0 : i;
                         Parts parts;
