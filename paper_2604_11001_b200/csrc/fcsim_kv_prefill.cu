@@ -610,49 +610,61 @@ __device__ __forceinline__ void store_columns(const PrefillParams& p, int64_t ou
     }
 }
 
-// O of a row, 32 columns of tensor memory at a time, to the output or to a part.  INFINITE: tiles that are not seen whole had infinite or NaN
-// elements of v, which were left out of the products: those that this row sees are added (tiles t0, t0 + by, .. of the segment).
-template <class T, class C, int KEYS, bool INFINITE>
-__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by, float* part, float f, bool none) {
+// Tiles that are not seen whole had infinite or NaN elements of v, which were left out of the products: those that this row sees are added to
+// its O (tiles t0, t0 + by, .. of the segment).
+template <class C, int KEYS>
+__device__ __noinline__ void add_infinite(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by) {
     const int D = p.pool.head_dim;
 #pragma unroll 1
-    for (int c = 0; c * 32 < D; c++) {
+    for (int c = 0; c * 16 < D; c++) {
+        float o[16];
+        tmem_load16(x.at + 16 * c, o);
+        wait_loads();
+        if (x.real)
+#pragma unroll 1
+            for (int j = k.j + t0; j < k.j + k.steps; j += by) {
+                if (!partly_seen(p, k, j * KEYS, KEYS)) continue;
+#pragma unroll 1
+                for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
+                    if (u > x.position || (u < x.from && u >= p.first)) continue;
+                    const int t = u + (u >= p.kept ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
+                    if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
+                    const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head + c * 16) * C::bytes;
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        if (c * 16 + 2 * e < D) {
+                            float2 y;
+                            if constexpr (C::bytes == 1) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
+                            else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
+                            if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
+                            if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
+                        }
+                }
+            }
+        __syncwarp();  // (lanes that are not here yet would lose registers to the next load from tensor memory)
+        uint32_t y[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++) y[e] = __float_as_uint(o[e]);
+        tmem_store16(x.at + 16 * c, y);
+    }
+    wait_stores();
+}
+
+// O of a row, 32 columns of tensor memory at a time, to the output or to a part.
+template <class T>
+__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, float* part, float f, bool none) {
+#pragma unroll 1
+    for (int c = 0; c * 32 < p.pool.head_dim; c++) {
         float o[32];
         tmem_load(x.at + 32 * c, o);
         wait_loads();
-        if constexpr (INFINITE) {
-            if (x.real)
-#pragma unroll 1
-                for (int j = k.j + t0; j < k.j + k.steps; j += by) {
-                    if (!partly_seen(p, k, j * KEYS, KEYS)) continue;
-#pragma unroll 1
-                    for (int u = j * KEYS; u < min(k.seen, (j + 1) * KEYS); u++) {
-                        if (u > x.position || (u < x.from && u >= p.first)) continue;
-                        const int t = u + (u >= p.kept ? k.gap : 0), i = page_of(p.pool, t), page = p.table[k.r * p.table_row + i];
-                        if ((unsigned)page >= (unsigned)p.pool.n_pages) continue;
-                        const char* const v = p.pool.v + (page * p.pool.stride_page + (t - i * p.pool.page_size) * p.pool.stride_slot + k.kv * p.pool.stride_head + c * 32) * C::bytes;
-#pragma unroll
-                        for (int e = 0; e < 16; e++)
-                            if (c * 32 + 2 * e < D) {
-                                float2 y;
-                                if constexpr (C::bytes == 1) y = F16::unpack(E4M3::halves(*reinterpret_cast<const uint16_t*>(v + 2 * e)));
-                                else y = C::unpack(*reinterpret_cast<const uint32_t*>(v + 4 * e));
-                                if (!(fabsf(y.x) < INFINITY)) o[2 * e] += y.x;
-                                if (!(fabsf(y.y) < INFINITY)) o[2 * e + 1] += y.y;
-                            }
-                    }
-                }
-        }
         if (part) {  // fours of columns
 #pragma unroll
             for (int e = 0; e < 32; e += 4) reinterpret_cast<float4*>(part)[(c * 8 + e / 4) * 128 + x.row] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         } else if (x.real)
             store_columns<T>(p, x.out, c, o, f, none);
+        __syncwarp();  // (as above)
     }
-}
-template <class T, class C, int KEYS>
-__device__ __noinline__ void leave_with_infinite(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by, float* part, float f, bool none) {
-    leave<T, C, KEYS, true>(p, x, k, t0, by, part, f, none);
 }
 
 // A row's log-sum-exp from the sum of its weights 2^(logit + add).
@@ -961,6 +973,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                             limit = most + kLag;
                             sum *= shrink;
                         }
+                        __syncwarp();  // (a warp that has come apart must not load from tensor memory: what comes is written to all lanes' registers)
                         if (t > step_first) {
                             if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
                             fence_after_sync();
@@ -1018,8 +1031,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 // this CTA's part is the first of its two, unless the block begins here
                 float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
                 if (worked && !idle) {
-                    if (infinite[segment % kSegments]) leave_with_infinite<T, C, kKeys>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
-                    else leave<T, C, kKeys, false>(p, x, k, step_first, step_by, part, f, sum == 0.0f);
+                    if (infinite[segment % kSegments]) add_infinite<C, kKeys>(p, x, k, step_first, step_by);
+                    leave<T>(p, x, part, f, sum == 0.0f);
                     fence_before_sync();
                 }
                 if (!has_part) {

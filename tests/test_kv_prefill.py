@@ -1,17 +1,12 @@
 """prefill against plain 64-bit forms of its definition: several query tokens per request over a paged cache."""
-import ctypes as C
 import math
-import os
-import subprocess
 
 import pytest
 import torch
 
-from kv_common import DT, make_table, wide
+from kv_common import DT, make_table
 from kv_prompt_common import assert_prompt
-from paper_2604_11001_b200 import kvcache as kv
 from test_kv_gpu import gen, make_cache, randn
-from test_kv_host import CACHE, EINVAL, ESIZE, ROOT
 
 
 def spoil(c, table, lengths, page, window, first, new):
