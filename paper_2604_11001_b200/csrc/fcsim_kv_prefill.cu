@@ -177,8 +177,9 @@ struct Shape {
     static constexpr int kBytes = kQuery + kStages * kStage;
     static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 6;
     static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 2, kThreads = 32 * kWarps;
-    // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's.
-    static constexpr int kSoftmaxRegisters = 160, kOtherRegisters = 96;
+    // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's: fewer where they turn
+    // 8-bit rows (8 192 tokens, 32 heads, 8-bit cache: 144 and 112 take 1 065 us, 160 and 96 1 155; a 16-bit one 718 and 682).
+    static constexpr int kSoftmaxRegisters = C::bytes == 1 ? 144 : 160, kOtherRegisters = 256 - kSoftmaxRegisters;
     // A warp loads half a tile at a time.  It waits for the place of a tile by the parity of one barrier, so the tile that was there two rounds before
     // has to be gone: it is, as what the warp has loaded last waited for a later one.
     static_assert(kLoadWarps <= 2 * kStages, "parities");
@@ -1197,6 +1198,21 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             auto place = [&](int row, int at) { return (uint32_t)(at / 8 * (kKeys * 128) + row * 128 + ((at % 8) ^ (row % 8)) * 16); };
             constexpr int kRaw = kNarrow ? DP / 16 : 0;
             uint32_t landed_parity = 0, turn = 0;  // of the two barriers, a bit each; the next
+            // 8-bit rows are turned by eight lanes that take four pieces each of rows r and r ^ 5: so both what they read and what they write lies in all
+            // banks.  The places of a lane's pieces, as they were and as they will be, for the first rows; the others follow 8 rows apart.
+            constexpr int kGroups = kLanes < 4 ? 1 : kLanes / 4, kPairs = 4 / kGroups, kBases = kGroups;
+            const int turned_chunk = (lane >> 3) % kGroups * 4 + (lane & 3), swap = lane & 4 ? 5 : 0;
+            auto turned_row = [&](int i) {
+                const int pair = i * kPairs + (lane >> 3) / kGroups;
+                return pair / 4 * 8 + (pair % 4 ^ swap);
+            };
+            uint32_t place_raw[kBases], place_low[kBases], place_high[kBases];
+            if constexpr (kNarrow)
+#pragma unroll
+                for (int i = 0; i < kBases; i++) {
+                    place_raw[i] = place(turned_row(i), kRaw + turned_chunk);
+                    place_low[i] = place(turned_row(i), 2 * turned_chunk), place_high[i] = place(turned_row(i), 2 * turned_chunk + 1);
+                }
             while (next_segment(wait)) {
                 const Segment& k = segments[segment % kSegments];
                 const int steps = k.steps, halves = 4 * steps, gap = k.gap, seen = k.seen;
@@ -1369,14 +1385,9 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         auto is_gone = [&](int row) { return (row < 32 || kOffs == 1 ? gone[0] : gone[kOffs - 1]) >> row % 32 & 1; };
                         bool found = false;
                         if constexpr (kNarrow) {
-                            // Eight lanes take four pieces each of rows r and r ^ 5: so both what they read and what they write lies in all banks.
-                            constexpr int kGroups = kLanes / 4, kPairs = 4 / kGroups, kBatch = 4;  // rows a lane reads before the first is written over
-                            const int turned_chunk = (lane >> 3) % kGroups * 4 + (lane & 3), swap = lane & 4 ? 5 : 0;
+                            constexpr int kBatch = 4;  // rows a lane reads before the first is written over
                             const bool turns = turned_chunk < chunks;
-                            auto turned_row = [&](int i) {
-                                const int pair = i * kPairs + (lane >> 3) / kGroups;
-                                return pair / 4 * 8 + (pair % 4 ^ swap);
-                            };
+                            auto rows_on = [&](int i0, int i) { return to + (i0 / kBases + i / kBases) * 1024; };
 #pragma unroll 1
                             for (int i0 = 0; i0 < kRounds; i0 += kBatch) {
                                 uint4 raw[kBatch];
@@ -1384,7 +1395,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
 #pragma unroll
                                 for (int i = 0; i < kBatch; i++) {
                                     raw[i] = make_uint4(0, 0, 0, 0);
-                                    if (turns) raw[i] = load16(to + place(turned_row(i0 + i), kRaw + turned_chunk));
+                                    if (turns) raw[i] = load16(rows_on(i0, i) + place_raw[i % kBases]);
                                 }
                                 if (edge) {
 #pragma unroll 1
@@ -1407,8 +1418,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                     uint4 a, b;
                                     widen<T>(raw[i], a, b);
                                     if (turns) {
-                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk), a);
-                                        store16(to + place(turned_row(i0 + i), 2 * turned_chunk + 1), b);
+                                        store16(rows_on(i0, i) + place_low[i % kBases], a);
+                                        store16(rows_on(i0, i) + place_high[i % kBases], b);
                                     }
                                 }
                             }
