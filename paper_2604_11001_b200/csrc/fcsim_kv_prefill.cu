@@ -6,14 +6,22 @@
 // * The query heads of a kv head and a run of tokens are the rows of a block: one or two tiles of 128 (token, head) pairs, so that
 //   few new tokens fill a tile as well as many do, and what is loaded of K and V serves all of them.
 // * Both products run on tcgen05: S = Q K^T from shared memory into tensor memory, P back into the columns S had, O += P V with
-//   P read from tensor memory.  One thread issues them; two groups of four warps, a row each thread, do the softmax of one tile while the
-//   other tile's products run; three warps load.
-// * Pages may have any size and strides, so rows come by cp.async, 16 bytes a lane, into the 128-byte swizzled layout that the products
-//   read (8-bit rows through registers, as 16 bits, exactly).
+//   P read from tensor memory.  One thread issues them.  Each tile of rows has a group of four warps, a row a thread, for its softmax, whose
+//   time is that of the other tile's products; with one tile of rows the groups take its tiles of keys in turn.
+// * Six warps load, half a tile each in turn, into a ring: by bulk copies of the pages' tokens where a page is whole boxes of 8 tokens or
+//   more, else 16 bytes a lane (cp.async), both in the 128-byte swizzled layout that the products read.  (8 192 tokens, 32 heads:
+//   688 us in boxes, 745 by lanes.)  8-bit rows are turned into 16 bits, exactly, in shared memory.  What some row of a tile does not see is
+//   looked over in v: infinities and NaN would reach rows whose weight for them is zero.  One warp walks over the work ahead of the others.
 // * The work is counted in tiles of keys, laid end to end over all requests, heads and blocks, and every CTA takes an equal stretch (or, where
 //   there are few blocks, one piece of one block).  Parts of a block that lies across stretches are joined by the last to come, in
 //   their order: the same call gives the same bits.
-// * s, m, the sums and o are 32-bit.  p meets v in two 16-bit parts that add up to it to 2^-16 or better.
+// * s, m, the sums and o are 32-bit.  p meets v in two 16-bit parts that add up to it to 2^-14 (bf16) or 2^-20 (f16): with one, its rounding
+//   would be as large as the output's own.  The second part is a third of the products: of two tiles of rows and 128 keys the scores take 1 024
+//   clocks (64 a product of 128 x 128 x 16), the parts 1 024 each; the exponentials, beside them, 2 050.
+//
+// Bounds.  Long prompts: the products, 3 072 clocks of the 4 300 that such a step takes (8 192 tokens, 32 heads of 128: 680 us, 810 TFLOP/s with p
+// counted once, 1 215 of products done); the rest is what one tile's softmax takes longer than the other tile's products.  Few tokens over a long context: the loads, at 4.1 TB/s
+// (16 x 7 tokens over 8 000: 129 us), and with an 8-bit cache the instructions that turn them (231 us).  Small calls: latency, 10 us.
 #include <math.h>
 
 #include <algorithm>
@@ -597,10 +605,9 @@ __device__ __forceinline__ void store32(char* to, const uint32_t (&y)[8], bool a
     }
 }
 template <class T>
-__device__ __forceinline__ void store_columns(const PrefillParams& p, int64_t out_row, int c, const float (&o)[32], float f, bool none) {
-    const int D = p.pool.head_dim;
-    char* const to = p.out + (out_row * D + c * 32) * 2;
-    const bool aligned = D % 16 == 0 && ((uintptr_t)p.out & 31) == 0;
+__device__ __forceinline__ void store_columns(char* out, int D, int64_t out_row, int c, const float (&o)[32], float f, bool none) {
+    char* const to = out + (out_row * D + c * 32) * 2;
+    const bool aligned = D % 16 == 0 && ((uintptr_t)out & 31) == 0;
 #pragma unroll
     for (int e = 0; e < 2; e++) {
         uint32_t y[8];
@@ -614,7 +621,7 @@ __device__ __forceinline__ void store_columns(const PrefillParams& p, int64_t ou
 // Tiles that are not seen whole had infinite or NaN elements of v, which were left out of the products: those that this row sees are added to
 // its O (tiles t0, t0 + by, .. of the segment).
 template <class C, int KEYS>
-__device__ __noinline__ void add_infinite(const PrefillParams& p, const Row& x, const Segment& k, int t0, int by) {
+__device__ __noinline__ void add_infinite(const PrefillParams& p, Row x, const Segment& k, int t0, int by) {
     const int D = p.pool.head_dim;
 #pragma unroll 1
     for (int c = 0; c * 16 < D; c++) {
@@ -663,30 +670,31 @@ __device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, floa
 #pragma unroll
             for (int e = 0; e < 32; e += 4) reinterpret_cast<float4*>(part)[(c * 8 + e / 4) * 128 + x.row] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         } else if (x.real)
-            store_columns<T>(p, x.out, c, o, f, none);
+            store_columns<T>(p.out, p.pool.head_dim, x.out, c, o, f, none);
         __syncwarp();  // (as above)
     }
 }
 
 // A row's log-sum-exp from the sum of its weights 2^(logit + add).
-__device__ __forceinline__ void leave_lse(const PrefillParams& p, int64_t out, float sum, float add) {
-    if (p.lse) p.lse[out] = sum == 0.0f ? -INFINITY : logf(sum) - add * 0.6931471805599453f;
+__device__ __forceinline__ void leave_lse(float* lse, int64_t out, float sum, float add) {
+    if (lse) lse[out] = sum == 0.0f ? -INFINITY : logf(sum) - add * 0.6931471805599453f;
 }
 
-// Parts of a row, `n` of them, in their order: the first at `first`, the others from `rest` on, `stride` floats apart.
-struct Parts {
-    const float *first, *rest;
-    int64_t stride;
-    int n;
-    __device__ __forceinline__ const float* at(int x) const { return x == 0 ? first : rest + (x - 1) * stride; }
-};
-// Adds up the parts of a block's tile: references, sums and outputs of each, a row a thread.  With `shared` a part is a pair of tiles' parts.
+// Adds up the parts of a block's tile, in their order: references, sums and outputs of each; of row `at` a thread, 32 columns of every `by` times 32, from
+// `c0` times 32 on (few rows are shared by the warps).  The first is at `first`, the others of
+// `n` from `rest` on, `stride` floats apart; with `pairs` = 2 each is one of a tile's group and, kPart behind it, one of the other's.  (All that it is
+// told comes in registers.  What is passed by its address lies in memory, and with the shared memory that this kernel takes there is next to no
+// cache before L2: a join of 16 parts took 70 us that way.)
 template <class T, int DP>
-__device__ __noinline__ void join(const PrefillParams& p, const Row& row, const Parts& parts, bool shared, float vscale) {
+__device__ __noinline__ void join(char* out, float* lse, int D, int at, int64_t out_row, bool real, const float* first, const float* rest, int64_t stride, int n, int pairs,
+                                  int c0, int by, float vscale) {
     constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
-    const int pairs = shared ? 2 : 1, n = parts.n * pairs;
-    auto part = [&](int x) { return shared ? parts.at(x >> 1) + (x & 1) * kPart : parts.at(x); };
-    // They come from L2 at a microsecond each: what can be asked for at once is.
+    n *= pairs;
+    auto part = [&](int x) {
+        const int y = pairs == 2 ? x >> 1 : x;
+        return (y == 0 ? first : rest + (y - 1) * stride) + (pairs == 2 ? (x & 1) * kPart : 0);
+    };
+    // What can be asked for at once is.
     constexpr int kMost = 8;
     float add[kMost], least = INFINITY, all = 0;  // references as numbers to add; the least is the highest reference
 #pragma unroll 1
@@ -694,7 +702,7 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
         float sum[kMost];
 #pragma unroll
         for (int x = 0; x < kMost; x++) {
-            const float* const from = part(min(x0 + x, n - 1)) + DP * 128 + row.row;
+            const float* const from = part(min(x0 + x, n - 1)) + DP * 128 + at;
             add[x] = __ldcg(from), sum[x] = __ldcg(from + 128);
         }
         const float before = least;
@@ -713,14 +721,14 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
         for (int x = 0; x < kMost; x++) add[x] = add[x] == INFINITY ? 0.0f : power2(least - add[x]);  // now factors
     }
 #pragma unroll 1
-    for (int c = 0; c * 32 < p.pool.head_dim; c++) {
+    for (int c = c0; c * 32 < D; c += by) {
         float o[32] = {};
 #pragma unroll 1
         for (int x0 = 0; x0 < n; x0 += kMost) {
             if (n > kMost) {
 #pragma unroll
                 for (int x = 0; x < kMost; x++) {
-                    const float a = x0 + x < n ? __ldcg(part(x0 + x) + DP * 128 + row.row) : INFINITY;
+                    const float a = x0 + x < n ? __ldcg(part(x0 + x) + DP * 128 + at) : INFINITY;
                     add[x] = a == INFINITY ? 0.0f : power2(least - a);
                 }
             }
@@ -730,24 +738,25 @@ __device__ __noinline__ void join(const PrefillParams& p, const Row& row, const 
                 float4 z[2][8];
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
-                    const bool there = __any_sync(~0u, add[x1 + x] != 0.0f);  // (a part without a tile has no output)
+                    const float4* const from = reinterpret_cast<const float4*>(part(min(x0 + x1 + x, n - 1))) + c * 1024 + at;
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        z[x][e] = there ? __ldcg(reinterpret_cast<const float4*>(part(x0 + x1 + x)) + (c * 8 + e) * 128 + row.row) : make_float4(0, 0, 0, 0);
+                    for (int e = 0; e < 8; e++) z[x][e] = __ldcg(from + e * 128);
                 }
 #pragma unroll
-                for (int x = 0; x < 2; x++)
+                for (int x = 0; x < 2; x++) {
+                    const float y = add[x1 + x];
+                    if (y == 0.0f) continue;  // (a part without a tile has no output, but what was there before)
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
                         float* const to = o + 4 * e;
-                        const float y = add[x1 + x];
                         to[0] += y * z[x][e].x, to[1] += y * z[x][e].y, to[2] += y * z[x][e].z, to[3] += y * z[x][e].w;
                     }
+                }
             }
         }
-        if (row.real) store_columns<T>(p, row.out, c, o, f, all == 0.0f);
+        if (real) store_columns<T>(out, D, out_row, c, o, f, all == 0.0f);
     }
-    if (row.real) leave_lse(p, row.out, all, least);
+    if (real && c0 == 0) leave_lse(lse, out_row, all, least);
 }
 
 // A wait of a warp that ends: false when the time is up, and then for every other wait of the CTA too.  (One function for each side of the kernel:
@@ -1037,7 +1046,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     fence_before_sync();
                 }
                 if (!has_part) {
-                    if (x.real) leave_lse(p, x.out, sum, add);
+                    if (x.real) leave_lse(p.lse, x.out, sum, add);
                 } else {
                     if (!idle) {
                         part[DP * 128 + x.row] = add;
@@ -1052,15 +1061,18 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         if (last) *counter = 0;
                     }
                     if (!(fine = meet())) break;
-                    if (joins[i] && !idle) {
+                    if (joins[i]) {
                         __threadfence();
                         const int tile = shared ? 0 : i;
-                        Parts parts;
-                        parts.first = p.parts + ((2 * (int64_t)k.first_part + 1) * kTiles + tile) * kPart;
-                        parts.rest = p.parts + ((2 * (int64_t)k.first_part + 2) * kTiles + tile) * kPart;
-                        parts.stride = 2 * kTiles * kPart;
-                        parts.n = k.final_part - k.first_part + 1;
-                        join<T, DP>(p, x, parts, shared, vscale);
+                        const float* const first = p.parts + ((2 * (int64_t)k.first_part + 1) * kTiles + tile) * kPart;
+                        // one, two or four warps for the rows, and so four, two or one for the columns
+                        const int rows = k.tokens * heads_a_tile - 128 * tile, row_warps = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, w = warp & 3;
+                        const int at = w % row_warps * 32 + lane, token = (uint32_t)(at + 128 * tile) / (uint32_t)heads_a_tile;
+                        const int head = k.ht * heads_a_tile + at + 128 * tile - token * heads_a_tile;
+                        const bool real = token < k.tokens && head < group;
+                        if (__any_sync(~0u, real))
+                            join<T, DP>(p.out, p.lse, D, at, (int64_t)(k.row + token) * p.n_heads + k.kv * group + head, real, first, first + kTiles * kPart, 2 * kTiles * kPart,
+                                        k.final_part - k.first_part + 1, shared ? 2 : 1, w / row_warps, 4 / row_warps, vscale);
                     }
                 }
             }
