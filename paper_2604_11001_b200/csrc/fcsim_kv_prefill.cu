@@ -205,7 +205,7 @@ constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are c
 constexpr int kShareCost = 4;
 // A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and
 // their outputs are joined as those of different CTAs are.
-constexpr int kSharedLeast = 6;
+constexpr int kSharedLeast = 2;
 
 // A block of rows: tokens [b * tokens_a_block, + tokens) of the new ones of a request, heads of one head tile.
 struct Block {
@@ -658,14 +658,24 @@ __device__ __noinline__ void add_infinite(const PrefillParams& p, Row x, const S
     wait_stores();
 }
 
-// O of a row, 32 columns of tensor memory at a time, to the output or to a part.
+// O of a row, 32 columns of tensor memory at a time, to the output or to a part.  `with`: columns from there to a second O, or none; the sum
+// of both, times f1 and f2, is what leaves (either may be anything where its factor is zero).
 template <class T>
-__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, float* part, float f, bool none) {
+__device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, float* part, float f, bool none, int with, float f1, float f2) {
 #pragma unroll 1
     for (int c = 0; c * 32 < p.pool.head_dim; c++) {
         float o[32];
         tmem_load(x.at + 32 * c, o);
         wait_loads();
+        if (with)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                float y[16];
+                tmem_load16(x.at + with + 32 * c + 16 * h, y);
+                wait_loads();
+#pragma unroll
+                for (int e = 0; e < 16; e++) o[16 * h + e] = (f1 == 0.0f ? 0.0f : o[16 * h + e] * f1) + (f2 == 0.0f ? 0.0f : y[e] * f2);
+            }
         if (part) {  // fours of columns
 #pragma unroll
             for (int e = 0; e < 32; e += 4) reinterpret_cast<float4*>(part)[(c * 8 + e / 4) * 128 + x.row] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -682,18 +692,12 @@ __device__ __forceinline__ void leave_lse(float* lse, int64_t out, float sum, fl
 
 // Adds up the parts of a block's tile, in their order: references, sums and outputs of each; of row `at` a thread, 32 columns of every `by` times 32, from
 // `c0` times 32 on (few rows are shared by the warps).  The first is at `first`, the others of
-// `n` from `rest` on, `stride` floats apart; with `pairs` = 2 each is one of a tile's group and, kPart behind it, one of the other's.  (All that it is
-// told comes in registers.  What is passed by its address lies in memory, and with the shared memory that this kernel takes there is next to no
+// `n` from `rest` on, `stride` floats apart.  (All that it is told comes in registers.  What is passed by its address lies in memory, and with the shared memory that this kernel takes there is next to no
 // cache before L2: a join of 16 parts took 70 us that way.)
 template <class T, int DP>
-__device__ __noinline__ void join(char* out, float* lse, int D, int at, int64_t out_row, bool real, const float* first, const float* rest, int64_t stride, int n, int pairs,
-                                  int c0, int by, float vscale) {
-    constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
-    n *= pairs;
-    auto part = [&](int x) {
-        const int y = pairs == 2 ? x >> 1 : x;
-        return (y == 0 ? first : rest + (y - 1) * stride) + (pairs == 2 ? (x & 1) * kPart : 0);
-    };
+__device__ __noinline__ void join(char* out, float* lse, int D, int at, int64_t out_row, bool real, const float* first, const float* rest, int64_t stride, int n, int c0,
+                                  int by, float vscale) {
+    auto part = [&](int x) { return x == 0 ? first : rest + (x - 1) * stride; };
     // What can be asked for at once is.
     constexpr int kMost = 8;
     float add[kMost], least = INFINITY, all = 0;  // references as numbers to add; the least is the highest reference
@@ -785,7 +789,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     constexpr bool kNarrow = C::bytes == 1;
     constexpr float kRaise = kRaiseOf<T>, kLag = kLagOf<T>, kLog2e = 1.4426950408889634f;
     extern __shared__ __align__(1024) char raw_smem[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 12 + 2 * S::kLoadWarps];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kSegments + 14 + 2 * S::kLoadWarps];
+    __shared__ float2 others[kTiles == 2 ? 128 : 1];
     __shared__ uint32_t tmem_at, valid[8][4];
     __shared__ int stuck, infinite[kSegments], joins[kTiles];
     __shared__ Walk start;
@@ -805,8 +810,9 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     auto weights_ready = [&](int s) { return rest + 16 + s * 8; };
     auto output_full = [&](int s) { return rest + 32 + s * 8; };
     auto meeting = [&](int i) { return rest + 48 + i * 8; };
-    auto landed = [&](int me, int turn) { return rest + 96 + (me * 2 + turn) * 8; };  // a warp's bulk copies that it looks over
+    auto landed = [&](int me, int turn) { return rest + 112 + (me * 2 + turn) * 8; };  // a warp's bulk copies that it looks over
     const uint32_t query_full = rest + 64, query_empty = rest + 72, added = rest + 80, drained = rest + 88;
+    const uint32_t other_ready = rest + 96, other_taken = rest + 104;  // the second group's output of a tile that both have, for the first
     auto wait_on = [&](auto side, uint32_t bar, uint32_t parity) {
         return __all_sync(~0u, bar_try(bar, parity)) || wait_long<decltype(side)::value>(bar, parity, &stuck, p.status);
     };
@@ -814,13 +820,13 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     constexpr int kProductWarp = S::kWarps - 2, kPlanWarp = S::kWarps - 1;
     {
         // how many arrivals each of the barriers, in the order in which they lie, waits for
-        constexpr int kBars = 2 * kStages + 2 * kSegments + 12 + 2 * S::kLoadWarps;
+        constexpr int kBars = 2 * kStages + 2 * kSegments + 14 + 2 * S::kLoadWarps;
         if (tid < kBars) {
             const int i = tid - 2 * kStages - 2 * kSegments;
             int count = 1;
             if (tid < kStages) count = 64;                                                        // full
             else if (tid >= 2 * kStages + kSegments && i < 0) count = S::kWarps - 1;              // done_with
-            else if ((i >= 2 && i < 4) || (i >= 6 && i < 8)) count = 128;                         // weights_ready, meeting
+            else if ((i >= 2 && i < 4) || (i >= 6 && i < 8) || (i >= 12 && i < 14)) count = 128;  // weights_ready, meeting, other_ready, other_taken
             else if (i == 8) count = p.box ? 1 : 32 * S::kLoadWarps;                              // query_full
             bar_init(bar0 + tid * 8, count);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -903,7 +909,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         const int token_own = (uint32_t)tid / (uint32_t)heads_a_tile, g_own = tid - token_own * heads_a_tile;
         const int token_first = (uint32_t)x.row / (uint32_t)heads_a_tile, g_first = x.row - token_first * heads_a_tile;
         int step0 = 0;
-        uint32_t score_parity[2] = {0, 0}, output_parity = 0, meeting_parity = 0;
+        uint32_t score_parity[2] = {0, 0}, output_parity = 0, meeting_parity = 0, other_parity = 0;
         auto meet = [&]() {
             bar_arrive(meeting(i));
             const bool ok = wait(meeting(i), meeting_parity);
@@ -915,7 +921,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             const int steps = k.steps;
             const bool shared = k.shared, whole = k.whole;
             const int step_first = shared ? i : i >= k.tiles_in_use ? steps : 0, step_by = shared ? 2 : 1;
-            const bool worked = step_first < steps, has_part = !whole || shared;
+            const bool worked = step_first < steps;
             if (worked || shared) {
                 const int token = shared ? token_first : token_own, head = k.ht * heads_a_tile + (shared ? g_first : g_own);
                 x.real = token < k.tokens && head < group;
@@ -1036,43 +1042,60 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     output_parity ^= 1;
                     fence_after_sync();
                 }
-                constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
-                const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
-                // this CTA's part is the first of its two, unless the block begins here
-                float* const part = has_part ? p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart : nullptr;
-                if (worked && !idle) {
-                    if (infinite[segment % kSegments]) add_infinite<C, kKeys>(p, x, k, step_first, step_by);
-                    leave<T>(p, x, part, f, sum == 0.0f);
-                    fence_before_sync();
+                if (worked && !idle && infinite[segment % kSegments]) add_infinite<C, kKeys>(p, x, k, step_first, step_by);
+                float f1 = 1, f2 = 0;
+                if (kTiles == 2 && shared) {
+                    if (i == 1) {  // the first group takes this one's output with its own
+                        others[x.row] = make_float2(add, sum);
+                        fence_before_sync();
+                        bar_arrive(other_ready);
+                        if (!(fine = wait(other_taken, other_parity))) break;
+                    } else {
+                        if (!(fine = wait(other_ready, other_parity))) break;
+                        const float2 other = others[x.row];
+                        const float least = fminf(add, other.x);
+                        f1 = add == INFINITY ? 0.0f : power2(least - add), f2 = other.x == INFINITY ? 0.0f : power2(least - other.x);
+                        sum = f1 * sum + f2 * other.y, add = least;  // (NaN stays NaN)
+                    }
+                    other_parity ^= 1;
+                    fence_after_sync();
                 }
-                if (!has_part) {
-                    if (x.real) leave_lse(p.lse, x.out, sum, add);
-                } else {
-                    if (!idle) {
-                        part[DP * 128 + x.row] = add;
-                        part[(DP + 1) * 128 + x.row] = sum;
-                        __threadfence();
-                    }
-                    if (!(fine = meet())) break;
-                    if (x.row == 0) {
-                        int* const counter = p.counters + k.first_part * 2 + (shared ? 0 : i);
-                        const bool last = atomicAdd(counter, 1) == (k.final_part - k.first_part + 1) * (shared ? 2 : 1) - 1;
-                        joins[i] = last;
-                        if (last) *counter = 0;
-                    }
-                    if (!(fine = meet())) break;
-                    if (joins[i]) {
-                        __threadfence();
-                        const int tile = shared ? 0 : i;
-                        const float* const first = p.parts + ((2 * (int64_t)k.first_part + 1) * kTiles + tile) * kPart;
-                        // one, two or four warps for the rows, and so four, two or one for the columns
-                        const int rows = k.tokens * heads_a_tile - 128 * tile, row_warps = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, w = warp & 3;
-                        const int at = w % row_warps * 32 + lane, token = (uint32_t)(at + 128 * tile) / (uint32_t)heads_a_tile;
-                        const int head = k.ht * heads_a_tile + at + 128 * tile - token * heads_a_tile;
-                        const bool real = token < k.tokens && head < group;
-                        if (__any_sync(~0u, real))
-                            join<T, DP>(p.out, p.lse, D, at, (int64_t)(k.row + token) * p.n_heads + k.kv * group + head, real, first, first + kTiles * kPart, 2 * kTiles * kPart,
-                                        k.final_part - k.first_part + 1, shared ? 2 : 1, w / row_warps, 4 / row_warps, vscale);
+                if (!(kTiles == 2 && shared && i == 1)) {
+                    constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
+                    const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
+                    // this CTA's part is the first of its two, unless the block begins here
+                    float* const part = whole ? nullptr : p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart;
+                    if (!idle) leave<T>(p, x, part, f, sum == 0.0f, kTiles == 2 && shared ? DP : 0, f1, f2);
+                    fence_before_sync();
+                    if (kTiles == 2 && shared) bar_arrive(other_taken);
+                    if (whole) {
+                        if (x.real) leave_lse(p.lse, x.out, sum, add);
+                    } else {
+                        if (!idle) {
+                            part[DP * 128 + x.row] = add;
+                            part[(DP + 1) * 128 + x.row] = sum;
+                            __threadfence();
+                        }
+                        if (!(fine = meet())) break;
+                        if (x.row == 0) {
+                            int* const counter = p.counters + k.first_part * 2 + i;
+                            const bool last = atomicAdd(counter, 1) == k.final_part - k.first_part;
+                            joins[i] = last;
+                            if (last) *counter = 0;
+                        }
+                        if (!(fine = meet())) break;
+                        if (joins[i]) {
+                            __threadfence();
+                            const float* const first = p.parts + ((2 * (int64_t)k.first_part + 1) * kTiles + i) * kPart;
+                            // one, two or four warps for the rows, and so four, two or one for the columns
+                            const int rows = k.tokens * heads_a_tile - 128 * i, row_warps = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, w = warp & 3;
+                            const int at = w % row_warps * 32 + lane, token = (uint32_t)(at + 128 * i) / (uint32_t)heads_a_tile;
+                            const int head = k.ht * heads_a_tile + at + 128 * i - token * heads_a_tile;
+                            const bool real = token < k.tokens && head < group;
+                            if (__any_sync(~0u, real))
+                                join<T, DP>(p.out, p.lse, D, at, (int64_t)(k.row + token) * p.n_heads + k.kv * group + head, real, first, first + kTiles * kPart, 2 * kTiles * kPart,
+                                            k.final_part - k.first_part + 1, w / row_warps, 4 / row_warps, vscale);
+                        }
                     }
                 }
             }

@@ -140,12 +140,16 @@ def test_scales_of_either_sign(dtype, scale, page):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-def test_a_scale_that_is_no_number_shows(dtype):
+@pytest.mark.parametrize("n", [60, 1900])
+@pytest.mark.parametrize("head_dim", [64, 256])
+def test_a_scale_that_is_no_number_shows(dtype, n, head_dim):
+    """In one piece, in several, by one tile of rows and by two."""
     one = torch.ones(2, device="cuda")
-    ones = torch.ones(4, PAGE, 2, 64, device="cuda")
+    pages = -(-n // PAGE)
+    ones = torch.ones(pages, PAGE, 2, head_dim, device="cuda")
     c = kv.PagedKV(stored(ones, "e4m3"), stored(ones, "e4m3"), None, torch.tensor([float("nan"), 1.0], device="cuda"), one)
-    q = torch.ones(20, 4, 64, device="cuda").to(DT[dtype])
-    out, lse = c.prefill(q, to_int([0, 20]), to_int([[0, 1, 2, 3]]), to_int([60]), return_lse=True)
+    q = torch.ones(20, 4, head_dim, device="cuda").to(DT[dtype])
+    out, lse = c.prefill(q, to_int([0, 20]), torch.arange(pages, dtype=torch.int32, device="cuda")[None], to_int([n]), return_lse=True)
     assert bool(torch.isnan(out[:, :2]).all()) and bool(torch.isnan(lse[:, :2]).all())
     assert bool((out[:, 2:] == 1).all()) and bool(torch.isfinite(lse[:, 2:]).all())
 
