@@ -108,6 +108,22 @@ def test_reads_on_streams_and_in_graphs():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_outputs_that_begin_at_any_16_bytes(cache):
+    c = make_cache(gen(5), 10, 16, 3, 80, cache)
+    slots = torch.randint(0, 160, (37,), generator=gen(6), device="cuda")
+    want = c.read(slots, dtype=torch.float16)
+    for at in (8, 16, 24):
+        out = torch.full((2, 37 * 3 * 80 + 64), 7.0, dtype=torch.float16, device="cuda")
+        k, v = (x[at:at + 37 * 3 * 80] for x in out)
+        args = kv.fcsim_kv_read_args(slots=slots.data_ptr(), k_out=k.data_ptr(), v_out=v.data_ptr(), status=c.status.data_ptr(), n_tokens=37, dtype=kv.F16)
+        assert kv.load().fcsim_kv_read(c._c_ref, C.byref(args), torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(k.view_as(want[0]), want[0]) and torch.equal(v.view_as(want[1]), want[1])
+        assert bool((out[:, :at] == 7).all()) and bool((out[:, at + 37 * 3 * 80:] == 7).all())
+    c.check()
+
+
+@pytest.mark.gpu
 def test_the_binding_refuses():
     c = make_cache(gen(1), 4, 16, 1, 64, "f16")
     slots = torch.zeros(4, dtype=torch.int64, device="cuda")
