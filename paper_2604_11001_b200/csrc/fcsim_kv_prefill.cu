@@ -20,8 +20,11 @@
 //   clocks (64 a product of 128 x 128 x 16), the parts 1 024 each; the exponentials, beside them, 2 050.
 //
 // Bounds.  Long prompts: the products, 3 072 clocks of the 4 300 that such a step takes (8 192 tokens, 32 heads of 128: 680 us, 810 TFLOP/s with p
-// counted once, 1 215 of products done); the rest is what one tile's softmax takes longer than the other tile's products.  Few tokens over a long context: the loads, at 4.1 TB/s
-// (16 x 7 tokens over 8 000: 129 us), and with an 8-bit cache the instructions that turn them (231 us).  Small calls: latency, 10 us.
+// counted once, 1 215 of products done); the rest is what one tile's softmax takes longer than the other tile's products.
+// Few tokens over a long context: the loads, at 4.7 TB/s (16 x 7 tokens over 8 000, 64 heads: 113 us), and with an 8-bit cache the instructions that turn
+// them (213 us).  Small calls: latency, 10 us.
+// With the shared memory that this kernel takes there is next to no L1 cache, so what lies in local memory (spilled registers, structs whose address is
+// taken) is at L2's distance: hence the registers' split by role, and values in place of references.
 #include <math.h>
 
 #include <algorithm>
