@@ -189,8 +189,9 @@ struct Shape {
     static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 6;
     static constexpr int kWarps = kSoftmaxWarps + kLoadWarps + 2, kThreads = 32 * kWarps;
     // With two tiles the kernel starts with 128 registers a thread, and the loads' warps leave some of theirs to the softmax's: fewer where they turn
-    // 8-bit rows (8 192 tokens, 32 heads, 8-bit cache: 144 and 112 take 1 065 us, 160 and 96 1 155; a 16-bit one 718 and 682).
-    static constexpr int kSoftmaxRegisters = C::bytes == 1 ? 144 : 160, kOtherRegisters = 256 - kSoftmaxRegisters;
+    // 8-bit rows (8 192 tokens, 32 heads, 8-bit cache: 144 and 112 take 1 065 us, 160 and 96 1 155; a 16-bit one 718 and 682), and at width 64, where
+    // more is spilled otherwise (2 048 tokens: 72 us, 76).
+    static constexpr int kSoftmaxRegisters = C::bytes == 1 || DP == 64 ? 144 : 160, kOtherRegisters = 256 - kSoftmaxRegisters;
     // A warp loads half a tile at a time.  It waits for the place of a tile by the parity of one barrier, so the tile that was there two rounds before
     // has to be gone: it is, as what the warp has loaded last waited for a later one.
     static_assert(kLoadWarps <= 2 * kStages, "parities");
