@@ -43,7 +43,8 @@ enum { /* bits of *status */
     FCSIM_KV_BAD_LENGTH = 2,   /* length < 0 (taken as 0) or > max_length (taken as max_length) */
     FCSIM_KV_BAD_POSITION = 4, /* position outside the rope table: q_out row zero, nothing stored */
     FCSIM_KV_BAD_BUDGET = 8,   /* budget < 0 (taken as 0) or > max_budget (taken as max_budget) */
-    FCSIM_KV_STUCK = 16        /* a wait inside a kernel took seconds and was given up: the call's results are wrong */
+    FCSIM_KV_STUCK = 16        /* a wait inside a kernel took seconds and was given up: the call's results are wrong, and its workspace
+                                  has to be cleared again before it is used */
 };
 
 /* head_dim: a multiple of 8 (16-bit caches) or 16 (E4M3), at most 256.  k and v have the same strides.
@@ -132,7 +133,7 @@ int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* arg
  * out: [n_rows][n_heads][head_dim] contiguous, in q's type.  lse: [n_rows][n_heads] fp32, or NULL.  A row that sees nothing, or belongs to no
  * request, gives zeros and -infinity.  What a row does not see may hold anything, infinities and NaN too.
  * Softmax weights of F16 queries are multiples of 2^-38 of the row's largest; of BF16 queries and a 16-bit cache, values below 2^-94 lose bits.
- * starts beyond 0 .. n_rows are taken as these ends, a request of more rows than tokens has rows that see nothing (FCSIM_KV_BAD_LENGTH
+ * starts beyond 0 .. n_rows are taken as these ends, rows that two requests claim hold either's output, a request of more rows than tokens has rows that see nothing (FCSIM_KV_BAD_LENGTH
  * for either).  n_rows and max_length are at most 2^31 - 2^16, n_requests 65535, n_heads * head_dim below 2^31. */
 typedef struct {
     const void* q;

@@ -427,7 +427,9 @@ class PagedKV:
         if bits:
             self.status.zero_()
             if bits & STUCK:
-                raise RuntimeError("a wait inside a kernel was given up: results are wrong")
+                with _LOCK:
+                    self._workspaces.clear()   # what has to be zero in them may not be
+                raise RuntimeError("a wait inside a kernel was given up: results are wrong (graphs captured before have to be captured again)")
             names = [s for b, s in ((BAD_PAGE, "page or slot outside the pool"),
                                     (BAD_LENGTH, "length outside 0 .. max_length"),
                                     (BAD_POSITION, "position outside the rope table"),

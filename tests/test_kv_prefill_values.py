@@ -512,6 +512,49 @@ def test_threads_with_caches_of_their_own_share_a_stream():
         c.check()
 
 
+def test_a_wait_that_was_given_up_shows_and_leaves_no_workspace():
+    """(The bit is set from here: no wait runs out.)"""
+    c, *args = setting(3, [700, 40], [30, 40])
+    want = c.prefill(*args)
+    assert c._workspaces
+    c.status.fill_(kv.STUCK | kv.BAD_PAGE)
+    with pytest.raises(RuntimeError, match="given up"):
+        c.check()
+    assert not c._workspaces
+    assert torch.equal(c.prefill(*args), want)
+    c.check()
+
+
+def test_requests_that_claim_the_same_rows_are_flagged():
+    """Rows of two requests hold the output of one of them, the other rows their own."""
+    c, q, starts, table, ln = setting(4, [100, 200, 300], [20, 20, 20])
+    out = c.prefill(q, to_int([0, 40, 20, 60]), table, ln)     # requests of 40, none and 40 rows
+    with pytest.raises(ValueError, match="length"):
+        c.check()
+    first = c.prefill(q[:40], to_int([0, 40]), table[:1], ln[:1])
+    last = c.prefill(q[20:], to_int([0, 40]), table[2:], ln[2:])
+    unit, tiny = 2.0 ** -6, 2.0 ** -6    # (other tiles, other order of sums: a step of the type or two of values below 4)
+    near = lambda a, b: bool(((a.double() - b.double()).abs() <= unit * b.double().abs() + tiny).all())  # noqa: E731
+    assert near(out[:20], first[:20]) and near(out[40:], last[20:])
+    for i in range(20):
+        for h in range(q.shape[1]):
+            assert near(out[20 + i, h], first[20 + i, h]) or near(out[20 + i, h], last[i, h])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_a_first_call_under_capture(cache):
+    """Nothing is set up by a call before: what a kernel needs once is set under capture too."""
+    c, q, starts, table, ln = setting(6, [900, 33], [300, 33], cache)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out = c.prefill(q, starts, table, ln)
+        k, v = c.read(torch.arange(40, device="cuda"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, c.prefill(q, starts, table, ln)) and torch.equal(k, c.read(torch.arange(40, device="cuda"))[0])
+    c.check()
+
+
 # ------------------------------------------------------------------------------------------ together
 @pytest.mark.parametrize("cache,page", [("bf16", 16), ("f16", 24), ("e4m3", 64)])
 @pytest.mark.parametrize("window,first", [(0, 0), (100, 4)])
