@@ -10,7 +10,7 @@
 //   time is that of the other tile's products; with one tile of rows the groups take its tiles of keys in turn.
 // * Six warps load, half a tile each in turn, into a ring: by bulk copies of the pages' tokens where a page is whole boxes of 8 tokens or
 //   more, else 16 bytes a lane (cp.async), both in the 128-byte swizzled layout that the products read.  (8 192 tokens, 32 heads:
-//   688 us in boxes, 745 by lanes.)  8-bit rows are turned into 16 bits, exactly, in shared memory.  What some row of a tile does not see is
+//   688 us in boxes when 745 by lanes.)  8-bit rows are turned into 16 bits, exactly, in shared memory.  What some row of a tile does not see is
 //   looked over in v: infinities and NaN would reach rows whose weight for them is zero.  One warp walks over the work ahead of the others.
 // * The work is counted in tiles of keys, laid end to end over all requests, heads and blocks, and every CTA takes an equal stretch (or, where
 //   there are few blocks, one piece of one block).  Parts of a block that lies across stretches are joined by the last to come, in
@@ -19,9 +19,9 @@
 //   would be as large as the output's own.  The second part is a third of the products: of two tiles of rows and 128 keys the scores take 1 024
 //   clocks (64 a product of 128 x 128 x 16), the parts 1 024 each; the exponentials, beside them, 2 050.
 //
-// Bounds.  Long prompts: the products, 3 072 clocks of the 4 300 that such a step takes (8 192 tokens, 32 heads of 128: 680 us, 810 TFLOP/s with p
-// counted once, 1 215 of products done); the rest is what one tile's softmax takes longer than the other tile's products.
-// Few tokens over a long context: the loads, at 4.7 TB/s (16 x 7 tokens over 8 000, 64 heads: 113 us), and with an 8-bit cache the instructions that turn
+// Bounds.  Long prompts: the products, three quarters of the 4 200 clocks that such a step takes (8 192 tokens, 32 heads of 128: 660 us, 830 TFLOP/s with p
+// counted once, 1 245 of products done); the rest is what one tile's softmax takes longer than the other tile's products.
+// Few tokens over a long context: the loads, at 4.7 TB/s (16 x 7 tokens over 8 000, 64 heads: 114 us), and with an 8-bit cache the instructions that turn
 // them (213 us).  Small calls: latency, 10 us.
 // With the shared memory that this kernel takes there is next to no L1 cache, so what lies in local memory (spilled registers, structs whose address is
 // taken) is at L2's distance: hence the registers' split by role, and values in place of references.
@@ -183,7 +183,7 @@ struct Shape {
     static constexpr int kKeys = DP <= 128 ? 128 : 64;  // of a tile
     static constexpr int kQuery = kRows * DP * 2;       // bytes
     static constexpr int kStage = kKeys * DP * 2;       // of K or V
-    static constexpr int kRoom = (227 * 1024 - 3072 - kQuery) / kStage;  // (beside what the kernel keeps itself)
+    static constexpr int kRoom = (224 * 1024 - kQuery) / kStage;  // (of 227 KB, 3 for what the kernel keeps itself)
     static constexpr int kStages = kRoom < 8 ? kRoom : 8;
     static constexpr int kBytes = kQuery + kStages * kStage;
     static constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarps = 6;
@@ -202,13 +202,14 @@ struct Shape {
 };
 
 // ---------------------------------------------------------------------------------------------- the walk over the work
-// Cost of a block's start and end beside one tile of keys.
+// Cost of a block's start and end beside one tile of keys (4 096 tokens, 32 heads: 221 us, without it 256; 12 x 200 tokens, 64 heads: 72, 94).
 constexpr int kOverhead = 2;
 constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are cut
-// Tiles by which the longest piece may exceed an equal share: what the joins of shares cost.
+// Tiles by which the longest piece may exceed an equal share: what the joins of shares cost.  (Always pieces: a request of 60 000 tokens beside 16
+// of 50, 8 new ones each, takes 340 us instead of 84.  Always shares: 16 tokens over 60 000 take 90 us instead of 88, 50 x 20 over 2 000 122 and 121.)
 constexpr int kShareCost = 4;
-// A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and
-// their outputs are joined as those of different CTAs are.
+// A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and the first
+// adds up what both have (16 x 7 tokens over 8 000: 113 us, by one group alone 174).
 constexpr int kSharedLeast = 2;
 
 // A block of rows: tokens [b * tokens_a_block, + tokens) of the new ones of a request, heads of one head tile.
