@@ -206,7 +206,7 @@ struct Shape {
 constexpr int kOverhead = 2;
 constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are cut
 // Tiles by which the longest piece may exceed an equal share: what the joins of shares cost.  (Always pieces: a request of 60 000 tokens beside 16
-// of 50, 8 new ones each, takes 340 us instead of 84.  Always shares: 16 tokens over 60 000 take 90 us instead of 88, 50 x 20 over 2 000 122 and 121.)
+// of 50, 8 new ones each, takes 340 us instead of 84.  Pieces where whole blocks are as few tiles longer: 400 tokens 27.3 us instead of 19.7.  Always shares: 16 tokens over 60 000 take 90 us instead of 88, 50 x 20 over 2 000 122 and 121.)
 constexpr int kShareCost = 4;
 // A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and the first
 // adds up what both have (16 x 7 tokens over 8 000: 113 us, by one group alone 174).
@@ -287,17 +287,18 @@ __device__ __forceinline__ int64_t warp_sum(int64_t x) {
 // Tiles of one of the heads of a lane's request (`rows` of them from position0 on), or, with `d`, its units.  Long requests are added up by the warp.
 template <int KEYS>
 __device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, int position0, int cut, int over) {
-    constexpr int kAlone = 2;
-    const int lane = threadIdx.x & 31, blocks = blocks_of(p, rows);
+    // A lane adds up to two blocks itself, or where several requests have more, up to 24: the warp takes as long for a request as a lane for six
+    // (12 requests of 200 tokens, 64 heads: 56.5 us a call, with two always 61.4; one of 400: 27.4, with 24 always 28.3).
+    const int lane = threadIdx.x & 31, blocks = blocks_of(p, rows), alone = __popc(__ballot_sync(~0u, blocks > 2)) > 2 ? 24 : 2;
     int64_t own = 0;
     auto cost = [&](int position, int n, int b) {
         const int t = tiles_of<KEYS>(p, position, n, b);
         return cut ? (unsigned)(t + cut - 1) / (unsigned)cut : t + over;
     };
-    if (blocks <= kAlone)
+    if (blocks <= alone)
 #pragma unroll 1
         for (int b = 0; b < blocks; b++) own += cost(position0, rows, b);
-    uint32_t together = __ballot_sync(~0u, blocks > kAlone);
+    uint32_t together = __ballot_sync(~0u, blocks > alone);
 #pragma unroll 1
     while (together) {
         const int src = __ffs(together) - 1;
@@ -361,6 +362,7 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, in
         if (all[1] * heads <= gridDim.x) {
             const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);
             d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
+            if (longest <= d.cut + kShareCost) d.cut = max(d.cut, longest);  // whole, if a join costs more
             if (warps == 1 && d.cut >= longest) {
                 // Every block whole, one a CTA: few numbers, all small.  (The general way takes 4 us, as long as the rest of a small call.)
                 const int own = blocks_of(p, rows) * heads;
