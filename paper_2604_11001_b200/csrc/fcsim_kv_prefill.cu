@@ -67,6 +67,10 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrie
 __device__ __forceinline__ void bar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// as many bytes of bulk copies to come, and the arrival itself later
+__device__ __forceinline__ void bar_bytes(uint32_t bar, int bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 // the same, the thread asleep for up to so many nanoseconds
 __device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity, uint32_t ns) {
     uint32_t done;
@@ -1318,13 +1322,15 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                     rows_there[c] = any_bad ? ~__reduce_or_sync(~0u, bad ? lowest(my_box + p.box - c * 32) & ~lowest(my_box - c * 32) : 0u) : ~0u;
                                 const bool looks = kNarrow || (!key && (any_bad || partly_seen(p, k, u0 - h % 2 * kHalf, kKeys)));
                                 const uint32_t bar = looks ? landed(me, turn) : full(s);
-                                if (lane == 0) bar_expect(bar, __popc(issues) * p.box * 128);
+                                if (lane == 0) {
+                                    if (looks) bar_expect(bar, __popc(issues) * p.box * 128);
+                                    else bar_bytes(bar, __popc(issues) * p.box * 128);
+                                }
                                 __syncwarp();
                                 if (issue)
                                     copy_box(to + (my_part + (kNarrow ? kAcross : 0)) * (kKeys * 128) + my_box * 128, key ? &p.k_map : &p.v_map, my_part * (kNarrow ? 128 : 64),
                                              p.key_dim ? slot : k.kv, p.key_dim ? k.kv : slot, page, bar);
                                 if (looks) issued = h, issued_turn = turn, turn ^= 1;
-                                else if (lane != 0) bar_arrive(full(s));
                             } else {
                                 int64_t off[kOffs];  // of the rows of this lane's tokens, or -1
 #pragma unroll
@@ -1361,6 +1367,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                 if (any_bad) flag(p.status, FCSIM_KV_BAD_PAGE);
                             }
                             __syncwarp();
+                            // (Behind `valid`: who waits for the tile reads that too, and where no page of it is in the pool no copy is waited for.)
+                            if (in_boxes && issued < 0) bar_arrive(full(s));
                             h += S::kLoadWarps;
                             if (h < halves) fetch_pages(h);
                         }
