@@ -1022,7 +1022,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     }
                     const float plus = limit == -INFINITY ? 0.0f : add;
                     const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
-                    uint64_t sums2[2] = {pair(sum, 0.0f), pair(0.0f, 0.0f)};
+                    uint64_t sums2[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};  // of this tile: the row's total takes one rounding of each
 #pragma unroll 1
                     for (int c = 0; c < kKeys / 64; c++) {
                         float s[4][16];
@@ -1041,7 +1041,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                         }
                     }
                     const float2 z = unpair(add2(sums2[0], sums2[1]));
-                    sum = z.x + z.y;
+                    sum += z.x + z.y;
                     wait_stores();
                     fence_before_sync();
                     bar_arrive(weights_ready(slot));
