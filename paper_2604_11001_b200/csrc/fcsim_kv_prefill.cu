@@ -209,9 +209,17 @@ struct Shape {
 // Cost of a block's start and end beside one tile of keys (4 096 tokens, 32 heads: 221 us, without it 256; 12 x 200 tokens, 64 heads: 72, 94).
 constexpr int kOverhead = 2;
 constexpr int kPieceLeast = 2;  // tiles of a piece at least, where blocks are cut
-// Tiles by which the longest piece may exceed an equal share: what the joins of shares cost.  (Always pieces: a request of 60 000 tokens beside 16
+// Tiles by which the longest piece may exceed an equal share: what the joins of shares cost more than those of pieces.  (Always pieces: a request of 60 000 tokens beside 16
 // of 50, 8 new ones each, takes 340 us instead of 84.  Pieces where whole blocks are as few tiles longer: 400 tokens 27.3 us instead of 19.7.  Always shares: 16 tokens over 60 000 take 90 us instead of 88, 50 x 20 over 2 000 122 and 121.)
 constexpr int kShareCost = 4;
+// And by which whole blocks, one a CTA, may exceed it, since they need no join: fewer where 8-bit rows are turned, which doubles a tile's time.  (16 x 7
+// tokens, whole and in shares: over 6 000 of 16 bits 89 and 95 us, over 24 000 302 and 290; over 3 000 of 8 bits 93 and 97, over 16 000 392 and 350.
+// Lengths from 1 000 to 16 000: 194 and 124 us of 16 bits, 397 and 180 of 8.)
+template <class C, int DP>
+constexpr int kWholeGain = C::bytes == 1 && DP > 64 ? 5 : 11;
+// So many requests are planned for by one warp, a lane each, without barriers, while the others set up; with more every warp takes part.  (18 x 30 tokens,
+// whole blocks: 23.5 us, by all warps 25.6.  32 x 8 tokens, more blocks than CTAs: 30, of 33 by all warps 28.)
+constexpr int kOneWarpPlans = 32;
 // A block with one tile of rows is shared by the two groups of warps from so many tiles of keys on: each takes every other one, and the first
 // adds up what both have (16 x 7 tokens over 8 000: 113 us, by one group alone 174).
 constexpr int kSharedLeast = 2;
@@ -320,7 +328,7 @@ __device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, 
 // The division of the work, and where this CTA's part begins.  Warps 0 .. warps - 1 take part, each with a stretch of the requests; one of them
 // finds the start and leaves it in `start`.
 template <int KEYS>
-__device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, int64_t (*sums)[16], int me, int warps) {
+__device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, int64_t (*sums)[16], int me, int warps, int whole_gain) {
     const int lane = threadIdx.x & 31;
     const int heads = p.pool.n_kv * p.head_tiles, each = (unsigned)(p.n_requests + warps - 1) / (unsigned)warps;
     const int r0 = min(me * each, p.n_requests), r1 = min(r0 + each, p.n_requests);
@@ -362,12 +370,13 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, in
             total = all[0] * heads;
             break;
         }
-        // Pieces that fit the grid, if there are as few blocks and that leaves none much longer than an equal share.
+        // Whole blocks, or pieces that fit the grid, if there are as few blocks and that leaves none much longer than an equal share.
         if (all[1] * heads <= gridDim.x) {
-            const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads);
-            d.cut = (int)max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare));
+            const int64_t spare = max((int64_t)1, gridDim.x - all[1] * heads), equal = divide(all[0] * heads, gridDim.x);
+            d.cut = (int)min((int64_t)1 << 30, max((int64_t)kPieceLeast, divide(all[0] * heads + spare - 1, spare)));
             if (longest <= d.cut + kShareCost) d.cut = max(d.cut, longest);  // whole, if a join costs more
-            if (warps == 1 && d.cut >= longest) {
+            const bool whole = d.cut >= longest, pieces = whole ? longest <= equal + whole_gain : d.cut <= equal + kShareCost;
+            if (whole && pieces && warps == 1) {
                 // Every block whole, one a CTA: few numbers, all small.  (The general way takes 4 us, as long as the rest of a small call.)
                 const int own = blocks_of(p, rows) * heads;
                 int upto = own;
@@ -391,7 +400,7 @@ __device__ __forceinline__ Division plan(const PrefillParams& p, Walk& start, in
                 }
                 return d;
             }
-            if (min(d.cut, longest) <= divide(all[0] * heads, gridDim.x) + kShareCost) continue;
+            if (pieces) continue;
             d.cut = 0;
         }
         total = (all[0] + kOverhead * all[1]) * heads;
@@ -863,9 +872,9 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         fence_for_products();
     }
     Division work;
-    if (p.n_requests > 32) {
+    if (p.n_requests > kOneWarpPlans) {
         __syncthreads();  // (start.left)
-        work = plan<kKeys>(p, start, sums, warp, S::kWarps);
+        work = plan<kKeys>(p, start, sums, warp, S::kWarps, kWholeGain<C, DP>);
     }
     fence_before_sync();
     __syncthreads();
@@ -1118,7 +1127,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
         auto wait = [&](uint32_t bar, uint32_t parity) { return wait_on(std::integral_constant<int, 1>(), bar, parity); };
         if (warp == kPlanWarp) {
             // ------------------------------------------------------------------------------------------ the walk
-            if (p.n_requests <= 32) work = plan<kKeys>(p, start, sums, 0, 1);
+            if (p.n_requests <= kOneWarpPlans) work = plan<kKeys>(p, start, sums, 0, 1, kWholeGain<C, DP>);
             __syncwarp();
             Walk w = start;
             bool more = w.left > 0;
