@@ -17,6 +17,7 @@ import ctypes as C
 import math
 import struct
 import threading
+import weakref
 
 import torch
 
@@ -32,6 +33,9 @@ _ESIZE = -3
 # keeps the launches of one call together where threads share a stream)
 _WORKSPACES = {}
 _LOCK = threading.Lock()
+# device -> (cache, its status word) of every cache whose word may hold something, also of those that are gone; and how often a wait was given up
+# there: what that has left wrong is in the workspaces, which are all caches'
+_STATUS, _GIVEN_UP = {}, {}
 _NO_FIT = struct.error   # of a number that an argument struct has no room for
 _MOST = 2 ** 31 - 2 ** 16   # tokens of a request or a budget, at most
 _grad_enabled = torch.is_grad_enabled
@@ -172,6 +176,9 @@ class PagedKV:
         self._status = self.status.data_ptr()
         torch.cuda.current_stream(k.device).synchronize()   # cleared, whatever stream the calls come on
         self._workspaces = _WORKSPACES.setdefault(self._index, {})   # of the device
+        with _LOCK:
+            _STATUS.setdefault(self._index, []).append((weakref.ref(self), self.status))
+            self._given_up = _GIVEN_UP.setdefault(self._index, 0)   # what this cache's check() has told of
         self._c = fcsim_kv_cache(k.data_ptr(), v.data_ptr(), _pointer(weight), _pointer(k_scale), _pointer(v_scale),
                                  k.stride(0), k.stride(1), k.stride(2), _TYPES[k.dtype], n_pages, page_size, n_kv,
                                  head_dim, 0)
@@ -421,15 +428,25 @@ class PagedKV:
 
     def check(self):
         """Wait for all calls, on every stream, read and clear the device status; raise when a call met a bad page, length, position
-        or budget."""
+        or budget, or when a wait inside a kernel was given up, in a call of this cache or of another one on its device (all share the
+        workspaces that it leaves wrong: each of them tells of it once)."""
         torch.cuda.synchronize(self.device)
+        with _LOCK:
+            words = torch.cat([word for _, word in _STATUS[self._index]]).tolist()
+            if any(bits & STUCK for bits in words):
+                _GIVEN_UP[self._index] += 1
+                self._workspaces.clear()   # what has to be zero in them may not be
+                for _, word in _STATUS[self._index]:
+                    word.bitwise_and_(~STUCK)
+            _STATUS[self._index] = [entry for entry in _STATUS[self._index] if entry[0]() is not None]
+            told, self._given_up = self._given_up, _GIVEN_UP[self._index]
         bits = int(self.status.item())
         if bits:
             self.status.zero_()
-            if bits & STUCK:
-                with _LOCK:
-                    self._workspaces.clear()   # what has to be zero in them may not be
-                raise RuntimeError("a wait inside a kernel was given up: results are wrong (graphs captured before have to be captured again)")
+        if told != self._given_up:
+            raise RuntimeError("a wait inside a kernel was given up: results since the last check() are wrong (graphs captured before have to be "
+                               "captured again)")
+        if bits:
             names = [s for b, s in ((BAD_PAGE, "page or slot outside the pool"),
                                     (BAD_LENGTH, "length outside 0 .. max_length"),
                                     (BAD_POSITION, "position outside the rope table"),
