@@ -124,6 +124,9 @@ class Layer:
     def prompt_inputs(self, lengths, chunk=0):
         """Random inputs of `prompts` for prompts of these lengths, at most those that the layer was made with; `chunk` tokens of each at a time."""
         torch, made = self.torch, []
+        room = min(self.columns * PAGE, self.rope.shape[0])
+        if len(lengths) != self.lengths.numel() or min(lengths) < 0 or not 0 < max(lengths) <= room or chunk < 0:
+            raise ValueError(f"prompts: {self.lengths.numel()} lengths up to {room}, not all 0, and no chunk below 0")
         chunk = chunk or max(lengths)
         for at in range(0, max(lengths), chunk):
             upto = [min(n, at + chunk) for n in lengths]
