@@ -688,16 +688,17 @@ int check_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a, AttendP
     p->status = a->status, p->q_row = a->q_row, p->q_head = a->q_head, p->table_row = a->table_row;
     p->n_requests = a->n_requests, p->n_heads = a->n_heads, p->max_length = a->max_length;
     const bool all = (int64_t)a->window + a->first >= a->max_length || a->window == 0;  // (of the longest request, and so of all)
-    p->window = all ? 0 : a->window, p->first = all ? 0 : a->first;
+    p->most_seen = all ? a->max_length : a->window + a->first, p->first = all ? 0 : a->first;
     p->add_weight = a->add_weight != 0, p->scale = a->scale;
     return FCSIM_OK;
 }
 
-AttendVariant attend_variant(const fcsim_kv_cache* c, const fcsim_kv_attend_args* a) {
-    const int group = a->n_heads / c->n_kv_heads;
+AttendVariant attend_variant(const fcsim_kv_cache* c, const AttendParams& p, int dtype) {
+    const int group = p.n_heads / c->n_kv_heads;
+    const bool first = p.first > 0;
     if (c->dtype == FCSIM_KV_E4M3)
-        return a->dtype == FCSIM_KV_F16 ? attend_variant_f16_e4m3(c->head_dim, group) : attend_variant_bf16_e4m3(c->head_dim, group);
-    return a->dtype == FCSIM_KV_F16 ? attend_variant_f16(c->head_dim, group) : attend_variant_bf16(c->head_dim, group);
+        return dtype == FCSIM_KV_F16 ? attend_variant_f16_e4m3(c->head_dim, group, first) : attend_variant_bf16_e4m3(c->head_dim, group, first);
+    return dtype == FCSIM_KV_F16 ? attend_variant_f16(c->head_dim, group, first) : attend_variant_bf16(c->head_dim, group, first);
 }
 
 // The current device and its SMs (asked once per device).
@@ -724,9 +725,8 @@ struct AttendLayout {
 // requests that share no page hold at most the pool's tokens, and each at most one tile that is not full
 int64_t logit_tiles(const AttendParams& p) {
     if (!p.add_weight) return 0;
-    const int64_t seen = p.window > 0 ? p.window + p.first : p.max_length;
     const int64_t tile = 1 << p.tile_bits;
-    return std::min((seen + tile - 1) / tile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / tile + p.n_requests);
+    return std::min((p.most_seen + tile - 1) / tile * p.n_requests, (int64_t)p.pool.n_pages * p.pool.page_size / tile + p.n_requests);
 }
 // The part of the workspace that does not depend on the device.
 size_t attend_kept(const AttendParams& p) {
@@ -737,8 +737,7 @@ int attend_layout(const AttendParams& p, const AttendVariant& v, AttendLayout* l
     int device = 0, sms = 0, per_sm = 0, rc = device_and_sms(&device, &sms);
     if (rc != FCSIM_OK) return rc;
     if ((rc = v.ctas_per_sm(device, &per_sm)) != 0) return cuda_status((cudaError_t)rc);
-    const int64_t seen = p.window > 0 ? p.window + p.first : p.max_length;
-    const int64_t tiles = (seen + (1 << p.tile_bits) - 1) >> p.tile_bits, group = p.n_heads / p.pool.n_kv;
+    const int64_t tiles = ((int64_t)p.most_seen + (1 << p.tile_bits) - 1) >> p.tile_bits, group = p.n_heads / p.pool.n_kv;
     const int64_t most = tiles * p.n_requests * p.pool.n_kv * ((group + v.head_cols - 1) / v.head_cols);
     l->grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms * per_sm, (int64_t)kMaxCtas, std::max<int64_t>(most + most / 3 + 1, p.n_requests)}));
     // the kernel counts the tiles of all requests, and the work of a CTA, in 32 bits
@@ -914,7 +913,7 @@ extern "C" int fcsim_kv_attend_workspace(const fcsim_kv_cache* c, const fcsim_kv
     if (!out) return FCSIM_EINVAL;
     *out = {0, 0};
     if (p.n_requests == 0) return FCSIM_OK;
-    const AttendVariant v = attend_variant(c, a);
+    const AttendVariant v = attend_variant(c, p, a->dtype);
     p.tile_bits = v.tile_bits;
     AttendLayout l;
     if ((rc = attend_layout(p, v, &l)) != FCSIM_OK) return rc;
@@ -928,7 +927,7 @@ extern "C" int fcsim_kv_attend(const fcsim_kv_cache* c, const fcsim_kv_attend_ar
     int rc = check_attend(c, a, &p);
     if (rc != FCSIM_OK) return rc;
     if (p.n_requests == 0) return FCSIM_OK;
-    const AttendVariant v = attend_variant(c, a);
+    const AttendVariant v = attend_variant(c, p, a->dtype);
     p.tile_bits = v.tile_bits;
     if (!workspace || !aligned16(workspace) || workspace_bytes < attend_kept(p)) return FCSIM_ESIZE;
     AttendLayout l;

@@ -145,11 +145,14 @@ __device__ __forceinline__ int length_of(const AttendParams& p, int b) {
     return n < 0 ? 0 : n > p.max_length ? p.max_length : n;
 }
 // Tokens between the first ones and the window, which are not seen.  What is seen is counted without them: seen token u is token
-// u, or behind the first ones u + gap.
-__device__ __forceinline__ int gap_of(const AttendParams& p, int len) {
-    return p.window > 0 && len > p.window + p.first ? len - p.window - p.first : 0;
+// u, or behind the first ones u + gap.  (Kernels for calls without first tokens are compiled for themselves: with the comparison, and
+// that of the runs of 16 tokens below, in their tile loop too, 64 requests over e4m3 took 83.8 us instead of 82.6, and one of 131 072
+// tokens 96.9 instead of 96.0.)
+__device__ __forceinline__ int gap_of(const AttendParams& p, int len) { return max(len - p.most_seen, 0); }
+template <bool FIRST>
+__device__ __forceinline__ int token_of(const AttendParams& p, int gap, int u) {
+    return FIRST && u < p.first ? u : u + gap;
 }
-__device__ __forceinline__ int token_of(const AttendParams& p, int gap, int u) { return u + (u >= p.first ? gap : 0); }
 __device__ __forceinline__ int tiles_of(const AttendParams& p, int len, int bits) {
     return (len - gap_of(p, len) + (1 << bits) - 1) >> bits;
 }
@@ -489,7 +492,7 @@ __device__ __noinline__ void join_alone(const AttendParams& p, int first_worker,
     }
 }
 
-template <class T, class C, int DP, int NT>
+template <class T, class C, int DP, int NT, bool FIRST>
 __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv_attend_kernel(const __grid_constant__ AttendParams p) {
     using S = Shape<T, C, DP, NT>;
     using M = typename OperandOf<T, C>::type;
@@ -552,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     const uint32_t lane_dst = ring + lane_row * S::kPitch + chunk * 16;
     int page = -1, place = 0;
     auto fetch_page = [&]() {  // for tile `in`
-        const int u = in.j * step + offset + lane % kTokens, t = token_of(p, in.gap, u), i = page_of(p.pool, t);
+        const int u = in.j * step + offset + lane % kTokens, t = token_of<FIRST>(p, in.gap, u), i = page_of(p.pool, t);
         place = t - i * p.pool.page_size;
         page = u < in.seen ? p.table[in.b * p.table_row + i] : -1;
     };
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
                 const uint32_t dst = lane_dst + stage * S::kStage + b * 16 * S::kPitch, half = mask >> (16 * b) & 0xffff;
                 const int page0 = __shfl_sync(~0u, page, 16 * b), place0 = __shfl_sync(~0u, place, 16 * b);
                 const int before = p.first - (in.j * step + offset + 16 * b);  // first tokens among the 16
-                const bool split = before > 0 && before < 16 && in.gap > 0;
+                const bool split = FIRST && before > 0 && before < 16 && in.gap > 0;
                 if (half == 0xffff && place0 + 16 <= p.pool.page_size && !split) {  // 16 tokens of one page: rows at equal distances
                     const char* src = p.pool.k + (page0 * p.pool.stride_page + (place0 + lane_row) * p.pool.stride_slot + head) * C::bytes + chunk * 16;
                     if (copies) {
@@ -1237,19 +1240,19 @@ __global__ void __launch_bounds__(kThreads, Shape<T, C, DP, NT>::kCtas) fcsim_kv
     }
 }
 
-template <class T, class C, int DP, int NT>
+template <class T, class C, int DP, int NT, bool FIRST>
 int launch(const AttendParams& p, int grid, cudaStream_t stream) {
     using S = Shape<T, C, DP, NT>;
-    fcsim_kv_attend_kernel<T, C, DP, NT><<<grid, kThreads, S::kBytes, stream>>>(p);
+    fcsim_kv_attend_kernel<T, C, DP, NT, FIRST><<<grid, kThreads, S::kBytes, stream>>>(p);
     return (int)cudaGetLastError();
 }
-template <class T, class C, int DP, int NT>
+template <class T, class C, int DP, int NT, bool FIRST>
 int ctas_per_sm(int device, int* out) {
     using S = Shape<T, C, DP, NT>;
     static std::atomic<int> known[kMaxDevices];
     int n = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
     if (n == 0) {
-        auto* kernel = fcsim_kv_attend_kernel<T, C, DP, NT>;
+        auto* kernel = fcsim_kv_attend_kernel<T, C, DP, NT, FIRST>;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kThreads, S::kBytes);
         if (e != cudaSuccess) return (int)e;
@@ -1258,29 +1261,33 @@ int ctas_per_sm(int device, int* out) {
     *out = n;
     return 0;
 }
-template <class T, class C, int DP>
+template <class T, class C, int DP, bool FIRST>
 AttendVariant of_group(int group) {
     // more than 8 heads: two column tiles share every load; beyond 16, and for the widest rows (whose registers do not
     // suffice: 32 requests, 16 heads on each kv head of 256, 172 us, rows read twice 136), the rows are read again
     if constexpr (DP <= 128)
-        if (group > 8) return {launch<T, C, DP, 2>, ctas_per_sm<T, C, DP, 2>, 16, DP, Shape<T, C, DP, 2>::kTileBits};
-    return {launch<T, C, DP, 1>, ctas_per_sm<T, C, DP, 1>, 8, DP, Shape<T, C, DP, 1>::kTileBits};
+        if (group > 8) return {launch<T, C, DP, 2, FIRST>, ctas_per_sm<T, C, DP, 2, FIRST>, 16, DP, Shape<T, C, DP, 2>::kTileBits};
+    return {launch<T, C, DP, 1, FIRST>, ctas_per_sm<T, C, DP, 1, FIRST>, 8, DP, Shape<T, C, DP, 1>::kTileBits};
+}
+template <class T, class C, bool FIRST>
+AttendVariant of_width(int head_dim, int group) {
+    return head_dim <= 64 ? of_group<T, C, 64, FIRST>(group) : head_dim <= 128 ? of_group<T, C, 128, FIRST>(group) : of_group<T, C, 256, FIRST>(group);
 }
 template <class T, class C>
-AttendVariant of(int head_dim, int group) {
-    return head_dim <= 64 ? of_group<T, C, 64>(group) : head_dim <= 128 ? of_group<T, C, 128>(group) : of_group<T, C, 256>(group);
+AttendVariant of(int head_dim, int group, bool first) {
+    return first ? of_width<T, C, true>(head_dim, group) : of_width<T, C, false>(head_dim, group);
 }
 
 }  // namespace
 
 #if FCSIM_KV_TYPES == 0
-AttendVariant attend_variant_f16(int head_dim, int group) { return of<F16, F16>(head_dim, group); }
+AttendVariant attend_variant_f16(int head_dim, int group, bool first) { return of<F16, F16>(head_dim, group, first); }
 #elif FCSIM_KV_TYPES == 1
-AttendVariant attend_variant_bf16(int head_dim, int group) { return of<BF16, BF16>(head_dim, group); }
+AttendVariant attend_variant_bf16(int head_dim, int group, bool first) { return of<BF16, BF16>(head_dim, group, first); }
 #elif FCSIM_KV_TYPES == 2
-AttendVariant attend_variant_f16_e4m3(int head_dim, int group) { return of<F16, E4M3>(head_dim, group); }
+AttendVariant attend_variant_f16_e4m3(int head_dim, int group, bool first) { return of<F16, E4M3>(head_dim, group, first); }
 #else
-AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16, E4M3>(head_dim, group); }
+AttendVariant attend_variant_bf16_e4m3(int head_dim, int group, bool first) { return of<BF16, E4M3>(head_dim, group, first); }
 #endif
 
 #if FCSIM_KV_TYPES == 0
@@ -1289,6 +1296,7 @@ AttendVariant attend_variant_bf16_e4m3(int head_dim, int group) { return of<BF16
 // overhead: a CTA takes eight tiles (of 64 tokens) of (request, kv head) at a time, four tokens a thread, two
 // heads' logits at once and their sum in order.  Bound by the latency of a few dependent loads, so what matters is that
 // one round of the grid is all of it, and what does not need the logits is loaded before the first kernel has ended.
+template <bool FIRST>
 __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(const AttendParams p) {
     constexpr int kAtOnce = 2;
     const int threads = 1 << (p.tile_bits - 2), tiles = kThreads / threads;  // of a tile; at a time
@@ -1306,8 +1314,8 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
     float old[4];
     auto load_weights = [&]() {
         in = (at.j << p.tile_bits) + threadIdx.x % threads * 4;
-        const int t0 = token_of(p, at.gap, in);
-        aligned = size % 4 == 0 && t0 % 4 == 0 && token_of(p, at.gap, in + 3) == t0 + 3;
+        const int t0 = token_of<FIRST>(p, at.gap, in);
+        aligned = size % 4 == 0 && t0 % 4 == 0 && token_of<FIRST>(p, at.gap, in + 3) == t0 + 3;
         room = at.tiles_before + at.tiles <= p.logit_tiles;
         if (!room) flag(p.status, FCSIM_KV_BAD_PAGE);  // more tokens than the pool has: pages are shared
         const int32_t* const table = p.table + at.b * p.table_row;
@@ -1315,7 +1323,7 @@ __global__ void __launch_bounds__(kThreads, kWeightCtas) fcsim_kv_weight_kernel(
         for (int i = 0; i < 4; i++) {
             weight[i] = nullptr;
             if (room && in + i < at.seen && (i == 0 || !aligned)) {
-                const int t = token_of(p, at.gap, in + i), index = page_of(p.pool, t), page = table[index];
+                const int t = token_of<FIRST>(p, at.gap, in + i), index = page_of(p.pool, t), page = table[index];
                 if ((unsigned)page < (unsigned)p.pool.n_pages) weight[i] = p.pool.weight + ((int64_t)page * n_kv + at.kv) * size + t - index * size;
             }
         }
@@ -1373,7 +1381,7 @@ int launch_weights(const AttendParams& p, int grid, cudaStream_t stream) {
     early.val.programmaticStreamSerializationAllowed = 1;
     config.attrs = &early;
     config.numAttrs = 1;
-    return (int)cudaLaunchKernelEx(&config, fcsim_kv_weight_kernel, p);
+    return (int)cudaLaunchKernelEx(&config, p.first ? fcsim_kv_weight_kernel<true> : fcsim_kv_weight_kernel<false>, p);
 }
 #endif
 

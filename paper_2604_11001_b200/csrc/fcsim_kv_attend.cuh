@@ -18,7 +18,7 @@ struct AttendParams {
     int32_t* status;
     int64_t q_row, q_head, table_row;
     int n_requests, n_heads, max_length, add_weight;
-    int window, first;   // both 0 where everything is seen; their sum is below max_length
+    int most_seen, first;  // tokens that a request sees at most: all, or a window and before it the `first` oldest (0 where all are seen)
     float scale;
     int tile_bits;       // tokens a CTA takes at once, of the variant
     // workspace
@@ -37,11 +37,11 @@ struct AttendVariant {
     int tile_bits;                 // its tokens: 64 or 128
 };
 
-// The variant for a type of q, a type of cache, a head width and a group of query heads per kv head.
-AttendVariant attend_variant_f16(int head_dim, int group);
-AttendVariant attend_variant_bf16(int head_dim, int group);
-AttendVariant attend_variant_f16_e4m3(int head_dim, int group);
-AttendVariant attend_variant_bf16_e4m3(int head_dim, int group);
+// The variant for a type of q, a type of cache, a head width and a group of query heads per kv head, with first tokens before a window or without.
+AttendVariant attend_variant_f16(int head_dim, int group, bool first);
+AttendVariant attend_variant_bf16(int head_dim, int group, bool first);
+AttendVariant attend_variant_f16_e4m3(int head_dim, int group, bool first);
+AttendVariant attend_variant_bf16_e4m3(int head_dim, int group, bool first);
 int launch_weights(const AttendParams&, int grid, cudaStream_t);
 
 }  // namespace fcsim_kv_dev
