@@ -180,7 +180,7 @@ int fcsim_kv_evict(const fcsim_kv_cache* cache, const fcsim_kv_evict_args* args,
                    size_t workspace_bytes, void* cuda_stream);
 
 /* k_out, v_out: [n_tokens][n_kv_heads][head_dim] contiguous in `dtype` (F16 or BF16, whatever the cache's type), 16-byte aligned.  Row i
- * is what stands at slots[i] (int64, page * page_size + place), an E4M3 value times its scale, rounded once; negative: zeros.
+ * is what stands at slots[i] (int64, page * page_size + place), an E4M3 value as its fp32 product with its scale, rounded to `dtype`; negative: zeros.
  * A slot outside the pool gives zeros (FCSIM_KV_BAD_PAGE).  A slot may come more than once.  n_tokens is at most 2^31 - 2^16. */
 typedef struct {
     const int64_t* slots;

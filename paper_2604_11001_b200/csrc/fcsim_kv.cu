@@ -254,7 +254,8 @@ __device__ __forceinline__ int divide_by(uint64_t magic, int x) {
     return (int)__umul64hi(magic, (uint64_t)x << 1);
 }
 
-// 16 cached bytes as 8 or 16 elements of type T, times `scale` where the cache has scales
+// 16 cached bytes as 8 or 16 elements of type T, times `scale` where the cache has scales (in 32 bits: a product of 4 and 24 bits is rounded there, and
+// then to T, which near the middle of two values of T may be the other one of them)
 template <class T, class C>
 __device__ __forceinline__ void convert_piece(const uint4& raw, float scale, char* out) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};

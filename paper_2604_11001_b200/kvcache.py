@@ -409,7 +409,7 @@ class PagedKV:
 
     def read(self, slots, *, dtype=None):
         """What stands at ``slots`` (int64 [n], page * page_size + place, negative = zeros): k and v as [n, n_kv_heads, head_dim]
-        of ``dtype`` (float16 or bfloat16; default: the cache's own, of an 8-bit cache bfloat16), 8-bit values times their scales."""
+        of ``dtype`` (float16 or bfloat16; default: the cache's own, of an 8-bit cache bfloat16), 8-bit values times their scales (the float32 product, rounded)."""
         if dtype is None:
             dtype = torch.bfloat16 if self.k_scale is not None else self.k.dtype
         if dtype not in _WIDE:
