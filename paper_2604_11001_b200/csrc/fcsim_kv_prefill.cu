@@ -97,7 +97,18 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 __device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// What was loaded from tensor memory is there.  (`x`: where it was loaded to.  Nothing else says that it changes here, and the compiler is free to
+// move what reads a register to before a wait that does not name it.)
+template <int N>
+__device__ __forceinline__ void loaded(float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i++) asm volatile("" : "+f"(x[i])::"memory");
+}
+template <int... N>
+__device__ __forceinline__ void wait_loads(float (&... x)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    (loaded(x), ...);
+}
 __device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // all products issued so far by this thread, then one arrival
 __device__ __forceinline__ void commit_products(uint32_t bar) {
@@ -625,9 +636,9 @@ __device__ __forceinline__ void store32(char* to, const uint32_t (&y)[8], bool a
     }
 }
 template <class T>
-__device__ __forceinline__ void store_columns(char* out, int D, int64_t out_row, int c, const float (&o)[32], float f, bool none) {
+__device__ __forceinline__ void store_columns(char* out, int D, int64_t out_row, int c, const float (&o)[32], float f, bool none, bool wide = true) {
     char* const to = out + (out_row * D + c * 32) * 2;
-    const bool aligned = D % 16 == 0 && ((uintptr_t)out & 31) == 0;
+    const bool aligned = wide && D % 16 == 0 && ((uintptr_t)out & 31) == 0;
 #pragma unroll
     for (int e = 0; e < 2; e++) {
         uint32_t y[8];
@@ -647,7 +658,7 @@ __device__ __noinline__ void add_infinite(const PrefillParams& p, Row x, const S
     for (int c = 0; c * 16 < D; c++) {
         float o[16];
         tmem_load16(x.at + 16 * c, o);
-        wait_loads();
+        wait_loads(o);
         if (x.real)
 #pragma unroll 1
             for (int j = k.j + t0; j < k.j + k.steps; j += by) {
@@ -686,13 +697,13 @@ __device__ __forceinline__ void leave(const PrefillParams& p, const Row& x, floa
     for (int c = 0; c * 32 < p.pool.head_dim; c++) {
         float o[32];
         tmem_load(x.at + 32 * c, o);
-        wait_loads();
+        wait_loads(o);
         if (with)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 float y[16];
                 tmem_load16(x.at + with + 32 * c + 16 * h, y);
-                wait_loads();
+                wait_loads(y);
 #pragma unroll
                 for (int e = 0; e < 16; e++) o[16 * h + e] = (f1 == 0.0f ? 0.0f : o[16 * h + e] * f1) + (f2 == 0.0f ? 0.0f : y[e] * f2);
             }
@@ -778,7 +789,8 @@ __device__ __noinline__ void join(char* out, float* lse, int D, int at, int64_t 
                 }
             }
         }
-        if (real) store_columns<T>(out, D, out_row, c, o, f, all == 0.0f);
+        // (16 bytes at once: of 32, in a function that two kernels call, this compiler (12.9.86) stores the first 4)
+        if (real) store_columns<T>(out, D, out_row, c, o, f, all == 0.0f, false);
     }
     if (real && c0 == 0) leave_lse(lse, out_row, all, least);
 }
@@ -976,7 +988,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     auto load = [&](int c, float (&s)[4][16]) {  // 64 logits; those that are not seen are -infinity
 #pragma unroll
                         for (int e = 0; e < 4; e++) tmem_load16(at + c * 64 + 16 * e, s[e]);
-                        wait_loads();
+                        wait_loads(s[0], s[1], s[2], s[3]);
                         if (masked) {
 #pragma unroll
                             for (int y = 0; y < 2; y++) {
@@ -1018,7 +1030,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                                 float o[2][16];
                                 tmem_load16(x.at + 32 * c, o[0]);
                                 tmem_load16(x.at + 32 * c + 16, o[1]);
-                                wait_loads();
+                                wait_loads(o[0], o[1]);
 #pragma unroll
                                 for (int h = 0; h < 2; h++) {
                                     uint32_t y[16];
