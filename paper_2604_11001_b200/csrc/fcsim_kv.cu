@@ -787,6 +787,7 @@ int check_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, Prefi
     p->head_tiles = (group + v->rows - 1) / v->rows;
     p->heads_a_tile = (group + p->head_tiles - 1) / p->head_tiles;
     p->tokens_a_block = v->rows / p->heads_a_tile;
+    p->aside = p->max_length > (int64_t)kAsideTiles * v->keys;
     return FCSIM_OK;
 }
 
@@ -848,7 +849,7 @@ int prefill_layout(const PrefillParams& p, const PrefillVariant& v, int* device,
     const int64_t blocks = (int64_t)p.n_rows / p.tokens_a_block + std::min(p.n_requests, p.n_rows), tiles = (p.max_length + (int64_t)v.keys - 1) / v.keys;
     const int64_t most = std::min<int64_t>(blocks * p.pool.n_kv, 1 << 20) * p.head_tiles * std::max<int64_t>(tiles, 1);
     *grid = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)sms, (int64_t)kMaxCtas, most}));
-    *bytes = kPrefillCounters + (size_t)*grid * 2 * (v.rows / 128) * (v.width + 2) * 128 * 4;
+    *bytes = kPrefillCounters + (size_t)*grid * (p.aside ? 3 : 2) * (v.rows / 128) * (v.width + 2) * 128 * 4;
     return FCSIM_OK;
 }
 

@@ -689,6 +689,58 @@ __device__ __noinline__ void add_infinite(const PrefillParams& p, Row x, const S
     wait_stores();
 }
 
+// What a row's O has summed up goes to `aside`, laid out like a part, and O begins again at zero; `again`: onto what is there already, which stands for
+// the reference that it had.  (A row without a finite logit so far keeps its O.)
+template <int DP>
+__device__ __forceinline__ void put_aside_here(uint32_t at, float* aside, int row, int D, float add, bool again) {
+    float* const reference = aside + DP * 128 + row;
+    const float before = again ? *reference : INFINITY, f = before == INFINITY ? 0.0f : power2(add - before);
+#pragma unroll 1
+    for (int c = 0; c * 16 < D; c++) {
+        float o[16];
+        tmem_load16(at + 16 * c, o);
+        wait_loads(o);
+        uint32_t y[16];
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            float4* const to = reinterpret_cast<float4*>(aside) + (c * 4 + e / 4) * 128 + row;
+            float4 z = make_float4(0, 0, 0, 0);
+            if (before != INFINITY) z = *to;
+            *to = make_float4(z.x * f + o[e], z.y * f + o[e + 1], z.z * f + o[e + 2], z.w * f + o[e + 3]);
+        }
+        __syncwarp();  // (as above)
+#pragma unroll
+        for (int e = 0; e < 16; e++) y[e] = add == INFINITY ? __float_as_uint(o[e]) : 0u;
+        tmem_store16(at + 16 * c, y);
+    }
+    *reference = add;
+    wait_stores();
+}
+template <int DP>
+__device__ __noinline__ void put_aside(uint32_t at, float* aside, int row, int D, float add, bool again) { put_aside_here<DP>(at, aside, row, D, add, again); }
+// And back again, at the end of the walk.
+template <int DP>
+__device__ __noinline__ void take_back(uint32_t at, const float* aside, int row, int D, float add) {
+    const float before = aside[DP * 128 + row], f = before == INFINITY ? 0.0f : power2(add - before);
+#pragma unroll 1
+    for (int c = 0; c * 16 < D; c++) {
+        float o[16];
+        tmem_load16(at + 16 * c, o);
+        wait_loads(o);
+        uint32_t y[16];
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            float4 z = make_float4(0, 0, 0, 0);
+            if (before != INFINITY) z = reinterpret_cast<const float4*>(aside)[(c * 4 + e / 4) * 128 + row];
+            y[e] = __float_as_uint(z.x * f + o[e]), y[e + 1] = __float_as_uint(z.y * f + o[e + 1]);
+            y[e + 2] = __float_as_uint(z.z * f + o[e + 2]), y[e + 3] = __float_as_uint(z.w * f + o[e + 3]);
+        }
+        __syncwarp();  // (as above)
+        tmem_store16(at + 16 * c, y);
+    }
+    wait_stores();
+}
+
 // O of a row, 32 columns of tensor memory at a time, to the output or to a part.  `with`: columns from there to a second O, or none; the sum
 // of both, times f1 and f2, is what leaves (either may be anything where its factor is zero).
 template <class T>
@@ -814,7 +866,10 @@ __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, volatile i
 }
 
 // ---------------------------------------------------------------------------------------------- the kernel
-template <class T, class C, int DP>
+// LONG: walks of more than kAsideTiles tiles.  (Kernels of their own, so that other calls take what they took: 8 192 tokens of width 64 574 us with it and 561
+// without.  Width 128: 661 and 691 of 16 bits, 985 and 924 of 8, within what repeats differ by; there a call of the function costs 2 % more than the
+// function in place, with 16 bits it is the other way around.)
+template <class T, class C, int DP, bool LONG>
 __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill_kernel(const __grid_constant__ PrefillParams p) {
     using S = Shape<T, C, DP>;
     constexpr int kTiles = S::kTiles, kKeys = S::kKeys, kStages = S::kStages, kSegments = 4;
@@ -948,6 +1003,8 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
             meeting_parity ^= 1;
             return ok;
         };
+        constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
+        auto aside = [&]() { return p.parts + ((2 * (int64_t)gridDim.x + blockIdx.x) * kTiles + i) * kPart; };  // (there is room where a walk may be so long)
         while (next_segment(wait)) {
             const Segment& k = segments[segment % kSegments];
             const int steps = k.steps;
@@ -967,106 +1024,120 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                 x.position = x.real ? k.position + token : -1;
                 x.from = p.window > 0 && x.position >= p.window ? x.position - p.window + 1 : 0;
                 float add = INFINITY, limit = -INFINITY, sum = 0;  // weights are 2^(unit s + add); add is infinite until there is a finite logit
-#pragma unroll 1
-                for (int t = step_first; t < steps; t += step_by) {
-                    const int slot = kTiles == 2 ? i : t & 1, tile_base = (k.j + t) * kKeys;
-                    const uint32_t at = tmem + S::kScore + slot * kKeys + lanes;
-                    const bool edge = partly_seen(p, k, tile_base, kKeys);
-                    if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
-                    score_parity[slot] ^= 1;
-                    fence_after_sync();
-                    if (idle) {
-                        fence_before_sync();
-                        bar_arrive(weights_ready(slot));
-                        continue;
+                int t0 = step_first;
+                do {
+                    if (LONG && t0 >= kAsideTiles) {
+                        const int slot = kTiles == 2 ? i : t0 & 1;
+                        if (!(fine = wait(score_full(slot), score_parity[slot]) && (kTiles == 2 || wait(added, (step0 + t0 - 1) & 1)))) break;
+                        fence_after_sync();
+                        if (!idle) {
+                            if constexpr (kNarrow) put_aside_here<DP>(x.at, aside(), x.row, D, add, t0 >= 2 * kAsideTiles);
+                            else put_aside<DP>(x.at, aside(), x.row, D, add, t0 >= 2 * kAsideTiles);
+                        }
                     }
-                    const uint32_t* const there = valid[(step0 + t) & 7];
-                    uint32_t some = ~0u;
+                    const int t_end = LONG ? min(steps, t0 + kAsideTiles) : steps;
+#pragma unroll 1
+                    for (int t = t0; t < t_end; t += step_by) {
+                        const int slot = kTiles == 2 ? i : t & 1, tile_base = (k.j + t) * kKeys;
+                        const uint32_t at = tmem + S::kScore + slot * kKeys + lanes;
+                        const bool edge = partly_seen(p, k, tile_base, kKeys);
+                        if (!(fine = wait(score_full(slot), score_parity[slot]))) break;
+                        score_parity[slot] ^= 1;
+                        fence_after_sync();
+                        if (idle) {
+                            fence_before_sync();
+                            bar_arrive(weights_ready(slot));
+                            continue;
+                        }
+                        const uint32_t* const there = valid[(step0 + t) & 7];
+                        uint32_t some = ~0u;
 #pragma unroll
-                    for (int c = 0; c < kKeys / 32; c++) some &= there[c];
-                    const bool masked = edge || some != ~0u;
-                    auto load = [&](int c, float (&s)[4][16]) {  // 64 logits; those that are not seen are -infinity
+                        for (int c = 0; c < kKeys / 32; c++) some &= there[c];
+                        const bool masked = edge || some != ~0u;
+                        auto load = [&](int c, float (&s)[4][16]) {  // 64 logits; those that are not seen are -infinity
 #pragma unroll
-                        for (int e = 0; e < 4; e++) tmem_load16(at + c * 64 + 16 * e, s[e]);
-                        wait_loads(s[0], s[1], s[2], s[3]);
-                        if (masked) {
+                            for (int e = 0; e < 4; e++) tmem_load16(at + c * 64 + 16 * e, s[e]);
+                            wait_loads(s[0], s[1], s[2], s[3]);
+                            if (masked) {
 #pragma unroll
-                            for (int y = 0; y < 2; y++) {
-                                const int b = tile_base + 64 * c + 32 * y;
-                                const uint32_t mask = lowest(x.position + 1 - b) & (~lowest(x.from - b) | lowest(p.first - b)) & there[2 * c + y];
+                                for (int y = 0; y < 2; y++) {
+                                    const int b = tile_base + 64 * c + 32 * y;
+                                    const uint32_t mask = lowest(x.position + 1 - b) & (~lowest(x.from - b) | lowest(p.first - b)) & there[2 * c + y];
 #pragma unroll
-                                for (int e = 0; e < 32; e++) s[2 * y + e / 16][e % 16] = mask >> e & 1 ? s[2 * y + e / 16][e % 16] : -INFINITY;
+                                    for (int e = 0; e < 32; e++) s[2 * y + e / 16][e % 16] = mask >> e & 1 ? s[2 * y + e / 16][e % 16] : -INFINITY;
+                                }
                             }
-                        }
-                    };
-                    float top = -INFINITY;
+                        };
+                        float top = -INFINITY;
 #pragma unroll 1
-                    for (int c = 0; c < kKeys / 64; c++) {
-                        float s[4][16];
-                        load(c, s);
-                        float tops[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+                        for (int c = 0; c < kKeys / 64; c++) {
+                            float s[4][16];
+                            load(c, s);
+                            float tops[4] = {top, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fmaxf(fmaxf(tops[e / 2 % 4], s[e / 16][e % 16]), s[e / 16][e % 16 + 1]);
-                        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                    }
-                    const float most = top * unit;
-                    // The reference moves only when a logit is 2^kLag above it, so that the output is seldom taken through registers.
-                    const bool moves = most > limit;
-                    if (__any_sync(~0u, moves)) {
-                        float shrink = 1;
-                        if (moves) {
-                            const float now = kRaise - most;
-                            shrink = limit == -INFINITY ? 0.0f : power2(now - add);
-                            add = now;
-                            limit = most + kLag;
-                            sum *= shrink;
+                            for (int e = 0; e < 64; e += 2) tops[e / 2 % 4] = fmaxf(fmaxf(tops[e / 2 % 4], s[e / 16][e % 16]), s[e / 16][e % 16 + 1]);
+                            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                         }
-                        __syncwarp();  // (a warp that has come apart must not load from tensor memory: what comes is written to all lanes' registers)
-                        if (t > step_first) {
-                            if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
-                            fence_after_sync();
+                        const float most = top * unit;
+                        // The reference moves only when a logit is 2^kLag above it, so that the output is seldom taken through registers.
+                        const bool moves = most > limit;
+                        if (__any_sync(~0u, moves)) {
+                            float shrink = 1;
+                            if (moves) {
+                                const float now = kRaise - most;
+                                shrink = limit == -INFINITY ? 0.0f : power2(now - add);
+                                add = now;
+                                limit = most + kLag;
+                                sum *= shrink;
+                            }
+                            __syncwarp();  // (a warp that has come apart must not load from tensor memory: what comes is written to all lanes' registers)
+                            if (t > step_first) {
+                                if (kTiles == 1 && !(fine = wait(added, (step0 + t - 1) & 1))) break;
+                                fence_after_sync();
 #pragma unroll 1
-                            for (int c = 0; c * 32 < D; c++) {
-                                float o[2][16];
-                                tmem_load16(x.at + 32 * c, o[0]);
-                                tmem_load16(x.at + 32 * c + 16, o[1]);
-                                wait_loads(o[0], o[1]);
+                                for (int c = 0; c * 32 < D; c++) {
+                                    float o[2][16];
+                                    tmem_load16(x.at + 32 * c, o[0]);
+                                    tmem_load16(x.at + 32 * c + 16, o[1]);
+                                    wait_loads(o[0], o[1]);
 #pragma unroll
-                                for (int h = 0; h < 2; h++) {
-                                    uint32_t y[16];
+                                    for (int h = 0; h < 2; h++) {
+                                        uint32_t y[16];
 #pragma unroll
-                                    for (int e = 0; e < 16; e++) y[e] = __float_as_uint(o[h][e] * shrink);
-                                    tmem_store16(x.at + 32 * c + 16 * h, y);
+                                        for (int e = 0; e < 16; e++) y[e] = __float_as_uint(o[h][e] * shrink);
+                                        tmem_store16(x.at + 32 * c + 16 * h, y);
+                                    }
                                 }
                             }
                         }
-                    }
-                    const float plus = limit == -INFINITY ? 0.0f : add;
-                    const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
-                    uint64_t sums2[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};  // of this tile: the row's total takes one rounding of each
+                        const float plus = limit == -INFINITY ? 0.0f : add;
+                        const uint64_t unit2 = pair(unit, unit), plus2 = pair(plus, plus);
+                        uint64_t sums2[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};  // of this tile: the row's total takes one rounding of each
 #pragma unroll 1
-                    for (int c = 0; c < kKeys / 64; c++) {
-                        float s[4][16];
-                        load(c, s);
+                        for (int c = 0; c < kKeys / 64; c++) {
+                            float s[4][16];
+                            load(c, s);
 #pragma unroll
-                        for (int h = 0; h < 4; h++) {
-                            uint32_t y[16];
+                            for (int h = 0; h < 4; h++) {
+                                uint32_t y[16];
 #pragma unroll
-                            for (int e = 0; e < 8; e++) {
-                                const float2 z = unpair(fma2(pair(s[h][2 * e], s[h][2 * e + 1]), unit2, plus2));
-                                const float a = power2(z.x), b = power2(z.y);
-                                sums2[e & 1] = add2(sums2[e & 1], pair(a, b));
-                                split<T>(a, b, y[e], y[8 + e]);
+                                for (int e = 0; e < 8; e++) {
+                                    const float2 z = unpair(fma2(pair(s[h][2 * e], s[h][2 * e + 1]), unit2, plus2));
+                                    const float a = power2(z.x), b = power2(z.y);
+                                    sums2[e & 1] = add2(sums2[e & 1], pair(a, b));
+                                    split<T>(a, b, y[e], y[8 + e]);
+                                }
+                                tmem_store16(at + c * 64 + 16 * h, y);
                             }
-                            tmem_store16(at + c * 64 + 16 * h, y);
                         }
+                        const float2 z = unpair(add2(sums2[0], sums2[1]));
+                        sum += z.x + z.y;
+                        wait_stores();
+                        fence_before_sync();
+                        bar_arrive(weights_ready(slot));
                     }
-                    const float2 z = unpair(add2(sums2[0], sums2[1]));
-                    sum += z.x + z.y;
-                    wait_stores();
-                    fence_before_sync();
-                    bar_arrive(weights_ready(slot));
-                }
+                    t0 += kAsideTiles;
+                } while (LONG && fine && t0 < steps);
                 if (!fine) break;
                 // -------------------------------------------------------------- end of this CTA's part of a block
                 if (worked) {
@@ -1074,6 +1145,7 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     output_parity ^= 1;
                     fence_after_sync();
                 }
+                if (LONG && step_first + kAsideTiles < steps && !idle) take_back<DP>(x.at, aside(), x.row, D, add);
                 if (worked && !idle && infinite[segment % kSegments]) add_infinite<C, kKeys>(p, x, k, step_first, step_by);
                 float f1 = 1, f2 = 0;
                 if (kTiles == 2 && shared) {
@@ -1093,7 +1165,6 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
                     fence_after_sync();
                 }
                 if (!(kTiles == 2 && shared && i == 1)) {
-                    constexpr int64_t kPart = (int64_t)(DP + 2) * 128;
                     const float vscale = kNarrow ? p.pool.v_scale[k.kv] : 1.0f, f = sum == 0.0f ? 0.0f : vscale / sum;
                     // this CTA's part is the first of its two, unless the block begins here
                     float* const part = whole ? nullptr : p.parts + ((2 * (int64_t)blockIdx.x + (k.first_part == (int)blockIdx.x ? 1 : 0)) * kTiles + i) * kPart;
@@ -1541,12 +1612,12 @@ __global__ void __launch_bounds__(Shape<T, C, DP>::kThreads, 1) fcsim_kv_prefill
     }
 }
 
-template <class T, class C, int DP>
-int launch(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
+template <class T, class C, int DP, bool LONG>
+int launch_walks(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
     using S = Shape<T, C, DP>;
     static std::atomic<bool> raised[kMaxDevices];
     if (device >= kMaxDevices || !raised[device].load(std::memory_order_relaxed)) {
-        auto* kernel = fcsim_kv_prefill_kernel<T, C, DP>;
+        auto* kernel = fcsim_kv_prefill_kernel<T, C, DP, LONG>;
         cudaFuncAttributes a;
         cudaError_t e = cudaFuncGetAttributes(&a, kernel);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
@@ -1554,8 +1625,12 @@ int launch(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
         if (S::kTiles == 2 && a.numRegs * S::kThreads < 256 * (S::kSoftmaxRegisters + S::kOtherRegisters)) return (int)cudaErrorLaunchOutOfResources;
         if (device < kMaxDevices) raised[device].store(true, std::memory_order_relaxed);
     }
-    fcsim_kv_prefill_kernel<T, C, DP><<<grid, S::kThreads, S::kBytes, stream>>>(p);
+    fcsim_kv_prefill_kernel<T, C, DP, LONG><<<grid, S::kThreads, S::kBytes, stream>>>(p);
     return (int)cudaGetLastError();
+}
+template <class T, class C, int DP>
+int launch(const PrefillParams& p, int grid, int device, cudaStream_t stream) {
+    return p.aside ? launch_walks<T, C, DP, true>(p, grid, device, stream) : launch_walks<T, C, DP, false>(p, grid, device, stream);
 }
 template <class T, class C, int DP>
 PrefillVariant variant() {

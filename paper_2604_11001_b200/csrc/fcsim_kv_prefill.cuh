@@ -6,6 +6,10 @@
 
 namespace fcsim_kv_dev {
 
+// Tiles of keys after which a walk's output is put aside and begun again (a multiple of 2).  The tensor core cuts its sums off: up to 2^-23 of the sum is
+// lost at each of 16 additions a tile (8 over width 128), always towards zero, 2^-12 in so many tiles.  (With 2 048 of them outputs were 1.7e-3 too small.)
+constexpr int kAsideTiles = 128;
+
 struct PrefillParams {
     Pool pool;
     const char* q;
@@ -20,10 +24,11 @@ struct PrefillParams {
     int key_dim, query_tokens;       // tensor maps: whether slots come before heads; tokens of a box of q
     int heads_a_tile, head_tiles;    // query heads that share a block's rows; such tiles of a kv head
     int tokens_a_block;
+    int aside;                       // whether a walk may be longer than kAsideTiles
     float scale;
     // workspace
     int* counters;  // [CTAs][2], zero between calls: the parts that are done of the block that begins in a CTA's stretch
-    float* parts;   // [CTAs][2][tiles of rows][head_dim of the variant + 2][128]
+    float* parts;   // [CTAs][2][tiles of rows][head_dim of the variant + 2][128]; with `aside`, behind these as much as for one of the 2
     // with `box`: [pages][heads, slots in the order of their strides][head_dim], and q
     CUtensorMap k_map, v_map, q_map;
 };
