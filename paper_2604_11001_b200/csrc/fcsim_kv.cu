@@ -787,7 +787,9 @@ int check_prefill(const fcsim_kv_cache* c, const fcsim_kv_prefill_args* a, Prefi
     p->head_tiles = (group + v->rows - 1) / v->rows;
     p->heads_a_tile = (group + p->head_tiles - 1) / p->head_tiles;
     p->tokens_a_block = v->rows / p->heads_a_tile;
-    p->aside = p->max_length > (int64_t)kAsideTiles * v->keys;
+    // what a block sees at most: with a window, that of all its tokens, the first ones, and what their rounding to whole boxes adds
+    const int64_t seen = p->window > 0 ? (int64_t)p->window + p->first + p->tokens_a_block + 2 * v->keys : p->max_length;
+    p->aside = std::min<int64_t>(seen, p->max_length) > (int64_t)kAsideTiles * v->keys;
     return FCSIM_OK;
 }
 
