@@ -92,9 +92,12 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
 
 /* table: [n_requests] rows of table_cols int32, row r at table + r * table_row; only the entries that a request's
  *   length reaches are read.  lengths: [n_requests] int32 tokens held, 0 .. max_length <= table_cols * page_size.
- * window > 0: only the newest `window` tokens are seen, and the oldest `first` (without a window `first` has no effect).  n_heads: a multiple of n_kv_heads; head h reads kv head
- *   h / (n_heads / n_kv_heads).  q: request r at q + r * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.  (Of a BF16
- *   query over E4M3, elements below 2^-31 of the head's largest finite one are rounded to 2^-38 of it.)
+ * window > 0: only the newest `window` tokens are seen, and the oldest `first` (without a window `first` has no effect).
+ *   n_heads: a multiple of n_kv_heads; head h reads kv head h / (n_heads / n_kv_heads).  q: request r at q + r * q_row +
+ *   head * q_head, F16 or BF16, that of a 16-bit cache.  (Of a BF16 query over E4M3, elements below 2^-31 of the head's
+ *   largest finite one are rounded to 2^-38 of it.)
+ * Sums over tokens are the tensor core's: in 32 bits, cut off, up to 2^-23 of the sum lost at each of 16 to 24 additions per
+ *   128 tokens of one warp's share.
  * out: [n_requests][n_heads][head_dim] contiguous, in q's type.  lse: [n_requests][n_heads] fp32, the natural
  *   logarithm of the softmax sums, or NULL.  A request without tokens gives zeros and -infinity.
  * add_weight: cache->weight[token] += the softmax weights, summed over the heads of its group.  The requests of such
@@ -103,7 +106,9 @@ int fcsim_kv_append(const fcsim_kv_cache* cache, const fcsim_kv_append_args* arg
  *   calls) must be zero before the first call and are zero again after every call.  Calls that share it must be ordered;
  *   they may differ in everything else.
  * At most 65535 requests, n_requests * max_length below 2^36, max_length at most 2^31 - 2^16 and n_heads * head_dim below 2^31
- * (FCSIM_EINVAL). */
+ * (FCSIM_EINVAL).
+ * The struct has no size or version in it: `first` and `reserved` stand behind what it held before there were first tokens, so what
+ * was compiled against a header without them has to be compiled again. */
 typedef struct {
     const void* q;
     void* out;
@@ -127,14 +132,18 @@ int fcsim_kv_attend(const fcsim_kv_cache* cache, const fcsim_kv_attend_args* arg
 
 /* q: n_rows rows, row i at q + i * q_row + head * q_head, F16 or BF16, that of a 16-bit cache.  Request r has the rows starts[r] ..
  * starts[r + 1] - 1 (starts: [n_requests + 1] int32, not falling, 0 .. n_rows): the newest of its lengths[r] tokens, which are all in
- * the cache already.  A row whose token is number p sees the tokens t <= p, with window > 0 only those of t > p - window or t < first (without
- * a window `first` has no effect).  n_heads: a multiple of n_kv_heads; head h reads kv head h / (n_heads / n_kv_heads).
- * table, lengths, max_length, workspace: as for attend (one workspace serves both).
- * out: [n_rows][n_heads][head_dim] contiguous, in q's type.  lse: [n_rows][n_heads] fp32, or NULL.  A row that sees nothing, or belongs to no
- * request, gives zeros and -infinity.  What a row does not see may hold anything, infinities and NaN too.
- * Softmax weights of F16 queries are multiples of 2^-38 of the row's largest; of BF16 queries and a 16-bit cache, values below 2^-94 lose bits.
- * starts beyond 0 .. n_rows are taken as these ends, rows that two requests claim hold either's output, a request of more rows than tokens has rows that see nothing (FCSIM_KV_BAD_LENGTH
- * for either).  n_rows and max_length are at most 2^31 - 2^16, n_requests 65535, n_heads * head_dim below 2^31. */
+ * the cache already.  A row whose token is number p sees the tokens t <= p, with window > 0 only those of t > p - window or
+ * t < first (without a window `first` has no effect).  n_heads: a multiple of n_kv_heads; head h reads kv head
+ * h / (n_heads / n_kv_heads).  table, lengths, max_length, workspace: as for attend (one workspace serves both).  The cache's
+ * weights do not grow by it.
+ * out: [n_rows][n_heads][head_dim] contiguous, in q's type.  lse: [n_rows][n_heads] fp32, or NULL.  A row that sees nothing, or
+ * belongs to no request, gives zeros and -infinity.  What a row does not see may hold anything, infinities and NaN too.
+ * Rounding: a softmax weight meets v in two 16-bit parts, off by up to 2^-14 (BF16) or 2^-20 (F16) of it.  Those of F16 queries are
+ * multiples of 2^-38 of the row's largest; of BF16 queries and a 16-bit cache, values below 2^-94 lose bits.  Sums over tokens
+ * are the tensor core's, in 32 bits, cut off: up to 2^-12 of an output, whatever its length.
+ * starts beyond 0 .. n_rows are taken as these ends, rows that two requests claim hold either's output, a request of more rows than
+ * tokens has rows that see nothing (FCSIM_KV_BAD_LENGTH for either).  n_rows and max_length are at most 2^31 - 2^16, n_requests
+ * 65535, n_heads * head_dim below 2^31. */
 typedef struct {
     const void* q;
     void* out;

@@ -15,14 +15,16 @@
 // * The work is counted in tiles of keys, laid end to end over all requests, heads and blocks, and every CTA takes an equal stretch (or, where
 //   there are few blocks, one piece of one block).  Parts of a block that lies across stretches are joined by the last to come, in
 //   their order: the same call gives the same bits.
-// * s, m, the sums and o are 32-bit.  p meets v in two 16-bit parts that add up to it to 2^-14 (bf16) or 2^-20 (f16): with one, its rounding
+// * s, m, the sums and o are 32-bit; a tile's weights are added up by themselves, and what 128 tiles have added to o is put aside, since the tensor core
+//   cuts its sums off.  p meets v in two 16-bit parts that add up to it to 2^-14 (bf16) or 2^-20 (f16): with one, its rounding
 //   would be as large as the output's own.  The second part is a third of the products: of two tiles of rows and 128 keys the scores take 1 024
 //   clocks (64 a product of 128 x 128 x 16), the parts 1 024 each; the exponentials, beside them, 2 050.
 //
 // Bounds.  Long prompts: the products, three quarters of the 4 200 clocks that such a step takes (8 192 tokens, 32 heads of 128: 660 us, 830 TFLOP/s with p
 // counted once, 1 245 of products done); the rest is what one tile's softmax takes longer than the other tile's products.
-// Few tokens over a long context: the loads, at 4.7 TB/s (16 x 7 tokens over 8 000, 64 heads: 114 us), and with an 8-bit cache the instructions that turn
-// them (213 us).  Small calls: latency, 10 us.
+// Few tokens over a long context: the loads, at 4.6 TB/s (16 x 7 tokens over 8 000, 64 heads: 115 us), and with an 8-bit cache the instructions that turn
+// them (197 us; 8 192 tokens 904 to 985 us by the GPU).  Widths over 128, with one tile of rows, one group for the softmax and 64 keys a tile: products, 68 and
+// 59 % of their rate (4 096 tokens, 32 heads of 256: 370 us, 744 TFLOP/s with p counted once; of 192 321; over 8 bits 671 and 636).  Small calls: latency, 10 us.
 // With the shared memory that this kernel takes there is next to no L1 cache, so what lies in local memory (spilled registers, structs whose address is
 // taken) is at L2's distance: hence the registers' split by role, and values in place of references.
 #include <math.h>
@@ -67,11 +69,11 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrie
 __device__ __forceinline__ void bar_expect(uint32_t bar, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// as many bytes of bulk copies to come, and the arrival itself later
+// as many bytes of bulk copies to come, the arrival itself being still to come too
 __device__ __forceinline__ void bar_bytes(uint32_t bar, int bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// the same, the thread asleep for up to so many nanoseconds
+// whether the phase of this parity is over; the thread sleeps for up to so many nanoseconds
 __device__ __forceinline__ bool bar_sleep(uint32_t bar, uint32_t parity, uint32_t ns) {
     uint32_t done;
     asm volatile(
@@ -307,7 +309,8 @@ __device__ __forceinline__ int64_t warp_sum(int64_t x) {
     return x;
 }
 
-// Tiles of one of the heads of a lane's request (`rows` of them from position0 on), or, with `d`, its units.  Long requests are added up by the warp.
+// Tiles of one of the heads of a lane's request (`rows` of them from position0 on), with `cut` its pieces of so many tiles, `over` more for each block.
+// Long requests are added up by the warp.
 template <int KEYS>
 __device__ __forceinline__ int64_t add_blocks(const PrefillParams& p, int rows, int position0, int cut, int over) {
     // A lane adds up to two blocks itself, or where several requests have more, up to 24: the warp takes as long for a request as a lane for six

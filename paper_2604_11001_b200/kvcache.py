@@ -351,7 +351,8 @@ class PagedKV:
         ``starts[r + 1] - 1`` (``starts``: int32 [requests + 1]) of ``q`` [n, heads, head_dim] are the newest of the ``lengths`` (int32)
         tokens of request r, which the rows of ``table`` (int32 [requests, pages]) hold already.  Each sees the tokens up to its own, with
         ``window`` > 0 only the newest so many of these and the ``first`` oldest.  Returns [n, heads, head_dim], with ``return_lse``
-        also the float32 [n, heads] log-sum-exp; rows of no request are zeros."""
+        also the float32 [n, heads] log-sum-exp; rows of no request are zeros.  The cache's weights, by which ``evict`` ranks, do not
+        grow by it: only those tokens' shares count that ``attend`` adds."""
         if q.requires_grad and _grad_enabled():
             _refuse_gradient()
         dtype, shape, index = q.dtype, q.shape, self._index
@@ -384,7 +385,8 @@ class PagedKV:
         """Cut every request to its ``budget`` (int32 [requests]) of tokens per kv head: the ``recent`` newest, the
         ``first`` oldest and the largest weights, copied in order to the pages of ``new_table`` (none of which the
         call may read).  Returns the new lengths (int32 [requests]) and the old index of every kept token (int32
-        [requests, n_kv_heads, max_budget], -1 beyond)."""
+        [requests, n_kv_heads, max_budget], -1 beyond).  Weights are what ``attend`` has added: a prompt that ``prefill`` has loaded ranks
+        by the tokens that followed it."""
         n, index = lengths.numel(), self._index
         cols, new_cols = self._table(table, "table", n), self._table(new_table, "new_table", n)
         if lengths.dtype != _I32 or lengths.get_device() != index or not lengths.is_contiguous():
